@@ -434,6 +434,59 @@ int moe_encoder_pair_backward(const moe_config* cfg, const moe_encoder_dims* dim
                               const void* fwd_ws, size_t fwd_ws_bytes, void* dx,
                               const moe_encoder_grads* g, void* ws, size_t ws_bytes, void* stream);
 
+/*
+ * ---- The end of the model: loss over a vocabulary -----------------------------------
+ * The paper's models are trained on the cross entropy of the next word (Section 4), over vocabularies of
+ * 32k and 64k entries (Appendix, training details).  The entry points below take the last hidden states
+ * x [G,S,M] and one weight row per vocabulary entry, w [V,M] (an embedding table is one), and never keep the
+ * logits z[g,s,v] = sum_m x[g,s,m] w[v,m]:
+ *   moe_vocab_loss      loss = lse - z[target],  lse = log sum_v exp z[v]
+ *   moe_vocab_distill   a teacher's K entries per token, q = softmax(teacher_logit / T) over them:
+ *                       loss = sum_k q_k (log q_k - z[i_k] / T + lse),  lse = log sum_v exp(z[v] / T)
+ *                       (the student's softmax is over all V entries; a caller who wants T^2 puts it in dloss)
+ * A token has no target, and no part in any output but the zeros written for it, if its target is outside
+ * 0 .. V-1, or if none of its teacher's entries is there: one is not if its index is outside 0 .. V-1 or its
+ * logit is -inf.  Whatever x and dloss hold for such a token is not used.  Entries of one token may name the
+ * same index: each counts.
+ * Reductions over tokens are the caller's: loss is per token, and dloss its gradient.
+ */
+typedef struct {
+  int32_t V;           /* entries of the vocabulary, up to 2^23; tokens . V below 2^38, tokens below 2^24 */
+  int32_t K;           /* moe_vocab_distill: entries per token, 1 .. 256; else not read */
+  int32_t piece;       /* entries of the vocabulary worked on at a time where a piece of dz (fp32: of z) is kept,
+                          rounded to whole 256; 0: as many as make 1 GiB, 4096 at least */
+  float temperature;   /* moe_vocab_distill: T > 0; else not read */
+} moe_vocab_dims;
+
+/* Bytes of workspace of the forward and of the backward calls (either loss).  Pure host functions. */
+int moe_vocab_workspace_bytes(const moe_config* cfg, const moe_vocab_dims* dims, size_t* bytes);
+int moe_vocab_backward_workspace_bytes(const moe_config* cfg, const moe_vocab_dims* dims, size_t* bytes);
+
+/* in: x [G,S,M], w [V,M] act_dtype; target [G,S] i32.  out: loss, lse [G,S] fp32 (0 without a target).
+ * ws >= moe_vocab_workspace_bytes, 256-byte aligned.  Logits, maxima and sums are fp32. */
+int moe_vocab_loss(const moe_config* cfg, const moe_vocab_dims* dims, const void* x, const void* w,
+                   const int32_t* target, float* loss, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* in: x, w, target as given to moe_vocab_loss, loss and lse as it left them; dloss [G,S] fp32.
+ * out: dx [G,S,M], dw [V,M] act_dtype, of L = sum dloss loss; every element is written.  They must not overlap the inputs.
+ * ws >= moe_vocab_backward_workspace_bytes, 256-byte aligned.  bf16: the gradient of the logits is rounded to
+ * bf16 once, sums are fp32, in a fixed order: results are reproducible bit for bit. */
+int moe_vocab_loss_backward(const moe_config* cfg, const moe_vocab_dims* dims, const void* x, const void* w,
+                            const int32_t* target, const float* loss, const float* lse, const float* dloss,
+                            void* dx, void* dw, void* ws, size_t ws_bytes, void* stream);
+
+/* in: teacher_idx [G,S,K] i32, teacher_logit [G,S,K] fp32.  out: loss, lse [G,S] and the student's logits at the
+ * entries, entry_logit [G,S,K] fp32 (0 where no entry is there).  The rest as moe_vocab_loss. */
+int moe_vocab_distill(const moe_config* cfg, const moe_vocab_dims* dims, const void* x, const void* w,
+                      const int32_t* teacher_idx, const float* teacher_logit, float* loss, float* lse,
+                      float* entry_logit, void* ws, size_t ws_bytes, void* stream);
+
+/* entry_logit and lse as moe_vocab_distill left them; the rest as moe_vocab_loss_backward. */
+int moe_vocab_distill_backward(const moe_config* cfg, const moe_vocab_dims* dims, const void* x, const void* w,
+                               const int32_t* teacher_idx, const float* teacher_logit,
+                               const float* entry_logit, const float* lse, const float* dloss,
+                               void* dx, void* dw, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -29,7 +29,9 @@ EXPORTS = ("moe_status_string", "moe_prepare", "moe_gate_workspace_bytes", "moe_
            "moe_attention_workspace_bytes", "moe_encoder_workspace_bytes", "moe_self_attention",
            "moe_dense_ffn", "moe_encoder_pair_forward", "moe_encoder_train_workspace_bytes",
            "moe_encoder_backward_workspace_bytes", "moe_encoder_pair_forward_train",
-           "moe_encoder_pair_backward")
+           "moe_encoder_pair_backward",
+           "moe_vocab_workspace_bytes", "moe_vocab_backward_workspace_bytes", "moe_vocab_loss", "moe_vocab_loss_backward",
+           "moe_vocab_distill", "moe_vocab_distill_backward")
 FORWARD_EVENTS = 6
 BACKWARD_EVENTS = 8
 
@@ -53,6 +55,23 @@ class _EncoderWeights(ctypes.Structure):
                 ("wqkv", ctypes.c_void_p * 2), ("wo_att", ctypes.c_void_p * 2),
                 ("w1", ctypes.c_void_p), ("w2", ctypes.c_void_p), ("wg", ctypes.c_void_p),
                 ("wi", ctypes.c_void_p), ("wo", ctypes.c_void_p)]
+
+
+class _VocabDims(ctypes.Structure):
+    _fields_ = [("V", ctypes.c_int32), ("K", ctypes.c_int32), ("piece", ctypes.c_int32), ("temperature", ctypes.c_float)]
+
+
+@dataclass(frozen=True)
+class VocabDims:
+    """V vocabulary entries, K teacher entries per token and the temperature of a distillation, entries worked on at a
+    time (0: chosen by the library)."""
+    V: int
+    K: int = 0
+    temperature: float = 1.0
+    piece: int = 0
+
+    def _c(self):
+        return _VocabDims(self.V, self.K, self.piece, self.temperature)
 
 
 @dataclass(frozen=True)
@@ -140,6 +159,12 @@ def load_library() -> ctypes.CDLL:
         "moe_encoder_pair_backward": [cfgp, ctypes.POINTER(_EncoderDims), vp,
                                       ctypes.POINTER(_EncoderWeights), vp, vp, vp, sz, vp,
                                       ctypes.POINTER(_EncoderWeights), vp, sz, vp],
+        "moe_vocab_workspace_bytes": [cfgp, ctypes.POINTER(_VocabDims), ctypes.POINTER(sz)],
+        "moe_vocab_backward_workspace_bytes": [cfgp, ctypes.POINTER(_VocabDims), ctypes.POINTER(sz)],
+        "moe_vocab_loss": [cfgp, ctypes.POINTER(_VocabDims)] + [vp] * 6 + [sz, vp],
+        "moe_vocab_loss_backward": [cfgp, ctypes.POINTER(_VocabDims)] + [vp] * 9 + [sz, vp],
+        "moe_vocab_distill": [cfgp, ctypes.POINTER(_VocabDims)] + [vp] * 8 + [sz, vp],
+        "moe_vocab_distill_backward": [cfgp, ctypes.POINTER(_VocabDims)] + [vp] * 10 + [sz, vp],
         "moe_backward_workspace_bytes": [cfgp, ctypes.POINTER(sz)],
         "moe_backward": [cfgp] + [vp] * 7 + [sz] + [vp] * 5 + [sz, vp],
         "moe_backward_events": [cfgp] + [vp] * 7 + [sz] + [vp] * 5 + [sz, vp,
@@ -562,3 +587,85 @@ def moe_encoder_pair_backward(shape: MoEShape, dims: EncoderDims, x, weights: di
         _ptr(dy, dt, (G, S, M), "dy"), _ptr(daux, f32, (G,), "daux"), fwp, fwn,
         _ptr(dx, dt, (G, S, M), "dx"), ctypes.byref(g), wsp, wsn, _stream()),
         "moe_encoder_pair_backward")
+
+
+# ---- the end of the model: loss over a vocabulary
+def _on_current_device(**tensors):
+    """The kernels run on the current device: tensors of another one are refused."""
+    here = torch.cuda.current_device()
+    for name, t in tensors.items():
+        if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != here:
+            raise ValueError(f"{name}: on cuda:{t.device.index}, the current device is cuda:{here}")
+
+
+def moe_vocab_workspace_bytes(shape: MoEShape, dims: VocabDims) -> int:
+    return _ws_query("moe_vocab_workspace_bytes", shape, dims)
+
+
+def moe_vocab_backward_workspace_bytes(shape: MoEShape, dims: VocabDims) -> int:
+    return _ws_query("moe_vocab_backward_workspace_bytes", shape, dims)
+
+
+def _given(**tensors):
+    for name, t in tensors.items():
+        if t is None:
+            raise TypeError(f"{name}: expected a GPU tensor")
+    _on_current_device(**tensors)
+
+
+def moe_vocab_loss(shape: MoEShape, dims: VocabDims, x, w, target, loss, lse, ws):
+    """Softmax cross entropy of x [G,S,M] . w [V,M]^T against target [G,S] (outside 0 .. V-1: none); loss, lse [G,S]."""
+    _given(x=x, w=w, target=target, loss=loss, lse=lse, ws=ws)
+    G, S, M = shape.G, shape.S, shape.M
+    dt, f32 = shape.torch_dtype, torch.float32
+    c, d = shape._c(), dims._c()
+    wsp, wsn = _ws(ws)
+    _check(load_library().moe_vocab_loss(
+        ctypes.byref(c), ctypes.byref(d), _ptr(x, dt, (G, S, M), "x"), _ptr(w, dt, (dims.V, M), "w"),
+        _ptr(target, torch.int32, (G, S), "target"), _ptr(loss, f32, (G, S), "loss"), _ptr(lse, f32, (G, S), "lse"),
+        wsp, wsn, _stream()), "moe_vocab_loss")
+
+
+def moe_vocab_loss_backward(shape: MoEShape, dims: VocabDims, x, w, target, loss, lse, dloss, dx, dw, ws):
+    """Gradients dx [G,S,M], dw [V,M] of sum(dloss * loss); loss and lse as moe_vocab_loss left them."""
+    _given(x=x, w=w, target=target, loss=loss, lse=lse, dloss=dloss, dx=dx, dw=dw, ws=ws)
+    G, S, M = shape.G, shape.S, shape.M
+    dt, f32 = shape.torch_dtype, torch.float32
+    c, d = shape._c(), dims._c()
+    wsp, wsn = _ws(ws)
+    _check(load_library().moe_vocab_loss_backward(
+        ctypes.byref(c), ctypes.byref(d), _ptr(x, dt, (G, S, M), "x"), _ptr(w, dt, (dims.V, M), "w"),
+        _ptr(target, torch.int32, (G, S), "target"), _ptr(loss, f32, (G, S), "loss"), _ptr(lse, f32, (G, S), "lse"),
+        _ptr(dloss, f32, (G, S), "dloss"), _ptr(dx, dt, (G, S, M), "dx"), _ptr(dw, dt, (dims.V, M), "dw"),
+        wsp, wsn, _stream()), "moe_vocab_loss_backward")
+
+
+def moe_vocab_distill(shape: MoEShape, dims: VocabDims, x, w, teacher_idx, teacher_logit, loss, lse, entry_logit, ws):
+    """Loss against the softmax of a teacher's K logits per token (index outside 0 .. V-1 or logit -inf: no entry), and the
+    student's logits at them, entry_logit [G,S,K]."""
+    _given(x=x, w=w, teacher_idx=teacher_idx, teacher_logit=teacher_logit, loss=loss, lse=lse, entry_logit=entry_logit, ws=ws)
+    G, S, M, K = shape.G, shape.S, shape.M, dims.K
+    dt, f32 = shape.torch_dtype, torch.float32
+    c, d = shape._c(), dims._c()
+    wsp, wsn = _ws(ws)
+    _check(load_library().moe_vocab_distill(
+        ctypes.byref(c), ctypes.byref(d), _ptr(x, dt, (G, S, M), "x"), _ptr(w, dt, (dims.V, M), "w"),
+        _ptr(teacher_idx, torch.int32, (G, S, K), "teacher_idx"), _ptr(teacher_logit, f32, (G, S, K), "teacher_logit"),
+        _ptr(loss, f32, (G, S), "loss"), _ptr(lse, f32, (G, S), "lse"), _ptr(entry_logit, f32, (G, S, K), "entry_logit"),
+        wsp, wsn, _stream()), "moe_vocab_distill")
+
+
+def moe_vocab_distill_backward(shape: MoEShape, dims: VocabDims, x, w, teacher_idx, teacher_logit, entry_logit, lse, dloss,
+                               dx, dw, ws):
+    """Gradients dx, dw of sum(dloss * loss); entry_logit and lse as moe_vocab_distill left them."""
+    _given(x=x, w=w, teacher_idx=teacher_idx, teacher_logit=teacher_logit, entry_logit=entry_logit, lse=lse, dloss=dloss,
+           dx=dx, dw=dw, ws=ws)
+    G, S, M, K = shape.G, shape.S, shape.M, dims.K
+    dt, f32 = shape.torch_dtype, torch.float32
+    c, d = shape._c(), dims._c()
+    wsp, wsn = _ws(ws)
+    _check(load_library().moe_vocab_distill_backward(
+        ctypes.byref(c), ctypes.byref(d), _ptr(x, dt, (G, S, M), "x"), _ptr(w, dt, (dims.V, M), "w"),
+        _ptr(teacher_idx, torch.int32, (G, S, K), "teacher_idx"), _ptr(teacher_logit, f32, (G, S, K), "teacher_logit"),
+        _ptr(entry_logit, f32, (G, S, K), "entry_logit"), _ptr(lse, f32, (G, S), "lse"), _ptr(dloss, f32, (G, S), "dloss"),
+        _ptr(dx, dt, (G, S, M), "dx"), _ptr(dw, dt, (dims.V, M), "dw"), wsp, wsn, _stream()), "moe_vocab_distill_backward")

@@ -304,6 +304,47 @@ int attention_bwd_impl(const moe_config& c, const moe_encoder_dims& d, const voi
   return moe::launch_dense_grads(c, N, c.M, 3 * A, u, dqkv, wqkv, nullptr, du, dwqkv, wpart, st);
 }
 
+// ---- loss over a vocabulary
+int check_vocab(const moe_config* cfg, const moe_vocab_dims* d) {
+  const int rc = check_config(cfg);
+  if (rc != MOE_OK) return rc;
+  if (d == nullptr || d->V < 1 || d->piece < 0) return MOE_EINVAL;
+  if (d->V > (1 << 23) || cfg->M > (1 << 20)) return MOE_EUNSUPPORTED;
+  // a launch has less than 2^32 threads: 256 per row, 256 per 128 x 128 tile of the logits, one per 16 bytes of x
+  const long long N = (long long)cfg->G * cfg->S;
+  if (N >= 1 << 24 || ((N + 127) / 128) * ((d->V + 127) / 128) >= 1 << 24 || N * (cfg->M / 4) >= (1LL << 32) - 256)
+    return MOE_EUNSUPPORTED;
+  return MOE_OK;
+}
+int check_teacher(const moe_vocab_dims* d) {
+  if (d->K < 1 || !(d->temperature > 0.f) || !(1.f / d->temperature > 0.f) || 1.f / d->temperature > 3e38f) return MOE_EINVAL;
+  return d->K <= 256 ? MOE_OK : MOE_EUNSUPPORTED;
+}
+int vocab_call(const moe_config* cfg, const moe_vocab_dims* d, const moe::VocabCall& a, void* ws, size_t ws_bytes, void* stream,
+               bool backward) {
+  int rc = check_vocab(cfg, d);
+  if (rc != MOE_OK) return rc;
+  const bool teacher = a.target == nullptr;
+  if (teacher && (rc = check_teacher(d)) != MOE_OK) return rc;
+  const void* req[] = {a.x, a.w, teacher ? static_cast<const void*>(a.idx) : a.target, teacher ? static_cast<const void*>(a.logit) : a.x,
+                       a.lse, teacher ? a.entry_logit : a.loss, a.loss != nullptr ? a.loss : a.lse, ws,
+                       backward ? a.dloss : a.lse, backward ? a.dx : ws, backward ? a.dw : ws};
+  for (const void* p : req)
+    if (p == nullptr || !aligned16(p)) return MOE_EINVAL;
+  if (!backward && a.loss == nullptr) return MOE_EINVAL;
+  if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return MOE_EINVAL;
+  if (ws_bytes < moe::carve_vocab(*cfg, *d, teacher, backward).total) return MOE_EWORKSPACE;
+  return backward ? moe::launch_vocab_backward(*cfg, *d, a, ws, static_cast<hipStream_t>(stream))
+                  : moe::launch_vocab_forward(*cfg, *d, a, ws, static_cast<hipStream_t>(stream));
+}
+int vocab_bytes(const moe_config* cfg, const moe_vocab_dims* d, bool backward, size_t* bytes) {
+  const int rc = check_vocab(cfg, d);
+  if (rc != MOE_OK) return rc;
+  if (bytes == nullptr) return MOE_EINVAL;
+  *bytes = moe::carve_vocab(*cfg, *d, true, backward).total;      // (a teacher's entries take 12 bytes a token more)
+  return MOE_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -861,6 +902,53 @@ int moe_encoder_pair_backward(const moe_config* cfg, const moe_encoder_dims* dim
   if (rc != MOE_OK) return rc;
   return moe::launch_layer_norm_bwd(dt, x, dn, w->ln_gamma[0], g0, dx, partial, g->ln_gamma[0],
                                     g->ln_beta[0], N, cfg->M, st);
+}
+
+int moe_vocab_workspace_bytes(const moe_config* cfg, const moe_vocab_dims* dims, size_t* bytes) {
+  return vocab_bytes(cfg, dims, false, bytes);
+}
+
+int moe_vocab_backward_workspace_bytes(const moe_config* cfg, const moe_vocab_dims* dims, size_t* bytes) {
+  return vocab_bytes(cfg, dims, true, bytes);
+}
+
+int moe_vocab_loss(const moe_config* cfg, const moe_vocab_dims* dims, const void* x, const void* w, const int32_t* target,
+                   float* loss, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  if (target == nullptr) return MOE_EINVAL;
+  moe::VocabCall a{x, w, target};
+  a.loss = loss;
+  a.lse = lse;
+  return vocab_call(cfg, dims, a, ws, ws_bytes, stream, false);
+}
+
+int moe_vocab_loss_backward(const moe_config* cfg, const moe_vocab_dims* dims, const void* x, const void* w,
+                            const int32_t* target, const float* loss, const float* lse, const float* dloss, void* dx, void* dw,
+                            void* ws, size_t ws_bytes, void* stream) {
+  if (target == nullptr) return MOE_EINVAL;
+  moe::VocabCall a{x, w, target};
+  a.loss = const_cast<float*>(loss);
+  a.lse = const_cast<float*>(lse);
+  a.dloss = dloss;
+  a.dx = dx;
+  a.dw = dw;
+  return vocab_call(cfg, dims, a, ws, ws_bytes, stream, true);
+}
+
+int moe_vocab_distill(const moe_config* cfg, const moe_vocab_dims* dims, const void* x, const void* w, const int32_t* teacher_idx,
+                      const float* teacher_logit, float* loss, float* lse, float* entry_logit, void* ws, size_t ws_bytes,
+                      void* stream) {
+  moe::VocabCall a{x, w, nullptr, teacher_idx, teacher_logit, loss, lse, entry_logit};
+  return vocab_call(cfg, dims, a, ws, ws_bytes, stream, false);
+}
+
+int moe_vocab_distill_backward(const moe_config* cfg, const moe_vocab_dims* dims, const void* x, const void* w,
+                               const int32_t* teacher_idx, const float* teacher_logit, const float* entry_logit,
+                               const float* lse, const float* dloss, void* dx, void* dw, void* ws, size_t ws_bytes, void* stream) {
+  moe::VocabCall a{x, w, nullptr, teacher_idx, teacher_logit, nullptr, const_cast<float*>(lse), const_cast<float*>(entry_logit)};
+  a.dloss = dloss;
+  a.dx = dx;
+  a.dw = dw;
+  return vocab_call(cfg, dims, a, ws, ws_bytes, stream, true);
 }
 
 }  // extern "C"

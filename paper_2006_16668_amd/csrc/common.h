@@ -151,6 +151,16 @@ inline RowPacking carve_row_packing(const moe_config& c, void* base) {
 //   kept:    NULL, or the occupied rows of each expert (packed layout)
 //   row_pad: 255: zero rows follow the occupied ones in C up to the next multiple of 256 (bf16)
 //   scatter: NULL, or row p of expert e of C goes to the absolute row scatter[e R + p] (bf16)
+//   lda, ldc: row pitches of A and C in the products that take them (the vocabulary's), 0: dense
+// What the epilogues of a vocabulary's logits read and write, per packed row (vocab_loss.hip).
+struct VocabRows {
+  float scale = 0.f;                   // log2(e) / temperature
+  float2* stats = nullptr;             // [slots, rows]: maximum m of scale z over a slot's entries, sum of 2^(scale z - m)
+  const float *lse2 = nullptr, *grad = nullptr;                // log2 of the sum over all entries; upstream / temperature
+  const int32_t* hit = nullptr;        // NULL, or the entry whose gradient is hit_value instead
+  const float* hit_value = nullptr;
+  int first = 0;                       // entry of the product's first column
+};
 struct GemmArgs {
   const void *A, *B;
   void* C;
@@ -158,6 +168,9 @@ struct GemmArgs {
   const int32_t *gather = nullptr, *kept = nullptr;
   int row_pad = 0;
   const int32_t* scatter = nullptr;
+  int lda = 0, ldc = 0;
+  int k_total = 0, add = 0;            // of the sums over ranges of a vocabulary: their whole length, add to C
+  VocabRows vocab = {};
 };
 
 // host-side launchers (each returns a moe_status)
@@ -268,6 +281,38 @@ int launch_gemm_bf16_f32out(bool transposed_a, const void* A, const void* B, flo
 enum GemmKind { kForward, kForwardRelu, kDataGrad, kDataGradMask, kWeightGrad };
 int launch_gemm_f32(GemmKind kind, const GemmArgs& a, int E, int R, int N, int K, hipStream_t st);
 
+// A vocabulary's products (fp32: launch_gemm_f32 with pitches) in bf16 (expert_gemm.hip): rows = the tokens, of which a.kept[0] count, entries = those of a piece
+//   z = a.A[a.gather] . a.B^T: a.vocab.stats, or the gradient in a.C (rows of a.ldc)
+int vocab_stat_slots(int rows, int entries, int M);
+int launch_vocab_logits(const GemmArgs& a, int rows, int entries, int M, hipStream_t st);
+//   dx: C [splits, rows, M] fp32 = (or +=) sums over the plan's ranges of A [rows, lda] . B [entries, M]
+struct DenseWgradPlan { int splits, k; };      // ranges, length of each (the last may be shorter)
+DenseWgradPlan vocab_dx_plan(int rows, int entries, int M);
+DenseWgradPlan vocab_dx_plan_f32(int rows, int entries, int M);        // gemm_f32.hip
+int launch_vocab_dx(const GemmArgs& a, const DenseWgradPlan& p, int rows, int M, hipStream_t st);
+//   dw: C [entries, M] = A [rows, lda]^T . B [rows, M]
+int launch_vocab_dw(const GemmArgs& a, int rows, int entries, int M, hipStream_t st);
+
+// The loss over a vocabulary (vocab_loss.hip)
+struct VocabPieces { int entries, count; };    // of the vocabulary; a piece's entries are whole 256, the last may have fewer
+VocabPieces vocab_pieces(const moe_config& c, const moe_vocab_dims& d);
+struct VocabWs {
+  size_t kept, perm, tstat, has, stats, pos, lse2, grad, hit, hit_value, packed, dz, sums, total;
+  int slots;                           // of stats
+  DenseWgradPlan dx_plan;              // of a whole piece
+};
+VocabWs carve_vocab(const moe_config& c, const moe_vocab_dims& d, bool teacher, bool backward);
+struct VocabCall {                     // target: cross entropy, else the teacher's entries
+  const void *x, *w;
+  const int32_t *target, *idx;
+  const float* logit;
+  float *loss, *lse, *entry_logit;     // outputs of the forward, inputs of the backward pass
+  const float* dloss;
+  void *dx, *dw;
+};
+int launch_vocab_forward(const moe_config& c, const moe_vocab_dims& d, const VocabCall& a, void* ws, hipStream_t st);
+int launch_vocab_backward(const moe_config& c, const moe_vocab_dims& d, const VocabCall& a, void* ws, hipStream_t st);
+
 // Transformer encoder sub-layers around the MoE layer (encoder.hip)
 int launch_add_layer_norm(int act_dtype, const void* x, const void* delta, const float* gamma,
                           const float* beta, void* sum_out, void* norm_out, long long rows, int M,
@@ -288,7 +333,6 @@ int launch_layer_norm_bwd(int act_dtype, const void* s, const void* dn, const fl
 //   dqkv [B*L, 3*heads*d] from qkv, ctx, dctx [B*L, heads*d] and lse; dvec: [B*heads*L] scratch
 // dW [in,out] = X^T dY over rows tokens (X [rows,in], dY [rows,out]); partial: scratch of
 // dense_wgrad_partial_bytes() for the token ranges of the split (may be NULL: no split)
-struct DenseWgradPlan { int splits, k; };      // ranges, tokens of each (the last may be shorter)
 DenseWgradPlan dense_wgrad_plan(long long rows, int in, int out);     // expert_gemm.hip
 int launch_dense_wgrad_ranges(const DenseWgradPlan& p, long long rows, int in, int out, const void* X, const void* dY,
                               float* partial, hipStream_t st);

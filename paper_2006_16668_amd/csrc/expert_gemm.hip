@@ -625,10 +625,18 @@ struct EdgeArgs {
   int row_pad;
   const int32_t* scatter;
   int k_total;
+  int lda, ldc, add;                     // row pitches of A and C, C is added to: where kEpi... below says so
+  VocabRows vocab;
 };
 // EPI of the products of a pair: decided by their arguments
 constexpr int kEpiMaskIfAny = 6;       // 2 with a mask, else 0
 constexpr int kEpiRangesIfAny = 7;     // 3 with a k_total, else 0; kept is K_KEPT's
+// The products of a vocabulary's loss (vocab_loss.hip); E is 1 and kept[0] the rows with a target.
+//   z = x . w^T: no C, the maximum and the sum of exponentials of each row's columns of a wavefront tile (kEpiStats), or
+//     C = the gradient with respect to z, bf16 in rows of ldc, zeros in the columns N .. of the last 16 bytes (kEpiLogitGrad)
+//   dx = dz . w: A in rows of lda, "expert" e sums the k from e K on, up to k_total; C[e] fp32, or is added to
+//   dw = dz^T . x: A in rows of lda, a plain bf16 result
+constexpr int kEpiStats = 8, kEpiLogitGrad = 9, kEpiSums = 10, kEpiPitch = 11;
 
 template <int BM, int BN, int BK, int ST, int EPI, bool A_MNC, bool B_KC, bool K_KEPT>
 __device__ __forceinline__ void edge_tile(const EdgeArgs& arg, const int logical) {
@@ -637,6 +645,8 @@ __device__ __forceinline__ void edge_tile(const EdgeArgs& arg, const int logical
   const int R = arg.R, N = arg.N, K = arg.K, tiles_m = arg.tiles_m, tiles_n = arg.tiles_n, row_pad = arg.row_pad;
   const int32_t *const __restrict__ gather = arg.gather, *const __restrict__ kept = arg.kept, *const __restrict__ scatter = arg.scatter;
   const int k_total = arg.k_total;
+  constexpr bool LOGITS = EPI == kEpiStats || EPI == kEpiLogitGrad, SUMS = EPI == kEpiSums;
+  const int lda = SUMS || EPI == kEpiPitch ? arg.lda : A_MNC ? R : K;
   const bool masked = EPI == 2 || (EPI == kEpiMaskIfAny && mask != nullptr);
   const bool ranges = EPI == 3 || (EPI == kEpiRangesIfAny && k_total != 0);
   const bool k_kept = K_KEPT || (EPI == kEpiRangesIfAny && kept != nullptr);
@@ -666,14 +676,15 @@ __device__ __forceinline__ void edge_tile(const EdgeArgs& arg, const int logical
   const int ct = rem / brows, rt = band * kBand + (rem - ct * brows);
   const int m0 = rt * BM, n0 = ct * BN;
   int rows = R, rows_out = R;                                  // rows of A that count, of C that are stored
-  if (kept != nullptr && !k_kept) {
+  if (LOGITS || SUMS) rows = rows_out = kept[0];
+  else if (kept != nullptr && !k_kept) {
     rows = kept[e];
     rows_out = (rows + row_pad) & ~row_pad;
     rows_out = rows_out < R ? rows_out : R;
   }
   if (m0 >= rows_out) return;                                  // block-uniform
   int KE = k_kept ? kept[e] : K;                               // length of the sum
-  if (ranges) KE = k_total - e * K < K ? k_total - e * K : K;
+  if (ranges || SUMS) KE = k_total - e * K < K ? k_total - e * K : K;
   const int KT = (KE + BK - 1) / BK;
 
   // Per-lane source addresses of the copies and their advance per K step (0 for a lane that reads
@@ -690,20 +701,20 @@ __device__ __forceinline__ void edge_tile(const EdgeArgs& arg, const int logical
     if (A_MNC) {                                               // 512 / BM k rows of BM / 8 chunks per copy
       const int kr = ARPC * c + lane / ACH, col = m0 + 8 * ((lane % ACH) ^ edge_swizzle<BM>(kr));
       ok = col < R && kr < KE;
-      src = A + ((size_t)e * K + kr) * R + col;
+      src = A + ((size_t)e * K + kr) * lda + col;
     } else {
       const int row = KRPC * c + lane / KCH, ch = (lane % KCH) ^ kc_swizzle(row);
       ok = m0 + row < rows && 8 * ch < KE;
-      long long arow = (long long)e * R + m0 + row;
+      long long arow = (SUMS ? 0 : (long long)e * R) + m0 + row;
       if (gather != nullptr) {
         const int tok = ok ? gather[arow] : -1;
         ok = tok >= 0;
         arow = tok;
       }
-      src = A + arow * K + 8 * ch;
+      src = A + arow * lda + (SUMS ? (size_t)e * K : 0) + 8 * ch;
     }
     a_addr[q] = ok ? (uint64_t)(uintptr_t)src : zline;
-    a_inc[q] = ok ? (A_MNC ? (uint32_t)R * BK * 2 : BK * 2) : 0u;
+    a_inc[q] = ok ? (A_MNC ? (uint32_t)lda * BK * 2 : BK * 2) : 0u;
   }
 #pragma unroll
   for (int q = 0; q < BC; ++q) {
@@ -895,6 +906,75 @@ __device__ __forceinline__ void edge_tile(const EdgeArgs& arg, const int logical
     __builtin_amdgcn_sched_barrier(0);
     multiply();
   }
+  // log2(e) / temperature times a logit is the argument of a power of two.  Of a row the lanes l and l + 32 hold the columns.
+  if constexpr (EPI == kEpiStats) {
+    const float c = arg.vocab.scale;
+    const int left = N - n0 - wn0;                             // columns of the wavefront tile that exist
+    if (left < WN) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int col = 32 * j + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
+#pragma unroll
+          for (int i = 0; i < TM; ++i) acc[i][j][r] = col < left ? acc[i][j][r] : -INFINITY;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, acc[i][j][r]);
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * c;
+      const float m = fabsf(mx) == INFINITY ? 0.f : mx;        // (no column left or all -inf: a sum of 0; an infinite logit: inf)
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], c, -m));
+      sum += __shfl_xor(sum, 32, 64);
+      const int row = m0 + wm0 + 32 * i + (lane & 31);
+      if (lane < 32 && row < rows) arg.vocab.stats[(size_t)(2 * ct + (wave & 1)) * R + row] = float2{mx == INFINITY ? 0.f : mx, sum};
+    }
+    return;
+  }
+  if constexpr (EPI == kEpiLogitGrad) {
+    const float c = arg.vocab.scale;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const int row = m0 + wm0 + 32 * i + (lane & 31), at = row < rows ? row : rows - 1;
+      const float lse = arg.vocab.lse2[at], up = arg.vocab.grad[at];
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          acc[i][j][r] = n0 + wn0 + 32 * j + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3) < N
+                             ? __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], c, -lse)) * up : 0.f;
+    }
+  }
+  if constexpr (SUMS) {
+    typedef float f32x4_t __attribute__((ext_vector_type(4)));
+    float* const Cf = reinterpret_cast<float*>(Cout) + (size_t)e * R * N;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const int row = m0 + wm0 + 32 * i + (lane & 31);
+      if (row >= rows) continue;
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int col = n0 + wn0 + 32 * j + 8 * q + 4 * (lane >> 5);
+          if (col >= N) continue;
+          f32x4_t* const at = reinterpret_cast<f32x4_t*>(Cf + (size_t)row * N + col);
+          f32x4_t v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+          if (arg.add != 0) v += *at;
+          *at = v;
+        }
+    }
+    return;
+  }
   if (RANGES && ranges) {                                      // a lane owns four consecutive columns of a row
     typedef float f32x4_t __attribute__((ext_vector_type(4)));
     float* const Cf = reinterpret_cast<float*>(Cout) + (size_t)e * R * N;
@@ -935,6 +1015,15 @@ __device__ __forceinline__ void edge_tile(const EdgeArgs& arg, const int logical
         if (EPI == 1) { lo = relu_bf16x2(lo); hi = relu_bf16x2(hi); }
         *(lds_u2_ptr)(uintptr_t)(st_wr + (((4 * j + q) ^ (r32 & (CH - 1))) * 16)) = u32x2_t{lo, hi};
       }
+    if (EPI == kEpiLogitGrad && arg.vocab.hit != nullptr && hh == 0) {       // the target's column, in its place
+      const int row = m0 + wm0 + 32 * i + r32;
+      const int t = row < rows ? arg.vocab.hit[row] - (arg.vocab.first + n0 + wn0) : -1;
+      if (t >= 0 && t < WN) {
+        typedef bf16_t __attribute__((address_space(3))) * lds_bf16_ptr;
+        *(lds_bf16_ptr)(uintptr_t)(st_base + r32 * (WN * 2) + (((t >> 3) ^ (r32 & (CH - 1))) * 16) +
+                                   8 * (((t >> 2) & 1) ^ ((r32 / CH) & 1)) + 2 * (t & 3)) = f32_to_bf16(arg.vocab.hit_value[row]);
+      }
+    }
 #pragma unroll
     for (int ps = 0; ps < 32 / RPP; ++ps) {
       const int rr = RPP * ps + lane / CH, c = lane % CH;
@@ -942,7 +1031,7 @@ __device__ __forceinline__ void edge_tile(const EdgeArgs& arg, const int logical
       if ((rr / CH) & 1) d = u32x4_t{d[2], d[3], d[0], d[1]};
       const int row = m0 + wm0 + 32 * i + rr, col = n0 + wn0 + 8 * c;
       if (row < rows_out && col < N) {
-        const size_t o = ((size_t)e * R + row) * N + col;
+        const size_t o = ((size_t)e * R + row) * (EPI == kEpiLogitGrad ? arg.ldc : N) + col;
         if (MASKS && masked) {
 #pragma unroll
           for (int w = 0; w < 4; ++w)          // a bf16 is positive iff its bits, as an integer, are
@@ -962,7 +1051,15 @@ __device__ __forceinline__ void edge_tile(const EdgeArgs& arg, const int logical
 template <int BM, int BN> constexpr int kEdgeBlocks = BN == 256 ? 2 : BM == 128 ? 3 : 4;      // per compute unit
 template <int BM, int BN, int BK, int ST, int EPI, bool A_MNC, bool B_KC, bool K_KEPT>
 __global__ __launch_bounds__(256, (kEdgeBlocks<BM, BN>)) void expert_gemm_bf16_edge_kernel(EdgeArgs arg) {
-  edge_tile<BM, BN, BK, ST, EPI, A_MNC, B_KC, K_KEPT>(arg, xcd_remap(blockIdx.x, arg.nblk));
+  if constexpr (EPI == kEpiStats || EPI == kEpiLogitGrad || EPI == kEpiSums) {
+    // the row tiles that hold a target, in the order of their XCDs: their number is known here only
+    const int tiles_m = (arg.kept[0] + BM - 1) / BM, n = arg.nblk / arg.tiles_m * tiles_m;
+    if ((int)blockIdx.x >= n) return;
+    arg.tiles_m = tiles_m;
+    edge_tile<BM, BN, BK, ST, EPI, A_MNC, B_KC, K_KEPT>(arg, xcd_remap(blockIdx.x, n));
+  } else {
+    edge_tile<BM, BN, BK, ST, EPI, A_MNC, B_KC, K_KEPT>(arg, xcd_remap(blockIdx.x, arg.nblk));
+  }
 }
 
 // The data gradient and the weight gradient of one linear layer in one launch: both read the layer's upstream gradient,
@@ -1195,7 +1292,7 @@ inline bool edge_args(EdgeArgs* out, int BM, int BN, const GemmArgs& a, int E, i
   if (nblk > 0x7fffffffLL) return false;
   *out = EdgeArgs{static_cast<const bf16_t*>(a.A), static_cast<const bf16_t*>(a.B), static_cast<bf16_t*>(a.C),
                   static_cast<const bf16_t*>(a.mask), R, N, K, tiles_m, tiles_n, (int)nblk, a.gather, a.kept, a.row_pad,
-                  a.scatter, k_total};
+                  a.scatter, k_total, a.lda, a.ldc, a.add, a.vocab};
   return true;
 }
 template <int BM, int BN, int BK, int ST, int EPI, bool A_MNC, bool B_KC, bool K_KEPT>
@@ -1222,13 +1319,13 @@ int gemm_bf16_edge(GemmForm form, const GemmArgs& a, int E, int R, int N, int K,
     }
   } else {
     switch (form) {
-      case kEdge64x64: return launch_edge<64, 64, 64, 3, EPI, A_MNC, B_KC, K_KEPT>(a, E, R, N, K, st);
-      case kEdge64x64Deep: return launch_edge<64, 64, 64, 4, EPI, A_MNC, B_KC, K_KEPT>(a, E, R, N, K, st);
-      case kEdge64x128: return launch_edge<64, 128, 64, 2, EPI, A_MNC, B_KC, K_KEPT>(a, E, R, N, K, st);
-      case kEdge64x128Deep: return launch_edge<64, 128, 64, 3, EPI, A_MNC, B_KC, K_KEPT>(a, E, R, N, K, st);
-      case kEdge128x128: return launch_edge<128, 128, 64, 2, EPI, A_MNC, B_KC, K_KEPT>(a, E, R, N, K, st);
-      case kEdge128x128Deep: return launch_edge<128, 128, 64, 3, EPI, A_MNC, B_KC, K_KEPT>(a, E, R, N, K, st);
-      default: return launch_edge<128, 256, 32, 3, EPI, A_MNC, B_KC, K_KEPT>(a, E, R, N, K, st);
+      case kEdge64x64: return launch_edge<64, 64, 64, 3, EPI, A_MNC, B_KC, K_KEPT>(a, E, R, N, K, st, k_total);
+      case kEdge64x64Deep: return launch_edge<64, 64, 64, 4, EPI, A_MNC, B_KC, K_KEPT>(a, E, R, N, K, st, k_total);
+      case kEdge64x128: return launch_edge<64, 128, 64, 2, EPI, A_MNC, B_KC, K_KEPT>(a, E, R, N, K, st, k_total);
+      case kEdge64x128Deep: return launch_edge<64, 128, 64, 3, EPI, A_MNC, B_KC, K_KEPT>(a, E, R, N, K, st, k_total);
+      case kEdge128x128: return launch_edge<128, 128, 64, 2, EPI, A_MNC, B_KC, K_KEPT>(a, E, R, N, K, st, k_total);
+      case kEdge128x128Deep: return launch_edge<128, 128, 64, 3, EPI, A_MNC, B_KC, K_KEPT>(a, E, R, N, K, st, k_total);
+      default: return launch_edge<128, 256, 32, 3, EPI, A_MNC, B_KC, K_KEPT>(a, E, R, N, K, st, k_total);
     }
   }
 }
@@ -1378,6 +1475,9 @@ int prepare_expert_gemm() {
       MOE_EDGE_KC(1, false, false, false), MOE_EDGE_KC(0, false, false, false), MOE_EDGE_KC(0, false, true, false),
       MOE_EDGE_KC(2, false, true, false), MOE_EDGE_MNC(0, true, false, false), MOE_EDGE_MNC(0, true, false, true),
       MOE_EDGE_MNC(3, true, false, false),
+      // vocabulary
+      MOE_EDGE_KC(kEpiStats, false, true, false), MOE_EDGE_KC(kEpiLogitGrad, false, true, false),
+      MOE_EDGE_KC(kEpiSums, false, false, false), MOE_EDGE_MNC(kEpiPitch, true, false, true),
 #define MOE_PAIR(BM, BN, DEEP, FLAT) \
   prepare_pair<BM, BN, DEEP, 64, 64, 5>(), prepare_pair<BM, BN, DEEP, 64, 128, 4>(), prepare_pair<BM, BN, FLAT, 128, 128, 3>()
       MOE_PAIR(64, 64, 4, 3), MOE_PAIR(64, 128, 2, 2), MOE_PAIR(128, 128, 2, 2)};
@@ -1533,6 +1633,42 @@ int launch_dense_wgrad_ranges(const DenseWgradPlan& p, long long rows, int in, i
   const GemmForm form = gemm_form(persistent, p.splits, in, out, p.k, kLayoutWeightGrad, kPlanUnits);
   if (form == kPersistent) return launch_gemm_bf16_f32out(true, X, dY, partial, p.splits, in, out, p.k, st);
   return gemm_bf16_edge<3, true, false>(form, GemmArgs{X, dY, partial}, p.splits, in, out, p.k, st, (int)rows);
+}
+
+// ---- the products of a vocabulary's loss; bf16, forms by the rule of a whole device (they size a workspace)
+static GemmForm vocab_logits_form(int rows, int entries, int M) {
+  return gemm_form(false, 1, rows, entries, M, kLayoutDataGrad, kPlanUnits);
+}
+int vocab_stat_slots(int rows, int entries, int M) {
+  const int bn = form_costs(kLayoutDataGrad)[vocab_logits_form(rows, entries, M)].bn;
+  return 2 * ((entries + bn - 1) / bn);
+}
+int launch_vocab_logits(const GemmArgs& a, int rows, int entries, int M, hipStream_t st) {
+  const GemmForm form = vocab_logits_form(rows, entries, M);
+  return a.vocab.stats != nullptr ? gemm_bf16_edge<kEpiStats, false, true>(form, a, 1, rows, entries, M, st)
+                                  : gemm_bf16_edge<kEpiLogitGrad, false, true>(form, a, 1, rows, entries, M, st);
+}
+// Ranges of the vocabulary's entries that dx is summed over side by side: few rows make few tiles of a long sum.
+DenseWgradPlan vocab_dx_plan(int rows, int entries, int M) {
+  DenseWgradPlan best{1, (entries + 63) / 64 * 64};
+  double best_us = 0;
+  for (int want = 1; want <= 64; want += want < 4 ? 1 : want < 8 ? 2 : want / 4) {
+    const int k = ((entries + want - 1) / want + 63) / 64 * 64, sp = (entries + k - 1) / k;
+    if (want > 1 && (k < 256 || sp < want)) continue;
+    double us = 0;
+    gemm_form(false, sp, rows, M, sp == 1 ? entries : k, kLayoutForward, kPlanUnits, &us);
+    us += 1e-6 * 8 * sp * rows * M / 5.0;                      // written and read once more, us at 5 TB/s
+    if (want == 1 || us < best_us) { best_us = us; best = DenseWgradPlan{sp, k}; }
+  }
+  return best;
+}
+int launch_vocab_dx(const GemmArgs& a, const DenseWgradPlan& p, int rows, int M, hipStream_t st) {
+  const GemmForm form = gemm_form(false, p.splits, rows, M, p.k, kLayoutForward, kPlanUnits);
+  return gemm_bf16_edge<kEpiSums, false, false>(form, a, p.splits, rows, M, p.k, st, a.k_total);
+}
+int launch_vocab_dw(const GemmArgs& a, int rows, int entries, int M, hipStream_t st) {
+  const GemmForm form = gemm_form(false, 1, entries, M, rows, kLayoutWeightGrad, kPlanUnits);
+  return gemm_bf16_edge<kEpiPitch, true, false, true>(form, a, 1, entries, M, rows, st);
 }
 
 int launch_expert_gemm2(const moe_config& c, const void* h, const void* wo, void* out,

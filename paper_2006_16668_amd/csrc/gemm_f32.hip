@@ -79,12 +79,18 @@ struct F32Smem {
 // TM x TN tiles of 32 x 32 per wavefront, PD steps of 16 k on their way in registers; KG groups of four
 // wavefronts share a tile, group g taking steps g, g + KG, ...  The other parameters are those of GemmArgs
 // and of the bf16 kernel: EPI 0 plain, 1 relu, 2 zero where mask[e,r,n] <= 0; gathered rows of A, kept rows
-// of an expert (or, K_KEPT, the length of its sum).
-template <int TM, int TN, int PD, int KG, int EPI, bool A_KC, bool B_KC, bool K_KEPT>
+// of an expert (or, K_KEPT, the length of its sum).  PITCH: rows of A and C lie lda and ldc elements apart, where the dense
+// matrix has as many columns (a piece of a vocabulary, whose number of entries is any), and kept[0] rows of A and C count, or
+// terms of the sum with row-of-k operands.  Then "expert" e of A [R,lda] . B [k_total,N] sums the k from e K on, `add`: to
+// what C [e,R,N] holds.
+template <int TM, int TN, int PD, int KG, int EPI, bool A_KC, bool B_KC, bool K_KEPT, bool PITCH>
 __global__ __launch_bounds__(256 * KG, TM * TN >= 4 ? 2 : TM * TN >= 2 ? 3 : 4) void gemm_f32_mfma_kernel(
     const float* __restrict__ A, const float* __restrict__ B, float* __restrict__ Cout,
     const float* __restrict__ mask, int R, int N, int K, int tiles_r, int tiles_n,
-    const int32_t* __restrict__ gather, const int32_t* __restrict__ kept) {
+    const int32_t* __restrict__ gather, const int32_t* __restrict__ kept, int lda_arg, int ldc_arg, int k_total,
+    int add) {
+  const int lda = PITCH ? lda_arg : A_KC ? K : R, ldc = PITCH ? ldc_arg : N;
+  constexpr bool SUMS = PITCH && A_KC && !B_KC;
   using PA = F32Plane<TM, A_KC>;
   using PB = F32Plane<TN, B_KC>;
   static_assert(PD % 2 == 0, "a buffer per parity of the step");
@@ -100,7 +106,14 @@ __global__ __launch_bounds__(256 * KG, TM * TN >= 4 ? 2 : TM * TN >= 2 ? 3 : 4) 
   // contiguous range of tiles, in bands of 8 row tiles with the row tile fastest, so that the tiles
   // that share panels run next to each other under one L2.
   unsigned blk = blockIdx.x;
-  const unsigned per_xcd = gridDim.x / 8;
+  unsigned nblk = gridDim.x;
+  if (PITCH && !K_KEPT) {                                      // row tiles that count, which the host does not know
+    const int tiles = (kept[0] + BM - 1) / BM;
+    nblk = nblk / tiles_r * tiles;
+    tiles_r = tiles;
+    if (blk >= nblk) return;
+  }
+  const unsigned per_xcd = nblk / 8;
   if (blk < per_xcd * 8) blk = (blk % 8) * per_xcd + blk / 8;
   const int per_e = tiles_r * tiles_n;
   const int e = (int)(blk / per_e), t = (int)(blk - (unsigned)e * per_e);
@@ -108,9 +121,9 @@ __global__ __launch_bounds__(256 * KG, TM * TN >= 4 ? 2 : TM * TN >= 2 ? 3 : 4) 
   const int left = tiles_r - 8 * band, brows = left < 8 ? left : 8;
   const int ct = rem / brows, rt = 8 * band + (rem - ct * brows);
   const int r0 = rt * BM, n0 = ct * BN;
-  const int rows = kept != nullptr && !K_KEPT ? kept[e] : R;
+  const int rows = kept != nullptr && !K_KEPT ? kept[PITCH ? 0 : e] : R;
   if (r0 >= rows) return;                                      // block-uniform
-  const int KE = K_KEPT ? kept[e] : K;
+  const int KE = K_KEPT ? kept[e] : SUMS && k_total - e * K < K ? k_total - e * K : K;
   const int KT = (KE + KG * kBK - 1) / (KG * kBK);             // steps of a group
   const int wm0 = (wave >> 1) * 32 * TM, wn0 = (wave & 1) * 32 * TN;
   const int l32 = lane & 31, hf = lane >> 5;
@@ -131,19 +144,19 @@ __global__ __launch_bounds__(256 * KG, TM * TN >= 4 ? 2 : TM * TN >= 2 ? 3 : 4) 
     const float* src;
     if (A_KC) {
       ok = r0 + row < rows && kg + k < KE;
-      long long arow = (long long)e * R + r0 + row;
+      long long arow = (SUMS ? 0 : (long long)e * R) + r0 + row;
       if (gather != nullptr) {
         const int tok = ok ? gather[arow] : -1;
         ok = tok >= 0;
         arow = tok;
       }
-      src = A + arow * K + kg + k;
+      src = A + arow * lda + (SUMS ? (size_t)e * K : 0) + kg + k;
     } else {
       ok = r0 + row < R && kg + k < KE;
-      src = A + ((size_t)e * K + kg + k) * R + r0 + row;
+      src = A + ((size_t)e * K + kg + k) * lda + r0 + row;
     }
     a_addr[q] = ok ? (uint64_t)(uintptr_t)src : zline;
-    a_inc[q] = ok ? (A_KC ? 1u : (uint32_t)R) * (KG * kBK * 4) : 0u;
+    a_inc[q] = ok ? (A_KC ? 1u : (uint32_t)lda) * (KG * kBK * 4) : 0u;
     a_put[q] = PA::offset(row, k);
   }
 #pragma unroll
@@ -332,14 +345,17 @@ __global__ __launch_bounds__(256 * KG, TM * TN >= 4 ? 2 : TM * TN >= 2 ? 3 : 4) 
   auto store_tile = [&](int i, int j, const f32x16_t& c, const f32x16_t& m) {
     const int n = n0 + wn0 + 32 * j + l32, rb = r0 + wm0 + 32 * i + 4 * hf;
     if (n >= N) return;
-    const size_t o = ((size_t)e * R + rb) * N + n;
+    const size_t o = ((size_t)e * R + rb) * ldc + n;
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
       const int dr = 8 * (v >> 2) + (v & 3);
       float x = c[v];
       if (EPI == 1) x = fmaxf(x, 0.f);
       if (EPI == 2) x = m[v] > 0.f ? x : 0.f;
-      if (rb + dr < rows) Cout[o + (size_t)dr * N] = x;
+      if (rb + dr < rows) {
+        if (SUMS && add) x += Cout[o + (size_t)dr * ldc];
+        Cout[o + (size_t)dr * ldc] = x;
+      }
     }
   };
 
@@ -373,12 +389,12 @@ __global__ __launch_bounds__(256 * KG, TM * TN >= 4 ? 2 : TM * TN >= 2 ? 3 : 4) 
     for (int i = 0; i < TM; ++i) {
       const int row = r0 + wm0 + 32 * i + l32;
       bool ok = row < (A_KC ? rows : R);
-      long long arow = (long long)e * R + row;
+      long long arow = (SUMS ? 0 : (long long)e * R) + row;
       if (A_KC && gather != nullptr) {
         arow = ok ? gather[arow] : -1;
         ok = arow >= 0;
       }
-      const float* src = A_KC ? A + arow * K + 4 * hf : A + ((size_t)e * K + 4 * hf) * R + row;
+      const float* src = A_KC ? A + arow * lda + (SUMS ? (size_t)e * K : 0) + 4 * hf : A + ((size_t)e * K + 4 * hf) * lda + row;
       ap[i] = ok ? (uint64_t)(uintptr_t)src : 0;
     }
 #pragma unroll
@@ -399,7 +415,7 @@ __global__ __launch_bounds__(256 * KG, TM * TN >= 4 ? 2 : TM * TN >= 2 ? 3 : 4) 
     f32x4_t x[2][TM], y[2][TN];
     auto fetch8 = [&](int k0, int u) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < TM; ++i) x[u][i] = load(A_KC, ap[i], k0, R);
+      for (int i = 0; i < TM; ++i) x[u][i] = load(A_KC, ap[i], k0, lda);
 #pragma unroll
       for (int j = 0; j < TN; ++j) y[u][j] = load(B_KC, bp[j], k0, N);
     };
@@ -444,25 +460,26 @@ __global__ __launch_bounds__(256 * KG, TM * TN >= 4 ? 2 : TM * TN >= 2 ? 3 : 4) 
     for (int j = 0; j < TN; ++j) store_tile(i, j, main[i][j], masks[i][j]);
 }
 
-template <int TM, int TN, int PD, int KG, int EPI, bool A_KC, bool B_KC, bool K_KEPT>
+template <int TM, int TN, int PD, int KG, int EPI, bool A_KC, bool B_KC, bool K_KEPT, bool PITCH = false>
 int prepare_tiles() {
   static LdsLimitOnce once;
   return ensure_lds_limit(
-      once, reinterpret_cast<const void*>(gemm_f32_mfma_kernel<TM, TN, PD, KG, EPI, A_KC, B_KC, K_KEPT>),
+      once, reinterpret_cast<const void*>(gemm_f32_mfma_kernel<TM, TN, PD, KG, EPI, A_KC, B_KC, K_KEPT, PITCH>),
       F32Smem<TM, TN, KG, A_KC, B_KC>::kBytes);
 }
 
-template <int TM, int TN, int PD, int KG, int EPI, bool A_KC, bool B_KC, bool K_KEPT>
+template <int TM, int TN, int PD, int KG, int EPI, bool A_KC, bool B_KC, bool K_KEPT, bool PITCH = false>
 int launch_tiles(const GemmArgs& a, int E, int R, int N, int K, hipStream_t st) {
-  if (prepare_tiles<TM, TN, PD, KG, EPI, A_KC, B_KC, K_KEPT>() != MOE_OK) return MOE_EHIP;
+  if (prepare_tiles<TM, TN, PD, KG, EPI, A_KC, B_KC, K_KEPT, PITCH>() != MOE_OK) return MOE_EHIP;
   constexpr size_t kLds = F32Smem<TM, TN, KG, A_KC, B_KC>::kBytes;
   const int tiles_r = (R + 64 * TM - 1) / (64 * TM), tiles_n = (N + 64 * TN - 1) / (64 * TN);
   const long long nblk = (long long)E * tiles_r * tiles_n;
   if (nblk > 0x7fffffffLL) return MOE_EUNSUPPORTED;
-  hipLaunchKernelGGL((gemm_f32_mfma_kernel<TM, TN, PD, KG, EPI, A_KC, B_KC, K_KEPT>), dim3((unsigned)nblk),
+  hipLaunchKernelGGL((gemm_f32_mfma_kernel<TM, TN, PD, KG, EPI, A_KC, B_KC, K_KEPT, PITCH>), dim3((unsigned)nblk),
                      dim3(256 * KG), kLds, st, static_cast<const float*>(a.A), static_cast<const float*>(a.B),
                      static_cast<float*>(a.C), static_cast<const float*>(a.mask), R, N, K, tiles_r,
-                     tiles_n, a.gather, a.kept);
+                     tiles_n, a.gather, a.kept, a.lda != 0 ? a.lda : A_KC ? K : R, a.ldc != 0 ? a.ldc : N,
+                     a.k_total, a.add);
   return check_launch();
 }
 
@@ -475,7 +492,7 @@ int launch_tiles(const GemmArgs& a, int E, int R, int N, int K, hipStream_t st) 
 //   E 66 R 12  M 848  H 3424  393 / 403 / 438 / 341 / 523  E 40 R 100 M 600 H 1500  169 / 184 / 224 / 148 / 142
 //   E 16 R 512 M 1024 H 2048  543 / 567 / 628 / 469 / 426  E 2  R 300 M 512 H 2048    67 / 56 / 56 / 75 / 109
 enum F32Form { k64x64, k64x64x2, k64x64x4, k64x128, k128x128 };
-F32Form f32_form(int E, int R, int N, int K, int cus) {
+F32Form f32_form(int E, int R, int N, int K, int cus, double* time = nullptr) {
   static const double t64[] = {425, 635, 915, 1230}, t64x2[] = {375, 615}, t64x4[] = {345}, t64x128[] = {590, 990, 1550},
                       t128[] = {890, 1700};
   F32Form form = k64x64;
@@ -492,19 +509,20 @@ F32Form f32_form(int E, int R, int N, int K, int cus) {
   consider(k64x64x4, 64, 64, 4, 1, t64x4);
   consider(k64x128, 64, 128, 1, 3, t64x128);
   consider(k128x128, 128, 128, 1, 2, t128);
+  if (time != nullptr) *time = 1e-3 * best;
   return form;
 }
 
-template <int EPI, bool A_KC, bool B_KC, bool K_KEPT = false>
+template <int EPI, bool A_KC, bool B_KC, bool K_KEPT = false, bool PITCH = false>
 int launch_form(const GemmArgs& a, int E, int R, int N, int K, hipStream_t st) {
   int cus = 0;
   if (compute_units(&cus) != MOE_OK) return MOE_EHIP;
   switch (f32_form(E, R, N, K, cus)) {
-    case k64x64: return launch_tiles<1, 1, 4, 1, EPI, A_KC, B_KC, K_KEPT>(a, E, R, N, K, st);
-    case k64x64x2: return launch_tiles<1, 1, 2, 2, EPI, A_KC, B_KC, K_KEPT>(a, E, R, N, K, st);
-    case k64x64x4: return launch_tiles<1, 1, 2, 4, EPI, A_KC, B_KC, K_KEPT>(a, E, R, N, K, st);
-    case k64x128: return launch_tiles<1, 2, 2, 1, EPI, A_KC, B_KC, K_KEPT>(a, E, R, N, K, st);
-    default: return launch_tiles<2, 2, 2, 1, EPI, A_KC, B_KC, K_KEPT>(a, E, R, N, K, st);
+    case k64x64: return launch_tiles<1, 1, 4, 1, EPI, A_KC, B_KC, K_KEPT, PITCH>(a, E, R, N, K, st);
+    case k64x64x2: return launch_tiles<1, 1, 2, 2, EPI, A_KC, B_KC, K_KEPT, PITCH>(a, E, R, N, K, st);
+    case k64x64x4: return launch_tiles<1, 1, 2, 4, EPI, A_KC, B_KC, K_KEPT, PITCH>(a, E, R, N, K, st);
+    case k64x128: return launch_tiles<1, 2, 2, 1, EPI, A_KC, B_KC, K_KEPT, PITCH>(a, E, R, N, K, st);
+    default: return launch_tiles<2, 2, 2, 1, EPI, A_KC, B_KC, K_KEPT, PITCH>(a, E, R, N, K, st);
   }
 }
 
@@ -517,14 +535,40 @@ int prepare_gemm_f32() {
       prepare_tiles<1, 1, 2, 4, __VA_ARGS__>(), prepare_tiles<1, 2, 2, 1, __VA_ARGS__>(),            \
       prepare_tiles<2, 2, 2, 1, __VA_ARGS__>()
       MOE_F32_ALL(0, true, false, false), MOE_F32_ALL(1, true, false, false), MOE_F32_ALL(0, true, true, false),
-      MOE_F32_ALL(2, true, true, false), MOE_F32_ALL(0, false, false, true), MOE_F32_ALL(0, false, false, false)};
+      MOE_F32_ALL(2, true, true, false), MOE_F32_ALL(0, false, false, true), MOE_F32_ALL(0, false, false, false),
+      MOE_F32_ALL(0, true, true, false, true), MOE_F32_ALL(0, true, false, false, true),
+      MOE_F32_ALL(0, false, false, true, true)};
 #undef MOE_F32_ALL
   for (int rc : rcs)
     if (rc != MOE_OK) return rc;
   return MOE_OK;
 }
 
+DenseWgradPlan vocab_dx_plan_f32(int rows, int entries, int M) {
+  constexpr int kPlanUnits = 256;                              // (sizes a workspace: of a whole device)
+  DenseWgradPlan best{1, (entries + 63) / 64 * 64};
+  double best_us = 0;
+  for (int want = 1; want <= 64; want += want < 4 ? 1 : want < 8 ? 2 : want / 4) {
+    const int k = ((entries + want - 1) / want + 63) / 64 * 64, sp = (entries + k - 1) / k;
+    if (want > 1 && (k < 256 || sp < want)) continue;
+    double us = 0;
+    f32_form(sp, rows, M, k, kPlanUnits, &us);
+    us += 1e-6 * 8 * sp * rows * M / 5.0;                      // written and read once more, us at 5 TB/s
+    if (want == 1 || us < best_us) { best_us = us; best = DenseWgradPlan{sp, k}; }
+  }
+  return best;
+}
+
 int launch_gemm_f32(GemmKind kind, const GemmArgs& a, int E, int R, int N, int K, hipStream_t st) {
+  if (a.lda != 0 || a.ldc != 0) {
+    // pitches in whole 16-byte pieces; what A's rows hold up to the next whole piece is multiplied by zeros, so is finite.
+    // Rows of A (kWeightGrad), columns of C (kDataGrad) and the sum (kForward) of any number.
+    if (E < 1 || R < 1 || N < 1 || K < 1 || a.lda % 4 != 0 || a.ldc % 4 != 0 || a.kept == nullptr) return MOE_EUNSUPPORTED;
+    if (kind == kDataGrad && K % 4 == 0 && E == 1) return launch_form<0, true, true, false, true>(a, E, R, N, K, st);
+    if (kind == kForward && N % 4 == 0 && K % 4 == 0) return launch_form<0, true, false, false, true>(a, E, R, N, K, st);
+    if (kind == kWeightGrad && N % 4 == 0 && E == 1) return launch_form<0, false, false, true, true>(a, E, R, N, K, st);
+    return MOE_EUNSUPPORTED;
+  }
   // unit strides along K (kForward: A; kDataGrad: A and B), N and R in whole 16-byte pieces
   if (E < 1 || R < 1 || N < 1 || K < 1 || N % 4 != 0 || (kind == kWeightGrad ? R : K) % 4 != 0)
     return MOE_EUNSUPPORTED;

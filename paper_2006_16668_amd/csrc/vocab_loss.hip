@@ -1,0 +1,528 @@
+// The loss at the end of a model (the paper trains its models on the cross entropy of the next word, over vocabularies of 32k
+// and 64k entries): x [N,M] are the last hidden states, w [V,M] one row per vocabulary entry, z = x . w^T the logits.
+//
+//   cross entropy   loss_n = lse_n - z[n,target_n],  lse_n = log sum_v exp z[n,v]
+//                   dz[n,v] = g_n (exp(z[n,v] - lse_n) - [v = target_n])
+//   distillation    q = softmax(t_n / T) over a teacher's K entries,  lse_n = log sum_v exp(z[n,v] / T)
+//                   loss_n = sum_k q_k (log q_k - z[n,i_k] / T + lse_n)
+//                   dz[n,v] = g_n / T (exp(z[n,v] / T - lse_n) - sum_{k: i_k = v} q_k)
+//   both            dx = dz . w,  dw = dz^T . x
+//
+// The logits are never kept.  bf16: the forward product leaves of every row and wavefront tile the maximum and the sum of
+// exponentials (8 bytes for 32 to 128 logits), the backward pass multiplies again and keeps one piece of the vocabulary's dz,
+// rounded to bf16 once, as the upstream gradients of the expert layers are, for the two products that read it.  fp32: a piece
+// of the logits is multiplied into memory and read once (forward), turned into dz in place (backward).
+//
+// Tokens without a target (padding, prompts) are left out of every product: the rows that have one are numbered first
+// (vocab_rows_kernel), so neither their work nor what their x holds, NaN included, reaches anything.
+//
+// This file holds the passes over rows; the products are in expert_gemm.hip and gemm_f32.hip.
+#include <math.h>
+#include "common.h"
+
+namespace moe {
+namespace {
+
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
+
+// ---------------------------------------------------------------- rows with a target
+// perm[p] = the p-th token with a target, pos[n] = its p or -1, kept[0] their number.  A block of 256 threads numbers 1024
+// tokens and counts those before them by itself: no order of blocks, one launch (32768 tokens: 4 us).
+struct VocabRowArgs {
+  const int32_t* has;          // targets (a target is 0 .. entries - 1), or with entries 0: flags
+  int entries;
+  long long N;
+  int32_t *perm, *pos, *kept;
+  // forward: zeros for the tokens without a target
+  float *loss, *lse;
+  // backward: what the products read per packed row
+  const float *loss_in, *lse_in, *dloss;
+  float inv_t, *lse2, *grad, *hit_value;
+  int32_t* hit;
+};
+__global__ __launch_bounds__(256) void vocab_rows_kernel(VocabRowArgs a) {
+  const long long first = (long long)blockIdx.x * 1024;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  auto valid = [&](int32_t v) { return a.entries != 0 ? (uint32_t)v < (uint32_t)a.entries : v != 0; };
+  int before = 0;
+#pragma unroll 4
+  for (long long i = 4 * tid; i < first; i += 1024) {
+    const int4 v = *reinterpret_cast<const int4*>(a.has + i);
+    before += (int)valid(v.x) + (int)valid(v.y) + (int)valid(v.z) + (int)valid(v.w);
+  }
+  const long long n0 = first + 4 * tid;
+  int32_t v[4];
+  int own = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[i] = n0 + i < a.N ? a.has[n0 + i] : (a.entries != 0 ? -1 : 0);
+    own += (int)valid(v[i]);
+  }
+  int incl = own;                                              // within the wavefront, then of the wavefronts before
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int u = __shfl_up(incl, o, 64);
+    if (lane >= o) incl += u;
+    before += __shfl_xor(before, o, 64);
+  }
+  __shared__ int sums[8];
+  if (lane == 63) { sums[wave] = incl; sums[4 + wave] = before; }
+  __syncthreads();
+  int p = incl - own;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) p += sums[4 + w] + (w < wave ? sums[w] : 0);
+  if (blockIdx.x == gridDim.x - 1 && tid == 255) a.kept[0] = p + own;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const long long n = n0 + i;
+    if (n >= a.N) break;
+    const bool ok = valid(v[i]);
+    if (a.pos != nullptr) a.pos[n] = ok ? p : -1;
+    if (!ok) {
+      if (a.loss != nullptr) { a.loss[n] = 0.f; a.lse[n] = 0.f; }
+      continue;
+    }
+    a.perm[p] = (int32_t)n;
+    if (a.lse_in != nullptr) {
+      const float g = a.dloss[n] * a.inv_t;
+      a.lse2[p] = a.lse_in[n] * kLog2e;
+      a.grad[p] = g;
+      if (a.hit != nullptr) {                                  // exp(z - lse) - 1 at the target, where z - lse = -loss
+        a.hit[p] = v[i];
+        a.hit_value[p] = expm1f(-a.loss_in[n]) * g;
+      }
+    }
+    ++p;
+  }
+}
+
+// ---------------------------------------------------------------- single logits
+// The dot product of two rows of M by the 16 lanes l of a group, in all of them; rows in pieces of 16 bytes.
+template <typename T>
+__device__ __forceinline__ float row_dot(const uint4* __restrict__ x, const uint4* __restrict__ w, int pieces, int l) {
+  constexpr int K = Vec16<T>::kElts;
+  float acc = 0.f;
+#pragma unroll 4
+  for (int i = l; i < pieces; i += 16) {
+    float a[K], b[K];
+    Vec16<T>::unpack(x[i], a);
+    Vec16<T>::unpack(w[i], b);
+#pragma unroll
+    for (int k = 0; k < K; ++k) acc = fmaf(a[k], b[k], acc);
+  }
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) acc += __shfl_xor(acc, o, 64);
+  return acc;
+}
+
+// ---------------------------------------------------------------- the teacher's entries
+// An entry is there if its index is one of the vocabulary's and its logit is not -inf.
+struct TeacherArgs {
+  const int32_t* idx;          // [N,K]
+  const float* logit;          // [N,K]
+  int K, entries;
+  float inv_t;
+};
+__device__ __forceinline__ bool teacher_has(const TeacherArgs& t, int32_t i, float l) {
+  return (uint32_t)i < (uint32_t)t.entries && l != -INFINITY;
+}
+// One wavefront per token: maximum of its teacher's logits and the sum of exponentials, whether there is any, and (z not NULL)
+// the student's logits at the entries, 0 where there is none: a group of 16 lanes per entry.
+template <typename T>
+__global__ __launch_bounds__(256) void vocab_teacher_kernel(TeacherArgs t, const uint4* __restrict__ x,
+                                                            const uint4* __restrict__ w, int pieces, long long N,
+                                                            float2* __restrict__ stat, int32_t* __restrict__ has,
+                                                            float* __restrict__ z) {
+  const long long n = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (n >= N) return;
+  const int lane = threadIdx.x & 63;
+  const int32_t* idx = t.idx + n * t.K;
+  const float* logit = t.logit + n * t.K;
+  float mx = -INFINITY;
+  bool any = false;
+  for (int k = lane; k < t.K; k += 64)
+    if (teacher_has(t, idx[k], logit[k])) { mx = fmaxf(mx, logit[k]); any = true; }
+  mx = wave_max(mx);
+  any = __builtin_amdgcn_ballot_w64(any) != 0;
+  float sum = 0.f;
+  for (int k = lane; k < t.K; k += 64)
+    if (teacher_has(t, idx[k], logit[k])) sum += expf((logit[k] - mx) * t.inv_t);
+  sum = wave_sum(sum);
+  if (lane == 0) { stat[n] = float2{mx, sum}; has[n] = any; }
+  if (z == nullptr) return;
+  const int group = lane >> 4, l = lane & 15;
+  for (int k0 = 0; k0 < t.K; k0 += 4) {                        // (the four groups stay together: row_dot's shuffles)
+    const int k = k0 + group;
+    const bool ok = k < t.K && teacher_has(t, idx[k], logit[k]);
+    const float d = row_dot<T>(x + (size_t)n * pieces, w + (size_t)(ok ? idx[k] : 0) * pieces, ok ? pieces : 0, l);
+    if (l == 0 && k < t.K) z[n * t.K + k] = ok ? d : 0.f;
+  }
+}
+
+// ---------------------------------------------------------------- loss of the packed rows
+// 16 rows a block: 16 threads of a row meet the slots' maxima and sums, then the 16 lanes of a group finish one row: its
+// target's logit (cross entropy), or the sum over the teacher's entries.
+template <typename T, bool TEACHER>
+__global__ __launch_bounds__(256) void vocab_finish_kernel(const float2* __restrict__ stats, int slots, long long N,
+                                                           const int32_t* __restrict__ perm, const int32_t* __restrict__ kept,
+                                                           const uint4* __restrict__ x, const uint4* __restrict__ w, int pieces,
+                                                           const int32_t* __restrict__ target, TeacherArgs t,
+                                                           const float2* __restrict__ tstat, const float* __restrict__ z,
+                                                           float* __restrict__ loss, float* __restrict__ lse) {
+  __shared__ float2 part[16][17];
+  __shared__ float lse_of[16];
+  const long long p0 = (long long)blockIdx.x * 16;
+  const int rows = kept[0];
+  if (p0 >= rows) return;
+  const int r = threadIdx.x & 15, sl = threadIdx.x >> 4;
+  const long long p = p0 + r < rows ? p0 + r : rows - 1;
+  float m = -INFINITY, s = 0.f;
+  auto meet = [](float& m, float& s, const float2 o) {
+    const float up = fmaxf(m, o.x), at = up == -INFINITY ? 0.f : up;
+    s = s * __builtin_amdgcn_exp2f(m - at) + o.y * __builtin_amdgcn_exp2f(o.x - at);
+    m = up;
+  };
+#pragma unroll 4
+  for (int i = sl; i < slots; i += 16) meet(m, s, stats[(size_t)i * N + p]);
+  part[r][sl] = float2{m, s};
+  __syncthreads();
+  if (threadIdx.x < 16) {
+#pragma unroll
+    for (int i = 1; i < 16; ++i) meet(m, s, part[r][i]);
+    lse_of[r] = (m + log2f(s)) * kLn2;
+  }
+  __syncthreads();
+  if (p0 + sl >= rows) return;                                 // (whole groups of 16 lanes)
+  const long long n = perm[p0 + sl];
+  const float l = lse_of[sl];
+  float out;
+  if (!TEACHER) {
+    out = l - row_dot<T>(x + (size_t)n * pieces, w + (size_t)target[n] * pieces, pieces, r);
+  } else {
+    const float2 ts = tstat[n];
+    const float inv = 1.f / ts.y, log_sum = logf(ts.y);
+    out = 0.f;
+    for (int k = r; k < t.K; k += 16) {
+      const float tl = t.logit[n * t.K + k];
+      if (!teacher_has(t, t.idx[n * t.K + k], tl)) continue;
+      const float a = (tl - ts.x) * t.inv_t, q = expf(a) * inv;
+      if (!(q == 0.f)) out += q * (a - log_sum - z[n * t.K + k] * t.inv_t + l);     // (0 log 0 = 0; NaN stays)
+    }
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) out += __shfl_xor(out, o, 64);
+  }
+  if (r == 0) { loss[n] = out; lse[n] = l; }
+}
+
+// ---------------------------------------------------------------- fp32: passes over a piece of the logits
+// z [rows, ld]: a block per packed row leaves the maximum and sum of its `entries` logits.
+__global__ __launch_bounds__(256) void vocab_stats_f32_kernel(const float* __restrict__ z, int ld, int entries, float scale,
+                                                              const int32_t* __restrict__ kept, float2* __restrict__ stats) {
+  if ((int)blockIdx.x >= kept[0]) return;
+  const float* row = z + (size_t)blockIdx.x * ld;
+  const int lane = threadIdx.x & 63;
+  float mx = -INFINITY;
+  for (int v = threadIdx.x; v < entries; v += 256) mx = fmaxf(mx, row[v]);
+  __shared__ float red[8];
+  mx = wave_max(mx);
+  if (lane == 0) red[threadIdx.x >> 6] = mx;
+  __syncthreads();
+  mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])) * scale;
+  const float m = fabsf(mx) == INFINITY ? 0.f : mx;
+  float s = 0.f;
+  for (int v = threadIdx.x; v < entries; v += 256) s += __builtin_amdgcn_exp2f(fmaf(row[v], scale, -m));
+  s = wave_sum(s);
+  if (lane == 0) red[4 + (threadIdx.x >> 6)] = s;
+  __syncthreads();
+  if (threadIdx.x == 0)
+    stats[blockIdx.x] = float2{mx == INFINITY ? 0.f : mx, (red[4] + red[5]) + (red[6] + red[7])};
+}
+// z -> dz in place, zeros up to the next whole 16 bytes
+__global__ __launch_bounds__(256) void vocab_grad_f32_kernel(float* __restrict__ z, int ld, int entries, VocabRows a,
+                                                             const int32_t* __restrict__ kept) {
+  const int p = blockIdx.x;
+  if (p >= kept[0]) return;
+  float* row = z + (size_t)p * ld;
+  const float lse = a.lse2[p], g = a.grad[p];
+  const int hit = a.hit != nullptr ? a.hit[p] - a.first : -1;
+  for (int v = threadIdx.x; v < (entries + 3) / 4 * 4; v += 256) {
+    float d = v < entries ? __builtin_amdgcn_exp2f(fmaf(row[v], a.scale, -lse)) * g : 0.f;
+    if (v == hit) d = a.hit_value[p];
+    row[v] = d;
+  }
+}
+
+// ---------------------------------------------------------------- dz at the teacher's entries
+// One wavefront per packed row: (exp(z/T - lse) - the q of all its entries with that index) g/T, at the entries of this piece.
+template <typename T>
+__global__ __launch_bounds__(256) void vocab_entry_grad_kernel(TeacherArgs t, const float2* __restrict__ tstat,
+                                                               const float* __restrict__ z, VocabRows a,
+                                                               const int32_t* __restrict__ perm,
+                                                               const int32_t* __restrict__ kept, T* __restrict__ dz, int ld,
+                                                               int entries) {
+  extern __shared__ float2 entry_smem[];                       // [4 wavefronts][K]: index (its bits) and q
+  const long long p = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (p >= kept[0]) return;
+  const int lane = threadIdx.x & 63;
+  float2* const e = entry_smem + (threadIdx.x >> 6) * t.K;
+  const long long n = perm[p];
+  const float2 ts = tstat[n];
+  const float inv = 1.f / ts.y;
+  for (int k = lane; k < t.K; k += 64) {
+    const int32_t i = t.idx[n * t.K + k];
+    const float l = t.logit[n * t.K + k];
+    const bool ok = teacher_has(t, i, l);
+    e[k] = float2{__int_as_float(ok ? i : -1), ok ? expf((l - ts.x) * t.inv_t) * inv : 0.f};
+  }
+  __builtin_amdgcn_wave_barrier();
+  for (int k = lane; k < t.K; k += 64) {
+    const int i = __float_as_int(e[k].x), at = i - a.first;
+    if (i < 0 || at < 0 || at >= entries) continue;
+    float q = 0.f;
+    for (int j = 0; j < t.K; ++j) q += __float_as_int(e[j].x) == i ? e[j].y : 0.f;
+    const float d = __builtin_amdgcn_exp2f(fmaf(z[n * t.K + k], a.scale, -a.lse2[p])) - q;
+    Elt<T>::store(dz + (size_t)p * ld + at, d * a.grad[p]);
+  }
+}
+
+// ---------------------------------------------------------------- rows in and out
+// packed[p] = x[perm[p]], 16 bytes a thread: dw sums over rows that lie together
+__global__ __launch_bounds__(256) void vocab_pack_kernel(const uint4* __restrict__ x, uint4* __restrict__ packed,
+                                                         const int32_t* __restrict__ perm, const int32_t* __restrict__ kept,
+                                                         int pieces, long long total) {
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= total) return;
+  const long long p = i / pieces;
+  if (p >= kept[0]) return;
+  packed[i] = x[(size_t)perm[p] * pieces + (i - p * pieces)];
+}
+// dx[n] = the sum of the ranges' sums of its packed row, zeros without one
+template <typename T>
+__global__ __launch_bounds__(256) void vocab_dx_kernel(const float4* __restrict__ sums, int splits, long long N,
+                                                       const int32_t* __restrict__ pos, uint4* __restrict__ dx, int pieces) {
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= N * pieces) return;
+  constexpr int K = Vec16<T>::kElts;
+  const long long n = i / pieces;
+  const int p = pos[n];
+  float v[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) v[k] = 0.f;
+  if (p >= 0) {
+    const size_t at = ((size_t)p * pieces + (i - n * pieces)) * (K / 4);
+    for (int s = 0; s < splits; ++s)
+#pragma unroll
+      for (int k = 0; k < K; k += 4) {
+        const float4 f = sums[(size_t)s * N * pieces * (K / 4) + at + k / 4];
+        v[k] += f.x; v[k + 1] += f.y; v[k + 2] += f.z; v[k + 3] += f.w;
+      }
+  }
+  dx[i] = Vec16<T>::pack(v);
+}
+
+unsigned blocks_of(long long threads) { return (unsigned)((threads + 255) / 256); }
+
+}  // namespace
+
+// Pieces of the vocabulary: as many entries as keep a piece of [N, entries] within 1 GiB, 4096 at least (a sum of dx over
+// fewer would spend its time on adding to dx), all alike; in whole 256.
+VocabPieces vocab_pieces(const moe_config& c, const moe_vocab_dims& d) {
+  const long long N = (long long)c.G * c.S, elt = c.act_dtype == MOE_F32 ? 4 : 2;
+  long long most = d.piece;
+  if (most == 0) {
+    most = (1LL << 30) / (N * elt);
+    if (most < 4096) most = 4096;
+  }
+  if (most > d.V) most = d.V;
+  const long long n = (d.V + most - 1) / most;
+  VocabPieces p;
+  p.entries = (int)(((d.V + n - 1) / n + 255) / 256 * 256);
+  p.count = (d.V + p.entries - 1) / p.entries;
+  return p;
+}
+
+VocabWs carve_vocab(const moe_config& c, const moe_vocab_dims& d, bool teacher, bool backward) {
+  const size_t N = (size_t)c.G * c.S, elt = c.act_dtype == MOE_F32 ? 4 : 2;
+  const VocabPieces p = vocab_pieces(c, d);
+  VocabWs w{};
+  size_t off = 0;
+  auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes, 256); return o; };
+  w.kept = take(4);
+  w.perm = take(N * 4);
+  w.tstat = take(teacher ? N * 8 : 0);
+  w.has = take(teacher ? N * 4 : 0);
+  if (!backward) {
+    w.slots = c.act_dtype == MOE_F32 ? p.count : vocab_stat_slots((int)N, d.V, c.M);
+    w.stats = take((size_t)w.slots * N * 8);
+    w.dz = take(c.act_dtype == MOE_F32 ? N * p.entries * 4 : 0);
+  } else {
+    w.pos = take(N * 4);
+    w.lse2 = take(N * 4);
+    w.grad = take(N * 4);
+    w.hit = take(N * 4);
+    w.hit_value = take(N * 4);
+    w.dx_plan = c.act_dtype == MOE_F32 ? vocab_dx_plan_f32((int)N, p.entries < d.V ? p.entries : d.V, c.M)
+                                       : vocab_dx_plan((int)N, p.entries < d.V ? p.entries : d.V, c.M);
+    w.packed = take(N * c.M * elt);
+    w.dz = take(N * p.entries * elt);
+    w.sums = take((size_t)w.dx_plan.splits * N * c.M * 4);
+  }
+  w.total = off;
+  return w;
+}
+
+static int launch_teacher(const moe_config& c, const TeacherArgs& t, const void* x, const void* w, char* base, const VocabWs& ws,
+                          float* z, hipStream_t st) {
+  const long long N = (long long)c.G * c.S;
+  const int pieces = c.M * (c.act_dtype == MOE_F32 ? 4 : 2) / 16;
+  auto args = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((N + 3) / 4)), dim3(256), 0, st, t, static_cast<const uint4*>(x),
+                       static_cast<const uint4*>(w), pieces, N, reinterpret_cast<float2*>(base + ws.tstat),
+                       reinterpret_cast<int32_t*>(base + ws.has), z);
+  };
+  if (c.act_dtype == MOE_F32) args(vocab_teacher_kernel<float>); else args(vocab_teacher_kernel<bf16_t>);
+  return check_launch();
+}
+
+static VocabRowArgs row_args(const moe_config& c, const moe_vocab_dims& d, const VocabCall& a, char* base, const VocabWs& ws) {
+  VocabRowArgs r{};
+  r.has = a.target != nullptr ? a.target : reinterpret_cast<const int32_t*>(base + ws.has);
+  r.entries = a.target != nullptr ? d.V : 0;
+  r.N = (long long)c.G * c.S;
+  r.perm = reinterpret_cast<int32_t*>(base + ws.perm);
+  r.kept = reinterpret_cast<int32_t*>(base + ws.kept);
+  return r;
+}
+static int launch_rows(const VocabRowArgs& r, hipStream_t st) {
+  hipLaunchKernelGGL(vocab_rows_kernel, dim3((unsigned)((r.N + 1023) / 1024)), dim3(256), 0, st, r);
+  return check_launch();
+}
+
+int launch_vocab_forward(const moe_config& c, const moe_vocab_dims& d, const VocabCall& a, void* base_, hipStream_t st) {
+  char* const base = static_cast<char*>(base_);
+  const VocabWs ws = carve_vocab(c, d, a.target == nullptr, false);
+  const VocabPieces pc = vocab_pieces(c, d);
+  const long long N = (long long)c.G * c.S;
+  const bool f32 = c.act_dtype == MOE_F32;
+  const float inv_t = a.target != nullptr ? 1.f : 1.f / d.temperature;
+  const TeacherArgs t{a.idx, a.logit, d.K, d.V, inv_t};
+  int rc = MOE_OK;
+  if (a.target == nullptr && (rc = launch_teacher(c, t, a.x, a.w, base, ws, a.entry_logit, st)) != MOE_OK) return rc;
+  VocabRowArgs r = row_args(c, d, a, base, ws);
+  r.loss = a.loss;
+  r.lse = a.lse;
+  if ((rc = launch_rows(r, st)) != MOE_OK) return rc;
+  float2* const stats = reinterpret_cast<float2*>(base + ws.stats);
+  GemmArgs g{a.x, a.w, nullptr};
+  g.gather = r.perm;
+  g.kept = r.kept;
+  g.vocab.scale = kLog2e * inv_t;
+  if (!f32) {
+    g.vocab.stats = stats;
+    if ((rc = launch_vocab_logits(g, (int)N, d.V, c.M, st)) != MOE_OK) return rc;
+  } else {
+    float* const z = reinterpret_cast<float*>(base + ws.dz);
+    for (int i = 0; i < pc.count; ++i) {
+      const int first = i * pc.entries, n = d.V - first < pc.entries ? d.V - first : pc.entries;
+      g.B = static_cast<const float*>(a.w) + (size_t)first * c.M;
+      g.C = z;
+      g.ldc = pc.entries;
+      if ((rc = launch_gemm_f32(kDataGrad, g, 1, (int)N, n, c.M, st)) != MOE_OK) return rc;
+      hipLaunchKernelGGL(vocab_stats_f32_kernel, dim3((unsigned)N), dim3(256), 0, st, z, pc.entries, n, g.vocab.scale, r.kept,
+                         stats + (size_t)i * N);
+      if ((rc = check_launch()) != MOE_OK) return rc;
+    }
+  }
+  const int pieces = c.M * (f32 ? 4 : 2) / 16;
+  auto finish = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((N + 15) / 16)), dim3(256), 0, st, stats, ws.slots, N, r.perm, r.kept,
+                       static_cast<const uint4*>(a.x), static_cast<const uint4*>(a.w), pieces, a.target, t,
+                       reinterpret_cast<const float2*>(base + ws.tstat), a.entry_logit, a.loss, a.lse);
+  };
+  if (a.target != nullptr) { if (f32) finish(vocab_finish_kernel<float, false>); else finish(vocab_finish_kernel<bf16_t, false>); }
+  else { if (f32) finish(vocab_finish_kernel<float, true>); else finish(vocab_finish_kernel<bf16_t, true>); }
+  return check_launch();
+}
+
+int launch_vocab_backward(const moe_config& c, const moe_vocab_dims& d, const VocabCall& a, void* base_, hipStream_t st) {
+  char* const base = static_cast<char*>(base_);
+  const VocabWs ws = carve_vocab(c, d, a.target == nullptr, true);
+  const VocabPieces pc = vocab_pieces(c, d);
+  const long long N = (long long)c.G * c.S;
+  const bool f32 = c.act_dtype == MOE_F32;
+  const size_t elt = f32 ? 4 : 2;
+  const int pieces = (int)(c.M * elt / 16);
+  const float inv_t = a.target != nullptr ? 1.f : 1.f / d.temperature;
+  const TeacherArgs t{a.idx, a.logit, d.K, d.V, inv_t};
+  int rc = MOE_OK;
+  if (a.target == nullptr && (rc = launch_teacher(c, t, a.x, a.w, base, ws, nullptr, st)) != MOE_OK) return rc;
+  VocabRowArgs r = row_args(c, d, a, base, ws);
+  r.pos = reinterpret_cast<int32_t*>(base + ws.pos);
+  r.lse_in = a.lse;
+  r.loss_in = a.loss;
+  r.dloss = a.dloss;
+  r.inv_t = inv_t;
+  r.lse2 = reinterpret_cast<float*>(base + ws.lse2);
+  r.grad = reinterpret_cast<float*>(base + ws.grad);
+  if (a.target != nullptr) {
+    r.hit = reinterpret_cast<int32_t*>(base + ws.hit);
+    r.hit_value = reinterpret_cast<float*>(base + ws.hit_value);
+  }
+  if ((rc = launch_rows(r, st)) != MOE_OK) return rc;
+  hipLaunchKernelGGL(vocab_pack_kernel, dim3(blocks_of(N * pieces)), dim3(256), 0, st, static_cast<const uint4*>(a.x),
+                     reinterpret_cast<uint4*>(base + ws.packed), r.perm, r.kept, pieces, N * pieces);
+  if ((rc = check_launch()) != MOE_OK) return rc;
+  for (int i = 0; i < pc.count; ++i) {
+    const int first = i * pc.entries, n = d.V - first < pc.entries ? d.V - first : pc.entries;
+    const char* const w = static_cast<const char*>(a.w) + (size_t)first * c.M * elt;
+    GemmArgs z{base + ws.packed, w, base + ws.dz};
+    z.kept = r.kept;
+    z.ldc = pc.entries;
+    z.vocab.scale = kLog2e * inv_t;
+    z.vocab.lse2 = r.lse2;
+    z.vocab.grad = r.grad;
+    z.vocab.hit = r.hit;
+    z.vocab.hit_value = r.hit_value;
+    z.vocab.first = first;
+    if (f32) {
+      if ((rc = launch_gemm_f32(kDataGrad, z, 1, (int)N, n, c.M, st)) != MOE_OK) return rc;
+      hipLaunchKernelGGL(vocab_grad_f32_kernel, dim3((unsigned)N), dim3(256), 0, st, static_cast<float*>(z.C), pc.entries, n,
+                         z.vocab, r.kept);
+      rc = check_launch();
+    } else {
+      rc = launch_vocab_logits(z, (int)N, n, c.M, st);
+    }
+    if (rc != MOE_OK) return rc;
+    if (a.target == nullptr) {
+      auto entries = [&](auto kernel, auto* dz) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((N + 3) / 4)), dim3(256), (size_t)4 * d.K * sizeof(float2), st, t,
+                           reinterpret_cast<const float2*>(base + ws.tstat), a.entry_logit, z.vocab, r.perm, r.kept, dz,
+                           pc.entries, n);
+      };
+      if (f32) entries(vocab_entry_grad_kernel<float>, static_cast<float*>(z.C));
+      else entries(vocab_entry_grad_kernel<bf16_t>, static_cast<bf16_t*>(z.C));
+      if ((rc = check_launch()) != MOE_OK) return rc;
+    }
+    GemmArgs gx{z.C, w, base + ws.sums};
+    gx.kept = r.kept;
+    gx.lda = pc.entries;
+    gx.k_total = n;
+    gx.add = i > 0;
+    const DenseWgradPlan plan{(n + ws.dx_plan.k - 1) / ws.dx_plan.k, ws.dx_plan.k};      // (a last piece fills fewer ranges)
+    rc = f32 ? launch_gemm_f32(kForward, gx, plan.splits, (int)N, c.M, plan.k, st) : launch_vocab_dx(gx, plan, (int)N, c.M, st);
+    if (rc != MOE_OK) return rc;
+    GemmArgs gw{z.C, base + ws.packed, static_cast<char*>(a.dw) + (size_t)first * c.M * elt};
+    gw.kept = r.kept;
+    gw.lda = pc.entries;
+    rc = f32 ? launch_gemm_f32(kWeightGrad, gw, 1, n, c.M, (int)N, st) : launch_vocab_dw(gw, (int)N, n, c.M, st);
+    if (rc != MOE_OK) return rc;
+  }
+  auto out = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3(blocks_of(N * pieces)), dim3(256), 0, st, reinterpret_cast<const float4*>(base + ws.sums),
+                       ws.dx_plan.splits, N, r.pos, static_cast<uint4*>(a.dx), pieces);
+  };
+  if (f32) out(vocab_dx_kernel<float>); else out(vocab_dx_kernel<bf16_t>);
+  return check_launch();
+}
+
+}  // namespace moe
