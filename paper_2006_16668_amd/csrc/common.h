@@ -281,17 +281,25 @@ int launch_gemm_bf16_f32out(bool transposed_a, const void* A, const void* B, flo
 enum GemmKind { kForward, kForwardRelu, kDataGrad, kDataGradMask, kWeightGrad };
 int launch_gemm_f32(GemmKind kind, const GemmArgs& a, int E, int R, int N, int K, hipStream_t st);
 
-// A vocabulary's products (fp32: launch_gemm_f32 with pitches) in bf16 (expert_gemm.hip): rows = the tokens, of which a.kept[0] count, entries = those of a piece
-//   z = a.A[a.gather] . a.B^T: a.vocab.stats, or the gradient in a.C (rows of a.ldc)
+// A vocabulary's products (fp32: launch_gemm_f32 with pitches) in bf16 (expert_gemm.hip): rows = the tokens, of which a.kept[0]
+// count, entries = those of a piece.  dz lies in rows of a multiple of 256 and holds zeros up to the next whole 16 bytes and in the
+// rows up to the next whole 64 (rows up to whole 256 exist).
+//   z = a.A[a.gather] . a.B^T: a.vocab.stats, or dz in a.C (rows of a.ldc)
+bool vocab_logits_on_tiles(int rows, int entries, int M, bool pack);   // pack: x is packed for it alone, and gather is NULL
 int vocab_stat_slots(int rows, int entries, int M);
 int launch_vocab_logits(const GemmArgs& a, int rows, int entries, int M, hipStream_t st);
 //   dx: C [splits, rows, M] fp32 = (or +=) sums over the plan's ranges of A [rows, lda] . B [entries, M]
-struct DenseWgradPlan { int splits, k; };      // ranges, length of each (the last may be shorter)
-DenseWgradPlan vocab_dx_plan(int rows, int entries, int M);
-DenseWgradPlan vocab_dx_plan_f32(int rows, int entries, int M);        // gemm_f32.hip
-int launch_vocab_dx(const GemmArgs& a, const DenseWgradPlan& p, int rows, int M, hipStream_t st);
-//   dw: C [entries, M] = A [rows, lda]^T . B [rows, M]
+struct VocabDxPlan { int splits, k; bool tiles; };     // ranges, length of each (the last may be shorter)
+VocabDxPlan vocab_dx_plan(int rows, int entries, int M);
+VocabDxPlan vocab_dx_plan_f32(int rows, int entries, int M);           // gemm_f32.hip
+int launch_vocab_dx(const GemmArgs& a, const VocabDxPlan& p, int rows, int M, hipStream_t st);
+//   dw: C [entries, M] = A [rows, lda]^T . B [rows, M], which has rows of zeros like dz
+bool vocab_dw_on_tiles(int rows, int entries, int M);
 int launch_vocab_dw(const GemmArgs& a, int rows, int entries, int M, hipStream_t st);
+// on 256 x 256 tiles (vocab_gemm.hip), M more than 64 for the logits
+int launch_vocab_tiles_logits(const GemmArgs& a, int rows, int entries, int M, hipStream_t st);
+int launch_vocab_tiles_dx(const GemmArgs& a, const VocabDxPlan& p, int rows, int M, hipStream_t st);
+int launch_vocab_tiles_dw(const GemmArgs& a, int entries, int M, hipStream_t st);
 
 // The loss over a vocabulary (vocab_loss.hip)
 struct VocabPieces { int entries, count; };    // of the vocabulary; a piece's entries are whole 256, the last may have fewer
@@ -299,7 +307,7 @@ VocabPieces vocab_pieces(const moe_config& c, const moe_vocab_dims& d);
 struct VocabWs {
   size_t kept, perm, tstat, has, stats, pos, lse2, grad, hit, hit_value, packed, dz, sums, total;
   int slots;                           // of stats
-  DenseWgradPlan dx_plan;              // of a whole piece
+  VocabDxPlan dx_plan;                 // of a whole piece
 };
 VocabWs carve_vocab(const moe_config& c, const moe_vocab_dims& d, bool teacher, bool backward);
 struct VocabCall {                     // target: cross entropy, else the teacher's entries
@@ -333,6 +341,7 @@ int launch_layer_norm_bwd(int act_dtype, const void* s, const void* dn, const fl
 //   dqkv [B*L, 3*heads*d] from qkv, ctx, dctx [B*L, heads*d] and lse; dvec: [B*heads*L] scratch
 // dW [in,out] = X^T dY over rows tokens (X [rows,in], dY [rows,out]); partial: scratch of
 // dense_wgrad_partial_bytes() for the token ranges of the split (may be NULL: no split)
+struct DenseWgradPlan { int splits, k; };      // ranges, tokens of each (the last may be shorter)
 DenseWgradPlan dense_wgrad_plan(long long rows, int in, int out);     // expert_gemm.hip
 int launch_dense_wgrad_ranges(const DenseWgradPlan& p, long long rows, int in, int out, const void* X, const void* dY,
                               float* partial, hipStream_t st);
@@ -382,6 +391,7 @@ int compute_units(int* cus);      // of the current device (cached per device)
 
 int prepare_expert_gemm();        // expert_gemm.hip
 int prepare_gemm_f32();           // gemm_f32.hip
+int prepare_vocab_gemm();         // vocab_gemm.hip
 int prepare_gate();               // gate.hip
 int prepare_backward();           // backward.hip
 int prepare_attention_mfma();     // attention_mfma.hip

@@ -633,7 +633,8 @@ constexpr int kEpiMaskIfAny = 6;       // 2 with a mask, else 0
 constexpr int kEpiRangesIfAny = 7;     // 3 with a k_total, else 0; kept is K_KEPT's
 // The products of a vocabulary's loss (vocab_loss.hip); E is 1 and kept[0] the rows with a target.
 //   z = x . w^T: no C, the maximum and the sum of exponentials of each row's columns of a wavefront tile (kEpiStats), or
-//     C = the gradient with respect to z, bf16 in rows of ldc, zeros in the columns N .. of the last 16 bytes (kEpiLogitGrad)
+//     C = the gradient with respect to z, bf16 in rows of ldc, with zeros in the columns N .. of the last 16
+//     bytes and in the rows behind the last of a tile (kEpiLogitGrad)
 //   dx = dz . w: A in rows of lda, "expert" e sums the k from e K on, up to k_total; C[e] fp32, or is added to
 //   dw = dz^T . x: A in rows of lda, a plain bf16 result
 constexpr int kEpiStats = 8, kEpiLogitGrad = 9, kEpiSums = 10, kEpiPitch = 11;
@@ -945,7 +946,7 @@ __device__ __forceinline__ void edge_tile(const EdgeArgs& arg, const int logical
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
       const int row = m0 + wm0 + 32 * i + (lane & 31), at = row < rows ? row : rows - 1;
-      const float lse = arg.vocab.lse2[at], up = arg.vocab.grad[at];
+      const float lse = row < rows ? arg.vocab.lse2[at] : INFINITY, up = row < rows ? arg.vocab.grad[at] : 0.f;
 #pragma unroll
       for (int j = 0; j < TN; ++j)
 #pragma unroll
@@ -1030,7 +1031,7 @@ __device__ __forceinline__ void edge_tile(const EdgeArgs& arg, const int logical
       u32x4_t d = *(lds_u4_ptr)(uintptr_t)(st_base + rr * (WN * 2) + ((c ^ (rr & (CH - 1))) * 16));
       if ((rr / CH) & 1) d = u32x4_t{d[2], d[3], d[0], d[1]};
       const int row = m0 + wm0 + 32 * i + rr, col = n0 + wn0 + 8 * c;
-      if (row < rows_out && col < N) {
+      if ((EPI == kEpiLogitGrad || row < rows_out) && col < N) {
         const size_t o = ((size_t)e * R + row) * (EPI == kEpiLogitGrad ? arg.ldc : N) + col;
         if (MASKS && masked) {
 #pragma unroll
@@ -1635,38 +1636,80 @@ int launch_dense_wgrad_ranges(const DenseWgradPlan& p, long long rows, int in, i
   return gemm_bf16_edge<3, true, false>(form, GemmArgs{X, dY, partial}, p.splits, in, out, p.k, st, (int)rows);
 }
 
-// ---- the products of a vocabulary's loss; bf16, forms by the rule of a whole device (they size a workspace)
-static GemmForm vocab_logits_form(int rows, int entries, int M) {
-  return gemm_form(false, 1, rows, entries, M, kLayoutDataGrad, kPlanUnits);
+// ---- the products of a vocabulary's loss, bf16: each runs on the 256 x 256 tiles of vocab_gemm.hip or in a form of the edge
+// kernel, whichever the rule expects to be done first on a whole device (the choice sizes a workspace).  All leave dz alike.
+//
+// Time of a product on 256 x 256 tiles (us): a launch, and per round of tiles its ends and its steps of 64 k, which take
+// longer the more units are at work, or the time in which dz passes from memory.
+//   measured / by this, us: z (M, rows, entries) 1024 1024 20000 57 / 57, 1024 1024 32000 64 / 65, 1024 6000 32000 369 / 368,
+//   256 6000 32000 158 / 157, 2048 512 32000 60 / 57; dx 1024 2048 100000 335 / 333; dw 1024 6000 32000 324 / 317
+struct TileCost { double launch, ends, alone, full; };
+constexpr TileCost kTilesLogits{4, 7.5, 0.95, 1.45}, kTilesDx{5, 5, 1.15, 1.65}, kTilesDw{4, 6, 1.0, 1.6};
+static double tiles_time(const TileCost& c, long long tiles, int k, double dz_bytes) {
+  const int steps = (k + 63) / 64;
+  const long long full = tiles / kPlanUnits;
+  const double part = (double)(tiles - full * kPlanUnits) / kPlanUnits;
+  double us = c.launch + full * (c.ends + steps * c.full);
+  if (part > 0) us += c.ends + steps * (c.alone + (c.full - c.alone) * part * part);
+  const double stream = c.launch + dz_bytes / 3.5e6;
+  return us > stream ? us : stream;
+}
+static int tiles_of(int n) { return (n + 255) / 256; }
+// What the edge kernel needs beyond the costs of its forms, which were fitted to the expert layers: exponentials at the end of a
+// tile, and short sums of many tiles.  Of 94 sizes (M 256 to 2048, 256 to 6000 rows, 1000 to 100000 entries) the choice is within
+// 6 % of the faster kernel for all z and 92 dw; without these factors for 89 and 90.
+constexpr double kEdgeLogits = 1.09, kEdgeDw = 1.05;
+static GemmForm vocab_logits_form(int rows, int entries, int M, double* us = nullptr) {
+  return gemm_form(false, 1, rows, entries, M, kLayoutDataGrad, kPlanUnits, us);
+}
+bool vocab_logits_on_tiles(int rows, int entries, int M, bool pack) {
+  if (M <= 64) return false;                                   // (two steps at least)
+  double us = 0;
+  vocab_logits_form(rows, entries, M, &us);
+  // (the edge kernel gathers the rows of x by itself, the tiles' are packed: one more launch)
+  const double packing = pack ? 4.0 + 4e-6 * rows * M / 5.0 : 0.0;
+  return tiles_time(kTilesLogits, (long long)tiles_of(rows) * tiles_of(entries), M, 0) + packing < kEdgeLogits * us;
 }
 int vocab_stat_slots(int rows, int entries, int M) {
+  if (vocab_logits_on_tiles(rows, entries, M, true)) return tiles_of(entries);
   const int bn = form_costs(kLayoutDataGrad)[vocab_logits_form(rows, entries, M)].bn;
   return 2 * ((entries + bn - 1) / bn);
 }
 int launch_vocab_logits(const GemmArgs& a, int rows, int entries, int M, hipStream_t st) {
+  const bool stats = a.vocab.stats != nullptr;
+  if (vocab_logits_on_tiles(rows, entries, M, stats)) return launch_vocab_tiles_logits(a, rows, entries, M, st);
   const GemmForm form = vocab_logits_form(rows, entries, M);
-  return a.vocab.stats != nullptr ? gemm_bf16_edge<kEpiStats, false, true>(form, a, 1, rows, entries, M, st)
-                                  : gemm_bf16_edge<kEpiLogitGrad, false, true>(form, a, 1, rows, entries, M, st);
+  return stats ? gemm_bf16_edge<kEpiStats, false, true>(form, a, 1, rows, entries, M, st)
+               : gemm_bf16_edge<kEpiLogitGrad, false, true>(form, a, 1, rows, entries, M, st);
 }
 // Ranges of the vocabulary's entries that dx is summed over side by side: few rows make few tiles of a long sum.
-DenseWgradPlan vocab_dx_plan(int rows, int entries, int M) {
-  DenseWgradPlan best{1, (entries + 63) / 64 * 64};
+VocabDxPlan vocab_dx_plan(int rows, int entries, int M) {
+  VocabDxPlan best{1, (entries + 63) / 64 * 64, false};
   double best_us = 0;
-  for (int want = 1; want <= 64; want += want < 4 ? 1 : want < 8 ? 2 : want / 4) {
+  for (int want = 1; want <= 64; ++want) {
     const int k = ((entries + want - 1) / want + 63) / 64 * 64, sp = (entries + k - 1) / k;
     if (want > 1 && (k < 256 || sp < want)) continue;
+    const double sums = 1e-6 * 8 * sp * rows * M / 5.0;        // written and read once more, us at 5 TB/s
     double us = 0;
     gemm_form(false, sp, rows, M, sp == 1 ? entries : k, kLayoutForward, kPlanUnits, &us);
-    us += 1e-6 * 8 * sp * rows * M / 5.0;                      // written and read once more, us at 5 TB/s
-    if (want == 1 || us < best_us) { best_us = us; best = DenseWgradPlan{sp, k}; }
+    if (want == 1 || us + sums < best_us) { best_us = us + sums; best = VocabDxPlan{sp, k, false}; }
+    us = tiles_time(kTilesDx, (long long)sp * tiles_of(rows) * tiles_of(M), sp == 1 ? entries : k, 2.0 * rows * entries);
+    if (us + sums < best_us) { best_us = us + sums; best = VocabDxPlan{sp, k, true}; }
   }
   return best;
 }
-int launch_vocab_dx(const GemmArgs& a, const DenseWgradPlan& p, int rows, int M, hipStream_t st) {
+int launch_vocab_dx(const GemmArgs& a, const VocabDxPlan& p, int rows, int M, hipStream_t st) {
+  if (p.tiles) return launch_vocab_tiles_dx(a, p, rows, M, st);
   const GemmForm form = gemm_form(false, p.splits, rows, M, p.k, kLayoutForward, kPlanUnits);
   return gemm_bf16_edge<kEpiSums, false, false>(form, a, p.splits, rows, M, p.k, st, a.k_total);
 }
+bool vocab_dw_on_tiles(int rows, int entries, int M) {
+  double us = 0;
+  gemm_form(false, 1, entries, M, rows, kLayoutWeightGrad, kPlanUnits, &us);
+  return tiles_time(kTilesDw, (long long)tiles_of(entries) * tiles_of(M), rows, 0) < kEdgeDw * us;
+}
 int launch_vocab_dw(const GemmArgs& a, int rows, int entries, int M, hipStream_t st) {
+  if (vocab_dw_on_tiles(rows, entries, M)) return launch_vocab_tiles_dw(a, entries, M, st);
   const GemmForm form = gemm_form(false, 1, entries, M, rows, kLayoutWeightGrad, kPlanUnits);
   return gemm_bf16_edge<kEpiPitch, true, false, true>(form, a, 1, entries, M, rows, st);
 }

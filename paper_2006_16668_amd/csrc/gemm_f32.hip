@@ -544,17 +544,17 @@ int prepare_gemm_f32() {
   return MOE_OK;
 }
 
-DenseWgradPlan vocab_dx_plan_f32(int rows, int entries, int M) {
+VocabDxPlan vocab_dx_plan_f32(int rows, int entries, int M) {
   constexpr int kPlanUnits = 256;                              // (sizes a workspace: of a whole device)
-  DenseWgradPlan best{1, (entries + 63) / 64 * 64};
+  VocabDxPlan best{1, (entries + 63) / 64 * 64, false};
   double best_us = 0;
-  for (int want = 1; want <= 64; want += want < 4 ? 1 : want < 8 ? 2 : want / 4) {
+  for (int want = 1; want <= 64; ++want) {
     const int k = ((entries + want - 1) / want + 63) / 64 * 64, sp = (entries + k - 1) / k;
     if (want > 1 && (k < 256 || sp < want)) continue;
     double us = 0;
     f32_form(sp, rows, M, k, kPlanUnits, &us);
     us += 1e-6 * 8 * sp * rows * M / 5.0;                      // written and read once more, us at 5 TB/s
-    if (want == 1 || us < best_us) { best_us = us; best = DenseWgradPlan{sp, k}; }
+    if (want == 1 || us < best_us) { best_us = us; best = VocabDxPlan{sp, k, false}; }
   }
   return best;
 }

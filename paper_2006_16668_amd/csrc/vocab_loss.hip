@@ -286,15 +286,16 @@ __global__ __launch_bounds__(256) void vocab_entry_grad_kernel(TeacherArgs t, co
 }
 
 // ---------------------------------------------------------------- rows in and out
-// packed[p] = x[perm[p]], 16 bytes a thread: dw sums over rows that lie together
+// packed[p] = x[perm[p]], 16 bytes a thread: dw sums over rows that lie together, in whole 64 (zeros behind the last)
 __global__ __launch_bounds__(256) void vocab_pack_kernel(const uint4* __restrict__ x, uint4* __restrict__ packed,
                                                          const int32_t* __restrict__ perm, const int32_t* __restrict__ kept,
                                                          int pieces, long long total) {
   const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
   if (i >= total) return;
   const long long p = i / pieces;
-  if (p >= kept[0]) return;
-  packed[i] = x[(size_t)perm[p] * pieces + (i - p * pieces)];
+  const int rows = kept[0];
+  if (p >= (rows + 63) / 64 * 64) return;
+  packed[i] = p < rows ? x[(size_t)perm[p] * pieces + (i - p * pieces)] : uint4{0u, 0u, 0u, 0u};
 }
 // dx[n] = the sum of the ranges' sums of its packed row, zeros without one
 template <typename T>
@@ -347,12 +348,15 @@ VocabWs carve_vocab(const moe_config& c, const moe_vocab_dims& d, bool teacher, 
   VocabWs w{};
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes, 256); return o; };
+  const bool packs = c.act_dtype == MOE_BF16 && vocab_logits_on_tiles((int)N, d.V, c.M, true);
+  const size_t whole = align_up(N, 256);                       // rows in whole tiles
   w.kept = take(4);
   w.perm = take(N * 4);
   w.tstat = take(teacher ? N * 8 : 0);
   w.has = take(teacher ? N * 4 : 0);
   if (!backward) {
     w.slots = c.act_dtype == MOE_F32 ? p.count : vocab_stat_slots((int)N, d.V, c.M);
+    w.packed = take(packs ? whole * c.M * elt : 0);
     w.stats = take((size_t)w.slots * N * 8);
     w.dz = take(c.act_dtype == MOE_F32 ? N * p.entries * 4 : 0);
   } else {
@@ -363,8 +367,8 @@ VocabWs carve_vocab(const moe_config& c, const moe_vocab_dims& d, bool teacher, 
     w.hit_value = take(N * 4);
     w.dx_plan = c.act_dtype == MOE_F32 ? vocab_dx_plan_f32((int)N, p.entries < d.V ? p.entries : d.V, c.M)
                                        : vocab_dx_plan((int)N, p.entries < d.V ? p.entries : d.V, c.M);
-    w.packed = take(N * c.M * elt);
-    w.dz = take(N * p.entries * elt);
+    w.packed = take(whole * c.M * elt);
+    w.dz = take(whole * p.entries * elt);
     w.sums = take((size_t)w.dx_plan.splits * N * c.M * 4);
   }
   w.total = off;
@@ -398,6 +402,14 @@ static int launch_rows(const VocabRowArgs& r, hipStream_t st) {
   return check_launch();
 }
 
+static int launch_pack(const moe_config& c, const void* x, void* packed, const VocabRowArgs& r, hipStream_t st) {
+  const int pieces = c.M * (c.act_dtype == MOE_F32 ? 4 : 2) / 16;
+  const long long total = (r.N + 63) / 64 * 64 * pieces;
+  hipLaunchKernelGGL(vocab_pack_kernel, dim3(blocks_of(total)), dim3(256), 0, st, static_cast<const uint4*>(x),
+                     static_cast<uint4*>(packed), r.perm, r.kept, pieces, total);
+  return check_launch();
+}
+
 int launch_vocab_forward(const moe_config& c, const moe_vocab_dims& d, const VocabCall& a, void* base_, hipStream_t st) {
   char* const base = static_cast<char*>(base_);
   const VocabWs ws = carve_vocab(c, d, a.target == nullptr, false);
@@ -413,8 +425,10 @@ int launch_vocab_forward(const moe_config& c, const moe_vocab_dims& d, const Voc
   r.lse = a.lse;
   if ((rc = launch_rows(r, st)) != MOE_OK) return rc;
   float2* const stats = reinterpret_cast<float2*>(base + ws.stats);
-  GemmArgs g{a.x, a.w, nullptr};
-  g.gather = r.perm;
+  const bool packs = !f32 && vocab_logits_on_tiles((int)N, d.V, c.M, true);
+  if (packs && (rc = launch_pack(c, a.x, base + ws.packed, r, st)) != MOE_OK) return rc;
+  GemmArgs g{packs ? base + ws.packed : a.x, a.w, nullptr};
+  g.gather = packs ? nullptr : r.perm;
   g.kept = r.kept;
   g.vocab.scale = kLog2e * inv_t;
   if (!f32) {
@@ -469,9 +483,7 @@ int launch_vocab_backward(const moe_config& c, const moe_vocab_dims& d, const Vo
     r.hit_value = reinterpret_cast<float*>(base + ws.hit_value);
   }
   if ((rc = launch_rows(r, st)) != MOE_OK) return rc;
-  hipLaunchKernelGGL(vocab_pack_kernel, dim3(blocks_of(N * pieces)), dim3(256), 0, st, static_cast<const uint4*>(a.x),
-                     reinterpret_cast<uint4*>(base + ws.packed), r.perm, r.kept, pieces, N * pieces);
-  if ((rc = check_launch()) != MOE_OK) return rc;
+  if ((rc = launch_pack(c, a.x, base + ws.packed, r, st)) != MOE_OK) return rc;
   for (int i = 0; i < pc.count; ++i) {
     const int first = i * pc.entries, n = d.V - first < pc.entries ? d.V - first : pc.entries;
     const char* const w = static_cast<const char*>(a.w) + (size_t)first * c.M * elt;
@@ -508,13 +520,13 @@ int launch_vocab_backward(const moe_config& c, const moe_vocab_dims& d, const Vo
     gx.lda = pc.entries;
     gx.k_total = n;
     gx.add = i > 0;
-    const DenseWgradPlan plan{(n + ws.dx_plan.k - 1) / ws.dx_plan.k, ws.dx_plan.k};      // (a last piece fills fewer ranges)
-    rc = f32 ? launch_gemm_f32(kForward, gx, plan.splits, (int)N, c.M, plan.k, st) : launch_vocab_dx(gx, plan, (int)N, c.M, st);
+    const VocabDxPlan plan{(n + ws.dx_plan.k - 1) / ws.dx_plan.k, ws.dx_plan.k, ws.dx_plan.tiles};      // (a last piece fills fewer ranges)
+    rc = f32 ? launch_gemm_f32(kForward, gx, plan.splits, (int)N, c.M, plan.k, st)  : launch_vocab_dx(gx, plan, (int)N, c.M, st);
     if (rc != MOE_OK) return rc;
     GemmArgs gw{z.C, base + ws.packed, static_cast<char*>(a.dw) + (size_t)first * c.M * elt};
     gw.kept = r.kept;
     gw.lda = pc.entries;
-    rc = f32 ? launch_gemm_f32(kWeightGrad, gw, 1, n, c.M, (int)N, st) : launch_vocab_dw(gw, (int)N, n, c.M, st);
+    rc = f32 ? launch_gemm_f32(kWeightGrad, gw, 1, n, c.M, (int)N, st)  : launch_vocab_dw(gw, (int)N, n, c.M, st);
     if (rc != MOE_OK) return rc;
   }
   auto out = [&](auto kernel) {

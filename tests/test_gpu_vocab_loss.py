@@ -112,7 +112,12 @@ CE = [(1, 1, 8, 1, "bf16", 0, 0), (1, 1, 4, 1, "f32", 0, 0), (1, 1, 64, 2, "bf16
       (1, 3, 36, 17, "f32", 0, 0), (2, 65, 72, 257, "bf16", 0.3, 0), (2, 65, 68, 255, "f32", 0.3, 0), (1, 300, 264, 1000, "bf16", 0, 256),
       (3, 100, 520, 515, "bf16", 0.7, 256), (3, 100, 260, 515, "f32", 0.7, 256), (1, 1, 1024, 4001, "bf16", 0, 0),
       (1, 17, 512, 8193, "f32", 0.1, 0), (1, 1025, 128, 1031, "bf16", 0.5, 512), (1, 2049, 32, 300, "bf16", 0.05, 0),
-      (4, 1000, 200, 3001, "bf16", 0.1, 0), (1, 5000, 256, 12000, "bf16", 0.1, 0), (1, 3000, 1000, 2500, "f32", 0.1, 1024)]
+      (4, 1000, 200, 3001, "bf16", 0.1, 0), (1, 5000, 256, 12000, "bf16", 0.1, 0), (1, 3000, 1000, 2500, "f32", 0.1, 1024),
+      # products on 256 x 256 tiles (test_vocab_rules.py: which): ragged in every dimension, several pieces, the last of few entries,
+      # most rows without a target
+      (1, 2100, 448, 33333, "bf16", 0.1, 0), (3, 1021, 776, 20257, "bf16", 0.6, 0), (1, 6000, 192, 9999, "bf16", 0.3, 0),
+      (1, 3000, 1000, 9001, "bf16", 0, 4096), (2, 1250, 1344, 7003, "bf16", 0.02, 0), (1, 32, 4096, 16000, "bf16", 0, 0),
+      (1, 1024, 1024, 32000, "bf16", 0.97, 0), (1, 9001, 72, 26001, "bf16", 0, 8192)]
 
 
 @pytest.mark.parametrize("G,S,M,V,dtype,empty,piece", CE)
