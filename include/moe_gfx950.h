@@ -366,6 +366,18 @@ int moe_add_layer_norm(const moe_config* cfg, const void* x, const void* delta,
                        const float* gamma, const float* beta, void* sum_out, void* norm_out,
                        void* stream);
 
+/* Its derivative, for L = sum dn * norm_out + sum dres * s: with xhat = (s - mean) / sqrt(var + 1e-6) and g = gamma dn,
+ *   ds = (g - mean(g) - xhat mean(g xhat)) / sqrt(var + 1e-6) + dres,  dgamma = sum_rows dn xhat,  dbeta = sum_rows dn
+ * (ds is the gradient of x and of delta).  in: s [G,S,M] (sum_out, or x where delta was NULL), dn [G,S,M]; dres [G,S,M] or
+ * NULL (what reaches s past the normalisation: the residual branch); gamma [M] fp32.  out: ds [G,S,M] (may be dres, no other
+ * input); dgamma, dbeta [M] fp32, fully overwritten.  Sums over rows run in a fixed order.
+ * ws >= moe_layer_norm_backward_workspace_bytes, 256-byte aligned.  Rows of any width, forward and backward, below 2^22 of
+ * them where one is wider than 8 KB forward, 32 KB backward. */
+int moe_layer_norm_backward_workspace_bytes(const moe_config* cfg, size_t* bytes);
+int moe_add_layer_norm_backward(const moe_config* cfg, const void* s, const void* dn, const float* gamma,
+                                const void* dres, void* ds, float* dgamma, float* dbeta,
+                                void* ws, size_t ws_bytes, void* stream);
+
 /* Bytes of workspace of moe_self_attention / moe_encoder_pair_forward.  Pure host functions. */
 int moe_attention_workspace_bytes(const moe_config* cfg, const moe_encoder_dims* dims, size_t* bytes);
 int moe_encoder_workspace_bytes(const moe_config* cfg, const moe_encoder_dims* dims, size_t* bytes);
@@ -427,8 +439,7 @@ int moe_encoder_pair_forward_train(const moe_config* cfg, const moe_encoder_dims
  * ws >= moe_encoder_backward_workspace_bytes, 256-byte aligned.  Errors as the other calls;
  * MOE_EUNSUPPORTED also when the attention shape is served by neither form of the core's
  * derivative: the MFMA kernels take bf16 with d in {64,128}, other calls (fp32 ones
- * of MFMA kernels included) need (2 L + 2 d) * 16 bytes of LDS <= 64 KB; and when M * 16 bytes > 64 KB (layer-norm
- * parameter sums).  Results are bit-reproducible (no atomics). */
+ * of MFMA kernels included) need (2 L + 2 d) * 16 bytes of LDS <= 64 KB.  Results are bit-reproducible (no atomics). */
 int moe_encoder_pair_backward(const moe_config* cfg, const moe_encoder_dims* dims, const void* x,
                               const moe_encoder_weights* w, const void* dy, const float* daux,
                               const void* fwd_ws, size_t fwd_ws_bytes, void* dx,

@@ -31,7 +31,8 @@ EXPORTS = ("moe_status_string", "moe_prepare", "moe_gate_workspace_bytes", "moe_
            "moe_encoder_backward_workspace_bytes", "moe_encoder_pair_forward_train",
            "moe_encoder_pair_backward",
            "moe_vocab_workspace_bytes", "moe_vocab_backward_workspace_bytes", "moe_vocab_loss", "moe_vocab_loss_backward",
-           "moe_vocab_distill", "moe_vocab_distill_backward")
+           "moe_vocab_distill", "moe_vocab_distill_backward",
+           "moe_layer_norm_backward_workspace_bytes", "moe_add_layer_norm_backward")
 FORWARD_EVENTS = 6
 BACKWARD_EVENTS = 8
 
@@ -159,6 +160,8 @@ def load_library() -> ctypes.CDLL:
         "moe_encoder_pair_backward": [cfgp, ctypes.POINTER(_EncoderDims), vp,
                                       ctypes.POINTER(_EncoderWeights), vp, vp, vp, sz, vp,
                                       ctypes.POINTER(_EncoderWeights), vp, sz, vp],
+        "moe_layer_norm_backward_workspace_bytes": [cfgp, ctypes.POINTER(sz)],
+        "moe_add_layer_norm_backward": [cfgp] + [vp] * 8 + [sz, vp],
         "moe_vocab_workspace_bytes": [cfgp, ctypes.POINTER(_VocabDims), ctypes.POINTER(sz)],
         "moe_vocab_backward_workspace_bytes": [cfgp, ctypes.POINTER(_VocabDims), ctypes.POINTER(sz)],
         "moe_vocab_loss": [cfgp, ctypes.POINTER(_VocabDims)] + [vp] * 6 + [sz, vp],
@@ -482,6 +485,28 @@ def moe_add_layer_norm(shape: MoEShape, x, delta, gamma, beta, sum_out, norm_out
         _ptr(gamma, f32, (M,), "gamma"), _ptr(beta, f32, (M,), "beta"),
         _ptr(sum_out, dt, (G, S, M), "sum_out"), _ptr(norm_out, dt, (G, S, M), "norm_out"), _stream()),
         "moe_add_layer_norm")
+
+
+def moe_layer_norm_backward_workspace_bytes(shape: MoEShape) -> int:
+    n = ctypes.c_size_t(0)
+    c = shape._c()
+    _check(load_library().moe_layer_norm_backward_workspace_bytes(ctypes.byref(c), ctypes.byref(n)),
+           "moe_layer_norm_backward_workspace_bytes")
+    return n.value
+
+
+def moe_add_layer_norm_backward(shape: MoEShape, s, dn, gamma, dres, ds, dgamma, dbeta, ws):
+    """Gradients of moe_add_layer_norm: ds (of x and of delta) from dn and dres (None: nothing reaches s past the norm)."""
+    _given(s=s, dn=dn, gamma=gamma, ds=ds, dgamma=dgamma, dbeta=dbeta, ws=ws)
+    _on_current_device(dres=dres)
+    G, S, M = shape.G, shape.S, shape.M
+    dt, f32 = shape.torch_dtype, torch.float32
+    c = shape._c()
+    wsp, wsn = _ws(ws)
+    _check(load_library().moe_add_layer_norm_backward(
+        ctypes.byref(c), _ptr(s, dt, (G, S, M), "s"), _ptr(dn, dt, (G, S, M), "dn"), _ptr(gamma, f32, (M,), "gamma"),
+        _ptr(dres, dt, (G, S, M), "dres"), _ptr(ds, dt, (G, S, M), "ds"), _ptr(dgamma, f32, (M,), "dgamma"),
+        _ptr(dbeta, f32, (M,), "dbeta"), wsp, wsn, _stream()), "moe_add_layer_norm_backward")
 
 
 def _ws_query(fn_name, shape: MoEShape, dims: EncoderDims) -> int:

@@ -272,7 +272,7 @@ EncoderBwdWs carve_enc_bwd(const moe_config& c, const moe_encoder_dims& d) {
   w.dctx = take(N * A * elt);
   w.dhden = take(N * c.H * elt);
   w.dvec = take((size_t)d.B * d.heads * d.L * sizeof(float));
-  w.partial = take((size_t)moe::layer_norm_bwd_parts((long long)N) * 2 * c.M * sizeof(float));
+  w.partial = take(moe::layer_norm_bwd_bytes(c.act_dtype, (long long)N, c.M));
   // token ranges of the dense weight gradients (the largest of the four shapes)
   size_t wp = moe::dense_wgrad_partial_bytes(c.act_dtype, (long long)N, (int)A, c.M);
   const size_t wp2 = moe::dense_wgrad_partial_bytes(c.act_dtype, (long long)N, c.M, 3 * (int)A);
@@ -678,6 +678,29 @@ int moe_add_layer_norm(const moe_config* cfg, const void* x, const void* delta, 
     return MOE_EINVAL;
   return moe::launch_add_layer_norm(cfg->act_dtype, x, delta, gamma, beta, sum_out, norm_out,
                                     (long long)cfg->G * cfg->S, cfg->M,
+                                    static_cast<hipStream_t>(stream));
+}
+
+int moe_layer_norm_backward_workspace_bytes(const moe_config* cfg, size_t* bytes) {
+  const int rc = check_config(cfg);
+  if (rc != MOE_OK) return rc;
+  if (bytes == nullptr) return MOE_EINVAL;
+  *bytes = align_up(moe::layer_norm_bwd_bytes(cfg->act_dtype, (long long)cfg->G * cfg->S, cfg->M), 256);
+  return MOE_OK;
+}
+
+int moe_add_layer_norm_backward(const moe_config* cfg, const void* s, const void* dn, const float* gamma, const void* dres,
+                                void* ds, float* dgamma, float* dbeta, void* ws, size_t ws_bytes, void* stream) {
+  const int rc = check_config(cfg);
+  if (rc != MOE_OK) return rc;
+  const void* req[] = {s, dn, gamma, ds, dgamma, dbeta, ws};
+  for (const void* p : req)
+    if (p == nullptr || !aligned16(p)) return MOE_EINVAL;
+  if (dres != nullptr && !aligned16(dres)) return MOE_EINVAL;
+  if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return MOE_EINVAL;
+  const long long rows = (long long)cfg->G * cfg->S;
+  if (ws_bytes < moe::layer_norm_bwd_bytes(cfg->act_dtype, rows, cfg->M)) return MOE_EWORKSPACE;
+  return moe::launch_layer_norm_bwd(cfg->act_dtype, s, dn, gamma, dres, ds, static_cast<float*>(ws), dgamma, dbeta, rows, cfg->M,
                                     static_cast<hipStream_t>(stream));
 }
 

@@ -333,8 +333,8 @@ int launch_attention_core(int act_dtype, const void* qkv, void* ctx, float* lse,
 
 // backward of the encoder sub-layers (encoder_bwd.hip)
 //   ds = dres (may be NULL) + d LN(s) / d s applied to dn; dgamma, dbeta [M]; partial:
-//   layer_norm_bwd_parts(rows) * 2 * M floats of scratch.  dx may alias dres.
-int layer_norm_bwd_parts(long long rows);
+//   layer_norm_bwd_bytes() of scratch.  dx may alias dres.
+size_t layer_norm_bwd_bytes(int act_dtype, long long rows, int M);
 int launch_layer_norm_bwd(int act_dtype, const void* s, const void* dn, const float* gamma,
                           const void* dres, void* dx, float* partial, float* dgamma, float* dbeta,
                           long long rows, int M, hipStream_t st);

@@ -127,6 +127,203 @@ __global__ __launch_bounds__(256) void layer_norm_bwd_kernel(
   }
 }
 
+// Rows wider than that: one block per row, which walks rows block, block + blocks, ... with the parameters' column sums in
+// registers (VPT vectors of 16 bytes per thread) and fetches the next row while the sums of one meet.  4096 rows of 8192 bf16 with a
+// residual's gradient, 256 blocks of 1024 threads 67 us, of 512 61 (4.4 TB/s), of 256 64, 512 blocks of 512 71 (more sums).
+constexpr int kLnThreads = 512;
+template <typename T, int VPT>
+__global__ __launch_bounds__(kLnThreads) void layer_norm_bwd_wide_kernel(
+    const uint4* __restrict__ s, const uint4* __restrict__ dn, const float* __restrict__ gamma, const uint4* dres, uint4* dx,
+    float* __restrict__ partial, int M, int vec_per_row, long long rows, float eps) {
+  constexpr int K = Vec16<T>::kElts, TH = kLnThreads, W = TH / 64;
+  __shared__ float4 red[2][W];
+  const int tid = threadIdx.x;
+  float ag[VPT][K], ab[VPT][K], gam[VPT][K];
+#pragma unroll
+  for (int j = 0; j < VPT; ++j)
+#pragma unroll
+    for (int i = 0; i < K; i += 4) {
+      const int col = (tid + TH * j) * K + i;
+      const float4 g4 = col < M ? *reinterpret_cast<const float4*>(gamma + col) : float4{0.f, 0.f, 0.f, 0.f};
+      gam[j][i] = g4.x; gam[j][i + 1] = g4.y; gam[j][i + 2] = g4.z; gam[j][i + 3] = g4.w;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) ag[j][i + k] = ab[j][i + k] = 0.f;
+    }
+  const float inv_m = 1.0f / (float)M;
+  uint4 sv[VPT], dv[VPT], rv[VPT];
+  auto fetch = [&](long long row) {
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+      const int vi = tid + TH * j;
+      sv[j] = dv[j] = rv[j] = uint4{0u, 0u, 0u, 0u};
+      if (vi < vec_per_row) {
+        sv[j] = s[row * vec_per_row + vi];
+        dv[j] = dn[row * vec_per_row + vi];
+        if (dres != nullptr) rv[j] = dres[row * vec_per_row + vi];
+      }
+    }
+  };
+  if ((long long)blockIdx.x < rows) fetch(blockIdx.x);
+  for (long long row = blockIdx.x; row < rows; row += gridDim.x) {
+    // (the row stays packed, three uses unpack it: as floats it would not fit beside the next one and the columns' sums)
+    uint4 cs[VPT], cd[VPT], cr[VPT];
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+      cs[j] = sv[j]; cd[j] = dv[j]; cr[j] = rv[j];
+      float v[K];
+      Vec16<T>::unpack(cs[j], v);
+#pragma unroll
+      for (int i = 0; i < K; ++i) sum += v[i];
+    }
+    if (row + gridDim.x < rows) fetch(row + gridDim.x);
+    auto keep_packed = [&]() {                                 // (the compiler would keep what it unpacked)
+#pragma unroll
+      for (int j = 0; j < VPT; ++j)
+        asm volatile("" : "+v"(cs[j].x), "+v"(cs[j].y), "+v"(cs[j].z), "+v"(cs[j].w), "+v"(cd[j].x), "+v"(cd[j].y), "+v"(cd[j].z), "+v"(cd[j].w));
+    };
+    auto meet = [&](float4 a, int which) {                     // three sums of the block
+      a.x = wave_sum(a.x); a.y = wave_sum(a.y); a.z = wave_sum(a.z);
+      if ((tid & 63) == 0) red[which][tid >> 6] = a;
+      __syncthreads();
+      float4 t = red[which][0];
+#pragma unroll
+      for (int w = 1; w < W; ++w) { t.x += red[which][w].x; t.y += red[which][w].y; t.z += red[which][w].z; }
+      return t;
+    };
+    const float mean = meet(float4{sum, 0.f, 0.f, 0.f}, 0).x * inv_m;
+    keep_packed();
+    // sums of (v - mean)^2, g and g (v - mean): of the last two the factor rstd is left out until it is known
+    float q = 0.f, sg = 0.f, sgx = 0.f;
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+      float v[K], g[K];
+      Vec16<T>::unpack(cs[j], v);
+      Vec16<T>::unpack(cd[j], g);
+#pragma unroll
+      for (int i = 0; i < K; ++i) {
+        const float c = tid + TH * j < vec_per_row ? v[i] - mean : 0.f, up = g[i] * gam[j][i];
+        q += c * c;
+        sg += up;
+        sgx += up * c;
+      }
+    }
+    const float4 t = meet(float4{q, sg, sgx, 0.f}, 1);
+    const float rstd = 1.0f / sqrtf(t.x * inv_m + eps);
+    keep_packed();
+    const float mg = t.y * inv_m, mgx = t.z * rstd * inv_m;
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+      const int vi = tid + TH * j;
+      if (vi < vec_per_row) {
+        float v[K], g[K], o[K];
+        Vec16<T>::unpack(cs[j], v);
+        Vec16<T>::unpack(cd[j], g);
+        Vec16<T>::unpack(cr[j], o);
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+          const float xh = (v[i] - mean) * rstd;
+          ag[j][i] += g[i] * xh;
+          ab[j][i] += g[i];
+          o[i] += rstd * (g[i] * gam[j][i] - mg - xh * mgx);
+        }
+        dx[row * vec_per_row + vi] = Vec16<T>::pack(o);
+      }
+    }
+    // (the next row's first sums go to red[0], which all have read before they met in red[1])
+  }
+  float* const pg = partial + (size_t)blockIdx.x * 2 * M;
+#pragma unroll
+  for (int j = 0; j < VPT; ++j) {
+    const int vi = tid + TH * j;
+    if (vi < vec_per_row)
+#pragma unroll
+      for (int i = 0; i < K; i += 4) {
+        *reinterpret_cast<float4*>(pg + vi * K + i) = float4{ag[j][i], ag[j][i + 1], ag[j][i + 2], ag[j][i + 3]};
+        *reinterpret_cast<float4*>(pg + M + vi * K + i) = float4{ab[j][i], ab[j][i + 1], ab[j][i + 2], ab[j][i + 3]};
+      }
+  }
+}
+// Rows of any width: a block of 1024 threads per row, every pass reads the row again, and its mean and rstd are left for the
+// columns' sums.
+template <typename T>
+__global__ __launch_bounds__(1024) void layer_norm_bwd_any_kernel(
+    const uint4* __restrict__ s, const uint4* __restrict__ dn, const float* __restrict__ gamma, const uint4* dres, uint4* dx,
+    float2* __restrict__ stats, int M, int vec_per_row, float eps) {
+  constexpr int K = Vec16<T>::kElts;
+  __shared__ float red[4][16];
+  const size_t base = (size_t)blockIdx.x * vec_per_row;
+  const int tid = threadIdx.x;
+  const float inv_m = 1.0f / (float)M;
+  auto block_sum = [&](float a, int which) {
+    a = wave_sum(a);
+    if ((tid & 63) == 0) red[which][tid >> 6] = a;
+    __syncthreads();
+    float t = 0.f;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) t += red[which][w];
+    return t;
+  };
+  float f[K], g[K];
+  float sum = 0.f;
+  for (int vi = tid; vi < vec_per_row; vi += 1024) {
+    Vec16<T>::unpack(s[base + vi], f);
+#pragma unroll
+    for (int i = 0; i < K; ++i) sum += f[i];
+  }
+  const float mean = block_sum(sum, 0) * inv_m;
+  float q = 0.f, sg = 0.f, sgx = 0.f;
+  for (int vi = tid; vi < vec_per_row; vi += 1024) {
+    Vec16<T>::unpack(s[base + vi], f);
+    Vec16<T>::unpack(dn[base + vi], g);
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+      f[i] -= mean;
+      g[i] *= gamma[vi * K + i];
+      q += f[i] * f[i];
+      sg += g[i];
+      sgx += g[i] * f[i];
+    }
+  }
+  const float rstd = 1.0f / sqrtf(block_sum(q, 1) * inv_m + eps);
+  const float mg = block_sum(sg, 2) * inv_m, mgx = block_sum(sgx, 3) * rstd * inv_m;
+  if (tid == 0) stats[blockIdx.x] = float2{mean, rstd};
+  for (int vi = tid; vi < vec_per_row; vi += 1024) {
+    Vec16<T>::unpack(s[base + vi], f);
+    Vec16<T>::unpack(dn[base + vi], g);
+    float o[K], r[K];
+#pragma unroll
+    for (int i = 0; i < K; ++i) r[i] = 0.f;
+    if (dres != nullptr) Vec16<T>::unpack(dres[base + vi], r);
+#pragma unroll
+    for (int i = 0; i < K; ++i) o[i] = rstd * (g[i] * gamma[vi * K + i] - mg - (f[i] - mean) * rstd * mgx) + r[i];
+    dx[base + vi] = Vec16<T>::pack(o);
+  }
+}
+// partial sums of dn xhat and dn over rows part, part + parts, ...: a thread per 16 bytes of the columns
+template <typename T>
+__global__ __launch_bounds__(256) void layer_norm_param_any_kernel(
+    const uint4* __restrict__ s, const uint4* __restrict__ dn, const float2* __restrict__ stats, float* __restrict__ partial,
+    int M, int vec_per_row, long long rows) {
+  constexpr int K = Vec16<T>::kElts;
+  const int vi = blockIdx.x * 256 + threadIdx.x;
+  if (vi >= vec_per_row) return;
+  float ag[K], ab[K];
+#pragma unroll
+  for (int i = 0; i < K; ++i) ag[i] = ab[i] = 0.f;
+  for (long long row = blockIdx.y; row < rows; row += gridDim.y) {
+    float f[K], g[K];
+    Vec16<T>::unpack(s[row * vec_per_row + vi], f);
+    Vec16<T>::unpack(dn[row * vec_per_row + vi], g);
+    const float2 st = stats[row];
+#pragma unroll
+    for (int i = 0; i < K; ++i) { ag[i] += g[i] * ((f[i] - st.x) * st.y); ab[i] += g[i]; }
+  }
+  float* const pg = partial + (size_t)blockIdx.y * 2 * M + vi * K;
+#pragma unroll
+  for (int i = 0; i < K; ++i) { pg[i] = ag[i]; pg[M + i] = ab[i]; }
+}
+
 // dgamma[m] = sum_p partial[p][0][m], dbeta[m] = sum_p partial[p][1][m]: a block owns 16 of the
 // 2 M columns, its 64 groups of 16 threads each sum every 64th partial row, LDS adds the groups
 // in a fixed order (bit-reproducible).  Bound by the latency of a thread's dependent loads, so many short
@@ -335,9 +532,20 @@ int launch_dense_grads(const moe_config& c, long long rows, int in, int out, con
                          : launch_expert_dgrad1(g, dY, W, dX, nullptr, st);
 }
 
-int layer_norm_bwd_parts(long long rows) {
-  const long long blocks = (rows + 3) / 4;
-  return (int)(blocks < 1024 ? blocks : 1024);
+// How the rows are walked: up to 8 KB and 4096 columns by wavefronts, up to 32 KB by blocks (one per unit: the sums that a block
+// leaves are as long as four rows), wider ones in any number of passes, which keep every row's mean and rstd.
+enum LayerNormBwdForm { kLnWavefronts, kLnBlocks, kLnAny };
+static LayerNormBwdForm layer_norm_bwd_plan(int act_dtype, long long rows, int M, int* parts) {
+  const int vec = M * (act_dtype == MOE_F32 ? 4 : 2) / 16;
+  const LayerNormBwdForm form = vec <= 512 && M <= 4096 ? kLnWavefronts : vec <= 2048 ? kLnBlocks : kLnAny;
+  const long long most = form == kLnWavefronts ? 1024 : form == kLnBlocks ? 256 : 64, blocks = (rows + 3) / 4;
+  *parts = (int)(blocks < most ? blocks : most);
+  return form;
+}
+size_t layer_norm_bwd_bytes(int act_dtype, long long rows, int M) {
+  int parts;
+  const LayerNormBwdForm form = layer_norm_bwd_plan(act_dtype, rows, M, &parts);
+  return (size_t)parts * 2 * M * sizeof(float) + (form == kLnAny ? (size_t)rows * sizeof(float2) : 0);
 }
 
 int launch_layer_norm_bwd(int act_dtype, const void* s, const void* dn, const float* gamma,
@@ -347,10 +555,40 @@ int launch_layer_norm_bwd(int act_dtype, const void* s, const void* dn, const fl
   const int vec_per_row = M * elt / 16;
   const int vpl = (vec_per_row + 63) / 64;
   const size_t lds = (size_t)4 * M * sizeof(float);
-  if (vpl > 8 || lds > 64 * 1024) return MOE_EUNSUPPORTED;
-  const int parts = layer_norm_bwd_parts(rows);
-  const unsigned grid = (unsigned)parts;
   const float eps = 1e-6f;
+  int parts;
+  const LayerNormBwdForm form = layer_norm_bwd_plan(act_dtype, rows, M, &parts);
+  auto reduce = [&]() {
+    hipLaunchKernelGGL(layer_norm_param_reduce_kernel, dim3((unsigned)((2 * M + 15) / 16)), dim3(16 * kReduceGroups), 0, st,
+                       partial, parts, M, dgamma, dbeta);
+    return check_launch();
+  };
+  if (form != kLnWavefronts) {
+    if (form == kLnAny && rows >= 1 << 22) return MOE_EUNSUPPORTED;      // (a launch has less than 2^32 threads)
+    auto wide = [&](auto kernel, int threads) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)parts), dim3(threads), 0, st, static_cast<const uint4*>(s),
+                         static_cast<const uint4*>(dn), gamma, static_cast<const uint4*>(dres), static_cast<uint4*>(dx), partial,
+                         M, vec_per_row, rows, eps);
+    };
+    auto any = [&](auto rows_kernel, auto columns_kernel) {
+      float2* const stats = reinterpret_cast<float2*>(partial + (size_t)parts * 2 * M);
+      hipLaunchKernelGGL(rows_kernel, dim3((unsigned)rows), dim3(1024), 0, st, static_cast<const uint4*>(s),
+                         static_cast<const uint4*>(dn), gamma, static_cast<const uint4*>(dres), static_cast<uint4*>(dx), stats, M,
+                         vec_per_row, eps);
+      hipLaunchKernelGGL(columns_kernel, dim3((unsigned)((vec_per_row + 255) / 256), (unsigned)parts), dim3(256), 0, st,
+                         static_cast<const uint4*>(s), static_cast<const uint4*>(dn), stats, partial, M, vec_per_row, rows);
+    };
+#define MOE_LNB_WIDE(T)                                                                       \
+  if (form == kLnBlocks && vec_per_row <= 1024) wide(layer_norm_bwd_wide_kernel<T, 2>, kLnThreads); \
+  else if (form == kLnBlocks && vec_per_row <= 1536) wide(layer_norm_bwd_wide_kernel<T, 3>, kLnThreads); \
+  else if (form == kLnBlocks) wide(layer_norm_bwd_wide_kernel<T, 4>, kLnThreads);             \
+  else any(layer_norm_bwd_any_kernel<T>, layer_norm_param_any_kernel<T>);
+    if (act_dtype == MOE_F32) { MOE_LNB_WIDE(float) } else { MOE_LNB_WIDE(bf16_t) }
+#undef MOE_LNB_WIDE
+    const int rc = check_launch();
+    return rc != MOE_OK ? rc : reduce();
+  }
+  const unsigned grid = (unsigned)parts;
 #define MOE_LNB_CASE(T, V)                                                                    \
   hipLaunchKernelGGL((layer_norm_bwd_kernel<T, V>), dim3(grid), dim3(256), lds, st,           \
                      static_cast<const uint4*>(s), static_cast<const uint4*>(dn), gamma,      \
@@ -364,11 +602,8 @@ int launch_layer_norm_bwd(int act_dtype, const void* s, const void* dn, const fl
     else if (vpl <= 4) MOE_LNB_CASE(bf16_t, 4); else MOE_LNB_CASE(bf16_t, 8);
   }
 #undef MOE_LNB_CASE
-  int rc = check_launch();
-  if (rc != MOE_OK) return rc;
-  hipLaunchKernelGGL(layer_norm_param_reduce_kernel, dim3((unsigned)((2 * M + 15) / 16)), dim3(16 * kReduceGroups),
-                     0, st, partial, parts, M, dgamma, dbeta);
-  return check_launch();
+  const int rc = check_launch();
+  return rc != MOE_OK ? rc : reduce();
 }
 
 // dqkv [B*L, 3*heads*d] from qkv, ctx, dctx [B*L, heads*d], lse [B*heads*L]; dvec [B*heads*L] scratch
