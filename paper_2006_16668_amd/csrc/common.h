@@ -296,9 +296,26 @@ int launch_vocab_dx(const GemmArgs& a, const VocabDxPlan& p, int rows, int M, hi
 //   dw: C [entries, M] = A [rows, lda]^T . B [rows, M], which has rows of zeros like dz
 bool vocab_dw_on_tiles(int rows, int entries, int M);
 int launch_vocab_dw(const GemmArgs& a, int rows, int entries, int M, hipStream_t st);
-// on 256 x 256 tiles (vocab_gemm.hip), M more than 64 for the logits
+// Time of a product on 256 x 256 tiles (us): a launch, and per round of tiles its ends and its steps of 64 k, which take
+// longer the more units are at work, or the time in which dz passes from memory.
+//   measured / by this, us: z (M, rows, entries) 1024 1024 20000 57 / 57, 1024 1024 32000 64 / 65, 1024 6000 32000 369 / 368,
+//   256 6000 32000 158 / 157, 2048 512 32000 60 / 57; dx 1024 2048 100000 335 / 333; dw 1024 6000 32000 324 / 317
+struct VocabTileCost { double launch, ends, alone, full; };
+constexpr VocabTileCost kTilesLogits{4, 7.5, 0.95, 1.45}, kTilesDx{5, 5, 1.15, 1.65}, kTilesDw{4, 6, 1.0, 1.6};
+__host__ __device__ inline double vocab_tiles_time(const VocabTileCost& c, long long tiles, int k, double dz_bytes) {
+  constexpr int kUnits = 256;                                  // of a whole device: the choice sizes a workspace
+  const int steps = (k + 63) / 64;
+  const long long full = tiles / kUnits;
+  const double part = (double)(tiles - full * kUnits) / kUnits;
+  double us = c.launch + full * (c.ends + steps * c.full);
+  if (part > 0) us += c.ends + steps * (c.alone + (c.full - c.alone) * part * part);
+  const double stream = c.launch + dz_bytes / 3.5e6;
+  return us > stream ? us : stream;
+}
+// on 256 x 256 tiles (vocab_gemm.hip), M more than 64 for the logits; dx in the ranges that a.kept[1] and [2] say, sums of
+// a.kept[0] rows each
 int launch_vocab_tiles_logits(const GemmArgs& a, int rows, int entries, int M, hipStream_t st);
-int launch_vocab_tiles_dx(const GemmArgs& a, const VocabDxPlan& p, int rows, int M, hipStream_t st);
+int launch_vocab_tiles_dx(const GemmArgs& a, int M, hipStream_t st);
 int launch_vocab_tiles_dw(const GemmArgs& a, int entries, int M, hipStream_t st);
 
 // The loss over a vocabulary (vocab_loss.hip)

@@ -1639,21 +1639,6 @@ int launch_dense_wgrad_ranges(const DenseWgradPlan& p, long long rows, int in, i
 // ---- the products of a vocabulary's loss, bf16: each runs on the 256 x 256 tiles of vocab_gemm.hip or in a form of the edge
 // kernel, whichever the rule expects to be done first on a whole device (the choice sizes a workspace).  All leave dz alike.
 //
-// Time of a product on 256 x 256 tiles (us): a launch, and per round of tiles its ends and its steps of 64 k, which take
-// longer the more units are at work, or the time in which dz passes from memory.
-//   measured / by this, us: z (M, rows, entries) 1024 1024 20000 57 / 57, 1024 1024 32000 64 / 65, 1024 6000 32000 369 / 368,
-//   256 6000 32000 158 / 157, 2048 512 32000 60 / 57; dx 1024 2048 100000 335 / 333; dw 1024 6000 32000 324 / 317
-struct TileCost { double launch, ends, alone, full; };
-constexpr TileCost kTilesLogits{4, 7.5, 0.95, 1.45}, kTilesDx{5, 5, 1.15, 1.65}, kTilesDw{4, 6, 1.0, 1.6};
-static double tiles_time(const TileCost& c, long long tiles, int k, double dz_bytes) {
-  const int steps = (k + 63) / 64;
-  const long long full = tiles / kPlanUnits;
-  const double part = (double)(tiles - full * kPlanUnits) / kPlanUnits;
-  double us = c.launch + full * (c.ends + steps * c.full);
-  if (part > 0) us += c.ends + steps * (c.alone + (c.full - c.alone) * part * part);
-  const double stream = c.launch + dz_bytes / 3.5e6;
-  return us > stream ? us : stream;
-}
 static int tiles_of(int n) { return (n + 255) / 256; }
 // What the edge kernel needs beyond the costs of its forms, which were fitted to the expert layers: exponentials at the end of a
 // tile, and short sums of many tiles.  Of 94 sizes (M 256 to 2048, 256 to 6000 rows, 1000 to 100000 entries) the choice is within
@@ -1668,7 +1653,7 @@ bool vocab_logits_on_tiles(int rows, int entries, int M, bool pack) {
   vocab_logits_form(rows, entries, M, &us);
   // (the edge kernel gathers the rows of x by itself, the tiles' are packed: one more launch)
   const double packing = pack ? 4.0 + 4e-6 * rows * M / 5.0 : 0.0;
-  return tiles_time(kTilesLogits, (long long)tiles_of(rows) * tiles_of(entries), M, 0) + packing < kEdgeLogits * us;
+  return vocab_tiles_time(kTilesLogits, (long long)tiles_of(rows) * tiles_of(entries), M, 0) + packing < kEdgeLogits * us;
 }
 int vocab_stat_slots(int rows, int entries, int M) {
   if (vocab_logits_on_tiles(rows, entries, M, true)) return tiles_of(entries);
@@ -1693,20 +1678,20 @@ VocabDxPlan vocab_dx_plan(int rows, int entries, int M) {
     double us = 0;
     gemm_form(false, sp, rows, M, sp == 1 ? entries : k, kLayoutForward, kPlanUnits, &us);
     if (want == 1 || us + sums < best_us) { best_us = us + sums; best = VocabDxPlan{sp, k, false}; }
-    us = tiles_time(kTilesDx, (long long)sp * tiles_of(rows) * tiles_of(M), sp == 1 ? entries : k, 2.0 * rows * entries);
+    us = vocab_tiles_time(kTilesDx, (long long)sp * tiles_of(rows) * tiles_of(M), sp == 1 ? entries : k, 2.0 * rows * entries);
     if (us + sums < best_us) { best_us = us + sums; best = VocabDxPlan{sp, k, true}; }
   }
   return best;
 }
 int launch_vocab_dx(const GemmArgs& a, const VocabDxPlan& p, int rows, int M, hipStream_t st) {
-  if (p.tiles) return launch_vocab_tiles_dx(a, p, rows, M, st);
+  if (p.tiles) return launch_vocab_tiles_dx(a, M, st);
   const GemmForm form = gemm_form(false, p.splits, rows, M, p.k, kLayoutForward, kPlanUnits);
   return gemm_bf16_edge<kEpiSums, false, false>(form, a, p.splits, rows, M, p.k, st, a.k_total);
 }
 bool vocab_dw_on_tiles(int rows, int entries, int M) {
   double us = 0;
   gemm_form(false, 1, entries, M, rows, kLayoutWeightGrad, kPlanUnits, &us);
-  return tiles_time(kTilesDw, (long long)tiles_of(entries) * tiles_of(M), rows, 0) < kEdgeDw * us;
+  return vocab_tiles_time(kTilesDw, (long long)tiles_of(entries) * tiles_of(M), rows, 0) < kEdgeDw * us;
 }
 int launch_vocab_dw(const GemmArgs& a, int rows, int entries, int M, hipStream_t st) {
   if (vocab_dw_on_tiles(rows, entries, M)) return launch_vocab_tiles_dw(a, entries, M, st);

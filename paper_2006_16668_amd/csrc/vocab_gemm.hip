@@ -48,8 +48,8 @@ struct VocabGemmArgs {
   const bf16_t *A, *B;
   void* C;
   int lda, ldb, ldc;
-  int R, N, K;                 // rows and columns of C, length of the sum (of a range: kSums); R or K (kPlain) is kept[0]
-  int k_total, tiles_n, ranges, add;
+  int R, N, K;                 // rows and columns of C, length of the sum; R, or K (kPlain), is kept[0], K of a range (kSums) kept[2]
+  int k_total, tiles_n, add;
   const int32_t* kept;
   VocabRows v;
 };
@@ -85,13 +85,14 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
   const int kept = __builtin_amdgcn_readfirstlane(g.kept[0]);
   const int R = EPI == kPlain ? g.R : kept;
   const int tiles_m = (R + 255) >> 8, tiles_n = g.tiles_n;
-  const int per_range = tiles_m * tiles_n, ntiles = per_range * g.ranges;
+  const int range = EPI == kSums ? __builtin_amdgcn_readfirstlane(g.kept[2]) : 0;      // (a last piece fills fewer of them)
+  const int per_range = tiles_m * tiles_n, ntiles = EPI == kSums ? per_range * ((g.k_total + range - 1) / range) : per_range;
   // k of a range, and its steps
   auto range_k = [&](int e) {
     if (EPI == kPlain) return kept;
     if (EPI != kSums) return g.K;
-    const int left = g.k_total - e * g.K;
-    return left < g.K ? left : g.K;
+    const int left = g.k_total - e * range;
+    return left < range ? left : range;
   };
   // this block's tiles: a contiguous share of them per XCD, taken in turn by its blocks
   const int xcd = blockIdx.x % kXcds;
@@ -125,8 +126,8 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
       if (p_steps == 0) continue;                              // (dw without a single row)
       p_more = 1;
       const int m0 = rt * 256, n0 = ct * 256, lane = lane_here();
-      p_a = A_MNC ? g.A + m0 : g.A + (size_t)m0 * g.lda + (EPI == kSums ? (size_t)e * g.K : 0);
-      p_b = B_MNC ? g.B + (EPI == kSums ? (size_t)e * g.K * g.ldb : 0) : g.B + (size_t)n0 * g.ldb;
+      p_a = A_MNC ? g.A + m0 : g.A + (size_t)m0 * g.lda + (EPI == kSums ? (size_t)e * range : 0);
+      p_b = B_MNC ? g.B + (EPI == kSums ? (size_t)e * range * g.ldb : 0) : g.B + (size_t)n0 * g.ldb;
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -371,7 +372,7 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
       const int row = m0 + 128 * (wn >> 1) + 64 * wm + 32 * (wn & 1) + r32;
       if (hh == 0 && row < R) g.v.stats[(size_t)ct * g.R + row] = float2{m, s};
     } else if constexpr (EPI == kSums) {
-      float* const C = static_cast<float*>(g.C) + (size_t)e * g.R * g.N;
+      float* const C = static_cast<float*>(g.C) + (size_t)e * R * g.N;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int row = m0 + 128 * (i >> 1) + 64 * wm + 32 * (i & 1) + r32;
@@ -469,7 +470,6 @@ VocabGemmArgs args_of(const GemmArgs& a) {
   g.C = a.C;
   g.kept = a.kept;
   g.v = a.vocab;
-  g.ranges = 1;
   return g;
 }
 int tiles_of(int n) { return (n + 255) / 256; }
@@ -498,17 +498,15 @@ int launch_vocab_tiles_logits(const GemmArgs& a, int rows, int entries, int M, h
                                   : launch_tiles<kLogitGrad>(g, tiles, M % 64 != 0, st);
 }
 
-int launch_vocab_tiles_dx(const GemmArgs& a, const VocabDxPlan& p, int rows, int M, hipStream_t st) {
+int launch_vocab_tiles_dx(const GemmArgs& a, int M, hipStream_t st) {
   VocabGemmArgs g = args_of(a);
   g.lda = a.lda;
   g.ldb = g.N = M;
-  g.R = rows;
-  g.K = p.k;
   g.k_total = a.k_total;
-  g.ranges = p.splits;
   g.add = a.add;
   g.tiles_n = tiles_of(M);
-  return launch_tiles<kSums>(g, (long long)p.splits * tiles_of(rows) * g.tiles_n, a.k_total % 64 != 0, st);
+  // (how many tiles there are the device decides)
+  return launch_tiles<kSums>(g, 0x7fffffff, a.k_total % 64 != 0, st);
 }
 
 int launch_vocab_tiles_dw(const GemmArgs& a, int entries, int M, hipStream_t st) {

@@ -26,8 +26,8 @@ namespace {
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
 
 // ---------------------------------------------------------------- rows with a target
-// perm[p] = the p-th token with a target, pos[n] = its p or -1, kept[0] their number.  A block of 256 threads numbers 1024
-// tokens and counts those before them by itself: no order of blocks, one launch (32768 tokens: 4 us).
+// perm[p] = the p-th token with a target, pos[n] = its p or -1, kept[0] their number.  A block of 1024 threads numbers 4096
+// tokens and counts those before them by itself: no order of blocks, one launch.
 struct VocabRowArgs {
   const int32_t* has;          // targets (a target is 0 .. entries - 1), or with entries 0: flags
   int entries;
@@ -39,14 +39,32 @@ struct VocabRowArgs {
   const float *loss_in, *lse_in, *dloss;
   float inv_t, *lse2, *grad, *hit_value;
   int32_t* hit;
+  // backward with dx on 256 x 256 tiles: its ranges are chosen here, for the rows that there are
+  int dx_entries, dx_tiles_n, M;     // dx_entries 0: no
+  long long dx_rows;                 // rows of sums that there is room for
+  VocabTileCost dx_cost;
 };
-__global__ __launch_bounds__(256) void vocab_rows_kernel(VocabRowArgs a) {
-  const long long first = (long long)blockIdx.x * 1024;
+constexpr int kRowThreads = 1024, kRowWaves = kRowThreads / 64;
+// kept[1] ranges of kept[2] entries: the fastest by tiles_time of vocab_dx_plan, one candidate per lane
+__device__ void vocab_dx_ranges(const VocabRowArgs& a, int rows) {
+  const int lane = threadIdx.x & 63, want = lane + 1, tiles = (rows + 255) / 256 * a.dx_tiles_n;
+  const int k = ((a.dx_entries + want - 1) / want + 63) / 64 * 64, n = (a.dx_entries + k - 1) / k;
+  float us = 3e38f;
+  if (want == 1 || (k >= 256 && n == want && (long long)n * rows <= a.dx_rows))
+    us = (float)(vocab_tiles_time(a.dx_cost, (long long)n * tiles, k, 2.0 * rows * a.dx_entries) +
+                 1.6e-6 * n * rows * a.M);
+  float best = us;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) best = fminf(best, __shfl_xor(best, o, 64));
+  if (lane == __builtin_ctzll(__builtin_amdgcn_ballot_w64(us == best))) { a.kept[1] = n; a.kept[2] = k; }
+}
+__global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabRowArgs a) {
+  const long long first = (long long)blockIdx.x * (4 * kRowThreads);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   auto valid = [&](int32_t v) { return a.entries != 0 ? (uint32_t)v < (uint32_t)a.entries : v != 0; };
   int before = 0;
-#pragma unroll 4
-  for (long long i = 4 * tid; i < first; i += 1024) {
+#pragma unroll 8
+  for (long long i = 4 * tid; i < first; i += 4 * kRowThreads) {
     const int4 v = *reinterpret_cast<const int4*>(a.has + i);
     before += (int)valid(v.x) + (int)valid(v.y) + (int)valid(v.z) + (int)valid(v.w);
   }
@@ -65,13 +83,19 @@ __global__ __launch_bounds__(256) void vocab_rows_kernel(VocabRowArgs a) {
     if (lane >= o) incl += u;
     before += __shfl_xor(before, o, 64);
   }
-  __shared__ int sums[8];
-  if (lane == 63) { sums[wave] = incl; sums[4 + wave] = before; }
+  __shared__ int sums[2 * kRowWaves];
+  if (lane == 63) { sums[wave] = incl; sums[kRowWaves + wave] = before; }
   __syncthreads();
-  int p = incl - own;
+  int p = incl - own, total = 0;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) p += sums[4 + w] + (w < wave ? sums[w] : 0);
-  if (blockIdx.x == gridDim.x - 1 && tid == 255) a.kept[0] = p + own;
+  for (int w = 0; w < kRowWaves; ++w) {
+    p += sums[kRowWaves + w] + (w < wave ? sums[w] : 0);
+    total += sums[kRowWaves + w] + sums[w];
+  }
+  if (blockIdx.x == gridDim.x - 1 && wave == 0) {
+    if (lane == 0) a.kept[0] = total;
+    if (a.dx_entries != 0) vocab_dx_ranges(a, total);
+  }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const long long n = n0 + i;
@@ -297,10 +321,10 @@ __global__ __launch_bounds__(256) void vocab_pack_kernel(const uint4* __restrict
   if (p >= (rows + 63) / 64 * 64) return;
   packed[i] = p < rows ? x[(size_t)perm[p] * pieces + (i - p * pieces)] : uint4{0u, 0u, 0u, 0u};
 }
-// dx[n] = the sum of the ranges' sums of its packed row, zeros without one
+// dx[n] = the sum of the ranges' sums of its packed row, zeros without one; kept not NULL: as many ranges as kept[1], of as many rows
 template <typename T>
 __global__ __launch_bounds__(256) void vocab_dx_kernel(const float4* __restrict__ sums, int splits, long long N,
-                                                       const int32_t* __restrict__ pos, uint4* __restrict__ dx, int pieces) {
+                                                       const int32_t* __restrict__ kept, const int32_t* __restrict__ pos, uint4* __restrict__ dx, int pieces) {
   const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
   if (i >= N * pieces) return;
   constexpr int K = Vec16<T>::kElts;
@@ -311,10 +335,13 @@ __global__ __launch_bounds__(256) void vocab_dx_kernel(const float4* __restrict_
   for (int k = 0; k < K; ++k) v[k] = 0.f;
   if (p >= 0) {
     const size_t at = ((size_t)p * pieces + (i - n * pieces)) * (K / 4);
+    const size_t next = (size_t)(kept != nullptr ? kept[0] : N) * pieces * (K / 4);
+    if (kept != nullptr) splits = kept[1];
+#pragma unroll 8
     for (int s = 0; s < splits; ++s)
 #pragma unroll
       for (int k = 0; k < K; k += 4) {
-        const float4 f = sums[(size_t)s * N * pieces * (K / 4) + at + k / 4];
+        const float4 f = sums[s * next + at + k / 4];
         v[k] += f.x; v[k + 1] += f.y; v[k + 2] += f.z; v[k + 3] += f.w;
       }
   }
@@ -350,7 +377,7 @@ VocabWs carve_vocab(const moe_config& c, const moe_vocab_dims& d, bool teacher, 
   auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes, 256); return o; };
   const bool packs = c.act_dtype == MOE_BF16 && vocab_logits_on_tiles((int)N, d.V, c.M, true);
   const size_t whole = align_up(N, 256);                       // rows in whole tiles
-  w.kept = take(4);
+  w.kept = take(12);
   w.perm = take(N * 4);
   w.tstat = take(teacher ? N * 8 : 0);
   w.has = take(teacher ? N * 4 : 0);
@@ -398,7 +425,8 @@ static VocabRowArgs row_args(const moe_config& c, const moe_vocab_dims& d, const
   return r;
 }
 static int launch_rows(const VocabRowArgs& r, hipStream_t st) {
-  hipLaunchKernelGGL(vocab_rows_kernel, dim3((unsigned)((r.N + 1023) / 1024)), dim3(256), 0, st, r);
+  constexpr int kTokens = 4 * kRowThreads;
+  hipLaunchKernelGGL(vocab_rows_kernel, dim3((unsigned)((r.N + kTokens - 1) / kTokens)), dim3(kRowThreads), 0, st, r);
   return check_launch();
 }
 
@@ -482,6 +510,14 @@ int launch_vocab_backward(const moe_config& c, const moe_vocab_dims& d, const Vo
     r.hit = reinterpret_cast<int32_t*>(base + ws.hit);
     r.hit_value = reinterpret_cast<float*>(base + ws.hit_value);
   }
+  const bool ranges = ws.dx_plan.tiles;                        // chosen by the rows kernel
+  if (ranges) {
+    r.dx_entries = pc.entries < d.V ? pc.entries : d.V;
+    r.dx_tiles_n = (c.M + 255) / 256;
+    r.M = c.M;
+    r.dx_rows = (long long)ws.dx_plan.splits * N;
+    r.dx_cost = kTilesDx;
+  }
   if ((rc = launch_rows(r, st)) != MOE_OK) return rc;
   if ((rc = launch_pack(c, a.x, base + ws.packed, r, st)) != MOE_OK) return rc;
   for (int i = 0; i < pc.count; ++i) {
@@ -531,7 +567,7 @@ int launch_vocab_backward(const moe_config& c, const moe_vocab_dims& d, const Vo
   }
   auto out = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3(blocks_of(N * pieces)), dim3(256), 0, st, reinterpret_cast<const float4*>(base + ws.sums),
-                       ws.dx_plan.splits, N, r.pos, static_cast<uint4*>(a.dx), pieces);
+                       ws.dx_plan.splits, N, ranges ? r.kept : nullptr, r.pos, static_cast<uint4*>(a.dx), pieces);
   };
   if (f32) out(vocab_dx_kernel<float>); else out(vocab_dx_kernel<bf16_t>);
   return check_launch();
