@@ -436,7 +436,9 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
           if (s >= 2) d = u32x4_t{d[2], d[3], d[0], d[1]};
           const int col = n0 + col_of(c >> 2) + 8 * (c & 3);
           bf16_t* const C = static_cast<bf16_t*>(g.C) + (size_t)(row0 + rr) * g.ldc + col;
-          if ((EPI == kLogitGrad || row0 + rr < R) && col < g.N) *reinterpret_cast<u32x4_t*>(C) = d;
+          if ((EPI == kLogitGrad || row0 + rr < R) && col < g.N) {
+            *reinterpret_cast<u32x4_t*>(C) = d;
+          }
         }
       }
     }
