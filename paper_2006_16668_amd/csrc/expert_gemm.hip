@@ -637,6 +637,7 @@ constexpr int kEpiRangesIfAny = 7;     // 3 with a k_total, else 0; kept is K_KE
 //     bytes and in the rows behind the last of a tile (kEpiLogitGrad)
 //   dx = dz . w: A in rows of lda, "expert" e sums the k from e K on, up to k_total; C[e] fp32, or is added to
 //   dw = dz^T . x: A in rows of lda, a plain bf16 result
+// (a.kept NULL: all rows count)
 constexpr int kEpiStats = 8, kEpiLogitGrad = 9, kEpiSums = 10, kEpiPitch = 11;
 
 template <int BM, int BN, int BK, int ST, int EPI, bool A_MNC, bool B_KC, bool K_KEPT>
@@ -677,7 +678,7 @@ __device__ __forceinline__ void edge_tile(const EdgeArgs& arg, const int logical
   const int ct = rem / brows, rt = band * kBand + (rem - ct * brows);
   const int m0 = rt * BM, n0 = ct * BN;
   int rows = R, rows_out = R;                                  // rows of A that count, of C that are stored
-  if (LOGITS || SUMS) rows = rows_out = kept[0];
+  if (LOGITS || SUMS) rows = rows_out = kept != nullptr ? kept[0] : R;
   else if (kept != nullptr && !k_kept) {
     rows = kept[e];
     rows_out = (rows + row_pad) & ~row_pad;
@@ -1054,7 +1055,7 @@ template <int BM, int BN, int BK, int ST, int EPI, bool A_MNC, bool B_KC, bool K
 __global__ __launch_bounds__(256, (kEdgeBlocks<BM, BN>)) void expert_gemm_bf16_edge_kernel(EdgeArgs arg) {
   if constexpr (EPI == kEpiStats || EPI == kEpiLogitGrad || EPI == kEpiSums) {
     // the row tiles that hold a target, in the order of their XCDs: their number is known here only
-    const int tiles_m = (arg.kept[0] + BM - 1) / BM, n = arg.nblk / arg.tiles_m * tiles_m;
+    const int tiles_m = ((arg.kept != nullptr ? arg.kept[0] : arg.R) + BM - 1) / BM, n = arg.nblk / arg.tiles_m * tiles_m;
     if ((int)blockIdx.x >= n) return;
     arg.tiles_m = tiles_m;
     edge_tile<BM, BN, BK, ST, EPI, A_MNC, B_KC, K_KEPT>(arg, xcd_remap(blockIdx.x, n));

@@ -58,6 +58,18 @@ __device__ void vocab_dx_ranges(const VocabRowArgs& a, int rows) {
   for (int o = 32; o > 0; o >>= 1) best = fminf(best, __shfl_xor(best, o, 64));
   if (lane == __builtin_ctzll(__builtin_amdgcn_ballot_w64(us == best))) { a.kept[1] = n; a.kept[2] = k; }
 }
+// token n, whose target is `target`, is packed row p
+__device__ void vocab_row_data(const VocabRowArgs& a, int p, long long n, int32_t target) {
+  a.perm[p] = (int32_t)n;
+  if (a.lse_in == nullptr) return;
+  const float g = a.dloss[n] * a.inv_t;
+  a.lse2[p] = a.lse_in[n] * kLog2e;
+  a.grad[p] = g;
+  if (a.hit != nullptr) {                                      // exp(z - lse) - 1 at the target, where z - lse = -loss
+    a.hit[p] = target;
+    a.hit_value[p] = expm1f(-a.loss_in[n]) * g;
+  }
+}
 __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabRowArgs a) {
   const long long first = (long long)blockIdx.x * (4 * kRowThreads);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -106,16 +118,7 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabRowArgs a)
       if (a.loss != nullptr) { a.loss[n] = 0.f; a.lse[n] = 0.f; }
       continue;
     }
-    a.perm[p] = (int32_t)n;
-    if (a.lse_in != nullptr) {
-      const float g = a.dloss[n] * a.inv_t;
-      a.lse2[p] = a.lse_in[n] * kLog2e;
-      a.grad[p] = g;
-      if (a.hit != nullptr) {                                  // exp(z - lse) - 1 at the target, where z - lse = -loss
-        a.hit[p] = v[i];
-        a.hit_value[p] = expm1f(-a.loss_in[n]) * g;
-      }
-    }
+    vocab_row_data(a, p, n, v[i]);
     ++p;
   }
 }
@@ -150,15 +153,8 @@ struct TeacherArgs {
 __device__ __forceinline__ bool teacher_has(const TeacherArgs& t, int32_t i, float l) {
   return (uint32_t)i < (uint32_t)t.entries && l != -INFINITY;
 }
-// One wavefront per token: maximum of its teacher's logits and the sum of exponentials, whether there is any, and (z not NULL)
-// the student's logits at the entries, 0 where there is none: a group of 16 lanes per entry.
-template <typename T>
-__global__ __launch_bounds__(256) void vocab_teacher_kernel(TeacherArgs t, const uint4* __restrict__ x,
-                                                            const uint4* __restrict__ w, int pieces, long long N,
-                                                            float2* __restrict__ stat, int32_t* __restrict__ has,
-                                                            float* __restrict__ z) {
-  const long long n = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (n >= N) return;
+// A wavefront's look at one token: maximum of its teacher's logits and the sum of exponentials, and whether there is any entry
+__device__ __forceinline__ bool teacher_stat(const TeacherArgs& t, long long n, float2* stat) {
   const int lane = threadIdx.x & 63;
   const int32_t* idx = t.idx + n * t.K;
   const float* logit = t.logit + n * t.K;
@@ -167,26 +163,89 @@ __global__ __launch_bounds__(256) void vocab_teacher_kernel(TeacherArgs t, const
   for (int k = lane; k < t.K; k += 64)
     if (teacher_has(t, idx[k], logit[k])) { mx = fmaxf(mx, logit[k]); any = true; }
   mx = wave_max(mx);
-  any = __builtin_amdgcn_ballot_w64(any) != 0;
   float sum = 0.f;
   for (int k = lane; k < t.K; k += 64)
     if (teacher_has(t, idx[k], logit[k])) sum += expf((logit[k] - mx) * t.inv_t);
-  sum = wave_sum(sum);
-  if (lane == 0) { stat[n] = float2{mx, sum}; has[n] = any; }
-  if (z == nullptr) return;
-  const int group = lane >> 4, l = lane & 15;
-  for (int k0 = 0; k0 < t.K; k0 += 4) {                        // (the four groups stay together: row_dot's shuffles)
-    const int k = k0 + group;
-    const bool ok = k < t.K && teacher_has(t, idx[k], logit[k]);
-    const float d = row_dot<T>(x + (size_t)n * pieces, w + (size_t)(ok ? idx[k] : 0) * pieces, ok ? pieces : 0, l);
+  *stat = float2{mx, wave_sum(sum)};
+  return __builtin_amdgcn_ballot_w64(any) != 0;
+}
+// The student's logits z at the entries of token n, 0 where there is none: a group of 16 lanes per entry, of 16 groups `at` .. by
+// `groups` (a wavefront's four stay together: row_dot's shuffles)
+template <typename T>
+__device__ __forceinline__ void entry_logits(const TeacherArgs& t, long long n, const uint4* __restrict__ x,
+                                             const uint4* __restrict__ w, int pieces, float* __restrict__ z, int at, int groups) {
+  const int l = threadIdx.x & 15, first = at & ~3;
+  for (int k0 = first; k0 < t.K; k0 += groups) {
+    const int k = k0 + (at & 3);
+    const bool ok = k < t.K && teacher_has(t, t.idx[n * t.K + k], t.logit[n * t.K + k]);
+    const float d = row_dot<T>(x + (size_t)n * pieces, w + (size_t)(ok ? t.idx[n * t.K + k] : 0) * pieces, ok ? pieces : 0, l);
     if (l == 0 && k < t.K) z[n * t.K + k] = ok ? d : 0.f;
   }
 }
+// one wavefront per token; z may be NULL
+template <typename T>
+__global__ __launch_bounds__(256) void vocab_teacher_kernel(TeacherArgs t, const uint4* __restrict__ x,
+                                                            const uint4* __restrict__ w, int pieces, long long N,
+                                                            float2* __restrict__ stat, int32_t* __restrict__ has,
+                                                            float* __restrict__ z) {
+  const long long n = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (n >= N) return;
+  float2 s;
+  const bool any = teacher_stat(t, n, &s);
+  if ((threadIdx.x & 63) == 0) { stat[n] = s; has[n] = any; }
+  if (z != nullptr) entry_logits<T>(t, n, x, w, pieces, z, (threadIdx.x >> 4) & 3, 4);
+}
+
+// Up to 64 tokens, a block each: what vocab_teacher_kernel, vocab_rows_kernel and vocab_pack_kernel do, in one launch.  Every block
+// looks at all tokens to number its own.
+constexpr int kFewTokens = 64;
+template <typename T>
+__global__ __launch_bounds__(256) void vocab_few_kernel(VocabRowArgs a, TeacherArgs t, const uint4* __restrict__ x,
+                                                        const uint4* __restrict__ w, int pieces, float2* __restrict__ stat,
+                                                        float* __restrict__ z, uint4* __restrict__ packed) {
+  const int n = blockIdx.x, N = (int)a.N, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __shared__ int has[kFewTokens];
+  if (t.K == 0) {
+    if (threadIdx.x < N) has[threadIdx.x] = (uint32_t)a.has[threadIdx.x] < (uint32_t)a.entries;
+  } else {
+    if (threadIdx.x < kFewTokens) has[threadIdx.x] = 0;
+    __syncthreads();
+    for (int e = threadIdx.x; e < N * t.K; e += 256)
+      if (teacher_has(t, t.idx[e], t.logit[e])) has[e / t.K] = 1;
+    if (wave == 0) {
+      float2 s;
+      teacher_stat(t, n, &s);
+      if (lane == 0) stat[n] = s;
+    }
+    if (z != nullptr) entry_logits<T>(t, n, x, w, pieces, z, threadIdx.x >> 4, 16);
+  }
+  __syncthreads();
+  const uint64_t which = __builtin_amdgcn_ballot_w64(lane < N && has[lane] != 0);
+  const int p = __builtin_popcountll(which & ((1ull << n) - 1)), rows = __builtin_popcountll(which);
+  const bool ok = (which >> n) & 1;
+  if (threadIdx.x == 0) {
+    if (n == 0) a.kept[0] = rows;
+    if (a.pos != nullptr) a.pos[n] = ok ? p : -1;
+    if (ok) vocab_row_data(a, p, n, t.K == 0 ? a.has[n] : 0);
+    else if (a.loss != nullptr) { a.loss[n] = 0.f; a.lse[n] = 0.f; }
+  }
+  if (n == 0 && wave == 0 && a.dx_entries != 0) vocab_dx_ranges(a, rows);
+  if (packed == nullptr) return;
+  if (ok)
+    for (int i = threadIdx.x; i < pieces; i += 256) packed[(size_t)p * pieces + i] = x[(size_t)n * pieces + i];
+  // rows of zeros up to 64: the p-th block without a target writes the one behind the last that many on
+  else
+    for (int i = threadIdx.x; i < pieces; i += 256) packed[(size_t)(rows + n - p) * pieces + i] = uint4{0u, 0u, 0u, 0u};
+  if (n == N - 1)
+    for (int r = N; r < kFewTokens; ++r)
+      for (int i = threadIdx.x; i < pieces; i += 256) packed[(size_t)r * pieces + i] = uint4{0u, 0u, 0u, 0u};
+}
 
 // ---------------------------------------------------------------- loss of the packed rows
-// 16 rows a block: 16 threads of a row meet the slots' maxima and sums, then the 16 lanes of a group finish one row: its
-// target's logit (cross entropy), or the sum over the teacher's entries.
-template <typename T, bool TEACHER>
+// ROWS rows a block: the 256 / ROWS threads of a row meet the slots' maxima and sums, then the 16 lanes of a group finish one row:
+// its target's logit (cross entropy), or the sum over the teacher's entries.  16 rows read whole lines of the statistics; a row
+// by itself is done sooner where there are few.  kept NULL: no rows were numbered, row n is token n.
+template <typename T, bool TEACHER, int ROWS>
 __global__ __launch_bounds__(256) void vocab_finish_kernel(const float2* __restrict__ stats, int slots, long long N,
                                                            const int32_t* __restrict__ perm, const int32_t* __restrict__ kept,
                                                            const uint4* __restrict__ x, const uint4* __restrict__ w, int pieces,
@@ -195,11 +254,11 @@ __global__ __launch_bounds__(256) void vocab_finish_kernel(const float2* __restr
                                                            float* __restrict__ loss, float* __restrict__ lse) {
   __shared__ float2 part[16][17];
   __shared__ float lse_of[16];
-  const long long p0 = (long long)blockIdx.x * 16;
-  const int rows = kept[0];
+  const long long p0 = (long long)blockIdx.x * ROWS;
+  const int rows = kept != nullptr ? kept[0] : (int)N;
   if (p0 >= rows) return;
   const int r = threadIdx.x & 15, sl = threadIdx.x >> 4;
-  const long long p = p0 + r < rows ? p0 + r : rows - 1;
+  const long long p = ROWS == 1 ? p0 : p0 + r < rows ? p0 + r : rows - 1;
   float m = -INFINITY, s = 0.f;
   auto meet = [](float& m, float& s, const float2 o) {
     const float up = fmaxf(m, o.x), at = up == -INFINITY ? 0.f : up;
@@ -207,17 +266,25 @@ __global__ __launch_bounds__(256) void vocab_finish_kernel(const float2* __restr
     m = up;
   };
 #pragma unroll 4
-  for (int i = sl; i < slots; i += 16) meet(m, s, stats[(size_t)i * N + p]);
+  for (int i = ROWS == 1 ? threadIdx.x : sl; i < slots; i += 256 / ROWS) meet(m, s, stats[(size_t)i * N + p]);
   part[r][sl] = float2{m, s};
   __syncthreads();
   if (threadIdx.x < 16) {
 #pragma unroll
     for (int i = 1; i < 16; ++i) meet(m, s, part[r][i]);
+    if (ROWS == 1) {
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) meet(m, s, float2{__shfl_xor(m, o, 64), __shfl_xor(s, o, 64)});
+    }
     lse_of[r] = (m + log2f(s)) * kLn2;
   }
   __syncthreads();
-  if (p0 + sl >= rows) return;                                 // (whole groups of 16 lanes)
-  const long long n = perm[p0 + sl];
+  if (sl >= ROWS || p0 + sl >= rows) return;                   // (whole groups of 16 lanes)
+  if (kept == nullptr && (uint32_t)target[p0 + sl] >= (uint32_t)t.entries) {
+    if (r == 0) { loss[p0 + sl] = 0.f; lse[p0 + sl] = 0.f; }
+    return;
+  }
+  const long long n = kept != nullptr ? perm[p0 + sl] : p0 + sl;
   const float l = lse_of[sl];
   float out;
   if (!TEACHER) {
@@ -322,11 +389,14 @@ __global__ __launch_bounds__(256) void vocab_pack_kernel(const uint4* __restrict
   packed[i] = p < rows ? x[(size_t)perm[p] * pieces + (i - p * pieces)] : uint4{0u, 0u, 0u, 0u};
 }
 // dx[n] = the sum of the ranges' sums of its packed row, zeros without one; kept not NULL: as many ranges as kept[1], of as many rows
-template <typename T>
+// PARTS neighbouring threads share the ranges of a piece (few rows: more loads on their way at once).
+template <typename T, int PARTS>
 __global__ __launch_bounds__(256) void vocab_dx_kernel(const float4* __restrict__ sums, int splits, long long N,
-                                                       const int32_t* __restrict__ kept, const int32_t* __restrict__ pos, uint4* __restrict__ dx, int pieces) {
-  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-  if (i >= N * pieces) return;
+                                                       const int32_t* __restrict__ kept, const int32_t* __restrict__ pos,
+                                                       uint4* __restrict__ dx, int pieces) {
+  const long long id = (long long)blockIdx.x * 256 + threadIdx.x, i = id / PARTS;
+  const int part = (int)(id % PARTS);
+  if (i >= N * pieces) return;                                 // (a piece's threads together)
   constexpr int K = Vec16<T>::kElts;
   const long long n = i / pieces;
   const int p = pos[n];
@@ -337,15 +407,19 @@ __global__ __launch_bounds__(256) void vocab_dx_kernel(const float4* __restrict_
     const size_t at = ((size_t)p * pieces + (i - n * pieces)) * (K / 4);
     const size_t next = (size_t)(kept != nullptr ? kept[0] : N) * pieces * (K / 4);
     if (kept != nullptr) splits = kept[1];
-#pragma unroll 8
-    for (int s = 0; s < splits; ++s)
+#pragma unroll 4
+    for (int s = part; s < splits; s += PARTS)
 #pragma unroll
       for (int k = 0; k < K; k += 4) {
         const float4 f = sums[s * next + at + k / 4];
         v[k] += f.x; v[k + 1] += f.y; v[k + 2] += f.z; v[k + 3] += f.w;
       }
   }
-  dx[i] = Vec16<T>::pack(v);
+#pragma unroll
+  for (int o = 1; o < PARTS; o <<= 1)
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], o, 64);
+  if (part == 0) dx[i] = Vec16<T>::pack(v);
 }
 
 unsigned blocks_of(long long threads) { return (unsigned)((threads + 255) / 256); }
@@ -424,6 +498,18 @@ static VocabRowArgs row_args(const moe_config& c, const moe_vocab_dims& d, const
   r.kept = reinterpret_cast<int32_t*>(base + ws.kept);
   return r;
 }
+// up to 64 tokens; packed and z may be NULL
+static int launch_few(const moe_config& c, const VocabRowArgs& r, const TeacherArgs& t, const VocabCall& a, char* base,
+                      const VocabWs& ws, float* z, void* packed, hipStream_t st) {
+  const int pieces = c.M * (c.act_dtype == MOE_F32 ? 4 : 2) / 16;
+  auto args = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)r.N), dim3(256), 0, st, r, t, static_cast<const uint4*>(a.x),
+                       static_cast<const uint4*>(a.w), pieces, reinterpret_cast<float2*>(base + ws.tstat), z,
+                       static_cast<uint4*>(packed));
+  };
+  if (c.act_dtype == MOE_F32) args(vocab_few_kernel<float>); else args(vocab_few_kernel<bf16_t>);
+  return check_launch();
+}
 static int launch_rows(const VocabRowArgs& r, hipStream_t st) {
   constexpr int kTokens = 4 * kRowThreads;
   hipLaunchKernelGGL(vocab_rows_kernel, dim3((unsigned)((r.N + kTokens - 1) / kTokens)), dim3(kRowThreads), 0, st, r);
@@ -445,19 +531,26 @@ int launch_vocab_forward(const moe_config& c, const moe_vocab_dims& d, const Voc
   const long long N = (long long)c.G * c.S;
   const bool f32 = c.act_dtype == MOE_F32;
   const float inv_t = a.target != nullptr ? 1.f : 1.f / d.temperature;
-  const TeacherArgs t{a.idx, a.logit, d.K, d.V, inv_t};
+  const TeacherArgs t{a.idx, a.logit, a.target != nullptr ? 0 : d.K, d.V, inv_t};
   int rc = MOE_OK;
-  if (a.target == nullptr && (rc = launch_teacher(c, t, a.x, a.w, base, ws, a.entry_logit, st)) != MOE_OK) return rc;
   VocabRowArgs r = row_args(c, d, a, base, ws);
   r.loss = a.loss;
   r.lse = a.lse;
-  if ((rc = launch_rows(r, st)) != MOE_OK) return rc;
-  float2* const stats = reinterpret_cast<float2*>(base + ws.stats);
   const bool packs = !f32 && vocab_logits_on_tiles((int)N, d.V, c.M, true);
-  if (packs && (rc = launch_pack(c, a.x, base + ws.packed, r, st)) != MOE_OK) return rc;
+  // a row tile of the edge kernel takes as long whether all its tokens have a target or not: no need to number them
+  const bool few = N <= kFewTokens && !packs, all = few && a.target != nullptr && !f32;
+  if (few) {
+    if (!all) rc = launch_few(c, r, t, a, base, ws, a.entry_logit, nullptr, st);
+  } else {
+    if (a.target == nullptr) rc = launch_teacher(c, t, a.x, a.w, base, ws, a.entry_logit, st);
+    if (rc == MOE_OK) rc = launch_rows(r, st);
+    if (rc == MOE_OK && packs) rc = launch_pack(c, a.x, base + ws.packed, r, st);
+  }
+  if (rc != MOE_OK) return rc;
+  float2* const stats = reinterpret_cast<float2*>(base + ws.stats);
   GemmArgs g{packs ? base + ws.packed : a.x, a.w, nullptr};
-  g.gather = packs ? nullptr : r.perm;
-  g.kept = r.kept;
+  g.gather = packs || all ? nullptr : r.perm;
+  g.kept = all ? nullptr : r.kept;
   g.vocab.scale = kLog2e * inv_t;
   if (!f32) {
     g.vocab.stats = stats;
@@ -476,13 +569,20 @@ int launch_vocab_forward(const moe_config& c, const moe_vocab_dims& d, const Voc
     }
   }
   const int pieces = c.M * (f32 ? 4 : 2) / 16;
+  const bool single = N <= 1024;                               // a block per row where 16 rows each would not fill the units
   auto finish = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)((N + 15) / 16)), dim3(256), 0, st, stats, ws.slots, N, r.perm, r.kept,
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(single ? N : (N + 15) / 16)), dim3(256), 0, st, stats, ws.slots, N, r.perm, g.kept,
                        static_cast<const uint4*>(a.x), static_cast<const uint4*>(a.w), pieces, a.target, t,
                        reinterpret_cast<const float2*>(base + ws.tstat), a.entry_logit, a.loss, a.lse);
   };
-  if (a.target != nullptr) { if (f32) finish(vocab_finish_kernel<float, false>); else finish(vocab_finish_kernel<bf16_t, false>); }
-  else { if (f32) finish(vocab_finish_kernel<float, true>); else finish(vocab_finish_kernel<bf16_t, true>); }
+  auto finish_as = [&](auto one, auto many) { if (single) finish(one); else finish(many); };
+  if (a.target != nullptr) {
+    if (f32) finish_as(vocab_finish_kernel<float, false, 1>, vocab_finish_kernel<float, false, 16>);
+    else finish_as(vocab_finish_kernel<bf16_t, false, 1>, vocab_finish_kernel<bf16_t, false, 16>);
+  } else {
+    if (f32) finish_as(vocab_finish_kernel<float, true, 1>, vocab_finish_kernel<float, true, 16>);
+    else finish_as(vocab_finish_kernel<bf16_t, true, 1>, vocab_finish_kernel<bf16_t, true, 16>);
+  }
   return check_launch();
 }
 
@@ -495,9 +595,8 @@ int launch_vocab_backward(const moe_config& c, const moe_vocab_dims& d, const Vo
   const size_t elt = f32 ? 4 : 2;
   const int pieces = (int)(c.M * elt / 16);
   const float inv_t = a.target != nullptr ? 1.f : 1.f / d.temperature;
-  const TeacherArgs t{a.idx, a.logit, d.K, d.V, inv_t};
+  const TeacherArgs t{a.idx, a.logit, a.target != nullptr ? 0 : d.K, d.V, inv_t};
   int rc = MOE_OK;
-  if (a.target == nullptr && (rc = launch_teacher(c, t, a.x, a.w, base, ws, nullptr, st)) != MOE_OK) return rc;
   VocabRowArgs r = row_args(c, d, a, base, ws);
   r.pos = reinterpret_cast<int32_t*>(base + ws.pos);
   r.lse_in = a.lse;
@@ -518,8 +617,14 @@ int launch_vocab_backward(const moe_config& c, const moe_vocab_dims& d, const Vo
     r.dx_rows = (long long)ws.dx_plan.splits * N;
     r.dx_cost = kTilesDx;
   }
-  if ((rc = launch_rows(r, st)) != MOE_OK) return rc;
-  if ((rc = launch_pack(c, a.x, base + ws.packed, r, st)) != MOE_OK) return rc;
+  if (N <= kFewTokens) {
+    rc = launch_few(c, r, t, a, base, ws, nullptr, base + ws.packed, st);
+  } else {
+    if (a.target == nullptr) rc = launch_teacher(c, t, a.x, a.w, base, ws, nullptr, st);
+    if (rc == MOE_OK) rc = launch_rows(r, st);
+    if (rc == MOE_OK) rc = launch_pack(c, a.x, base + ws.packed, r, st);
+  }
+  if (rc != MOE_OK) return rc;
   for (int i = 0; i < pc.count; ++i) {
     const int first = i * pc.entries, n = d.V - first < pc.entries ? d.V - first : pc.entries;
     const char* const w = static_cast<const char*>(a.w) + (size_t)first * c.M * elt;
@@ -565,11 +670,13 @@ int launch_vocab_backward(const moe_config& c, const moe_vocab_dims& d, const Vo
     rc = f32 ? launch_gemm_f32(kWeightGrad, gw, 1, n, c.M, (int)N, st)  : launch_vocab_dw(gw, (int)N, n, c.M, st);
     if (rc != MOE_OK) return rc;
   }
+  const int parts = N * pieces < 65536 ? 8 : 1;
   auto out = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3(blocks_of(N * pieces)), dim3(256), 0, st, reinterpret_cast<const float4*>(base + ws.sums),
+    hipLaunchKernelGGL(kernel, dim3(blocks_of(N * pieces * parts)), dim3(256), 0, st, reinterpret_cast<const float4*>(base + ws.sums),
                        ws.dx_plan.splits, N, ranges ? r.kept : nullptr, r.pos, static_cast<uint4*>(a.dx), pieces);
   };
-  if (f32) out(vocab_dx_kernel<float>); else out(vocab_dx_kernel<bf16_t>);
+  if (f32) { if (parts == 1) out(vocab_dx_kernel<float, 1>); else out(vocab_dx_kernel<float, 8>); }
+  else { if (parts == 1) out(vocab_dx_kernel<bf16_t, 1>); else out(vocab_dx_kernel<bf16_t, 8>); }
   return check_launch();
 }
 

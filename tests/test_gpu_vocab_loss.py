@@ -108,7 +108,8 @@ def check(G, S, M, V, dtype, d, r, K=0, T=1.0):
 
 
 # G, S, M, V, dtype, share without a target, piece
-CE = [(1, 1, 8, 1, "bf16", 0, 0), (1, 1, 4, 1, "f32", 0, 0), (1, 1, 64, 2, "bf16", 0, 0), (1, 3, 40, 17, "bf16", 0, 0),
+CE = [(1, 64, 128, 900, "bf16", 0.5, 0), (1, 33, 72, 515, "f32", 0.5, 0), (5, 13, 256, 2100, "bf16", 0.2, 512), (2, 31, 64, 70, "bf16", 0.9, 0),
+      (1, 1, 8, 1, "bf16", 0, 0), (1, 1, 4, 1, "f32", 0, 0), (1, 1, 64, 2, "bf16", 0, 0), (1, 3, 40, 17, "bf16", 0, 0),
       (1, 3, 36, 17, "f32", 0, 0), (2, 65, 72, 257, "bf16", 0.3, 0), (2, 65, 68, 255, "f32", 0.3, 0), (1, 300, 264, 1000, "bf16", 0, 256),
       (3, 100, 520, 515, "bf16", 0.7, 256), (3, 100, 260, 515, "f32", 0.7, 256), (1, 1, 1024, 4001, "bf16", 0, 0),
       (1, 17, 512, 8193, "f32", 0.1, 0), (1, 1025, 128, 1031, "bf16", 0.5, 512), (1, 2049, 32, 300, "bf16", 0.05, 0),
@@ -127,7 +128,8 @@ def test_cross_entropy(G, S, M, V, dtype, empty, piece):
 
 
 # G, S, M, V, K, T, dtype, share without, piece
-KD = [(1, 1, 8, 1, 1, 1.0, "bf16", 0, 0), (1, 5, 40, 3, 9, 0.5, "bf16", 0, 0), (1, 5, 36, 33, 3, 2.0, "f32", 0.2, 0),
+KD = [(1, 64, 72, 300, 20, 2.0, "bf16", 0.5, 0), (5, 8, 132, 700, 3, 1.5, "f32", 0.4, 0), (1, 63, 256, 2048, 256, 1.0, "bf16", 0.1, 0),
+      (1, 1, 8, 1, 1, 1.0, "bf16", 0, 0), (1, 5, 40, 3, 9, 0.5, "bf16", 0, 0), (1, 5, 36, 33, 3, 2.0, "f32", 0.2, 0),
       (2, 65, 72, 257, 16, 2.0, "bf16", 0.3, 0), (1, 200, 136, 1500, 65, 3.0, "bf16", 0.1, 256), (1, 77, 68, 700, 256, 1.0, "f32", 0.1, 256),
       (1, 1, 1024, 4001, 31, 4.0, "bf16", 0, 0), (2, 1100, 256, 2999, 32, 2.0, "bf16", 0.1, 0)]
 
@@ -141,8 +143,8 @@ def test_distillation(G, S, M, V, K, T, dtype, empty, piece):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("K", [0, 5])
 def test_no_token_and_one_token_with_a_target(dtype, K):
-    G, S, M, V = 2, 700, 64, 777
-    for keep in ([], [1399], [0], [63, 64, 1023, 1024]):
+    for G, S, M, V, keep in [(2, 700, 64, 777, k) for k in ([], [1399], [0], [63, 64, 1023, 1024])] + \
+            [(1, 64, 72, 777, k) for k in ([], [63], [0], [5, 6])]:
         d = make(G, S, M, V, dtype, K=K)
         gone = torch.ones(G * S, dtype=torch.bool, device=DEV)
         gone[keep] = False
