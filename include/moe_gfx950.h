@@ -464,8 +464,8 @@ int moe_encoder_pair_backward(const moe_config* cfg, const moe_encoder_dims* dim
 typedef struct {
   int32_t V;           /* entries of the vocabulary, up to 2^23; tokens . V below 2^38, tokens below 2^24 */
   int32_t K;           /* moe_vocab_distill: entries per token, 1 .. 256; else not read */
-  int32_t piece;       /* entries of the vocabulary worked on at a time where a piece of dz (fp32: of z) is kept,
-                          rounded to whole 256; 0: as many as make 1 GiB, 4096 at least */
+  int32_t piece;       /* backward: entries of the vocabulary whose gradient dz is kept at a time, in whole 256;
+                          0: as many as make 1 GiB, 4096 at least */
   float temperature;   /* moe_vocab_distill: T > 0; else not read */
 } moe_vocab_dims;
 

@@ -281,7 +281,7 @@ int launch_gemm_bf16_f32out(bool transposed_a, const void* A, const void* B, flo
 enum GemmKind { kForward, kForwardRelu, kDataGrad, kDataGradMask, kWeightGrad };
 int launch_gemm_f32(GemmKind kind, const GemmArgs& a, int E, int R, int N, int K, hipStream_t st);
 
-// A vocabulary's products (fp32: launch_gemm_f32 with pitches) in bf16 (expert_gemm.hip): rows = the tokens, of which a.kept[0]
+// A vocabulary's products (fp32: launch_gemm_f32 with pitches, kDataGrad the logits) in bf16 (expert_gemm.hip): rows = the tokens, of which a.kept[0]
 // count, entries = those of a piece.  dz lies in rows of a multiple of 256 and holds zeros up to the next whole 16 bytes and in the
 // rows up to the next whole 64 (rows up to whole 256 exist).
 //   z = a.A[a.gather] . a.B^T: a.vocab.stats, or dz in a.C (rows of a.ldc)
@@ -292,6 +292,7 @@ int launch_vocab_logits(const GemmArgs& a, int rows, int entries, int M, hipStre
 struct VocabDxPlan { int splits, k; bool tiles; };     // ranges, length of each (the last may be shorter)
 VocabDxPlan vocab_dx_plan(int rows, int entries, int M);
 VocabDxPlan vocab_dx_plan_f32(int rows, int entries, int M);           // gemm_f32.hip
+int vocab_stat_slots_f32(int rows, int entries, int M);
 int launch_vocab_dx(const GemmArgs& a, const VocabDxPlan& p, int rows, int M, hipStream_t st);
 //   dw: C [entries, M] = A [rows, lda]^T . B [rows, M], which has rows of zeros like dz
 bool vocab_dw_on_tiles(int rows, int entries, int M);

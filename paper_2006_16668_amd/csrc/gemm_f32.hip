@@ -82,13 +82,14 @@ struct F32Smem {
 // of an expert (or, K_KEPT, the length of its sum).  PITCH: rows of A and C lie lda and ldc elements apart, where the dense
 // matrix has as many columns (a piece of a vocabulary, whose number of entries is any), and kept[0] rows of A and C count, or
 // terms of the sum with row-of-k operands.  Then "expert" e of A [R,lda] . B [k_total,N] sums the k from e K on, `add`: to
-// what C [e,R,N] holds.
+// what C [e,R,N] holds.  EPI 3 and 4, of the logits A . B^T: C is the gradient with respect to them, with zeros up to the next whole
+// 16 bytes, or nothing is stored but the maximum and sum of exponentials of each row's columns of a wavefront tile (VocabRows).
 template <int TM, int TN, int PD, int KG, int EPI, bool A_KC, bool B_KC, bool K_KEPT, bool PITCH>
 __global__ __launch_bounds__(256 * KG, TM * TN >= 4 ? 2 : TM * TN >= 2 ? 3 : 4) void gemm_f32_mfma_kernel(
     const float* __restrict__ A, const float* __restrict__ B, float* __restrict__ Cout,
     const float* __restrict__ mask, int R, int N, int K, int tiles_r, int tiles_n,
     const int32_t* __restrict__ gather, const int32_t* __restrict__ kept, int lda_arg, int ldc_arg, int k_total,
-    int add) {
+    int add, VocabRows vocab) {
   const int lda = PITCH ? lda_arg : A_KC ? K : R, ldc = PITCH ? ldc_arg : N;
   constexpr bool SUMS = PITCH && A_KC && !B_KC;
   using PA = F32Plane<TM, A_KC>;
@@ -340,11 +341,27 @@ __global__ __launch_bounds__(256 * KG, TM * TN >= 4 ? 2 : TM * TN >= 2 ? 3 : 4) 
           for (int v = 0; v < 16; ++v) main[i][j][v] += sums[g * (TM * TN * 4096) + ((i * TN + j) * 16 + v) * 64];
   }
 
+  // EPI 3: what a tile needs of its rows, one of which each lane fetches (a row's own fetch for every result took 45 us more than the
+  // 140 of 1350 rows, M 512, V 16001)
+  float row_lse = 0.f, row_up = 0.f, row_value = 0.f;
+  int row_hit = -1;
+  if constexpr (EPI == 3) {
+    const int row = r0 + wm0 + (lane & (32 * TM - 1)), at = row < rows ? row : rows - 1;
+    row_lse = vocab.lse2[at];
+    row_up = vocab.grad[at];
+    if (vocab.hit != nullptr) { row_hit = vocab.hit[at] - vocab.first; row_value = vocab.hit_value[at]; }
+  }
+  auto of_row = [&](auto of_lane, int row) {                   // row of the lower half, row + 4 of the upper
+    const int bits = __builtin_bit_cast(int, of_lane);
+    const int lo = __builtin_amdgcn_readlane(bits, row), hi = __builtin_amdgcn_readlane(bits, row + 4);
+    return __builtin_bit_cast(decltype(of_lane), hf != 0 ? hi : lo);
+  };
+
   // c[v] of the wavefront's 32 x 32 tile (i, j): row 32 i + 8 (v/4) + 4 hf + v%4, column 32 j + lane%32: a
   // store covers whole 128-byte pieces of two rows
   auto store_tile = [&](int i, int j, const f32x16_t& c, const f32x16_t& m) {
     const int n = n0 + wn0 + 32 * j + l32, rb = r0 + wm0 + 32 * i + 4 * hf;
-    if (n >= N) return;
+    if (n >= (EPI == 3 ? (N + 3) / 4 * 4 : N)) return;
     const size_t o = ((size_t)e * R + rb) * ldc + n;
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
@@ -352,6 +369,12 @@ __global__ __launch_bounds__(256 * KG, TM * TN >= 4 ? 2 : TM * TN >= 2 ? 3 : 4) 
       float x = c[v];
       if (EPI == 1) x = fmaxf(x, 0.f);
       if (EPI == 2) x = m[v] > 0.f ? x : 0.f;
+      if (EPI == 3) {
+        const int at = 32 * i + dr;                            // of the half's row
+        x = __builtin_amdgcn_exp2f(fmaf(x, vocab.scale, -of_row(row_lse, at))) * of_row(row_up, at);
+        if (of_row(row_hit, at) == n) x = of_row(row_value, at);
+        if (n >= N) x = 0.f;
+      }
       if (rb + dr < rows) {
         if (SUMS && add) x += Cout[o + (size_t)dr * ldc];
         Cout[o + (size_t)dr * ldc] = x;
@@ -454,6 +477,37 @@ __global__ __launch_bounds__(256 * KG, TM * TN >= 4 ? 2 : TM * TN >= 2 ? 3 : 4) 
         main[i][j][v] *= kDown;
       }
   if (__builtin_amdgcn_ballot_w64(!(zero == 0.f)) != 0) fp32_products(main);
+  if constexpr (EPI == 4) {
+    // a row's columns of the wavefront tile lie in the 32 lanes of a half
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+      if (n0 + wn0 + 32 * j + l32 >= N) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) main[i][j][v] = -INFINITY;
+      }
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        float mx = main[i][0][v];
+#pragma unroll
+        for (int j = 1; j < TN; ++j) mx = fmaxf(mx, main[i][j][v]);
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
+        mx *= vocab.scale;
+        const float at = fabsf(mx) == INFINITY ? 0.f : mx;
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) sum += __builtin_amdgcn_exp2f(fmaf(main[i][j][v], vocab.scale, -at));
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) sum += __shfl_xor(sum, o, 64);
+        const int row = r0 + wm0 + 32 * i + 8 * (v >> 2) + 4 * hf + (v & 3);
+        if (l32 == 0 && row < rows) vocab.stats[(size_t)(2 * ct + (wave & 1)) * R + row] = float2{mx == INFINITY ? 0.f : mx, sum};
+      }
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -479,7 +533,7 @@ int launch_tiles(const GemmArgs& a, int E, int R, int N, int K, hipStream_t st) 
                      dim3(256 * KG), kLds, st, static_cast<const float*>(a.A), static_cast<const float*>(a.B),
                      static_cast<float*>(a.C), static_cast<const float*>(a.mask), R, N, K, tiles_r,
                      tiles_n, a.gather, a.kept, a.lda != 0 ? a.lda : A_KC ? K : R, a.ldc != 0 ? a.ldc : N,
-                     a.k_total, a.add);
+                     a.k_total, a.add, a.vocab);
   return check_launch();
 }
 
@@ -491,6 +545,7 @@ int launch_tiles(const GemmArgs& a, int E, int R, int N, int K, hipStream_t st) 
 //   E 3  R 64  M 1024 H 4096  112 / 89 / 77 / 136 / 206    E 16 R 128 M 512 H 1024    47 / 44 / 45 / 51 / 73
 //   E 66 R 12  M 848  H 3424  393 / 403 / 438 / 341 / 523  E 40 R 100 M 600 H 1500  169 / 184 / 224 / 148 / 142
 //   E 16 R 512 M 1024 H 2048  543 / 567 / 628 / 469 / 426  E 2  R 300 M 512 H 2048    67 / 56 / 56 / 75 / 109
+constexpr int kPlanUnits = 256;          // where the form sizes a workspace: those of a whole device
 enum F32Form { k64x64, k64x64x2, k64x64x4, k64x128, k128x128 };
 F32Form f32_form(int E, int R, int N, int K, int cus, double* time = nullptr) {
   static const double t64[] = {425, 635, 915, 1230}, t64x2[] = {375, 615}, t64x4[] = {345}, t64x128[] = {590, 990, 1550},
@@ -517,7 +572,7 @@ template <int EPI, bool A_KC, bool B_KC, bool K_KEPT = false, bool PITCH = false
 int launch_form(const GemmArgs& a, int E, int R, int N, int K, hipStream_t st) {
   int cus = 0;
   if (compute_units(&cus) != MOE_OK) return MOE_EHIP;
-  switch (f32_form(E, R, N, K, cus)) {
+  switch (f32_form(E, R, N, K, EPI == 4 ? kPlanUnits : cus)) {
     case k64x64: return launch_tiles<1, 1, 4, 1, EPI, A_KC, B_KC, K_KEPT, PITCH>(a, E, R, N, K, st);
     case k64x64x2: return launch_tiles<1, 1, 2, 2, EPI, A_KC, B_KC, K_KEPT, PITCH>(a, E, R, N, K, st);
     case k64x64x4: return launch_tiles<1, 1, 2, 4, EPI, A_KC, B_KC, K_KEPT, PITCH>(a, E, R, N, K, st);
@@ -536,7 +591,7 @@ int prepare_gemm_f32() {
       prepare_tiles<2, 2, 2, 1, __VA_ARGS__>()
       MOE_F32_ALL(0, true, false, false), MOE_F32_ALL(1, true, false, false), MOE_F32_ALL(0, true, true, false),
       MOE_F32_ALL(2, true, true, false), MOE_F32_ALL(0, false, false, true), MOE_F32_ALL(0, false, false, false),
-      MOE_F32_ALL(0, true, true, false, true), MOE_F32_ALL(0, true, false, false, true),
+      MOE_F32_ALL(3, true, true, false, true), MOE_F32_ALL(4, true, true, false, true), MOE_F32_ALL(0, true, false, false, true),
       MOE_F32_ALL(0, false, false, true, true)};
 #undef MOE_F32_ALL
   for (int rc : rcs)
@@ -544,8 +599,13 @@ int prepare_gemm_f32() {
   return MOE_OK;
 }
 
+int vocab_stat_slots_f32(int rows, int entries, int M) {
+  const F32Form f = f32_form(1, rows, entries, M, kPlanUnits);
+  const int bn = f == k64x128 || f == k128x128 ? 128 : 64;
+  return 2 * ((entries + bn - 1) / bn);
+}
+
 VocabDxPlan vocab_dx_plan_f32(int rows, int entries, int M) {
-  constexpr int kPlanUnits = 256;                              // (sizes a workspace: of a whole device)
   VocabDxPlan best{1, (entries + 63) / 64 * 64, false};
   double best_us = 0;
   for (int want = 1; want <= 64; ++want) {
@@ -553,18 +613,20 @@ VocabDxPlan vocab_dx_plan_f32(int rows, int entries, int M) {
     if (want > 1 && (k < 256 || sp < want)) continue;
     double us = 0;
     f32_form(sp, rows, M, k, kPlanUnits, &us);
-    us += 1e-6 * 8 * sp * rows * M / 5.0;                      // written and read once more, us at 5 TB/s
+    us += 1e-6 * 5 * sp * rows * M / 5.0;                      // written, half behind the products, and read, us at 5 TB/s
     if (want == 1 || us < best_us) { best_us = us; best = VocabDxPlan{sp, k, false}; }
   }
   return best;
 }
 
 int launch_gemm_f32(GemmKind kind, const GemmArgs& a, int E, int R, int N, int K, hipStream_t st) {
-  if (a.lda != 0 || a.ldc != 0) {
+  if (a.lda != 0 || a.ldc != 0 || a.vocab.stats != nullptr) {
     // pitches in whole 16-byte pieces; what A's rows hold up to the next whole piece is multiplied by zeros, so is finite.
-    // Rows of A (kWeightGrad), columns of C (kDataGrad) and the sum (kForward) of any number.
+    // Rows of A (kWeightGrad), columns of C (kDataGrad: a vocabulary's logits) and the sum (kForward) of any number.
     if (E < 1 || R < 1 || N < 1 || K < 1 || a.lda % 4 != 0 || a.ldc % 4 != 0 || a.kept == nullptr) return MOE_EUNSUPPORTED;
-    if (kind == kDataGrad && K % 4 == 0 && E == 1) return launch_form<0, true, true, false, true>(a, E, R, N, K, st);
+    if (kind == kDataGrad && K % 4 == 0 && E == 1)
+      return a.vocab.stats != nullptr ? launch_form<4, true, true, false, true>(a, E, R, N, K, st)
+                                      : launch_form<3, true, true, false, true>(a, E, R, N, K, st);
     if (kind == kForward && N % 4 == 0 && K % 4 == 0) return launch_form<0, true, false, false, true>(a, E, R, N, K, st);
     if (kind == kWeightGrad && N % 4 == 0 && E == 1) return launch_form<0, false, false, true, true>(a, E, R, N, K, st);
     return MOE_EUNSUPPORTED;

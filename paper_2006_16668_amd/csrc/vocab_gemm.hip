@@ -23,6 +23,7 @@
 // LDS, bank conflicts: a K-contiguous piece is [128 rows][8 chunks of 8 k], chunk c of row r at c ^ ((r >> 1) & 7); a row-of-k
 // piece is [64 k][16 chunks of 8 columns], chunk c of row k at c ^ 4 (k & 3), read transposing.
 #include <math.h>
+#include <type_traits>
 #include "common.h"
 
 namespace moe {
@@ -242,8 +243,10 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
     to_other = -to_other;
   };
   f32x16_t acc[4][2];
-  // one turn of the matrix pipe: between two barriers, what was fetched before the first of them
-  auto turn = [&](int h, int j) __attribute__((always_inline)) {
+  // one turn of the matrix pipe: between two barriers, what was fetched before the first of them.  A tile's first step starts
+  // from an operand of zeros: 128 registers need no clearing.
+  const f32x16_t zeros = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  auto turn = [&](auto first, int h, int j) __attribute__((always_inline)) {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
@@ -253,7 +256,8 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
     for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
       for (int i = 0; i < 2; ++i)
-        acc[2 * h + i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[j][kk], a[h][i][kk], acc[2 * h + i][j], 0, 0, 0);
+        acc[2 * h + i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[j][kk], a[h][i][kk],
+                                                                    decltype(first)::value && kk == 0 ? zeros : acc[2 * h + i][j], 0, 0, 0);
     __builtin_amdgcn_s_setprio(0);
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("" ::: "memory");
@@ -262,8 +266,7 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
     __builtin_amdgcn_sched_barrier(0);
   };
 
-  // Start: step 0, and B and A0 of step 1, as a step finds them.  `ahead`: steps whose copies have been started
-  // (all but A1 of the last).
+  // Start: step 0, and B and A0 of step 1, as a step finds them
   int steps_left = 0;                                          // of all this block's tiles, to know which steps exist
   for (int t = first; t < t_end; t += stride) {
     int e, rt, ct;
@@ -283,19 +286,11 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
     tile_at(tile, e, rt, ct);
     const int m0 = rt * 256, n0 = ct * 256;
     const int steps = (range_k(e) + 63) >> 6;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-    if (steps > 0) read_a(0);                                  // (after the last tile's stores: they need the registers)
-#pragma unroll 1
-    for (int kt = 0; kt < steps; ++kt, --steps_left) {
-      const bool landed = kt == 0 && tile != first;            // what this step waits for: before the last tile's stores
+    auto step = [&](auto first_step, int kt) __attribute__((always_inline)) {
+      const bool landed = decltype(first_step)::value && tile != first;        // what it waits for: before the last tile's stores
       // phase 1
       read_b(0);
-      turn(0, 0);
+      turn(first_step, 0, 0);
       // phase 2; A1 of this step must have landed (younger: B and A0 of the next).  A1 of the next step is started here and not
       // before: its place is where the last tile's results passed through.
       read_b(1);
@@ -305,18 +300,30 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
       }
       copy_a(1);
       advance();
-      turn(0, 1);
+      turn(first_step, 0, 1);
       // phase 3; B and A0 of the next step (younger: its A1)
       read_a(1);
       if (!landed) asm volatile("s_waitcnt vmcnt(2)" ::: "memory");
-      if (EPI == kLogitGrad && kt == 0) copy_row_data(m0);
+      if (EPI == kLogitGrad && decltype(first_step)::value) copy_row_data(m0);
       copy_b();
-      turn(1, 1);
+      turn(first_step, 1, 1);
       // phase 4
       other_stage();
       if (kt + 1 < steps) read_a(0);
       copy_a(0);
-      turn(1, 0);
+      turn(first_step, 1, 0);
+      --steps_left;
+    };
+    if (steps > 0) {
+      read_a(0);                                               // (after the last tile's stores: they need the registers)
+      step(std::true_type{}, 0);
+#pragma unroll 1
+      for (int kt = 1; kt < steps; ++kt) step(std::false_type{}, kt);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[i][j] = zeros;
     }
 
     // acc[2 h + i][j][4 q + r] = C[128 h + 64 wm + 32 i + r32][col(j) + 8 q + 4 hh + r] of the tile.  A wavefront's columns lie

@@ -8,10 +8,9 @@
 //                   dz[n,v] = g_n / T (exp(z[n,v] / T - lse_n) - sum_{k: i_k = v} q_k)
 //   both            dx = dz . w,  dw = dz^T . x
 //
-// The logits are never kept.  bf16: the forward product leaves of every row and wavefront tile the maximum and the sum of
-// exponentials (8 bytes for 32 to 128 logits), the backward pass multiplies again and keeps one piece of the vocabulary's dz,
-// rounded to bf16 once, as the upstream gradients of the expert layers are, for the two products that read it.  fp32: a piece
-// of the logits is multiplied into memory and read once (forward), turned into dz in place (backward).
+// The logits are never kept: the forward product leaves of every row and wavefront tile the maximum and the sum of exponentials
+// (8 bytes for 32 to 256 logits), the backward pass multiplies again and keeps one piece of the vocabulary's dz for the two
+// products that read it, in bf16 rounded once, as the upstream gradients of the expert layers are.
 //
 // Tokens without a target (padding, prompts) are left out of every product: the rows that have one are numbered first
 // (vocab_rows_kernel), so neither their work nor what their x holds, NaN included, reaches anything.
@@ -305,44 +304,6 @@ __global__ __launch_bounds__(256) void vocab_finish_kernel(const float2* __restr
   if (r == 0) { loss[n] = out; lse[n] = l; }
 }
 
-// ---------------------------------------------------------------- fp32: passes over a piece of the logits
-// z [rows, ld]: a block per packed row leaves the maximum and sum of its `entries` logits.
-__global__ __launch_bounds__(256) void vocab_stats_f32_kernel(const float* __restrict__ z, int ld, int entries, float scale,
-                                                              const int32_t* __restrict__ kept, float2* __restrict__ stats) {
-  if ((int)blockIdx.x >= kept[0]) return;
-  const float* row = z + (size_t)blockIdx.x * ld;
-  const int lane = threadIdx.x & 63;
-  float mx = -INFINITY;
-  for (int v = threadIdx.x; v < entries; v += 256) mx = fmaxf(mx, row[v]);
-  __shared__ float red[8];
-  mx = wave_max(mx);
-  if (lane == 0) red[threadIdx.x >> 6] = mx;
-  __syncthreads();
-  mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])) * scale;
-  const float m = fabsf(mx) == INFINITY ? 0.f : mx;
-  float s = 0.f;
-  for (int v = threadIdx.x; v < entries; v += 256) s += __builtin_amdgcn_exp2f(fmaf(row[v], scale, -m));
-  s = wave_sum(s);
-  if (lane == 0) red[4 + (threadIdx.x >> 6)] = s;
-  __syncthreads();
-  if (threadIdx.x == 0)
-    stats[blockIdx.x] = float2{mx == INFINITY ? 0.f : mx, (red[4] + red[5]) + (red[6] + red[7])};
-}
-// z -> dz in place, zeros up to the next whole 16 bytes
-__global__ __launch_bounds__(256) void vocab_grad_f32_kernel(float* __restrict__ z, int ld, int entries, VocabRows a,
-                                                             const int32_t* __restrict__ kept) {
-  const int p = blockIdx.x;
-  if (p >= kept[0]) return;
-  float* row = z + (size_t)p * ld;
-  const float lse = a.lse2[p], g = a.grad[p];
-  const int hit = a.hit != nullptr ? a.hit[p] - a.first : -1;
-  for (int v = threadIdx.x; v < (entries + 3) / 4 * 4; v += 256) {
-    float d = v < entries ? __builtin_amdgcn_exp2f(fmaf(row[v], a.scale, -lse)) * g : 0.f;
-    if (v == hit) d = a.hit_value[p];
-    row[v] = d;
-  }
-}
-
 // ---------------------------------------------------------------- dz at the teacher's entries
 // One wavefront per packed row: (exp(z/T - lse) - the q of all its entries with that index) g/T, at the entries of this piece.
 template <typename T>
@@ -456,10 +417,9 @@ VocabWs carve_vocab(const moe_config& c, const moe_vocab_dims& d, bool teacher, 
   w.tstat = take(teacher ? N * 8 : 0);
   w.has = take(teacher ? N * 4 : 0);
   if (!backward) {
-    w.slots = c.act_dtype == MOE_F32 ? p.count : vocab_stat_slots((int)N, d.V, c.M);
+    w.slots = c.act_dtype == MOE_F32 ? vocab_stat_slots_f32((int)N, d.V, c.M) : vocab_stat_slots((int)N, d.V, c.M);
     w.packed = take(packs ? whole * c.M * elt : 0);
     w.stats = take((size_t)w.slots * N * 8);
-    w.dz = take(c.act_dtype == MOE_F32 ? N * p.entries * 4 : 0);
   } else {
     w.pos = take(N * 4);
     w.lse2 = take(N * 4);
@@ -527,7 +487,6 @@ static int launch_pack(const moe_config& c, const void* x, void* packed, const V
 int launch_vocab_forward(const moe_config& c, const moe_vocab_dims& d, const VocabCall& a, void* base_, hipStream_t st) {
   char* const base = static_cast<char*>(base_);
   const VocabWs ws = carve_vocab(c, d, a.target == nullptr, false);
-  const VocabPieces pc = vocab_pieces(c, d);
   const long long N = (long long)c.G * c.S;
   const bool f32 = c.act_dtype == MOE_F32;
   const float inv_t = a.target != nullptr ? 1.f : 1.f / d.temperature;
@@ -552,22 +511,9 @@ int launch_vocab_forward(const moe_config& c, const moe_vocab_dims& d, const Voc
   g.gather = packs || all ? nullptr : r.perm;
   g.kept = all ? nullptr : r.kept;
   g.vocab.scale = kLog2e * inv_t;
-  if (!f32) {
-    g.vocab.stats = stats;
-    if ((rc = launch_vocab_logits(g, (int)N, d.V, c.M, st)) != MOE_OK) return rc;
-  } else {
-    float* const z = reinterpret_cast<float*>(base + ws.dz);
-    for (int i = 0; i < pc.count; ++i) {
-      const int first = i * pc.entries, n = d.V - first < pc.entries ? d.V - first : pc.entries;
-      g.B = static_cast<const float*>(a.w) + (size_t)first * c.M;
-      g.C = z;
-      g.ldc = pc.entries;
-      if ((rc = launch_gemm_f32(kDataGrad, g, 1, (int)N, n, c.M, st)) != MOE_OK) return rc;
-      hipLaunchKernelGGL(vocab_stats_f32_kernel, dim3((unsigned)N), dim3(256), 0, st, z, pc.entries, n, g.vocab.scale, r.kept,
-                         stats + (size_t)i * N);
-      if ((rc = check_launch()) != MOE_OK) return rc;
-    }
-  }
+  g.vocab.stats = stats;
+  rc = f32 ? launch_gemm_f32(kDataGrad, g, 1, (int)N, d.V, c.M, st) : launch_vocab_logits(g, (int)N, d.V, c.M, st);
+  if (rc != MOE_OK) return rc;
   const int pieces = c.M * (f32 ? 4 : 2) / 16;
   const bool single = N <= 1024;                               // a block per row where 16 rows each would not fill the units
   auto finish = [&](auto kernel) {
@@ -637,14 +583,7 @@ int launch_vocab_backward(const moe_config& c, const moe_vocab_dims& d, const Vo
     z.vocab.hit = r.hit;
     z.vocab.hit_value = r.hit_value;
     z.vocab.first = first;
-    if (f32) {
-      if ((rc = launch_gemm_f32(kDataGrad, z, 1, (int)N, n, c.M, st)) != MOE_OK) return rc;
-      hipLaunchKernelGGL(vocab_grad_f32_kernel, dim3((unsigned)N), dim3(256), 0, st, static_cast<float*>(z.C), pc.entries, n,
-                         z.vocab, r.kept);
-      rc = check_launch();
-    } else {
-      rc = launch_vocab_logits(z, (int)N, n, c.M, st);
-    }
+    rc = f32 ? launch_gemm_f32(kDataGrad, z, 1, (int)N, n, c.M, st) : launch_vocab_logits(z, (int)N, n, c.M, st);
     if (rc != MOE_OK) return rc;
     if (a.target == nullptr) {
       auto entries = [&](auto kernel, auto* dz) {
