@@ -160,6 +160,12 @@ struct VocabRows {
   const int32_t* hit = nullptr;        // NULL, or the entry whose gradient is hit_value instead
   const float* hit_value = nullptr;
   int first = 0;                       // entry of the product's first column
+  // NULL, or a teacher's entries by 256 x 256 tiles: where a tile's start (row tiles of 256 K, column tiles + 1), each its row << 8 |
+  // column in the tile and its place in entry_logit, which receives its logit
+  const int32_t* starts = nullptr;
+  const uint2* sorted = nullptr;
+  float* entry_logit = nullptr;
+  int K = 0;
 };
 struct GemmArgs {
   const void *A, *B;
@@ -323,7 +329,7 @@ int launch_vocab_tiles_dw(const GemmArgs& a, int entries, int M, hipStream_t st)
 struct VocabPieces { int entries, count; };    // of the vocabulary; a piece's entries are whole 256, the last may have fewer
 VocabPieces vocab_pieces(const moe_config& c, const moe_vocab_dims& d);
 struct VocabWs {
-  size_t kept, perm, tstat, has, stats, pos, lse2, grad, hit, hit_value, packed, dz, sums, total;
+  size_t kept, perm, tstat, has, stats, starts, sorted, pos, lse2, grad, hit, hit_value, packed, dz, sums, total;
   int slots;                           // of stats
   VocabDxPlan dx_plan;                 // of a whole piece
 };

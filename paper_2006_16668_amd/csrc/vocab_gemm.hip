@@ -39,7 +39,7 @@ typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 constexpr int kXcds = 8;
 constexpr uint32_t kPiece = 16384, kStage = 4 * kPiece, kStaging = 2 * kStage;
 constexpr uint32_t kRowData = kStaging + 8 * 2048;             // lse2, grad, hit, hit_value of a tile's rows (kLogitGrad)
-constexpr uint32_t kSmem = kRowData + 4 * 1024;
+constexpr uint32_t kSmem = kStaging + 8 * 4096;                // all 160 KB (kStats: 4 KB of staging per wavefront)
 
 static __device__ const u32x4_t vocab_zero_line = {0u, 0u, 0u, 0u};
 
@@ -191,16 +191,15 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
     }
   };
 
+#define MOE_VG_WORDS(LDS, P)                                                                   \
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(LDS), "v"((uint64_t)(uintptr_t)(P)) : "memory")
   // kLogitGrad: what the tile's epilogue needs of its rows, 64 of them per wavefront.  Started in the tile's first step, when
   // all have left the last tile's epilogue, and landed with what the second step waits for (sums have two steps at least).
   auto copy_row_data = [&](int m0) __attribute__((always_inline)) {
     const int row = m0 + 64 * wn + lane_here(), at = row < R ? row : R - 1;
     const uint32_t to = lds0 + kRowData + wm * 1024 + wn * 256;
-#define MOE_VG_ROWS(LDS, P) \
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(LDS), "v"((uint64_t)(uintptr_t)(P)) : "memory")
-    MOE_VG_ROWS(to, (wm == 0 ? g.v.lse2 : g.v.grad) + at);
-    if (g.v.hit != nullptr) MOE_VG_ROWS(to + 2048, (wm == 0 ? reinterpret_cast<const float*>(g.v.hit) : g.v.hit_value) + at);
-#undef MOE_VG_ROWS
+    MOE_VG_WORDS(to, (wm == 0 ? g.v.lse2 : g.v.grad) + at);
+    if (g.v.hit != nullptr) MOE_VG_WORDS(to + 2048, (wm == 0 ? reinterpret_cast<const float*>(g.v.hit) : g.v.hit_value) + at);
   };
 
   // ---- fragments
@@ -286,6 +285,11 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
     tile_at(tile, e, rt, ct);
     const int m0 = rt * 256, n0 = ct * 256;
     const int steps = (range_k(e) + 63) >> 6;
+    // kStats: the tile's teacher entries.  Where they are is asked in its first step, the first 64 of them are copied, as 128 words,
+    // to A1's place in the last one (read by all when phase 4 begins, free until the next tile's phase 2).
+    int entries = 0;
+    const uint2* list = nullptr;
+    uint32_t list_at = 0;
     auto step = [&](auto first_step, int kt) __attribute__((always_inline)) {
       const bool landed = decltype(first_step)::value && tile != first;        // what it waits for: before the last tile's stores
       // phase 1
@@ -305,9 +309,22 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
       read_a(1);
       if (!landed) asm volatile("s_waitcnt vmcnt(2)" ::: "memory");
       if (EPI == kLogitGrad && decltype(first_step)::value) copy_row_data(m0);
+      if (EPI == kStats && decltype(first_step)::value && g.v.starts != nullptr) {
+        typedef const int __attribute__((address_space(4))) * scalar_ptr;
+        const scalar_ptr start = (scalar_ptr)(uintptr_t)(g.v.starts + (size_t)rt * (tiles_n + 1) + ct);
+        const int found = start[0];
+        entries = start[1] - found;
+        list = g.v.sorted + (size_t)m0 * g.v.K + found;
+      }
       copy_b();
       turn(first_step, 1, 1);
       // phase 4
+      if (EPI == kStats && kt + 1 == steps && entries > 0) {
+        list_at = lds0 + (to_other == kStage ? 0 : kStage) + kPiece + wave * 2048;
+        const uint32_t* const from = reinterpret_cast<const uint32_t*>(list) + lane_here();
+        MOE_VG_WORDS(list_at, from);
+        MOE_VG_WORDS(list_at + 256, from + 64);
+      }
       other_stage();
       if (kt + 1 < steps) read_a(0);
       copy_a(0);
@@ -333,9 +350,42 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
     const int lane = lane_here(), r32 = lane & 31, hh = lane >> 5;
     auto col_of = [&](int j) { return B_MNC ? 128 * j + 32 * wn : 64 * wn + 32 * j; };
     if constexpr (EPI == kStats) {
+      // Logits at a teacher's entries: of each 32 x 32 part that has any of the 64 at hand, its results pass through LDS (the
+      // register that holds an entry's differs from lane to lane).
+      for (int at = 0; at < entries; at += 64) {
+        uint2 entry = {0xffffffffu, 0u};
+        if (at + lane < entries) {
+          if (at == 0) {
+            const u32x2_t e = *(lds_u2_ptr)(uintptr_t)(list_at + 8 * lane);
+            entry = uint2{e[0], e[1]};
+          } else {
+            entry = list[at + lane];
+          }
+        }
+        const uint32_t row = entry.x >> 8, col = entry.x & 255;
+        const bool mine = (int)entry.x >= 0 && (int)((row >> 6) & 1) == wm && (int)(col >> 6) == wn;
+        const int part = (int)(4 * (row >> 7) + 2 * ((row >> 5) & 1) + ((col >> 5) & 1));
+        const uint32_t st = lds0 + kStaging + wave * 4096;
+        const uint32_t from = st + ((col >> 3) & 3) * 1024 + ((row & 31) + 32 * ((col >> 2) & 1)) * 16 + (col & 3) * 4;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const bool here = mine && part == 2 * i + j;
+            if (__builtin_amdgcn_ballot_w64(here) == 0) continue;
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              *(lds_u4_ptr)(uintptr_t)(st + q * 1024 + lane * 16) =
+                  u32x4_t{__float_as_uint(acc[i][j][4 * q]), __float_as_uint(acc[i][j][4 * q + 1]),
+                          __float_as_uint(acc[i][j][4 * q + 2]), __float_as_uint(acc[i][j][4 * q + 3])};
+            __builtin_amdgcn_wave_barrier();
+            if (here) g.v.entry_logit[entry.y] = *(lds_f_ptr)(uintptr_t)from;
+            __builtin_amdgcn_wave_barrier();
+          }
+      }
       const float c = g.v.scale;
       const int left = g.N - n0 - 64 * wn - 4 * hh;
-      const uint32_t mine = lds0 + kStaging + wave * 1024;     // (maximum, sum) of 128 rows
+      const uint32_t mine = lds0 + kStaging + wave * 4096;     // (maximum, sum) of 128 rows
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float mx = -INFINITY;
@@ -365,12 +415,12 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      const uint32_t at = lds0 + kStaging + 4 * wm * 1024 + (32 * wn + r32) * 8;
+      const uint32_t at = lds0 + kStaging + 4 * wm * 4096 + (32 * wn + r32) * 8;
       float m = -INFINITY, s = 0.f;
       u32x2_t o[4];
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        o[w] = *(lds_u2_ptr)(uintptr_t)(at + w * 1024);
+        o[w] = *(lds_u2_ptr)(uintptr_t)(at + w * 4096);
         m = fmaxf(m, __uint_as_float(o[w][0]));
       }
       const float base = m == -INFINITY ? 0.f : m;
@@ -453,6 +503,7 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
   if (wm == 0) __builtin_amdgcn_s_barrier();                   // the half phase
 #undef MOE_VG_COPY
 #undef MOE_VG_COPY_AT
+#undef MOE_VG_WORDS
 }
 
 template <int EPI, bool TAIL>

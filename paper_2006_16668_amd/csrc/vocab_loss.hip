@@ -181,8 +181,8 @@ __device__ __forceinline__ void entry_logits(const TeacherArgs& t, long long n, 
     if (l == 0 && k < t.K) z[n * t.K + k] = ok ? d : 0.f;
   }
 }
-// one wavefront per token; z may be NULL
-template <typename T>
+// one wavefront per token; z may be NULL.  SORTED: the logits of the entries that are there come from the product (vocab_sort_kernel)
+template <typename T, bool SORTED>
 __global__ __launch_bounds__(256) void vocab_teacher_kernel(TeacherArgs t, const uint4* __restrict__ x,
                                                             const uint4* __restrict__ w, int pieces, long long N,
                                                             float2* __restrict__ stat, int32_t* __restrict__ has,
@@ -192,8 +192,63 @@ __global__ __launch_bounds__(256) void vocab_teacher_kernel(TeacherArgs t, const
   float2 s;
   const bool any = teacher_stat(t, n, &s);
   if ((threadIdx.x & 63) == 0) { stat[n] = s; has[n] = any; }
-  if (z != nullptr) entry_logits<T>(t, n, x, w, pieces, z, (threadIdx.x >> 4) & 3, 4);
+  if (SORTED) {
+    for (int k = threadIdx.x & 63; k < t.K; k += 64)
+      if (!teacher_has(t, t.idx[n * t.K + k], t.logit[n * t.K + k])) z[n * t.K + k] = 0.f;
+  } else if (z != nullptr) {
+    entry_logits<T>(t, n, x, w, pieces, z, (threadIdx.x >> 4) & 3, 4);
+  }
 }
+// The entries of the packed rows in the order of the product's 256 x 256 tiles, so that each tile finds its own (a handful, where
+// their dot products one by one would read a row of w each: 8192 tokens, M 1024, 32 entries 86 us).  A block per row tile; the
+// entries of a tile come in no fixed order, which no result depends on.
+__global__ __launch_bounds__(1024) void vocab_sort_kernel(TeacherArgs t, const int32_t* __restrict__ perm,
+                                                          const int32_t* __restrict__ kept, int tiles_n,
+                                                          int32_t* __restrict__ starts, uint2* __restrict__ sorted) {
+  extern __shared__ int place[];                               // [tiles_n] counts, then where the next entry goes
+  __shared__ int sums[16];
+  const int p0 = blockIdx.x * 256, rows = kept[0], tid = threadIdx.x, lane = tid & 63;
+  if (p0 >= rows) return;
+  const int entries = (rows - p0 < 256 ? rows - p0 : 256) * t.K;
+  for (int i = tid; i < tiles_n; i += 1024) place[i] = 0;
+  __syncthreads();
+  auto each = [&](auto take) {
+    for (int e = tid; e < entries; e += 1024) {
+      const int r = e / t.K, k = e - r * t.K;
+      const long long at = (long long)perm[p0 + r] * t.K + k;
+      const int32_t i = t.idx[at];
+      if (teacher_has(t, i, t.logit[at])) take(r, i, (uint32_t)at);
+    }
+  };
+  each([&](int, int i, uint32_t) { atomicAdd(&place[i >> 8], 1); });
+  __syncthreads();
+  // running counts: a thread's stretch of tiles, the stretches in a wavefront, the wavefronts
+  const int per = (tiles_n + 1023) / 1024, b0 = tid * per;
+  int own = 0;
+  for (int i = b0; i < b0 + per && i < tiles_n; ++i) own += place[i];
+  int incl = own;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int u = __shfl_up(incl, o, 64);
+    if (lane >= o) incl += u;
+  }
+  if (lane == 63) sums[tid >> 6] = incl;
+  __syncthreads();
+  int run = incl - own;
+  for (int w = 0; w < (tid >> 6); ++w) run += sums[w];
+  int32_t* const mine = starts + (size_t)blockIdx.x * (tiles_n + 1);
+  for (int i = b0; i < b0 + per && i < tiles_n; ++i) {
+    const int n = place[i];
+    place[i] = mine[i] = run;
+    run += n;
+  }
+  if (tid == 1023) mine[tiles_n] = run;                        // (of all: its stretch is the last, empty or not)
+  __syncthreads();
+  each([&](int r, int i, uint32_t at) {
+    sorted[(size_t)p0 * t.K + atomicAdd(&place[i >> 8], 1)] = uint2{(uint32_t)(r << 8 | (i & 255)), at};
+  });
+}
+constexpr int kSortTiles = 16000;                              // column tiles whose counts fit 64 KB of LDS
 
 // Up to 64 tokens, a block each: what vocab_teacher_kernel, vocab_rows_kernel and vocab_pack_kernel do, in one launch.  Every block
 // looks at all tokens to number its own.
@@ -404,6 +459,12 @@ VocabPieces vocab_pieces(const moe_config& c, const moe_vocab_dims& d) {
   return p;
 }
 
+// Whether the product of the logits leaves those at the teacher's entries: for more than 100 MB of rows of w, about the time of the
+// sort and of the tiles' looks at it (8192 tokens, M 1024, V 64000, 32 entries: 952 -> 911 us)
+static bool vocab_sorts(const moe_config& c, const moe_vocab_dims& d) {
+  return (d.V + 255) / 256 <= kSortTiles && 2LL * c.G * c.S * d.K * c.M > 100000000LL;
+}
+
 VocabWs carve_vocab(const moe_config& c, const moe_vocab_dims& d, bool teacher, bool backward) {
   const size_t N = (size_t)c.G * c.S, elt = c.act_dtype == MOE_F32 ? 4 : 2;
   const VocabPieces p = vocab_pieces(c, d);
@@ -419,6 +480,9 @@ VocabWs carve_vocab(const moe_config& c, const moe_vocab_dims& d, bool teacher, 
   if (!backward) {
     w.slots = c.act_dtype == MOE_F32 ? vocab_stat_slots_f32((int)N, d.V, c.M) : vocab_stat_slots((int)N, d.V, c.M);
     w.packed = take(packs ? whole * c.M * elt : 0);
+    const bool sorts = packs && teacher && vocab_sorts(c, d);
+    w.starts = take(sorts ? whole / 256 * ((d.V + 255) / 256 + 1) * 4 : 0);
+    w.sorted = take(sorts ? (N * d.K + 64) * 8 : 0);             // (a tile fetches 64)
     w.stats = take((size_t)w.slots * N * 8);
   } else {
     w.pos = take(N * 4);
@@ -436,8 +500,9 @@ VocabWs carve_vocab(const moe_config& c, const moe_vocab_dims& d, bool teacher, 
   return w;
 }
 
+// sorted: not the logits of the entries that are there
 static int launch_teacher(const moe_config& c, const TeacherArgs& t, const void* x, const void* w, char* base, const VocabWs& ws,
-                          float* z, hipStream_t st) {
+                          float* z, bool sorted, hipStream_t st) {
   const long long N = (long long)c.G * c.S;
   const int pieces = c.M * (c.act_dtype == MOE_F32 ? 4 : 2) / 16;
   auto args = [&](auto kernel) {
@@ -445,7 +510,9 @@ static int launch_teacher(const moe_config& c, const TeacherArgs& t, const void*
                        static_cast<const uint4*>(w), pieces, N, reinterpret_cast<float2*>(base + ws.tstat),
                        reinterpret_cast<int32_t*>(base + ws.has), z);
   };
-  if (c.act_dtype == MOE_F32) args(vocab_teacher_kernel<float>); else args(vocab_teacher_kernel<bf16_t>);
+  if (sorted) args(vocab_teacher_kernel<bf16_t, true>);
+  else if (c.act_dtype == MOE_F32) args(vocab_teacher_kernel<float, false>);
+  else args(vocab_teacher_kernel<bf16_t, false>);
   return check_launch();
 }
 
@@ -496,14 +563,22 @@ int launch_vocab_forward(const moe_config& c, const moe_vocab_dims& d, const Voc
   r.loss = a.loss;
   r.lse = a.lse;
   const bool packs = !f32 && vocab_logits_on_tiles((int)N, d.V, c.M, true);
+  const bool sorts = packs && a.target == nullptr && vocab_sorts(c, d);
   // a row tile of the edge kernel takes as long whether all its tokens have a target or not: no need to number them
   const bool few = N <= kFewTokens && !packs, all = few && a.target != nullptr && !f32;
   if (few) {
     if (!all) rc = launch_few(c, r, t, a, base, ws, a.entry_logit, nullptr, st);
   } else {
-    if (a.target == nullptr) rc = launch_teacher(c, t, a.x, a.w, base, ws, a.entry_logit, st);
+    if (a.target == nullptr) rc = launch_teacher(c, t, a.x, a.w, base, ws, a.entry_logit, sorts, st);
     if (rc == MOE_OK) rc = launch_rows(r, st);
     if (rc == MOE_OK && packs) rc = launch_pack(c, a.x, base + ws.packed, r, st);
+    if (rc == MOE_OK && sorts) {
+      const int tiles_n = (d.V + 255) / 256;
+      hipLaunchKernelGGL(vocab_sort_kernel, dim3((unsigned)((N + 255) / 256)), dim3(1024), (size_t)tiles_n * sizeof(int), st, t,
+                         r.perm, r.kept, tiles_n, reinterpret_cast<int32_t*>(base + ws.starts),
+                         reinterpret_cast<uint2*>(base + ws.sorted));
+      rc = check_launch();
+    }
   }
   if (rc != MOE_OK) return rc;
   float2* const stats = reinterpret_cast<float2*>(base + ws.stats);
@@ -512,6 +587,12 @@ int launch_vocab_forward(const moe_config& c, const moe_vocab_dims& d, const Voc
   g.kept = all ? nullptr : r.kept;
   g.vocab.scale = kLog2e * inv_t;
   g.vocab.stats = stats;
+  if (sorts) {
+    g.vocab.starts = reinterpret_cast<const int32_t*>(base + ws.starts);
+    g.vocab.sorted = reinterpret_cast<const uint2*>(base + ws.sorted);
+    g.vocab.entry_logit = a.entry_logit;
+    g.vocab.K = d.K;
+  }
   rc = f32 ? launch_gemm_f32(kDataGrad, g, 1, (int)N, d.V, c.M, st) : launch_vocab_logits(g, (int)N, d.V, c.M, st);
   if (rc != MOE_OK) return rc;
   const int pieces = c.M * (f32 ? 4 : 2) / 16;
@@ -566,7 +647,7 @@ int launch_vocab_backward(const moe_config& c, const moe_vocab_dims& d, const Vo
   if (N <= kFewTokens) {
     rc = launch_few(c, r, t, a, base, ws, nullptr, base + ws.packed, st);
   } else {
-    if (a.target == nullptr) rc = launch_teacher(c, t, a.x, a.w, base, ws, nullptr, st);
+    if (a.target == nullptr) rc = launch_teacher(c, t, a.x, a.w, base, ws, nullptr, false, st);
     if (rc == MOE_OK) rc = launch_rows(r, st);
     if (rc == MOE_OK) rc = launch_pack(c, a.x, base + ws.packed, r, st);
   }

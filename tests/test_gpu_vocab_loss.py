@@ -118,7 +118,8 @@ CE = [(1, 64, 128, 900, "bf16", 0.5, 0), (1, 33, 72, 515, "f32", 0.5, 0), (5, 13
       # most rows without a target
       (1, 2100, 448, 33333, "bf16", 0.1, 0), (3, 1021, 776, 20257, "bf16", 0.6, 0), (1, 6000, 192, 9999, "bf16", 0.3, 0),
       (1, 3000, 1000, 9001, "bf16", 0, 4096), (2, 1250, 1344, 7003, "bf16", 0.02, 0), (1, 32, 4096, 16000, "bf16", 0, 0),
-      (1, 1024, 1024, 32000, "bf16", 0.97, 0), (1, 9001, 72, 26001, "bf16", 0, 8192)]
+      (1, 1024, 1024, 32000, "bf16", 0.97, 0), (1, 2048, 1024, 32000, "bf16", 0.05, 0),
+      (1, 9001, 72, 26001, "bf16", 0, 8192)]
 
 
 @pytest.mark.parametrize("G,S,M,V,dtype,empty,piece", CE)
@@ -131,7 +132,9 @@ def test_cross_entropy(G, S, M, V, dtype, empty, piece):
 KD = [(1, 64, 72, 300, 20, 2.0, "bf16", 0.5, 0), (5, 8, 132, 700, 3, 1.5, "f32", 0.4, 0), (1, 63, 256, 2048, 256, 1.0, "bf16", 0.1, 0),
       (1, 1, 8, 1, 1, 1.0, "bf16", 0, 0), (1, 5, 40, 3, 9, 0.5, "bf16", 0, 0), (1, 5, 36, 33, 3, 2.0, "f32", 0.2, 0),
       (2, 65, 72, 257, 16, 2.0, "bf16", 0.3, 0), (1, 200, 136, 1500, 65, 3.0, "bf16", 0.1, 256), (1, 77, 68, 700, 256, 1.0, "f32", 0.1, 256),
-      (1, 1, 1024, 4001, 31, 4.0, "bf16", 0, 0), (2, 1100, 256, 2999, 32, 2.0, "bf16", 0.1, 0)]
+      (1, 1, 1024, 4001, 31, 4.0, "bf16", 0, 0), (2, 1100, 256, 2999, 32, 2.0, "bf16", 0.1, 0),
+      # the product leaves the logits at the entries (test_vocab_rules.py)
+      (1, 2500, 1024, 16001, 32, 2.0, "bf16", 0.2, 0), (3, 700, 520, 31011, 256, 1.0, "bf16", 0.1, 8192), (1, 4096, 256, 33000, 100, 3.0, "bf16", 0, 0)]
 
 
 @pytest.mark.parametrize("G,S,M,V,K,T,dtype,empty,piece", KD)
@@ -179,6 +182,15 @@ def test_teacher_lists_with_gaps(dtype):
     d["idx"][7], d["logit"][7] = V - 1, low
     for T in (0.25, 1.0, 8.0):
         check(G, S, M, V, dtype, d, call(G, S, M, V, dtype, d, K, T), K, T)
+
+
+def test_entries_crowded_into_few_tiles():
+    """More entries in a 256 x 256 tile of the logits than a wavefront has lanes, many of them the same."""
+    G, S, M, V, K = 1, 2100, 1032, 17000, 64
+    d = make(G, S, M, V, "bf16", 0.1, K)
+    there = d["idx"] >= 0
+    d["idx"] = torch.where(there & (torch.arange(K, device=DEV) > 0), 16640 + d["idx"] % 360, d["idx"]).int()
+    check(G, S, M, V, "bf16", d, call(G, S, M, V, "bf16", d, K, 2.0), K, 2.0)
 
 
 def test_far_logits():
