@@ -245,6 +245,44 @@ def time_encoder(moe, cfg, sh, inp, K, W, peak):
             "note": "x -> attention + dense FFN layer -> attention + MoE layer, forward and backward; not part of value"}
 
 
+def time_model_end(moe, cfg, sh, K, W, peak, V=32000):
+    """What follows the encoder layers in training, for this workload's tokens and a vocabulary of 32k entries (the size the
+    paper's one-language models use): the loss with its gradient, and the derivative of the last normalisation."""
+    import torch
+    dev, dt = "cuda:0", sh.torch_dtype
+    g = torch.Generator(device=dev).manual_seed(11)
+    rand = lambda *s: torch.randn(*s, generator=g, device=dev)
+    x, w = rand(cfg.G, cfg.S, cfg.M).to(dt), (rand(V, cfg.M) / cfg.M ** 0.5).to(dt)
+    target = torch.randint(0, V, (cfg.G, cfg.S), generator=g, device=dev).int()
+    f = lambda *s: torch.empty(*s, device=dev)
+    loss, lse, dloss = f(cfg.G, cfg.S), f(cfg.G, cfg.S), torch.full((cfg.G, cfg.S), 1.0 / cfg.N, device=dev)
+    dx, dw, ds = torch.empty_like(x), torch.empty_like(w), torch.empty_like(x)
+    gamma, dgamma, dbeta = torch.ones(cfg.M, device=dev), f(cfg.M), f(cfg.M)
+    dims = moe.VocabDims(V)
+    u8 = lambda n: torch.empty(n, dtype=torch.uint8, device=dev)
+    ws, bws = u8(moe.moe_vocab_workspace_bytes(sh, dims)), u8(moe.moe_vocab_backward_workspace_bytes(sh, dims))
+    lws = u8(moe.moe_layer_norm_backward_workspace_bytes(sh))
+
+    def timed(fn):
+        for _ in range(W):
+            fn()
+        torch.cuda.synchronize()
+        t0 = time.perf_counter()
+        for _ in range(K):
+            fn()
+        torch.cuda.synchronize()
+        return (time.perf_counter() - t0) * 1e3 / K
+
+    fwd = timed(lambda: moe.moe_vocab_loss(sh, dims, x, w, target, loss, lse, ws))
+    bwd = timed(lambda: moe.moe_vocab_loss_backward(sh, dims, x, w, target, loss, lse, dloss, dx, dw, bws))
+    norm = timed(lambda: moe.moe_add_layer_norm_backward(sh, x, dx, gamma, None, ds, dgamma, dbeta, lws))
+    product = 2.0 * cfg.N * cfg.M * V
+    return {"workload": f"{cfg.N} tokens, M={cfg.M}, V={V}, {cfg.act_dtype}", "vocab_loss_ms": fwd,
+            "vocab_loss_mfma_frac": product / fwd / 1e9 / peak, "vocab_loss_backward_ms": bwd,
+            "vocab_loss_backward_mfma_frac": 3 * product / bwd / 1e9 / peak, "layer_norm_backward_ms": norm,
+            "layer_norm_backward_hbm_frac": 3.0 * cfg.N * cfg.M * x.element_size() / norm / 1e6 / PEAK_HBM_GBS}
+
+
 def time_backward(moe, cfg, sh, inp, ws, y, aux, K, W, kept_rows, peak):
     """Backward pass of the same layer (not part of `value`): K calls of moe_backward_events
     after one moe_forward_train, stage times from HIP events on the kernels' stream."""
@@ -523,7 +561,8 @@ def main():
                     help="also time the forward as replays of one captured HIP graph (reported as "
                          "an extra field; the metric itself is always the eager call sequence)")
     ap.add_argument("--no-encoder", action="store_true",
-                    help="skip the extra measurement of the encoder layers around the MoE layer")
+                    help="skip the extra measurements of the encoder layers around the MoE layer and of the "
+                         "loss at the model's end")
     ap.add_argument("--no-yardsticks", action="store_true",
                     help="skip the copy / vendor-GEMM context measurements")
     ap.add_argument("--no-f32", action="store_true",
@@ -606,6 +645,7 @@ def main():
         out["hip_graph_ms_per_step"] = (time.perf_counter() - g0) * 1e3 / K
     if not args.no_encoder and cfg.act_dtype == "bf16":
         out["encoder_pair"] = time_encoder(moe, cfg, sh, inp, K, W, peak)
+        out["model_end"] = time_model_end(moe, cfg, sh, K, W, peak)
     if not args.no_yardsticks:
         out["yardsticks"] = yardsticks(cfg, dev)
     if not args.no_backward:
