@@ -303,6 +303,8 @@ int launch_vocab_dx(const GemmArgs& a, const VocabDxPlan& p, int rows, int M, hi
 //   dw: C [entries, M] = A [rows, lda]^T . B [rows, M], which has rows of zeros like dz
 bool vocab_dw_on_tiles(int rows, int entries, int M);
 int launch_vocab_dw(const GemmArgs& a, int rows, int entries, int M, hipStream_t st);
+int launch_vocab_grads_pair(const GemmArgs& dx, const VocabDxPlan& p, const GemmArgs& dw, int rows, int entries, int M,
+                            hipStream_t st, bool* done);
 // Time of a product on 256 x 256 tiles (us): a launch, and per round of tiles its ends and its steps of 64 k, which take
 // longer the more units are at work, or the time in which dz passes from memory.
 //   measured / by this, us: z (M, rows, entries) 1024 1024 20000 57 / 57, 1024 1024 32000 64 / 65, 1024 6000 32000 369 / 368,

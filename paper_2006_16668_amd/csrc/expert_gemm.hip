@@ -1075,6 +1075,21 @@ void expert_gemm_bf16_pair_kernel(EdgeArgs data, EdgeArgs weight) {
   else edge_tile<BMW, BNW, 32, STW, kEpiRangesIfAny, true, false, false>(weight, xcd_remap(id - data.nblk, weight.nblk));
 }
 
+// dx and dw of a vocabulary's loss in one launch, likewise: both read dz (vocab_grads_pair says when).
+template <int BMD, int BND, int STD, int BMW, int BNW, int STW>
+__global__ __launch_bounds__(256, (kEdgeBlocks<BMD, BND> < kEdgeBlocks<BMW, BNW> ? kEdgeBlocks<BMD, BND> : kEdgeBlocks<BMW, BNW>))
+void vocab_gemm_bf16_pair_kernel(EdgeArgs data, EdgeArgs weight) {
+  const int id = blockIdx.x;
+  if (id < data.nblk) {
+    const int tiles_m = (data.kept[0] + BMD - 1) / BMD, n = data.nblk / data.tiles_m * tiles_m;
+    if (id >= n) return;
+    data.tiles_m = tiles_m;
+    edge_tile<BMD, BND, 64, STD, kEpiSums, false, false, false>(data, xcd_remap(id, n));
+  } else {
+    edge_tile<BMW, BNW, 32, STW, kEpiPitch, true, false, true>(weight, xcd_remap(id - data.nblk, weight.nblk));
+  }
+}
+
 // LDS limit of one instantiation of the persistent kernel on the current device (all of the
 // 160 KB when the size depends on the number of experts)
 template <int ST, int EPI, bool GATHER, bool A_MNC = false, bool B_KC = false, bool PACKED = false,
@@ -1340,33 +1355,46 @@ struct PairProduct {
   double us;
   int k_total = 0;
 };
-template <int BMD, int BND, int STD, int BMW, int BNW, int STW>
+template <bool VOCAB, int BMD, int BND, int STD, int BMW, int BNW, int STW>
+constexpr auto pair_kernel() {
+  if constexpr (VOCAB) return vocab_gemm_bf16_pair_kernel<BMD, BND, STD, BMW, BNW, STW>;
+  else return expert_gemm_bf16_pair_kernel<BMD, BND, STD, BMW, BNW, STW>;
+}
+template <bool VOCAB, int BMD, int BND, int STD, int BMW, int BNW, int STW>
 int prepare_pair() {
   static LdsLimitOnce once;
   constexpr size_t d = EdgeSmem<BMD, BND, 64, STD>::kBytes, w = EdgeSmem<BMW, BNW, 32, STW>::kBytes;
-  return ensure_lds_limit(once, reinterpret_cast<const void*>(expert_gemm_bf16_pair_kernel<BMD, BND, STD, BMW, BNW, STW>),
+  return ensure_lds_limit(once, reinterpret_cast<const void*>(pair_kernel<VOCAB, BMD, BND, STD, BMW, BNW, STW>()),
                           (int)(d > w ? d : w));
 }
-template <int BMD, int BND, int STD, int BMW, int BNW, int STW>
+template <bool VOCAB, int BMD, int BND, int STD, int BMW, int BNW, int STW>
 int launch_pair_as(const PairProduct& d, const PairProduct& w, hipStream_t st) {
-  if (prepare_pair<BMD, BND, STD, BMW, BNW, STW>() != MOE_OK) return MOE_EHIP;
+  if (prepare_pair<VOCAB, BMD, BND, STD, BMW, BNW, STW>() != MOE_OK) return MOE_EHIP;
   constexpr size_t kLdsD = EdgeSmem<BMD, BND, 64, STD>::kBytes, kLdsW = EdgeSmem<BMW, BNW, 32, STW>::kBytes;
   EdgeArgs da, wa;
-  if (!edge_args(&da, BMD, BND, d.a, d.E, d.R, d.N, d.K, 0) || !edge_args(&wa, BMW, BNW, w.a, w.E, w.R, w.N, w.K, w.k_total) ||
+  if (!edge_args(&da, BMD, BND, d.a, d.E, d.R, d.N, d.K, d.k_total) || !edge_args(&wa, BMW, BNW, w.a, w.E, w.R, w.N, w.K, w.k_total) ||
       (long long)da.nblk + wa.nblk > 0x7fffffffLL)
     return MOE_EUNSUPPORTED;
-  hipLaunchKernelGGL((expert_gemm_bf16_pair_kernel<BMD, BND, STD, BMW, BNW, STW>), dim3((unsigned)(da.nblk + wa.nblk)), dim3(256),
+  hipLaunchKernelGGL((pair_kernel<VOCAB, BMD, BND, STD, BMW, BNW, STW>()), dim3((unsigned)(da.nblk + wa.nblk)), dim3(256),
                      kLdsD > kLdsW ? kLdsD : kLdsW, st, da, wa);
   return check_launch();
 }
 // as many stages as leave a unit the blocks that its larger tiles would have alone
-template <int BMD, int BND>
+template <bool VOCAB, int BMD, int BND>
 int launch_pair_weight(const PairProduct& d, const PairProduct& w, hipStream_t st) {
   constexpr int kDeep = BND == 64 ? 4 : 2, kFlat = BND == 64 ? 3 : 2;
   switch (w.form) {
-    case kEdge64x64: return launch_pair_as<BMD, BND, kDeep, 64, 64, 5>(d, w, st);
-    case kEdge64x128: return launch_pair_as<BMD, BND, kDeep, 64, 128, 4>(d, w, st);
-    default: return launch_pair_as<BMD, BND, kFlat, 128, 128, 3>(d, w, st);
+    case kEdge64x64: return launch_pair_as<VOCAB, BMD, BND, kDeep, 64, 64, 5>(d, w, st);
+    case kEdge64x128: return launch_pair_as<VOCAB, BMD, BND, kDeep, 64, 128, 4>(d, w, st);
+    default: return launch_pair_as<VOCAB, BMD, BND, kFlat, 128, 128, 3>(d, w, st);
+  }
+}
+template <bool VOCAB>
+int launch_pair_forms(const PairProduct& d, const PairProduct& w, hipStream_t st) {
+  switch (d.form) {
+    case kEdge64x64: case kEdge64x64Deep: return launch_pair_weight<VOCAB, 64, 64>(d, w, st);
+    case kEdge64x128: case kEdge64x128Deep: return launch_pair_weight<VOCAB, 64, 128>(d, w, st);
+    default: return launch_pair_weight<VOCAB, 128, 128>(d, w, st);
   }
 }
 // Which pairs of gradients share a launch.  A small product leaves units idle at its start and end and its successor waits
@@ -1414,11 +1442,7 @@ bool pair_ok(PairProduct* d, GemmLayout data, PairProduct* w, int cus) {
 int launch_pair(const PairProduct& d, const PairProduct& w, hipStream_t st, bool* done) {
   *done = independent(d, w) && independent(w, d);
   if (!*done) return MOE_OK;
-  switch (d.form) {
-    case kEdge64x64: case kEdge64x64Deep: return launch_pair_weight<64, 64>(d, w, st);
-    case kEdge64x128: case kEdge64x128Deep: return launch_pair_weight<64, 128>(d, w, st);
-    default: return launch_pair_weight<128, 128>(d, w, st);
-  }
+  return launch_pair_forms<false>(d, w, st);
 }
 
 template <bool RELU>
@@ -1480,9 +1504,10 @@ int prepare_expert_gemm() {
       // vocabulary
       MOE_EDGE_KC(kEpiStats, false, true, false), MOE_EDGE_KC(kEpiLogitGrad, false, true, false),
       MOE_EDGE_KC(kEpiSums, false, false, false), MOE_EDGE_MNC(kEpiPitch, true, false, true),
-#define MOE_PAIR(BM, BN, DEEP, FLAT) \
-  prepare_pair<BM, BN, DEEP, 64, 64, 5>(), prepare_pair<BM, BN, DEEP, 64, 128, 4>(), prepare_pair<BM, BN, FLAT, 128, 128, 3>()
-      MOE_PAIR(64, 64, 4, 3), MOE_PAIR(64, 128, 2, 2), MOE_PAIR(128, 128, 2, 2)};
+#define MOE_PAIR(V, BM, BN, DEEP, FLAT) \
+  prepare_pair<V, BM, BN, DEEP, 64, 64, 5>(), prepare_pair<V, BM, BN, DEEP, 64, 128, 4>(), prepare_pair<V, BM, BN, FLAT, 128, 128, 3>()
+      MOE_PAIR(false, 64, 64, 4, 3), MOE_PAIR(false, 64, 128, 2, 2), MOE_PAIR(false, 128, 128, 2, 2),
+      MOE_PAIR(true, 64, 64, 4, 3),  MOE_PAIR(true, 64, 128, 2, 2),  MOE_PAIR(true, 128, 128, 2, 2)};
 #undef MOE_PAIR
 #undef MOE_EDGE_KC
 #undef MOE_EDGE_MNC
@@ -1698,6 +1723,22 @@ int launch_vocab_dw(const GemmArgs& a, int rows, int entries, int M, hipStream_t
   if (vocab_dw_on_tiles(rows, entries, M)) return launch_vocab_tiles_dw(a, entries, M, st);
   const GemmForm form = gemm_form(false, 1, entries, M, rows, kLayoutWeightGrad, kPlanUnits);
   return gemm_bf16_edge<kEpiPitch, true, false, true>(form, a, 1, entries, M, rows, st);
+}
+
+// Both products of dz, dx's and dw's arguments as above, in one launch where that is faster (*done: else one after the other): small
+// ones in the edge kernel, by the line that is drawn for the gradients of a layer.
+int launch_vocab_grads_pair(const GemmArgs& dx, const VocabDxPlan& p, const GemmArgs& dw, int rows, int entries, int M,
+                            hipStream_t st, bool* done) {
+  *done = false;
+  if (p.tiles || vocab_dw_on_tiles(rows, entries, M)) return MOE_OK;
+  PairProduct d{dx, p.splits, rows, M, p.splits == 1 ? entries : p.k, kPersistent, 0};
+  d.form = gemm_form(false, d.E, rows, M, d.K, kLayoutForward, kPlanUnits, &d.us);
+  d.k_total = dx.k_total;
+  PairProduct w{dw, 1, entries, M, rows, kPersistent, 0};
+  w.form = gemm_form(false, 1, entries, M, rows, kLayoutWeightGrad, kPlanUnits, &w.us);
+  if (!pair_ok(&d, kLayoutForward, &w, kPlanUnits)) return MOE_OK;
+  *done = true;
+  return launch_pair_forms<true>(d, w, st);
 }
 
 int launch_expert_gemm2(const moe_config& c, const void* h, const void* wo, void* out,

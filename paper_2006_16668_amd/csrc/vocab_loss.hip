@@ -682,11 +682,15 @@ int launch_vocab_backward(const moe_config& c, const moe_vocab_dims& d, const Vo
     gx.k_total = n;
     gx.add = i > 0;
     const VocabDxPlan plan{(n + ws.dx_plan.k - 1) / ws.dx_plan.k, ws.dx_plan.k, ws.dx_plan.tiles};      // (a last piece fills fewer ranges)
-    rc = f32 ? launch_gemm_f32(kForward, gx, plan.splits, (int)N, c.M, plan.k, st)  : launch_vocab_dx(gx, plan, (int)N, c.M, st);
-    if (rc != MOE_OK) return rc;
     GemmArgs gw{z.C, base + ws.packed, static_cast<char*>(a.dw) + (size_t)first * c.M * elt};
     gw.kept = r.kept;
     gw.lda = pc.entries;
+    bool done = false;
+    if (!f32) rc = launch_vocab_grads_pair(gx, plan, gw, (int)N, n, c.M, st, &done);
+    if (rc != MOE_OK) return rc;
+    if (done) continue;
+    rc = f32 ? launch_gemm_f32(kForward, gx, plan.splits, (int)N, c.M, plan.k, st) : launch_vocab_dx(gx, plan, (int)N, c.M, st);
+    if (rc != MOE_OK) return rc;
     rc = f32 ? launch_gemm_f32(kWeightGrad, gw, 1, n, c.M, (int)N, st)  : launch_vocab_dw(gw, (int)N, n, c.M, st);
     if (rc != MOE_OK) return rc;
   }
