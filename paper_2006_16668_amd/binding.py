@@ -497,8 +497,9 @@ def moe_layer_norm_backward_workspace_bytes(shape: MoEShape) -> int:
 
 def moe_add_layer_norm_backward(shape: MoEShape, s, dn, gamma, dres, ds, dgamma, dbeta, ws):
     """Gradients of moe_add_layer_norm: ds (of x and of delta) from dn and dres (None: nothing reaches s past the norm)."""
-    _given(s=s, dn=dn, gamma=gamma, ds=ds, dgamma=dgamma, dbeta=dbeta, ws=ws)
-    _on_current_device(dres=dres)
+    _given("s dn gamma ds dgamma dbeta ws", s, dn, gamma, ds, dgamma, dbeta, ws)
+    if dres is not None:
+        _given("dres", dres)
     G, S, M = shape.G, shape.S, shape.M
     dt, f32 = shape.torch_dtype, torch.float32
     c = shape._c()
@@ -615,12 +616,17 @@ def moe_encoder_pair_backward(shape: MoEShape, dims: EncoderDims, x, weights: di
 
 
 # ---- the end of the model: loss over a vocabulary
-def _on_current_device(**tensors):
-    """The kernels run on the current device: tensors of another one are refused."""
-    here = torch.cuda.current_device()
-    for name, t in tensors.items():
-        if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != here:
-            raise ValueError(f"{name}: on cuda:{t.device.index}, the current device is cuda:{here}")
+def _given(names, *tensors):
+    """None is refused, and so are tensors of another device than the current one, on which the kernels run."""
+    here = None
+    for i, t in enumerate(tensors):
+        if t is None:
+            raise TypeError(f"{names.split()[i]}: expected a GPU tensor")
+        if isinstance(t, torch.Tensor) and t.is_cuda:
+            if here is None:
+                here = torch.cuda.current_device()
+            if t.get_device() != here:
+                raise ValueError(f"{names.split()[i]}: on {t.device}, the current device is cuda:{here}")
 
 
 def moe_vocab_workspace_bytes(shape: MoEShape, dims: VocabDims) -> int:
@@ -631,16 +637,9 @@ def moe_vocab_backward_workspace_bytes(shape: MoEShape, dims: VocabDims) -> int:
     return _ws_query("moe_vocab_backward_workspace_bytes", shape, dims)
 
 
-def _given(**tensors):
-    for name, t in tensors.items():
-        if t is None:
-            raise TypeError(f"{name}: expected a GPU tensor")
-    _on_current_device(**tensors)
-
-
 def moe_vocab_loss(shape: MoEShape, dims: VocabDims, x, w, target, loss, lse, ws):
     """Softmax cross entropy of x [G,S,M] . w [V,M]^T against target [G,S] (outside 0 .. V-1: none); loss, lse [G,S]."""
-    _given(x=x, w=w, target=target, loss=loss, lse=lse, ws=ws)
+    _given("x w target loss lse ws", x, w, target, loss, lse, ws)
     G, S, M = shape.G, shape.S, shape.M
     dt, f32 = shape.torch_dtype, torch.float32
     c, d = shape._c(), dims._c()
@@ -653,7 +652,7 @@ def moe_vocab_loss(shape: MoEShape, dims: VocabDims, x, w, target, loss, lse, ws
 
 def moe_vocab_loss_backward(shape: MoEShape, dims: VocabDims, x, w, target, loss, lse, dloss, dx, dw, ws):
     """Gradients dx [G,S,M], dw [V,M] of sum(dloss * loss); loss and lse as moe_vocab_loss left them."""
-    _given(x=x, w=w, target=target, loss=loss, lse=lse, dloss=dloss, dx=dx, dw=dw, ws=ws)
+    _given("x w target loss lse dloss dx dw ws", x, w, target, loss, lse, dloss, dx, dw, ws)
     G, S, M = shape.G, shape.S, shape.M
     dt, f32 = shape.torch_dtype, torch.float32
     c, d = shape._c(), dims._c()
@@ -668,7 +667,7 @@ def moe_vocab_loss_backward(shape: MoEShape, dims: VocabDims, x, w, target, loss
 def moe_vocab_distill(shape: MoEShape, dims: VocabDims, x, w, teacher_idx, teacher_logit, loss, lse, entry_logit, ws):
     """Loss against the softmax of a teacher's K logits per token (index outside 0 .. V-1 or logit -inf: no entry), and the
     student's logits at them, entry_logit [G,S,K]."""
-    _given(x=x, w=w, teacher_idx=teacher_idx, teacher_logit=teacher_logit, loss=loss, lse=lse, entry_logit=entry_logit, ws=ws)
+    _given("x w teacher_idx teacher_logit loss lse entry_logit ws", x, w, teacher_idx, teacher_logit, loss, lse, entry_logit, ws)
     G, S, M, K = shape.G, shape.S, shape.M, dims.K
     dt, f32 = shape.torch_dtype, torch.float32
     c, d = shape._c(), dims._c()
@@ -683,8 +682,7 @@ def moe_vocab_distill(shape: MoEShape, dims: VocabDims, x, w, teacher_idx, teach
 def moe_vocab_distill_backward(shape: MoEShape, dims: VocabDims, x, w, teacher_idx, teacher_logit, entry_logit, lse, dloss,
                                dx, dw, ws):
     """Gradients dx, dw of sum(dloss * loss); entry_logit and lse as moe_vocab_distill left them."""
-    _given(x=x, w=w, teacher_idx=teacher_idx, teacher_logit=teacher_logit, entry_logit=entry_logit, lse=lse, dloss=dloss,
-           dx=dx, dw=dw, ws=ws)
+    _given("x w teacher_idx teacher_logit entry_logit lse dloss dx dw ws", x, w, teacher_idx, teacher_logit, entry_logit, lse, dloss, dx, dw, ws)
     G, S, M, K = shape.G, shape.S, shape.M, dims.K
     dt, f32 = shape.torch_dtype, torch.float32
     c, d = shape._c(), dims._c()

@@ -701,7 +701,7 @@ int moe_add_layer_norm_backward(const moe_config* cfg, const void* s, const void
   const long long rows = (long long)cfg->G * cfg->S;
   if (ws_bytes < moe::layer_norm_bwd_bytes(cfg->act_dtype, rows, cfg->M)) return MOE_EWORKSPACE;
   return moe::launch_layer_norm_bwd(cfg->act_dtype, s, dn, gamma, dres, ds, static_cast<float*>(ws), dgamma, dbeta, rows, cfg->M,
-                                    static_cast<hipStream_t>(stream));
+                                    true, static_cast<hipStream_t>(stream));
 }
 
 int moe_attention_workspace_bytes(const moe_config* cfg, const moe_encoder_dims* dims, size_t* bytes) {
@@ -901,7 +901,7 @@ int moe_encoder_pair_backward(const moe_config* cfg, const moe_encoder_dims* dim
   if (rc != MOE_OK) return rc;
   // g0 = d L / d c = dy + LN4'(dn)
   rc = moe::launch_layer_norm_bwd(dt, f + e.c, dn, w->ln_gamma[3], dy, g0, partial, g->ln_gamma[3],
-                                  g->ln_beta[3], N, cfg->M, st);
+                                  g->ln_beta[3], N, cfg->M, false, st);
   if (rc != MOE_OK) return rc;
   // c = b + Attention_2(n3)
   rc = attention_bwd_impl(*cfg, *dims, f + e.n[2], w->wqkv[1], w->wo_att[1], f + e.qkv[1],
@@ -909,7 +909,7 @@ int moe_encoder_pair_backward(const moe_config* cfg, const moe_encoder_dims* dim
                           base + bw.dctx, dvec, wpart, st);
   if (rc != MOE_OK) return rc;
   rc = moe::launch_layer_norm_bwd(dt, f + e.b, dn, w->ln_gamma[2], g0, g1, partial, g->ln_gamma[2],
-                                  g->ln_beta[2], N, cfg->M, st);
+                                  g->ln_beta[2], N, cfg->M, false, st);
   if (rc != MOE_OK) return rc;
   // b = a + relu(n2 w1) w2
   rc = moe::launch_dense_grads(*cfg, N, cfg->H, cfg->M, f + e.hden, g1, w->w2, f + e.hden, base + bw.dhden, g->w2, wpart, st);
@@ -917,7 +917,7 @@ int moe_encoder_pair_backward(const moe_config* cfg, const moe_encoder_dims* dim
   rc = moe::launch_dense_grads(*cfg, N, cfg->M, cfg->H, f + e.n[1], base + bw.dhden, w->w1, nullptr, dn, g->w1, wpart, st);
   if (rc != MOE_OK) return rc;
   rc = moe::launch_layer_norm_bwd(dt, f + e.a, dn, w->ln_gamma[1], g1, g0, partial, g->ln_gamma[1],
-                                  g->ln_beta[1], N, cfg->M, st);
+                                  g->ln_beta[1], N, cfg->M, false, st);
   if (rc != MOE_OK) return rc;
   // a = x + Attention_1(n1)
   rc = attention_bwd_impl(*cfg, *dims, f + e.n[0], w->wqkv[0], w->wo_att[0], f + e.qkv[0],
@@ -925,7 +925,7 @@ int moe_encoder_pair_backward(const moe_config* cfg, const moe_encoder_dims* dim
                           base + bw.dctx, dvec, wpart, st);
   if (rc != MOE_OK) return rc;
   return moe::launch_layer_norm_bwd(dt, x, dn, w->ln_gamma[0], g0, dx, partial, g->ln_gamma[0],
-                                    g->ln_beta[0], N, cfg->M, st);
+                                    g->ln_beta[0], N, cfg->M, false, st);
 }
 
 int moe_vocab_workspace_bytes(const moe_config* cfg, const moe_vocab_dims* dims, size_t* bytes) {

@@ -21,16 +21,17 @@ namespace {
 
 // ---------------------------------------------------------------- layer normalisation
 // One wavefront per row, a wavefront walks rows wave, wave + waves, ...; its column sums of
-// dn * xhat and dn stay in registers; the four wavefronts of a block add theirs in LDS (fixed
-// order) and the block leaves one partial row.
-template <typename T, int VPL>
-__global__ __launch_bounds__(256) void layer_norm_bwd_kernel(
+// dn * xhat and dn stay in registers; the WAVES wavefronts of a block add theirs in LDS (fixed
+// order) and the block leaves one partial row.  The sums of dn start `pitch` floats behind the others: M, or, with one
+// block whose sums are dgamma and dbeta themselves, what lies between those.
+template <typename T, int VPL, int WAVES = 4>
+__global__ __launch_bounds__(64 * WAVES) void layer_norm_bwd_kernel(
     const uint4* __restrict__ s, const uint4* __restrict__ dn, const float* __restrict__ gamma,
-    const uint4* dres, uint4* dx, float* __restrict__ partial, int M, int vec_per_row,
+    const uint4* dres, uint4* dx, float* __restrict__ partial, long long pitch, int M, int vec_per_row,
     long long rows, float eps) {
   const int lane = threadIdx.x & 63;
-  const long long wave_id = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const long long waves = (long long)gridDim.x * 4;
+  const long long wave_id = (long long)blockIdx.x * WAVES + (threadIdx.x >> 6);
+  const long long waves = (long long)gridDim.x * WAVES;
   constexpr int K = Vec16<T>::kElts;
   float ag[VPL][K], ab[VPL][K], gam[VPL][K];
 #pragma unroll
@@ -100,7 +101,7 @@ __global__ __launch_bounds__(256) void layer_norm_bwd_kernel(
       }
     }
   }
-  extern __shared__ float ln_bwd_smem[];              // [4 wavefronts][M], used twice
+  extern __shared__ float ln_bwd_smem[];              // [wavefronts][M], used twice
   float* mine = ln_bwd_smem + (size_t)(threadIdx.x >> 6) * M;
   float* pg = partial + (size_t)blockIdx.x * 2 * M;
 #pragma unroll
@@ -114,14 +115,14 @@ __global__ __launch_bounds__(256) void layer_norm_bwd_kernel(
         if (col < M) *reinterpret_cast<float4*>(mine + col) = float4{a[0], a[1], a[2], a[3]};
       }
     __syncthreads();
-    for (int i = threadIdx.x * 4; i < M; i += 1024) {
+    for (int i = threadIdx.x * 4; i < M; i += 256 * WAVES) {
       float4 t = *reinterpret_cast<const float4*>(ln_bwd_smem + i);
 #pragma unroll
-      for (int w = 1; w < 4; ++w) {
+      for (int w = 1; w < WAVES; ++w) {
         const float4 o = *reinterpret_cast<const float4*>(ln_bwd_smem + w * M + i);
         t.x += o.x; t.y += o.y; t.z += o.z; t.w += o.w;
       }
-      *reinterpret_cast<float4*>(pg + which * M + i) = t;
+      *reinterpret_cast<float4*>(pg + which * pitch + i) = t;
     }
     __syncthreads();
   }
@@ -550,10 +551,27 @@ size_t layer_norm_bwd_bytes(int act_dtype, long long rows, int M) {
 
 int launch_layer_norm_bwd(int act_dtype, const void* s, const void* dn, const float* gamma,
                           const void* dres, void* dx, float* partial, float* dgamma, float* dbeta,
-                          long long rows, int M, hipStream_t st) {
+                          long long rows, int M, bool one_block, hipStream_t st) {
   const int elt = act_dtype == MOE_F32 ? 4 : 2;
   const int vec_per_row = M * elt / 16;
   const int vpl = (vec_per_row + 63) / 64;
+  if (one_block && rows <= 64 && M <= 1024) {
+    // One block of 16 wavefronts, whose sums are the parameters' gradients: one launch (37 rows of 520 fp32, with the call from Python
+    // 17.6 -> 12.5 us).
+    auto one = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3(1), dim3(1024), (size_t)16 * M * sizeof(float), st, static_cast<const uint4*>(s),
+                         static_cast<const uint4*>(dn), gamma, static_cast<const uint4*>(dres), static_cast<uint4*>(dx), dgamma,
+                         ((intptr_t)dbeta - (intptr_t)dgamma) / (long long)sizeof(float), M, vec_per_row, rows, 1e-6f);
+    };
+    if (act_dtype == MOE_F32) {
+      if (vpl <= 1) one(layer_norm_bwd_kernel<float, 1, 16>);
+      else if (vpl <= 2) one(layer_norm_bwd_kernel<float, 2, 16>);
+      else one(layer_norm_bwd_kernel<float, 4, 16>);
+    } else {
+      if (vpl <= 1) one(layer_norm_bwd_kernel<bf16_t, 1, 16>); else one(layer_norm_bwd_kernel<bf16_t, 2, 16>);
+    }
+    return check_launch();
+  }
   const size_t lds = (size_t)4 * M * sizeof(float);
   const float eps = 1e-6f;
   int parts;
@@ -592,7 +610,7 @@ int launch_layer_norm_bwd(int act_dtype, const void* s, const void* dn, const fl
 #define MOE_LNB_CASE(T, V)                                                                    \
   hipLaunchKernelGGL((layer_norm_bwd_kernel<T, V>), dim3(grid), dim3(256), lds, st,           \
                      static_cast<const uint4*>(s), static_cast<const uint4*>(dn), gamma,      \
-                     static_cast<const uint4*>(dres), static_cast<uint4*>(dx), partial, M,    \
+                     static_cast<const uint4*>(dres), static_cast<uint4*>(dx), partial, M, M, \
                      vec_per_row, rows, eps)
   if (act_dtype == MOE_F32) {
     if (vpl <= 1) MOE_LNB_CASE(float, 1); else if (vpl <= 2) MOE_LNB_CASE(float, 2);

@@ -34,7 +34,7 @@ def xhat(s):
 
 # wavefronts up to 8 KB a row; blocks, two to four vectors a thread backward; any
 WIDTHS = [("bf16", M) for M in (8, 520, 4096, 4104, 8192, 8200, 12288, 12296, 16384, 16392, 40000)] + \
-         [("f32", M) for M in (4, 260, 2048, 2052, 4100, 8192, 8196, 20004)]
+         [("bf16", 1024)] + [("f32", M) for M in (4, 260, 520, 1024, 2048, 2052, 4100, 8192, 8196, 20004)]
 
 
 @pytest.mark.parametrize("dtype,M", WIDTHS)
