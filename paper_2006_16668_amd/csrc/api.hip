@@ -341,7 +341,8 @@ int vocab_bytes(const moe_config* cfg, const moe_vocab_dims* d, bool backward, s
   const int rc = check_vocab(cfg, d);
   if (rc != MOE_OK) return rc;
   if (bytes == nullptr) return MOE_EINVAL;
-  *bytes = moe::carve_vocab(*cfg, *d, true, backward).total;      // (a teacher's entries take 12 bytes a token more)
+  const bool teacher = d->K >= 1 && d->K <= 256;                // (a cross entropy, whose K is not read, takes less than any)
+  *bytes = moe::carve_vocab(*cfg, *d, teacher, backward).total;
   return MOE_OK;
 }
 

@@ -131,6 +131,17 @@ def test_argument_checks_of_the_c_calls():
     assert f(ctypes.byref(cfg), *[vp(ok)] * 8, sz(10), None) == -3
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_workspace_without_teacher_ignores_its_entries(dtype):
+    """K is not read for a cross entropy: whatever stands there, the sizes asked for serve one.  The size of a distillation's, large
+    enough for its entries to be sorted, grows with K."""
+    sh = moe.MoEShape(1, 8192, 1024, 64, 2, 1, dtype)
+    for f in (moe.moe_vocab_workspace_bytes, moe.moe_vocab_backward_workspace_bytes):
+        plain = f(sh, moe.VocabDims(64000))
+        assert all(f(sh, moe.VocabDims(64000, K=K)) == plain for K in (-1, -(1 << 31), 257, (1 << 31) - 1))
+        assert plain <= f(sh, moe.VocabDims(64000, K=32)) <= f(sh, moe.VocabDims(64000, K=256)) < plain + (1 << 26)
+
+
 def test_tensors_of_another_kind_are_refused():
     import torch
     sh, d = moe.MoEShape(1, 8, 64, 64, 2, 1, "bf16"), moe.VocabDims(100)
