@@ -116,7 +116,7 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
   int p_tile = first, p_kt = 0, p_steps = 0, p_more = 0, p_left = 0;
   uint32_t p_stage = 0;
   const bf16_t *p_a = nullptr, *p_b = nullptr;
-  uint32_t a_off[2][2], b_off[2][2];                           // [piece][copy] byte offsets of this lane from p_a, p_b
+  uint32_t a_off[2][2], b_off[2][2];                           // [piece][copy] byte offsets of this lane from p_a, p_b (255 rows of 2^24 bytes at most)
   auto set_sources = [&]() __attribute__((always_inline)) {
     p_more = 0;
     for (; p_tile < t_end; p_tile += stride) {
@@ -142,8 +142,8 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
           }
           const int pr = 8 * c + (lane >> 3), ch = (lane & 7) ^ ((pr >> 1) & 7);       // row of the piece
           const int row = 128 * h + pr, col = 64 * (pr >> 5) + 32 * h + (pr & 31);
-          if (!A_MNC) a_off[h][q] = (uint32_t)(((m0 + row < R ? row : R - 1 - m0) * g.lda + 8 * ch) * 2);
-          if (!B_MNC) b_off[h][q] = (uint32_t)(((n0 + col < g.N ? col : g.N - 1 - n0) * g.ldb + 8 * ch) * 2);
+          if (!A_MNC) a_off[h][q] = ((uint32_t)(m0 + row < R ? row : R - 1 - m0) * (uint32_t)g.lda + 8 * ch) * 2;
+          if (!B_MNC) b_off[h][q] = ((uint32_t)(n0 + col < g.N ? col : g.N - 1 - n0) * (uint32_t)g.ldb + 8 * ch) * 2;
         }
       break;
     }
