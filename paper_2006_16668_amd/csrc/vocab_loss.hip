@@ -25,7 +25,7 @@ namespace {
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
 
 // ---------------------------------------------------------------- rows with a target
-// perm[p] = the p-th token with a target, pos[n] = its p or -1, kept[0] their number.  A block of 1024 threads numbers 4096
+// perm[p] = the p-th token with a target, pos[n] = its p or -1, kept[0] their number.  A block of 1024 threads numbers its
 // tokens and counts those before them by itself: no order of blocks, one launch.
 struct VocabRowArgs {
   const int32_t* has;          // targets (a target is 0 .. entries - 1), or with entries 0: flags
@@ -58,35 +58,45 @@ __device__ void vocab_dx_ranges(const VocabRowArgs& a, int rows) {
   if (lane == __builtin_ctzll(__builtin_amdgcn_ballot_w64(us == best))) { a.kept[1] = n; a.kept[2] = k; }
 }
 // token n, whose target is `target`, is packed row p
-__device__ void vocab_row_data(const VocabRowArgs& a, int p, long long n, int32_t target) {
+struct TokenData { float lse, loss, dloss; };
+__device__ TokenData vocab_token_data(const VocabRowArgs& a, long long n) {
+  return TokenData{a.lse_in[n], a.hit != nullptr ? a.loss_in[n] : 0.f, a.dloss[n]};
+}
+__device__ void vocab_row_data(const VocabRowArgs& a, int p, long long n, int32_t target, const TokenData& d) {
   a.perm[p] = (int32_t)n;
   if (a.lse_in == nullptr) return;
-  const float g = a.dloss[n] * a.inv_t;
-  a.lse2[p] = a.lse_in[n] * kLog2e;
+  const float g = d.dloss * a.inv_t;
+  a.lse2[p] = d.lse * kLog2e;
   a.grad[p] = g;
   if (a.hit != nullptr) {                                      // exp(z - lse) - 1 at the target, where z - lse = -loss
     a.hit[p] = target;
-    a.hit_value[p] = expm1f(-a.loss_in[n]) * g;
+    a.hit_value[p] = expm1f(-d.loss) * g;
   }
 }
+// PER neighbouring tokens a thread.  One, for whole lines of all that is written, as long as counting the tokens before takes few
+// fetches (8336 tokens, all that a backward pass needs: four 9.5 us, one 4.8; 32768: 15.8 and 7.2); four where blocks are many.
+template <int PER>
 __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabRowArgs a) {
-  const long long first = (long long)blockIdx.x * (4 * kRowThreads);
+  const long long first = (long long)blockIdx.x * (PER * kRowThreads);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   auto valid = [&](int32_t v) { return a.entries != 0 ? (uint32_t)v < (uint32_t)a.entries : v != 0; };
-  int before = 0;
+  const long long n0 = first + PER * tid;
+  int32_t v[PER];
+  TokenData data[PER] = {};
+  int own = 0, before = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const long long n = n0 + i < a.N ? n0 + i : a.N - 1;
+    v[i] = a.has[n];
+    if (a.lse_in != nullptr) data[i] = vocab_token_data(a, n);
+  }
 #pragma unroll 8
   for (long long i = 4 * tid; i < first; i += 4 * kRowThreads) {
-    const int4 v = *reinterpret_cast<const int4*>(a.has + i);
-    before += (int)valid(v.x) + (int)valid(v.y) + (int)valid(v.z) + (int)valid(v.w);
+    const int4 u = *reinterpret_cast<const int4*>(a.has + i);
+    before += (int)valid(u.x) + (int)valid(u.y) + (int)valid(u.z) + (int)valid(u.w);
   }
-  const long long n0 = first + 4 * tid;
-  int32_t v[4];
-  int own = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[i] = n0 + i < a.N ? a.has[n0 + i] : (a.entries != 0 ? -1 : 0);
-    own += (int)valid(v[i]);
-  }
+  for (int i = 0; i < PER; ++i) own += (int)(n0 + i < a.N && valid(v[i]));
   int incl = own;                                              // within the wavefront, then of the wavefronts before
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -103,12 +113,8 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabRowArgs a)
     p += sums[kRowWaves + w] + (w < wave ? sums[w] : 0);
     total += sums[kRowWaves + w] + sums[w];
   }
-  if (blockIdx.x == gridDim.x - 1 && wave == 0) {
-    if (lane == 0) a.kept[0] = total;
-    if (a.dx_entries != 0) vocab_dx_ranges(a, total);
-  }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < PER; ++i) {
     const long long n = n0 + i;
     if (n >= a.N) break;
     const bool ok = valid(v[i]);
@@ -117,8 +123,12 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabRowArgs a)
       if (a.loss != nullptr) { a.loss[n] = 0.f; a.lse[n] = 0.f; }
       continue;
     }
-    vocab_row_data(a, p, n, v[i]);
+    vocab_row_data(a, p, n, v[i], data[i]);
     ++p;
+  }
+  if (blockIdx.x == gridDim.x - 1 && wave == kRowWaves - 1) {  // (the wavefront with the fewest tokens)
+    if (lane == 0) a.kept[0] = total;
+    if (a.dx_entries != 0) vocab_dx_ranges(a, total);
   }
 }
 
@@ -259,6 +269,7 @@ __global__ __launch_bounds__(256) void vocab_few_kernel(VocabRowArgs a, TeacherA
                                                         float* __restrict__ z, uint4* __restrict__ packed) {
   const int n = blockIdx.x, N = (int)a.N, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   __shared__ int has[kFewTokens];
+  const TokenData data = threadIdx.x == 0 && a.lse_in != nullptr ? vocab_token_data(a, n) : TokenData{0.f, 0.f, 0.f};
   if (t.K == 0) {
     if (threadIdx.x < N) has[threadIdx.x] = (uint32_t)a.has[threadIdx.x] < (uint32_t)a.entries;
   } else {
@@ -280,7 +291,7 @@ __global__ __launch_bounds__(256) void vocab_few_kernel(VocabRowArgs a, TeacherA
   if (threadIdx.x == 0) {
     if (n == 0) a.kept[0] = rows;
     if (a.pos != nullptr) a.pos[n] = ok ? p : -1;
-    if (ok) vocab_row_data(a, p, n, t.K == 0 ? a.has[n] : 0);
+    if (ok) vocab_row_data(a, p, n, t.K == 0 ? a.has[n] : 0, data);
     else if (a.loss != nullptr) { a.loss[n] = 0.f; a.lse[n] = 0.f; }
   }
   if (n == 0 && wave == 0 && a.dx_entries != 0) vocab_dx_ranges(a, rows);
@@ -538,8 +549,9 @@ static int launch_few(const moe_config& c, const VocabRowArgs& r, const TeacherA
   return check_launch();
 }
 static int launch_rows(const VocabRowArgs& r, hipStream_t st) {
-  constexpr int kTokens = 4 * kRowThreads;
-  hipLaunchKernelGGL(vocab_rows_kernel, dim3((unsigned)((r.N + kTokens - 1) / kTokens)), dim3(kRowThreads), 0, st, r);
+  const int per = r.N <= 64 * kRowThreads ? 1 : 4, tokens = per * kRowThreads;
+  hipLaunchKernelGGL(per == 1 ? vocab_rows_kernel<1> : vocab_rows_kernel<4>, dim3((unsigned)((r.N + tokens - 1) / tokens)),
+                     dim3(kRowThreads), 0, st, r);
   return check_launch();
 }
 
