@@ -341,8 +341,11 @@ int vocab_bytes(const moe_config* cfg, const moe_vocab_dims* d, bool backward, s
   const int rc = check_vocab(cfg, d);
   if (rc != MOE_OK) return rc;
   if (bytes == nullptr) return MOE_EINVAL;
-  const bool teacher = d->K >= 1 && d->K <= 256;                // (a cross entropy, whose K is not read, takes less than any)
-  *bytes = moe::carve_vocab(*cfg, *d, teacher, backward).total;
+  *bytes = moe::carve_vocab(*cfg, *d, false, backward).total;
+  if (d->K >= 1 && d->K <= 256) {                               // (a cross entropy's is not read)
+    const size_t teacher = moe::carve_vocab(*cfg, *d, true, backward).total;
+    if (teacher > *bytes) *bytes = teacher;
+  }
   return MOE_OK;
 }
 

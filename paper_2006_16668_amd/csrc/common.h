@@ -160,8 +160,8 @@ struct VocabRows {
   const int32_t* hit = nullptr;        // NULL, or the entry whose gradient is hit_value instead
   const float* hit_value = nullptr;
   int first = 0;                       // entry of the product's first column
-  // NULL, or a teacher's entries by 256 x 256 tiles: where a tile's start (row tiles of 256 K, column tiles + 1), each its row << 8 |
-  // column in the tile and its place in entry_logit, which receives its logit
+  // NULL, or a teacher's entries by 256 x 256 tiles and wavefronts: where a list starts (row tiles of 256 K, 8 column tiles + 1),
+  // each entry's row << 8 | column in the tile and its place in entry_logit, which receives its logit
   const int32_t* starts = nullptr;
   const uint2* sorted = nullptr;
   float* entry_logit = nullptr;
@@ -291,8 +291,10 @@ int launch_gemm_f32(GemmKind kind, const GemmArgs& a, int E, int R, int N, int K
 // count, entries = those of a piece.  dz lies in rows of a multiple of 256 and holds zeros up to the next whole 16 bytes and in the
 // rows up to the next whole 64 (rows up to whole 256 exist).
 //   z = a.A[a.gather] . a.B^T: a.vocab.stats, or dz in a.C (rows of a.ldc)
-bool vocab_logits_on_tiles(int rows, int entries, int M, bool pack);   // pack: x is packed for it alone, and gather is NULL
-int vocab_stat_slots(int rows, int entries, int M);
+//   pack: x is packed for it alone, and gather is NULL; saved: us of other work that is left out then.  With a.vocab.starts on
+//   tiles in any case.
+bool vocab_logits_on_tiles(int rows, int entries, int M, bool pack, double saved);
+int vocab_stat_slots(int rows, int entries, int M, double saved);
 int launch_vocab_logits(const GemmArgs& a, int rows, int entries, int M, hipStream_t st);
 //   dx: C [splits, rows, M] fp32 = (or +=) sums over the plan's ranges of A [rows, lda] . B [entries, M]
 struct VocabDxPlan { int splits, k; bool tiles; };     // ranges, length of each (the last may be shorter)

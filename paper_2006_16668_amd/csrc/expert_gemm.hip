@@ -1673,22 +1673,22 @@ constexpr double kEdgeLogits = 1.09, kEdgeDw = 1.05;
 static GemmForm vocab_logits_form(int rows, int entries, int M, double* us = nullptr) {
   return gemm_form(false, 1, rows, entries, M, kLayoutDataGrad, kPlanUnits, us);
 }
-bool vocab_logits_on_tiles(int rows, int entries, int M, bool pack) {
+bool vocab_logits_on_tiles(int rows, int entries, int M, bool pack, double saved) {
   if (M <= 64) return false;                                   // (two steps at least)
   double us = 0;
   vocab_logits_form(rows, entries, M, &us);
   // (the edge kernel gathers the rows of x by itself, the tiles' are packed: one more launch)
   const double packing = pack ? 4.0 + 4e-6 * rows * M / 5.0 : 0.0;
-  return vocab_tiles_time(kTilesLogits, (long long)tiles_of(rows) * tiles_of(entries), M, 0) + packing < kEdgeLogits * us;
+  return vocab_tiles_time(kTilesLogits, (long long)tiles_of(rows) * tiles_of(entries), M, 0) + packing < kEdgeLogits * us + saved;
 }
-int vocab_stat_slots(int rows, int entries, int M) {
-  if (vocab_logits_on_tiles(rows, entries, M, true)) return tiles_of(entries);
+int vocab_stat_slots(int rows, int entries, int M, double saved) {
+  if (vocab_logits_on_tiles(rows, entries, M, true, saved)) return tiles_of(entries);
   const int bn = form_costs(kLayoutDataGrad)[vocab_logits_form(rows, entries, M)].bn;
   return 2 * ((entries + bn - 1) / bn);
 }
 int launch_vocab_logits(const GemmArgs& a, int rows, int entries, int M, hipStream_t st) {
   const bool stats = a.vocab.stats != nullptr;
-  if (vocab_logits_on_tiles(rows, entries, M, stats)) return launch_vocab_tiles_logits(a, rows, entries, M, st);
+  if (a.vocab.starts != nullptr || vocab_logits_on_tiles(rows, entries, M, stats, 0.0)) return launch_vocab_tiles_logits(a, rows, entries, M, st);
   const GemmForm form = vocab_logits_form(rows, entries, M);
   return stats ? gemm_bf16_edge<kEpiStats, false, true>(form, a, 1, rows, entries, M, st)
                : gemm_bf16_edge<kEpiLogitGrad, false, true>(form, a, 1, rows, entries, M, st);

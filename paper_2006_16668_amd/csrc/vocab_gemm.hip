@@ -285,8 +285,9 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
     tile_at(tile, e, rt, ct);
     const int m0 = rt * 256, n0 = ct * 256;
     const int steps = (range_k(e) + 63) >> 6;
-    // kStats: the tile's teacher entries.  Where they are is asked in its first step, the first 64 of them are copied, as 128 words,
-    // to A1's place in the last one (read by all when phase 4 begins, free until the next tile's phase 2).
+    // kStats: the teacher's entries among this wavefront's results.  Where they are is fetched in the tile's first step, into the
+    // wavefront's staging (as copy_row_data), the first 256 of them are copied to A1's place in the last one (read by all when phase 4
+    // begins, free until the next tile's phase 2).
     int entries = 0;
     const uint2* list = nullptr;
     uint32_t list_at = 0;
@@ -309,21 +310,20 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
       read_a(1);
       if (!landed) asm volatile("s_waitcnt vmcnt(2)" ::: "memory");
       if (EPI == kLogitGrad && decltype(first_step)::value) copy_row_data(m0);
-      if (EPI == kStats && decltype(first_step)::value && g.v.starts != nullptr) {
-        typedef const int __attribute__((address_space(4))) * scalar_ptr;
-        const scalar_ptr start = (scalar_ptr)(uintptr_t)(g.v.starts + (size_t)rt * (tiles_n + 1) + ct);
-        const int found = start[0];
-        entries = start[1] - found;
-        list = g.v.sorted + (size_t)m0 * g.v.K + found;
-      }
+      if (EPI == kStats && decltype(first_step)::value && g.v.starts != nullptr)
+        MOE_VG_WORDS(lds0 + kStaging + wave * 4096, g.v.starts + (size_t)rt * (8 * tiles_n + 1) + 8 * ct + wave + lane_here());
       copy_b();
       turn(first_step, 1, 1);
       // phase 4
-      if (EPI == kStats && kt + 1 == steps && entries > 0) {
+      if (EPI == kStats && !decltype(first_step)::value && kt + 1 == steps && g.v.starts != nullptr) {
+        const u32x2_t start = *(lds_u2_ptr)(uintptr_t)(lds0 + kStaging + wave * 4096);
+        const int found = __builtin_amdgcn_readfirstlane((int)start[0]);
+        entries = __builtin_amdgcn_readfirstlane((int)start[1]) - found;
+        list = g.v.sorted + (size_t)m0 * g.v.K + found;
         list_at = lds0 + (to_other == kStage ? 0 : kStage) + kPiece + wave * 2048;
         const uint32_t* const from = reinterpret_cast<const uint32_t*>(list) + lane_here();
-        MOE_VG_WORDS(list_at, from);
-        MOE_VG_WORDS(list_at + 256, from + 64);
+#pragma unroll 1
+        for (int c = 0; c < 8 && 32 * c < entries; ++c) MOE_VG_WORDS(list_at + 256 * c, from + 64 * c);
       }
       other_stage();
       if (kt + 1 < steps) read_a(0);
@@ -350,36 +350,52 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
     const int lane = lane_here(), r32 = lane & 31, hh = lane >> 5;
     auto col_of = [&](int j) { return B_MNC ? 128 * j + 32 * wn : 64 * wn + 32 * j; };
     if constexpr (EPI == kStats) {
-      // Logits at a teacher's entries: of each 32 x 32 part that has any of the 64 at hand, its results pass through LDS (the
-      // register that holds an entry's differs from lane to lane).
-      for (int at = 0; at < entries; at += 64) {
-        uint2 entry = {0xffffffffu, 0u};
-        if (at + lane < entries) {
-          if (at == 0) {
-            const u32x2_t e = *(lds_u2_ptr)(uintptr_t)(list_at + 8 * lane);
-            entry = uint2{e[0], e[1]};
-          } else {
-            entry = list[at + lane];
+      // Logits at a teacher's entries, 256 at a time: each 32 x 32 part of the wavefront's that has any passes through LDS (the
+      // register that holds an entry's logit differs from lane to lane).
+      for (int done = 0; done < entries; done += 256) {
+        const int n = entries - done < 256 ? entries - done : 256;
+        if (done > 0)
+          for (int at = lane; at < n; at += 64) {
+            const uint2 e = list[done + at];
+            *(lds_u2_ptr)(uintptr_t)(list_at + 8 * at) = u32x2_t{e.x, e.y};
           }
-        }
-        const uint32_t row = entry.x >> 8, col = entry.x & 255;
-        const bool mine = (int)entry.x >= 0 && (int)((row >> 6) & 1) == wm && (int)(col >> 6) == wn;
-        const int part = (int)(4 * (row >> 7) + 2 * ((row >> 5) & 1) + ((col >> 5) & 1));
+        __builtin_amdgcn_wave_barrier();
+        // the first 64 in registers (there are seldom more), of the others the parts that they lie in
+        auto part_of = [](uint32_t x) { return (int)(4 * (x >> 15 & 1) + 2 * (x >> 13 & 1) + (x >> 5 & 1)); };
         const uint32_t st = lds0 + kStaging + wave * 4096;
-        const uint32_t from = st + ((col >> 3) & 3) * 1024 + ((row & 31) + 32 * ((col >> 2) & 1)) * 16 + (col & 3) * 4;
+        auto store = [&](u32x2_t e) __attribute__((always_inline)) {
+          const uint32_t row = e[0] >> 8, col = e[0] & 255;
+          g.v.entry_logit[e[1]] = *(lds_f_ptr)(uintptr_t)(st + ((col >> 3) & 3) * 1024 +
+                                                          ((row & 31) + 32 * ((col >> 2) & 1)) * 16 + (col & 3) * 4);
+        };
+        u32x2_t entry = {0u, 0u};
+        if (lane < n) entry = *(lds_u2_ptr)(uintptr_t)(list_at + 8 * lane);
+        const int part = lane < n ? part_of(entry[0]) : -1;
+        int more = 0;
+#pragma unroll 1
+        for (int at = 64; at < n; at += 64) {
+          const int p = at + lane < n ? part_of((*(lds_u2_ptr)(uintptr_t)(list_at + 8 * (at + lane)))[0]) : -1;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) more |= __builtin_amdgcn_ballot_w64(p == k) != 0 ? 1 << k : 0;
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            const bool here = mine && part == 2 * i + j;
-            if (__builtin_amdgcn_ballot_w64(here) == 0) continue;
+            const bool here = part == 2 * i + j;
+            if (__builtin_amdgcn_ballot_w64(here) == 0 && (more >> (2 * i + j) & 1) == 0) continue;
 #pragma unroll
             for (int q = 0; q < 4; ++q)
               *(lds_u4_ptr)(uintptr_t)(st + q * 1024 + lane * 16) =
                   u32x4_t{__float_as_uint(acc[i][j][4 * q]), __float_as_uint(acc[i][j][4 * q + 1]),
                           __float_as_uint(acc[i][j][4 * q + 2]), __float_as_uint(acc[i][j][4 * q + 3])};
             __builtin_amdgcn_wave_barrier();
-            if (here) g.v.entry_logit[entry.y] = *(lds_f_ptr)(uintptr_t)from;
+            if (here) store(entry);
+#pragma unroll 1
+            for (int at = 64 + lane; at < n; at += 64) {
+              const u32x2_t e = *(lds_u2_ptr)(uintptr_t)(list_at + 8 * at);
+              if (part_of(e[0]) == 2 * i + j) store(e);
+            }
             __builtin_amdgcn_wave_barrier();
           }
       }

@@ -209,19 +209,20 @@ __global__ __launch_bounds__(256) void vocab_teacher_kernel(TeacherArgs t, const
     entry_logits<T>(t, n, x, w, pieces, z, (threadIdx.x >> 4) & 3, 4);
   }
 }
-// The entries of the packed rows in the order of the product's 256 x 256 tiles, so that each tile finds its own (a handful, where
-// their dot products one by one would read a row of w each: 8192 tokens, M 1024, 32 entries 86 us).  A block per row tile; the
-// entries of a tile come in no fixed order, which no result depends on.
+// The entries of the packed rows in the order of the product's 256 x 256 tiles and their eight wavefronts, so that each finds its
+// own (a handful, where their dot products one by one would read a row of w each: 8192 tokens, M 1024, 32 entries 86 us).  A block
+// per row tile; the entries of a wavefront come in no fixed order, which no result depends on.
 __global__ __launch_bounds__(1024) void vocab_sort_kernel(TeacherArgs t, const int32_t* __restrict__ perm,
-                                                          const int32_t* __restrict__ kept, int tiles_n,
+                                                          const int32_t* __restrict__ kept, int lists,
                                                           int32_t* __restrict__ starts, uint2* __restrict__ sorted) {
-  extern __shared__ int place[];                               // [tiles_n] counts, then where the next entry goes
+  extern __shared__ int place[];                               // [lists] counts, then where the next entry goes
   __shared__ int sums[16];
   const int p0 = blockIdx.x * 256, rows = kept[0], tid = threadIdx.x, lane = tid & 63;
   if (p0 >= rows) return;
   const int entries = (rows - p0 < 256 ? rows - p0 : 256) * t.K;
-  for (int i = tid; i < tiles_n; i += 1024) place[i] = 0;
+  for (int i = tid; i < lists; i += 1024) place[i] = 0;
   __syncthreads();
+  auto list_of = [](int r, int i) { return 8 * (i >> 8) + 4 * (r >> 6 & 1) + (i >> 6 & 3); };      // tile, wavefront
   auto each = [&](auto take) {
     for (int e = tid; e < entries; e += 1024) {
       const int r = e / t.K, k = e - r * t.K;
@@ -230,12 +231,12 @@ __global__ __launch_bounds__(1024) void vocab_sort_kernel(TeacherArgs t, const i
       if (teacher_has(t, i, t.logit[at])) take(r, i, (uint32_t)at);
     }
   };
-  each([&](int, int i, uint32_t) { atomicAdd(&place[i >> 8], 1); });
+  each([&](int r, int i, uint32_t) { atomicAdd(&place[list_of(r, i)], 1); });
   __syncthreads();
-  // running counts: a thread's stretch of tiles, the stretches in a wavefront, the wavefronts
-  const int per = (tiles_n + 1023) / 1024, b0 = tid * per;
+  // running counts: a thread's stretch of lists, the stretches in a wavefront, the wavefronts
+  const int per = (lists + 1023) / 1024, b0 = tid * per;
   int own = 0;
-  for (int i = b0; i < b0 + per && i < tiles_n; ++i) own += place[i];
+  for (int i = b0; i < b0 + per && i < lists; ++i) own += place[i];
   int incl = own;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -246,19 +247,19 @@ __global__ __launch_bounds__(1024) void vocab_sort_kernel(TeacherArgs t, const i
   __syncthreads();
   int run = incl - own;
   for (int w = 0; w < (tid >> 6); ++w) run += sums[w];
-  int32_t* const mine = starts + (size_t)blockIdx.x * (tiles_n + 1);
-  for (int i = b0; i < b0 + per && i < tiles_n; ++i) {
+  int32_t* const mine = starts + (size_t)blockIdx.x * (lists + 1);
+  for (int i = b0; i < b0 + per && i < lists; ++i) {
     const int n = place[i];
     place[i] = mine[i] = run;
     run += n;
   }
-  if (tid == 1023) mine[tiles_n] = run;                        // (of all: its stretch is the last, empty or not)
+  if (tid == 1023) mine[lists] = run;                          // (of all: its stretch is the last, empty or not)
   __syncthreads();
   each([&](int r, int i, uint32_t at) {
-    sorted[(size_t)p0 * t.K + atomicAdd(&place[i >> 8], 1)] = uint2{(uint32_t)(r << 8 | (i & 255)), at};
+    sorted[(size_t)p0 * t.K + atomicAdd(&place[list_of(r, i)], 1)] = uint2{(uint32_t)(r << 8 | (i & 255)), at};
   });
 }
-constexpr int kSortTiles = 16000;                              // column tiles whose counts fit 64 KB of LDS
+constexpr int kSortTiles = 2000;                               // column tiles whose counts fit 64 KB of LDS
 
 // Up to 64 tokens, a block each: what vocab_teacher_kernel, vocab_rows_kernel and vocab_pack_kernel do, in one launch.  Every block
 // looks at all tokens to number its own.
@@ -470,10 +471,21 @@ VocabPieces vocab_pieces(const moe_config& c, const moe_vocab_dims& d) {
   return p;
 }
 
-// Whether the product of the logits leaves those at the teacher's entries: for more than 100 MB of rows of w, about the time of the
-// sort and of the tiles' looks at it (8192 tokens, M 1024, V 64000, 32 entries: 952 -> 911 us)
-static bool vocab_sorts(const moe_config& c, const moe_vocab_dims& d) {
-  return (d.V + 255) / 256 <= kSortTiles && 2LL * c.G * c.S * d.K * c.M > 100000000LL;
+// The product of the logits on tiles leaves those at the teacher's entries too.  Asked one by one they read as many rows of w, 6 GB a
+// ms; the sort and the tiles' looks at it take about 16 us: worth it for more than 100 MB (8192 tokens, M 1024, V 64000, 32 entries
+// 952 -> 911 us), and then also a reason for tiles (13384 tokens, M 1256, V 1630, 25 entries 148 -> 98 us).  us saved, or 0: not sorted.
+static double vocab_sort_saves(const moe_config& c, const moe_vocab_dims& d) {
+  const double bytes = 2.0 * c.G * c.S * d.K * c.M;
+  return (d.V + 255) / 256 <= kSortTiles && bytes > 1e8 ? bytes / 6e6 - 16.0 : 0.0;
+}
+// How the forward pass goes about the logits
+struct VocabForwardPlan { bool packs, sorts; int slots; };
+static VocabForwardPlan forward_plan(const moe_config& c, const moe_vocab_dims& d, bool teacher) {
+  const int N = c.G * c.S;
+  if (c.act_dtype == MOE_F32) return {false, false, vocab_stat_slots_f32(N, d.V, c.M)};
+  const double saved = teacher ? vocab_sort_saves(c, d) : 0.0;
+  const bool packs = vocab_logits_on_tiles(N, d.V, c.M, true, saved);
+  return {packs, packs && saved > 0, vocab_stat_slots(N, d.V, c.M, saved)};
 }
 
 VocabWs carve_vocab(const moe_config& c, const moe_vocab_dims& d, bool teacher, bool backward) {
@@ -482,18 +494,17 @@ VocabWs carve_vocab(const moe_config& c, const moe_vocab_dims& d, bool teacher, 
   VocabWs w{};
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes, 256); return o; };
-  const bool packs = c.act_dtype == MOE_BF16 && vocab_logits_on_tiles((int)N, d.V, c.M, true);
   const size_t whole = align_up(N, 256);                       // rows in whole tiles
   w.kept = take(12);
   w.perm = take(N * 4);
   w.tstat = take(teacher ? N * 8 : 0);
   w.has = take(teacher ? N * 4 : 0);
   if (!backward) {
-    w.slots = c.act_dtype == MOE_F32 ? vocab_stat_slots_f32((int)N, d.V, c.M) : vocab_stat_slots((int)N, d.V, c.M);
-    w.packed = take(packs ? whole * c.M * elt : 0);
-    const bool sorts = packs && teacher && vocab_sorts(c, d);
-    w.starts = take(sorts ? whole / 256 * ((d.V + 255) / 256 + 1) * 4 : 0);
-    w.sorted = take(sorts ? (N * d.K + 64) * 8 : 0);             // (a tile fetches 64)
+    const VocabForwardPlan f = forward_plan(c, d, teacher);
+    w.slots = f.slots;
+    w.packed = take(f.packs ? whole * c.M * elt : 0);
+    w.starts = take(f.sorts ? (whole / 256 * ((size_t)8 * ((d.V + 255) / 256) + 1) + 64) * 4 : 0);      // (a wavefront fetches 64)
+    w.sorted = take(f.sorts ? (N * d.K + 64) * 8 : 0);             // (a wavefront fetches whole 32)
     w.stats = take((size_t)w.slots * N * 8);
   } else {
     w.pos = take(N * 4);
@@ -574,8 +585,8 @@ int launch_vocab_forward(const moe_config& c, const moe_vocab_dims& d, const Voc
   VocabRowArgs r = row_args(c, d, a, base, ws);
   r.loss = a.loss;
   r.lse = a.lse;
-  const bool packs = !f32 && vocab_logits_on_tiles((int)N, d.V, c.M, true);
-  const bool sorts = packs && a.target == nullptr && vocab_sorts(c, d);
+  const VocabForwardPlan plan = forward_plan(c, d, a.target == nullptr);
+  const bool packs = plan.packs, sorts = plan.sorts;
   // a row tile of the edge kernel takes as long whether all its tokens have a target or not: no need to number them
   const bool few = N <= kFewTokens && !packs, all = few && a.target != nullptr && !f32;
   if (few) {
@@ -585,9 +596,9 @@ int launch_vocab_forward(const moe_config& c, const moe_vocab_dims& d, const Voc
     if (rc == MOE_OK) rc = launch_rows(r, st);
     if (rc == MOE_OK && packs) rc = launch_pack(c, a.x, base + ws.packed, r, st);
     if (rc == MOE_OK && sorts) {
-      const int tiles_n = (d.V + 255) / 256;
-      hipLaunchKernelGGL(vocab_sort_kernel, dim3((unsigned)((N + 255) / 256)), dim3(1024), (size_t)tiles_n * sizeof(int), st, t,
-                         r.perm, r.kept, tiles_n, reinterpret_cast<int32_t*>(base + ws.starts),
+      const int lists = 8 * ((d.V + 255) / 256);
+      hipLaunchKernelGGL(vocab_sort_kernel, dim3((unsigned)((N + 255) / 256)), dim3(1024), (size_t)lists * sizeof(int), st, t,
+                         r.perm, r.kept, lists, reinterpret_cast<int32_t*>(base + ws.starts),
                          reinterpret_cast<uint2*>(base + ws.sorted));
       rc = check_launch();
     }

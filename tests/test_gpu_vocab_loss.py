@@ -134,7 +134,9 @@ KD = [(1, 64, 72, 300, 20, 2.0, "bf16", 0.5, 0), (5, 8, 132, 700, 3, 1.5, "f32",
       (2, 65, 72, 257, 16, 2.0, "bf16", 0.3, 0), (1, 200, 136, 1500, 65, 3.0, "bf16", 0.1, 256), (1, 77, 68, 700, 256, 1.0, "f32", 0.1, 256),
       (1, 1, 1024, 4001, 31, 4.0, "bf16", 0, 0), (2, 1100, 256, 2999, 32, 2.0, "bf16", 0.1, 0),
       # the product leaves the logits at the entries (test_vocab_rules.py)
-      (1, 2500, 1024, 16001, 32, 2.0, "bf16", 0.2, 0), (3, 700, 520, 31011, 256, 1.0, "bf16", 0.1, 8192), (1, 4096, 256, 33000, 100, 3.0, "bf16", 0, 0)]
+      (1, 2500, 1024, 16001, 32, 2.0, "bf16", 0.2, 0), (3, 700, 520, 31011, 256, 1.0, "bf16", 0.1, 8192), (1, 4096, 256, 33000, 100, 3.0, "bf16", 0, 0),
+      # a product that is on tiles for that reason
+      (1, 6011, 520, 1111, 40, 2.0, "bf16", 0.4, 0)]
 
 
 @pytest.mark.parametrize("G,S,M,V,K,T,dtype,empty,piece", KD)

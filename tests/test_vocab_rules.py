@@ -20,7 +20,14 @@ def _f(mangled, restype, n):
     return f
 
 
-logits_on_tiles = _f("_ZN3moe21vocab_logits_on_tilesEiiib", ctypes.c_bool, 4)
+_on_tiles = _f("_ZN3moe21vocab_logits_on_tilesEiiibd", ctypes.c_bool, 4)
+_on_tiles.argtypes = [ctypes.c_int] * 4 + [ctypes.c_double]
+
+
+def logits_on_tiles(rows, entries, M, pack, saved=0.0):
+    return _on_tiles(rows, entries, M, pack, saved)
+
+
 dx_plan = _f("_ZN3moe13vocab_dx_planEiii", DxPlan, 3)
 dw_on_tiles = _f("_ZN3moe17vocab_dw_on_tilesEiii", ctypes.c_bool, 3)
 
@@ -59,8 +66,10 @@ def test_cases_reach_every_kernel():
             seen.add(("dx tail", n % 64 != 0 or V % n % 64 != 0))
     assert seen == {(k, b) for k in ("z", "dz", "dx", "dx ranges", "dw", "dz tail", "dz empty") for b in (True, False)} | \
         {("dx tail", b) for b in (True, False)}
-    # the product leaves the logits at a teacher's entries: more than 100 MB of w's rows
-    assert any(logits_on_tiles(G * S, V, M, True) and 2 * G * S * K * M > 1e8 for G, S, M, V, K, T, dtype, e, p in KD if dtype == "bf16")
+    # the product leaves the logits at a teacher's entries: more than 100 MB of w's rows, on tiles in any case or because of them
+    sorts = [(G * S, V, M, True, 2 * G * S * K * M / 6e6 - 16) for G, S, M, V, K, T, dtype, e, p in KD
+             if dtype == "bf16" and 2 * G * S * K * M > 1e8]
+    assert {logits_on_tiles(*s[:4]) for s in sorts if logits_on_tiles(*s)} == {True, False}
 
 
 def test_what_the_entry_points_refuse():
