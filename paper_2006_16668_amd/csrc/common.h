@@ -302,7 +302,11 @@ VocabDxPlan vocab_dx_plan(int rows, int entries, int M);
 VocabDxPlan vocab_dx_plan_f32(int rows, int entries, int M);           // gemm_f32.hip
 int vocab_stat_slots_f32(int rows, int entries, int M);
 int launch_vocab_dx(const GemmArgs& a, const VocabDxPlan& p, int rows, int M, hipStream_t st);
-//   dw: C [entries, M] = A [rows, lda]^T . B [rows, M], which has rows of zeros like dz
+//   dw: C [entries, M] = A [rows, lda]^T . B [rows, M], which has rows of zeros like dz; with a.k_total > 1 fp32
+//   [a.k_total, entries, M], sums over as many ranges of row_range() rows
+__host__ __device__ inline int row_range(int rows, int ranges) { return ((rows + ranges - 1) / ranges + 63) / 64 * 64; }
+int vocab_dw_splits(int rows, int entries, int M);
+int vocab_dw_splits_f32(int rows, int entries, int M);                 // gemm_f32.hip
 bool vocab_dw_on_tiles(int rows, int entries, int M);
 int launch_vocab_dw(const GemmArgs& a, int rows, int entries, int M, hipStream_t st);
 int launch_vocab_grads_pair(const GemmArgs& dx, const VocabDxPlan& p, const GemmArgs& dw, int rows, int entries, int M,
@@ -333,9 +337,10 @@ int launch_vocab_tiles_dw(const GemmArgs& a, int entries, int M, hipStream_t st)
 struct VocabPieces { int entries, count; };    // of the vocabulary; a piece's entries are whole 256, the last may have fewer
 VocabPieces vocab_pieces(const moe_config& c, const moe_vocab_dims& d);
 struct VocabWs {
-  size_t kept, perm, tstat, has, stats, starts, sorted, pos, lse2, grad, hit, hit_value, packed, dz, sums, total;
+  size_t kept, perm, tstat, has, stats, starts, sorted, pos, lse2, grad, hit, hit_value, packed, dz, sums, dw_sums, total;
   int slots;                           // of stats
   VocabDxPlan dx_plan;                 // of a whole piece
+  int dw_splits;                       // likewise
 };
 VocabWs carve_vocab(const moe_config& c, const moe_vocab_dims& d, bool teacher, bool backward);
 struct VocabCall {                     // target: cross entropy, else the teacher's entries

@@ -636,7 +636,8 @@ constexpr int kEpiRangesIfAny = 7;     // 3 with a k_total, else 0; kept is K_KE
 //     C = the gradient with respect to z, bf16 in rows of ldc, with zeros in the columns N .. of the last 16
 //     bytes and in the rows behind the last of a tile (kEpiLogitGrad)
 //   dx = dz . w: A in rows of lda, "expert" e sums the k from e K on, up to k_total; C[e] fp32, or is added to
-//   dw = dz^T . x: A in rows of lda, a plain bf16 result
+//   dw = dz^T . x: A in rows of lda, a plain bf16 result (kEpiPitch), or sums over as many ranges of the rows as k_total says,
+//     "expert" e the e-th in C[e] fp32 (kEpiSums with K_KEPT): the ranges are alike for the rows that there are
 // (a.kept NULL: all rows count)
 constexpr int kEpiStats = 8, kEpiLogitGrad = 9, kEpiSums = 10, kEpiPitch = 11;
 
@@ -644,11 +645,12 @@ template <int BM, int BN, int BK, int ST, int EPI, bool A_MNC, bool B_KC, bool K
 __device__ __forceinline__ void edge_tile(const EdgeArgs& arg, const int logical) {
   const bf16_t *const __restrict__ A = arg.A, *const __restrict__ B = arg.B, *const __restrict__ mask = arg.mask;
   bf16_t* const __restrict__ Cout = arg.C;
-  const int R = arg.R, N = arg.N, K = arg.K, tiles_m = arg.tiles_m, tiles_n = arg.tiles_n, row_pad = arg.row_pad;
+  constexpr bool ROW_SUMS = EPI == kEpiSums && K_KEPT;
+  const int R = arg.R, N = arg.N, K = ROW_SUMS ? row_range(arg.kept[0], arg.k_total) : arg.K, tiles_m = arg.tiles_m, tiles_n = arg.tiles_n, row_pad = arg.row_pad;
   const int32_t *const __restrict__ gather = arg.gather, *const __restrict__ kept = arg.kept, *const __restrict__ scatter = arg.scatter;
   const int k_total = arg.k_total;
-  constexpr bool LOGITS = EPI == kEpiStats || EPI == kEpiLogitGrad, SUMS = EPI == kEpiSums;
-  const int lda = SUMS || EPI == kEpiPitch ? arg.lda : A_MNC ? R : K;
+  constexpr bool LOGITS = EPI == kEpiStats || EPI == kEpiLogitGrad, SUMS = EPI == kEpiSums && !K_KEPT;
+  const int lda = EPI == kEpiSums || EPI == kEpiPitch ? arg.lda : A_MNC ? R : K;
   const bool masked = EPI == 2 || (EPI == kEpiMaskIfAny && mask != nullptr);
   const bool ranges = EPI == 3 || (EPI == kEpiRangesIfAny && k_total != 0);
   const bool k_kept = K_KEPT || (EPI == kEpiRangesIfAny && kept != nullptr);
@@ -685,7 +687,8 @@ __device__ __forceinline__ void edge_tile(const EdgeArgs& arg, const int logical
     rows_out = rows_out < R ? rows_out : R;
   }
   if (m0 >= rows_out) return;                                  // block-uniform
-  int KE = k_kept ? kept[e] : K;                               // length of the sum
+  int KE = ROW_SUMS ? kept[0] - e * K : k_kept ? kept[e] : K;  // length of the sum
+  if (ROW_SUMS) KE = KE < 0 ? 0 : KE < K ? KE : K;
   if (ranges || SUMS) KE = k_total - e * K < K ? k_total - e * K : K;
   const int KT = (KE + BK - 1) / BK;
 
@@ -956,7 +959,7 @@ __device__ __forceinline__ void edge_tile(const EdgeArgs& arg, const int logical
                              ? __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], c, -lse)) * up : 0.f;
     }
   }
-  if constexpr (SUMS) {
+  if constexpr (EPI == kEpiSums) {
     typedef float f32x4_t __attribute__((ext_vector_type(4)));
     float* const Cf = reinterpret_cast<float*>(Cout) + (size_t)e * R * N;
 #pragma unroll
@@ -1053,7 +1056,7 @@ __device__ __forceinline__ void edge_tile(const EdgeArgs& arg, const int logical
 template <int BM, int BN> constexpr int kEdgeBlocks = BN == 256 ? 2 : BM == 128 ? 3 : 4;      // per compute unit
 template <int BM, int BN, int BK, int ST, int EPI, bool A_MNC, bool B_KC, bool K_KEPT>
 __global__ __launch_bounds__(256, (kEdgeBlocks<BM, BN>)) void expert_gemm_bf16_edge_kernel(EdgeArgs arg) {
-  if constexpr (EPI == kEpiStats || EPI == kEpiLogitGrad || EPI == kEpiSums) {
+  if constexpr (EPI == kEpiStats || EPI == kEpiLogitGrad || (EPI == kEpiSums && !K_KEPT)) {
     // the row tiles that hold a target, in the order of their XCDs: their number is known here only
     const int tiles_m = ((arg.kept != nullptr ? arg.kept[0] : arg.R) + BM - 1) / BM, n = arg.nblk / arg.tiles_m * tiles_m;
     if ((int)blockIdx.x >= n) return;
@@ -1504,6 +1507,7 @@ int prepare_expert_gemm() {
       // vocabulary
       MOE_EDGE_KC(kEpiStats, false, true, false), MOE_EDGE_KC(kEpiLogitGrad, false, true, false),
       MOE_EDGE_KC(kEpiSums, false, false, false), MOE_EDGE_MNC(kEpiPitch, true, false, true),
+      MOE_EDGE_MNC(kEpiSums, true, false, true),
 #define MOE_PAIR(V, BM, BN, DEEP, FLAT) \
   prepare_pair<V, BM, BN, DEEP, 64, 64, 5>(), prepare_pair<V, BM, BN, DEEP, 64, 128, 4>(), prepare_pair<V, BM, BN, FLAT, 128, 128, 3>()
       MOE_PAIR(false, 64, 64, 4, 3), MOE_PAIR(false, 64, 128, 2, 2), MOE_PAIR(false, 128, 128, 2, 2),
@@ -1720,25 +1724,60 @@ bool vocab_dw_on_tiles(int rows, int entries, int M) {
   return vocab_tiles_time(kTilesDw, (long long)tiles_of(entries) * tiles_of(M), rows, 0) < kEdgeDw * us;
 }
 int launch_vocab_dw(const GemmArgs& a, int rows, int entries, int M, hipStream_t st) {
+  if (a.k_total > 1) {
+    const int k = row_range(rows, a.k_total);
+    const GemmForm form = gemm_form(false, a.k_total, entries, M, k, kLayoutWeightGrad, kPlanUnits);
+    return gemm_bf16_edge<kEpiSums, true, false, true>(form, a, a.k_total, entries, M, k, st, a.k_total);
+  }
   if (vocab_dw_on_tiles(rows, entries, M)) return launch_vocab_tiles_dw(a, entries, M, st);
   const GemmForm form = gemm_form(false, 1, entries, M, rows, kLayoutWeightGrad, kPlanUnits);
   return gemm_bf16_edge<kEpiPitch, true, false, true>(form, a, 1, entries, M, rows, st);
 }
 
-// Both products of dz, dx's and dw's arguments as above, in one launch where that is faster (*done: else one after the other): small
-// ones in the edge kernel, by the line that is drawn for the gradients of a layer.
+// Both products of dz, dx's and dw's arguments as above, in one launch where that is faster: small ones in the edge kernel, by the
+// line that is drawn for the gradients of a layer.
+static bool vocab_pair(const GemmArgs& dx, const VocabDxPlan& p, const GemmArgs& dw, int rows, int entries, int M, PairProduct* d,
+                       PairProduct* w) {
+  if (p.tiles || vocab_dw_on_tiles(rows, entries, M)) return false;
+  *d = PairProduct{dx, p.splits, rows, M, p.splits == 1 ? entries : p.k, kPersistent, 0};
+  d->form = gemm_form(false, d->E, rows, M, d->K, kLayoutForward, kPlanUnits, &d->us);
+  d->k_total = dx.k_total;
+  *w = PairProduct{dw, 1, entries, M, rows, kPersistent, 0};
+  w->form = gemm_form(false, 1, entries, M, rows, kLayoutWeightGrad, kPlanUnits, &w->us);
+  return pair_ok(d, kLayoutForward, w, kPlanUnits);
+}
+// (*done: else one after the other)
 int launch_vocab_grads_pair(const GemmArgs& dx, const VocabDxPlan& p, const GemmArgs& dw, int rows, int entries, int M,
                             hipStream_t st, bool* done) {
-  *done = false;
-  if (p.tiles || vocab_dw_on_tiles(rows, entries, M)) return MOE_OK;
-  PairProduct d{dx, p.splits, rows, M, p.splits == 1 ? entries : p.k, kPersistent, 0};
-  d.form = gemm_form(false, d.E, rows, M, d.K, kLayoutForward, kPlanUnits, &d.us);
-  d.k_total = dx.k_total;
-  PairProduct w{dw, 1, entries, M, rows, kPersistent, 0};
-  w.form = gemm_form(false, 1, entries, M, rows, kLayoutWeightGrad, kPlanUnits, &w.us);
-  if (!pair_ok(&d, kLayoutForward, &w, kPlanUnits)) return MOE_OK;
-  *done = true;
-  return launch_pair_forms<true>(d, w, st);
+  PairProduct d, w;
+  *done = dw.k_total <= 1 && vocab_pair(dx, p, dw, rows, entries, M, &d, &w);
+  return *done ? launch_pair_forms<true>(d, w, st) : MOE_OK;
+}
+// Ranges of the rows that dw is summed over side by side: a small vocabulary makes few tiles of a long sum.  Of two ways that come
+// within 10 % the one without sums in memory is taken, and a launch shared with dx is worth a fifth of both products.  us of the
+// backward pass (rows, M, entries), one range / as many as this says: 4811 216 461 46.7 / 35.6, 6848 112 8935 108.5 / 106.1,
+// 11656 472 863 127 / 81, 20354 448 5208 446 / 356, 32562 152 211 195 / 55; against it 1878 1008 242 34.3 / 36.1 and
+// 4222 312 3434 65.6 / 72.9, which share a launch.
+int vocab_dw_splits(int rows, int entries, int M) {
+  PairProduct d, w;
+  double us = 0, best_us = 0;
+  if (vocab_pair(GemmArgs{}, vocab_dx_plan(rows, entries, M), GemmArgs{}, rows, entries, M, &d, &w)) {
+    best_us = w.us - 0.2 * (d.us + w.us);
+  } else {
+    gemm_form(false, 1, entries, M, rows, kLayoutWeightGrad, kPlanUnits, &us);
+    us *= kEdgeDw;
+    const double on_tiles = vocab_tiles_time(kTilesDw, (long long)tiles_of(entries) * tiles_of(M), rows, 0);
+    best_us = 0.9 * (us < on_tiles ? us : on_tiles);
+  }
+  int best = 1;
+  for (int want = 2; want <= 32; ++want) {
+    const int k = row_range(rows, want), sp = (rows + k - 1) / k;
+    if (k < 256 || sp < want) continue;
+    gemm_form(false, sp, entries, M, k, kLayoutWeightGrad, kPlanUnits, &us);
+    us = kEdgeDw * us + 4.0 + 1e-6 * 8 * sp * entries * M / 5.0;       // one more launch; written and read, us at 5 TB/s
+    if (us < best_us) { best_us = us; best = sp; }
+  }
+  return best;
 }
 
 int launch_expert_gemm2(const moe_config& c, const void* h, const void* wo, void* out,

@@ -82,14 +82,16 @@ struct F32Smem {
 // of an expert (or, K_KEPT, the length of its sum).  PITCH: rows of A and C lie lda and ldc elements apart, where the dense
 // matrix has as many columns (a piece of a vocabulary, whose number of entries is any), and kept[0] rows of A and C count, or
 // terms of the sum with row-of-k operands.  Then "expert" e of A [R,lda] . B [k_total,N] sums the k from e K on, `add`: to
-// what C [e,R,N] holds.  EPI 3 and 4, of the logits A . B^T: C is the gradient with respect to them, with zeros up to the next whole
+// what C [e,R,N] holds; with row-of-k operands and k_total > 1 it sums the e-th of as many ranges of row_range() rows.  EPI 3 and 4, of the logits A . B^T: C is the gradient with respect to them, with zeros up to the next whole
 // 16 bytes, or nothing is stored but the maximum and sum of exponentials of each row's columns of a wavefront tile (VocabRows).
 template <int TM, int TN, int PD, int KG, int EPI, bool A_KC, bool B_KC, bool K_KEPT, bool PITCH>
 __global__ __launch_bounds__(256 * KG, TM * TN >= 4 ? 2 : TM * TN >= 2 ? 3 : 4) void gemm_f32_mfma_kernel(
     const float* __restrict__ A, const float* __restrict__ B, float* __restrict__ Cout,
-    const float* __restrict__ mask, int R, int N, int K, int tiles_r, int tiles_n,
+    const float* __restrict__ mask, int R, int N, int K_arg, int tiles_r, int tiles_n,
     const int32_t* __restrict__ gather, const int32_t* __restrict__ kept, int lda_arg, int ldc_arg, int k_total,
     int add, VocabRows vocab) {
+  constexpr bool ROW_SUMS = PITCH && K_KEPT;
+  const int K = ROW_SUMS && k_total > 1 ? row_range(kept[0], k_total) : K_arg;
   const int lda = PITCH ? lda_arg : A_KC ? K : R, ldc = PITCH ? ldc_arg : N;
   constexpr bool SUMS = PITCH && A_KC && !B_KC;
   using PA = F32Plane<TM, A_KC>;
@@ -124,7 +126,8 @@ __global__ __launch_bounds__(256 * KG, TM * TN >= 4 ? 2 : TM * TN >= 2 ? 3 : 4) 
   const int r0 = rt * BM, n0 = ct * BN;
   const int rows = kept != nullptr && !K_KEPT ? kept[PITCH ? 0 : e] : R;
   if (r0 >= rows) return;                                      // block-uniform
-  const int KE = K_KEPT ? kept[e] : SUMS && k_total - e * K < K ? k_total - e * K : K;
+  const int ranged = ROW_SUMS && k_total > 1 ? kept[0] - e * K : 0;
+  const int KE = ROW_SUMS && k_total > 1 ? (ranged < 0 ? 0 : ranged < K ? ranged : K) : K_KEPT ? kept[e] : SUMS && k_total - e * K < K ? k_total - e * K : K;
   const int KT = (KE + KG * kBK - 1) / (KG * kBK);             // steps of a group
   const int wm0 = (wave >> 1) * 32 * TM, wn0 = (wave & 1) * 32 * TN;
   const int l32 = lane & 31, hf = lane >> 5;
@@ -619,6 +622,21 @@ VocabDxPlan vocab_dx_plan_f32(int rows, int entries, int M) {
   return best;
 }
 
+int vocab_dw_splits_f32(int rows, int entries, int M) {
+  int best = 1;
+  double best_us = 0, us = 0;
+  f32_form(1, entries, M, rows, kPlanUnits, &best_us);
+  best_us *= 0.9;                                              // (as vocab_dw_splits)
+  for (int want = 2; want <= 32; ++want) {
+    const int k = row_range(rows, want), sp = (rows + k - 1) / k;
+    if (k < 256 || sp < want) continue;
+    f32_form(sp, entries, M, k, kPlanUnits, &us);
+    us += 6.0 + 1e-6 * 8 * sp * entries * M / 5.0;
+    if (us < best_us) { best_us = us; best = sp; }
+  }
+  return best;
+}
+
 int launch_gemm_f32(GemmKind kind, const GemmArgs& a, int E, int R, int N, int K, hipStream_t st) {
   if (a.lda != 0 || a.ldc != 0 || a.vocab.stats != nullptr) {
     // pitches in whole 16-byte pieces; what A's rows hold up to the next whole piece is multiplied by zeros, so is finite.
@@ -628,7 +646,7 @@ int launch_gemm_f32(GemmKind kind, const GemmArgs& a, int E, int R, int N, int K
       return a.vocab.stats != nullptr ? launch_form<4, true, true, false, true>(a, E, R, N, K, st)
                                       : launch_form<3, true, true, false, true>(a, E, R, N, K, st);
     if (kind == kForward && N % 4 == 0 && K % 4 == 0) return launch_form<0, true, false, false, true>(a, E, R, N, K, st);
-    if (kind == kWeightGrad && N % 4 == 0 && E == 1) return launch_form<0, false, false, true, true>(a, E, R, N, K, st);
+    if (kind == kWeightGrad && N % 4 == 0 && E == (a.k_total > 1 ? a.k_total : 1)) return launch_form<0, false, false, true, true>(a, E, R, N, K, st);
     return MOE_EUNSUPPORTED;
   }
   // unit strides along K (kForward: A; kDataGrad: A and B), N and R in whole 16-byte pieces

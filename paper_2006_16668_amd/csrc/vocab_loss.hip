@@ -450,6 +450,26 @@ __global__ __launch_bounds__(256) void vocab_dx_kernel(const float4* __restrict_
   if (part == 0) dx[i] = Vec16<T>::pack(v);
 }
 
+// dw = the sum over ranges of rows, 16 bytes a thread
+template <typename T>
+__global__ __launch_bounds__(256) void vocab_dw_kernel(const float4* __restrict__ sums, int splits, long long total,
+                                                       uint4* __restrict__ dw) {
+  constexpr int K = Vec16<T>::kElts;
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= total) return;
+  float v[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) v[k] = 0.f;
+#pragma unroll 4
+  for (int s = 0; s < splits; ++s)
+#pragma unroll
+    for (int k = 0; k < K; k += 4) {
+      const float4 f = sums[(s * total + i) * (K / 4) + k / 4];
+      v[k] += f.x; v[k + 1] += f.y; v[k + 2] += f.z; v[k + 3] += f.w;
+    }
+  dw[i] = Vec16<T>::pack(v);
+}
+
 unsigned blocks_of(long long threads) { return (unsigned)((threads + 255) / 256); }
 
 }  // namespace
@@ -517,6 +537,9 @@ VocabWs carve_vocab(const moe_config& c, const moe_vocab_dims& d, bool teacher, 
     w.packed = take(whole * c.M * elt);
     w.dz = take(whole * p.entries * elt);
     w.sums = take((size_t)w.dx_plan.splits * N * c.M * 4);
+    const int entries = p.entries < d.V ? p.entries : d.V;
+    w.dw_splits = c.act_dtype == MOE_F32 ? vocab_dw_splits_f32((int)N, entries, c.M) : vocab_dw_splits((int)N, entries, c.M);
+    w.dw_sums = take(w.dw_splits > 1 ? (size_t)w.dw_splits * entries * c.M * 4 : 0);
   }
   w.total = off;
   return w;
@@ -708,14 +731,23 @@ int launch_vocab_backward(const moe_config& c, const moe_vocab_dims& d, const Vo
     GemmArgs gw{z.C, base + ws.packed, static_cast<char*>(a.dw) + (size_t)first * c.M * elt};
     gw.kept = r.kept;
     gw.lda = pc.entries;
+    if (ws.dw_splits > 1) { gw.C = base + ws.dw_sums; gw.k_total = ws.dw_splits; }
     bool done = false;
     if (!f32) rc = launch_vocab_grads_pair(gx, plan, gw, (int)N, n, c.M, st, &done);
     if (rc != MOE_OK) return rc;
     if (done) continue;
     rc = f32 ? launch_gemm_f32(kForward, gx, plan.splits, (int)N, c.M, plan.k, st) : launch_vocab_dx(gx, plan, (int)N, c.M, st);
     if (rc != MOE_OK) return rc;
-    rc = f32 ? launch_gemm_f32(kWeightGrad, gw, 1, n, c.M, (int)N, st)  : launch_vocab_dw(gw, (int)N, n, c.M, st);
+    rc = f32 ? launch_gemm_f32(kWeightGrad, gw, ws.dw_splits, n, c.M, row_range((int)N, ws.dw_splits), st)
+             : launch_vocab_dw(gw, (int)N, n, c.M, st);
     if (rc != MOE_OK) return rc;
+    if (ws.dw_splits > 1) {
+      uint4* const dw = reinterpret_cast<uint4*>(static_cast<char*>(a.dw) + (size_t)first * c.M * elt);
+      const long long total = (long long)n * pieces;
+      hipLaunchKernelGGL(f32 ? vocab_dw_kernel<float> : vocab_dw_kernel<bf16_t>, dim3(blocks_of(total)), dim3(256), 0, st,
+                         reinterpret_cast<const float4*>(base + ws.dw_sums), ws.dw_splits, total, dw);
+      if ((rc = check_launch()) != MOE_OK) return rc;
+    }
   }
   const int parts = N * pieces < 65536 ? 8 : 1;
   auto out = [&](auto kernel) {

@@ -119,7 +119,10 @@ CE = [(1, 64, 128, 900, "bf16", 0.5, 0), (1, 33, 72, 515, "f32", 0.5, 0), (5, 13
       (1, 2100, 448, 33333, "bf16", 0.1, 0), (3, 1021, 776, 20257, "bf16", 0.6, 0), (1, 6000, 192, 9999, "bf16", 0.3, 0),
       (1, 3000, 1000, 9001, "bf16", 0, 4096), (2, 1250, 1344, 7003, "bf16", 0.02, 0), (1, 32, 4096, 16000, "bf16", 0, 0),
       (1, 1024, 1024, 32000, "bf16", 0.97, 0), (1, 2048, 1024, 32000, "bf16", 0.05, 0),
-      (1, 9001, 72, 26001, "bf16", 0, 8192)]
+      (1, 9001, 72, 26001, "bf16", 0, 8192),
+      # dw summed over ranges of the rows: ragged ones, hardly any row, one piece of the vocabulary after the other
+      (1, 5003, 216, 461, "bf16", 0.2, 0), (3, 3001, 152, 211, "bf16", 0.995, 0), (1, 12001, 72, 1030, "bf16", 0.4, 512),
+      (1, 3001, 68, 701, "f32", 0.3, 0), (7, 701, 36, 333, "f32", 0.995, 0), (1, 6001, 100, 515, "f32", 0, 256)]
 
 
 @pytest.mark.parametrize("G,S,M,V,dtype,empty,piece", CE)
@@ -149,6 +152,7 @@ def test_distillation(G, S, M, V, K, T, dtype, empty, piece):
 @pytest.mark.parametrize("K", [0, 5])
 def test_no_token_and_one_token_with_a_target(dtype, K):
     for G, S, M, V, keep in [(2, 700, 64, 777, k) for k in ([], [1399], [0], [63, 64, 1023, 1024])] + \
+            [(1, 9000, 64, 300, k) for k in ([], [8999])] + \
             [(1, 64, 72, 777, k) for k in ([], [63], [0], [5, 6])]:
         d = make(G, S, M, V, dtype, K=K)
         gone = torch.ones(G * S, dtype=torch.bool, device=DEV)

@@ -29,6 +29,7 @@ def logits_on_tiles(rows, entries, M, pack, saved=0.0):
 
 
 dx_plan = _f("_ZN3moe13vocab_dx_planEiii", DxPlan, 3)
+dw_splits, dw_splits_f32 = (_f(f, ctypes.c_int, 3) for f in ("_ZN3moe15vocab_dw_splitsEiii", "_ZN3moe19vocab_dw_splits_f32Eiii"))
 dw_on_tiles = _f("_ZN3moe17vocab_dw_on_tilesEiii", ctypes.c_bool, 3)
 
 
@@ -70,6 +71,19 @@ def test_cases_reach_every_kernel():
     sorts = [(G * S, V, M, True, 2 * G * S * K * M / 6e6 - 16) for G, S, M, V, K, T, dtype, e, p in KD
              if dtype == "bf16" and 2 * G * S * K * M > 1e8]
     assert {logits_on_tiles(*s[:4]) for s in sorts if logits_on_tiles(*s)} == {True, False}
+
+
+def test_ranges_of_the_rows():
+    """A small vocabulary's dw is summed over ranges of many tokens, and such are among the cases: all rows, hardly any, pieces."""
+    for f in (dw_splits, dw_splits_f32):
+        assert all(f(N, 300, 64) == 1 for N in (1, 64, 300)) and f(32768, 300, 128) > 8
+        assert all(1 <= f(N, V, M) <= 32 for N in (1, 700, 5000, 32768) for V in (1, 200, 3000, 50257) for M in (8, 256, 2048))
+    # (two launches where one for both gradients is faster)
+    assert dw_splits(1878, 242, 1008) == 1 and dw_splits(4222, 3434, 312) == 1 and dw_splits(11656, 863, 472) > 1
+    for dtype, f in (("bf16", dw_splits), ("f32", dw_splits_f32)):
+        ranged = [(empty > 0.9, piece > 0) for G, S, M, V, dt, empty, piece in CE if dt == dtype and f(G * S, min(V, piece or V), M) > 1]
+        assert {(False, False), (True, False), (False, True)} <= set(ranged)
+        assert f(9000, 300, 64) > 1
 
 
 def test_what_the_entry_points_refuse():
