@@ -294,6 +294,7 @@ int launch_gemm_f32(GemmKind kind, const GemmArgs& a, int E, int R, int N, int K
 //   pack: x is packed for it alone, and gather is NULL; saved: us of other work that is left out then.  With a.vocab.starts on
 //   tiles in any case.
 bool vocab_logits_on_tiles(int rows, int entries, int M, bool pack, double saved);
+double vocab_logits_edge_us(int rows, int entries, int M);             // in the edge kernel, as expected
 int vocab_stat_slots(int rows, int entries, int M, double saved);
 int launch_vocab_logits(const GemmArgs& a, int rows, int entries, int M, hipStream_t st);
 //   dx: C [splits, rows, M] fp32 = (or +=) sums over the plan's ranges of A [rows, lda] . B [entries, M]

@@ -1677,13 +1677,17 @@ constexpr double kEdgeLogits = 1.09, kEdgeDw = 1.05;
 static GemmForm vocab_logits_form(int rows, int entries, int M, double* us = nullptr) {
   return gemm_form(false, 1, rows, entries, M, kLayoutDataGrad, kPlanUnits, us);
 }
-bool vocab_logits_on_tiles(int rows, int entries, int M, bool pack, double saved) {
-  if (M <= 64) return false;                                   // (two steps at least)
+double vocab_logits_edge_us(int rows, int entries, int M) {
   double us = 0;
   vocab_logits_form(rows, entries, M, &us);
+  return kEdgeLogits * us;
+}
+bool vocab_logits_on_tiles(int rows, int entries, int M, bool pack, double saved) {
+  if (M <= 64) return false;                                   // (two steps at least)
   // (the edge kernel gathers the rows of x by itself, the tiles' are packed: one more launch)
   const double packing = pack ? 4.0 + 4e-6 * rows * M / 5.0 : 0.0;
-  return vocab_tiles_time(kTilesLogits, (long long)tiles_of(rows) * tiles_of(entries), M, 0) + packing < kEdgeLogits * us + saved;
+  return vocab_tiles_time(kTilesLogits, (long long)tiles_of(rows) * tiles_of(entries), M, 0) + packing <
+         vocab_logits_edge_us(rows, entries, M) + saved;
 }
 int vocab_stat_slots(int rows, int entries, int M, double saved) {
   if (vocab_logits_on_tiles(rows, entries, M, true, saved)) return tiles_of(entries);
