@@ -204,7 +204,7 @@ def _ptr(t, dtype, shape, name):
         raise TypeError(f"{name}: expected a GPU tensor")
     if t.dtype != dtype:
         raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{name}: must be contiguous")
@@ -219,7 +219,8 @@ def _ws(ws, name="ws"):
 
 
 def _stream():
-    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    # (its handle alone: torch.cuda.current_stream() makes an object around it, 2 us)
+    return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
 
 
 def moe_gate_workspace_bytes(shape: MoEShape) -> int:

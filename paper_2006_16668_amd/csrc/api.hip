@@ -333,9 +333,10 @@ int vocab_call(const moe_config* cfg, const moe_vocab_dims* d, const moe::VocabC
     if (p == nullptr || !aligned16(p)) return MOE_EINVAL;
   if (!backward && a.loss == nullptr) return MOE_EINVAL;
   if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return MOE_EINVAL;
-  if (ws_bytes < moe::carve_vocab(*cfg, *d, teacher, backward).total) return MOE_EWORKSPACE;
-  return backward ? moe::launch_vocab_backward(*cfg, *d, a, ws, static_cast<hipStream_t>(stream))
-                  : moe::launch_vocab_forward(*cfg, *d, a, ws, static_cast<hipStream_t>(stream));
+  const moe::VocabWs w = moe::carve_vocab(*cfg, *d, teacher, backward);
+  if (ws_bytes < w.total) return MOE_EWORKSPACE;
+  return backward ? moe::launch_vocab_backward(*cfg, *d, a, ws, w, static_cast<hipStream_t>(stream))
+                  : moe::launch_vocab_forward(*cfg, *d, a, ws, w, static_cast<hipStream_t>(stream));
 }
 int vocab_bytes(const moe_config* cfg, const moe_vocab_dims* d, bool backward, size_t* bytes) {
   const int rc = check_vocab(cfg, d);

@@ -306,7 +306,7 @@ int launch_vocab_dx(const GemmArgs& a, const VocabDxPlan& p, int rows, int M, hi
 //   dw: C [entries, M] = A [rows, lda]^T . B [rows, M], which has rows of zeros like dz; with a.k_total > 1 fp32
 //   [a.k_total, entries, M], sums over as many ranges of row_range() rows
 __host__ __device__ inline int row_range(int rows, int ranges) { return ((rows + ranges - 1) / ranges + 63) / 64 * 64; }
-int vocab_dw_splits(int rows, int entries, int M);
+int vocab_dw_splits(int rows, int entries, int M, const VocabDxPlan& dx);
 int vocab_dw_splits_f32(int rows, int entries, int M);                 // gemm_f32.hip
 bool vocab_dw_on_tiles(int rows, int entries, int M);
 int launch_vocab_dw(const GemmArgs& a, int rows, int entries, int M, hipStream_t st);
@@ -352,8 +352,11 @@ struct VocabCall {                     // target: cross entropy, else the teache
   const float* dloss;
   void *dx, *dw;
 };
-int launch_vocab_forward(const moe_config& c, const moe_vocab_dims& d, const VocabCall& a, void* ws, hipStream_t st);
-int launch_vocab_backward(const moe_config& c, const moe_vocab_dims& d, const VocabCall& a, void* ws, hipStream_t st);
+// base: the workspace, laid out as carve_vocab says
+int launch_vocab_forward(const moe_config& c, const moe_vocab_dims& d, const VocabCall& a, void* base, const VocabWs& ws,
+                         hipStream_t st);
+int launch_vocab_backward(const moe_config& c, const moe_vocab_dims& d, const VocabCall& a, void* base, const VocabWs& ws,
+                          hipStream_t st);
 
 // Transformer encoder sub-layers around the MoE layer (encoder.hip)
 int launch_add_layer_norm(int act_dtype, const void* x, const void* delta, const float* gamma,

@@ -1762,10 +1762,10 @@ int launch_vocab_grads_pair(const GemmArgs& dx, const VocabDxPlan& p, const Gemm
 // backward pass (rows, M, entries), one range / as many as this says: 4811 216 461 46.7 / 35.6, 6848 112 8935 108.5 / 106.1,
 // 11656 472 863 127 / 81, 20354 448 5208 446 / 356, 32562 152 211 195 / 55; against it 1878 1008 242 34.3 / 36.1 and
 // 4222 312 3434 65.6 / 72.9, which share a launch.
-int vocab_dw_splits(int rows, int entries, int M) {
+int vocab_dw_splits(int rows, int entries, int M, const VocabDxPlan& dx) {
   PairProduct d, w;
   double us = 0, best_us = 0;
-  if (vocab_pair(GemmArgs{}, vocab_dx_plan(rows, entries, M), GemmArgs{}, rows, entries, M, &d, &w)) {
+  if (vocab_pair(GemmArgs{}, dx, GemmArgs{}, rows, entries, M, &d, &w)) {
     best_us = w.us - 0.2 * (d.us + w.us);
   } else {
     gemm_form(false, 1, entries, M, rows, kLayoutWeightGrad, kPlanUnits, &us);

@@ -544,13 +544,13 @@ VocabWs carve_vocab(const moe_config& c, const moe_vocab_dims& d, bool teacher, 
     w.grad = take(N * 4);
     w.hit = take(N * 4);
     w.hit_value = take(N * 4);
-    w.dx_plan = c.act_dtype == MOE_F32 ? vocab_dx_plan_f32((int)N, p.entries < d.V ? p.entries : d.V, c.M)
-                                       : vocab_dx_plan((int)N, p.entries < d.V ? p.entries : d.V, c.M);
+    const int entries = p.entries < d.V ? p.entries : d.V;
+    w.dx_plan = c.act_dtype == MOE_F32 ? vocab_dx_plan_f32((int)N, entries, c.M) : vocab_dx_plan((int)N, entries, c.M);
     w.packed = take(whole * c.M * elt);
     w.dz = take(whole * p.entries * elt);
     w.sums = take((size_t)w.dx_plan.splits * N * c.M * 4);
-    const int entries = p.entries < d.V ? p.entries : d.V;
-    w.dw_splits = c.act_dtype == MOE_F32 ? vocab_dw_splits_f32((int)N, entries, c.M) : vocab_dw_splits((int)N, entries, c.M);
+    w.dw_splits = c.act_dtype == MOE_F32 ? vocab_dw_splits_f32((int)N, entries, c.M)
+                                         : vocab_dw_splits((int)N, entries, c.M, w.dx_plan);
     w.dw_sums = take(w.dw_splits > 1 ? (size_t)w.dw_splits * entries * c.M * 4 : 0);
   }
   w.total = off;
@@ -617,9 +617,9 @@ static int launch_numbered(const moe_config& c, const VocabRowArgs& r, const Voc
   return rc != MOE_OK || packed == nullptr ? rc : launch_pack(c, a.x, packed, r, st);
 }
 
-int launch_vocab_forward(const moe_config& c, const moe_vocab_dims& d, const VocabCall& a, void* base_, hipStream_t st) {
+int launch_vocab_forward(const moe_config& c, const moe_vocab_dims& d, const VocabCall& a, void* base_, const VocabWs& ws,
+                         hipStream_t st) {
   char* const base = static_cast<char*>(base_);
-  const VocabWs ws = carve_vocab(c, d, a.target == nullptr, false);
   const long long N = (long long)c.G * c.S;
   const bool f32 = c.act_dtype == MOE_F32;
   const float inv_t = a.target != nullptr ? 1.f : 1.f / d.temperature;
@@ -677,9 +677,9 @@ int launch_vocab_forward(const moe_config& c, const moe_vocab_dims& d, const Voc
   return check_launch();
 }
 
-int launch_vocab_backward(const moe_config& c, const moe_vocab_dims& d, const VocabCall& a, void* base_, hipStream_t st) {
+int launch_vocab_backward(const moe_config& c, const moe_vocab_dims& d, const VocabCall& a, void* base_, const VocabWs& ws,
+                          hipStream_t st) {
   char* const base = static_cast<char*>(base_);
-  const VocabWs ws = carve_vocab(c, d, a.target == nullptr, true);
   const VocabPieces pc = vocab_pieces(c, d);
   const long long N = (long long)c.G * c.S;
   const bool f32 = c.act_dtype == MOE_F32;

@@ -29,7 +29,15 @@ def logits_on_tiles(rows, entries, M, pack, saved=0.0):
 
 
 dx_plan = _f("_ZN3moe13vocab_dx_planEiii", DxPlan, 3)
-dw_splits, dw_splits_f32 = (_f(f, ctypes.c_int, 3) for f in ("_ZN3moe15vocab_dw_splitsEiii", "_ZN3moe19vocab_dw_splits_f32Eiii"))
+dw_splits_f32 = _f("_ZN3moe19vocab_dw_splits_f32Eiii", ctypes.c_int, 3)
+_dw_splits = LIB["_ZN3moe15vocab_dw_splitsEiiiRKNS_11VocabDxPlanE"]
+_dw_splits.argtypes = [ctypes.c_int] * 3 + [ctypes.POINTER(DxPlan)]
+
+
+def dw_splits(rows, entries, M):
+    return _dw_splits(rows, entries, M, ctypes.byref(dx_plan(rows, entries, M)))
+
+
 dw_on_tiles = _f("_ZN3moe17vocab_dw_on_tilesEiii", ctypes.c_bool, 3)
 
 
