@@ -272,7 +272,7 @@ EncoderBwdWs carve_enc_bwd(const moe_config& c, const moe_encoder_dims& d) {
   w.dctx = take(N * A * elt);
   w.dhden = take(N * c.H * elt);
   w.dvec = take((size_t)d.B * d.heads * d.L * sizeof(float));
-  w.partial = take(moe::layer_norm_bwd_bytes(c.act_dtype, (long long)N, c.M));
+  w.partial = take(moe::layer_norm_bwd_bytes(c.act_dtype, (long long)N, c.M, true));
   // token ranges of the dense weight gradients (the largest of the four shapes)
   size_t wp = moe::dense_wgrad_partial_bytes(c.act_dtype, (long long)N, (int)A, c.M);
   const size_t wp2 = moe::dense_wgrad_partial_bytes(c.act_dtype, (long long)N, c.M, 3 * (int)A);
@@ -690,7 +690,7 @@ int moe_layer_norm_backward_workspace_bytes(const moe_config* cfg, size_t* bytes
   const int rc = check_config(cfg);
   if (rc != MOE_OK) return rc;
   if (bytes == nullptr) return MOE_EINVAL;
-  *bytes = align_up(moe::layer_norm_bwd_bytes(cfg->act_dtype, (long long)cfg->G * cfg->S, cfg->M), 256);
+  *bytes = align_up(moe::layer_norm_bwd_bytes(cfg->act_dtype, (long long)cfg->G * cfg->S, cfg->M, false), 256);
   return MOE_OK;
 }
 
@@ -704,9 +704,9 @@ int moe_add_layer_norm_backward(const moe_config* cfg, const void* s, const void
   if (dres != nullptr && !aligned16(dres)) return MOE_EINVAL;
   if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return MOE_EINVAL;
   const long long rows = (long long)cfg->G * cfg->S;
-  if (ws_bytes < moe::layer_norm_bwd_bytes(cfg->act_dtype, rows, cfg->M)) return MOE_EWORKSPACE;
+  if (ws_bytes < moe::layer_norm_bwd_bytes(cfg->act_dtype, rows, cfg->M, false)) return MOE_EWORKSPACE;
   return moe::launch_layer_norm_bwd(cfg->act_dtype, s, dn, gamma, dres, ds, static_cast<float*>(ws), dgamma, dbeta, rows, cfg->M,
-                                    true, static_cast<hipStream_t>(stream));
+                                    false, static_cast<hipStream_t>(stream));
 }
 
 int moe_attention_workspace_bytes(const moe_config* cfg, const moe_encoder_dims* dims, size_t* bytes) {
@@ -906,7 +906,7 @@ int moe_encoder_pair_backward(const moe_config* cfg, const moe_encoder_dims* dim
   if (rc != MOE_OK) return rc;
   // g0 = d L / d c = dy + LN4'(dn)
   rc = moe::launch_layer_norm_bwd(dt, f + e.c, dn, w->ln_gamma[3], dy, g0, partial, g->ln_gamma[3],
-                                  g->ln_beta[3], N, cfg->M, false, st);
+                                  g->ln_beta[3], N, cfg->M, true, st);
   if (rc != MOE_OK) return rc;
   // c = b + Attention_2(n3)
   rc = attention_bwd_impl(*cfg, *dims, f + e.n[2], w->wqkv[1], w->wo_att[1], f + e.qkv[1],
@@ -914,7 +914,7 @@ int moe_encoder_pair_backward(const moe_config* cfg, const moe_encoder_dims* dim
                           base + bw.dctx, dvec, wpart, st);
   if (rc != MOE_OK) return rc;
   rc = moe::launch_layer_norm_bwd(dt, f + e.b, dn, w->ln_gamma[2], g0, g1, partial, g->ln_gamma[2],
-                                  g->ln_beta[2], N, cfg->M, false, st);
+                                  g->ln_beta[2], N, cfg->M, true, st);
   if (rc != MOE_OK) return rc;
   // b = a + relu(n2 w1) w2
   rc = moe::launch_dense_grads(*cfg, N, cfg->H, cfg->M, f + e.hden, g1, w->w2, f + e.hden, base + bw.dhden, g->w2, wpart, st);
@@ -922,7 +922,7 @@ int moe_encoder_pair_backward(const moe_config* cfg, const moe_encoder_dims* dim
   rc = moe::launch_dense_grads(*cfg, N, cfg->M, cfg->H, f + e.n[1], base + bw.dhden, w->w1, nullptr, dn, g->w1, wpart, st);
   if (rc != MOE_OK) return rc;
   rc = moe::launch_layer_norm_bwd(dt, f + e.a, dn, w->ln_gamma[1], g1, g0, partial, g->ln_gamma[1],
-                                  g->ln_beta[1], N, cfg->M, false, st);
+                                  g->ln_beta[1], N, cfg->M, true, st);
   if (rc != MOE_OK) return rc;
   // a = x + Attention_1(n1)
   rc = attention_bwd_impl(*cfg, *dims, f + e.n[0], w->wqkv[0], w->wo_att[0], f + e.qkv[0],
@@ -930,7 +930,7 @@ int moe_encoder_pair_backward(const moe_config* cfg, const moe_encoder_dims* dim
                           base + bw.dctx, dvec, wpart, st);
   if (rc != MOE_OK) return rc;
   return moe::launch_layer_norm_bwd(dt, x, dn, w->ln_gamma[0], g0, dx, partial, g->ln_gamma[0],
-                                    g->ln_beta[0], N, cfg->M, false, st);
+                                    g->ln_beta[0], N, cfg->M, true, st);
 }
 
 int moe_vocab_workspace_bytes(const moe_config* cfg, const moe_vocab_dims* dims, size_t* bytes) {

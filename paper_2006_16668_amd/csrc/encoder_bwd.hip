@@ -128,15 +128,14 @@ __global__ __launch_bounds__(64 * WAVES) void layer_norm_bwd_kernel(
   }
 }
 
-// Rows wider than that: one block per row, which walks rows block, block + blocks, ... with the parameters' column sums in
+// Wide rows (layer_norm_bwd_plan says from where): one block per row, which walks rows block, block + blocks, ... with the parameters' column sums in
 // registers (VPT vectors of 16 bytes per thread) and fetches the next row while the sums of one meet.  4096 rows of 8192 bf16 with a
 // residual's gradient, 256 blocks of 1024 threads 67 us, of 512 61 (4.4 TB/s), of 256 64, 512 blocks of 512 71 (more sums).
-constexpr int kLnThreads = 512;
-template <typename T, int VPT>
-__global__ __launch_bounds__(kLnThreads) void layer_norm_bwd_wide_kernel(
+template <typename T, int TH, int VPT>
+__global__ __launch_bounds__(TH) void layer_norm_bwd_wide_kernel(
     const uint4* __restrict__ s, const uint4* __restrict__ dn, const float* __restrict__ gamma, const uint4* dres, uint4* dx,
     float* __restrict__ partial, int M, int vec_per_row, long long rows, float eps) {
-  constexpr int K = Vec16<T>::kElts, TH = kLnThreads, W = TH / 64;
+  constexpr int K = Vec16<T>::kElts, W = TH / 64;
   __shared__ float4 red[2][W];
   const int tid = threadIdx.x;
   float ag[VPT][K], ab[VPT][K], gam[VPT][K];
@@ -533,29 +532,36 @@ int launch_dense_grads(const moe_config& c, long long rows, int in, int out, con
                          : launch_expert_dgrad1(g, dY, W, dX, nullptr, st);
 }
 
-// How the rows are walked: up to 8 KB and 4096 columns by wavefronts, up to 32 KB by blocks (one per unit: the sums that a block
-// leaves are as long as four rows), wider ones in any number of passes, which keep every row's mean and rstd.
+// How the rows are walked: by wavefronts up to 3 KB bf16, 5 KB fp32 (with fewer than 1024 rows 8 KB and 4096 columns), by blocks up
+// to 32 KB, wider ones in any number of passes, which keep every row's mean and rstd.  A wavefront's column sums take three
+// registers for every 64 columns of its row and leave too few others on the unit: us by wavefronts / by blocks, bf16 with a residual's
+// gradient 6421 x 1600 33 / 25, 16000 x 2048 70 / 52, 8192 x 2400 68 / 49, 16000 x 4096 268 / 112 (105 is one pass over all), without
+// 16000 x 1400 40 / 41; fp32 without 6421 x 1196 29 / 36, with 8192 x 1500 48 / 44, 3000 x 2048 32 / 24.  As many blocks as units hold:
+// four, two or one per unit with one, one or more vectors a thread (the sums that a block leaves are as long as four rows; 8192 x 2400
+// 256 blocks 67, 512 49, 768 53).
 enum LayerNormBwdForm { kLnWavefronts, kLnBlocks, kLnAny };
-static LayerNormBwdForm layer_norm_bwd_plan(int act_dtype, long long rows, int M, int* parts) {
+static LayerNormBwdForm layer_norm_bwd_plan(int act_dtype, long long rows, int M, bool as_before, int* parts) {
   const int vec = M * (act_dtype == MOE_F32 ? 4 : 2) / 16;
-  const LayerNormBwdForm form = vec <= 512 && M <= 4096 ? kLnWavefronts : vec <= 2048 ? kLnBlocks : kLnAny;
-  const long long most = form == kLnWavefronts ? 1024 : form == kLnBlocks ? 256 : 64, blocks = (rows + 3) / 4;
+  const int waves = as_before || rows < 1024 ? 512 : act_dtype == MOE_F32 ? 320 : 192;
+  const LayerNormBwdForm form = vec <= waves && M <= 4096 ? kLnWavefronts : vec <= 2048 ? kLnBlocks : kLnAny;
+  const long long most = form == kLnWavefronts || (form == kLnBlocks && vec <= 256) ? 1024
+                         : form == kLnBlocks ? (vec <= 512 ? 512 : 256) : 64, blocks = (rows + 3) / 4;
   *parts = (int)(blocks < most ? blocks : most);
   return form;
 }
-size_t layer_norm_bwd_bytes(int act_dtype, long long rows, int M) {
+size_t layer_norm_bwd_bytes(int act_dtype, long long rows, int M, bool as_before) {
   int parts;
-  const LayerNormBwdForm form = layer_norm_bwd_plan(act_dtype, rows, M, &parts);
+  const LayerNormBwdForm form = layer_norm_bwd_plan(act_dtype, rows, M, as_before, &parts);
   return (size_t)parts * 2 * M * sizeof(float) + (form == kLnAny ? (size_t)rows * sizeof(float2) : 0);
 }
 
 int launch_layer_norm_bwd(int act_dtype, const void* s, const void* dn, const float* gamma,
                           const void* dres, void* dx, float* partial, float* dgamma, float* dbeta,
-                          long long rows, int M, bool one_block, hipStream_t st) {
+                          long long rows, int M, bool as_before, hipStream_t st) {
   const int elt = act_dtype == MOE_F32 ? 4 : 2;
   const int vec_per_row = M * elt / 16;
   const int vpl = (vec_per_row + 63) / 64;
-  if (one_block && rows <= 64 && M <= 1024) {
+  if (!as_before && rows <= 64 && M <= 1024) {
     // One block of 16 wavefronts, whose sums are the parameters' gradients: one launch (37 rows of 520 fp32, with the call from Python
     // 17.6 -> 12.5 us).
     auto one = [&](auto kernel) {
@@ -575,7 +581,7 @@ int launch_layer_norm_bwd(int act_dtype, const void* s, const void* dn, const fl
   const size_t lds = (size_t)4 * M * sizeof(float);
   const float eps = 1e-6f;
   int parts;
-  const LayerNormBwdForm form = layer_norm_bwd_plan(act_dtype, rows, M, &parts);
+  const LayerNormBwdForm form = layer_norm_bwd_plan(act_dtype, rows, M, as_before, &parts);
   auto reduce = [&]() {
     hipLaunchKernelGGL(layer_norm_param_reduce_kernel, dim3((unsigned)((2 * M + 15) / 16)), dim3(16 * kReduceGroups), 0, st,
                        partial, parts, M, dgamma, dbeta);
@@ -597,9 +603,11 @@ int launch_layer_norm_bwd(int act_dtype, const void* s, const void* dn, const fl
                          static_cast<const uint4*>(s), static_cast<const uint4*>(dn), stats, partial, M, vec_per_row, rows);
     };
 #define MOE_LNB_WIDE(T)                                                                       \
-  if (form == kLnBlocks && vec_per_row <= 1024) wide(layer_norm_bwd_wide_kernel<T, 2>, kLnThreads); \
-  else if (form == kLnBlocks && vec_per_row <= 1536) wide(layer_norm_bwd_wide_kernel<T, 3>, kLnThreads); \
-  else if (form == kLnBlocks) wide(layer_norm_bwd_wide_kernel<T, 4>, kLnThreads);             \
+  if (form == kLnBlocks && vec_per_row <= 256) wide(layer_norm_bwd_wide_kernel<T, 256, 1>, 256);  \
+  else if (form == kLnBlocks && vec_per_row <= 512) wide(layer_norm_bwd_wide_kernel<T, 512, 1>, 512); \
+  else if (form == kLnBlocks && vec_per_row <= 1024) wide(layer_norm_bwd_wide_kernel<T, 512, 2>, 512); \
+  else if (form == kLnBlocks && vec_per_row <= 1536) wide(layer_norm_bwd_wide_kernel<T, 512, 3>, 512); \
+  else if (form == kLnBlocks) wide(layer_norm_bwd_wide_kernel<T, 512, 4>, 512);               \
   else any(layer_norm_bwd_any_kernel<T>, layer_norm_param_any_kernel<T>);
     if (act_dtype == MOE_F32) { MOE_LNB_WIDE(float) } else { MOE_LNB_WIDE(bf16_t) }
 #undef MOE_LNB_WIDE
@@ -612,13 +620,12 @@ int launch_layer_norm_bwd(int act_dtype, const void* s, const void* dn, const fl
                      static_cast<const uint4*>(s), static_cast<const uint4*>(dn), gamma,      \
                      static_cast<const uint4*>(dres), static_cast<uint4*>(dx), partial, M, M, \
                      vec_per_row, rows, eps)
-  if (act_dtype == MOE_F32) {
-    if (vpl <= 1) MOE_LNB_CASE(float, 1); else if (vpl <= 2) MOE_LNB_CASE(float, 2);
-    else if (vpl <= 4) MOE_LNB_CASE(float, 4); else MOE_LNB_CASE(float, 8);
-  } else {
-    if (vpl <= 1) MOE_LNB_CASE(bf16_t, 1); else if (vpl <= 2) MOE_LNB_CASE(bf16_t, 2);
-    else if (vpl <= 4) MOE_LNB_CASE(bf16_t, 4); else MOE_LNB_CASE(bf16_t, 8);
-  }
+#define MOE_LNB_VPL(T)                                                                        \
+  if (vpl <= 1) MOE_LNB_CASE(T, 1); else if (vpl <= 2) MOE_LNB_CASE(T, 2);                    \
+  else if (vpl <= 4) MOE_LNB_CASE(T, 4);                                                      \
+  else if (vpl <= 5) MOE_LNB_CASE(T, 5); else if (vpl <= 6) MOE_LNB_CASE(T, 6); else MOE_LNB_CASE(T, 8)
+  if (act_dtype == MOE_F32) { MOE_LNB_VPL(float); } else { MOE_LNB_VPL(bf16_t); }
+#undef MOE_LNB_VPL
 #undef MOE_LNB_CASE
   const int rc = check_launch();
   return rc != MOE_OK ? rc : reduce();

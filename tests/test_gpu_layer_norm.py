@@ -32,9 +32,10 @@ def xhat(s):
     return c * rstd, rstd
 
 
-# wavefronts up to 8 KB a row; blocks, two to four vectors a thread backward; any
+# wavefronts (with many rows up to 3 or 5 KB, else 8 KB backward); blocks, one to four vectors a thread backward; any
 WIDTHS = [("bf16", M) for M in (8, 520, 4096, 4104, 8192, 8200, 12288, 12296, 16384, 16392, 40000)] + \
-         [("bf16", 1024)] + [("f32", M) for M in (4, 260, 520, 1024, 2048, 2052, 4100, 8192, 8196, 20004)]
+         [("bf16", M) for M in (1024, 1536, 1544, 2400, 2800)] + \
+         [("f32", M) for M in (4, 260, 520, 1024, 1196, 1284, 1500, 2048, 2052, 4100, 8192, 8196, 20004)]
 
 
 # (many rows: once per form)
