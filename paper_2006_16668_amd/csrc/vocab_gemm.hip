@@ -499,7 +499,7 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
             const int t = *(lds_i_ptr)(uintptr_t)(data + 2048) - (g.v.first + n0 + 64 * wn);   // the target's column, in its place
             if (t >= 0 && t < 64)
               *(lds_bf16_ptr)(uintptr_t)(wr + (((t >> 3) ^ ((r32 >> 1) & 7)) * 16) + 8 * (((t >> 2) & 1) ^ (r32 >> 4)) + 2 * (t & 3)) =
-                  f32_to_bf16(*(lds_f_ptr)(uintptr_t)(data + 3072));
+                  f32_to_bf16(*(lds_f_ptr)(uintptr_t)(data + 3 * 1024));
           }
         }
 #pragma unroll
