@@ -63,8 +63,10 @@ __device__ __forceinline__ int lane_here() {
   return lane;
 }
 
-// TAIL: the length of the sums is no multiple of 64 (checked in every step, it costs 5 % of the time).  dw's, the number of rows
-// with a target, is not known to the host: there both operands have rows of zeros up to the next multiple.
+// TAIL: the length of the sums is no multiple of 64.  Asked for in every step it costs 5 % of the time, so the steps before a sum's last
+// ones have a loop of their own (6027 tokens, M 1336, V 6322, backward 278 -> 266 us); a branch between two kinds of steps inside
+// one loop spills the accumulators.  dw's length, the number of rows with a target, is not known to the host: there both operands
+// have rows of zeros up to the next multiple.
 template <int EPI, bool TAIL>
 __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
   constexpr bool A_MNC = EPI == kPlain, B_MNC = EPI == kSums || EPI == kPlain;
@@ -155,8 +157,8 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
 #define MOE_VG_COPY_AT(LDS, ADDR)                                                              \
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(LDS), "v"(ADDR) : "memory")
   // one piece of an operand; in the last step of a sum, k behind its end comes from a line of zeros
-  auto copy_piece = [&](bool mnc, uint32_t at, const uint32_t (&off)[2], const bf16_t* base) __attribute__((always_inline)) {
-    if (!TAIL || p_left >= 64) {
+  auto copy_piece = [&](auto tail, bool mnc, uint32_t at, const uint32_t (&off)[2], const bf16_t* base) __attribute__((always_inline)) {
+    if (!decltype(tail)::value || p_left >= 64) {
 #pragma unroll
       for (int q = 0; q < 2; ++q) MOE_VG_COPY(at + q * 1024, off[q], base);
     } else {
@@ -170,13 +172,13 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
       }
     }
   };
-  auto copy_a = [&](int h) __attribute__((always_inline)) {
-    if (p_more) copy_piece(A_MNC, lds0 + p_stage + h * kPiece + wave * 2048, a_off[h], p_a);
+  auto copy_a = [&](auto tail, int h) __attribute__((always_inline)) {
+    if (p_more) copy_piece(tail, A_MNC, lds0 + p_stage + h * kPiece + wave * 2048, a_off[h], p_a);
   };
-  auto copy_b = [&]() __attribute__((always_inline)) {
+  auto copy_b = [&](auto tail) __attribute__((always_inline)) {
     if (!p_more) return;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) copy_piece(B_MNC, lds0 + p_stage + (2 + h) * kPiece + wave * 2048, b_off[h], p_b);
+    for (int h = 0; h < 2; ++h) copy_piece(tail, B_MNC, lds0 + p_stage + (2 + h) * kPiece + wave * 2048, b_off[h], p_b);
   };
   auto advance = [&]() __attribute__((always_inline)) {
     if (!p_more) return;
@@ -273,8 +275,9 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
     steps_left += (range_k(e) + 63) >> 6;
   }
   set_sources();
-  copy_b(); copy_a(0); copy_a(1); advance();
-  copy_b(); copy_a(0);
+  constexpr auto any = std::integral_constant<bool, TAIL>{};
+  copy_b(any); copy_a(any, 0); copy_a(any, 1); advance();
+  copy_b(any); copy_a(any, 0);
   if (steps_left > 1) asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
   else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_barrier();
@@ -291,7 +294,7 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
     int entries = 0;
     const uint2* list = nullptr;
     uint32_t list_at = 0;
-    auto step = [&](auto first_step, int kt) __attribute__((always_inline)) {
+    auto step = [&](auto first_step, auto tail, int kt) __attribute__((always_inline)) {
       const bool landed = decltype(first_step)::value && tile != first;        // what it waits for: before the last tile's stores
       // phase 1
       read_b(0);
@@ -303,7 +306,7 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
         if (steps_left > 1) asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       }
-      copy_a(1);
+      copy_a(tail, 1);
       advance();
       turn(first_step, 0, 1);
       // phase 3; B and A0 of the next step (younger: its A1)
@@ -312,7 +315,7 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
       if (EPI == kLogitGrad && decltype(first_step)::value) copy_row_data(m0);
       if (EPI == kStats && decltype(first_step)::value && g.v.starts != nullptr)
         MOE_VG_WORDS(lds0 + kStaging + wave * 4096, g.v.starts + (size_t)rt * (8 * tiles_n + 1) + 8 * ct + wave + lane_here());
-      copy_b();
+      copy_b(tail);
       turn(first_step, 1, 1);
       // phase 4
       if (EPI == kStats && !decltype(first_step)::value && kt + 1 == steps && g.v.starts != nullptr) {
@@ -327,15 +330,20 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
       }
       other_stage();
       if (kt + 1 < steps) read_a(0);
-      copy_a(0);
+      copy_a(tail, 0);
       turn(first_step, 1, 0);
       --steps_left;
     };
     if (steps > 0) {
       read_a(0);                                               // (after the last tile's stores: they need the registers)
-      step(std::true_type{}, 0);
+      step(std::true_type{}, any, 0);
+      int kt = 1;
+      if (TAIL) {                                              // (what a step copies lies within the next 128 k)
 #pragma unroll 1
-      for (int kt = 1; kt < steps; ++kt) step(std::false_type{}, kt);
+        for (; kt < steps && p_left >= 128; ++kt) step(std::false_type{}, std::false_type{}, kt);
+      }
+#pragma unroll 1
+      for (; kt < steps; ++kt) step(std::false_type{}, any, kt);
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
