@@ -17,6 +17,8 @@
 //     2       A0 B1      B1                                               A1 (one ahead)
 //     3       A1 B1      A1                                               B0 B1
 //     4       A1 B0      A0 of the tile's next step                       A0
+// Of a tile at the end whose second 128 rows, or columns, do not exist the phases that would multiply them only copy and pass the
+// barriers (2100 tokens, M 1096, V 32000, backward 513 -> 490 us; 496 tokens, 283 with a target, M 920, V 105770, forward 113 -> 107).
 // A piece is copied over as soon as both wavefronts of every SIMD have read it, so two stages (128 KB) give a copy more than a
 // step's time.  Copies bypass the registers (global_load_lds_dwordx4) and run on across tiles: a block walks its share of them.
 //
@@ -44,6 +46,7 @@ constexpr uint32_t kSmem = kStaging + 8 * 4096;                // all 160 KB (kS
 static __device__ const u32x4_t vocab_zero_line = {0u, 0u, 0u, 0u};
 
 enum VocabEpi { kStats, kLogitGrad, kSums, kPlain };
+enum VocabTile { kWhole, kUpper, kLeft };      // of a tile at the end the half that exists, its first 128 rows or columns
 
 struct VocabGemmArgs {
   const bf16_t *A, *B;
@@ -104,8 +107,15 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
   const int stride = ((int)gridDim.x - xcd + kXcds - 1) / kXcds;
   const int first = t_begin + (int)blockIdx.x / kXcds;
   if (first >= t_end) return;
-  // tile -> range, row tile, column tile: bands of 8 row tiles, row tile fastest (shared panels in an XCD's L2)
+  // tile -> range, row tile, column tile: bands of 8 row tiles, row tile fastest (shared panels in an XCD's L2).  With
+  // half tiles a round of them is dealt out nine blocks further on than the one before, so that a block does not get those, or none,
+  // of all rounds.
+  const bool halves = (R - 1) % 256 < 128 || (B_MNC && (g.N - 1) % 256 < 128);
   auto tile_at = [&](int t, int& e, int& rt, int& ct) {
+    if (halves) {
+      const int round = (t - t_begin) / stride, from = t_begin + round * stride;
+      if (from + stride <= t_end) t = from + (t - from + 9 * round) % stride;
+    }
     e = EPI == kSums ? t / per_range : 0;
     t -= e * per_range;
     const int band = t / (8 * tiles_n), rem = t - band * 8 * tiles_n;
@@ -247,19 +257,19 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
   // one turn of the matrix pipe: between two barriers, what was fetched before the first of them.  A tile's first step starts
   // from an operand of zeros: 128 registers need no clearing.
   const f32x16_t zeros = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  auto turn = [&](auto first, int h, int j) __attribute__((always_inline)) {
+  auto turn = [&](auto first, int h, int j, bool multiplies) __attribute__((always_inline)) {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_setprio(1);
+    if (multiplies) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk)
+    for (int kk = 0; kk < (multiplies ? 4 : 0); ++kk)
 #pragma unroll
       for (int i = 0; i < 2; ++i)
         acc[2 * h + i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[j][kk], a[h][i][kk],
                                                                     decltype(first)::value && kk == 0 ? zeros : acc[2 * h + i][j], 0, 0, 0);
-    __builtin_amdgcn_s_setprio(0);
+    if (multiplies) __builtin_amdgcn_s_setprio(0);
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
@@ -294,29 +304,30 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
     int entries = 0;
     const uint2* list = nullptr;
     uint32_t list_at = 0;
-    auto step = [&](auto first_step, auto tail, int kt) __attribute__((always_inline)) {
+    auto step = [&](auto first_step, auto tail, auto half, int kt) __attribute__((always_inline)) {
+      constexpr bool upper = decltype(half)::value == kUpper, left = decltype(half)::value == kLeft;
       const bool landed = decltype(first_step)::value && tile != first;        // what it waits for: before the last tile's stores
       // phase 1
       read_b(0);
-      turn(first_step, 0, 0);
+      turn(first_step, 0, 0, true);
       // phase 2; A1 of this step must have landed (younger: B and A0 of the next).  A1 of the next step is started here and not
       // before: its place is where the last tile's results passed through.
-      read_b(1);
+      if (!left) read_b(1);
       if (!landed) {
         if (steps_left > 1) asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       }
       copy_a(tail, 1);
       advance();
-      turn(first_step, 0, 1);
+      turn(first_step, 0, 1, !left);
       // phase 3; B and A0 of the next step (younger: its A1)
-      read_a(1);
+      if (!upper) read_a(1);
       if (!landed) asm volatile("s_waitcnt vmcnt(2)" ::: "memory");
       if (EPI == kLogitGrad && decltype(first_step)::value) copy_row_data(m0);
       if (EPI == kStats && decltype(first_step)::value && g.v.starts != nullptr)
         MOE_VG_WORDS(lds0 + kStaging + wave * 4096, g.v.starts + (size_t)rt * (8 * tiles_n + 1) + 8 * ct + wave + lane_here());
       copy_b(tail);
-      turn(first_step, 1, 1);
+      turn(first_step, 1, 1, !upper && !left);
       // phase 4
       if (EPI == kStats && !decltype(first_step)::value && kt + 1 == steps && g.v.starts != nullptr) {
         const u32x2_t start = *(lds_u2_ptr)(uintptr_t)(lds0 + kStaging + wave * 4096);
@@ -331,19 +342,27 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
       other_stage();
       if (kt + 1 < steps) read_a(0);
       copy_a(tail, 0);
-      turn(first_step, 1, 0);
+      turn(first_step, 1, 0, !upper);
       --steps_left;
     };
     if (steps > 0) {
       read_a(0);                                               // (after the last tile's stores: they need the registers)
-      step(std::true_type{}, any, 0);
+      step(std::true_type{}, any, std::integral_constant<int, kWhole>{}, 0);
       int kt = 1;
+      if (R - m0 <= 128) {
+#pragma unroll 1
+        for (; kt < steps; ++kt) step(std::false_type{}, any, std::integral_constant<int, kUpper>{}, kt);
+      }
+      if (B_MNC && g.N - n0 <= 128) {
+#pragma unroll 1
+        for (; kt < steps; ++kt) step(std::false_type{}, any, std::integral_constant<int, kLeft>{}, kt);
+      }
       if (TAIL) {                                              // (what a step copies lies within the next 128 k)
 #pragma unroll 1
-        for (; kt < steps && p_left >= 128; ++kt) step(std::false_type{}, std::false_type{}, kt);
+        for (; kt < steps && p_left >= 128; ++kt) step(std::false_type{}, std::false_type{}, std::integral_constant<int, kWhole>{}, kt);
       }
 #pragma unroll 1
-      for (; kt < steps; ++kt) step(std::false_type{}, any, kt);
+      for (; kt < steps; ++kt) step(std::false_type{}, any, std::integral_constant<int, kWhole>{}, kt);
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -412,6 +431,7 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
       const uint32_t mine = lds0 + kStaging + wave * 4096;     // (maximum, sum) of 128 rows
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
+        if (i >= 2 && R - m0 <= 128) continue;                 // (what is met below of these rows is not stored)
         float mx = -INFINITY;
         if (n0 + 256 > g.N) {
 #pragma unroll
