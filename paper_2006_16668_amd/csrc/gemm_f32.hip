@@ -354,7 +354,8 @@ __global__ __launch_bounds__(256 * KG, TM * TN >= 4 ? 2 : TM * TN >= 2 ? 3 : 4) 
     row_up = vocab.grad[at];
     if (vocab.hit != nullptr) { row_hit = vocab.hit[at] - vocab.first; row_value = vocab.hit_value[at]; }
   }
-  auto of_row = [&](auto of_lane, int row) {                   // row of the lower half, row + 4 of the upper
+  // row of the lower half, row + 4 of the upper; while all lanes are active: what one holds that is not, the compiler need not keep
+  auto of_row = [&](auto of_lane, int row) {
     const int bits = __builtin_bit_cast(int, of_lane);
     const int lo = __builtin_amdgcn_readlane(bits, row), hi = __builtin_amdgcn_readlane(bits, row + 4);
     return __builtin_bit_cast(decltype(of_lane), hf != 0 ? hi : lo);
@@ -364,7 +365,8 @@ __global__ __launch_bounds__(256 * KG, TM * TN >= 4 ? 2 : TM * TN >= 2 ? 3 : 4) 
   // store covers whole 128-byte pieces of two rows
   auto store_tile = [&](int i, int j, const f32x16_t& c, const f32x16_t& m) {
     const int n = n0 + wn0 + 32 * j + l32, rb = r0 + wm0 + 32 * i + 4 * hf;
-    if (n >= (EPI == 3 ? (N + 3) / 4 * 4 : N)) return;
+    const bool stored = n < (EPI == 3 ? (N + 3) / 4 * 4 : N);
+    if (EPI != 3 && !stored) return;                           // (EPI 3: of_row)
     const size_t o = ((size_t)e * R + rb) * ldc + n;
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
@@ -374,11 +376,12 @@ __global__ __launch_bounds__(256 * KG, TM * TN >= 4 ? 2 : TM * TN >= 2 ? 3 : 4) 
       if (EPI == 2) x = m[v] > 0.f ? x : 0.f;
       if (EPI == 3) {
         const int at = 32 * i + dr;                            // of the half's row
+        const float value = of_row(row_value, at);
         x = __builtin_amdgcn_exp2f(fmaf(x, vocab.scale, -of_row(row_lse, at))) * of_row(row_up, at);
-        if (of_row(row_hit, at) == n) x = of_row(row_value, at);
+        if (of_row(row_hit, at) == n) x = value;
         if (n >= N) x = 0.f;
       }
-      if (rb + dr < rows) {
+      if (stored && rb + dr < rows) {
         if (SUMS && add) x += Cout[o + (size_t)dr * ldc];
         Cout[o + (size_t)dr * ldc] = x;
       }
