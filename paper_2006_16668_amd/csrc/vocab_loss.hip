@@ -365,7 +365,10 @@ __global__ __launch_bounds__(256) void vocab_finish_kernel(const float2* __restr
   const float l = lse_of[sl];
   float out;
   if (!TEACHER) {
+    // never below 0 but for rounding: the sums are not in the products' order.  At a probability of 1 that would turn the gradient at
+    // the target, expm1(-loss), round.  (NaN stays)
     out = l - row_dot<T>(x + (size_t)n * pieces, w + (size_t)target[n] * pieces, pieces, r);
+    out = out < 0.f ? 0.f : out;
   } else {
     const float2 ts = tstat[n];
     const float inv = 1.f / ts.y, log_sum = logf(ts.y);
