@@ -462,7 +462,8 @@ int moe_encoder_pair_backward(const moe_config* cfg, const moe_encoder_dims* dim
  * Reductions over tokens are the caller's: loss is per token, and dloss its gradient.
  */
 typedef struct {
-  int32_t V;           /* entries of the vocabulary, up to 2^23; tokens . V below 2^38, tokens below 2^24 */
+  int32_t V;           /* entries of the vocabulary, up to 2^23; tokens . V below 2^38, tokens below 2^24, M up to 2^20,
+                          tokens . M below 2^34 - 2^10 (fp32 backward: counting the tokens up to whole 64) */
   int32_t K;           /* moe_vocab_distill: entries per token, 1 .. 256; else not read */
   int32_t piece;       /* backward: entries of the vocabulary whose gradient dz is kept at a time, in whole 256;
                           0: as many as make 1 GiB, 4096 at least */

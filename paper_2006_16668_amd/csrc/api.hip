@@ -305,7 +305,7 @@ int attention_bwd_impl(const moe_config& c, const moe_encoder_dims& d, const voi
 }
 
 // ---- loss over a vocabulary
-int check_vocab(const moe_config* cfg, const moe_vocab_dims* d) {
+int check_vocab(const moe_config* cfg, const moe_vocab_dims* d, bool backward) {
   const int rc = check_config(cfg);
   if (rc != MOE_OK) return rc;
   if (d == nullptr || d->V < 1 || d->piece < 0) return MOE_EINVAL;
@@ -314,6 +314,8 @@ int check_vocab(const moe_config* cfg, const moe_vocab_dims* d) {
   const long long N = (long long)cfg->G * cfg->S;
   if (N >= 1 << 24 || ((N + 127) / 128) * ((d->V + 127) / 128) >= 1 << 24 || N * (cfg->M / 4) >= (1LL << 32) - 256)
     return MOE_EUNSUPPORTED;
+  // (the backward pass packs whole 64 rows)
+  if (backward && (N + 63) / 64 * 64 * (cfg->M / (cfg->act_dtype == MOE_F32 ? 4 : 8)) >= (1LL << 32) - 256) return MOE_EUNSUPPORTED;
   return MOE_OK;
 }
 int check_teacher(const moe_vocab_dims* d) {
@@ -322,7 +324,7 @@ int check_teacher(const moe_vocab_dims* d) {
 }
 int vocab_call(const moe_config* cfg, const moe_vocab_dims* d, const moe::VocabCall& a, void* ws, size_t ws_bytes, void* stream,
                bool backward) {
-  int rc = check_vocab(cfg, d);
+  int rc = check_vocab(cfg, d, backward);
   if (rc != MOE_OK) return rc;
   const bool teacher = a.target == nullptr;
   if (teacher && (rc = check_teacher(d)) != MOE_OK) return rc;
@@ -339,7 +341,7 @@ int vocab_call(const moe_config* cfg, const moe_vocab_dims* d, const moe::VocabC
                   : moe::launch_vocab_forward(*cfg, *d, a, ws, w, static_cast<hipStream_t>(stream));
 }
 int vocab_bytes(const moe_config* cfg, const moe_vocab_dims* d, bool backward, size_t* bytes) {
-  const int rc = check_vocab(cfg, d);
+  const int rc = check_vocab(cfg, d, backward);
   if (rc != MOE_OK) return rc;
   if (bytes == nullptr) return MOE_EINVAL;
   *bytes = moe::carve_vocab(*cfg, *d, false, backward).total;
