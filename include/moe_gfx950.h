@@ -467,7 +467,7 @@ typedef struct {
   int32_t K;           /* moe_vocab_distill: entries per token, 1 .. 256; else not read */
   int32_t piece;       /* backward: entries of the vocabulary whose gradient dz is kept at a time, in whole 256;
                           0: as many as make 1 GiB, 4096 at least */
-  float temperature;   /* moe_vocab_distill: T > 0; else not read */
+  float temperature;   /* moe_vocab_distill: T > 0, finite, with log2(e) / T finite; else not read */
 } moe_vocab_dims;
 
 /* Bytes of workspace of the forward and of the backward calls (either loss).  Pure host functions. */

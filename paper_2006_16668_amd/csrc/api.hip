@@ -319,7 +319,9 @@ int check_vocab(const moe_config* cfg, const moe_vocab_dims* d, bool backward) {
   return MOE_OK;
 }
 int check_teacher(const moe_vocab_dims* d) {
-  if (d->K < 1 || !(d->temperature > 0.f) || !(1.f / d->temperature > 0.f) || 1.f / d->temperature > 3e38f) return MOE_EINVAL;
+  // (log2(e) / T scales the logits)
+  const float inv_t = 1.f / d->temperature;
+  if (d->K < 1 || !(d->temperature > 0.f) || !(inv_t > 0.f) || 1.4426951f * inv_t > 3.4028234e38f) return MOE_EINVAL;
   return d->K <= 256 ? MOE_OK : MOE_EUNSUPPORTED;
 }
 int vocab_call(const moe_config* cfg, const moe_vocab_dims* d, const moe::VocabCall& a, void* ws, size_t ws_bytes, void* stream,
