@@ -451,7 +451,8 @@ int moe_encoder_pair_backward(const moe_config* cfg, const moe_encoder_dims* dim
  * 32k and 64k entries (Appendix, training details).  The entry points below take the last hidden states
  * x [G,S,M] and one weight row per vocabulary entry, w [V,M] (an embedding table is one), and never keep the
  * logits z[g,s,v] = sum_m x[g,s,m] w[v,m]:
- *   moe_vocab_loss      loss = lse - z[target],  lse = log sum_v exp z[v]  (0 where rounding would leave less)
+ *   moe_vocab_loss      loss = lse - z[target],  lse = log sum_v exp z[v]  (accurate to its own size for sure tokens, never
+ *                       below 0: from the other entries' log-sum less z[target])
  *   moe_vocab_distill   a teacher's K entries per token, q = softmax(teacher_logit / T) over them:
  *                       loss = sum_k q_k (log q_k - z[i_k] / T + lse),  lse = log sum_v exp(z[v] / T)
  *                       (the student's softmax is over all V entries; a caller who wants T^2 puts it in dloss)

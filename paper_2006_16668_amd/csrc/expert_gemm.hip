@@ -632,7 +632,7 @@ struct EdgeArgs {
 constexpr int kEpiMaskIfAny = 6;       // 2 with a mask, else 0
 constexpr int kEpiRangesIfAny = 7;     // 3 with a k_total, else 0; kept is K_KEPT's
 // The products of a vocabulary's loss (vocab_loss.hip); E is 1 and kept[0] the rows with a target.
-//   z = x . w^T: no C, the maximum and the sum of exponentials of each row's columns of a wavefront tile (kEpiStats), or
+//   z = x . w^T: no C, the maximum and the sum of exponentials of each row's columns of a wavefront tile, but its target's (kEpiStats), or
 //     C = the gradient with respect to z, bf16 in rows of ldc, with zeros in the columns N .. of the last 16
 //     bytes and in the rows behind the last of a tile (kEpiLogitGrad)
 //   dx = dz . w: A in rows of lda, "expert" e sums the k from e K on, up to k_total; C[e] fp32, or is added to
@@ -737,6 +737,12 @@ __device__ __forceinline__ void edge_tile(const EdgeArgs& arg, const int logical
     }
     b_addr[q] = ok ? (uint64_t)(uintptr_t)src : zline;
     b_inc[q] = ok ? (B_KC ? BK * 2 : (uint32_t)N * BK * 2) : 0u;
+  }
+  int hit_of[TM];                                              // kEpiStats: the rows' targets, asked for before the sums
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int row = m0 + wm0 + 32 * i + (lane & 31);
+    hit_of[i] = EPI == kEpiStats && arg.vocab.hit != nullptr ? arg.vocab.hit[row < rows ? row : rows - 1] : -1;
   }
 #define MOE_EDGE_COPY(LDS_U32, ADDR_U64)                                                     \
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"            \
@@ -914,6 +920,21 @@ __device__ __forceinline__ void edge_tile(const EdgeArgs& arg, const int logical
   // log2(e) / temperature times a logit is the argument of a power of two.  Of a row the lanes l and l + 32 hold the columns.
   if constexpr (EPI == kEpiStats) {
     const float c = arg.vocab.scale;
+    if (arg.vocab.hit != nullptr) {                            // targets among the columns, left out and stored by themselves
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        const int t = (int)((uint32_t)hit_of[i] - (uint32_t)(n0 + wn0 + 4 * (lane >> 5)));      // (any number: not a target)
+        const bool in = t >= 0 && t < WN && (t & 4) == 0;      // of this half's columns
+        if (__builtin_amdgcn_ballot_w64(in) == 0) continue;
+        float at = 0.f;
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[i][j][r] = take_column(acc[i][j][r], 32 * j + 8 * (r >> 2) + (r & 3), t, &at);
+        const int row = m0 + wm0 + 32 * i + (lane & 31);
+        if (in && row < rows) arg.vocab.hit_value[row] = at;
+      }
+    }
     const int left = N - n0 - wn0;                             // columns of the wavefront tile that exist
     if (left < WN) {
 #pragma unroll

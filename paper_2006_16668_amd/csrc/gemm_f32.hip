@@ -83,7 +83,8 @@ struct F32Smem {
 // matrix has as many columns (a piece of a vocabulary, whose number of entries is any), and kept[0] rows of A and C count, or
 // terms of the sum with row-of-k operands.  Then "expert" e of A [R,lda] . B [k_total,N] sums the k from e K on, `add`: to
 // what C [e,R,N] holds; with row-of-k operands and k_total > 1 it sums the e-th of as many ranges of row_range() rows.  EPI 3 and 4, of the logits A . B^T: C is the gradient with respect to them, with zeros up to the next whole
-// 16 bytes, or nothing is stored but the maximum and sum of exponentials of each row's columns of a wavefront tile (VocabRows).
+// 16 bytes, or nothing is stored but the maximum and sum of exponentials of each row's columns of a wavefront tile and its target's
+// logit, which they leave out (VocabRows).
 template <int TM, int TN, int PD, int KG, int EPI, bool A_KC, bool B_KC, bool K_KEPT, bool PITCH>
 __global__ __launch_bounds__(256 * KG, TM * TN >= 4 ? 2 : TM * TN >= 2 ? 3 : 4) void gemm_f32_mfma_kernel(
     const float* __restrict__ A, const float* __restrict__ B, float* __restrict__ Cout,
@@ -344,7 +345,7 @@ __global__ __launch_bounds__(256 * KG, TM * TN >= 4 ? 2 : TM * TN >= 2 ? 3 : 4) 
           for (int v = 0; v < 16; ++v) main[i][j][v] += sums[g * (TM * TN * 4096) + ((i * TN + j) * 16 + v) * 64];
   }
 
-  // EPI 3: what a tile needs of its rows, one of which each lane fetches (a row's own fetch for every result took 45 us more than the
+  // EPI 3, 4: what a tile needs of its rows, one of which each lane fetches (a row's own fetch for every result took 45 us more than the
   // 140 of 1350 rows, M 512, V 16001)
   float row_lse = 0.f, row_up = 0.f, row_value = 0.f;
   int row_hit = -1;
@@ -353,6 +354,9 @@ __global__ __launch_bounds__(256 * KG, TM * TN >= 4 ? 2 : TM * TN >= 2 ? 3 : 4) 
     row_lse = vocab.lse2[at];
     row_up = vocab.grad[at];
     if (vocab.hit != nullptr) { row_hit = vocab.hit[at] - vocab.first; row_value = vocab.hit_value[at]; }
+  } else if (EPI == 4 && vocab.hit != nullptr) {
+    const int row = r0 + wm0 + (lane & (32 * TM - 1));
+    row_hit = vocab.hit[row < rows ? row : rows - 1];
   }
   // row of the lower half, row + 4 of the upper; while all lanes are active: what one holds that is not, the compiler need not keep
   auto of_row = [&](auto of_lane, int row) {
@@ -485,6 +489,19 @@ __global__ __launch_bounds__(256 * KG, TM * TN >= 4 ? 2 : TM * TN >= 2 ? 3 : 4) 
   if (__builtin_amdgcn_ballot_w64(!(zero == 0.f)) != 0) fp32_products(main);
   if constexpr (EPI == 4) {
     // a row's columns of the wavefront tile lie in the 32 lanes of a half
+    if (__builtin_amdgcn_ballot_w64((uint32_t)row_hit - (uint32_t)(n0 + wn0) < 32u * TN) != 0) {      // (few tiles have any)
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int at = 32 * i + 8 * (v >> 2) + (v & 3), hit = (int)((uint32_t)of_row(row_hit, at) - (uint32_t)(n0 + wn0 + l32));
+          float z = 0.f;
+#pragma unroll
+          for (int j = 0; j < TN; ++j) main[i][j][v] = take_column(main[i][j][v], 32 * j, hit, &z);
+          const int row = r0 + wm0 + at + 4 * hf;
+          if ((hit == 0 || (TN == 2 && hit == 32)) && row < rows) vocab.hit_value[row] = z;
+        }
+    }
 #pragma unroll
     for (int j = 0; j < TN; ++j)
       if (n0 + wn0 + 32 * j + l32 >= N) {

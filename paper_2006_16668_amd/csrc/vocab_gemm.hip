@@ -43,11 +43,13 @@ typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 constexpr int kXcds = 8;
 constexpr uint32_t kPiece = 16384, kStage = 4 * kPiece, kStaging = 2 * kStage;
 constexpr uint32_t kRowData = kStaging + 8 * 2048;             // lse2, grad, hit, hit_value of a tile's rows (kLogitGrad)
-constexpr uint32_t kSmem = kStaging + 8 * 4096;                // all 160 KB (kStats: 4 KB of staging per wavefront)
+constexpr uint32_t kSmem = kStaging + 8 * 4096;                // all 160 KB (statistics: 4 KB of staging per wavefront)
 
 static __device__ const u32x4_t vocab_zero_line = {0u, 0u, 0u, 0u};
 
-enum VocabEpi { kStats, kLogitGrad, kSums, kPlain };
+// kStats: statistics of the logits without the rows' targets, whose logits are stored (cross entropy).  kEntries: of all, and the logits
+// at a teacher's entries stored.  (As one kernel for both they hold more than the scalar registers take.)
+enum VocabEpi { kStats, kLogitGrad, kSums, kPlain, kEntries };
 enum VocabTile { kWhole, kUpper, kLeft };      // of a tile at the end the half that exists, its first 128 rows or columns
 
 struct VocabGemmArgs {
@@ -216,6 +218,16 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
     if (g.v.hit != nullptr) MOE_VG_WORDS(to + 2048, (wm == 0 ? reinterpret_cast<const float*>(g.v.hit) : g.v.hit_value) + at);
   };
 
+  // kStats: the targets of the wavefront's rows, into its own staging, behind what the wavefronts exchange
+  const uint32_t hits = lds0 + kStaging + wave * 4096 + 3072;
+  auto copy_hits = [&](int m0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int row = m0 + 128 * h + 64 * wm + lane_here();
+      MOE_VG_WORDS(hits + 256 * h, g.v.hit + (row < R ? row : R - 1));
+    }
+  };
+
   // ---- fragments
   const int p16 = lane & 15, bb = lane >> 4, bk = 8 * (bb >> 1) + (p16 >> 2);
   // where a wavefront's first fragment of a piece lies: K-contiguous ones of 16 k further on at ^ 32, of 32 rows at + 4096;
@@ -300,7 +312,7 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
     tile_at(tile, e, rt, ct);
     const int m0 = rt * 256, n0 = ct * 256;
     const int steps = (range_k(e) + 63) >> 6;
-    // kStats: the teacher's entries among this wavefront's results.  Where they are is fetched in the tile's first step, into the
+    // kEntries: the teacher's entries among this wavefront's results.  Where they are is fetched in the tile's first step, into the
     // wavefront's staging (as copy_row_data), the first 256 of them are copied to A1's place in the last one (read by all when phase 4
     // begins, free until the next tile's phase 2).
     int entries = 0;
@@ -326,12 +338,13 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
       if (!upper) read_a(1);
       if (!landed) asm volatile("s_waitcnt vmcnt(2)" ::: "memory");
       if (EPI == kLogitGrad && decltype(first_step)::value) copy_row_data(m0);
-      if (EPI == kStats && decltype(first_step)::value && g.v.starts != nullptr)
+      if (EPI == kStats && decltype(first_step)::value) copy_hits(m0);
+      if (EPI == kEntries && decltype(first_step)::value && g.v.starts != nullptr)
         MOE_VG_WORDS(lds0 + kStaging + wave * 4096, g.v.starts + (size_t)rt * (8 * tiles_n + 1) + 8 * ct + wave + lane_here());
       copy_b(tail);
       turn(first_step, 1, 1, !upper && !left);
       // phase 4
-      if (EPI == kStats && !decltype(first_step)::value && kt + 1 == steps && g.v.starts != nullptr) {
+      if (EPI == kEntries && !decltype(first_step)::value && kt + 1 == steps && g.v.starts != nullptr) {
         const u32x2_t start = *(lds_u2_ptr)(uintptr_t)(lds0 + kStaging + wave * 4096);
         const int found = __builtin_amdgcn_readfirstlane((int)start[0]);
         entries = __builtin_amdgcn_readfirstlane((int)start[1]) - found;
@@ -378,7 +391,7 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     const int lane = lane_here(), r32 = lane & 31, hh = lane >> 5;
     auto col_of = [&](int j) { return B_MNC ? 128 * j + 32 * wn : 64 * wn + 32 * j; };
-    if constexpr (EPI == kStats) {
+    if constexpr (EPI == kEntries) {
       // Logits at a teacher's entries, 256 at a time: each 32 x 32 part of the wavefront's that has any passes through LDS (the
       // register that holds an entry's logit differs from lane to lane).
       for (int done = 0; done < entries; done += 256) {
@@ -428,6 +441,8 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
             __builtin_amdgcn_wave_barrier();
           }
       }
+    }
+    if constexpr (EPI == kStats || EPI == kEntries) {
       const float c = g.v.scale;
       const int left = g.N - n0 - 64 * wn - 4 * hh;
       const uint32_t mine = lds0 + kStaging + wave * 4096;     // (maximum, sum) of 128 rows
@@ -435,11 +450,26 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
       for (int i = 0; i < 4; ++i) {
         if (i >= 2 && R - m0 <= 128) continue;                 // (what is met below of these rows is not stored)
         float mx = -INFINITY;
+        if constexpr (EPI == kStats) {                         // targets among these columns: few tiles have any
+          const int t = *(lds_i_ptr)(uintptr_t)(hits + 256 * (i >> 1) + 4 * (32 * (i & 1) + r32)) - (n0 + 64 * wn) - 4 * hh;
+          const bool in = t >= 0 && t < 64 && (t & 4) == 0;    // of this half's columns
+          if (__builtin_amdgcn_ballot_w64(in) != 0) {
+            float at = 0.f;
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) acc[i][j][r] = take_column(acc[i][j][r], 32 * j + 8 * (r >> 2) + (r & 3), t, &at);
+            const int row = m0 + 128 * (i >> 1) + 64 * wm + 32 * (i & 1) + r32;
+            if (in && row < R) g.v.hit_value[row] = at;
+          }
+        }
         if (n0 + 256 > g.N) {
+          int here = left;
+          if (EPI == kStats) asm volatile("" : "+v"(here));    // (nor are these masks kept from one i to the next)
 #pragma unroll
           for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][j][r] = 32 * j + 8 * (r >> 2) + (r & 3) < left ? acc[i][j][r] : -INFINITY;
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 32 * j + 8 * (r >> 2) + (r & 3) < here ? acc[i][j][r] : -INFINITY;
         }
 #pragma unroll
         for (int j = 0; j < 2; ++j)
@@ -584,6 +614,7 @@ int tiles_of(int n) { return (n + 255) / 256; }
 
 int prepare_vocab_gemm() {
   const int rcs[] = {prepare_vocab_tiles<kStats, false>(),     prepare_vocab_tiles<kStats, true>(),
+                     prepare_vocab_tiles<kEntries, false>(),   prepare_vocab_tiles<kEntries, true>(),
                      prepare_vocab_tiles<kLogitGrad, false>(), prepare_vocab_tiles<kLogitGrad, true>(),
                      prepare_vocab_tiles<kSums, false>(),      prepare_vocab_tiles<kSums, true>(),
                      prepare_vocab_tiles<kPlain, false>()};
@@ -600,8 +631,8 @@ int launch_vocab_tiles_logits(const GemmArgs& a, int rows, int entries, int M, h
   g.N = entries;
   g.tiles_n = tiles_of(entries);
   const long long tiles = (long long)tiles_of(rows) * g.tiles_n;
-  return a.vocab.stats != nullptr ? launch_tiles<kStats>(g, tiles, M % 64 != 0, st)
-                                  : launch_tiles<kLogitGrad>(g, tiles, M % 64 != 0, st);
+  if (a.vocab.stats == nullptr) return launch_tiles<kLogitGrad>(g, tiles, M % 64 != 0, st);
+  return a.vocab.hit != nullptr ? launch_tiles<kStats>(g, tiles, M % 64 != 0, st) : launch_tiles<kEntries>(g, tiles, M % 64 != 0, st);
 }
 
 int launch_vocab_tiles_dx(const GemmArgs& a, int M, hipStream_t st) {

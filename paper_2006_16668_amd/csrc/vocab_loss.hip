@@ -2,14 +2,16 @@
 // and 64k entries): x [N,M] are the last hidden states, w [V,M] one row per vocabulary entry, z = x . w^T the logits.
 //
 //   cross entropy   loss_n = lse_n - z[n,target_n],  lse_n = log sum_v exp z[n,v]
-//                   dz[n,v] = g_n (exp(z[n,v] - lse_n) - [v = target_n])
+//                          = log(1 + exp d_n),  d_n = log sum_{v != target_n} exp z[n,v]  -  z[n,target_n]
+//                   dz[n,v] = g_n (exp(z[n,v] - lse_n) - [v = target_n]),  exp(-loss_n) - 1 at the target
 //   distillation    q = softmax(t_n / T) over a teacher's K entries,  lse_n = log sum_v exp(z[n,v] / T)
 //                   loss_n = sum_k q_k (log q_k - z[n,i_k] / T + lse_n)
 //                   dz[n,v] = g_n / T (exp(z[n,v] / T - lse_n) - sum_{k: i_k = v} q_k)
 //   both            dx = dz . w,  dw = dz^T . x
 //
 // The logits are never kept: the forward product leaves of every row and wavefront tile the maximum and the sum of exponentials
-// (8 bytes for 32 to 256 logits), the backward pass multiplies again and keeps one piece of the vocabulary's dz for the two
+// (8 bytes for 32 to 256 logits), a target's logit left out of them and by itself, so that the loss of a token that is nearly sure is
+// no difference of near numbers (of lse and a logit, 16 each, 1e-6 would be left of 1e-4); the backward pass multiplies again and keeps one piece of the vocabulary's dz for the two
 // products that read it, in bf16 rounded once, as the upstream gradients of the expert layers are.
 //
 // The passes over rows take 50 of 1600 us forward, 65 of 5170 backward (32768 tokens, M 1024, V 32000): bound by memory.
@@ -36,10 +38,10 @@ struct VocabRowArgs {
   int32_t *perm, *pos, *kept;
   // forward: zeros for the tokens without a target
   float *loss, *lse;
+  int32_t* hit;                      // NULL, or the packed rows' targets
   // backward: what the products read per packed row
   const float *loss_in, *lse_in, *dloss;
   float inv_t, *lse2, *grad, *hit_value;
-  int32_t* hit;
   // backward with dx on 256 x 256 tiles: its ranges are chosen here, for the rows that there are
   int dx_entries, dx_tiles_n, M;     // dx_entries 0: no
   long long dx_rows;                 // rows of sums that there is room for
@@ -66,14 +68,12 @@ __device__ TokenData vocab_token_data(const VocabRowArgs& a, long long n) {
 }
 __device__ void vocab_row_data(const VocabRowArgs& a, int p, long long n, int32_t target, const TokenData& d) {
   a.perm[p] = (int32_t)n;
+  if (a.hit != nullptr) a.hit[p] = target;
   if (a.lse_in == nullptr) return;
   const float g = d.dloss * a.inv_t;
   a.lse2[p] = d.lse * kLog2e;
   a.grad[p] = g;
-  if (a.hit != nullptr) {                                      // exp(z - lse) - 1 at the target, where z - lse = -loss
-    a.hit[p] = target;
-    a.hit_value[p] = expm1f(-d.loss) * g;
-  }
+  if (a.hit != nullptr) a.hit_value[p] = expm1f(-d.loss) * g;  // exp(z - lse) - 1 at the target, where z - lse = -loss
 }
 // PER neighbouring tokens a thread.  One, for whole lines of all that is written, as long as counting the tokens before takes few
 // fetches (8336 tokens, all that a backward pass needs: four 9.5 us, one 4.8; 32768: 15.8 and 7.2); four where blocks are many.
@@ -319,18 +319,18 @@ __global__ __launch_bounds__(256) void vocab_few_kernel(VocabRowArgs a, TeacherA
 
 // ---------------------------------------------------------------- loss of the packed rows
 // ROWS rows a block: the 256 / ROWS threads of a row meet the slots' maxima and sums, then the 16 lanes of a group finish one row:
-// its target's logit (cross entropy), or the sum over the teacher's entries.  16 rows read whole lines of the statistics; a row
-// by itself is done sooner where there are few.  kept NULL: no rows were numbered, row n is token n.
-template <typename T, bool TEACHER, int ROWS>
+// the loss and log-sum from those of the other entries and the target's logit (cross entropy), or the sum over the teacher's entries.
+// 16 rows read whole lines of the statistics; a row by itself is done sooner where there are few.  kept NULL: no rows were numbered,
+// row n is token n.
+template <bool TEACHER, int ROWS>
 __global__ __launch_bounds__(256) void vocab_finish_kernel(const float2* __restrict__ stats, int slots, long long N,
                                                            const int32_t* __restrict__ perm, const int32_t* __restrict__ kept,
-                                                           const uint4* __restrict__ x, const uint4* __restrict__ w, int pieces,
                                                            const int32_t* __restrict__ target, const int32_t* __restrict__ flags,
-                                                           TeacherArgs t,
+                                                           const float* __restrict__ hit_logit, TeacherArgs t,
                                                            const float2* __restrict__ tstat, const float* __restrict__ z,
                                                            float* __restrict__ loss, float* __restrict__ lse) {
   __shared__ float2 part[16][17];
-  __shared__ float lse_of[16];
+  __shared__ float2 sum_of[16];                                // 2^(x + y) is the sum
   const long long p0 = (long long)blockIdx.x * ROWS;
   const int rows = kept != nullptr ? kept[0] : (int)N;
   if (p0 >= rows) return;
@@ -353,7 +353,7 @@ __global__ __launch_bounds__(256) void vocab_finish_kernel(const float2* __restr
 #pragma unroll
       for (int o = 1; o < 16; o <<= 1) meet(m, s, float2{__shfl_xor(m, o, 64), __shfl_xor(s, o, 64)});
     }
-    lse_of[r] = (m + log2f(s)) * kLn2;
+    sum_of[r] = float2{m, log2f(s)};
   }
   __syncthreads();
   if (sl >= ROWS || p0 + sl >= rows) return;                   // (whole groups of 16 lanes)
@@ -362,13 +362,13 @@ __global__ __launch_bounds__(256) void vocab_finish_kernel(const float2* __restr
     return;
   }
   const long long n = kept != nullptr ? perm[p0 + sl] : p0 + sl;
-  const float l = lse_of[sl];
-  float out;
+  const float2 q2 = sum_of[sl];
+  float l = (q2.x + q2.y) * kLn2, out;
   if (!TEACHER) {
-    // never below 0 but for rounding: the sums are not in the products' order.  At a probability of 1 that would turn the gradient at
-    // the target, expm1(-loss), round.  (NaN stays)
-    out = l - row_dot<T>(x + (size_t)n * pieces, w + (size_t)target[n] * pieces, pieces, r);
-    out = out < 0.f ? 0.f : out;
+    // d: what is added to the fma's difference is small where that is; the larger of the two logits stands outside the logarithm
+    const float zt = hit_logit[p0 + sl], d = (fmaf(-kLog2e, zt, q2.x) + q2.y) * kLn2, more = log1pf(expf(-fabsf(d)));
+    out = zt == INFINITY ? NAN : (d > 0.f ? d : 0.f) + more;
+    l = (d > 0.f ? l : zt) + more;
   } else {
     const float2 ts = tstat[n];
     const float inv = 1.f / ts.y, log_sum = logf(ts.y);
@@ -543,6 +543,8 @@ VocabWs carve_vocab(const moe_config& c, const moe_vocab_dims& d, bool teacher, 
     w.starts = take(f.sorts ? (whole / 256 * ((size_t)8 * ((d.V + 255) / 256) + 1) + 64) * 4 : 0);      // (a wavefront fetches 64)
     w.sorted = take(f.sorts ? (N * d.K + 64) * 8 : 0);             // (a wavefront fetches whole 32)
     w.stats = take((size_t)w.slots * N * 8);
+    w.hit = take(teacher ? 0 : N * 4);
+    w.hit_logit = take(teacher ? 0 : N * 4);
   } else {
     w.pos = take(N * 4);
     w.lse2 = take(N * 4);
@@ -587,7 +589,7 @@ static VocabRowArgs row_args(const moe_config& c, const moe_vocab_dims& d, const
   r.kept = reinterpret_cast<int32_t*>(base + ws.kept);
   return r;
 }
-// up to 64 tokens; packed and z may be NULL
+// up to 1024 tokens, with a teacher 64; packed and z may be NULL
 static int launch_few(const moe_config& c, const VocabRowArgs& r, const TeacherArgs& t, const VocabCall& a, char* base,
                       const VocabWs& ws, float* z, void* packed, hipStream_t st) {
   const int pieces = c.M * (c.act_dtype == MOE_F32 ? 4 : 2) / 16;
@@ -633,6 +635,7 @@ int launch_vocab_forward(const moe_config& c, const moe_vocab_dims& d, const Voc
   VocabRowArgs r = row_args(c, d, a, base, ws);
   r.loss = a.loss;
   r.lse = a.lse;
+  if (a.target != nullptr) r.hit = reinterpret_cast<int32_t*>(base + ws.hit);
   const VocabForwardPlan plan = forward_plan(c, d, a.target == nullptr);
   const bool packs = plan.packs, sorts = plan.sorts;
   const bool few = N <= kFewTokens && !packs, all = plan.all && !(few && a.target == nullptr);
@@ -656,6 +659,11 @@ int launch_vocab_forward(const moe_config& c, const moe_vocab_dims& d, const Voc
   g.kept = all ? nullptr : r.kept;
   g.vocab.scale = kLog2e * inv_t;
   g.vocab.stats = stats;
+  float* const hit_logit = reinterpret_cast<float*>(base + ws.hit_logit);
+  if (a.target != nullptr) {
+    g.vocab.hit = all ? a.target : r.hit;                      // (one outside the vocabulary is in no column)
+    g.vocab.hit_value = hit_logit;
+  }
   if (sorts) {
     g.vocab.starts = reinterpret_cast<const int32_t*>(base + ws.starts);
     g.vocab.sorted = reinterpret_cast<const uint2*>(base + ws.sorted);
@@ -664,21 +672,13 @@ int launch_vocab_forward(const moe_config& c, const moe_vocab_dims& d, const Voc
   }
   rc = f32 ? launch_gemm_f32(kDataGrad, g, 1, (int)N, d.V, c.M, st) : launch_vocab_logits(g, (int)N, d.V, c.M, st);
   if (rc != MOE_OK) return rc;
-  const int pieces = c.M * (f32 ? 4 : 2) / 16;
   const bool single = N <= 1024;                               // a block per row where 16 rows each would not fill the units
   auto finish = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)(single ? N : (N + 15) / 16)), dim3(256), 0, st, stats, ws.slots, N, r.perm, g.kept,
-                       static_cast<const uint4*>(a.x), static_cast<const uint4*>(a.w), pieces, a.target, r.has, t,
-                       reinterpret_cast<const float2*>(base + ws.tstat), a.entry_logit, a.loss, a.lse);
+                       a.target, r.has, hit_logit, t, reinterpret_cast<const float2*>(base + ws.tstat), a.entry_logit, a.loss, a.lse);
   };
-  auto finish_as = [&](auto one, auto many) { if (single) finish(one); else finish(many); };
-  if (a.target != nullptr) {
-    if (f32) finish_as(vocab_finish_kernel<float, false, 1>, vocab_finish_kernel<float, false, 16>);
-    else finish_as(vocab_finish_kernel<bf16_t, false, 1>, vocab_finish_kernel<bf16_t, false, 16>);
-  } else {
-    if (f32) finish_as(vocab_finish_kernel<float, true, 1>, vocab_finish_kernel<float, true, 16>);
-    else finish_as(vocab_finish_kernel<bf16_t, true, 1>, vocab_finish_kernel<bf16_t, true, 16>);
-  }
+  if (a.target != nullptr) finish(single ? vocab_finish_kernel<false, 1> : vocab_finish_kernel<false, 16>);
+  else finish(single ? vocab_finish_kernel<true, 1> : vocab_finish_kernel<true, 16>);
   return check_launch();
 }
 

@@ -48,7 +48,9 @@ def narrowed(code):
             if state.get(n) != met:
                 state[n] = met
                 todo.append(n)
-    reads = [i for i in state if code[i].name.startswith("v_readlane")]
+    # (scalar values that the compiler keeps in lanes of a register: v_writelane reaches a lane that is not active, too)
+    kept = {re.split(r",\s*", c.text.partition(" ")[2])[0] for c in code if c.name.startswith("v_writelane")}
+    reads = [i for i in state if code[i].name.startswith("v_readlane") and re.split(r",\s*", code[i].text)[1] not in kept]
     return len(reads), [code[i].text for i in reads if not state[i][0]]
 
 
@@ -81,6 +83,6 @@ def test_registers_of_other_lanes_are_read_by_whole_wavefronts(tmp_path):
                     os.path.join(build.CSRC, src), "-o", out], check=True, capture_output=True)
     found = {k: narrowed(code) for k, code in _kernels(open(out).read()).items() if code}
     reading = {k: v for k, v in found.items() if v[0]}
-    assert len(reading) == 5                             # the gradient of a vocabulary's logits, in every form
+    assert len(reading) == 10                            # a vocabulary's logits, their statistics and gradient, in every form
     for name, (reads, wrong) in reading.items():
         assert not wrong, (name, reads, len(wrong), wrong[:3])
