@@ -89,11 +89,17 @@ class _Stream:
 @pytest.mark.gpu
 @pytest.mark.parametrize("one,other", [(EDGE[0], EDGE[1]), (EDGE[2], EDGE[3]), (TILES[0], EDGE[2]), (TILES[1], TILES[0]), (TILES[2], TILES[3])])
 def test_streams_that_run_at_once(one, other):
-    """Several rounds of both passes on two streams with nothing between them that waits: kernels of one run beside kernels of the
-    other.  Other inputs on each, so that a result in the wrong place shows."""
+    """Several rounds of both passes on two streams with nothing between them that waits, all enqueued before the first may start (else
+    small calls are done before the host has made the next): kernels of one run beside kernels of the other.  Other inputs on each, so
+    that a result in the wrong place shows."""
     moe.moe_prepare()
     jobs = [_Stream(*one, seed=3), _Stream(*other, seed=4)]
     torch.cuda.synchronize()
+    start = torch.cuda.Event()
+    torch.cuda._sleep(60_000_000)                                # (some 30 ms of the default stream)
+    start.record()
+    for j in jobs:
+        j.stream.wait_event(start)
     for i in range(8):
         for j in jobs if i % 2 == 0 else jobs[::-1]:
             j.enqueue()
