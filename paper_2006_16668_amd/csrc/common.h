@@ -379,12 +379,12 @@ int launch_attention_core(int act_dtype, const void* qkv, void* ctx, float* lse,
 
 // backward of the encoder sub-layers (encoder_bwd.hip)
 //   ds = dres (may be NULL) + d LN(s) / d s applied to dn; dgamma, dbeta [M]; partial:
-//   layer_norm_bwd_bytes() of scratch.  dx may alias dres.  as_before: rows of up to 8 KB by wavefronts, as the
-//   encoder layers' calls have always had the sums of the parameters' gradients
-size_t layer_norm_bwd_bytes(int act_dtype, long long rows, int M, bool as_before);
+//   layer_norm_bwd_bytes() of scratch.  dx may alias dres.  by_wavefronts: rows of up to 8 KB (and 4096
+//   columns) by wavefronts in any case: the encoder layers' gradients of the parameters keep the order of their sums
+size_t layer_norm_bwd_bytes(int act_dtype, long long rows, int M, bool by_wavefronts);
 int launch_layer_norm_bwd(int act_dtype, const void* s, const void* dn, const float* gamma,
                           const void* dres, void* dx, float* partial, float* dgamma, float* dbeta,
-                          long long rows, int M, bool as_before, hipStream_t st);
+                          long long rows, int M, bool by_wavefronts, hipStream_t st);
 //   dqkv [B*L, 3*heads*d] from qkv, ctx, dctx [B*L, heads*d] and lse; dvec: [B*heads*L] scratch
 // dW [in,out] = X^T dY over rows tokens (X [rows,in], dY [rows,out]); partial: scratch of
 // dense_wgrad_partial_bytes() for the token ranges of the split (may be NULL: no split)

@@ -540,28 +540,28 @@ int launch_dense_grads(const moe_config& c, long long rows, int in, int out, con
 // four, two or one per unit with one, one or more vectors a thread (the sums that a block leaves are as long as four rows; 8192 x 2400
 // 256 blocks 67, 512 49, 768 53).
 enum LayerNormBwdForm { kLnWavefronts, kLnBlocks, kLnAny };
-static LayerNormBwdForm layer_norm_bwd_plan(int act_dtype, long long rows, int M, bool as_before, int* parts) {
+static LayerNormBwdForm layer_norm_bwd_plan(int act_dtype, long long rows, int M, bool by_wavefronts, int* parts) {
   const int vec = M * (act_dtype == MOE_F32 ? 4 : 2) / 16;
-  const int waves = as_before || rows < 1024 ? 512 : act_dtype == MOE_F32 ? 320 : 192;
+  const int waves = by_wavefronts || rows < 1024 ? 512 : act_dtype == MOE_F32 ? 320 : 192;
   const LayerNormBwdForm form = vec <= waves && M <= 4096 ? kLnWavefronts : vec <= 2048 ? kLnBlocks : kLnAny;
   const long long most = form == kLnWavefronts || (form == kLnBlocks && vec <= 256) ? 1024
                          : form == kLnBlocks ? (vec <= 512 ? 512 : 256) : 64, blocks = (rows + 3) / 4;
   *parts = (int)(blocks < most ? blocks : most);
   return form;
 }
-size_t layer_norm_bwd_bytes(int act_dtype, long long rows, int M, bool as_before) {
+size_t layer_norm_bwd_bytes(int act_dtype, long long rows, int M, bool by_wavefronts) {
   int parts;
-  const LayerNormBwdForm form = layer_norm_bwd_plan(act_dtype, rows, M, as_before, &parts);
+  const LayerNormBwdForm form = layer_norm_bwd_plan(act_dtype, rows, M, by_wavefronts, &parts);
   return (size_t)parts * 2 * M * sizeof(float) + (form == kLnAny ? (size_t)rows * sizeof(float2) : 0);
 }
 
 int launch_layer_norm_bwd(int act_dtype, const void* s, const void* dn, const float* gamma,
                           const void* dres, void* dx, float* partial, float* dgamma, float* dbeta,
-                          long long rows, int M, bool as_before, hipStream_t st) {
+                          long long rows, int M, bool by_wavefronts, hipStream_t st) {
   const int elt = act_dtype == MOE_F32 ? 4 : 2;
   const int vec_per_row = M * elt / 16;
   const int vpl = (vec_per_row + 63) / 64;
-  if (!as_before && rows <= 64 && M <= 1024) {
+  if (!by_wavefronts && rows <= 64 && M <= 1024) {
     // One block of 16 wavefronts, whose sums are the parameters' gradients: one launch (37 rows of 520 fp32, with the call from Python
     // 17.6 -> 12.5 us).
     auto one = [&](auto kernel) {
@@ -581,7 +581,7 @@ int launch_layer_norm_bwd(int act_dtype, const void* s, const void* dn, const fl
   const size_t lds = (size_t)4 * M * sizeof(float);
   const float eps = 1e-6f;
   int parts;
-  const LayerNormBwdForm form = layer_norm_bwd_plan(act_dtype, rows, M, as_before, &parts);
+  const LayerNormBwdForm form = layer_norm_bwd_plan(act_dtype, rows, M, by_wavefronts, &parts);
   auto reduce = [&]() {
     hipLaunchKernelGGL(layer_norm_param_reduce_kernel, dim3((unsigned)((2 * M + 15) / 16)), dim3(16 * kReduceGroups), 0, st,
                        partial, parts, M, dgamma, dbeta);

@@ -9,8 +9,9 @@
 // and starts copies, and a barrier makes them change places.  The matrix pipe is then handed from one to the other instead of
 // waiting for the LDS (one wavefront per SIMD with all 256 accumulators, the expert products' persistent kernel, keeps it 60 %
 // busy where clocks are not the limit, operands of zeros; 128 x 256 tiles, two blocks per unit, less).
-// Bound by power: 31130 rows, M 1024, 32000 entries, z and its statistics 1.55 ms (1.32 PFLOP/s at 1.44 GHz, the matrix pipe 75 %
-// busy), dz 1.05 to 1.15 (exponentials at a tile's end), dx 1.27 and dw 1.30 (87 % at 1.29 GHz); a library's 8192^3 is at 1.38.
+// Bound by power: 31130 rows, M 1024, 32000 entries, z and its statistics 1.54 to 1.6 ms, 1.28 to 1.33 PFLOP/s at 1.5 GHz, the
+// matrix pipe 73 % busy; dz 1.04 to 1.13 PFLOP/s, dx 1.27 to 1.33 and dw 1.30 to 1.36 (86 % busy at 1.4 GHz); a library's 8192^3 is at 1.38
+// PFLOP/s.  dz's tile end, of 982 us a launch of half the entries: stores 73, the pass through LDS 81, exponentials 40.
 //
 // A wavefront tile is 2 x 64 rows (of the upper and the lower 128 of the tile) by 2 x 32 columns, so the operands of a step are
 // four LDS pieces of 16 KB, A0 A1 B0 B1, and a step has four phases of eight MFMAs:

@@ -14,7 +14,7 @@
 // no difference of near numbers (of lse and a logit, 16 each, 1e-6 would be left of 1e-4); the backward pass multiplies again and keeps one piece of the vocabulary's dz for the two
 // products that read it, in bf16 rounded once, as the upstream gradients of the expert layers are.
 //
-// The passes over rows take 50 of 1600 us forward, 65 of 5170 backward (32768 tokens, M 1024, V 32000): bound by memory.
+// The passes over rows take 36 of 1600 us forward, 65 of 5100 backward (32768 tokens, M 1024, V 32000): bound by memory.
 //
 // Tokens without a target (padding, prompts) are left out of every product: the rows that have one are numbered first
 // (vocab_rows_kernel), so neither their work nor what their x holds, NaN included, reaches anything.
