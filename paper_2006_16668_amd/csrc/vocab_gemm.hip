@@ -220,7 +220,7 @@ __global__ __launch_bounds__(512, 2) void vocab_gemm_kernel(VocabGemmArgs g) {
   };
 
   // kStats: the targets of the wavefront's rows, into its own staging, behind what the wavefronts exchange
-  const uint32_t hits = lds0 + kStaging + wave * 4096 + 3072;
+  const uint32_t hits = lds0 + kStaging + wave * 4096 + 3 * 1024;
   auto copy_hits = [&](int m0) __attribute__((always_inline)) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {

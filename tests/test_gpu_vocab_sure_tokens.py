@@ -86,3 +86,13 @@ def test_gradient_of_a_sure_target(dtype, scale):
     t = want.abs() * (_relative(M, off, S_abs) + 16 * U + 3 * HALF[dtype]) + 2.0 ** -126
     ratio = ((r["dw"][d["target"][0].long()].double() - want).abs() / t).max().item()
     assert ratio <= 1
+
+
+@pytest.mark.parametrize("S,M,V,dtype", [(257, 64, 257, "bf16"), (60, 72, 60, "bf16"), (1030, 136, 515, "bf16"), (700, 520, 700, "bf16"), (255, 36, 255, "f32"),
+                                         (1030, 260, 515, "f32"), (700, 516, 700, "f32"), (2304, 1024, 9000, "bf16"), (2100, 448, 33333, "bf16")])
+def test_targets_in_every_column(S, M, V, dtype):
+    """Each column of a tile is some row's target, the last one of the vocabulary among them, and rows of a tile share one."""
+    d = make(1, S, M, V, dtype)
+    d["target"] = (V - 1 - torch.arange(S, device=DEV) * (1 if V <= S else 17) % V).int()
+    d["target"][S // 2:S // 2 + 9] = V // 2
+    check(1, S, M, V, dtype, d, call(1, S, M, V, dtype, d))

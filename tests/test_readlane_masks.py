@@ -1,7 +1,7 @@
 """v_readlane takes a value from a lane whether that lane is active or not, but what a register holds there is only what the lane
 computed while it was: the compiler may load, copy or reload a value under a mask that has left the lane out.  So the lanes of a
 wavefront that read each other's registers do it while all of them are active.  In the code the compiler makes of gemm_f32.hip
-today (no GPU: read from this build's own assembly), along every path: no v_readlane where the execution mask may be narrower
+today (no GPU: read from the library's own assembly), along every path: no v_readlane where the execution mask may be narrower
 than at the kernel's start."""
 import os
 import re
