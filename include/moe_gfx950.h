@@ -500,6 +500,123 @@ int moe_vocab_distill_backward(const moe_config* cfg, const moe_vocab_dims* dims
                                const float* entry_logit, const float* lse, const float* dloss,
                                void* dx, void* dw, void* ws, size_t ws_bytes, void* stream);
 
+/*
+ * ---- The decoder's attention to the encoder -----------------------------------------
+ * Section 2.1: a decoder layer attends to the encoder's states between its self-attention and its feed-forward layer.  Each of B
+ * sources has Lk states mem [B,Lk,M], of which the first src_len[b] hold (none to all; other values count as the nearest of
+ * these), and Lq tokens u [B,Lq,M] = [G,S,M] that attend to them, all to all: several hypotheses of a sentence are tokens of one
+ * source.  Heads may share keys and values: head h uses those of h / (heads / kv_heads).  With A = heads d, Akv = kv_heads d:
+ *     [K|V] = mem . wkv      q = u . wq      ctx = softmax(q K^T / sqrt(d)) V over the states that hold      out = ctx . wo
+ * Whatever kv and (backward) mem hold for states that do not is not used.  A token whose source has none gets a row of zeros.
+ */
+typedef struct {
+  int32_t B;                 /* sources; B Lq == cfg->G cfg->S */
+  int32_t Lq, Lk;            /* tokens and states of a source; B Lk up to 2^30 */
+  int32_t heads, kv_heads;   /* heads / kv_heads: 1, 2, 4, 8, 16 or 32; heads d below 2^23, Lq heads / kv_heads below 2^29 */
+  int32_t d;                 /* 64 or 128 */
+} moe_cross_dims;
+
+/* Bytes of workspace of moe_cross_attention, of moe_cross_attention_train and of the backward pass.  Pure host functions. */
+int moe_cross_workspace_bytes(const moe_config* cfg, const moe_cross_dims* dims, size_t* bytes);
+int moe_cross_train_workspace_bytes(const moe_config* cfg, const moe_cross_dims* dims, size_t* bytes);
+int moe_cross_backward_workspace_bytes(const moe_config* cfg, const moe_cross_dims* dims, size_t* bytes);
+
+/* kv [B,Lk,2 Akv] = mem [B,Lk,M] . wkv [M,2 Akv]: columns [0,Akv) K, [Akv,2 Akv) V; all rows.  Once per source in generation. */
+int moe_cross_keys(const moe_config* cfg, const moe_cross_dims* dims, const void* mem, const void* wkv, void* kv, void* stream);
+
+/* in: u [G,S,M], kv as moe_cross_keys leaves it, src_len [B] i32 or NULL (all states hold), wq [M,A], wo [A,M].  out [G,S,M].
+ * ws >= moe_cross_workspace_bytes, 256-byte aligned.  bf16: q, the probabilities and ctx are rounded once each (the probabilities
+ * of calls with few tokens are not); softmax statistics and sums are fp32, sums in a fixed order. */
+int moe_cross_attention(const moe_config* cfg, const moe_cross_dims* dims, const void* u, const void* kv, const int32_t* src_len,
+                        const void* wq, const void* wo, void* out, void* ws, size_t ws_bytes, void* stream);
+
+/* The same result; ws (>= moe_cross_train_workspace_bytes) keeps q, ctx and the row statistics for the backward pass. */
+int moe_cross_attention_train(const moe_config* cfg, const moe_cross_dims* dims, const void* u, const void* kv,
+                              const int32_t* src_len, const void* wq, const void* wo, void* out, void* ws, size_t ws_bytes,
+                              void* stream);
+
+/* Gradients of L = sum dout out, through kv to mem and wkv.  in: as given to moe_cross_keys and moe_cross_attention_train, kv as the
+ * first and fwd_ws as the second left it (read only); dout [G,S,M].  out, every element written: du [G,S,M], dmem [B,Lk,M] (zeros
+ * for states that do not hold), dwq, dwkv, dwo.  They must not overlap the inputs.  ws >= moe_cross_backward_workspace_bytes,
+ * 256-byte aligned.  bf16: dctx, the probabilities, their gradients, dq, dK and dV are rounded once each.  No atomics: results are
+ * reproducible bit for bit. */
+int moe_cross_attention_backward(const moe_config* cfg, const moe_cross_dims* dims, const void* u, const void* mem, const void* kv,
+                                 const int32_t* src_len, const void* wq, const void* wkv, const void* wo, const void* dout,
+                                 const void* fwd_ws, size_t fwd_ws_bytes, void* du, void* dmem, void* dwq, void* dwkv, void* dwo,
+                                 void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * ---- Losses of preference and policy ---------------------------------------------------
+ * Both take the token losses nll [G,S] that moe_vocab_loss leaves (minus the log-probability of the token's target) and give the
+ * gradient at them, which moe_vocab_loss_backward takes as dloss.  A token without a target (outside 0 .. V-1) has no part:
+ * whatever its other inputs hold is not used, and what is written for it is 0.  act_dtype, M and the experts of cfg do not count.
+ */
+#define MOE_PREFERENCE_LOGISTIC 0
+#define MOE_PREFERENCE_SQUARED 1
+typedef struct {
+  int32_t P;                 /* pairs of sequences: 2p is preferred to 2p + 1 */
+  int32_t V;                 /* entries of the vocabulary */
+  int32_t kind;              /* MOE_PREFERENCE_ */
+  double beta, smoothing;    /* beta > 0; smoothing in [0, 1), of the logistic loss */
+} moe_preference_dims;
+
+/* ratio[i] = sum over sequence i of ref_nll - nll (the log of the ratio to the reference model), h = ratio[2p] - ratio[2p + 1]:
+ *   logistic  loss[p] = -(1 - smoothing) log sigmoid(beta h) - smoothing log sigmoid(-beta h)
+ *   squared   loss[p] = (h - 1 / (2 beta))^2
+ * in: nll, ref_nll [G,S] fp32, target [G,S] i32; start [2P+1] i32, ascending: sequence i is the tokens start[i] .. start[i+1] - 1
+ * of the G S in order (values outside 0 .. G S count as the nearest of these).  out: loss [P], ratio [2P] fp32.  Sums in 64 bits. */
+int moe_preference_loss(const moe_config* cfg, const moe_preference_dims* dims, const float* nll, const float* ref_nll,
+                        const int32_t* target, const int32_t* start, float* loss, float* ratio, void* stream);
+
+/* dnll [G,S] of L = sum dloss[p] loss[p]; ratio as moe_preference_loss left it.  Every element is written, 0 outside the
+ * sequences. */
+int moe_preference_loss_backward(const moe_config* cfg, const moe_preference_dims* dims, const int32_t* target, const int32_t* start,
+                                 const float* ratio, const float* dloss, float* dnll, void* stream);
+
+typedef struct {
+  int32_t V;                 /* entries of the vocabulary */
+  int32_t adv_per_token;     /* adv is [G,S], or 0: [G] */
+  double clip_low, clip_high;/* the ratio is bounded to 1 - clip_low .. 1 + clip_high; 0 <= clip_low <= 1, clip_high >= 0 */
+  double beta;               /* of the KL term, >= 0 and finite; 0: without one */
+} moe_policy_dims;
+
+/* r = exp(old_nll - nll), x = nll - ref_nll, per token:
+ *   loss = -min(r adv, clip(r) adv) + beta kl,   kl = e^x - 1 - x >= 0
+ * in: nll, old_nll (of the policy that sampled the tokens), ref_nll (NULL with beta 0) [G,S], adv fp32; target [G,S] i32.  out: loss [G,S]; kl
+ * [G,S] or NULL.  Reductions are the caller's.  Which side of a bound r lies on is decided in 64 bits.  adv of 0 gives 0. */
+int moe_policy_loss(const moe_config* cfg, const moe_policy_dims* dims, const float* nll, const float* old_nll, const float* ref_nll,
+                    const float* adv, const int32_t* target, float* loss, float* kl, void* stream);
+
+/* dnll [G,S] of L = sum dloss loss: dloss (r adv where the bound does not hold the ratio + beta (e^x - 1)).  At a bound the ratio
+ * is not held.  (The gradient at nll: -d/d log p.) */
+int moe_policy_loss_backward(const moe_config* cfg, const moe_policy_dims* dims, const float* nll, const float* old_nll,
+                             const float* ref_nll, const float* adv, const int32_t* target, const float* dloss, float* dnll,
+                             void* stream);
+
+/*
+ * ---- Clipping by the norm of all gradients ---------------------------------------------
+ * A host array says where the gradients are; its addresses are 16-byte aligned, a tensor of no elements may have none.
+ */
+typedef struct {
+  const void* src;
+  void* dst;                 /* src itself or no other tensor's memory; written by moe_clip_gradients, not read else (may be NULL
+                                for moe_gradient_norm) */
+  int64_t count;             /* elements */
+  int32_t dtype;             /* moe_dtype */
+} moe_gradient;
+
+/* Bytes of workspace of moe_gradient_norm.  Pure host function. */
+int moe_gradient_norm_workspace_bytes(const moe_gradient* list, int32_t n, size_t* bytes);
+
+/* norm[0] = sqrt(sum of the squares of all elements of the n tensors), formed in 64 bits in a fixed order and rounded to fp32 once.
+ * ws >= moe_gradient_norm_workspace_bytes, 256-byte aligned. */
+int moe_gradient_norm(const moe_gradient* list, int32_t n, float* norm, void* ws, size_t ws_bytes, void* stream);
+
+/* dst = src min(1, max_norm / norm[0]), rounded once, for all n tensors.  A norm that is infinite or NaN leaves the gradients as
+ * they are, for the caller to see.  max_norm >= 0.  norm is a device pointer: a caller with shards on several devices puts the
+ * root of the sum of their squares there. */
+int moe_clip_gradients(const moe_gradient* list, int32_t n, const float* norm, double max_norm, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -5,7 +5,12 @@
 ``libmoe_gfx950.so`` (built by ``python -m paper_2006_16668_amd.build``).
 There is no CPU fallback: a missing library raises on first use.
 """
-from .binding import (EncoderDims, VocabDims, moe_add_layer_norm_backward, moe_layer_norm_backward_workspace_bytes,
+from .binding import (CrossDims, PreferenceDims, PolicyDims, GradientList, moe_cross_workspace_bytes, moe_cross_train_workspace_bytes,
+                      moe_cross_backward_workspace_bytes, moe_cross_keys, moe_cross_attention,
+                      moe_cross_attention_train, moe_cross_attention_backward, moe_preference_loss,
+                      moe_preference_loss_backward, moe_policy_loss, moe_policy_loss_backward,
+                      moe_gradient_norm_workspace_bytes, moe_gradient_norm, moe_clip_gradients,
+                      EncoderDims, VocabDims, moe_add_layer_norm_backward, moe_layer_norm_backward_workspace_bytes,
                       moe_vocab_loss, moe_vocab_loss_backward, moe_vocab_distill,
                       moe_vocab_distill_backward, moe_vocab_workspace_bytes, moe_vocab_backward_workspace_bytes, moe_add_layer_norm, moe_attention_workspace_bytes,
                       moe_dense_ffn, moe_encoder_pair_forward, moe_encoder_workspace_bytes,
@@ -17,7 +22,12 @@ from .binding import (EncoderDims, VocabDims, moe_add_layer_norm_backward, moe_l
                       moe_gate, moe_gate_pack, moe_gate_pack_bytes, moe_gate_prepacked, moe_forward_prepacked, moe_gate_noalloc, moe_gate_noalloc_max_bytes, moe_gate_workspace_bytes,
                       moe_prepare, moe_status_string, moe_train_workspace_bytes, moe_workspace_bytes)
 
-__all__ = ["moe_add_layer_norm_backward", "moe_layer_norm_backward_workspace_bytes", "VocabDims", "moe_vocab_loss", "moe_vocab_loss_backward", "moe_vocab_distill", "moe_vocab_distill_backward",
+__all__ = ["CrossDims", "PreferenceDims", "PolicyDims", "GradientList", "moe_cross_workspace_bytes",
+           "moe_cross_train_workspace_bytes", "moe_cross_backward_workspace_bytes", "moe_cross_keys",
+           "moe_cross_attention", "moe_cross_attention_train", "moe_cross_attention_backward", "moe_preference_loss",
+           "moe_preference_loss_backward", "moe_policy_loss", "moe_policy_loss_backward",
+           "moe_gradient_norm_workspace_bytes", "moe_gradient_norm", "moe_clip_gradients",
+           "moe_add_layer_norm_backward", "moe_layer_norm_backward_workspace_bytes", "VocabDims", "moe_vocab_loss", "moe_vocab_loss_backward", "moe_vocab_distill", "moe_vocab_distill_backward",
            "moe_vocab_workspace_bytes", "moe_vocab_backward_workspace_bytes", "EncoderDims", "moe_add_layer_norm", "moe_attention_workspace_bytes", "moe_dense_ffn",
            "moe_encoder_pair_forward", "moe_encoder_workspace_bytes", "moe_self_attention",
            "moe_encoder_pair_forward_train", "moe_encoder_pair_backward",

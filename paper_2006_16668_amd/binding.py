@@ -32,7 +32,12 @@ EXPORTS = ("moe_status_string", "moe_prepare", "moe_gate_workspace_bytes", "moe_
            "moe_encoder_pair_backward",
            "moe_vocab_workspace_bytes", "moe_vocab_backward_workspace_bytes", "moe_vocab_loss", "moe_vocab_loss_backward",
            "moe_vocab_distill", "moe_vocab_distill_backward",
-           "moe_layer_norm_backward_workspace_bytes", "moe_add_layer_norm_backward")
+           "moe_layer_norm_backward_workspace_bytes", "moe_add_layer_norm_backward",
+           "moe_cross_workspace_bytes", "moe_cross_train_workspace_bytes", "moe_cross_backward_workspace_bytes", "moe_cross_keys",
+           "moe_cross_attention", "moe_cross_attention_train", "moe_cross_attention_backward",
+           "moe_preference_loss", "moe_preference_loss_backward", "moe_policy_loss", "moe_policy_loss_backward",
+           "moe_gradient_norm_workspace_bytes", "moe_gradient_norm", "moe_clip_gradients")
+PREFERENCE_KINDS = {"logistic": 0, "squared": 1}
 FORWARD_EVENTS = 6
 BACKWARD_EVENTS = 8
 
@@ -73,6 +78,68 @@ class VocabDims:
 
     def _c(self):
         return _VocabDims(self.V, self.K, self.piece, self.temperature)
+
+
+class _CrossDims(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "Lq", "Lk", "heads", "kv_heads", "d")]
+
+
+class _PreferenceDims(ctypes.Structure):
+    _fields_ = [("P", ctypes.c_int32), ("V", ctypes.c_int32), ("kind", ctypes.c_int32), ("beta", ctypes.c_double),
+                ("smoothing", ctypes.c_double)]
+
+
+class _PolicyDims(ctypes.Structure):
+    _fields_ = [("V", ctypes.c_int32), ("adv_per_token", ctypes.c_int32), ("clip_low", ctypes.c_double), ("clip_high", ctypes.c_double),
+                ("beta", ctypes.c_double)]
+
+
+class _Gradient(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("count", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
+@dataclass(frozen=True)
+class CrossDims:
+    """B sources of Lk states, Lq tokens each (B*Lq == G*S), attention heads of width d (64 or 128); heads / kv_heads of them share
+    keys and values (0: none do)."""
+    B: int
+    Lq: int
+    Lk: int
+    heads: int
+    d: int
+    kv_heads: int = 0
+
+    @property
+    def key_heads(self):
+        return self.kv_heads or self.heads
+
+    def _c(self):
+        return _CrossDims(self.B, self.Lq, self.Lk, self.heads, self.key_heads, self.d)
+
+
+@dataclass(frozen=True)
+class PreferenceDims:
+    """P pairs of sequences over a vocabulary of V entries; kind "logistic" (with smoothing) or "squared"."""
+    P: int
+    V: int
+    beta: float
+    smoothing: float = 0.0
+    kind: str = "logistic"
+
+    def _c(self):
+        return _PreferenceDims(self.P, self.V, PREFERENCE_KINDS[self.kind], self.beta, self.smoothing)
+
+
+@dataclass(frozen=True)
+class PolicyDims:
+    """Vocabulary of V entries, ratios bounded to 1 - clip_low .. 1 + clip_high, weight beta of the KL term."""
+    V: int
+    clip_low: float = 0.2
+    clip_high: float = 0.2
+    beta: float = 0.0
+
+    def _c(self, adv_per_token):
+        return _PolicyDims(self.V, int(adv_per_token), self.clip_low, self.clip_high, self.beta)
 
 
 @dataclass(frozen=True)
@@ -168,6 +235,18 @@ def load_library() -> ctypes.CDLL:
         "moe_vocab_loss_backward": [cfgp, ctypes.POINTER(_VocabDims)] + [vp] * 9 + [sz, vp],
         "moe_vocab_distill": [cfgp, ctypes.POINTER(_VocabDims)] + [vp] * 8 + [sz, vp],
         "moe_vocab_distill_backward": [cfgp, ctypes.POINTER(_VocabDims)] + [vp] * 10 + [sz, vp],
+        **{f"moe_cross{k}_workspace_bytes": [cfgp, ctypes.POINTER(_CrossDims), ctypes.POINTER(sz)] for k in ("", "_train", "_backward")},
+        "moe_cross_keys": [cfgp, ctypes.POINTER(_CrossDims)] + [vp] * 4,
+        "moe_cross_attention": [cfgp, ctypes.POINTER(_CrossDims)] + [vp] * 7 + [sz, vp],
+        "moe_cross_attention_train": [cfgp, ctypes.POINTER(_CrossDims)] + [vp] * 7 + [sz, vp],
+        "moe_cross_attention_backward": [cfgp, ctypes.POINTER(_CrossDims)] + [vp] * 9 + [sz] + [vp] * 6 + [sz, vp],
+        "moe_preference_loss": [cfgp, ctypes.POINTER(_PreferenceDims)] + [vp] * 7,
+        "moe_preference_loss_backward": [cfgp, ctypes.POINTER(_PreferenceDims)] + [vp] * 6,
+        "moe_policy_loss": [cfgp, ctypes.POINTER(_PolicyDims)] + [vp] * 8,
+        "moe_policy_loss_backward": [cfgp, ctypes.POINTER(_PolicyDims)] + [vp] * 8,
+        "moe_gradient_norm_workspace_bytes": [ctypes.POINTER(_Gradient), i32, ctypes.POINTER(sz)],
+        "moe_gradient_norm": [ctypes.POINTER(_Gradient), i32, vp, vp, sz, vp],
+        "moe_clip_gradients": [ctypes.POINTER(_Gradient), i32, vp, ctypes.c_double, vp],
         "moe_backward_workspace_bytes": [cfgp, ctypes.POINTER(sz)],
         "moe_backward": [cfgp] + [vp] * 7 + [sz] + [vp] * 5 + [sz, vp],
         "moe_backward_events": [cfgp] + [vp] * 7 + [sz] + [vp] * 5 + [sz, vp,
@@ -693,3 +772,198 @@ def moe_vocab_distill_backward(shape: MoEShape, dims: VocabDims, x, w, teacher_i
         _ptr(teacher_idx, torch.int32, (G, S, K), "teacher_idx"), _ptr(teacher_logit, f32, (G, S, K), "teacher_logit"),
         _ptr(entry_logit, f32, (G, S, K), "entry_logit"), _ptr(lse, f32, (G, S), "lse"), _ptr(dloss, f32, (G, S), "dloss"),
         _ptr(dx, dt, (G, S, M), "dx"), _ptr(dw, dt, (dims.V, M), "dw"), wsp, wsn, _stream()), "moe_vocab_distill_backward")
+
+
+# ---- the decoder's attention to the encoder
+def moe_cross_workspace_bytes(shape: MoEShape, dims: CrossDims) -> int:
+    return _ws_query("moe_cross_workspace_bytes", shape, dims)
+
+
+def moe_cross_train_workspace_bytes(shape: MoEShape, dims: CrossDims) -> int:
+    return _ws_query("moe_cross_train_workspace_bytes", shape, dims)
+
+
+def moe_cross_backward_workspace_bytes(shape: MoEShape, dims: CrossDims) -> int:
+    return _ws_query("moe_cross_backward_workspace_bytes", shape, dims)
+
+
+def moe_cross_keys(shape: MoEShape, dims: CrossDims, mem, wkv, kv):
+    """kv [B,Lk,2 Akv] = mem [B,Lk,M] . wkv [M,2 Akv], keys in the first Akv columns, values in the others."""
+    _given("mem wkv kv", mem, wkv, kv)
+    M, dt, W = shape.M, shape.torch_dtype, 2 * dims.key_heads * dims.d
+    c, d = shape._c(), dims._c()
+    _check(load_library().moe_cross_keys(
+        ctypes.byref(c), ctypes.byref(d), _ptr(mem, dt, (dims.B, dims.Lk, M), "mem"), _ptr(wkv, dt, (M, W), "wkv"),
+        _ptr(kv, dt, (dims.B, dims.Lk, W), "kv"), _stream()), "moe_cross_keys")
+
+
+def _cross_forward(fn_name, shape, dims, u, kv, src_len, wq, wo, out, ws):
+    _given("u kv wq wo out ws", u, kv, wq, wo, out, ws)
+    if src_len is not None:
+        _given("src_len", src_len)
+    G, S, M, dt, A = shape.G, shape.S, shape.M, shape.torch_dtype, dims.heads * dims.d
+    c, d = shape._c(), dims._c()
+    wsp, wsn = _ws(ws)
+    _check(getattr(load_library(), fn_name)(
+        ctypes.byref(c), ctypes.byref(d), _ptr(u, dt, (G, S, M), "u"), _ptr(kv, dt, (dims.B, dims.Lk, 2 * dims.key_heads * dims.d), "kv"),
+        _ptr(src_len, torch.int32, (dims.B,), "src_len"), _ptr(wq, dt, (M, A), "wq"), _ptr(wo, dt, (A, M), "wo"),
+        _ptr(out, dt, (G, S, M), "out"), wsp, wsn, _stream()), fn_name)
+
+
+def moe_cross_attention(shape: MoEShape, dims: CrossDims, u, kv, src_len, wq, wo, out, ws):
+    """Attention of u [G,S,M] to kv as moe_cross_keys leaves it; src_len [B] i32: states that hold (None: all)."""
+    _cross_forward("moe_cross_attention", shape, dims, u, kv, src_len, wq, wo, out, ws)
+
+
+def moe_cross_attention_train(shape: MoEShape, dims: CrossDims, u, kv, src_len, wq, wo, out, ws):
+    """As moe_cross_attention; ws (moe_cross_train_workspace_bytes) keeps what moe_cross_attention_backward reads."""
+    _cross_forward("moe_cross_attention_train", shape, dims, u, kv, src_len, wq, wo, out, ws)
+
+
+def moe_cross_attention_backward(shape: MoEShape, dims: CrossDims, u, mem, kv, src_len, wq, wkv, wo, dout, fwd_ws, grads: dict, ws):
+    """grads: a dict of output tensors du, dmem, dwq, dwkv, dwo of the shapes of u, mem, wq, wkv, wo."""
+    du, dmem, dwq, dwkv, dwo = (grads[k] for k in ("du", "dmem", "dwq", "dwkv", "dwo"))
+    _given("u mem kv wq wkv wo dout fwd_ws du dmem dwq dwkv dwo ws", u, mem, kv, wq, wkv, wo, dout, fwd_ws, du, dmem, dwq, dwkv, dwo, ws)
+    if src_len is not None:
+        _given("src_len", src_len)
+    G, S, M, dt, A, W = shape.G, shape.S, shape.M, shape.torch_dtype, dims.heads * dims.d, 2 * dims.key_heads * dims.d
+    c, d = shape._c(), dims._c()
+    fwp, fwn = _ws(fwd_ws, "fwd_ws")
+    wsp, wsn = _ws(ws)
+    rows = (dims.B, dims.Lk)
+    _check(load_library().moe_cross_attention_backward(
+        ctypes.byref(c), ctypes.byref(d), _ptr(u, dt, (G, S, M), "u"), _ptr(mem, dt, (*rows, M), "mem"), _ptr(kv, dt, (*rows, W), "kv"),
+        _ptr(src_len, torch.int32, (dims.B,), "src_len"), _ptr(wq, dt, (M, A), "wq"), _ptr(wkv, dt, (M, W), "wkv"),
+        _ptr(wo, dt, (A, M), "wo"), _ptr(dout, dt, (G, S, M), "dout"), fwp, fwn, _ptr(du, dt, (G, S, M), "du"),
+        _ptr(dmem, dt, (*rows, M), "dmem"), _ptr(dwq, dt, (M, A), "dwq"), _ptr(dwkv, dt, (M, W), "dwkv"), _ptr(dwo, dt, (A, M), "dwo"),
+        wsp, wsn, _stream()), "moe_cross_attention_backward")
+
+
+# ---- losses of preference and policy
+def moe_preference_loss(shape: MoEShape, dims: PreferenceDims, nll, ref_nll, target, start, loss, ratio):
+    """Loss [P] of pairs of sequences (tokens start[i] .. start[i + 1] - 1) and their log-ratios [2P], from token losses [G,S]."""
+    _given("nll ref_nll target start loss ratio", nll, ref_nll, target, start, loss, ratio)
+    t, f32, i32 = (shape.G, shape.S), torch.float32, torch.int32
+    c, d = shape._c(), dims._c()
+    _check(load_library().moe_preference_loss(
+        ctypes.byref(c), ctypes.byref(d), _ptr(nll, f32, t, "nll"), _ptr(ref_nll, f32, t, "ref_nll"), _ptr(target, i32, t, "target"),
+        _ptr(start, i32, (2 * dims.P + 1,), "start"), _ptr(loss, f32, (dims.P,), "loss"), _ptr(ratio, f32, (2 * dims.P,), "ratio"),
+        _stream()), "moe_preference_loss")
+
+
+def moe_preference_loss_backward(shape: MoEShape, dims: PreferenceDims, target, start, ratio, dloss, dnll):
+    """Gradient dnll [G,S] of sum(dloss * loss); ratio as moe_preference_loss left it."""
+    _given("target start ratio dloss dnll", target, start, ratio, dloss, dnll)
+    t, f32, i32 = (shape.G, shape.S), torch.float32, torch.int32
+    c, d = shape._c(), dims._c()
+    _check(load_library().moe_preference_loss_backward(
+        ctypes.byref(c), ctypes.byref(d), _ptr(target, i32, t, "target"), _ptr(start, i32, (2 * dims.P + 1,), "start"),
+        _ptr(ratio, f32, (2 * dims.P,), "ratio"), _ptr(dloss, f32, (dims.P,), "dloss"), _ptr(dnll, f32, t, "dnll"), _stream()),
+        "moe_preference_loss_backward")
+
+
+def _policy_args(shape, dims, nll, old_nll, ref_nll, adv, target):
+    _given("nll old_nll adv target", nll, old_nll, adv, target)
+    if ref_nll is not None:
+        _given("ref_nll", ref_nll)
+    t, f32 = (shape.G, shape.S), torch.float32
+    per_token = isinstance(adv, torch.Tensor) and adv.dim() == 2
+    return dims._c(per_token), (_ptr(nll, f32, t, "nll"), _ptr(old_nll, f32, t, "old_nll"), _ptr(ref_nll, f32, t, "ref_nll"),
+                                _ptr(adv, f32, t if per_token else (shape.G,), "adv"), _ptr(target, torch.int32, t, "target"))
+
+
+def moe_policy_loss(shape: MoEShape, dims: PolicyDims, nll, old_nll, ref_nll, adv, target, loss, kl=None):
+    """Clipped loss [G,S] (and the KL term kl [G,S]) of token losses; adv [G] or [G,S]; ref_nll may be None where dims.beta is 0."""
+    d, args = _policy_args(shape, dims, nll, old_nll, ref_nll, adv, target)
+    _given("loss", loss)
+    if kl is not None:
+        _given("kl", kl)
+    t, f32, c = (shape.G, shape.S), torch.float32, shape._c()
+    _check(load_library().moe_policy_loss(ctypes.byref(c), ctypes.byref(d), *args, _ptr(loss, f32, t, "loss"), _ptr(kl, f32, t, "kl"),
+                                          _stream()), "moe_policy_loss")
+
+
+def moe_policy_loss_backward(shape: MoEShape, dims: PolicyDims, nll, old_nll, ref_nll, adv, target, dloss, dnll):
+    """Gradient dnll [G,S] of sum(dloss * loss)."""
+    d, args = _policy_args(shape, dims, nll, old_nll, ref_nll, adv, target)
+    _given("dloss dnll", dloss, dnll)
+    t, f32, c = (shape.G, shape.S), torch.float32, shape._c()
+    _check(load_library().moe_policy_loss_backward(ctypes.byref(c), ctypes.byref(d), *args, _ptr(dloss, f32, t, "dloss"),
+                                                   _ptr(dnll, f32, t, "dnll"), _stream()), "moe_policy_loss_backward")
+
+
+# ---- clipping by the norm of all gradients
+class GradientList:
+    """Where a program's gradients are: tensors of any shape, fp32 or bf16, contiguous and 16-byte aligned, and where the clipped
+    ones go (None: in their place).  It keeps the tensors, whose memory must stay where it is while the list is used."""
+
+    def __init__(self, tensors, out=None):
+        self.tensors = list(tensors)
+        self.out = self.tensors if out is None else list(out)
+        if len(self.out) != len(self.tensors):
+            raise ValueError(f"out: {len(self.out)} tensors for {len(self.tensors)}")
+        self.device = None
+        self._list = (_Gradient * max(1, len(self.tensors)))()
+        written = []
+        for i, (t, o) in enumerate(zip(self.tensors, self.out)):
+            for name, v in ((f"tensors[{i}]", t), (f"out[{i}]", o)):
+                if not isinstance(v, torch.Tensor) or not v.is_cuda:
+                    raise TypeError(f"{name}: expected a GPU tensor")
+                if v.dtype not in (torch.float32, torch.bfloat16):
+                    raise TypeError(f"{name}: expected torch.float32 or torch.bfloat16, got {v.dtype}")
+                if not v.is_contiguous():
+                    raise ValueError(f"{name}: must be contiguous")
+                if self.device is None:
+                    self.device = v.get_device()
+                if v.get_device() != self.device:
+                    raise ValueError(f"{name}: on {v.device}, the others on cuda:{self.device}")
+            if o.dtype != t.dtype or o.shape != t.shape:
+                raise ValueError(f"out[{i}]: expected {t.dtype} {tuple(t.shape)}, got {o.dtype} {tuple(o.shape)}")
+            size = t.numel() * t.element_size()
+            self._list[i] = _Gradient(t.data_ptr(), o.data_ptr(), t.numel(), MOE_F32 if t.dtype == torch.float32 else MOE_BF16)
+            if size:
+                written.append((o.data_ptr(), o.data_ptr() + size, f"out[{i}]", True, i))
+                if o.data_ptr() != t.data_ptr():
+                    written.append((t.data_ptr(), t.data_ptr() + size, f"tensors[{i}]", False, i))
+        # no output may share memory with another tensor of the list; inputs may with one another
+        written.sort()
+        end, of, writes = 0, "", False
+        for a, b, name, is_out, _ in written:
+            if a < end and (is_out or writes):
+                raise ValueError(f"{name}: shares memory with {of}")
+            if a >= end:
+                writes = False
+            writes = writes or is_out
+            if b > end:
+                end, of = b, name
+
+    def __len__(self):
+        return len(self.tensors)
+
+    def _here(self):
+        if self.device is not None and torch.cuda.current_device() != self.device:
+            raise ValueError(f"the list's tensors are on cuda:{self.device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def moe_gradient_norm_workspace_bytes(gradients: GradientList) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load_library().moe_gradient_norm_workspace_bytes(gradients._list, len(gradients), ctypes.byref(n)),
+           "moe_gradient_norm_workspace_bytes")
+    return n.value
+
+
+def moe_gradient_norm(gradients: GradientList, norm, ws):
+    """norm [1] fp32: the root of the sum of squares of all elements."""
+    _given("norm ws", norm, ws)
+    gradients._here()
+    wsp, wsn = _ws(ws)
+    _check(load_library().moe_gradient_norm(gradients._list, len(gradients), _ptr(norm, torch.float32, (1,), "norm"), wsp, wsn, _stream()),
+           "moe_gradient_norm")
+
+
+def moe_clip_gradients(gradients: GradientList, norm, max_norm: float):
+    """The list's outputs become its tensors times min(1, max_norm / norm[0]); an infinite norm or NaN leaves them as they are."""
+    _given("norm", norm)
+    gradients._here()
+    _check(load_library().moe_clip_gradients(gradients._list, len(gradients), _ptr(norm, torch.float32, (1,), "norm"), max_norm, _stream()),
+           "moe_clip_gradients")

@@ -1,6 +1,7 @@
 // C ABI of the library: argument checks, workspace carving, kernel sequencing.
 // Every step of the layer runs in the kernels of gate.hip, dispatch_combine.hip
 // and expert_gemm.hip; nothing here computes.
+#include <math.h>
 #include <mutex>
 #include "common.h"
 
@@ -350,6 +351,119 @@ int vocab_bytes(const moe_config* cfg, const moe_vocab_dims* d, bool backward, s
   if (d->K >= 1 && d->K <= 256) {                               // (a cross entropy's is not read)
     const size_t teacher = moe::carve_vocab(*cfg, *d, true, backward).total;
     if (teacher > *bytes) *bytes = teacher;
+  }
+  return MOE_OK;
+}
+
+int check_cross(const moe_config* cfg, const moe_cross_dims* d) {
+  const int rc = check_config(cfg);
+  if (rc != MOE_OK) return rc;
+  if (d == nullptr) return MOE_EINVAL;
+  if (d->B < 1 || d->Lq < 1 || d->Lk < 1 || d->heads < 1 || d->kv_heads < 1 || d->d < 1) return MOE_EINVAL;
+  if ((long long)d->B * d->Lq != (long long)cfg->G * cfg->S || d->heads % d->kv_heads != 0) return MOE_EINVAL;
+  const int share = d->heads / d->kv_heads;
+  if ((d->d != 64 && d->d != 128) || (share & (share - 1)) != 0 || share > 32) return MOE_EUNSUPPORTED;
+  if ((long long)d->heads * d->d > 0x7fffffLL || (long long)d->B * d->Lk > 0x3fffffffLL) return MOE_EUNSUPPORTED;
+  if ((long long)d->Lq * share >= 1LL << 29) return MOE_EUNSUPPORTED;
+  return MOE_OK;
+}
+moe::CrossShape cross_shape(const moe_cross_dims& d) { return {d.B, d.Lq, d.Lk, d.heads, d.kv_heads, d.d}; }
+
+// train: with the row statistics.  q, ctx and lse come first, so the backward pass finds them.
+struct CrossWs { size_t q, ctx, lse, scratch, total; };
+CrossWs carve_cross(const moe_config& c, const moe_cross_dims& d, bool train) {
+  const size_t elt = c.act_dtype == MOE_F32 ? 4 : 2, N = (size_t)c.G * c.S, A = (size_t)d.heads * d.d;
+  CrossWs w{};
+  size_t off = 0;
+  auto take = [&](size_t bytes) { size_t o = off; off += align_up(bytes, 256); return o; };
+  w.q = take(N * A * elt);
+  w.ctx = take(N * A * elt);
+  w.lse = take(train ? N * d.heads * 4 : 0);
+  w.scratch = take(moe::cross_scratch_bytes(c.act_dtype, cross_shape(d)));
+  w.total = off;
+  return w;
+}
+struct CrossBwdWs { size_t dctx, dq, dkv, mem, dvec, wpart, total; };
+CrossBwdWs carve_cross_bwd(const moe_config& c, const moe_cross_dims& d) {
+  const size_t elt = c.act_dtype == MOE_F32 ? 4 : 2, N = (size_t)c.G * c.S, A = (size_t)d.heads * d.d, rows = (size_t)d.B * d.Lk;
+  CrossBwdWs w{};
+  size_t off = 0;
+  auto take = [&](size_t bytes) { size_t o = off; off += align_up(bytes, 256); return o; };
+  w.dctx = take(N * A * elt);
+  w.dq = take(N * A * elt);
+  w.dkv = take(rows * 2 * d.kv_heads * d.d * elt);
+  w.mem = take(rows * c.M * elt);
+  w.dvec = take(N * d.heads * 4);
+  const int Akv2 = 2 * d.kv_heads * d.d;
+  const size_t parts[] = {moe::dense_wgrad_partial_bytes(c.act_dtype, (long long)N, (int)A, c.M),
+                          moe::dense_wgrad_partial_bytes(c.act_dtype, (long long)N, c.M, (int)A),
+                          moe::dense_wgrad_partial_bytes(c.act_dtype, (long long)rows, c.M, Akv2)};
+  size_t most = 0;
+  for (size_t p : parts) most = p > most ? p : most;
+  w.wpart = take(most);
+  w.total = off;
+  return w;
+}
+// what: 0 inference, 1 training, 2 backward
+int cross_bytes(const moe_config* cfg, const moe_cross_dims* dims, int what, size_t* bytes) {
+  const int rc = check_cross(cfg, dims);
+  if (rc != MOE_OK) return rc;
+  if (bytes == nullptr) return MOE_EINVAL;
+  *bytes = what == 2 ? carve_cross_bwd(*cfg, *dims).total : carve_cross(*cfg, *dims, what == 1).total;
+  return MOE_OK;
+}
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+int cross_forward(const moe_config* cfg, const moe_cross_dims* dims, const void* u, const void* kv, const int32_t* src_len,
+                  const void* wq, const void* wo, void* out, void* ws, size_t ws_bytes, void* stream, bool train) {
+  int rc = check_cross(cfg, dims);
+  if (rc != MOE_OK) return rc;
+  const void* req[] = {u, kv, wq, wo, out, ws};
+  for (const void* p : req)
+    if (p == nullptr || !aligned16(p)) return MOE_EINVAL;
+  if (!aligned4(src_len) || (reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return MOE_EINVAL;
+  const CrossWs w = carve_cross(*cfg, *dims, train);
+  if (ws_bytes < w.total) return MOE_EWORKSPACE;
+  char* base = static_cast<char*>(ws);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const long long N = (long long)cfg->G * cfg->S;
+  const int A = dims->heads * dims->d;
+  if ((rc = dense_gemm(*cfg, N, cfg->M, A, false, u, wq, base + w.q, st)) != MOE_OK) return rc;
+  rc = moe::launch_cross_attention(cfg->act_dtype, cross_shape(*dims), base + w.q, kv, src_len, base + w.ctx,
+                                   train ? reinterpret_cast<float*>(base + w.lse) : nullptr, base + w.scratch, st);
+  if (rc != MOE_OK) return rc;
+  return dense_gemm(*cfg, N, A, cfg->M, false, base + w.ctx, wo, out, st);
+}
+
+int check_preference(const moe_config* cfg, const moe_preference_dims* d) {
+  const int rc = check_config(cfg);
+  if (rc != MOE_OK) return rc;
+  if (d == nullptr || d->P < 1 || d->V < 1 || (d->kind != MOE_PREFERENCE_LOGISTIC && d->kind != MOE_PREFERENCE_SQUARED)) return MOE_EINVAL;
+  if (!(d->beta > 0.0 && d->beta < INFINITY) || !(d->smoothing >= 0.0 && d->smoothing < 1.0)) return MOE_EINVAL;
+  return d->P > 1 << 29 ? MOE_EUNSUPPORTED : MOE_OK;
+}
+int policy_call(const moe_config* cfg, const moe_policy_dims* d, const moe::PolicyCall& a, bool backward, void* stream) {
+  const int rc = check_config(cfg);
+  if (rc != MOE_OK) return rc;
+  if (d == nullptr || d->V < 1 || (d->adv_per_token != 0 && d->adv_per_token != 1)) return MOE_EINVAL;
+  if (!(d->clip_low >= 0.0 && d->clip_low <= 1.0) || !(d->clip_high >= 0.0 && d->clip_high < INFINITY) ||
+      !(d->beta >= 0.0 && d->beta < INFINITY))
+    return MOE_EINVAL;
+  if (a.ref == nullptr && d->beta != 0.0) return MOE_EINVAL;
+  const void* req[] = {a.nll, a.old_nll, a.adv, a.target, backward ? a.dloss : a.nll, backward ? a.dnll : a.loss};
+  for (const void* p : req)
+    if (p == nullptr || !aligned16(p)) return MOE_EINVAL;
+  if (!aligned16(a.ref) || !aligned16(a.kl)) return MOE_EINVAL;
+  return moe::launch_policy(*d, (long long)cfg->G * cfg->S, cfg->S, a, static_cast<hipStream_t>(stream));
+}
+
+int check_gradients(const moe_gradient* list, int32_t n, bool written) {
+  if (n < 0 || (n > 0 && list == nullptr)) return MOE_EINVAL;
+  for (int32_t i = 0; i < n; ++i) {
+    const moe_gradient& g = list[i];
+    if (g.count < 0 || (g.dtype != MOE_F32 && g.dtype != MOE_BF16)) return MOE_EINVAL;
+    if (g.count == 0) continue;
+    if (g.src == nullptr || !aligned16(g.src) || (written && (g.dst == nullptr || !aligned16(g.dst)))) return MOE_EINVAL;
+    if (g.count > 1LL << 42) return MOE_EUNSUPPORTED;
   }
   return MOE_OK;
 }
@@ -982,6 +1096,133 @@ int moe_vocab_distill_backward(const moe_config* cfg, const moe_vocab_dims* dims
   a.dx = dx;
   a.dw = dw;
   return vocab_call(cfg, dims, a, ws, ws_bytes, stream, true);
+}
+
+int moe_cross_workspace_bytes(const moe_config* cfg, const moe_cross_dims* dims, size_t* bytes) {
+  return cross_bytes(cfg, dims, 0, bytes);
+}
+
+int moe_cross_train_workspace_bytes(const moe_config* cfg, const moe_cross_dims* dims, size_t* bytes) {
+  return cross_bytes(cfg, dims, 1, bytes);
+}
+
+int moe_cross_backward_workspace_bytes(const moe_config* cfg, const moe_cross_dims* dims, size_t* bytes) {
+  return cross_bytes(cfg, dims, 2, bytes);
+}
+
+int moe_cross_keys(const moe_config* cfg, const moe_cross_dims* dims, const void* mem, const void* wkv, void* kv, void* stream) {
+  const int rc = check_cross(cfg, dims);
+  if (rc != MOE_OK) return rc;
+  const void* req[] = {mem, wkv, kv};
+  for (const void* p : req)
+    if (p == nullptr || !aligned16(p)) return MOE_EINVAL;
+  return dense_gemm(*cfg, (long long)dims->B * dims->Lk, cfg->M, 2 * dims->kv_heads * dims->d, false, mem, wkv, kv,
+                    static_cast<hipStream_t>(stream));
+}
+
+int moe_cross_attention(const moe_config* cfg, const moe_cross_dims* dims, const void* u, const void* kv, const int32_t* src_len,
+                        const void* wq, const void* wo, void* out, void* ws, size_t ws_bytes, void* stream) {
+  return cross_forward(cfg, dims, u, kv, src_len, wq, wo, out, ws, ws_bytes, stream, false);
+}
+
+int moe_cross_attention_train(const moe_config* cfg, const moe_cross_dims* dims, const void* u, const void* kv,
+                              const int32_t* src_len, const void* wq, const void* wo, void* out, void* ws, size_t ws_bytes,
+                              void* stream) {
+  return cross_forward(cfg, dims, u, kv, src_len, wq, wo, out, ws, ws_bytes, stream, true);
+}
+
+int moe_cross_attention_backward(const moe_config* cfg, const moe_cross_dims* dims, const void* u, const void* mem, const void* kv,
+                                 const int32_t* src_len, const void* wq, const void* wkv, const void* wo, const void* dout,
+                                 const void* fwd_ws, size_t fwd_ws_bytes, void* du, void* dmem, void* dwq, void* dwkv, void* dwo,
+                                 void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_cross(cfg, dims);
+  if (rc != MOE_OK) return rc;
+  const void* req[] = {u, mem, kv, wq, wkv, wo, dout, fwd_ws, du, dmem, dwq, dwkv, dwo, ws};
+  for (const void* p : req)
+    if (p == nullptr || !aligned16(p)) return MOE_EINVAL;
+  if (!aligned4(src_len) || ((reinterpret_cast<uintptr_t>(ws) | reinterpret_cast<uintptr_t>(fwd_ws)) & 255u) != 0) return MOE_EINVAL;
+  const CrossWs f = carve_cross(*cfg, *dims, true);
+  const CrossBwdWs w = carve_cross_bwd(*cfg, *dims);
+  if (fwd_ws_bytes < f.total || ws_bytes < w.total) return MOE_EWORKSPACE;
+  const char* fwd = static_cast<const char*>(fwd_ws);
+  char* base = static_cast<char*>(ws);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const long long N = (long long)cfg->G * cfg->S, rows = (long long)dims->B * dims->Lk;
+  const int A = dims->heads * dims->d, Akv2 = 2 * dims->kv_heads * dims->d;
+  float* wpart = reinterpret_cast<float*>(base + w.wpart);
+  // out = ctx . wo
+  rc = moe::launch_dense_grads(*cfg, N, A, cfg->M, fwd + f.ctx, dout, wo, nullptr, base + w.dctx, dwo, wpart, st);
+  if (rc != MOE_OK) return rc;
+  rc = moe::launch_cross_attention_bwd(cfg->act_dtype, cross_shape(*dims), fwd + f.q, kv, src_len, fwd + f.ctx, base + w.dctx,
+                                       reinterpret_cast<const float*>(fwd + f.lse), base + w.dq, base + w.dkv,
+                                       reinterpret_cast<float*>(base + w.dvec), st);
+  if (rc != MOE_OK) return rc;
+  // q = u . wq
+  rc = moe::launch_dense_grads(*cfg, N, cfg->M, A, u, base + w.dq, wq, nullptr, du, dwq, wpart, st);
+  if (rc != MOE_OK) return rc;
+  // [K|V] = mem . wkv; states that do not hold have gradients of zeros, which their rows of mem must not turn into NaN
+  if (src_len != nullptr) {
+    rc = moe::launch_held_rows(cfg->act_dtype, mem, src_len, base + w.mem, dims->B, dims->Lk, cfg->M, st);
+    if (rc != MOE_OK) return rc;
+    mem = base + w.mem;
+  }
+  return moe::launch_dense_grads(*cfg, rows, cfg->M, Akv2, mem, base + w.dkv, wkv, nullptr, dmem, dwkv, wpart, st);
+}
+
+int moe_preference_loss(const moe_config* cfg, const moe_preference_dims* dims, const float* nll, const float* ref_nll,
+                        const int32_t* target, const int32_t* start, float* loss, float* ratio, void* stream) {
+  const int rc = check_preference(cfg, dims);
+  if (rc != MOE_OK) return rc;
+  const void* req[] = {nll, ref_nll, target, start, loss, ratio};
+  for (const void* p : req)
+    if (p == nullptr || !aligned16(p)) return MOE_EINVAL;
+  return moe::launch_preference(*dims, (long long)cfg->G * cfg->S, nll, ref_nll, target, start, loss, ratio,
+                                static_cast<hipStream_t>(stream));
+}
+
+int moe_preference_loss_backward(const moe_config* cfg, const moe_preference_dims* dims, const int32_t* target, const int32_t* start,
+                                 const float* ratio, const float* dloss, float* dnll, void* stream) {
+  const int rc = check_preference(cfg, dims);
+  if (rc != MOE_OK) return rc;
+  const void* req[] = {target, start, ratio, dloss, dnll};
+  for (const void* p : req)
+    if (p == nullptr || !aligned16(p)) return MOE_EINVAL;
+  return moe::launch_preference_bwd(*dims, (long long)cfg->G * cfg->S, target, start, ratio, dloss, dnll,
+                                    static_cast<hipStream_t>(stream));
+}
+
+int moe_policy_loss(const moe_config* cfg, const moe_policy_dims* dims, const float* nll, const float* old_nll, const float* ref_nll,
+                    const float* adv, const int32_t* target, float* loss, float* kl, void* stream) {
+  return policy_call(cfg, dims, {nll, old_nll, ref_nll, adv, target, nullptr, loss, kl, nullptr}, false, stream);
+}
+
+int moe_policy_loss_backward(const moe_config* cfg, const moe_policy_dims* dims, const float* nll, const float* old_nll,
+                             const float* ref_nll, const float* adv, const int32_t* target, const float* dloss, float* dnll,
+                             void* stream) {
+  return policy_call(cfg, dims, {nll, old_nll, ref_nll, adv, target, dloss, nullptr, nullptr, dnll}, true, stream);
+}
+
+int moe_gradient_norm_workspace_bytes(const moe_gradient* list, int32_t n, size_t* bytes) {
+  const int rc = check_gradients(list, n, false);
+  if (rc != MOE_OK) return rc;
+  if (bytes == nullptr) return MOE_EINVAL;
+  *bytes = moe::gradient_norm_bytes(list, n);
+  return MOE_OK;
+}
+
+int moe_gradient_norm(const moe_gradient* list, int32_t n, float* norm, void* ws, size_t ws_bytes, void* stream) {
+  const int rc = check_gradients(list, n, false);
+  if (rc != MOE_OK) return rc;
+  if (norm == nullptr || !aligned4(norm) || ws == nullptr || (reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return MOE_EINVAL;
+  if (ws_bytes < moe::gradient_norm_bytes(list, n)) return MOE_EWORKSPACE;
+  return moe::launch_gradient_norm(list, n, norm, ws, static_cast<hipStream_t>(stream));
+}
+
+int moe_clip_gradients(const moe_gradient* list, int32_t n, const float* norm, double max_norm, void* stream) {
+  const int rc = check_gradients(list, n, true);
+  if (rc != MOE_OK) return rc;
+  if (norm == nullptr || !aligned4(norm) || !(max_norm >= 0.0)) return MOE_EINVAL;
+  return moe::launch_clip_gradients(list, n, norm, max_norm, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

@@ -416,6 +416,42 @@ int launch_attention_core_bwd(int act_dtype, const void* qkv, const void* ctx, c
                               const float* lse, void* dqkv, float* dvec, long long B, int L,
                               int heads, int d, hipStream_t st);
 
+// The decoder's attention to the encoder (cross_attention.hip).  Columns: the Lq share queries that use one key head, token by token,
+// share heads each: column c of key head k is head k share + c % share of token c / share.
+struct CrossShape {
+  long long B;
+  int Lq, Lk, heads, kv_heads, d;
+  int share() const { return heads / kv_heads; }
+  int columns() const { return Lq * share(); }
+};
+// q, ctx [B Lq, heads d], kv [B Lk, 2 kv_heads d]; lse: NULL or [B kv_heads columns]; scratch: cross_scratch_bytes()
+size_t cross_scratch_bytes(int act_dtype, const CrossShape& s);
+int launch_cross_attention(int act_dtype, const CrossShape& s, const void* q, const void* kv, const int32_t* src_len, void* ctx,
+                           float* lse, void* scratch, hipStream_t st);
+// dvec: [B kv_heads columns] of scratch; dkv: zeros in the rows of states that do not hold
+int launch_cross_attention_bwd(int act_dtype, const CrossShape& s, const void* q, const void* kv, const int32_t* src_len,
+                               const void* ctx, const void* dctx, const float* lse, void* dq, void* dkv, float* dvec, hipStream_t st);
+// out = mem with zeros in those rows
+int launch_held_rows(int act_dtype, const void* mem, const int32_t* src_len, void* out, long long B, int Lk, int M, hipStream_t st);
+
+// Losses on token losses (token_loss.hip)
+int launch_preference(const moe_preference_dims& d, long long N, const float* nll, const float* ref, const int32_t* target,
+                      const int32_t* start, float* loss, float* ratio, hipStream_t st);
+int launch_preference_bwd(const moe_preference_dims& d, long long N, const int32_t* target, const int32_t* start, const float* ratio,
+                          const float* dloss, float* dnll, hipStream_t st);
+struct PolicyCall {
+  const float *nll, *old_nll, *ref, *adv;
+  const int32_t* target;
+  const float* dloss;
+  float *loss, *kl, *dnll;             // forward: loss (and kl); backward: dnll
+};
+int launch_policy(const moe_policy_dims& d, long long N, int S, const PolicyCall& a, hipStream_t st);
+
+// Norm and clipping of gradients (gradient_norm.hip)
+size_t gradient_norm_bytes(const moe_gradient* list, int n);
+int launch_gradient_norm(const moe_gradient* list, int n, float* norm, void* ws, hipStream_t st);
+int launch_clip_gradients(const moe_gradient* list, int n, const float* norm, double max_norm, hipStream_t st);
+
 inline int check_launch() { return hipPeekAtLastError() == hipSuccess ? MOE_OK : MOE_EHIP; }
 
 // A kernel that uses more than 64 KB of dynamic LDS needs its limit raised once per device

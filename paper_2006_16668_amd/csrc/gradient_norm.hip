@@ -1,0 +1,213 @@
+// The norm over all of a model's gradients, and the gradients scaled by min(1, max_norm / norm).
+//
+// Squares are formed and added in 64 bits: the square of any fp32 or bf16 number is exact there and neither overflows nor
+// vanishes, and the fp64 units add far faster than memory delivers (2.5e12 bf16 elements a second at 5 TB/s are 5e12 of some 4e13 operations).
+// Both passes are bound by memory.  Tensors are cut into chunks of one size in bytes, a block each, whatever tensor they belong
+// to, so a list of many small tensors is as few launches as one large one.  Where the tensors are travels as a kernel argument, kTensors of them a launch:
+// nothing is copied to the device, and a captured graph holds it.  The second pass walks the chunks backwards: what
+// the first has read last is still in the memory-side cache.
+#include <math.h>
+#include "common.h"
+
+namespace moe {
+namespace {
+
+constexpr int kTensors = 100;                // of a launch: 32 bytes each of its 4 KB of arguments
+struct Piece {
+  const void* src;
+  void* dst;
+  unsigned long long count_f32;              // elements, and in the lowest bit whether they are fp32
+  unsigned first, pad;                       // the tensor's first chunk of the launch
+};
+struct Table {
+  Piece t[kTensors];
+  int n;
+  unsigned chunks;
+  unsigned chunk_bytes;                      // a multiple of 4 KB
+};
+static_assert(sizeof(Table) + 64 <= 4096, "the arguments of a launch");
+
+struct Chunk { const char* src; char* dst; unsigned bytes; bool f32; };
+__device__ __forceinline__ Chunk chunk_of(const Table& tab, unsigned c) {
+  int lo = 0, hi = tab.n - 1;                // the last tensor that begins at or before c (empty ones are not in the table)
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (tab.t[mid].first <= c) lo = mid;
+    else hi = mid - 1;
+  }
+  const Piece& p = tab.t[lo];
+  const bool f32 = (p.count_f32 & 1) != 0;
+  const unsigned long long size = (p.count_f32 >> 1) * (f32 ? 4 : 2), from = (unsigned long long)(c - p.first) * tab.chunk_bytes;
+  const unsigned long long rest = size - from;
+  return {static_cast<const char*>(p.src) + from, static_cast<char*>(p.dst) + from,
+          (unsigned)(rest < tab.chunk_bytes ? rest : tab.chunk_bytes), f32};
+}
+
+__device__ __forceinline__ double block_sum(double v) {
+  __shared__ double sums[16];
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = v;
+  __syncthreads();
+  double s = 0.0;
+  for (unsigned w = 0; w < blockDim.x >> 6; ++w) s += sums[w];
+  return s;
+}
+
+template <typename T>
+__device__ __forceinline__ double squares(const Chunk& c) {
+  constexpr int E = Vec16<T>::kElts, AHEAD = 4;
+  double s[2] = {0.0, 0.0};
+  const unsigned vecs = c.bytes / 16;
+  auto add = [&](const uint4& v) __attribute__((always_inline)) {
+    float f[E];
+    Vec16<T>::unpack(v, f);
+#pragma unroll
+    for (int i = 0; i < E; ++i) s[i & 1] = fma((double)f[i], (double)f[i], s[i & 1]);
+  };
+  unsigned v = threadIdx.x;
+  for (; v + (AHEAD - 1) * 256 < vecs; v += AHEAD * 256) {
+    uint4 x[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) x[k] = reinterpret_cast<const uint4*>(c.src)[v + k * 256];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) add(x[k]);
+  }
+  for (; v < vecs; v += 256) add(reinterpret_cast<const uint4*>(c.src)[v]);
+  const unsigned tail = (c.bytes - vecs * 16) / sizeof(T);
+  if (threadIdx.x < tail) {
+    const double f = Elt<T>::load(reinterpret_cast<const T*>(c.src + vecs * 16) + threadIdx.x);
+    s[0] = fma(f, f, s[0]);
+  }
+  return s[0] + s[1];
+}
+
+__global__ __launch_bounds__(256) void gradient_squares_kernel(Table tab, double* __restrict__ partial) {
+  const Chunk c = chunk_of(tab, blockIdx.x);
+  const double s = block_sum(c.f32 ? squares<float>(c) : squares<bf16_t>(c));
+  if (threadIdx.x == 0) partial[blockIdx.x] = s;
+}
+
+__global__ __launch_bounds__(1024) void gradient_norm_kernel(const double* __restrict__ partial, unsigned n, float* __restrict__ norm) {
+  double s = 0.0;
+  for (unsigned i = threadIdx.x; i < n; i += 1024) s += partial[i];
+  s = block_sum(s);
+  if (threadIdx.x == 0) *norm = (float)sqrt(s);
+}
+
+template <typename T>
+__device__ __forceinline__ void scale_chunk(const Chunk& c, float scale) {
+  constexpr int E = Vec16<T>::kElts, AHEAD = 4;
+  const unsigned vecs = c.bytes / 16;
+  auto scaled = [&](const uint4& v) __attribute__((always_inline)) {
+    float f[E];
+    Vec16<T>::unpack(v, f);
+#pragma unroll
+    for (int i = 0; i < E; ++i) f[i] *= scale;
+    return Vec16<T>::pack(f);
+  };
+  const uint4* src = reinterpret_cast<const uint4*>(c.src);
+  uint4* dst = reinterpret_cast<uint4*>(c.dst);
+  unsigned v = threadIdx.x;
+  for (; v + (AHEAD - 1) * 256 < vecs; v += AHEAD * 256) {
+    uint4 x[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) x[k] = src[v + k * 256];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) dst[v + k * 256] = scaled(x[k]);
+  }
+  for (; v < vecs; v += 256) dst[v] = scaled(src[v]);
+  const unsigned tail = (c.bytes - vecs * 16) / sizeof(T);
+  if (threadIdx.x < tail) {
+    const T* from = reinterpret_cast<const T*>(c.src + vecs * 16) + threadIdx.x;
+    Elt<T>::store(reinterpret_cast<T*>(c.dst + vecs * 16) + threadIdx.x, Elt<T>::load(from) * scale);
+  }
+}
+__device__ __forceinline__ void copy_chunk(const Chunk& c) {
+  const unsigned vecs = c.bytes / 16;
+  for (unsigned v = threadIdx.x; v < vecs; v += 256) reinterpret_cast<uint4*>(c.dst)[v] = reinterpret_cast<const uint4*>(c.src)[v];
+  const unsigned tail = (c.bytes - vecs * 16) / 2;
+  if (threadIdx.x < tail)
+    reinterpret_cast<bf16_t*>(c.dst + vecs * 16)[threadIdx.x] = reinterpret_cast<const bf16_t*>(c.src + vecs * 16)[threadIdx.x];
+}
+
+__global__ __launch_bounds__(256) void clip_gradients_kernel(Table tab, const float* __restrict__ norm, double max_norm) {
+  const Chunk c = chunk_of(tab, tab.chunks - 1 - blockIdx.x);
+  const float n = *norm;
+  // (a comparison with NaN is false, and an infinite norm scales nothing either: bits are kept, NaN and all)
+  if (!((double)n > max_norm && n < INFINITY)) {
+    if (c.dst != c.src) copy_chunk(c);
+    return;
+  }
+  const float scale = (float)(max_norm / (double)n);
+  if (c.f32) scale_chunk<float>(c, scale);
+  else scale_chunk<bf16_t>(c, scale);
+}
+
+size_t bytes_of(const moe_gradient& g) { return (size_t)g.count * (g.dtype == MOE_F32 ? 4 : 2); }
+// Chunks of 16 KB, or as many times that as keep their number near 4096 (16 of a compute unit).
+size_t chunk_size(const moe_gradient* list, int n) {
+  size_t total = 0;
+  for (int i = 0; i < n; ++i) total += bytes_of(list[i]);
+  const size_t unit = (size_t)16 << 10;
+  size_t c = (total / 4096 + unit - 1) / unit * unit;
+  if (c < unit) c = unit;
+  return c < ((size_t)1 << 30) ? c : (size_t)1 << 30;
+}
+size_t chunks_of(const moe_gradient& g, size_t chunk) { return (bytes_of(g) + chunk - 1) / chunk; }
+
+// f(table) for as many tensors at a time as a launch takes, forwards or backwards
+template <typename F>
+int for_tables(const moe_gradient* list, int n, size_t chunk, bool backwards, F&& f) {
+  Table tab;
+  int rc = MOE_OK;
+  for (int done = 0; done < n && rc == MOE_OK;) {
+    const int take = n - done < kTensors ? n - done : kTensors, from = backwards ? n - done - take : done;
+    unsigned long long chunks = 0;
+    tab.n = 0;
+    for (int i = from; i < from + take; ++i) {
+      if (list[i].count == 0) continue;
+      tab.t[tab.n++] = Piece{list[i].src, list[i].dst, (unsigned long long)list[i].count << 1 | (list[i].dtype == MOE_F32 ? 1u : 0u),
+                             (unsigned)chunks, 0};
+      chunks += chunks_of(list[i], chunk);
+    }
+    done += take;
+    if (tab.n == 0) continue;
+    if (chunks > 0x7fffffffULL) return MOE_EUNSUPPORTED;
+    tab.chunks = (unsigned)chunks;
+    tab.chunk_bytes = (unsigned)chunk;
+    rc = f(tab);
+  }
+  return rc;
+}
+
+}  // namespace
+
+size_t gradient_norm_bytes(const moe_gradient* list, int n) {
+  const size_t chunk = chunk_size(list, n);
+  size_t chunks = 0;
+  for (int i = 0; i < n; ++i) chunks += chunks_of(list[i], chunk);
+  return align_up((chunks + 1) * sizeof(double), 256);
+}
+
+int launch_gradient_norm(const moe_gradient* list, int n, float* norm, void* ws, hipStream_t st) {
+  double* const partial = static_cast<double*>(ws);
+  size_t used = 0;
+  const int rc = for_tables(list, n, chunk_size(list, n), false, [&](const Table& tab) {
+    hipLaunchKernelGGL(gradient_squares_kernel, dim3(tab.chunks), dim3(256), 0, st, tab, partial + used);
+    used += tab.chunks;
+    return check_launch();
+  });
+  if (rc != MOE_OK) return rc;
+  hipLaunchKernelGGL(gradient_norm_kernel, dim3(1), dim3(1024), 0, st, partial, (unsigned)used, norm);
+  return check_launch();
+}
+
+int launch_clip_gradients(const moe_gradient* list, int n, const float* norm, double max_norm, hipStream_t st) {
+  return for_tables(list, n, chunk_size(list, n), true, [&](const Table& tab) {
+    hipLaunchKernelGGL(clip_gradients_kernel, dim3(tab.chunks), dim3(256), 0, st, tab, norm, max_norm);
+    return check_launch();
+  });
+}
+
+}  // namespace moe
