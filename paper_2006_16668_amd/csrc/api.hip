@@ -490,6 +490,7 @@ int moe_prepare(void) {
   if (rc == MOE_OK) rc = moe::prepare_gate();
   if (rc == MOE_OK) rc = moe::prepare_backward();
   if (rc == MOE_OK) rc = moe::prepare_attention_mfma();
+  if (rc == MOE_OK) rc = moe::prepare_cross_attention();
   void* p = nullptr;
   if (rc == MOE_OK) rc = gate_scratch_ptr(&p);
   return rc;

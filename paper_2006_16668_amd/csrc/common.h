@@ -478,5 +478,6 @@ int prepare_vocab_gemm();         // vocab_gemm.hip
 int prepare_gate();               // gate.hip
 int prepare_backward();           // backward.hip
 int prepare_attention_mfma();     // attention_mfma.hip
+int prepare_cross_attention();    // cross_attention.hip
 
 }  // namespace moe

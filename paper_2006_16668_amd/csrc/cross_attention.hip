@@ -1,112 +1,700 @@
-// Attention of a decoder's tokens to an encoder's states, forward and backward.
+// Attention of a decoder's tokens to an encoder's states on the matrix cores, forward and backward (bf16, d = 64 or 128).
+//
+//   ctx = softmax(q K^T / sqrt(d)) V over the states that a source holds;  with p = exp(score - lse), D = rowsum(dctx * ctx):
+//   dV = p^T dctx,  ds = p * (dctx V^T - D) / sqrt(d),  dq = ds K,  dK = ds^T q
+//
+// The arrangement is that of attention_mfma.hip (everything transposed, a lane owns a column of a score tile; steps as lists of units).  What differs:
+//
+//   columns   Lq tokens times the `share` heads that use one key head: head k share + c % share of token c / share.  Heads that share
+//             fill a tile of columns of few tokens, and the gradients of a shared head are one sum, in a fixed order.
+//   states    a source's own number of them, read on the device.  Rows past it are staged as zeros and their probabilities are
+//             0 (what memory holds there has no part); a source without any gives rows of zeros.
+//   P, dS     are rounded to bf16 in front of the second products, as the self-attention of whole blocks does: three terms of them
+//             (attention_mfma.hip, RAGGED) cost a fifth more, and q, ctx and the results are rounded as much anyway.
 #include <float.h>
 #include <math.h>
-#include "common.h"
+#include "attention_tiles.h"
+#include "cross_attention.h"
 
 namespace moe {
 namespace {
 
-// One wavefront per column (a query, or backward a state), lanes over d: for every case, and nothing else.
-template <typename T, int D>
-struct Lanes {
-  static constexpr int PER = D / 64;
-  float v[PER];
-  __device__ void load(const T* p, int lane) {
-    for (int i = 0; i < PER; ++i) v[i] = Elt<T>::load(p + lane * PER + i);
+// rows of a block of 64 whose first is at `src`; rows from `rows` on are zeros
+template <int D>
+__device__ __forceinline__ void stage_rows(uint32_t lds, const bf16_t* src, int rows, const uint32_t (&off)[AttGeom<D>::kCopies], int q,
+                                           int wave, int lane) {
+  using GM = AttGeom<D>;
+  lds += (wave * GM::kCopies + q) * 1024;
+  if (rows < 64) {
+    const int row = GM::kRowsPerCopy * (GM::kCopies * wave + q) + lane / GM::kChunks;
+    const uint64_t at = row < rows ? (uint64_t)(uintptr_t)src + off[q] : (uint64_t)(uintptr_t)&att_zero_line;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(at) : "memory");
+  } else {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off[q]), "s"(src) : "memory");
   }
-  __device__ void store(T* p, int lane, float f) const {
-    for (int i = 0; i < PER; ++i) Elt<T>::store(p + lane * PER + i, v[i] * f);
+}
+// Per-lane byte offsets of this wavefront's copies of 64 columns (share divides 64).
+template <int D>
+__device__ __forceinline__ void column_offsets(uint32_t (&off)[AttGeom<D>::kCopies], const CrossCols& c, int wave, int lane) {
+  using GM = AttGeom<D>;
+#pragma unroll
+  for (int q = 0; q < GM::kCopies; ++q) {
+    const int row = GM::kRowsPerCopy * (GM::kCopies * wave + q) + lane / GM::kChunks;
+    off[q] = (uint32_t)(c.offset<D>(row) * 2) + 16 * ((lane % GM::kChunks) ^ att_swizzle<D>(row));
   }
-  __device__ float dot(const Lanes& o) const {
-    float s = 0.f;
-    for (int i = 0; i < PER; ++i) s = fmaf(v[i], o.v[i], s);
-    return wave_sum(s);
+}
+// Start the copies of the wavefront's own 32 CT rows to its own LDS block; address(row) is where row `row` is.
+template <int D, int CT, typename F>
+__device__ __forceinline__ void stage_own_rows(uint32_t lds, int lane, F&& address) {
+  using GM = AttGeom<D>;
+#pragma unroll
+  for (int q = 0; q < 32 * CT * GM::kRow / 1024; ++q) {
+    const int row = GM::kRowsPerCopy * q + lane / GM::kChunks;
+    const uint64_t src = (uint64_t)(uintptr_t)(address(row) + 8 * ((lane % GM::kChunks) ^ att_swizzle<D>(row)));
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds + q * 1024), "v"(src) : "memory");
   }
-  __device__ void add(const Lanes& o, float f) {
-    for (int i = 0; i < PER; ++i) v[i] = fmaf(o.v[i], f, v[i]);
+}
+// The wavefront's result tiles times factor as whole rows, turned through its own LDS block: put(row, chunk, 16 bytes).
+template <int D, int CT, typename F>
+__device__ __forceinline__ void store_rows(const f32x16_t (&acc)[CT][D / 32], float factor, uint32_t lds, int lane, F&& put) {
+  using GM = AttGeom<D>;
+  typedef u32x2_t __attribute__((address_space(3))) * lds_u2_ptr;
+  const int r = lane & 31, hf = lane >> 5;
+#pragma unroll
+  for (int c = 0; c < CT; ++c)
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *(lds_u2_ptr)(uintptr_t)(lds + (32 * c + r) * GM::kRow + (((4 * dt + g) ^ att_swizzle<D>(r)) << 4) + 8 * hf) =
+            u32x2_t{pack_bf16x2(acc[c][dt][4 * g] * factor, acc[c][dt][4 * g + 1] * factor),
+                    pack_bf16x2(acc[c][dt][4 * g + 2] * factor, acc[c][dt][4 * g + 3] * factor)};
+#pragma unroll
+  for (int q = 0; q < 32 * CT * GM::kRow / 1024; ++q) {
+    const int row = GM::kRowsPerCopy * q + lane / GM::kChunks, chunk = lane % GM::kChunks;
+    const u32x4_t v = *(lds_u4_ptr)(uintptr_t)(lds + row * GM::kRow + ((chunk ^ att_swizzle<D>(row)) << 4));
+    put(row, chunk, v);
   }
-  __device__ void clear() {
-    for (int i = 0; i < PER; ++i) v[i] = 0.f;
+}
+
+// the block's (source, key head), and the wavefront's first column of `blocks` blocks of 128 CT
+template <int CT> struct CrossWork {
+  long long bk, b;
+  int k, block0, col0;
+  __device__ __forceinline__ CrossWork(int count, int kv_heads, int wave) {
+    const int blocks = (count + 128 * CT - 1) / (128 * CT);
+    const unsigned work = xcd_contiguous(blockIdx.x, gridDim.x), pair = work / blocks;
+    bk = pair;
+    k = __builtin_amdgcn_readfirstlane(pair % kv_heads);
+    b = __builtin_amdgcn_readfirstlane(pair / kv_heads);
+    block0 = __builtin_amdgcn_readfirstlane((int)(work % blocks) * (128 * CT));
+    col0 = block0 + wave * (32 * CT);
   }
 };
-__device__ __forceinline__ int held(const int32_t* src_len, long long b, int Lk) {
-  if (src_len == nullptr) return Lk;
-  const int n = src_len[b];
-  return n < 0 ? 0 : n > Lk ? Lk : n;
-}
-struct Geo { int Lq, Lk, heads, kv_heads, share; };
 
-template <typename T, int D>
-__global__ void cross_plain_kernel(Geo g, const T* q, const T* kv, const int32_t* src_len, T* ctx, float* lse) {
-  const int lane = threadIdx.x, cols = g.Lq * g.share;
-  const long long item = blockIdx.x, bk = item / cols, b = bk / g.kv_heads;
-  const int c = (int)(item % cols), k = (int)(bk % g.kv_heads), h = k * g.share + c % g.share, A = g.heads * D, Akv = g.kv_heads * D;
-  const size_t row = ((size_t)b * g.Lq + c / g.share) * A + (size_t)h * D;
-  const int n = held(src_len, b, g.Lk);
-  Lanes<T, D> qv, o, x;
-  qv.load(q + row, lane);
-  o.clear();
-  float m = -FLT_MAX, l = 0.f;
-  const float scale = 1.f / sqrtf((float)D);
-  for (int j = 0; j < n; ++j) {
-    const T* kr = kv + ((size_t)b * g.Lk + j) * 2 * Akv + (size_t)k * D;
-    x.load(kr, lane);
-    const float s = qv.dot(x) * scale, mn = fmaxf(m, s), f = expf(m - mn), p = expf(s - mn);
-    x.load(kr + Akv, lane);
-    for (int i = 0; i < Lanes<T, D>::PER; ++i) o.v[i] = o.v[i] * f + p * x.v[i];
-    l = l * f + p;
-    m = mn;
+// zeros to the columns first .. first + 127 of a block, 256 threads
+template <int D>
+__device__ __forceinline__ void clear_columns(bf16_t* base, const CrossCols& c, int first) {
+  for (int i = threadIdx.x; i < 128 * (D / 8); i += 256) {
+    const int col = first + i / (D / 8);
+    if (col < c.count) *reinterpret_cast<u32x4_t*>(base + c.offset<D>(col) + 8 * (i % (D / 8))) = u32x4_t{0u, 0u, 0u, 0u};
   }
-  o.store(ctx + row, lane, n > 0 ? 1.f / l : 0.f);
-  if (lse != nullptr && lane == 0) lse[item] = n > 0 ? m + logf(l) : 0.f;
 }
-template <typename T, int D>
-__global__ void cross_plain_dq_kernel(Geo g, const T* q, const T* kv, const int32_t* src_len, const T* ctx, const T* dctx, const float* lse, T* dq,
-                                      float* dvec) {
-  const int lane = threadIdx.x, cols = g.Lq * g.share;
-  const long long item = blockIdx.x, bk = item / cols, b = bk / g.kv_heads;
-  const int c = (int)(item % cols), k = (int)(bk % g.kv_heads), h = k * g.share + c % g.share, A = g.heads * D, Akv = g.kv_heads * D;
-  const size_t row = ((size_t)b * g.Lq + c / g.share) * A + (size_t)h * D;
-  const int n = held(src_len, b, g.Lk);
-  Lanes<T, D> qv, gv, o, x, y;
-  qv.load(q + row, lane);
-  gv.load(dctx + row, lane);
-  x.load(ctx + row, lane);
-  const float dd = gv.dot(x), scale = 1.f / sqrtf((float)D);
-  if (lane == 0) dvec[item] = dd;
-  o.clear();
-  for (int j = 0; j < n; ++j) {
-    const T* kr = kv + ((size_t)b * g.Lk + j) * 2 * Akv + (size_t)k * D;
-    x.load(kr, lane);
-    y.load(kr + Akv, lane);
-    o.add(x, expf(qv.dot(x) * scale - lse[item]) * (gv.dot(y) - dd) * scale);
+
+// ---------------------------------------------------------------- forward
+template <int D>
+__global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossGeo g, const bf16_t* __restrict__ q, const bf16_t* __restrict__ kv,
+                                                               const int32_t* __restrict__ src_len, bf16_t* __restrict__ ctx,
+                                                               float* __restrict__ lse) {
+  using GM = AttGeom<D>;
+  constexpr int CT = 1, KS = D / 16, DT = D / 32, kOwnBlock = 32 * CT * GM::kRow;
+  constexpr int kV = 2 * GM::kBlock;                           // LDS: two K blocks, two V blocks
+  extern __shared__ __attribute__((aligned(256))) unsigned char att_lds[];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)((lds_ptr)att_lds);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 31, hf = lane >> 5;
+  const CrossCols cols(g, D);
+  const CrossWork<CT> w(cols.count, g.kv_heads, wave);
+  const size_t head = cols.base(w.b, w.k, D);
+  const int n = held_states(src_len, w.b, g.Lk);
+  if (n == 0) {
+    clear_columns<D>(ctx + head, cols, w.block0);
+    if (lse != nullptr && threadIdx.x < 128 && w.block0 + (int)threadIdx.x < cols.count) lse[(size_t)w.bk * cols.count + w.block0 + threadIdx.x] = 0.f;
+    return;
   }
-  o.store(dq + row, lane, 1.f);
+  const int Akv = g.kv_heads * D;
+  const size_t ld = (size_t)2 * Akv;
+  const bf16_t* const keys = kv + (size_t)w.b * g.Lk * ld + (size_t)w.k * D;
+  const bool live = w.col0 < cols.count;
+
+  uint32_t off[GM::kCopies];
+  copy_offsets<D>(off, ld, wave, lane);
+  const int nkb = (n + 63) / 64;
+  // copy x of step j's: K block j + 1 (after the last one, that once more), V block j
+  auto start = [&](int j, int x) __attribute__((always_inline)) {
+    const int k = j + 1 < nkb ? j + 1 : nkb - 1, v = j;
+    if (x < GM::kCopies) stage_rows<D>(lds0 + ((j + 1) & 1) * GM::kBlock, keys + (size_t)64 * k * ld, n - 64 * k, off, x, wave, lane);
+    else stage_rows<D>(lds0 + kV + (j & 1) * GM::kBlock, keys + Akv + (size_t)64 * v * ld, n - 64 * v, off, x - GM::kCopies, wave, lane);
+  };
+  constexpr int COPIES = 2 * GM::kCopies;
+  // the wavefront's own rows come (and its results go) through the second places of K and V
+  const uint32_t own = GM::kBlock + (wave & 1) * kOwnBlock + (wave >> 1) * kV;
+#pragma unroll
+  for (int x = 0; x < GM::kCopies; ++x) { start(-1, x); start(0, GM::kCopies + x); }     // K and V block 0
+  if (live)
+    stage_own_rows<D, CT>(lds0 + own, lane, [&](int row) __attribute__((always_inline)) { return q + head + cols.offset<D>(cols.within(w.col0 + row)); });
+  wait_all_copies();
+
+  const float sl2 = 1.4426950408889634f / sqrtf((float)D);
+  const AttReads<D> rd(lds0, lane);
+  u32x4_t qf[KS];                                              // Q^T fragments: lane (r, hf) holds d = 16 s + 8 hf .. + 7
+  f32x16_t o[DT];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    qf[s] = rd.row(own, 0, s);
+    asm volatile("" : "+v"(qf[s]) :: "memory");
+  }
+  __syncthreads();
+  if (nkb > 1) {
+#pragma unroll
+    for (int x = 0; x < GM::kCopies; ++x) start(0, x);         // K block 1
+  }
+  if (!live) {                                                 // a wavefront without columns only stages
+    for (int kb = 0; kb + 1 < nkb; ++kb) {
+      wait_all_copies();
+      __syncthreads();
+#pragma unroll
+      for (int x = 0; x < COPIES; ++x) start(kb + 1, x);
+    }
+    wait_all_copies();
+    __syncthreads();
+    __syncthreads();
+    return;
+  }
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+  // running maximum (in log2 units) and sum; the maximum starts finite, so that a block of states whose scores
+  // are all -inf adds nothing
+  float m_run = -FLT_MAX, l_run = 0.f, m_new;
+  f32x16_t sacc[2];                                            // scores of block kb [32-state tile], and the maximum with them
+  auto mask_end = [&](f32x16_t (&acc)[2], int kb) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (kb * 64 + 32 * t + 8 * (i >> 2) + 4 * hf + (i & 3) >= n) acc[t][i] = -INFINITY;
+  };
+  auto block_max = [&](const f32x16_t (&acc)[2]) __attribute__((always_inline)) {
+    float mx = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, acc[t][i]);
+    return mx;
+  };
+  auto new_max = [&](float mx) __attribute__((always_inline)) {
+    m_new = fmaxf(m_run, fmaxf(mx, __shfl_xor(mx, 32, 64)) * sl2);        // sl2 > 0: scaling commutes with max
+  };
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int s = 0; s < KS; ++s) sacc[t] = MOE_MFMA(rd.row(0, t, s), qf[s], s == 0 ? f32x16_t{} : sacc[t]);
+  if (64 > n) mask_end(sacc, 0);
+  new_max(block_max(sacc));
+
+  // One block of states; after the LAST there are no scores to multiply ahead.
+  auto step = [&](int kb, auto last) __attribute__((always_inline)) {
+    constexpr bool LAST = decltype(last)::value;
+    constexpr int FIRST = LAST ? 2 * KS : 0;                   // (units 0 .. 2 KS - 1 are those scores)
+    wait_all_copies();                                         // K block kb + 1 and V block kb are there;
+    __syncthreads();                                           // K block kb and V block kb - 1 are read, their places free
+    const uint32_t kst = ((kb + 1) & 1) * GM::kBlock, vst = kV + (kb & 1) * GM::kBlock;
+    // rescale only when some query of the wavefront needs it (alpha == 1 exactly otherwise)
+    if (__builtin_amdgcn_ballot_w64(m_new != m_run) != 0) {
+      const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);   // 0 on the first block
+      l_run *= alpha;
+#pragma unroll
+      for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[t][i] *= alpha;
+    }
+    m_run = m_new;
+    float psum = 0.f, mx = -INFINITY;
+    f32x16_t snext[2];
+    u32x4_t pf[2];                                             // P^T, k step % 2
+    auto exponentials = [&](int t, int first, int last) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = first; i < last; ++i) {
+        const float v = __builtin_amdgcn_exp2f(fmaf(sacc[t][i], sl2, -m_run));
+        sacc[t][i] = v;
+        psum += v;
+      }
+    };
+    if constexpr (LAST) {
+      exponentials(0, 0, 16);
+      pf[0] = pack8(sacc[0], 0);
+      pf[1] = pack8(sacc[0], 8);
+    }
+    // units 0 .. 2 KS - 1: scores of block kb + 1, under them the first tile's exponentials; then 4 DT units of O^T, under
+    // them the second tile's and the next block's maximum
+    run_units<FIRST, 2 * KS + 4 * DT, 4>(
+        [&](auto) __attribute__((always_inline)) { return std::integral_constant<int, 1>{}; },
+        [&](auto U) __attribute__((always_inline)) {
+          constexpr int u = decltype(U)::value, v = u - 2 * KS;
+          if constexpr (u < 2 * KS) return rd.row(kst, u / KS, u % KS);
+          else return rd.transposed(vst, 16 * (v / DT), v % DT);
+        },
+        [&](auto U, auto, const u32x4_t& f) __attribute__((always_inline)) {
+          constexpr int u = decltype(U)::value, v = u - 2 * KS;
+          if constexpr (u < 2 * KS) snext[u / KS] = MOE_MFMA(f, qf[u % KS], u % KS == 0 ? f32x16_t{} : snext[u / KS]);
+          else o[v % DT] = MOE_MFMA(f, pf[(v / DT) % 2], o[v % DT]);
+        },
+        [&](auto U, auto, auto) __attribute__((always_inline)) {
+          constexpr int u = decltype(U)::value, v = u - 2 * KS;
+          if constexpr (!LAST && u < COPIES) start(kb + 1, u);
+          if constexpr (u < 2 * KS) {
+            exponentials(0, u * 8 / KS, (u + 1) * 8 / KS);
+            if constexpr (u == KS + 1) pf[0] = pack8(sacc[0], 0);
+            if constexpr (u == 2 * KS - 1) pf[1] = pack8(sacc[0], 8);
+          } else if constexpr (v < 2 * DT) {
+            exponentials(1, v * 16 / (2 * DT), (v + 1) * 16 / (2 * DT));
+            // the fragment of k step 0 is free after DT units, the second tile's first 8 values done by then
+            if constexpr (v == DT) pf[0] = pack8(sacc[1], 0);
+          } else {
+            if constexpr (v == 2 * DT) pf[1] = pack8(sacc[1], 8);
+            constexpr int x = v - 2 * DT - 1, all = 2 * DT - 1;
+            if constexpr (!LAST && x >= 0) {
+#pragma unroll
+              for (int j = x * 32 / all; j < (x + 1) * 32 / all; ++j) mx = fmaxf(mx, snext[j >> 4][j & 15]);
+            }
+          }
+        });
+    l_run += psum + __shfl_xor(psum, 32, 64);
+    if constexpr (LAST) return;
+    if (kb + 2 == nkb && (n & 63) != 0) {                      // the last block comes next: without its rows past the end
+      mask_end(snext, kb + 1);
+      mx = block_max(snext);
+    }
+    new_max(mx);
+    sacc[0] = snext[0];
+    sacc[1] = snext[1];
+  };
+  for (int kb = 0; kb + 1 < nkb; ++kb) step(kb, std::false_type{});
+  step(nkb - 1, std::true_type{});
+  __syncthreads();                                             // the other wavefronts have read the last blocks
+  const int c = w.col0 + r;
+  // row statistic for the backward pass: log sum_k exp(score) in natural-log units
+  if (lse != nullptr && hf == 0 && c < cols.count) lse[(size_t)w.bk * cols.count + c] = (m_run + log2f(l_run)) * 0.6931471805599453f;
+  const f32x16_t (&tiles)[1][DT] = reinterpret_cast<const f32x16_t (&)[1][DT]>(o);
+  store_rows<D, CT>(tiles, 1.0f / l_run, lds0 + own, lane, [&](int row, int chunk, const u32x4_t& v) __attribute__((always_inline)) {
+    if (w.col0 + row < cols.count) *reinterpret_cast<u32x4_t*>(ctx + head + cols.offset<D>(w.col0 + row) + 8 * chunk) = v;
+  });
 }
-template <typename T, int D>
-__global__ void cross_plain_dkv_kernel(Geo g, const T* q, const T* kv, const int32_t* src_len, const T* dctx, const float* lse, const float* dvec, T* dkv) {
-  const int lane = threadIdx.x, cols = g.Lq * g.share;
-  const long long item = blockIdx.x, bk = item / g.Lk, b = bk / g.kv_heads;
-  const int j = (int)(item % g.Lk), k = (int)(bk % g.kv_heads), A = g.heads * D, Akv = g.kv_heads * D;
-  const size_t row = ((size_t)b * g.Lk + j) * 2 * Akv + (size_t)k * D;
-  Lanes<T, D> kk, vv, dk, dv, x, y;
-  dk.clear();
-  dv.clear();
-  if (j < held(src_len, b, g.Lk)) {
-    kk.load(kv + row, lane);
-    vv.load(kv + row + Akv, lane);
-    const float scale = 1.f / sqrtf((float)D);
-    for (int c = 0; c < cols; ++c) {
-      const size_t at = ((size_t)b * g.Lq + c / g.share) * A + (size_t)(k * g.share + c % g.share) * D;
-      x.load(q + at, lane);
-      y.load(dctx + at, lane);
-      const float p = expf(kk.dot(x) * scale - lse[bk * cols + c]);
-      dv.add(y, p);
-      dk.add(x, p * (vv.dot(y) - dvec[bk * cols + c]) * scale);
+
+// ---------------------------------------------------------------- dq (and D)
+template <int D>
+__global__ __launch_bounds__(256, 2) void cross_dq_kernel(CrossGeo g, const bf16_t* __restrict__ q, const bf16_t* __restrict__ kv,
+                                                          const int32_t* __restrict__ src_len, const bf16_t* __restrict__ ctx,
+                                                          const bf16_t* __restrict__ dctx, const float* __restrict__ lse,
+                                                          bf16_t* __restrict__ dqo, float* __restrict__ dvec) {
+  using GM = AttGeom<D>;
+  constexpr int CT = 1, KS = D / 16, DT = D / 32, kOwnBlock = 32 * CT * GM::kRow;
+  // LDS: three K blocks, two V blocks; the wavefronts' own rows go through all of their places but the first, so that
+  // two blocks share a compute unit
+  constexpr int kV = 3 * GM::kBlock, kQ = GM::kBlock, kGrad = kQ + 4 * kOwnBlock;
+  extern __shared__ __attribute__((aligned(256))) unsigned char att_lds[];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)((lds_ptr)att_lds);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 31, hf = lane >> 5;
+  const CrossCols cols(g, D);
+  const CrossWork<CT> w(cols.count, g.kv_heads, wave);
+  const size_t head = cols.base(w.b, w.k, D);
+  const int n = held_states(src_len, w.b, g.Lk);
+  if (n == 0) {                                                // (no state asks for D)
+    clear_columns<D>(dqo + head, cols, w.block0);
+    return;
+  }
+  const int Akv = g.kv_heads * D;
+  const size_t ld = (size_t)2 * Akv;
+  const bf16_t* const keys = kv + (size_t)w.b * g.Lk * ld + (size_t)w.k * D;
+  const bool live = w.col0 < cols.count;
+
+  uint32_t off[GM::kCopies];
+  copy_offsets<D>(off, ld, wave, lane);
+  const int nkb = (n + 63) / 64;
+  // copy x of step j's: K block j + 1 to place `slot`, V block j (after the last ones, those once more)
+  auto start = [&](int j, int slot, int x) __attribute__((always_inline)) {
+    const int k = j + 1 < nkb ? j + 1 : nkb - 1, v = j < nkb ? j : nkb - 1;
+    if (x < GM::kCopies) stage_rows<D>(lds0 + slot * GM::kBlock, keys + (size_t)64 * k * ld, n - 64 * k, off, x, wave, lane);
+    else stage_rows<D>(lds0 + kV + (j & 1) * GM::kBlock, keys + Akv + (size_t)64 * v * ld, n - 64 * v, off, x - GM::kCopies, wave, lane);
+  };
+  constexpr int COPIES = 2 * GM::kCopies;
+
+  // Q^T and dO^T fragments of this wavefront's columns, D and lse of the lane's.  The rows come through LDS: read as
+  // fragments from memory, 16 bytes of 32 rows at a time, they take longer (O, one of three, hides behind the others).
+  const uint32_t own = kQ + wave * kOwnBlock;
+  const float scale = 1.0f / sqrtf((float)D), sl2 = 1.4426950408889634f * scale;
+  const AttReads<D> rd(lds0, lane);
+  u32x4_t qf[KS], dof[KS], of[KS];
+#pragma unroll
+  for (int x = 0; x < GM::kCopies; ++x) start(-1, 0, x);       // K block 0
+  if (live) {
+    auto column = [&](int row) __attribute__((always_inline)) { return head + cols.offset<D>(cols.within(w.col0 + row)); };
+    stage_own_rows<D, CT>(lds0 + own, lane, [&](int row) __attribute__((always_inline)) { return q + column(row); });
+    stage_own_rows<D, CT>(lds0 + kGrad + wave * kOwnBlock, lane, [&](int row) __attribute__((always_inline)) { return dctx + column(row); });
+    const bf16_t* const orow = ctx + column(r);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) of[s] = *reinterpret_cast<const u32x4_t*>(orow + 16 * s + 8 * hf);
+    wait_all_copies();
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      qf[s] = rd.row(own, 0, s);
+      dof[s] = rd.row(kGrad + wave * kOwnBlock, 0, s);
+      asm volatile("" : "+a"(qf[s]), "+a"(dof[s]) :: "memory");
+      asm volatile("" : "+v"(of[s]));
     }
   }
-  dk.store(dkv + row, lane, 1.f);
-  dv.store(dkv + row + Akv, lane, 1.f);
+  wait_all_copies();
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < COPIES; ++x) start(0, 1, x);             // K block 1 and V block 0
+
+  if (!live) {                                                 // a wavefront without columns only stages
+    for (int kb = 0, k2 = 2; kb < nkb; ++kb) {
+      wait_all_copies();
+      __syncthreads();
+      if (kb + 1 < nkb) {
+#pragma unroll
+        for (int x = 0; x < COPIES; ++x) start(kb + 1, k2, x);
+      }
+      k2 = k2 == 2 ? 0 : k2 + 1;
+    }
+    wait_all_copies();
+    __syncthreads();
+    return;
+  }
+  f32x16_t dq[CT][DT];
+  float dd = 0.f, lse2;
+  {
+    const int c = w.col0 + r;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      float gr[8], ov[8];
+      Vec16<bf16_t>::unpack(uint4{dof[s][0], dof[s][1], dof[s][2], dof[s][3]}, gr);
+      Vec16<bf16_t>::unpack(uint4{of[s][0], of[s][1], of[s][2], of[s][3]}, ov);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) dd = fmaf(gr[i], ov[i], dd);
+    }
+    dd += __shfl_xor(dd, 32, 64);
+    if (hf == 0 && c < cols.count) dvec[(size_t)w.bk * cols.count + c] = dd;
+    lse2 = lse[(size_t)w.bk * cols.count + cols.within(c)] * 1.4426950408889634f;
+#pragma unroll
+    for (int t = 0; t < DT; ++t) clear_acc(dq[0][t]);
+  }
+  asm volatile("" : "+v"(lse2));                               // loaded here, not waited for in the loop
+  f32x16_t sacc;                                               // scores of 32 states
+#pragma unroll
+  for (int s = 0; s < KS; ++s) sacc = MOE_MFMA(rd.row(0, 0, s), qf[s], s == 0 ? f32x16_t{} : sacc);
+
+  int k0 = 0;                                                  // place of K block kb
+  // One block of states; LAST: nothing follows.
+  auto step = [&](int kb, auto last) __attribute__((always_inline)) {
+    constexpr bool LAST = decltype(last)::value;
+    wait_all_copies();                                         // K block kb + 1 and V block kb are there;
+    __syncthreads();                                           // K and V block kb - 1 are read, their places free
+    const int k1 = k0 == 2 ? 0 : k0 + 1, k2 = k1 == 2 ? 0 : k1 + 1;
+    const uint32_t kst = k0 * GM::kBlock, knext = k1 * GM::kBlock, vst = kV + (kb & 1) * GM::kBlock;
+    f32x16_t dpacc, snext;
+    u32x4_t dsf[2];                                            // [k step]
+    // per 32 states: KS units of dP, under them P; KS of the next 32 states' scores (unless there are none),
+    // under them dS; 2 DT of dQ
+    constexpr int UNITS = 2 * KS + 2 * DT;
+    run_units<0, 2 * UNITS, 4>(
+        [&](auto) __attribute__((always_inline)) { return std::integral_constant<int, 1>{}; },
+        [&](auto U) __attribute__((always_inline)) {
+          constexpr int t = decltype(U)::value / UNITS, u = decltype(U)::value % UNITS, v = u - 2 * KS;
+          if constexpr (u < KS) return rd.row(vst, t, u);
+          else if constexpr (u < 2 * KS) return rd.row(t == 0 ? kst : knext, 1 - t, u - KS);
+          else return rd.transposed(kst, 32 * t + 16 * (v / DT), v % DT);
+        },
+        [&](auto U, auto, const u32x4_t& f) __attribute__((always_inline)) {
+          constexpr int t = decltype(U)::value / UNITS, u = decltype(U)::value % UNITS, v = u - 2 * KS;
+          if constexpr (LAST && t == 1 && u >= KS && u < 2 * KS) return;         // (no scores to multiply ahead)
+          if constexpr (u < KS) dpacc = MOE_MFMA(f, dof[u], u == 0 ? f32x16_t{} : dpacc);
+          else if constexpr (u < 2 * KS) snext = MOE_MFMA(f, qf[u - KS], u == KS ? f32x16_t{} : snext);
+          else {
+            if constexpr (v % DT == 0) fresh_operand();
+            mfma_acc(dq[0][v % DT], f, dsf[v / DT]);
+          }
+        },
+        [&](auto U, auto, auto) __attribute__((always_inline)) {
+          constexpr int t = decltype(U)::value / UNITS, u = decltype(U)::value % UNITS;
+          if constexpr (!LAST && decltype(U)::value < COPIES) start(kb + 1, k2, decltype(U)::value);
+          if constexpr (u < KS) {
+#pragma unroll
+            for (int j = u * 16 / KS; j < (u + 1) * 16 / KS; ++j) sacc[j] = __builtin_amdgcn_exp2f(fmaf(sacc[j], sl2, -lse2));
+            if constexpr (LAST && u == KS - 1) {               // (dP of a row of zeros is 0, D is not)
+              if ((n & 63) != 0) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                  if (kb * 64 + 32 * t + 8 * (i >> 2) + 4 * hf + (i & 3) >= n) sacc[i] = 0.f;
+              }
+            }
+          } else if constexpr (u < 2 * KS) {
+            constexpr int x = u - KS - 1, all = KS - 1;        // (not right behind dP's last product)
+            if constexpr (x >= 0) {
+#pragma unroll
+              for (int j = x * 16 / all; j < (x + 1) * 16 / all; ++j) sacc[j] = sacc[j] * (dpacc[j] - dd);
+            }
+            if constexpr (u == KS + KS / 2 + 1) dsf[0] = pack8(sacc, 0);
+          } else if constexpr (u == 2 * KS) {
+            dsf[1] = pack8(sacc, 8);
+          }
+          if constexpr (u == UNITS - 1) sacc = snext;
+        });
+    k0 = k1;
+  };
+  for (int kb = 0; kb + 1 < nkb; ++kb) step(kb, std::false_type{});
+  step(nkb - 1, std::true_type{});
+  settle_all(dq);
+  __syncthreads();                                             // the other wavefronts have read the last blocks
+  store_rows<D, CT>(dq, scale, lds0 + own, lane, [&](int row, int chunk, const u32x4_t& v) __attribute__((always_inline)) {
+    if (w.col0 + row < cols.count) *reinterpret_cast<u32x4_t*>(dqo + head + cols.offset<D>(w.col0 + row) + 8 * chunk) = v;
+  });
+}
+
+// ---------------------------------------------------------------- dK, dV
+template <int D, int CT>
+__global__ __launch_bounds__(256, 1) void cross_dkv_kernel(CrossGeo g, const bf16_t* __restrict__ q, const bf16_t* __restrict__ kv,
+                                                           const int32_t* __restrict__ src_len, const bf16_t* __restrict__ dctx,
+                                                           const float* __restrict__ lse, const float* __restrict__ dvec,
+                                                           bf16_t* __restrict__ dkv) {
+  using GM = AttGeom<D>;
+  constexpr int KS = D / 16, DT = D / 32, kOwnBlock = 32 * CT * GM::kRow;
+  constexpr int kGrad = GM::kBlock, kStats = 2 * GM::kBlock, kStage = kStats + 512;   // Q rows, dO rows, 64 lse, 64 D
+  constexpr bool kValuesInLds = D == 128 && CT == 2;           // there both operands' fragments and both results are
+  constexpr int kOwn = 2 * kStage;                             // 384 registers, too many beside S and dP
+  extern __shared__ __attribute__((aligned(256))) unsigned char att_lds[];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)((lds_ptr)att_lds);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 31, hf = lane >> 5;
+  const CrossCols cols(g, D);
+  const CrossWork<CT> w(g.Lk, g.kv_heads, wave);
+  const int n = held_states(src_len, w.b, g.Lk), Akv = g.kv_heads * D;
+  const size_t ld = (size_t)2 * Akv;
+  const size_t states = (size_t)w.b * g.Lk * ld + (size_t)w.k * D;
+  // zeros to the rows first .. first + count - 1 that there are, by `threads` threads of which this is number i0
+  auto clear = [&](int first, int count, int i0, int threads) __attribute__((always_inline)) {
+    for (int i = i0; i < count * (D / 8); i += threads) {
+      const int row = first + i / (D / 8);
+      if (row >= g.Lk) return;
+      bf16_t* const at = dkv + states + (size_t)row * ld + 8 * (i % (D / 8));
+      *reinterpret_cast<u32x4_t*>(at) = u32x4_t{0u, 0u, 0u, 0u};
+      *reinterpret_cast<u32x4_t*>(at + Akv) = u32x4_t{0u, 0u, 0u, 0u};
+    }
+  };
+  if (w.block0 >= n) {
+    clear(w.block0, 128 * CT, threadIdx.x, 256);
+    return;
+  }
+  const size_t head = cols.base(w.b, w.k, D);
+  const bf16_t *const qbase = q + head, *const gbase = dctx + head;
+  const float* const stat = (wave & 1 ? dvec : lse) + (size_t)w.bk * cols.count;      // (two wavefronts copy the same 64 values)
+  const bool live = w.col0 < n;
+
+  uint32_t off[GM::kCopies];
+  column_offsets<D>(off, cols, wave, lane);
+  const int nqb = (cols.count + 63) / 64;
+  // copy x of block j: Q rows, dO rows, 64 values of lse and D
+  auto start = [&](int j, int x) __attribute__((always_inline)) {
+    const uint32_t st = lds0 + (j & 1) * kStage;
+    const int first = 64 * j;
+    const size_t at = cols.offset<D>(first);
+    if (x < GM::kCopies) stage_rows<D>(st, qbase + at, cols.count - first, off, x, wave, lane);
+    else if (x < 2 * GM::kCopies) stage_rows<D>(st + kGrad, gbase + at, cols.count - first, off, x - GM::kCopies, wave, lane);
+    else {
+      const uint32_t soff = 4 * cols.within(first + lane);
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(st + kStats + (wave & 1) * 256),
+                   "v"(soff), "s"(stat) : "memory");
+    }
+  };
+  constexpr int COPIES = 2 * GM::kCopies + 1;
+
+  // K and V fragments of this wavefront's states: lane (r, hf) holds d = 16 s + 8 hf .. + 7.  K comes through the places
+  // of Q and dO, V through the wavefront's own block.
+  const AttReads<D> rd(lds0, lane);
+  const uint32_t own = kOwn + wave * kOwnBlock;
+  u32x4_t kf[CT][KS], vf[CT][kValuesInLds ? 1 : KS];
+  if (live) {
+    auto state = [&](int row) __attribute__((always_inline)) {
+      const int at = w.col0 + row < n ? w.col0 + row : n - 1;
+      return kv + states + (size_t)at * ld;
+    };
+    stage_own_rows<D, CT>(lds0 + wave * kOwnBlock, lane, [&](int row) __attribute__((always_inline)) { return state(row); });
+    stage_own_rows<D, CT>(lds0 + own, lane, [&](int row) __attribute__((always_inline)) { return state(row) + Akv; });
+    wait_all_copies();
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        kf[c][s] = rd.row(wave * kOwnBlock, c, s);
+        asm volatile("" : "+v"(kf[c][s]) :: "memory");
+        if (!kValuesInLds) vf[c][s] = rd.row(own, c, s);
+      }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < COPIES; ++x) start(0, x);
+  if (!live) {                                                 // a wavefront without states that hold stages, and clears its rows
+    for (int qb = 0; qb + 1 < nqb; ++qb) {
+      wait_all_copies();
+      __syncthreads();
+#pragma unroll
+      for (int x = 0; x < COPIES; ++x) start(qb + 1, x);
+    }
+    wait_all_copies();
+    __syncthreads();
+    clear(w.col0, 32 * CT, lane, 64);
+    return;
+  }
+  f32x16_t dk[CT][DT], dv[CT][DT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c)
+#pragma unroll
+    for (int t = 0; t < DT; ++t) { clear_acc(dk[c][t]); clear_acc(dv[c][t]); }
+  const float scale = 1.0f / sqrtf((float)D), sl2 = 1.4426950408889634f * scale;
+  // value i of a tile belongs to column 32 t + 8 (i/4) + 4 hf + i%4: four consecutive columns per i/4
+  auto stat4 = [&](uint32_t block, int t, int i4) __attribute__((always_inline)) {
+    return *(lds_f4_ptr)(uintptr_t)(lds0 + block + 4 * (32 * t + 8 * i4 + 4 * hf));
+  };
+  auto step = [&](int qb, auto last) __attribute__((always_inline)) {
+    constexpr bool LAST = decltype(last)::value;
+    wait_all_copies();                                         // block qb is there;
+    __syncthreads();                                           // block qb - 1 is read, its place free
+    const uint32_t qst = (qb & 1) * kStage, gst = qst + kGrad, sst = qst + kStats;
+    f32x16_t p[CT], ds[CT];                                    // S, then P; dP, then dS: [query][state]
+    u32x4_t pt[2][CT], dst[2][CT];                             // [k step][column tile]
+    f32x4_t l4[2], d4[2];
+    u32x4_t vcol[3][CT];
+    // per 32 queries: KS units of S; KS of dP, under them P; 2 DT of dV, under them dS; 2 DT of dK
+    constexpr int UNITS = 2 * KS + 4 * DT;
+    auto end_mask = [&](f32x16_t (&v)[CT], int t, int first) __attribute__((always_inline)) {
+      if ((cols.count & 63) == 0) return;
+#pragma unroll
+      for (int i = first; i < first + 8; ++i)
+        if (qb * 64 + 32 * t + 8 * (i >> 2) + 4 * hf + (i & 3) >= cols.count) {
+#pragma unroll
+          for (int c = 0; c < CT; ++c) v[c][i] = 0.f;
+        }
+    };
+    run_units<0, 2 * UNITS, 3>(
+        [&](auto) __attribute__((always_inline)) { return std::integral_constant<int, CT>{}; },
+        [&](auto U) __attribute__((always_inline)) {
+          constexpr int t = decltype(U)::value / UNITS, u = decltype(U)::value % UNITS, v = u - 2 * KS, x = v - 2 * DT;
+          if constexpr (u < KS) return rd.row(qst, t, u);
+          else if constexpr (u < 2 * KS) return rd.row(gst, t, u - KS);
+          else if constexpr (v < 2 * DT) return rd.transposed(gst, 32 * t + 16 * (v / DT), v % DT);
+          else return rd.transposed(qst, 32 * t + 16 * (x / DT), x % DT);
+        },
+        [&](auto U, auto P, const u32x4_t& f) __attribute__((always_inline)) {
+          constexpr int u = decltype(U)::value % UNITS, v = u - 2 * KS, x = v - 2 * DT, c = decltype(P)::value;
+          if constexpr (kValuesInLds && u >= KS - 2 && u < 2 * KS - 2) vcol[(u - KS + 2) % 3][c] = rd.row(own, c, u - KS + 2);
+          if constexpr (u < KS) p[c] = MOE_MFMA(f, kf[c][u], u == 0 ? f32x16_t{} : p[c]);
+          else if constexpr (u < 2 * KS) {
+            u32x4_t col;                                       // (V from LDS was fetched two units ago)
+            if constexpr (kValuesInLds) col = vcol[(u - KS) % 3][c];
+            else col = vf[c][u - KS];
+            ds[c] = MOE_MFMA(f, col, u == KS ? f32x16_t{} : ds[c]);
+          } else {
+            if constexpr (v % DT == 0 && c == 0) fresh_operand();
+            if constexpr (x < 0) mfma_acc(dv[c][v % DT], f, pt[v / DT][c]);
+            else mfma_acc(dk[c][x % DT], f, dst[x / DT][c]);
+          }
+        },
+        [&](auto U, auto P, auto) __attribute__((always_inline)) {
+          constexpr int t = decltype(U)::value / UNITS, u = decltype(U)::value % UNITS, v = u - 2 * KS, x = v - 2 * DT;
+          constexpr int pc = decltype(P)::value;
+          if constexpr (!LAST && decltype(U)::value < COPIES && pc == 0) start(qb + 1, decltype(U)::value);
+          if constexpr (u == KS - 1 && pc == 0) l4[0] = stat4(sst, t, 0);
+          if constexpr (u >= KS && u < 2 * KS) {               // P
+            constexpr int z = CT * (u - KS) + pc, first = z * 16 / KS, to = (z + 1) * 16 / KS;      // value j: row j / CT, column tile j % CT
+            if constexpr (first % (4 * CT) == 0 && first + 4 * CT < 16 * CT) l4[(first / (4 * CT) + 1) % 2] = stat4(sst, t, first / (4 * CT) + 1);
+#pragma unroll
+            for (int j = first; j < to; ++j)
+              p[j % CT][j / CT] = __builtin_amdgcn_exp2f(fmaf(p[j % CT][j / CT], sl2, -(l4[j / (4 * CT) % 2][j / CT % 4] * 1.4426950408889634f)));
+            if constexpr (LAST && to % (8 * CT) == 0) end_mask(p, t, to / CT - 8);
+            if constexpr (u == KS + KS / 2 + 1) pt[0][pc] = pack8(p[pc], 0);
+            if constexpr (u == 2 * KS - 1 && pc == 0) d4[0] = stat4(sst + 256, t, 0);
+          }
+          if constexpr (v == 0) pt[1][pc] = pack8(p[pc], 8);
+          if constexpr (v >= 0 && x < 0) {                     // dS
+            constexpr int z = CT * v + pc, all = 2 * DT * CT, first = z * 16 * CT / all, to = (z + 1) * 16 * CT / all;
+            if constexpr (first % (4 * CT) == 0 && first != to && first + 4 * CT < 16 * CT) d4[(first / (4 * CT) + 1) % 2] = stat4(sst + 256, t, first / (4 * CT) + 1);
+#pragma unroll
+            for (int j = first; j < to; ++j) ds[j % CT][j / CT] = p[j % CT][j / CT] * (ds[j % CT][j / CT] - d4[j / (4 * CT) % 2][j / CT % 4]);
+            if constexpr (LAST && first != to && to % (8 * CT) == 0) end_mask(ds, t, to / CT - 8);
+            if constexpr (v == DT + 1) dst[0][pc] = pack8(ds[pc], 0);
+          }
+          if constexpr (x == 0) dst[1][pc] = pack8(ds[pc], 8);
+        });
+  };
+  for (int qb = 0; qb + 1 < nqb; ++qb) step(qb, std::false_type{});
+  step(nqb - 1, std::true_type{});
+  settle_all(dk);
+  settle_all(dv);
+  auto put = [&](bf16_t* to) __attribute__((always_inline)) {
+    return [=](int row, int chunk, const u32x4_t& v) __attribute__((always_inline)) {
+      const int at = w.col0 + row;
+      if (at < g.Lk) *reinterpret_cast<u32x4_t*>(to + (size_t)at * ld + 8 * chunk) = at < n ? v : u32x4_t{0u, 0u, 0u, 0u};
+    };
+  };
+  store_rows<D, CT>(dk, scale, lds0 + own, lane, put(dkv + states));
+  store_rows<D, CT>(dv, 1.f, lds0 + own, lane, put(dkv + states + Akv));
+}
+
+template <int D> constexpr int kLdsForward = 4 * AttGeom<D>::kBlock;
+template <int D> constexpr int kLdsQ = 5 * AttGeom<D>::kBlock;
+template <int D, int CT> constexpr int kLdsKV = 2 * (2 * AttGeom<D>::kBlock + 512) + 128 * CT * AttGeom<D>::kRow;
+
+template <int D>
+int prepare_kernels() {
+  static LdsLimitOnce once, once_q, once_kv1, once_kv2;
+  int rc = ensure_lds_limit(once, reinterpret_cast<const void*>(cross_forward_kernel<D>), kLdsForward<D>);
+  if (rc == MOE_OK) rc = ensure_lds_limit(once_q, reinterpret_cast<const void*>(cross_dq_kernel<D>), kLdsQ<D>);
+  if (rc == MOE_OK) rc = ensure_lds_limit(once_kv1, reinterpret_cast<const void*>(cross_dkv_kernel<D, 1>), (kLdsKV<D, 1>));
+  if constexpr (D == 128)
+    if (rc == MOE_OK) rc = ensure_lds_limit(once_kv2, reinterpret_cast<const void*>(cross_dkv_kernel<D, 2>), (kLdsKV<D, 2>));
+  return rc;
+}
+
+template <int D>
+int forward(const CrossShape& s, const bf16_t* q, const bf16_t* kv, const int32_t* src_len, bf16_t* ctx, float* lse, hipStream_t st) {
+  if (prepare_kernels<D>() != MOE_OK) return MOE_EHIP;
+  const long long blocks = s.B * s.kv_heads * ((s.columns() + 127) / 128);
+  if (blocks > 0x7fffffffLL) return MOE_EUNSUPPORTED;
+  hipLaunchKernelGGL((cross_forward_kernel<D>), dim3((unsigned)blocks), dim3(256), kLdsForward<D>, st, CrossGeo(s), q, kv, src_len, ctx, lse);
+  return check_launch();
+}
+template <int D>
+int backward(const CrossShape& s, const bf16_t* q, const bf16_t* kv, const int32_t* src_len, const bf16_t* ctx, const bf16_t* dctx,
+             const float* lse, bf16_t* dq, bf16_t* dkv, float* dvec, hipStream_t st) {
+  int cus = 0;
+  if (prepare_kernels<D>() != MOE_OK || compute_units(&cus) != MOE_OK) return MOE_EHIP;
+  const long long blocks = s.B * s.kv_heads * ((s.columns() + 127) / 128), blocks1 = s.B * s.kv_heads * ((s.Lk + 127) / 128),
+                  blocks2 = s.B * s.kv_heads * ((s.Lk + 255) / 256);
+  if (blocks > 0x7fffffffLL || blocks1 > 0x7fffffffLL) return MOE_EUNSUPPORTED;
+  const CrossGeo g(s);
+  hipLaunchKernelGGL((cross_dq_kernel<D>), dim3((unsigned)blocks), dim3(256), kLdsQ<D>, st, g, q, kv, src_len, ctx, dctx, lse, dq, dvec);
+  // two tiles of 32 states per wavefront where that takes fewer rounds of blocks (1.46 times as long each: attention_dkv_wide)
+  if constexpr (D == 128)
+    if (1.46 * (double)((blocks2 + cus - 1) / cus) < (double)((blocks1 + cus - 1) / cus)) {
+      hipLaunchKernelGGL((cross_dkv_kernel<D, 2>), dim3((unsigned)blocks2), dim3(256), (kLdsKV<D, 2>), st, g, q, kv, src_len, dctx, lse, dvec, dkv);
+      return check_launch();
+    }
+  hipLaunchKernelGGL((cross_dkv_kernel<D, 1>), dim3((unsigned)blocks1), dim3(256), (kLdsKV<D, 1>), st, g, q, kv, src_len, dctx, lse, dvec, dkv);
+  return check_launch();
 }
 
 // 16 bytes a thread: rows of states that hold, zeros for the others
@@ -115,43 +703,39 @@ __global__ __launch_bounds__(256) void held_rows_kernel(const uint4* __restrict_
   const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
   if (i >= total) return;
   const long long row = i / vecs, b = row / Lk;
-  out[i] = (int)(row - b * Lk) < held(src_len, b, Lk) ? mem[i] : uint4{0u, 0u, 0u, 0u};
+  const int n = src_len[b];
+  out[i] = (int)(row - b * Lk) < n ? mem[i] : uint4{0u, 0u, 0u, 0u};
 }
 
 }  // namespace
 
+int prepare_cross_attention() {
+  const int rc = prepare_kernels<64>();
+  return rc != MOE_OK ? rc : prepare_kernels<128>();
+}
+
 size_t cross_scratch_bytes(int, const CrossShape&) { return 0; }
 
-template <typename T, int D>
-int plain(const CrossShape& s, const void* q, const void* kv, const int32_t* len, void* ctx, float* lse, hipStream_t st) {
-  const Geo g{s.Lq, s.Lk, s.heads, s.kv_heads, s.share()};
-  hipLaunchKernelGGL((cross_plain_kernel<T, D>), dim3((unsigned)(s.B * s.kv_heads * s.columns())), dim3(64), 0, st, g, (const T*)q, (const T*)kv, len, (T*)ctx, lse);
-  return check_launch();
-}
-template <typename T, int D>
-int plain_bwd(const CrossShape& s, const void* q, const void* kv, const int32_t* len, const void* ctx, const void* dctx, const float* lse,
-              void* dq, void* dkv, float* dvec, hipStream_t st) {
-  const Geo g{s.Lq, s.Lk, s.heads, s.kv_heads, s.share()};
-  hipLaunchKernelGGL((cross_plain_dq_kernel<T, D>), dim3((unsigned)(s.B * s.kv_heads * s.columns())), dim3(64), 0, st, g, (const T*)q, (const T*)kv, len, (const T*)ctx,
-                     (const T*)dctx, lse, (T*)dq, dvec);
-  hipLaunchKernelGGL((cross_plain_dkv_kernel<T, D>), dim3((unsigned)(s.B * s.kv_heads * s.Lk)), dim3(64), 0, st, g, (const T*)q, (const T*)kv, len, (const T*)dctx, lse,
-                     dvec, (T*)dkv);
-  return check_launch();
+int launch_cross_attention(int act_dtype, const CrossShape& s, const void* q, const void* kv, const int32_t* src_len, void* ctx,
+                           float* lse, void* scratch, hipStream_t st) {
+  if (act_dtype == MOE_F32) return launch_cross_attention_f32(s, q, kv, src_len, ctx, lse, scratch, st);
+  auto qb = static_cast<const bf16_t*>(q);
+  auto kb = static_cast<const bf16_t*>(kv);
+  auto c = static_cast<bf16_t*>(ctx);
+  return s.d == 64 ? forward<64>(s, qb, kb, src_len, c, lse, st) : forward<128>(s, qb, kb, src_len, c, lse, st);
 }
 
-int launch_cross_attention(int act_dtype, const CrossShape& s, const void* q, const void* kv, const int32_t* src_len, void* ctx,
-                           float* lse, void*, hipStream_t st) {
-  if (act_dtype == MOE_F32)
-    return s.d == 64 ? plain<float, 64>(s, q, kv, src_len, ctx, lse, st) : plain<float, 128>(s, q, kv, src_len, ctx, lse, st);
-  return s.d == 64 ? plain<bf16_t, 64>(s, q, kv, src_len, ctx, lse, st) : plain<bf16_t, 128>(s, q, kv, src_len, ctx, lse, st);
-}
 int launch_cross_attention_bwd(int act_dtype, const CrossShape& s, const void* q, const void* kv, const int32_t* src_len,
                                const void* ctx, const void* dctx, const float* lse, void* dq, void* dkv, float* dvec, hipStream_t st) {
-  if (act_dtype == MOE_F32)
-    return s.d == 64 ? plain_bwd<float, 64>(s, q, kv, src_len, ctx, dctx, lse, dq, dkv, dvec, st)
-                     : plain_bwd<float, 128>(s, q, kv, src_len, ctx, dctx, lse, dq, dkv, dvec, st);
-  return s.d == 64 ? plain_bwd<bf16_t, 64>(s, q, kv, src_len, ctx, dctx, lse, dq, dkv, dvec, st)
-                   : plain_bwd<bf16_t, 128>(s, q, kv, src_len, ctx, dctx, lse, dq, dkv, dvec, st);
+  if (act_dtype == MOE_F32) return launch_cross_attention_f32_bwd(s, q, kv, src_len, ctx, dctx, lse, dq, dkv, dvec, st);
+  auto qb = static_cast<const bf16_t*>(q);
+  auto kb = static_cast<const bf16_t*>(kv);
+  auto c = static_cast<const bf16_t*>(ctx);
+  auto gb = static_cast<const bf16_t*>(dctx);
+  auto dqb = static_cast<bf16_t*>(dq);
+  auto dkb = static_cast<bf16_t*>(dkv);
+  return s.d == 64 ? backward<64>(s, qb, kb, src_len, c, gb, lse, dqb, dkb, dvec, st)
+                   : backward<128>(s, qb, kb, src_len, c, gb, lse, dqb, dkb, dvec, st);
 }
 
 int launch_held_rows(int act_dtype, const void* mem, const int32_t* src_len, void* out, long long B, int Lk, int M, hipStream_t st) {
