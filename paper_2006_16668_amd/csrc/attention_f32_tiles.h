@@ -32,6 +32,17 @@ template <int D> struct Rows {
       for (int t = 0; t < D / 32; ++t) v[i][t] = base[(size_t)row * ld + 32 * t + r];
     }
   }
+  // at(row): where row `row` is
+  template <typename F>
+  __device__ __forceinline__ void load_at(F&& at, int row0, int L, int r, int hf) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      int row = row0 + 8 * (i >> 2) + 4 * hf + (i & 3);
+      const float* const p = at(row < L ? row : L - 1);
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t) v[i][t] = p[32 * t + r];
+    }
+  }
   __device__ __forceinline__ void clear_past(int row0, int L, int hf) {
 #pragma unroll
     for (int i = 0; i < 16; ++i)
@@ -64,6 +75,18 @@ template <int D> struct Transit {
       row = row < L ? row : L - 1;
       a[i] = *reinterpret_cast<const f32x4_t*>(pa + (size_t)row * lda + c);
       b[i] = *reinterpret_cast<const f32x4_t*>(pb + (size_t)row * ldb + c);
+    }
+  }
+  // ata(row), atb(row): where the operands' row `row` is
+  template <typename FA, typename FB>
+  __device__ __forceinline__ void fetch_at(FA&& ata, FB&& atb, int blk, int L) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int f = threadIdx.x + 256 * i, c = 4 * (f % kVecs);
+      int row = 32 * blk + f / kVecs;
+      row = row < L ? row : L - 1;
+      a[i] = *reinterpret_cast<const f32x4_t*>(ata(row) + c);
+      b[i] = *reinterpret_cast<const f32x4_t*>(atb(row) + c);
     }
   }
   __device__ __forceinline__ void put(float* la, float* lb, int blk, int L) {

@@ -27,10 +27,21 @@ __device__ __forceinline__ int held_states(const int32_t* src_len, long long b, 
   return n < 0 ? 0 : n > Lk ? Lk : n;
 }
 
+// The forward pass of few columns cuts the states into ranges, side by side; what each leaves of a column: its maximum (log2 units in bf16, natural in
+// fp32) and sum, and its sum of rows of V.
+struct CrossParts {
+  int splits;
+  float2* stats;             // [B kv_heads columns, splits]
+  float* sums;               // [B kv_heads columns, splits, d]
+};
+// few: blocks of 32 columns whose wavefronts take the states' blocks in turn, in `splits` ranges; else blocks of 128 columns
+struct CrossPlan { bool few; int splits; };
+CrossPlan cross_plan(int act_dtype, const CrossShape& s);
+
 // fp32 (cross_attention_f32.hip)
-int launch_cross_attention_f32(const CrossShape& s, const void* q, const void* kv, const int32_t* src_len, void* ctx, float* lse,
-                               void* scratch, hipStream_t st);
-int launch_cross_attention_f32_bwd(const CrossShape& s, const void* q, const void* kv, const int32_t* src_len, const void* ctx,
-                                   const void* dctx, const float* lse, void* dq, void* dkv, float* dvec, hipStream_t st);
+int launch_cross_attention_f32(const CrossShape& s, const CrossPlan& plan, const float* q, const float* kv, const int32_t* src_len,
+                               float* ctx, float* lse, const CrossParts& parts, hipStream_t st);
+int launch_cross_attention_f32_bwd(const CrossShape& s, const float* q, const float* kv, const int32_t* src_len, const float* ctx,
+                                   const float* dctx, const float* lse, float* dq, float* dkv, float* dvec, hipStream_t st);
 
 }  // namespace moe

@@ -293,6 +293,189 @@ __global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossGeo g, const
   });
 }
 
+// ---------------------------------------------------------------- forward of few columns
+// A block's wavefronts share 32 columns and take blocks of 32 states in turn, each through two places of its own in LDS, one on its
+// way while the other is used: no barrier, 64 KB (d 128) on their way to a compute unit.  Memory bounds it, so the products are
+// not what counts: P keeps its 24 bits as three terms.
+template <int D>
+__global__ __launch_bounds__(256, 1) void cross_few_kernel(CrossGeo g, const bf16_t* __restrict__ q, const bf16_t* __restrict__ kv,
+                                                           const int32_t* __restrict__ src_len, bf16_t* __restrict__ ctx,
+                                                           float* __restrict__ lse, CrossParts parts) {
+  using GM = AttGeom<D>;
+  constexpr int KS = D / 16, DT = D / 32, kHalf = 32 * GM::kRow, kPlace = 2 * kHalf, COPIES = kHalf / 1024;      // K rows, V rows
+  extern __shared__ __attribute__((aligned(256))) unsigned char att_lds[];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)((lds_ptr)att_lds);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 31, hf = lane >> 5;
+  const CrossCols cols(g, D);
+  const int tiles = (cols.count + 31) / 32;
+  unsigned item = xcd_contiguous(blockIdx.x, gridDim.x);
+  const int split = __builtin_amdgcn_readfirstlane(item % parts.splits);
+  item /= parts.splits;
+  const unsigned pair = item / tiles;
+  const int k = __builtin_amdgcn_readfirstlane(pair % g.kv_heads), b = __builtin_amdgcn_readfirstlane(pair / g.kv_heads);
+  const int c = (int)(item % tiles) * 32 + r;
+  const size_t row = cols.base(b, k, D) + cols.offset<D>(cols.within(c));
+  u32x4_t qf[KS];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const u32x4_t*>(q + row + 16 * s + 8 * hf);
+  const int n = held_states(src_len, b, g.Lk), Akv = g.kv_heads * D;
+  const size_t ld = (size_t)2 * Akv;
+  const bf16_t* const keys = kv + (size_t)b * g.Lk * ld + (size_t)k * D;
+  const int nkb = (n + 31) / 32, per = (nkb + parts.splits - 1) / parts.splits;
+  const int from = split * per + wave, to = (split + 1) * per < nkb ? (split + 1) * per : nkb;
+
+  uint32_t off[COPIES];
+#pragma unroll
+  for (int x = 0; x < COPIES; ++x) {
+    const int at = GM::kRowsPerCopy * x + lane / GM::kChunks;
+    off[x] = (uint32_t)(at * ld * 2) + 16 * ((lane % GM::kChunks) ^ att_swizzle<D>(at));
+  }
+  // block kb to place p: K rows, V rows (zeros past the end)
+  auto start = [&](int kb, int p) __attribute__((always_inline)) {
+    const uint32_t at = lds0 + (2 * wave + p) * kPlace;
+    const bf16_t* const src = keys + (size_t)32 * kb * ld;
+    const int rows = n - 32 * kb;
+#pragma unroll
+    for (int x = 0; x < 2 * COPIES; ++x) {
+      const bf16_t* const from_ = x < COPIES ? src : src + Akv;
+      if (rows < 32) {
+        const int i = GM::kRowsPerCopy * (x % COPIES) + lane / GM::kChunks;
+        const uint64_t a = i < rows ? (uint64_t)(uintptr_t)from_ + off[x % COPIES] : (uint64_t)(uintptr_t)&att_zero_line;
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at + x * 1024), "v"(a) : "memory");
+      } else {
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at + x * 1024), "v"(off[x % COPIES]), "s"(from_) : "memory");
+      }
+    }
+  };
+  const float sl2 = 1.4426950408889634f / sqrtf((float)D);
+  const AttReads<D> rd(lds0, lane);
+  f32x16_t o[DT];
+#pragma unroll
+  for (int t = 0; t < DT; ++t) o[t] = f32x16_t{};
+  float m_run = -FLT_MAX, l_run = 0.f;                         // (finite: a block whose scores are all -inf adds nothing)
+  if (from < to) start(from, 0);
+  int p = 0;
+  for (int kb = from; kb < to; kb += 4, p ^= 1) {
+    if (kb + 4 < to) {
+      start(kb + 4, p ^ 1);
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * COPIES) : "memory");
+    } else {
+      wait_all_copies();
+    }
+    const uint32_t place = (2 * wave + p) * kPlace;
+    f32x16_t s;
+#pragma unroll
+    for (int i = 0; i < KS; ++i) s = MOE_MFMA(rd.row(place, 0, i), qf[i], i == 0 ? f32x16_t{} : s);
+    float mx = -INFINITY, psum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      if (32 * kb + 8 * (i >> 2) + 4 * hf + (i & 3) >= n) s[i] = -INFINITY;
+      mx = fmaxf(mx, s[i]);
+    }
+    const float m_new = fmaxf(m_run, fmaxf(mx, __shfl_xor(mx, 32, 64)) * sl2);
+    if (__builtin_amdgcn_ballot_w64(m_new != m_run) != 0) {
+      const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+      l_run *= alpha;
+#pragma unroll
+      for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[t][i] *= alpha;
+      m_run = m_new;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], sl2, -m_run));
+      psum += s[i];
+    }
+    l_run += psum + __shfl_xor(psum, 32, 64);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      bf16x8_bits_t pf[3];
+      split_bf16x8(s, 8 * h, pf);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const u32x4_t vt = rd.transposed(place + kHalf, 16 * h, dt);
+#pragma unroll
+        for (int x = 2; x >= 0; --x) o[dt] = MOE_MFMA(vt, pf[x], o[dt]);
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // the place is read before the next copies go there
+  }
+  // To the wavefronts' common maximum; then each adds up 32 values of d.  LDS: [wavefront][DT][16][64] and the statistics behind
+  typedef float __attribute__((address_space(3))) * lds_f_ptr;
+  constexpr uint32_t kStats = 4 * DT * 16 * 64 * 4;
+  __syncthreads();
+  auto at = [&](uint32_t byte) __attribute__((always_inline)) { return (lds_f_ptr)(uintptr_t)(lds0 + byte); };
+  *at(kStats + (wave * 64 + lane) * 4) = m_run;
+  *at(kStats + 1024 + (wave * 64 + lane) * 4) = l_run;
+  __syncthreads();
+  float m = m_run, l = 0.f;
+#pragma unroll
+  for (int x = 0; x < 4; ++x) m = fmaxf(m, *at(kStats + (x * 64 + lane) * 4));
+#pragma unroll
+  for (int x = 0; x < 4; ++x) l += *at(kStats + 1024 + (x * 64 + lane) * 4) * __builtin_amdgcn_exp2f(*at(kStats + (x * 64 + lane) * 4) - m);
+  const float alpha = __builtin_amdgcn_exp2f(m_run - m);       // (a wavefront without a block: sums of 0)
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) *at(((wave * DT + t) * 16 + i) * 256 + lane * 4) = o[t][i] * alpha;
+  __syncthreads();
+  if (wave >= DT || c >= cols.count) return;
+  float v[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    v[i] = 0.f;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) v[i] += *at(((x * DT + wave) * 16 + i) * 256 + lane * 4);
+  }
+  // v[i]: d = 32 wave + 8 (i/4) + 4 hf + i%4 of column c
+  const size_t column = ((size_t)b * g.kv_heads + k) * cols.count + c;
+  if (parts.splits > 1) {
+    if (wave == 0 && hf == 0) parts.stats[column * parts.splits + split] = float2{m, l};
+    float* const to_ = parts.sums + (column * parts.splits + split) * D + 32 * wave + 4 * hf;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) *reinterpret_cast<f32x4_t*>(to_ + 8 * x) = f32x4_t{v[4 * x], v[4 * x + 1], v[4 * x + 2], v[4 * x + 3]};
+    return;
+  }
+  if (lse != nullptr && wave == 0 && hf == 0) lse[column] = n == 0 ? 0.f : (m + log2f(l)) * 0.6931471805599453f;
+  const float inv = n == 0 ? 0.f : 1.0f / l;
+#pragma unroll
+  for (int x = 0; x < 4; ++x)
+    *reinterpret_cast<u32x2_t*>(ctx + row + 32 * wave + 8 * x + 4 * hf) =
+        u32x2_t{pack_bf16x2(v[4 * x] * inv, v[4 * x + 1] * inv), pack_bf16x2(v[4 * x + 2] * inv, v[4 * x + 3] * inv)};
+}
+
+// The ranges of a column put together: a wavefront a column, lanes over the ranges (64 at most), then over d.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void cross_join_kernel(CrossGeo g, CrossParts parts, const int32_t* __restrict__ src_len, T* __restrict__ ctx,
+                                                         float* __restrict__ lse, long long columns) {
+  constexpr bool F32 = sizeof(T) == 4;                         // (units of the maxima)
+  const int lane = threadIdx.x & 63;
+  const long long column = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (column >= columns) return;
+  const CrossCols cols(g, D);
+  const long long pair = column / cols.count, b = pair / g.kv_heads;
+  const int c = (int)(column - pair * cols.count), k = (int)(pair - b * g.kv_heads);
+  const float2 st = lane < parts.splits ? parts.stats[column * parts.splits + lane] : float2{-FLT_MAX, 0.f};
+  const float m = wave_max(st.x);
+  const float f = F32 ? expf(st.x - m) : __builtin_amdgcn_exp2f(st.x - m);
+  const float l = wave_sum(st.y * f);
+  float v[D / 64] = {};
+  const float* const sums = parts.sums + column * parts.splits * D + lane * (D / 64);
+  for (int s = 0; s < parts.splits; ++s) {
+    const float w = __shfl(f, s, 64);
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) v[i] = fmaf(sums[(size_t)s * D + i], w, v[i]);
+  }
+  const bool none = held_states(src_len, b, g.Lk) == 0;
+  if (lse != nullptr && lane == 0) lse[column] = none ? 0.f : F32 ? m + logf(l) : (m + log2f(l)) * 0.6931471805599453f;
+  const float inv = none ? 0.f : 1.0f / l;
+  T* const to = ctx + cols.base(b, k, D) + cols.offset<D>(c) + lane * (D / 64);
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) Elt<T>::store(to + i, v[i] * inv);
+}
+
 // ---------------------------------------------------------------- dq (and D)
 template <int D>
 __global__ __launch_bounds__(256, 2) void cross_dq_kernel(CrossGeo g, const bf16_t* __restrict__ q, const bf16_t* __restrict__ kv,
@@ -654,14 +837,17 @@ __global__ __launch_bounds__(256, 1) void cross_dkv_kernel(CrossGeo g, const bf1
   store_rows<D, CT>(dv, 1.f, lds0 + own, lane, put(dkv + states + Akv));
 }
 
+template <int D> constexpr int kLdsFew = 4 * 2 * 64 * AttGeom<D>::kRow;        // (the wavefronts' sums and statistics: 4 D 32 4 + 2048)
 template <int D> constexpr int kLdsForward = 4 * AttGeom<D>::kBlock;
 template <int D> constexpr int kLdsQ = 5 * AttGeom<D>::kBlock;
 template <int D, int CT> constexpr int kLdsKV = 2 * (2 * AttGeom<D>::kBlock + 512) + 128 * CT * AttGeom<D>::kRow;
 
 template <int D>
 int prepare_kernels() {
-  static LdsLimitOnce once, once_q, once_kv1, once_kv2;
+  static LdsLimitOnce once, once_few, once_q, once_kv1, once_kv2;
+  static_assert(kLdsFew<D> >= 4 * D * 32 * 4 + 2048);
   int rc = ensure_lds_limit(once, reinterpret_cast<const void*>(cross_forward_kernel<D>), kLdsForward<D>);
+  if (rc == MOE_OK) rc = ensure_lds_limit(once_few, reinterpret_cast<const void*>(cross_few_kernel<D>), kLdsFew<D>);
   if (rc == MOE_OK) rc = ensure_lds_limit(once_q, reinterpret_cast<const void*>(cross_dq_kernel<D>), kLdsQ<D>);
   if (rc == MOE_OK) rc = ensure_lds_limit(once_kv1, reinterpret_cast<const void*>(cross_dkv_kernel<D, 1>), (kLdsKV<D, 1>));
   if constexpr (D == 128)
@@ -670,11 +856,22 @@ int prepare_kernels() {
 }
 
 template <int D>
-int forward(const CrossShape& s, const bf16_t* q, const bf16_t* kv, const int32_t* src_len, bf16_t* ctx, float* lse, hipStream_t st) {
+int forward(const CrossShape& s, const CrossPlan& plan, const bf16_t* q, const bf16_t* kv, const int32_t* src_len, bf16_t* ctx, float* lse,
+            const CrossParts& parts, hipStream_t st) {
   if (prepare_kernels<D>() != MOE_OK) return MOE_EHIP;
-  const long long blocks = s.B * s.kv_heads * ((s.columns() + 127) / 128);
+  const int per = plan.few ? 32 : 128;
+  const long long blocks = s.B * s.kv_heads * ((s.columns() + per - 1) / per) * plan.splits;
   if (blocks > 0x7fffffffLL) return MOE_EUNSUPPORTED;
-  hipLaunchKernelGGL((cross_forward_kernel<D>), dim3((unsigned)blocks), dim3(256), kLdsForward<D>, st, CrossGeo(s), q, kv, src_len, ctx, lse);
+  if (plan.few) hipLaunchKernelGGL((cross_few_kernel<D>), dim3((unsigned)blocks), dim3(256), kLdsFew<D>, st, CrossGeo(s), q, kv, src_len, ctx, lse, parts);
+  else hipLaunchKernelGGL((cross_forward_kernel<D>), dim3((unsigned)blocks), dim3(256), kLdsForward<D>, st, CrossGeo(s), q, kv, src_len, ctx, lse);
+  return check_launch();
+}
+template <typename T>
+int join(const CrossShape& s, const CrossParts& parts, const int32_t* src_len, T* ctx, float* lse, hipStream_t st) {
+  const long long columns = s.B * s.kv_heads * s.columns();
+  const dim3 grid((unsigned)((columns + 3) / 4)), threads(256);
+  if (s.d == 64) hipLaunchKernelGGL((cross_join_kernel<T, 64>), grid, threads, 0, st, CrossGeo(s), parts, src_len, ctx, lse, columns);
+  else hipLaunchKernelGGL((cross_join_kernel<T, 128>), grid, threads, 0, st, CrossGeo(s), parts, src_len, ctx, lse, columns);
   return check_launch();
 }
 template <int D>
@@ -714,20 +911,51 @@ int prepare_cross_attention() {
   return rc != MOE_OK ? rc : prepare_kernels<128>();
 }
 
-size_t cross_scratch_bytes(int, const CrossShape&) { return 0; }
+// Few columns: up to 32 of them (a block of 128 would have one wavefront multiply and three stage).  Their states are cut into ranges until
+// every compute unit has work, a block of states for every wavefront at least.
+CrossPlan cross_plan(int act_dtype, const CrossShape& s) {
+  constexpr int kUnits = 256;                                  // of a whole device: the choice sizes a workspace
+  const int tiles = (s.columns() + 31) / 32, blocks = (s.Lk + 31) / 32;
+  const long long items = s.B * s.kv_heads * tiles;
+  bool few = s.columns() <= 32;
+  if (act_dtype == MOE_F32) few = few || (items <= 1024 && (double)((items + kUnits - 1) / kUnits) * ((blocks + 3) / 4 + 0.5) < blocks);
+  if (!few) return {false, 1};
+  const long long at_once = s.d == 64 ? 2 * kUnits : kUnits;
+  long long splits = at_once / items, most = (blocks + 3) / 4;
+  if (splits > most) splits = most;
+  if (splits > 64) splits = 64;
+  return {true, splits < 1 ? 1 : (int)splits};
+}
+
+size_t cross_scratch_bytes(int act_dtype, const CrossShape& s) {
+  const CrossPlan p = cross_plan(act_dtype, s);
+  const size_t columns = (size_t)s.B * s.kv_heads * s.columns();
+  return p.splits > 1 ? align_up(columns * p.splits * sizeof(float2), 256) + columns * p.splits * s.d * sizeof(float) : 0;
+}
 
 int launch_cross_attention(int act_dtype, const CrossShape& s, const void* q, const void* kv, const int32_t* src_len, void* ctx,
                            float* lse, void* scratch, hipStream_t st) {
-  if (act_dtype == MOE_F32) return launch_cross_attention_f32(s, q, kv, src_len, ctx, lse, scratch, st);
+  const CrossPlan plan = cross_plan(act_dtype, s);
+  const size_t columns = (size_t)s.B * s.kv_heads * s.columns();
+  const CrossParts parts{plan.splits, static_cast<float2*>(scratch),
+                         reinterpret_cast<float*>(static_cast<char*>(scratch) + align_up(columns * plan.splits * sizeof(float2), 256))};
+  if (act_dtype == MOE_F32) {
+    float* const c = static_cast<float*>(ctx);
+    const int rc = launch_cross_attention_f32(s, plan, static_cast<const float*>(q), static_cast<const float*>(kv), src_len, c, lse, parts, st);
+    return rc != MOE_OK || plan.splits == 1 ? rc : join(s, parts, src_len, c, lse, st);
+  }
   auto qb = static_cast<const bf16_t*>(q);
   auto kb = static_cast<const bf16_t*>(kv);
   auto c = static_cast<bf16_t*>(ctx);
-  return s.d == 64 ? forward<64>(s, qb, kb, src_len, c, lse, st) : forward<128>(s, qb, kb, src_len, c, lse, st);
+  const int rc = s.d == 64 ? forward<64>(s, plan, qb, kb, src_len, c, lse, parts, st) : forward<128>(s, plan, qb, kb, src_len, c, lse, parts, st);
+  return rc != MOE_OK || plan.splits == 1 ? rc : join(s, parts, src_len, c, lse, st);
 }
 
 int launch_cross_attention_bwd(int act_dtype, const CrossShape& s, const void* q, const void* kv, const int32_t* src_len,
                                const void* ctx, const void* dctx, const float* lse, void* dq, void* dkv, float* dvec, hipStream_t st) {
-  if (act_dtype == MOE_F32) return launch_cross_attention_f32_bwd(s, q, kv, src_len, ctx, dctx, lse, dq, dkv, dvec, st);
+  if (act_dtype == MOE_F32)
+    return launch_cross_attention_f32_bwd(s, static_cast<const float*>(q), static_cast<const float*>(kv), src_len, static_cast<const float*>(ctx),
+                                          static_cast<const float*>(dctx), lse, static_cast<float*>(dq), static_cast<float*>(dkv), dvec, st);
   auto qb = static_cast<const bf16_t*>(q);
   auto kb = static_cast<const bf16_t*>(kv);
   auto c = static_cast<const bf16_t*>(ctx);

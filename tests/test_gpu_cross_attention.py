@@ -62,7 +62,9 @@ CASES = [(1, 1, 1, 1, 1, 64, None), (6, 1, 1, 2, 2, 128, "ends"), (6, 3, 64, 2, 
          (6, 31, 129, 4, 1, 64, "ends"), (3, 128, 128, 2, 2, 128, None), (2, 129, 63, 8, 1, 128, "any"), (3, 200, 300, 4, 2, 64, "any"),
          (1, 300, 1000, 2, 2, 128, "any"), (5, 64, 257, 4, 4, 64, None), (2, 1, 4100, 2, 2, 128, "any"), (9, 5, 700, 16, 2, 64, "any"),
          (2, 1, 333, 32, 1, 64, "any"), (1, 515, 77, 2, 2, 64, None), (1, 1, 2000, 1, 1, 128, None), (40, 2, 190, 3, 3, 64, "any"),
-         (130, 130, 70, 2, 2, 128, "any")]
+         (130, 130, 70, 2, 2, 128, "any"),
+         # two tiles of states a wavefront backward; as many ranges of states as there are; ranges, some of which a short source leaves empty
+         (40, 70, 200, 8, 8, 128, "any"), (1, 2, 8200, 1, 1, 64, None), (6, 4, 2500, 1, 1, 128, "ends"), (70, 31, 33, 4, 4, 128, "any")]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
