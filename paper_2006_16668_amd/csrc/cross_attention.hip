@@ -297,12 +297,13 @@ __global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossGeo g, const
 // A block's wavefronts share 32 columns and take blocks of 32 states in turn, each through two places of its own in LDS, one on its
 // way while the other is used: no barrier, 64 KB (d 128) on their way to a compute unit.  Memory bounds it, so the products are
 // not what counts: P keeps its 24 bits as three terms.
+constexpr int kFewWaves = 4;
 template <int D>
-__global__ __launch_bounds__(256, 1) void cross_few_kernel(CrossGeo g, const bf16_t* __restrict__ q, const bf16_t* __restrict__ kv,
+__global__ __launch_bounds__(64 * kFewWaves, 1) void cross_few_kernel(CrossGeo g, const bf16_t* __restrict__ q, const bf16_t* __restrict__ kv,
                                                            const int32_t* __restrict__ src_len, bf16_t* __restrict__ ctx,
                                                            float* __restrict__ lse, CrossParts parts) {
   using GM = AttGeom<D>;
-  constexpr int KS = D / 16, DT = D / 32, kHalf = 32 * GM::kRow, kPlace = 2 * kHalf, COPIES = kHalf / 1024;      // K rows, V rows
+  constexpr int W = kFewWaves, KS = D / 16, DT = D / 32, kHalf = 32 * GM::kRow, kPlace = 2 * kHalf, COPIES = kHalf / 1024;      // K rows, V rows
   extern __shared__ __attribute__((aligned(256))) unsigned char att_lds[];
   const uint32_t lds0 = (uint32_t)(uintptr_t)((lds_ptr)att_lds);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -356,9 +357,9 @@ __global__ __launch_bounds__(256, 1) void cross_few_kernel(CrossGeo g, const bf1
   float m_run = -FLT_MAX, l_run = 0.f;                         // (finite: a block whose scores are all -inf adds nothing)
   if (from < to) start(from, 0);
   int p = 0;
-  for (int kb = from; kb < to; kb += 4, p ^= 1) {
-    if (kb + 4 < to) {
-      start(kb + 4, p ^ 1);
+  for (int kb = from; kb < to; kb += W, p ^= 1) {
+    if (kb + W < to) {
+      start(kb + W, p ^ 1);
       asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * COPIES) : "memory");
     } else {
       wait_all_copies();
@@ -404,46 +405,50 @@ __global__ __launch_bounds__(256, 1) void cross_few_kernel(CrossGeo g, const bf1
   }
   // To the wavefronts' common maximum; then each adds up 32 values of d.  LDS: [wavefront][DT][16][64] and the statistics behind
   typedef float __attribute__((address_space(3))) * lds_f_ptr;
-  constexpr uint32_t kStats = 4 * DT * 16 * 64 * 4;
+  constexpr uint32_t kStats = W * DT * 16 * 64 * 4;
   __syncthreads();
   auto at = [&](uint32_t byte) __attribute__((always_inline)) { return (lds_f_ptr)(uintptr_t)(lds0 + byte); };
   *at(kStats + (wave * 64 + lane) * 4) = m_run;
-  *at(kStats + 1024 + (wave * 64 + lane) * 4) = l_run;
+  *at(kStats + 256 * W + (wave * 64 + lane) * 4) = l_run;
   __syncthreads();
   float m = m_run, l = 0.f;
 #pragma unroll
-  for (int x = 0; x < 4; ++x) m = fmaxf(m, *at(kStats + (x * 64 + lane) * 4));
+  for (int x = 0; x < W; ++x) m = fmaxf(m, *at(kStats + (x * 64 + lane) * 4));
 #pragma unroll
-  for (int x = 0; x < 4; ++x) l += *at(kStats + 1024 + (x * 64 + lane) * 4) * __builtin_amdgcn_exp2f(*at(kStats + (x * 64 + lane) * 4) - m);
+  for (int x = 0; x < W; ++x) l += *at(kStats + 256 * W + (x * 64 + lane) * 4) * __builtin_amdgcn_exp2f(*at(kStats + (x * 64 + lane) * 4) - m);
   const float alpha = __builtin_amdgcn_exp2f(m_run - m);       // (a wavefront without a block: sums of 0)
 #pragma unroll
   for (int t = 0; t < DT; ++t)
 #pragma unroll
     for (int i = 0; i < 16; ++i) *at(((wave * DT + t) * 16 + i) * 256 + lane * 4) = o[t][i] * alpha;
   __syncthreads();
-  if (wave >= DT || c >= cols.count) return;
-  float v[16];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    v[i] = 0.f;
-#pragma unroll
-    for (int x = 0; x < 4; ++x) v[i] += *at(((x * DT + wave) * 16 + i) * 256 + lane * 4);
-  }
-  // v[i]: d = 32 wave + 8 (i/4) + 4 hf + i%4 of column c
+  if (c >= cols.count) return;
   const size_t column = ((size_t)b * g.kv_heads + k) * cols.count + c;
-  if (parts.splits > 1) {
-    if (wave == 0 && hf == 0) parts.stats[column * parts.splits + split] = float2{m, l};
-    float* const to_ = parts.sums + (column * parts.splits + split) * D + 32 * wave + 4 * hf;
-#pragma unroll
-    for (int x = 0; x < 4; ++x) *reinterpret_cast<f32x4_t*>(to_ + 8 * x) = f32x4_t{v[4 * x], v[4 * x + 1], v[4 * x + 2], v[4 * x + 3]};
-    return;
+  if (wave == 0 && hf == 0) {
+    if (parts.splits > 1) parts.stats[column * parts.splits + split] = float2{m, l};
+    else if (lse != nullptr) lse[column] = n == 0 ? 0.f : (m + log2f(l)) * 0.6931471805599453f;
   }
-  if (lse != nullptr && wave == 0 && hf == 0) lse[column] = n == 0 ? 0.f : (m + log2f(l)) * 0.6931471805599453f;
   const float inv = n == 0 ? 0.f : 1.0f / l;
 #pragma unroll
-  for (int x = 0; x < 4; ++x)
-    *reinterpret_cast<u32x2_t*>(ctx + row + 32 * wave + 8 * x + 4 * hf) =
-        u32x2_t{pack_bf16x2(v[4 * x] * inv, v[4 * x + 1] * inv), pack_bf16x2(v[4 * x + 2] * inv, v[4 * x + 3] * inv)};
+  for (int dt = wave; dt < DT; dt += W) {
+    float v[16];                                               // d = 32 dt + 8 (i/4) + 4 hf + i%4 of column c
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      v[i] = 0.f;
+#pragma unroll
+      for (int x = 0; x < W; ++x) v[i] += *at(((x * DT + dt) * 16 + i) * 256 + lane * 4);
+    }
+    if (parts.splits > 1) {
+      float* const to_ = parts.sums + (column * parts.splits + split) * D + 32 * dt + 4 * hf;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) *reinterpret_cast<f32x4_t*>(to_ + 8 * x) = f32x4_t{v[4 * x], v[4 * x + 1], v[4 * x + 2], v[4 * x + 3]};
+    } else {
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        *reinterpret_cast<u32x2_t*>(ctx + row + 32 * dt + 8 * x + 4 * hf) =
+            u32x2_t{pack_bf16x2(v[4 * x] * inv, v[4 * x + 1] * inv), pack_bf16x2(v[4 * x + 2] * inv, v[4 * x + 3] * inv)};
+    }
+  }
 }
 
 // The ranges of a column put together: a wavefront a column, lanes over the ranges (64 at most), then over d.
@@ -463,10 +468,16 @@ __global__ __launch_bounds__(256) void cross_join_kernel(CrossGeo g, CrossParts 
   const float l = wave_sum(st.y * f);
   float v[D / 64] = {};
   const float* const sums = parts.sums + column * parts.splits * D + lane * (D / 64);
-  for (int s = 0; s < parts.splits; ++s) {
-    const float w = __shfl(f, s, 64);
+  for (int s = 0; s < parts.splits; s += 8) {                  // eight on their way at a time
+    float x[8][D / 64];
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) v[i] = fmaf(sums[(size_t)s * D + i], w, v[i]);
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) x[j][i] = s + j < parts.splits ? sums[(size_t)(s + j) * D + i] : 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) v[i] = fmaf(x[j][i], __shfl(f, s + j, 64), v[i]);
   }
   const bool none = held_states(src_len, b, g.Lk) == 0;
   if (lse != nullptr && lane == 0) lse[column] = none ? 0.f : F32 ? m + logf(l) : (m + log2f(l)) * 0.6931471805599453f;
@@ -837,7 +848,7 @@ __global__ __launch_bounds__(256, 1) void cross_dkv_kernel(CrossGeo g, const bf1
   store_rows<D, CT>(dv, 1.f, lds0 + own, lane, put(dkv + states + Akv));
 }
 
-template <int D> constexpr int kLdsFew = 4 * 2 * 64 * AttGeom<D>::kRow;        // (the wavefronts' sums and statistics: 4 D 32 4 + 2048)
+template <int D> constexpr int kLdsFew = kFewWaves * 2 * 64 * AttGeom<D>::kRow;
 template <int D> constexpr int kLdsForward = 4 * AttGeom<D>::kBlock;
 template <int D> constexpr int kLdsQ = 5 * AttGeom<D>::kBlock;
 template <int D, int CT> constexpr int kLdsKV = 2 * (2 * AttGeom<D>::kBlock + 512) + 128 * CT * AttGeom<D>::kRow;
@@ -845,7 +856,7 @@ template <int D, int CT> constexpr int kLdsKV = 2 * (2 * AttGeom<D>::kBlock + 51
 template <int D>
 int prepare_kernels() {
   static LdsLimitOnce once, once_few, once_q, once_kv1, once_kv2;
-  static_assert(kLdsFew<D> >= 4 * D * 32 * 4 + 2048);
+  static_assert(kLdsFew<D> >= kFewWaves * (128 * D + 512), "the wavefronts' sums and statistics");
   int rc = ensure_lds_limit(once, reinterpret_cast<const void*>(cross_forward_kernel<D>), kLdsForward<D>);
   if (rc == MOE_OK) rc = ensure_lds_limit(once_few, reinterpret_cast<const void*>(cross_few_kernel<D>), kLdsFew<D>);
   if (rc == MOE_OK) rc = ensure_lds_limit(once_q, reinterpret_cast<const void*>(cross_dq_kernel<D>), kLdsQ<D>);
@@ -862,8 +873,10 @@ int forward(const CrossShape& s, const CrossPlan& plan, const bf16_t* q, const b
   const int per = plan.few ? 32 : 128;
   const long long blocks = s.B * s.kv_heads * ((s.columns() + per - 1) / per) * plan.splits;
   if (blocks > 0x7fffffffLL) return MOE_EUNSUPPORTED;
-  if (plan.few) hipLaunchKernelGGL((cross_few_kernel<D>), dim3((unsigned)blocks), dim3(256), kLdsFew<D>, st, CrossGeo(s), q, kv, src_len, ctx, lse, parts);
-  else hipLaunchKernelGGL((cross_forward_kernel<D>), dim3((unsigned)blocks), dim3(256), kLdsForward<D>, st, CrossGeo(s), q, kv, src_len, ctx, lse);
+  const CrossGeo g(s);
+  const dim3 grid((unsigned)blocks);
+  if (plan.few) hipLaunchKernelGGL((cross_few_kernel<D>), grid, dim3(64 * kFewWaves), kLdsFew<D>, st, g, q, kv, src_len, ctx, lse, parts);
+  else hipLaunchKernelGGL((cross_forward_kernel<D>), grid, dim3(256), kLdsForward<D>, st, g, q, kv, src_len, ctx, lse);
   return check_launch();
 }
 template <typename T>
@@ -911,20 +924,31 @@ int prepare_cross_attention() {
   return rc != MOE_OK ? rc : prepare_kernels<128>();
 }
 
-// Few columns: up to 32 of them (a block of 128 would have one wavefront multiply and three stage).  Their states are cut into ranges until
-// every compute unit has work, a block of states for every wavefront at least.
+// Which form a forward call takes, by what both are expected to take (us).  A block of 128 columns walks its states in steps, two blocks on a unit
+// (fp32: one at a time multiplies); one of 32 columns shares them among its wavefronts and `splits` blocks, which cost a launch to join and
+// bring only as much memory as they have units.  Source by source measured (bf16, d 128 unless said; 128 / 32 columns in the
+// best number of ranges): 64 x 1 token, 410 to 2048 states, 16 heads 120 / 128; 1 x 4, 53 5.0 / 6.1; 1 x 1, 1000 23.7 / 11.1 (8);
+// 1 x 1, 8000 155 / 24.5 (16); 8 x 1, 1000 23.1 / 19.1 (2); 4 x 8, 4000, 2 key heads 82 / 17.0 (16); 16 x 1, 2000, 8 heads of 64 28.1 / 16.4 (4).
 CrossPlan cross_plan(int act_dtype, const CrossShape& s) {
-  constexpr int kUnits = 256;                                  // of a whole device: the choice sizes a workspace
-  const int tiles = (s.columns() + 31) / 32, blocks = (s.Lk + 31) / 32;
-  const long long items = s.B * s.kv_heads * tiles;
-  bool few = s.columns() <= 32;
-  if (act_dtype == MOE_F32) few = few || (items <= 1024 && (double)((items + kUnits - 1) / kUnits) * ((blocks + 3) / 4 + 0.5) < blocks);
-  if (!few) return {false, 1};
-  const long long at_once = s.d == 64 ? 2 * kUnits : kUnits;
-  long long splits = at_once / items, most = (blocks + 3) / 4;
-  if (splits > most) splits = most;
-  if (splits > 64) splits = 64;
-  return {true, splits < 1 ? 1 : (int)splits};
+  constexpr double kUnits = 256;                               // of a whole device: the choice sizes a workspace
+  const bool f32 = act_dtype == MOE_F32;
+  const double pairs = (double)s.B * s.kv_heads, mb = pairs * s.Lk * 2 * s.d * (f32 ? 4 : 2) / 1e6;
+  const double step128 = f32 ? (s.d == 64 ? 3.5 : 7.0) : (s.d == 64 ? 0.75 : 1.2), step32 = f32 ? step128 : 0.75;
+  const int blocks = (s.Lk + 31) / 32;
+  auto rounds = [](double n, double at_once) { return ceil(n / at_once); };
+  auto longer = [](double a, double b) { return a > b ? a : b; };
+  CrossPlan best{false, 1};
+  double least = 4 + longer(step128 * (f32 ? blocks : (blocks + 1) / 2) * rounds(pairs * ((s.columns() + 127) / 128), f32 ? kUnits : 2 * kUnits), mb / 5.0);
+  for (int splits = 1; splits <= 64 && splits <= (blocks + 3) / 4; splits *= 2) {
+    const double items = pairs * ((s.columns() + 31) / 32) * splits, at_once = !f32 && s.d == 64 ? 2 * kUnits : kUnits;
+    const double us = 6 + (splits > 1 ? 4 : 0) + longer(step32 * ((blocks + 4 * splits - 1) / (4 * splits)) * rounds(items, at_once),
+                                                       mb / 5.0 * (items < kUnits ? kUnits / items : 1.0));
+    if (us < least) {
+      least = us;
+      best = {true, splits};
+    }
+  }
+  return best;
 }
 
 size_t cross_scratch_bytes(int act_dtype, const CrossShape& s) {
