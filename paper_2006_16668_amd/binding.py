@@ -775,6 +775,45 @@ def moe_vocab_distill_backward(shape: MoEShape, dims: VocabDims, x, w, teacher_i
 
 
 # ---- the decoder's attention to the encoder
+def _here():
+    """The current device, on which the kernels run."""
+    try:
+        return torch._C._cuda_getDevice()
+    except (AttributeError, RuntimeError):
+        return -2                                               # (without a GPU no tensor is on it)
+
+
+def _at(t, dtype, shape, name, here):
+    """The address of a tensor that must be there, on the current device, of this type and shape and contiguous.  One pass where it is, 0.4 us
+    instead of the 0.7 of _given and _ptr: a call of a few microseconds has up to fifteen."""
+    try:
+        if t.dtype is dtype and t.get_device() == here and t.shape == shape and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _given(name, t)
+    return _ptr(t, dtype, shape, name)
+
+
+def _stream_of(here):
+    return torch._C._cuda_getCurrentRawStream(here)
+
+
+def _room(ws, name, here):
+    try:
+        if ws.dtype is torch.uint8 and ws.get_device() == here and ws.is_contiguous():
+            return ws.data_ptr(), ws.numel()
+    except AttributeError:
+        pass
+    _given(name, ws)
+    return _ws(ws, name)
+
+
+def _run(status, where):
+    if status != 0:
+        raise MoEError(status, where)
+
+
 def moe_cross_workspace_bytes(shape: MoEShape, dims: CrossDims) -> int:
     return _ws_query("moe_cross_workspace_bytes", shape, dims)
 
@@ -789,25 +828,21 @@ def moe_cross_backward_workspace_bytes(shape: MoEShape, dims: CrossDims) -> int:
 
 def moe_cross_keys(shape: MoEShape, dims: CrossDims, mem, wkv, kv):
     """kv [B,Lk,2 Akv] = mem [B,Lk,M] . wkv [M,2 Akv], keys in the first Akv columns, values in the others."""
-    _given("mem wkv kv", mem, wkv, kv)
-    M, dt, W = shape.M, shape.torch_dtype, 2 * dims.key_heads * dims.d
+    M, dt, W, here = shape.M, shape.torch_dtype, 2 * dims.key_heads * dims.d, _here()
     c, d = shape._c(), dims._c()
-    _check(load_library().moe_cross_keys(
-        ctypes.byref(c), ctypes.byref(d), _ptr(mem, dt, (dims.B, dims.Lk, M), "mem"), _ptr(wkv, dt, (M, W), "wkv"),
-        _ptr(kv, dt, (dims.B, dims.Lk, W), "kv"), _stream()), "moe_cross_keys")
+    _run(load_library().moe_cross_keys(
+        ctypes.byref(c), ctypes.byref(d), _at(mem, dt, (dims.B, dims.Lk, M), "mem", here), _at(wkv, dt, (M, W), "wkv", here),
+        _at(kv, dt, (dims.B, dims.Lk, W), "kv", here), _stream_of(here)), "moe_cross_keys")
 
 
 def _cross_forward(fn_name, shape, dims, u, kv, src_len, wq, wo, out, ws):
-    _given("u kv wq wo out ws", u, kv, wq, wo, out, ws)
-    if src_len is not None:
-        _given("src_len", src_len)
-    G, S, M, dt, A = shape.G, shape.S, shape.M, shape.torch_dtype, dims.heads * dims.d
+    M, dt, A, here = shape.M, shape.torch_dtype, dims.heads * dims.d, _here()
+    tokens = (shape.G, shape.S, M)
     c, d = shape._c(), dims._c()
-    wsp, wsn = _ws(ws)
-    _check(getattr(load_library(), fn_name)(
-        ctypes.byref(c), ctypes.byref(d), _ptr(u, dt, (G, S, M), "u"), _ptr(kv, dt, (dims.B, dims.Lk, 2 * dims.key_heads * dims.d), "kv"),
-        _ptr(src_len, torch.int32, (dims.B,), "src_len"), _ptr(wq, dt, (M, A), "wq"), _ptr(wo, dt, (A, M), "wo"),
-        _ptr(out, dt, (G, S, M), "out"), wsp, wsn, _stream()), fn_name)
+    u, kv = _at(u, dt, tokens, "u", here), _at(kv, dt, (dims.B, dims.Lk, 2 * dims.key_heads * dims.d), "kv", here)
+    src_len = None if src_len is None else _at(src_len, torch.int32, (dims.B,), "src_len", here)
+    wq, wo, out = _at(wq, dt, (M, A), "wq", here), _at(wo, dt, (A, M), "wo", here), _at(out, dt, tokens, "out", here)
+    _run(getattr(load_library(), fn_name)(ctypes.byref(c), ctypes.byref(d), u, kv, src_len, wq, wo, out, *_room(ws, "ws", here), _stream_of(here)), fn_name)
 
 
 def moe_cross_attention(shape: MoEShape, dims: CrossDims, u, kv, src_len, wq, wo, out, ws):
@@ -822,74 +857,61 @@ def moe_cross_attention_train(shape: MoEShape, dims: CrossDims, u, kv, src_len, 
 
 def moe_cross_attention_backward(shape: MoEShape, dims: CrossDims, u, mem, kv, src_len, wq, wkv, wo, dout, fwd_ws, grads: dict, ws):
     """grads: a dict of output tensors du, dmem, dwq, dwkv, dwo of the shapes of u, mem, wq, wkv, wo."""
-    du, dmem, dwq, dwkv, dwo = (grads[k] for k in ("du", "dmem", "dwq", "dwkv", "dwo"))
-    _given("u mem kv wq wkv wo dout fwd_ws du dmem dwq dwkv dwo ws", u, mem, kv, wq, wkv, wo, dout, fwd_ws, du, dmem, dwq, dwkv, dwo, ws)
-    if src_len is not None:
-        _given("src_len", src_len)
-    G, S, M, dt, A, W = shape.G, shape.S, shape.M, shape.torch_dtype, dims.heads * dims.d, 2 * dims.key_heads * dims.d
+    M, dt, A, W, here = shape.M, shape.torch_dtype, dims.heads * dims.d, 2 * dims.key_heads * dims.d, _here()
+    tokens, states = (shape.G, shape.S, M), (dims.B, dims.Lk, M)
     c, d = shape._c(), dims._c()
-    fwp, fwn = _ws(fwd_ws, "fwd_ws")
-    wsp, wsn = _ws(ws)
-    rows = (dims.B, dims.Lk)
-    _check(load_library().moe_cross_attention_backward(
-        ctypes.byref(c), ctypes.byref(d), _ptr(u, dt, (G, S, M), "u"), _ptr(mem, dt, (*rows, M), "mem"), _ptr(kv, dt, (*rows, W), "kv"),
-        _ptr(src_len, torch.int32, (dims.B,), "src_len"), _ptr(wq, dt, (M, A), "wq"), _ptr(wkv, dt, (M, W), "wkv"),
-        _ptr(wo, dt, (A, M), "wo"), _ptr(dout, dt, (G, S, M), "dout"), fwp, fwn, _ptr(du, dt, (G, S, M), "du"),
-        _ptr(dmem, dt, (*rows, M), "dmem"), _ptr(dwq, dt, (M, A), "dwq"), _ptr(dwkv, dt, (M, W), "dwkv"), _ptr(dwo, dt, (A, M), "dwo"),
-        wsp, wsn, _stream()), "moe_cross_attention_backward")
+    at = lambda t, s, name: _at(t, dt, s, name, here)
+    args = (at(u, tokens, "u"), at(mem, states, "mem"), at(kv, (dims.B, dims.Lk, W), "kv"),
+            None if src_len is None else _at(src_len, torch.int32, (dims.B,), "src_len", here),
+            at(wq, (M, A), "wq"), at(wkv, (M, W), "wkv"), at(wo, (A, M), "wo"), at(dout, tokens, "dout"), *_room(fwd_ws, "fwd_ws", here),
+            at(grads["du"], tokens, "du"), at(grads["dmem"], states, "dmem"), at(grads["dwq"], (M, A), "dwq"),
+            at(grads["dwkv"], (M, W), "dwkv"), at(grads["dwo"], (A, M), "dwo"), *_room(ws, "ws", here))
+    _run(load_library().moe_cross_attention_backward(ctypes.byref(c), ctypes.byref(d), *args, _stream_of(here)), "moe_cross_attention_backward")
 
 
 # ---- losses of preference and policy
 def moe_preference_loss(shape: MoEShape, dims: PreferenceDims, nll, ref_nll, target, start, loss, ratio):
     """Loss [P] of pairs of sequences (tokens start[i] .. start[i + 1] - 1) and their log-ratios [2P], from token losses [G,S]."""
-    _given("nll ref_nll target start loss ratio", nll, ref_nll, target, start, loss, ratio)
-    t, f32, i32 = (shape.G, shape.S), torch.float32, torch.int32
+    t, f32, i32, P, here = (shape.G, shape.S), torch.float32, torch.int32, dims.P, _here()
     c, d = shape._c(), dims._c()
-    _check(load_library().moe_preference_loss(
-        ctypes.byref(c), ctypes.byref(d), _ptr(nll, f32, t, "nll"), _ptr(ref_nll, f32, t, "ref_nll"), _ptr(target, i32, t, "target"),
-        _ptr(start, i32, (2 * dims.P + 1,), "start"), _ptr(loss, f32, (dims.P,), "loss"), _ptr(ratio, f32, (2 * dims.P,), "ratio"),
-        _stream()), "moe_preference_loss")
+    _run(load_library().moe_preference_loss(
+        ctypes.byref(c), ctypes.byref(d), _at(nll, f32, t, "nll", here), _at(ref_nll, f32, t, "ref_nll", here),
+        _at(target, i32, t, "target", here), _at(start, i32, (2 * P + 1,), "start", here), _at(loss, f32, (P,), "loss", here),
+        _at(ratio, f32, (2 * P,), "ratio", here), _stream_of(here)), "moe_preference_loss")
 
 
 def moe_preference_loss_backward(shape: MoEShape, dims: PreferenceDims, target, start, ratio, dloss, dnll):
     """Gradient dnll [G,S] of sum(dloss * loss); ratio as moe_preference_loss left it."""
-    _given("target start ratio dloss dnll", target, start, ratio, dloss, dnll)
-    t, f32, i32 = (shape.G, shape.S), torch.float32, torch.int32
+    t, f32, i32, P, here = (shape.G, shape.S), torch.float32, torch.int32, dims.P, _here()
     c, d = shape._c(), dims._c()
-    _check(load_library().moe_preference_loss_backward(
-        ctypes.byref(c), ctypes.byref(d), _ptr(target, i32, t, "target"), _ptr(start, i32, (2 * dims.P + 1,), "start"),
-        _ptr(ratio, f32, (2 * dims.P,), "ratio"), _ptr(dloss, f32, (dims.P,), "dloss"), _ptr(dnll, f32, t, "dnll"), _stream()),
+    _run(load_library().moe_preference_loss_backward(
+        ctypes.byref(c), ctypes.byref(d), _at(target, i32, t, "target", here), _at(start, i32, (2 * P + 1,), "start", here),
+        _at(ratio, f32, (2 * P,), "ratio", here), _at(dloss, f32, (P,), "dloss", here), _at(dnll, f32, t, "dnll", here), _stream_of(here)),
         "moe_preference_loss_backward")
 
 
-def _policy_args(shape, dims, nll, old_nll, ref_nll, adv, target):
-    _given("nll old_nll adv target", nll, old_nll, adv, target)
-    if ref_nll is not None:
-        _given("ref_nll", ref_nll)
+def _policy_args(shape, dims, nll, old_nll, ref_nll, adv, target, here):
     t, f32 = (shape.G, shape.S), torch.float32
     per_token = isinstance(adv, torch.Tensor) and adv.dim() == 2
-    return dims._c(per_token), (_ptr(nll, f32, t, "nll"), _ptr(old_nll, f32, t, "old_nll"), _ptr(ref_nll, f32, t, "ref_nll"),
-                                _ptr(adv, f32, t if per_token else (shape.G,), "adv"), _ptr(target, torch.int32, t, "target"))
+    return dims._c(per_token), (_at(nll, f32, t, "nll", here), _at(old_nll, f32, t, "old_nll", here),
+                                None if ref_nll is None else _at(ref_nll, f32, t, "ref_nll", here),
+                                _at(adv, f32, t if per_token else (shape.G,), "adv", here), _at(target, torch.int32, t, "target", here))
 
 
 def moe_policy_loss(shape: MoEShape, dims: PolicyDims, nll, old_nll, ref_nll, adv, target, loss, kl=None):
     """Clipped loss [G,S] (and the KL term kl [G,S]) of token losses; adv [G] or [G,S]; ref_nll may be None where dims.beta is 0."""
-    d, args = _policy_args(shape, dims, nll, old_nll, ref_nll, adv, target)
-    _given("loss", loss)
-    if kl is not None:
-        _given("kl", kl)
-    t, f32, c = (shape.G, shape.S), torch.float32, shape._c()
-    _check(load_library().moe_policy_loss(ctypes.byref(c), ctypes.byref(d), *args, _ptr(loss, f32, t, "loss"), _ptr(kl, f32, t, "kl"),
-                                          _stream()), "moe_policy_loss")
+    here, t, f32, c = _here(), (shape.G, shape.S), torch.float32, shape._c()
+    d, args = _policy_args(shape, dims, nll, old_nll, ref_nll, adv, target, here)
+    _run(load_library().moe_policy_loss(ctypes.byref(c), ctypes.byref(d), *args, _at(loss, f32, t, "loss", here),
+                                        None if kl is None else _at(kl, f32, t, "kl", here), _stream_of(here)), "moe_policy_loss")
 
 
 def moe_policy_loss_backward(shape: MoEShape, dims: PolicyDims, nll, old_nll, ref_nll, adv, target, dloss, dnll):
     """Gradient dnll [G,S] of sum(dloss * loss)."""
-    d, args = _policy_args(shape, dims, nll, old_nll, ref_nll, adv, target)
-    _given("dloss dnll", dloss, dnll)
-    t, f32, c = (shape.G, shape.S), torch.float32, shape._c()
-    _check(load_library().moe_policy_loss_backward(ctypes.byref(c), ctypes.byref(d), *args, _ptr(dloss, f32, t, "dloss"),
-                                                   _ptr(dnll, f32, t, "dnll"), _stream()), "moe_policy_loss_backward")
+    here, t, f32, c = _here(), (shape.G, shape.S), torch.float32, shape._c()
+    d, args = _policy_args(shape, dims, nll, old_nll, ref_nll, adv, target, here)
+    _run(load_library().moe_policy_loss_backward(ctypes.byref(c), ctypes.byref(d), *args, _at(dloss, f32, t, "dloss", here),
+                                                 _at(dnll, f32, t, "dnll", here), _stream_of(here)), "moe_policy_loss_backward")
 
 
 # ---- clipping by the norm of all gradients
@@ -940,9 +962,9 @@ class GradientList:
     def __len__(self):
         return len(self.tensors)
 
-    def _here(self):
-        if self.device is not None and torch.cuda.current_device() != self.device:
-            raise ValueError(f"the list's tensors are on cuda:{self.device}, the current device is cuda:{torch.cuda.current_device()}")
+    def _on(self, here):
+        if self.device is not None and here != self.device:
+            raise ValueError(f"the list's tensors are on cuda:{self.device}, the current device is cuda:{here}")
 
 
 def moe_gradient_norm_workspace_bytes(gradients: GradientList) -> int:
@@ -954,16 +976,15 @@ def moe_gradient_norm_workspace_bytes(gradients: GradientList) -> int:
 
 def moe_gradient_norm(gradients: GradientList, norm, ws):
     """norm [1] fp32: the root of the sum of squares of all elements."""
-    _given("norm ws", norm, ws)
-    gradients._here()
-    wsp, wsn = _ws(ws)
-    _check(load_library().moe_gradient_norm(gradients._list, len(gradients), _ptr(norm, torch.float32, (1,), "norm"), wsp, wsn, _stream()),
-           "moe_gradient_norm")
+    here = _here()
+    norm = _at(norm, torch.float32, (1,), "norm", here)
+    gradients._on(here)
+    _run(load_library().moe_gradient_norm(gradients._list, len(gradients), norm, *_room(ws, "ws", here), _stream_of(here)), "moe_gradient_norm")
 
 
 def moe_clip_gradients(gradients: GradientList, norm, max_norm: float):
     """The list's outputs become its tensors times min(1, max_norm / norm[0]); an infinite norm or NaN leaves them as they are."""
-    _given("norm", norm)
-    gradients._here()
-    _check(load_library().moe_clip_gradients(gradients._list, len(gradients), _ptr(norm, torch.float32, (1,), "norm"), max_norm, _stream()),
-           "moe_clip_gradients")
+    here = _here()
+    norm = _at(norm, torch.float32, (1,), "norm", here)
+    gradients._on(here)
+    _run(load_library().moe_clip_gradients(gradients._list, len(gradients), norm, max_norm, _stream_of(here)), "moe_clip_gradients")

@@ -404,6 +404,11 @@ CrossBwdWs carve_cross_bwd(const moe_config& c, const moe_cross_dims& d) {
   w.total = off;
   return w;
 }
+// a projection: C [rows,N] = A [rows,K] . B [K,N]
+int cross_product(const moe_config& c, long long rows, int K, int N, const void* A, const void* B, void* C, hipStream_t st) {
+  if (moe::few_rows_ok(c.act_dtype, rows)) return moe::launch_few_rows(A, B, C, (int)rows, N, K, st);
+  return dense_gemm(c, rows, K, N, false, A, B, C, st);
+}
 // what: 0 inference, 1 training, 2 backward
 int cross_bytes(const moe_config* cfg, const moe_cross_dims* dims, int what, size_t* bytes) {
   const int rc = check_cross(cfg, dims);
@@ -427,11 +432,11 @@ int cross_forward(const moe_config* cfg, const moe_cross_dims* dims, const void*
   hipStream_t st = static_cast<hipStream_t>(stream);
   const long long N = (long long)cfg->G * cfg->S;
   const int A = dims->heads * dims->d;
-  if ((rc = dense_gemm(*cfg, N, cfg->M, A, false, u, wq, base + w.q, st)) != MOE_OK) return rc;
+  if ((rc = cross_product(*cfg, N, cfg->M, A, u, wq, base + w.q, st)) != MOE_OK) return rc;
   rc = moe::launch_cross_attention(cfg->act_dtype, cross_shape(*dims), base + w.q, kv, src_len, base + w.ctx,
                                    train ? reinterpret_cast<float*>(base + w.lse) : nullptr, base + w.scratch, st);
   if (rc != MOE_OK) return rc;
-  return dense_gemm(*cfg, N, A, cfg->M, false, base + w.ctx, wo, out, st);
+  return cross_product(*cfg, N, A, cfg->M, base + w.ctx, wo, out, st);
 }
 
 int check_preference(const moe_config* cfg, const moe_preference_dims* d) {
@@ -491,6 +496,7 @@ int moe_prepare(void) {
   if (rc == MOE_OK) rc = moe::prepare_backward();
   if (rc == MOE_OK) rc = moe::prepare_attention_mfma();
   if (rc == MOE_OK) rc = moe::prepare_cross_attention();
+  if (rc == MOE_OK) rc = moe::prepare_few_rows();
   void* p = nullptr;
   if (rc == MOE_OK) rc = gate_scratch_ptr(&p);
   return rc;
@@ -1117,8 +1123,8 @@ int moe_cross_keys(const moe_config* cfg, const moe_cross_dims* dims, const void
   const void* req[] = {mem, wkv, kv};
   for (const void* p : req)
     if (p == nullptr || !aligned16(p)) return MOE_EINVAL;
-  return dense_gemm(*cfg, (long long)dims->B * dims->Lk, cfg->M, 2 * dims->kv_heads * dims->d, false, mem, wkv, kv,
-                    static_cast<hipStream_t>(stream));
+  return cross_product(*cfg, (long long)dims->B * dims->Lk, cfg->M, 2 * dims->kv_heads * dims->d, mem, wkv, kv,
+                       static_cast<hipStream_t>(stream));
 }
 
 int moe_cross_attention(const moe_config* cfg, const moe_cross_dims* dims, const void* u, const void* kv, const int32_t* src_len,

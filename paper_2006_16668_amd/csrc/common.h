@@ -434,6 +434,10 @@ int launch_cross_attention_bwd(int act_dtype, const CrossShape& s, const void* q
 // out = mem with zeros in those rows
 int launch_held_rows(int act_dtype, const void* mem, const int32_t* src_len, void* out, long long B, int Lk, int M, hipStream_t st);
 
+// C [R,N] = A [R,K] . B [K,N] of few rows, bf16 (few_rows.hip)
+bool few_rows_ok(int act_dtype, long long rows);
+int launch_few_rows(const void* A, const void* B, void* C, int R, int N, int K, hipStream_t st);
+
 // Losses on token losses (token_loss.hip)
 int launch_preference(const moe_preference_dims& d, long long N, const float* nll, const float* ref, const int32_t* target,
                       const int32_t* start, float* loss, float* ratio, hipStream_t st);
@@ -479,5 +483,6 @@ int prepare_gate();               // gate.hip
 int prepare_backward();           // backward.hip
 int prepare_attention_mfma();     // attention_mfma.hip
 int prepare_cross_attention();    // cross_attention.hip
+int prepare_few_rows();           // few_rows.hip
 
 }  // namespace moe

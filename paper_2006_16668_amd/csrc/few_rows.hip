@@ -1,0 +1,94 @@
+// C [R,N] = A [R,K] . B [K,N] of up to 32 rows, bf16: the projections of a step of generation.
+//
+// Bound by the way of B to the matrix cores once, and, at a few MB, by latency: so all of a block's operands are asked for at once.  A block
+// has 32 columns (64 to 32 blocks for 2048 to 1024 of them: neighbours share lines of 128 bytes, so an XCD gets a contiguous range), its
+// eight wavefronts take chunks of 64 rows of B in turn, four at a time each, 128 KB of LDS together, by copies that bypass the registers.
+// Rows of 64 bytes need no swizzle: a transposing read takes 256 consecutive bytes per half.  Transposed as in attention_mfma.hip, C^T = B^T A^T: a
+// lane holds columns of one row, A comes as 16-byte pieces of rows.  The wavefronts' sums meet in LDS, in order.
+#include "attention_tiles.h"
+
+namespace moe {
+namespace {
+
+constexpr int kWaves = 8, kChunk64 = 64 * 64, kAhead = 4;      // bytes of 64 rows of 32 columns; chunks of a wavefront at a time
+constexpr int kLds = kWaves * kAhead * kChunk64;
+
+__global__ __launch_bounds__(64 * kWaves, 1) void few_rows_kernel(const bf16_t* __restrict__ A, const bf16_t* __restrict__ B,
+                                                                  bf16_t* __restrict__ C, int R, int N, int K) {
+  extern __shared__ __attribute__((aligned(256))) unsigned char few_lds[];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)((lds_ptr)few_lds);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 31, hf = lane >> 5, p16 = lane & 15, b1 = (lane >> 4) & 1;
+  const int col0 = (int)xcd_contiguous(blockIdx.x, gridDim.x) * 32;
+  const uint32_t own = lds0 + wave * (kAhead * kChunk64);
+  const uint32_t tr0 = own + (8 * hf + (p16 >> 2)) * 64 + 32 * b1 + 8 * (p16 & 3);
+  const bf16_t* const row = A + (size_t)(r < R ? r : R - 1) * K + 8 * hf;
+  const int chunks = (K + 63) / 64;
+  f32x16_t acc{};
+  for (int first = wave; first < chunks; first += kWaves * kAhead) {
+    u32x4_t a[kAhead][4];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int k0 = 64 * (first + kWaves * j);
+      if (k0 >= K) break;                                      // wavefront-uniform
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int k = k0 + 16 * x + lane / 4, c = col0 + 8 * (lane % 4);
+        const uint64_t at = k < K && c < N ? (uint64_t)(uintptr_t)(B + (size_t)k * N + c) : (uint64_t)(uintptr_t)&att_zero_line;
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(own + j * kChunk64 + x * 1024), "v"(at) : "memory");
+      }
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+        a[j][s] = k0 + 16 * s + 8 * hf < K ? *reinterpret_cast<const u32x4_t*>(row + k0 + 16 * s) : u32x4_t{0u, 0u, 0u, 0u};
+    }
+    wait_all_copies();
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (64 * (first + kWaves * j) >= K) break;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const uint32_t at = tr0 + j * kChunk64 + s * 1024;
+        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(uintptr_t)at);
+        const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(uintptr_t)(at + 256));
+        acc = MOE_MFMA(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), a[j][s], acc);
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // read before the next copies go there
+  }
+  // [wavefront][16][64]; then wavefront w adds up values 2 w and 2 w + 1
+  typedef float __attribute__((address_space(3))) * lds_f_ptr;
+  auto at = [&](int w, int i) __attribute__((always_inline)) { return (lds_f_ptr)(uintptr_t)(lds0 + ((w * 16 + i) * 64 + lane) * 4); };
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 16; ++i) *at(wave, i) = acc[i];
+  __syncthreads();
+  const int c = col0 + 8 * (wave / 2) + 4 * hf + 2 * (wave % 2);
+  float v[2] = {0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    v[0] += *at(w, 2 * wave);
+    v[1] += *at(w, 2 * wave + 1);
+  }
+  if (r < R && c < N) *reinterpret_cast<uint32_t*>(C + (size_t)r * N + c) = pack_bf16x2(v[0], v[1]);
+}
+
+}  // namespace
+
+int prepare_few_rows() {
+  static LdsLimitOnce once;
+  return ensure_lds_limit(once, reinterpret_cast<const void*>(few_rows_kernel), kLds);
+}
+
+// us, the edge kernel of expert_gemm.hip (tiles of 64 x 64, 65 rows) / this; rows, K, N: 1, 1024, 2048 6.0 / 3.2; 32, 1024, 2048 6.0 / 4.8;
+// 4, 2048, 1024 9.6 / 4.7; 16, 1024, 4096 6.3 / 4.2; 4, 512, 512 4.2 / 2.9; with a second tile of rows 64, 1024, 2048 6.0 / 7.0 (pieces of 16 bytes of so
+// many rows are what it waits for then).
+bool few_rows_ok(int act_dtype, long long rows) { return act_dtype == MOE_BF16 && rows <= 32; }
+
+int launch_few_rows(const void* A, const void* B, void* C, int R, int N, int K, hipStream_t st) {
+  if (prepare_few_rows() != MOE_OK) return MOE_EHIP;
+  hipLaunchKernelGGL(few_rows_kernel, dim3((unsigned)((N + 31) / 32)), dim3(64 * kWaves), kLds, st, static_cast<const bf16_t*>(A),
+                     static_cast<const bf16_t*>(B), static_cast<bf16_t*>(C), R, N, K);
+  return check_launch();
+}
+
+}  // namespace moe

@@ -3,24 +3,23 @@
 // Squares are formed and added in 64 bits: the square of any fp32 or bf16 number is exact there and neither overflows nor
 // vanishes, and the fp64 units add far faster than memory delivers (2.5e12 bf16 elements a second at 5 TB/s are 5e12 of some 4e13 operations).
 // Both passes are bound by memory.  Tensors are cut into chunks of one size in bytes, a block each, whatever tensor they belong
-// to, so a list of many small tensors is as few launches as one large one.  Where the tensors are travels as a kernel argument, kTensors of them a launch:
-// nothing is copied to the device, and a captured graph holds it.  The second pass walks the chunks backwards: what
-// the first has read last is still in the memory-side cache.
+// to, so a list of many small tensors is as few launches as one large one.  Where the tensors are travels as a kernel argument, kPieces of them a launch:
+// nothing is copied to the device, and a captured graph holds it.  The second pass walks backwards: what the first has read last is
+// still in the memory-side cache.
 #include <math.h>
 #include "common.h"
 
 namespace moe {
 namespace {
 
-constexpr int kTensors = 100;                // of a launch: 32 bytes each of its 4 KB of arguments
-struct Piece {
-  const void* src;
+struct Piece {                               // of a tensor, whole up to 2 GB
+  uintptr_t src;                             // lowest bit: fp32
   void* dst;
-  unsigned long long count_f32;              // elements, and in the lowest bit whether they are fp32
-  unsigned first, pad;                       // the tensor's first chunk of the launch
+  unsigned bytes, first;                     // its first chunk of the launch
 };
+constexpr int kPieces = 165;                 // of a launch, which has 4 KB of arguments
 struct Table {
-  Piece t[kTensors];
+  Piece t[kPieces];
   int n;
   unsigned chunks;
   unsigned chunk_bytes;                      // a multiple of 4 KB
@@ -28,19 +27,20 @@ struct Table {
 static_assert(sizeof(Table) + 64 <= 4096, "the arguments of a launch");
 
 struct Chunk { const char* src; char* dst; unsigned bytes; bool f32; };
+template <bool BACKWARDS>
 __device__ __forceinline__ Chunk chunk_of(const Table& tab, unsigned c) {
-  int lo = 0, hi = tab.n - 1;                // the last tensor that begins at or before c (empty ones are not in the table)
+  int lo = 0, hi = tab.n - 1;                // the last piece that begins at or before c
   while (lo < hi) {
     const int mid = (lo + hi + 1) / 2;
     if (tab.t[mid].first <= c) lo = mid;
     else hi = mid - 1;
   }
   const Piece& p = tab.t[lo];
-  const bool f32 = (p.count_f32 & 1) != 0;
-  const unsigned long long size = (p.count_f32 >> 1) * (f32 ? 4 : 2), from = (unsigned long long)(c - p.first) * tab.chunk_bytes;
-  const unsigned long long rest = size - from;
-  return {static_cast<const char*>(p.src) + from, static_cast<char*>(p.dst) + from,
-          (unsigned)(rest < tab.chunk_bytes ? rest : tab.chunk_bytes), f32};
+  unsigned k = c - p.first;
+  if (BACKWARDS) k = (p.bytes - 1) / tab.chunk_bytes - k;
+  const unsigned from = k * tab.chunk_bytes, rest = p.bytes - from;
+  return {reinterpret_cast<const char*>(p.src & ~(uintptr_t)1) + from, static_cast<char*>(p.dst) + from,
+          rest < tab.chunk_bytes ? rest : tab.chunk_bytes, (p.src & 1) != 0};
 }
 
 __device__ __forceinline__ double block_sum(double v) {
@@ -83,7 +83,7 @@ __device__ __forceinline__ double squares(const Chunk& c) {
 }
 
 __global__ __launch_bounds__(256) void gradient_squares_kernel(Table tab, double* __restrict__ partial) {
-  const Chunk c = chunk_of(tab, blockIdx.x);
+  const Chunk c = chunk_of<false>(tab, blockIdx.x);
   const double s = block_sum(c.f32 ? squares<float>(c) : squares<bf16_t>(c));
   if (threadIdx.x == 0) partial[blockIdx.x] = s;
 }
@@ -132,7 +132,7 @@ __device__ __forceinline__ void copy_chunk(const Chunk& c) {
 }
 
 __global__ __launch_bounds__(256) void clip_gradients_kernel(Table tab, const float* __restrict__ norm, double max_norm) {
-  const Chunk c = chunk_of(tab, tab.chunks - 1 - blockIdx.x);
+  const Chunk c = chunk_of<true>(tab, blockIdx.x);
   const float n = *norm;
   // (a comparison with NaN is false, and an infinite norm scales nothing either: bits are kept, NaN and all)
   if (!((double)n > max_norm && n < INFINITY)) {
@@ -149,36 +149,44 @@ size_t bytes_of(const moe_gradient& g) { return (size_t)g.count * (g.dtype == MO
 size_t chunk_size(const moe_gradient* list, int n) {
   size_t total = 0;
   for (int i = 0; i < n; ++i) total += bytes_of(list[i]);
-  const size_t unit = (size_t)16 << 10;
-  size_t c = (total / 4096 + unit - 1) / unit * unit;
-  if (c < unit) c = unit;
-  return c < ((size_t)1 << 30) ? c : (size_t)1 << 30;
+  const size_t unit = (size_t)16 << 10, most = (size_t)1 << 30;
+  const size_t c = (total / 4096 + unit - 1) / unit * unit;
+  return c < unit ? unit : c < most ? c : most;
 }
-size_t chunks_of(const moe_gradient& g, size_t chunk) { return (bytes_of(g) + chunk - 1) / chunk; }
+size_t chunks_of(size_t bytes, size_t chunk) { return (bytes + chunk - 1) / chunk; }
 
-// f(table) for as many tensors at a time as a launch takes, forwards or backwards
+// f(table) for as many pieces at a time as a launch takes, forwards or backwards
 template <typename F>
 int for_tables(const moe_gradient* list, int n, size_t chunk, bool backwards, F&& f) {
   Table tab;
-  int rc = MOE_OK;
-  for (int done = 0; done < n && rc == MOE_OK;) {
-    const int take = n - done < kTensors ? n - done : kTensors, from = backwards ? n - done - take : done;
-    unsigned long long chunks = 0;
-    tab.n = 0;
-    for (int i = from; i < from + take; ++i) {
-      if (list[i].count == 0) continue;
-      tab.t[tab.n++] = Piece{list[i].src, list[i].dst, (unsigned long long)list[i].count << 1 | (list[i].dtype == MOE_F32 ? 1u : 0u),
-                             (unsigned)chunks, 0};
-      chunks += chunks_of(list[i], chunk);
-    }
-    done += take;
-    if (tab.n == 0) continue;
-    if (chunks > 0x7fffffffULL) return MOE_EUNSUPPORTED;
+  tab.n = 0;
+  tab.chunk_bytes = (unsigned)chunk;
+  unsigned long long chunks = 0;
+  auto flush = [&]() {
+    if (tab.n == 0) return (int)MOE_OK;
+    if (chunks > 0x7fffffffULL) return (int)MOE_EUNSUPPORTED;
     tab.chunks = (unsigned)chunks;
-    tab.chunk_bytes = (unsigned)chunk;
-    rc = f(tab);
+    const int rc = f(tab);
+    tab.n = 0;
+    chunks = 0;
+    return rc;
+  };
+  const size_t piece = ((size_t)1 << 31) / chunk * chunk;      // whole chunks
+  for (int j = 0; j < n; ++j) {
+    const moe_gradient& g = list[backwards ? n - 1 - j : j];
+    const size_t bytes = bytes_of(g), parts = (bytes + piece - 1) / piece;
+    for (size_t x = 0; x < parts; ++x) {
+      if (tab.n == kPieces) {
+        const int rc = flush();
+        if (rc != MOE_OK) return rc;
+      }
+      const size_t from = (backwards ? parts - 1 - x : x) * piece, part = bytes - from < piece ? bytes - from : piece;
+      tab.t[tab.n++] = Piece{(reinterpret_cast<uintptr_t>(g.src) + from) | (g.dtype == MOE_F32 ? 1u : 0u),
+                             reinterpret_cast<void*>(reinterpret_cast<uintptr_t>(g.dst) + from), (unsigned)part, (unsigned)chunks};
+      chunks += chunks_of(part, chunk);
+    }
   }
-  return rc;
+  return flush();
 }
 
 }  // namespace
@@ -186,7 +194,7 @@ int for_tables(const moe_gradient* list, int n, size_t chunk, bool backwards, F&
 size_t gradient_norm_bytes(const moe_gradient* list, int n) {
   const size_t chunk = chunk_size(list, n);
   size_t chunks = 0;
-  for (int i = 0; i < n; ++i) chunks += chunks_of(list[i], chunk);
+  for (int i = 0; i < n; ++i) chunks += chunks_of(bytes_of(list[i]), chunk);
   return align_up((chunks + 1) * sizeof(double), 256);
 }
 

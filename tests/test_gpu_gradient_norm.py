@@ -29,7 +29,7 @@ def exact(tensors):
 
 
 SIZES = [[1], [3, 5], [8191, 8192, 8193], [0, 17, 0], [1, 2, 3, 4, 5, 6, 7, 8, 9, 15, 16, 17, 31, 33], [4096 * 4, 1, 4096 * 8 + 1],
-         [100] * 99, [101] * 100, [77] * 101, [33] * 250, [30_000_001, 5, 12_345_678]]
+         [100] * 99, [101] * 100, [77] * 165, [33] * 166, [33] * 500, [30_000_001, 5, 12_345_678]]
 
 
 @pytest.mark.parametrize("ratio", [0.25, 2.0, 0.0])
@@ -121,3 +121,18 @@ def test_refusals():
             moe.moe_clip_gradients(lst, norm, limit)
     with pytest.raises(moe.MoEError):
         moe.moe_gradient_norm(lst, norm, torch.empty(0, dtype=torch.uint8, device=DEV))
+
+
+def test_a_tensor_of_more_than_2_gb():
+    """Two launches' worth of pieces of one tensor, offsets past 2^31 bytes; the last elements are found and scaled."""
+    n = (1 << 30) + (1 << 29) + 12345
+    t = torch.zeros(n, dtype=torch.bfloat16, device=DEV)
+    for at in (0, (1 << 30) - 1, 1 << 30, n - 1):
+        t[at] = 3.0
+    lst = moe.GradientList([t])
+    norm = norm_of(lst)
+    assert float(norm) == 6.0
+    moe.moe_clip_gradients(lst, norm, 2.0)
+    for at in (0, (1 << 30) - 1, 1 << 30, n - 1):
+        assert float(t[at]) == 1.0
+    assert float(t[1]) == 0 and float(t[(1 << 30) + 1]) == 0
