@@ -406,7 +406,7 @@ CrossBwdWs carve_cross_bwd(const moe_config& c, const moe_cross_dims& d) {
 }
 // a projection: C [rows,N] = A [rows,K] . B [K,N]
 int cross_product(const moe_config& c, long long rows, int K, int N, const void* A, const void* B, void* C, hipStream_t st) {
-  if (moe::few_rows_ok(c.act_dtype, rows)) return moe::launch_few_rows(A, B, C, (int)rows, N, K, st);
+  if (moe::few_rows_ok(c.act_dtype, rows, N)) return moe::launch_few_rows(A, B, C, (int)rows, N, K, st);
   return dense_gemm(c, rows, K, N, false, A, B, C, st);
 }
 // what: 0 inference, 1 training, 2 backward

@@ -434,8 +434,8 @@ int launch_cross_attention_bwd(int act_dtype, const CrossShape& s, const void* q
 // out = mem with zeros in those rows
 int launch_held_rows(int act_dtype, const void* mem, const int32_t* src_len, void* out, long long B, int Lk, int M, hipStream_t st);
 
-// C [R,N] = A [R,K] . B [K,N] of few rows, bf16 (few_rows.hip)
-bool few_rows_ok(int act_dtype, long long rows);
+// C [R,N] = A [R,K] . B [K,N] in up to as many tiles of 32 x 32 as there are compute units, bf16 (few_rows.hip)
+bool few_rows_ok(int act_dtype, long long rows, int N);
 int launch_few_rows(const void* A, const void* B, void* C, int R, int N, int K, hipStream_t st);
 
 // Losses on token losses (token_loss.hip)

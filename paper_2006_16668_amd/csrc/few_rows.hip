@@ -1,17 +1,19 @@
-// C [R,N] = A [R,K] . B [K,N] of up to 32 rows, bf16: the projections of a step of generation.
+// C [R,N] = A [R,K] . B [K,N] of few rows or columns, bf16: the projections of a step of generation.
 //
-// Bound by the way of B to the matrix cores once, and, at a few MB, by latency: so all of a block's operands are asked for at once.  A block
-// has 32 columns (64 to 32 blocks for 2048 to 1024 of them: neighbours share lines of 128 bytes, so an XCD gets a contiguous range), its
-// eight wavefronts take chunks of 64 rows of B in turn, four at a time each, 128 KB of LDS together, by copies that bypass the registers.
-// Rows of 64 bytes need no swizzle: a transposing read takes 256 consecutive bytes per half.  Transposed as in attention_mfma.hip, C^T = B^T A^T: a
-// lane holds columns of one row, A comes as 16-byte pieces of rows.  The wavefronts' sums meet in LDS, in order.
+// Bound by the way of B to the matrix cores once, and, at a few MB, by latency: so all of a block's operands are asked for at once, by copies that
+// bypass the registers.  A block has 32 rows and 32 columns (64 to 32 blocks for 2048 to 1024 columns and 32 rows; neighbours share lines of
+// 128 bytes and columns of B, so an XCD gets a contiguous range); its eight wavefronts take chunks of 64 k in turn, two at a
+// time each, 128 KB of LDS together.  B's rows of 64 bytes need no swizzle, a transposing read takes 256 consecutive bytes per half; chunk c of
+// A's rows of 128 bytes sits at c ^ (row / 2) % 8, which spreads 16 rows over all banks.  (Read as fragments from memory, 16 bytes of 32 rows at a
+// time, A costs as much as B.)  Transposed as in attention_mfma.hip, C^T = B^T A^T: a lane holds columns of one row.  The
+// wavefronts' sums meet in LDS, in order.
 #include "attention_tiles.h"
 
 namespace moe {
 namespace {
 
-constexpr int kWaves = 8, kChunk64 = 64 * 64, kAhead = 4;      // bytes of 64 rows of 32 columns; chunks of a wavefront at a time
-constexpr int kLds = kWaves * kAhead * kChunk64;
+constexpr int kWaves = 8, kBytesB = 64 * 64, kBytesA = 32 * 128, kPlace = kBytesB + kBytesA, kAhead = 2;
+constexpr int kLds = kWaves * kAhead * kPlace;
 
 __global__ __launch_bounds__(64 * kWaves, 1) void few_rows_kernel(const bf16_t* __restrict__ A, const bf16_t* __restrict__ B,
                                                                   bf16_t* __restrict__ C, int R, int N, int K) {
@@ -19,14 +21,18 @@ __global__ __launch_bounds__(64 * kWaves, 1) void few_rows_kernel(const bf16_t* 
   const uint32_t lds0 = (uint32_t)(uintptr_t)((lds_ptr)few_lds);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 31, hf = lane >> 5, p16 = lane & 15, b1 = (lane >> 4) & 1;
-  const int col0 = (int)xcd_contiguous(blockIdx.x, gridDim.x) * 32;
-  const uint32_t own = lds0 + wave * (kAhead * kChunk64);
+  const unsigned item = xcd_contiguous(blockIdx.x, gridDim.x), row_tiles = (R + 31) / 32;
+  const int col0 = (int)(item / row_tiles) * 32, row0 = (int)(item % row_tiles) * 32;
+  const uint32_t own = lds0 + wave * (kAhead * kPlace);
   const uint32_t tr0 = own + (8 * hf + (p16 >> 2)) * 64 + 32 * b1 + 8 * (p16 & 3);
-  const bf16_t* const row = A + (size_t)(r < R ? r : R - 1) * K + 8 * hf;
+  const uint32_t a0 = own + kBytesB + r * 128 + ((hf ^ ((r >> 1) & 7)) << 4);
+  auto copy = [&](uint32_t to, const bf16_t* from, bool there) __attribute__((always_inline)) {
+    const uint64_t at = there ? (uint64_t)(uintptr_t)from : (uint64_t)(uintptr_t)&att_zero_line;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(at) : "memory");
+  };
   const int chunks = (K + 63) / 64;
   f32x16_t acc{};
   for (int first = wave; first < chunks; first += kWaves * kAhead) {
-    u32x4_t a[kAhead][4];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       const int k0 = 64 * (first + kWaves * j);
@@ -34,12 +40,13 @@ __global__ __launch_bounds__(64 * kWaves, 1) void few_rows_kernel(const bf16_t* 
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
         const int k = k0 + 16 * x + lane / 4, c = col0 + 8 * (lane % 4);
-        const uint64_t at = k < K && c < N ? (uint64_t)(uintptr_t)(B + (size_t)k * N + c) : (uint64_t)(uintptr_t)&att_zero_line;
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(own + j * kChunk64 + x * 1024), "v"(at) : "memory");
+        copy(own + j * kPlace + x * 1024, B + (size_t)k * N + c, k < K && c < N);
       }
 #pragma unroll
-      for (int s = 0; s < 4; ++s)
-        a[j][s] = k0 + 16 * s + 8 * hf < K ? *reinterpret_cast<const u32x4_t*>(row + k0 + 16 * s) : u32x4_t{0u, 0u, 0u, 0u};
+      for (int x = 0; x < 4; ++x) {
+        const int i = 8 * x + lane / 8, k = k0 + 8 * ((lane % 8) ^ ((i >> 1) & 7));
+        copy(own + j * kPlace + kBytesB + x * 1024, A + (size_t)(row0 + i) * K + k, row0 + i < R && k < K);
+      }
     }
     wait_all_copies();
 #pragma unroll
@@ -47,10 +54,11 @@ __global__ __launch_bounds__(64 * kWaves, 1) void few_rows_kernel(const bf16_t* 
       if (64 * (first + kWaves * j) >= K) break;
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
-        const uint32_t at = tr0 + j * kChunk64 + s * 1024;
+        const uint32_t at = tr0 + j * kPlace + s * 1024;
         const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(uintptr_t)at);
         const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(uintptr_t)(at + 256));
-        acc = MOE_MFMA(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), a[j][s], acc);
+        const u32x4_t a = *(lds_u4_ptr)(uintptr_t)((a0 ^ (s << 5)) + j * kPlace);
+        acc = MOE_MFMA(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), a, acc);
       }
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // read before the next copies go there
@@ -69,7 +77,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void few_rows_kernel(const bf16_t* 
     v[0] += *at(w, 2 * wave);
     v[1] += *at(w, 2 * wave + 1);
   }
-  if (r < R && c < N) *reinterpret_cast<uint32_t*>(C + (size_t)r * N + c) = pack_bf16x2(v[0], v[1]);
+  if (row0 + r < R && c < N) *reinterpret_cast<uint32_t*>(C + (size_t)(row0 + r) * N + c) = pack_bf16x2(v[0], v[1]);
 }
 
 }  // namespace
@@ -79,14 +87,16 @@ int prepare_few_rows() {
   return ensure_lds_limit(once, reinterpret_cast<const void*>(few_rows_kernel), kLds);
 }
 
-// us, the edge kernel of expert_gemm.hip (tiles of 64 x 64, 65 rows) / this; rows, K, N: 1, 1024, 2048 6.0 / 3.2; 32, 1024, 2048 6.0 / 4.8;
-// 4, 2048, 1024 9.6 / 4.7; 16, 1024, 4096 6.3 / 4.2; 4, 512, 512 4.2 / 2.9; with a second tile of rows 64, 1024, 2048 6.0 / 7.0 (pieces of 16 bytes of so
-// many rows are what it waits for then).
-bool few_rows_ok(int act_dtype, long long rows) { return act_dtype == MOE_BF16 && rows <= 32; }
+// Blocks fill the device once at most.  us, the edge kernel of expert_gemm.hip / this; K, N, rows: 1024, 2048, 1 5.7 / 3.4; 64 5.9 / 3.9; 128 6.0 / 4.4,
+// 192 6.1 / 7.2; 2048, 1024, 4 9.3 / 4.6; 64 9.4 / 4.7; 256 9.6 / 6.1; 1024, 4096, 64 6.0 / 4.6, 96 6.2 / 7.3; 512, 512, 4 4.0 / 3.0; 2048, 4096, 64 9.7 / 6.5.
+bool few_rows_ok(int act_dtype, long long rows, int N) {
+  constexpr long long kUnits = 256;
+  return act_dtype == MOE_BF16 && rows <= 32 * kUnits && (rows + 31) / 32 * ((N + 31) / 32) <= kUnits;
+}
 
 int launch_few_rows(const void* A, const void* B, void* C, int R, int N, int K, hipStream_t st) {
   if (prepare_few_rows() != MOE_OK) return MOE_EHIP;
-  hipLaunchKernelGGL(few_rows_kernel, dim3((unsigned)((N + 31) / 32)), dim3(64 * kWaves), kLds, st, static_cast<const bf16_t*>(A),
+  hipLaunchKernelGGL(few_rows_kernel, dim3((unsigned)((N + 31) / 32 * ((R + 31) / 32))), dim3(64 * kWaves), kLds, st, static_cast<const bf16_t*>(A),
                      static_cast<const bf16_t*>(B), static_cast<bf16_t*>(C), R, N, K);
   return check_launch();
 }

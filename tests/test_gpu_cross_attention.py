@@ -157,3 +157,18 @@ def test_gradients_against_differences():
             b = (q - step, kv) if t is q else (q, kv - step)
             want = float(ref[name][0][at])
             assert math.isclose((f(*a) - f(*b)) / 2e-5, want, rel_tol=1e-5, abs_tol=1e-8)
+
+
+@pytest.mark.parametrize("rows,M,heads", [(1, 8, 1), (1, 1024, 8), (3, 72, 2), (31, 520, 1), (32, 64, 3), (33, 2056, 1), (64, 1000, 8), (65, 264, 2),
+                                          (128, 1024, 16), (256, 128, 4), (257, 136, 1), (2048, 40, 1), (2049, 40, 1)])
+def test_keys_of_few_and_more_rows(rows, M, heads):
+    """Products whose tiles of 32 x 32 fill the device once, and larger ones: sums of 8 to 2056 terms, ends inside a tile, a chunk, a piece."""
+    g = torch.Generator(device=DEV).manual_seed(rows + M)
+    W = 2 * heads * 64
+    mem, wkv = _rand(g, 1, rows, M, dt=torch.bfloat16), _rand(g, M, W, dt=torch.bfloat16)
+    room = torch.full((rows * W + 256,), 7.0, dtype=torch.bfloat16, device=DEV)
+    kv = room[128:128 + rows * W].view(1, rows, W)
+    moe.moe_cross_keys(moe.MoEShape(1, 1, M, 64, 2, 1), moe.CrossDims(1, 1, rows, heads, 64), mem, wkv, kv)
+    want, size = mem.double() @ wkv.double(), mem.double().abs() @ wkv.double().abs()
+    assert_within(kv, want, HALF["bf16"] * want.abs() + M * U * size, "kv")
+    assert (room[:128] == 7).all() and (room[-128:] == 7).all()
