@@ -406,8 +406,22 @@ CrossBwdWs carve_cross_bwd(const moe_config& c, const moe_cross_dims& d) {
 }
 // a projection: C [rows,N] = A [rows,K] . B [K,N]
 int cross_product(const moe_config& c, long long rows, int K, int N, const void* A, const void* B, void* C, hipStream_t st) {
-  if (moe::few_rows_ok(c.act_dtype, rows, N)) return moe::launch_few_rows(A, B, C, (int)rows, N, K, st);
+  if (moe::few_rows_ok(c.act_dtype, rows, N)) return moe::launch_few_rows(c.act_dtype, false, A, B, C, (int)rows, N, K, st);
   return dense_gemm(c, rows, K, N, false, A, B, C, st);
+}
+// its gradients: dA = dC . B^T, dB = A^T . dC
+int cross_gradients(const moe_config& c, long long rows, int K, int N, const void* A, const void* dC, const void* B, void* dA, void* dB,
+                    float* wpart, hipStream_t st) {
+  if (c.act_dtype != MOE_F32 || !moe::few_rows_ok(c.act_dtype, rows, K))
+    return moe::launch_dense_grads(c, rows, K, N, A, dC, B, nullptr, dA, dB, wpart, st);
+  const int rc = moe::launch_few_rows(c.act_dtype, true, dC, B, dA, (int)rows, K, N, st);
+  if (rc != MOE_OK) return rc;
+  moe_config g = c;                                            // dB as the weight gradient of one expert
+  g.E = g.G = 1;
+  g.S = g.C = (int)rows;
+  g.M = K;
+  g.H = N;
+  return moe::launch_expert_wgrad1(g, A, dC, dB, nullptr, st);
 }
 // what: 0 inference, 1 training, 2 backward
 int cross_bytes(const moe_config* cfg, const moe_cross_dims* dims, int what, size_t* bytes) {
@@ -1158,14 +1172,14 @@ int moe_cross_attention_backward(const moe_config* cfg, const moe_cross_dims* di
   const int A = dims->heads * dims->d, Akv2 = 2 * dims->kv_heads * dims->d;
   float* wpart = reinterpret_cast<float*>(base + w.wpart);
   // out = ctx . wo
-  rc = moe::launch_dense_grads(*cfg, N, A, cfg->M, fwd + f.ctx, dout, wo, nullptr, base + w.dctx, dwo, wpart, st);
+  rc = cross_gradients(*cfg, N, A, cfg->M, fwd + f.ctx, dout, wo, base + w.dctx, dwo, wpart, st);
   if (rc != MOE_OK) return rc;
   rc = moe::launch_cross_attention_bwd(cfg->act_dtype, cross_shape(*dims), fwd + f.q, kv, src_len, fwd + f.ctx, base + w.dctx,
                                        reinterpret_cast<const float*>(fwd + f.lse), base + w.dq, base + w.dkv,
                                        reinterpret_cast<float*>(base + w.dvec), st);
   if (rc != MOE_OK) return rc;
   // q = u . wq
-  rc = moe::launch_dense_grads(*cfg, N, cfg->M, A, u, base + w.dq, wq, nullptr, du, dwq, wpart, st);
+  rc = cross_gradients(*cfg, N, cfg->M, A, u, base + w.dq, wq, du, dwq, wpart, st);
   if (rc != MOE_OK) return rc;
   // [K|V] = mem . wkv; states that do not hold have gradients of zeros, which their rows of mem must not turn into NaN
   if (src_len != nullptr) {
@@ -1173,7 +1187,7 @@ int moe_cross_attention_backward(const moe_config* cfg, const moe_cross_dims* di
     if (rc != MOE_OK) return rc;
     mem = base + w.mem;
   }
-  return moe::launch_dense_grads(*cfg, rows, cfg->M, Akv2, mem, base + w.dkv, wkv, nullptr, dmem, dwkv, wpart, st);
+  return cross_gradients(*cfg, rows, cfg->M, Akv2, mem, base + w.dkv, wkv, dmem, dwkv, wpart, st);
 }
 
 int moe_preference_loss(const moe_config* cfg, const moe_preference_dims* dims, const float* nll, const float* ref_nll,

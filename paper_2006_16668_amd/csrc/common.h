@@ -434,9 +434,9 @@ int launch_cross_attention_bwd(int act_dtype, const CrossShape& s, const void* q
 // out = mem with zeros in those rows
 int launch_held_rows(int act_dtype, const void* mem, const int32_t* src_len, void* out, long long B, int Lk, int M, hipStream_t st);
 
-// C [R,N] = A [R,K] . B [K,N] in up to as many tiles of 32 x 32 as there are compute units, bf16 (few_rows.hip)
+// C [R,N] = A [R,K] . B [K,N] (b_kc, fp32: B [N,K]^T) of few rows or columns (few_rows.hip)
 bool few_rows_ok(int act_dtype, long long rows, int N);
-int launch_few_rows(const void* A, const void* B, void* C, int R, int N, int K, hipStream_t st);
+int launch_few_rows(int act_dtype, bool b_kc, const void* A, const void* B, void* C, int R, int N, int K, hipStream_t st);
 
 // Losses on token losses (token_loss.hip)
 int launch_preference(const moe_preference_dims& d, long long N, const float* nll, const float* ref, const int32_t* target,

@@ -80,6 +80,54 @@ __global__ __launch_bounds__(64 * kWaves, 1) void few_rows_kernel(const bf16_t* 
   if (row0 + r < R && c < N) *reinterpret_cast<uint32_t*>(C + (size_t)(row0 + r) * N + c) = pack_bf16x2(v[0], v[1]);
 }
 
+// fp32 on v_mfma_f32_16x16x4, tiles of 16 x 16: a tile of 32 x 32 would keep its unit's matrix cores busy for 7 us at K 2048 and leave most units
+// without one.  Lane (r = lane % 16, q = lane / 16) takes k = 16 g + 4 q + j in step j of a group of 16, so A (and B [N,K], B_KC) comes as 16-byte
+// pieces of rows and B [K,N] as 64 bytes of four rows, straight to registers, 128 k of a wavefront at a time.
+template <bool B_KC>
+__global__ __launch_bounds__(64 * kWaves, 2) void few_rows_f32_kernel(const float* __restrict__ A, const float* __restrict__ B,
+                                                                      float* __restrict__ C, int R, int N, int K) {
+  constexpr int G = 8;                                         // groups of 16 k
+  __shared__ f32x4_t sums[kWaves][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, q = lane >> 4;
+  const unsigned item = xcd_contiguous(blockIdx.x, gridDim.x), row_tiles = (R + 15) / 16;
+  const int col0 = (int)(item / row_tiles) * 16, row0 = (int)(item % row_tiles) * 16;
+  const float* const row = A + (size_t)(row0 + r < R ? row0 + r : R - 1) * K + 4 * q;
+  const int col = col0 + r < N ? col0 + r : N - 1;
+  const float* const bcol = B + (size_t)col * K + 4 * q;       // (B_KC)
+  const unsigned boff = (unsigned)(4 * q * N + col);           // (else: from a row that all lanes share)
+  f32x4_t acc{};
+  for (int k0 = wave * 16 * G; k0 < K; k0 += kWaves * 16 * G) {
+    f32x4_t a[G], b[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const int k = k0 + 16 * g;
+      a[g] = b[g] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      if (k + 4 * q < K) {                                     // (K is a multiple of 4)
+        a[g] = *reinterpret_cast<const f32x4_t*>(row + k);
+        if constexpr (B_KC) b[g] = *reinterpret_cast<const f32x4_t*>(bcol + k);
+        else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) b[g][j] = (B + (size_t)(k + j) * N)[boff];
+        }
+      }
+    }
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      if (k0 + 16 * g >= K) break;                             // wavefront-uniform
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(b[g][j], a[g][j], acc, 0, 0, 0);
+    }
+  }
+  sums[wave][lane] = acc;                                      // columns 4 q .. + 3 of row r
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) acc += sums[w][lane];
+  const int c = col0 + 4 * q;
+  if (row0 + r < R && c < N) *reinterpret_cast<f32x4_t*>(C + (size_t)(row0 + r) * N + c) = acc;
+}
+
 }  // namespace
 
 int prepare_few_rows() {
@@ -87,17 +135,30 @@ int prepare_few_rows() {
   return ensure_lds_limit(once, reinterpret_cast<const void*>(few_rows_kernel), kLds);
 }
 
-// Blocks fill the device once at most.  us, the edge kernel of expert_gemm.hip / this; K, N, rows: 1024, 2048, 1 5.7 / 3.4; 64 5.9 / 3.9; 128 6.0 / 4.4,
+// bf16 blocks fill the device once at most, fp32 blocks, of which several share a unit, three times.  us, gemm_f32.hip / this, fp32: 1024, 2048, 1 16.6 / 4.3;
+// 32 16.8 / 5.7; 96 17.2 / 12.5, 128 17.0 / 16.1; 2048, 1024, 4 29.1 / 6.6; 64 29.3 / 9.2; 512, 512, 64 10.2 / 4.0.  bf16, us, the edge kernel of expert_gemm.hip / this; K, N, rows: 1024, 2048, 1 5.7 / 3.4; 64 5.9 / 3.9; 128 6.0 / 4.4,
 // 192 6.1 / 7.2; 2048, 1024, 4 9.3 / 4.6; 64 9.4 / 4.7; 256 9.6 / 6.1; 1024, 4096, 64 6.0 / 4.6, 96 6.2 / 7.3; 512, 512, 4 4.0 / 3.0; 2048, 4096, 64 9.7 / 6.5.
 bool few_rows_ok(int act_dtype, long long rows, int N) {
   constexpr long long kUnits = 256;
-  return act_dtype == MOE_BF16 && rows <= 32 * kUnits && (rows + 31) / 32 * ((N + 31) / 32) <= kUnits;
+  const long long side = act_dtype == MOE_F32 ? 16 : 32, most = act_dtype == MOE_F32 ? 3 * kUnits : kUnits;
+  return rows <= side * most && (rows + side - 1) / side * ((N + side - 1) / side) <= most;
 }
 
-int launch_few_rows(const void* A, const void* B, void* C, int R, int N, int K, hipStream_t st) {
+int launch_few_rows(int act_dtype, bool b_kc, const void* A, const void* B, void* C, int R, int N, int K, hipStream_t st) {
+  const int side = act_dtype == MOE_F32 ? 16 : 32;
+  const dim3 grid((unsigned)((N + side - 1) / side * ((R + side - 1) / side))), threads(64 * kWaves);
+  if (act_dtype == MOE_F32) {
+    auto a = static_cast<const float*>(A);
+    auto b = static_cast<const float*>(B);
+    auto c = static_cast<float*>(C);
+    if (b_kc) hipLaunchKernelGGL((few_rows_f32_kernel<true>), grid, threads, 0, st, a, b, c, R, N, K);
+    else hipLaunchKernelGGL((few_rows_f32_kernel<false>), grid, threads, 0, st, a, b, c, R, N, K);
+    return check_launch();
+  }
+  if (b_kc) return MOE_EUNSUPPORTED;
   if (prepare_few_rows() != MOE_OK) return MOE_EHIP;
-  hipLaunchKernelGGL(few_rows_kernel, dim3((unsigned)((N + 31) / 32 * ((R + 31) / 32))), dim3(64 * kWaves), kLds, st, static_cast<const bf16_t*>(A),
-                     static_cast<const bf16_t*>(B), static_cast<bf16_t*>(C), R, N, K);
+  hipLaunchKernelGGL(few_rows_kernel, grid, threads, kLds, st, static_cast<const bf16_t*>(A), static_cast<const bf16_t*>(B),
+                     static_cast<bf16_t*>(C), R, N, K);
   return check_launch();
 }
 

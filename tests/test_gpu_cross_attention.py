@@ -101,7 +101,8 @@ def test_attention_and_its_gradients(dtype, B, Lq, Lk, heads, kv_heads, d, kind)
 
 @pytest.mark.parametrize("dtype,B,Lq,Lk,M,heads,kv_heads,d,kind", [
     ("bf16", 3, 70, 150, 264, 4, 2, 64, "any"), ("f32", 3, 70, 150, 260, 4, 4, 64, "any"), ("bf16", 7, 1, 90, 512, 4, 4, 128, None),
-    ("f32", 2, 2, 333, 132, 2, 1, 128, "any"), ("bf16", 2, 200, 130, 1024, 8, 8, 64, None)])
+    ("f32", 2, 2, 333, 132, 2, 1, 128, "any"), ("f32", 2, 5, 7, 1284, 4, 2, 64, "any"), ("f32", 1, 1, 1, 4, 1, 1, 64, None), ("bf16", 1, 1, 1, 8, 1, 1, 64, None),
+    ("bf16", 2, 200, 130, 1024, 8, 8, 64, None)])
 def test_layer_with_its_projections(dtype, B, Lq, Lk, M, heads, kv_heads, d, kind):
     g = torch.Generator(device=DEV).manual_seed(M + Lk)
     dt, h, A, W = DT[dtype], HALF[dtype], heads * d, 2 * kv_heads * d
@@ -136,8 +137,9 @@ def test_layer_with_its_projections(dtype, B, Lq, Lk, M, heads, kv_heads, d, kin
         assert torch.isfinite(got).all(), name
         bound = err.norm() + (3 * rel + 2 * h + 2 * max(M, A, B * Lq, B * Lk) * U) * want.norm()
         assert (got - want).norm() <= bound, (name, float((got - want).norm() / want.norm()), float(bound / want.norm()))
-        # and not only within the worst case: roundings of independent sign leave a few h
-        assert (got - want).norm() <= (6 * h + 2000 * U) * want.norm(), (name, float((got - want).norm() / want.norm()))
+        # and not only within the worst case: roundings of independent sign leave a few h.  (One state: p = 1 and dS = 0, and what the 64-bit sums leave
+        # of it is their own rounding, n 2^-53 of magnitudes of which err has at least 2^-24: n 2^-29 err, below 2^-20 err for sums of 512 terms.)
+        assert (got - want).norm() <= (6 * h + 2000 * U) * want.norm() + 2.0 ** -20 * err.norm(), (name, float((got - want).norm() / want.norm()))
 
 
 def test_gradients_against_differences():
@@ -161,14 +163,15 @@ def test_gradients_against_differences():
 
 @pytest.mark.parametrize("rows,M,heads", [(1, 8, 1), (1, 1024, 8), (3, 72, 2), (31, 520, 1), (32, 64, 3), (33, 2056, 1), (64, 1000, 8), (65, 264, 2),
                                           (128, 1024, 16), (256, 128, 4), (257, 136, 1), (2048, 40, 1), (2049, 40, 1)])
-def test_keys_of_few_and_more_rows(rows, M, heads):
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_keys_of_few_and_more_rows(rows, M, heads, dtype):
     """Products whose tiles of 32 x 32 fill the device once, and larger ones: sums of 8 to 2056 terms, ends inside a tile, a chunk, a piece."""
     g = torch.Generator(device=DEV).manual_seed(rows + M)
     W = 2 * heads * 64
-    mem, wkv = _rand(g, 1, rows, M, dt=torch.bfloat16), _rand(g, M, W, dt=torch.bfloat16)
-    room = torch.full((rows * W + 256,), 7.0, dtype=torch.bfloat16, device=DEV)
+    mem, wkv = _rand(g, 1, rows, M, dt=DT[dtype]), _rand(g, M, W, dt=DT[dtype])
+    room = torch.full((rows * W + 256,), 7.0, dtype=DT[dtype], device=DEV)
     kv = room[128:128 + rows * W].view(1, rows, W)
-    moe.moe_cross_keys(moe.MoEShape(1, 1, M, 64, 2, 1), moe.CrossDims(1, 1, rows, heads, 64), mem, wkv, kv)
+    moe.moe_cross_keys(moe.MoEShape(1, 1, M, 64, 2, 1, dtype), moe.CrossDims(1, 1, rows, heads, 64), mem, wkv, kv)
     want, size = mem.double() @ wkv.double(), mem.double().abs() @ wkv.double().abs()
-    assert_within(kv, want, HALF["bf16"] * want.abs() + M * U * size, "kv")
+    assert_within(kv, want, HALF[dtype] * want.abs() + M * U * size, "kv")
     assert (room[:128] == 7).all() and (room[-128:] == 7).all()
