@@ -511,7 +511,8 @@ int moe_vocab_distill_backward(const moe_config* cfg, const moe_vocab_dims* dims
  */
 typedef struct {
   int32_t B;                 /* sources; B Lq == cfg->G cfg->S */
-  int32_t Lq, Lk;            /* tokens and states of a source; B Lk up to 2^30 */
+  int32_t Lq, Lk;            /* tokens and states of a source; B Lk below 2^30; B kv_heads ceil(Lq heads / kv_heads / 32) and
+                                B kv_heads ceil(Lk / 32) below 2^24 */
   int32_t heads, kv_heads;   /* heads / kv_heads: 1, 2, 4, 8, 16 or 32; heads d below 2^23, Lq heads / kv_heads below 2^29 */
   int32_t d;                 /* 64 or 128 */
 } moe_cross_dims;
@@ -525,8 +526,8 @@ int moe_cross_backward_workspace_bytes(const moe_config* cfg, const moe_cross_di
 int moe_cross_keys(const moe_config* cfg, const moe_cross_dims* dims, const void* mem, const void* wkv, void* kv, void* stream);
 
 /* in: u [G,S,M], kv as moe_cross_keys leaves it, src_len [B] i32 or NULL (all states hold), wq [M,A], wo [A,M].  out [G,S,M].
- * ws >= moe_cross_workspace_bytes, 256-byte aligned.  bf16: q, the probabilities and ctx are rounded once each (the probabilities
- * of calls with few tokens are not); softmax statistics and sums are fp32, sums in a fixed order. */
+ * ws >= moe_cross_workspace_bytes, 256-byte aligned.  bf16: q, ctx and, where a block has 128 columns (many tokens), the
+ * probabilities are rounded once each; softmax statistics and sums are fp32, sums in a fixed order. */
 int moe_cross_attention(const moe_config* cfg, const moe_cross_dims* dims, const void* u, const void* kv, const int32_t* src_len,
                         const void* wq, const void* wo, void* out, void* ws, size_t ws_bytes, void* stream);
 
@@ -554,7 +555,7 @@ int moe_cross_attention_backward(const moe_config* cfg, const moe_cross_dims* di
 #define MOE_PREFERENCE_LOGISTIC 0
 #define MOE_PREFERENCE_SQUARED 1
 typedef struct {
-  int32_t P;                 /* pairs of sequences: 2p is preferred to 2p + 1 */
+  int32_t P;                 /* pairs of sequences: 2p is preferred to 2p + 1; below 2^24 */
   int32_t V;                 /* entries of the vocabulary */
   int32_t kind;              /* MOE_PREFERENCE_ */
   double beta, smoothing;    /* beta > 0; smoothing in [0, 1), of the logistic loss */

@@ -365,6 +365,9 @@ int check_cross(const moe_config* cfg, const moe_cross_dims* d) {
   if ((d->d != 64 && d->d != 128) || (share & (share - 1)) != 0 || share > 32) return MOE_EUNSUPPORTED;
   if ((long long)d->heads * d->d > 0x7fffffLL || (long long)d->B * d->Lk > 0x3fffffffLL) return MOE_EUNSUPPORTED;
   if ((long long)d->Lq * share >= 1LL << 29) return MOE_EUNSUPPORTED;
+  // blocks of 256 threads, 32 columns or states at least, of which a launch has less than 2^32 threads
+  const long long pairs = (long long)d->B * d->kv_heads, most = 1LL << 24;
+  if (pairs >= most || pairs * (((long long)d->Lq * share + 31) / 32) >= most || pairs * ((d->Lk + 31LL) / 32) >= most) return MOE_EUNSUPPORTED;
   return MOE_OK;
 }
 moe::CrossShape cross_shape(const moe_cross_dims& d) { return {d.B, d.Lq, d.Lk, d.heads, d.kv_heads, d.d}; }
@@ -458,7 +461,7 @@ int check_preference(const moe_config* cfg, const moe_preference_dims* d) {
   if (rc != MOE_OK) return rc;
   if (d == nullptr || d->P < 1 || d->V < 1 || (d->kind != MOE_PREFERENCE_LOGISTIC && d->kind != MOE_PREFERENCE_SQUARED)) return MOE_EINVAL;
   if (!(d->beta > 0.0 && d->beta < INFINITY) || !(d->smoothing >= 0.0 && d->smoothing < 1.0)) return MOE_EINVAL;
-  return d->P > 1 << 29 ? MOE_EUNSUPPORTED : MOE_OK;
+  return d->P >= 1 << 24 ? MOE_EUNSUPPORTED : MOE_OK;           // (a block of 256 threads each)
 }
 int policy_call(const moe_config* cfg, const moe_policy_dims* d, const moe::PolicyCall& a, bool backward, void* stream) {
   const int rc = check_config(cfg);

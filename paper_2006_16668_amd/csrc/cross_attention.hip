@@ -872,7 +872,6 @@ int forward(const CrossShape& s, const CrossPlan& plan, const bf16_t* q, const b
   if (prepare_kernels<D>() != MOE_OK) return MOE_EHIP;
   const int per = plan.few ? 32 : 128;
   const long long blocks = s.B * s.kv_heads * ((s.columns() + per - 1) / per) * plan.splits;
-  if (blocks > 0x7fffffffLL) return MOE_EUNSUPPORTED;
   const CrossGeo g(s);
   const dim3 grid((unsigned)blocks);
   if (plan.few) hipLaunchKernelGGL((cross_few_kernel<D>), grid, dim3(64 * kFewWaves), kLdsFew<D>, st, g, q, kv, src_len, ctx, lse, parts);
@@ -894,7 +893,6 @@ int backward(const CrossShape& s, const bf16_t* q, const bf16_t* kv, const int32
   if (prepare_kernels<D>() != MOE_OK || compute_units(&cus) != MOE_OK) return MOE_EHIP;
   const long long blocks = s.B * s.kv_heads * ((s.columns() + 127) / 128), blocks1 = s.B * s.kv_heads * ((s.Lk + 127) / 128),
                   blocks2 = s.B * s.kv_heads * ((s.Lk + 255) / 256);
-  if (blocks > 0x7fffffffLL || blocks1 > 0x7fffffffLL) return MOE_EUNSUPPORTED;
   const CrossGeo g(s);
   hipLaunchKernelGGL((cross_dq_kernel<D>), dim3((unsigned)blocks), dim3(256), kLdsQ<D>, st, g, q, kv, src_len, ctx, dctx, lse, dq, dvec);
   // two tiles of 32 states per wavefront where that takes fewer rounds of blocks (1.46 times as long each: attention_dkv_wide)
@@ -907,14 +905,14 @@ int backward(const CrossShape& s, const bf16_t* q, const bf16_t* kv, const int32
   return check_launch();
 }
 
-// 16 bytes a thread: rows of states that hold, zeros for the others
+// 16 bytes at a time: rows of states that hold, zeros for the others
 __global__ __launch_bounds__(256) void held_rows_kernel(const uint4* __restrict__ mem, const int32_t* __restrict__ src_len,
                                                         uint4* __restrict__ out, int Lk, int vecs, long long total) {
-  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-  if (i >= total) return;
-  const long long row = i / vecs, b = row / Lk;
-  const int n = src_len[b];
-  out[i] = (int)(row - b * Lk) < n ? mem[i] : uint4{0u, 0u, 0u, 0u};
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
+    const long long row = i / vecs, b = row / Lk;
+    const int n = src_len[b];
+    out[i] = (int)(row - b * Lk) < n ? mem[i] : uint4{0u, 0u, 0u, 0u};
+  }
 }
 
 }  // namespace
@@ -926,14 +924,16 @@ int prepare_cross_attention() {
 
 // Which form a forward call takes, by what both are expected to take (us).  A block of 128 columns walks its states in steps, two blocks on a unit
 // (fp32: one at a time multiplies); one of 32 columns shares them among its wavefronts and `splits` blocks, which cost a launch to join and
-// bring only as much memory as they have units.  Source by source measured (bf16, d 128 unless said; 128 / 32 columns in the
-// best number of ranges): 64 x 1 token, 410 to 2048 states, 16 heads 120 / 128; 1 x 4, 53 5.0 / 6.1; 1 x 1, 1000 23.7 / 11.1 (8);
-// 1 x 1, 8000 155 / 24.5 (16); 8 x 1, 1000 23.1 / 19.1 (2); 4 x 8, 4000, 2 key heads 82 / 17.0 (16); 16 x 1, 2000, 8 heads of 64 28.1 / 16.4 (4).
+// bring only as much memory as they have units.  us, 128 / 32 columns in the best number of ranges, bf16, heads of 128: 64 x 1 tokens, 410 to 2048
+// states, 16 heads 120 / 128; 1 x 4, 53 5.0 / 6.1; 1 x 1, 1000 23.7 / 10.1 (8); 1 x 1, 8000 155 / 23 (16); 8 x 1, 1000 23.2 / 19.1 (2); 4 x 8, 4000, 2 key
+// heads of 16 82 / 13.7 (16); 4 x 64, 1000, 8 heads 26.9 / 14.2 (4); 3 x 700, up to 700, 4 heads 20.4 / 29; of 64: 16 x 1, 2000, 8 heads 28.2 / 16.9 (4);
+// 2 x 300, 2000 34.5 / 23.0 (2); 27 x 834, up to 100 18.9 / 47; fp32, of 64: 5 x 187, up to 411, 8 heads 40.8 / 16.3; 8 x 500, 500 59 / 64; 27 x 834, up to
+// 100 56 / 95.
 CrossPlan cross_plan(int act_dtype, const CrossShape& s) {
   constexpr double kUnits = 256;                               // of a whole device: the choice sizes a workspace
   const bool f32 = act_dtype == MOE_F32;
   const double pairs = (double)s.B * s.kv_heads, mb = pairs * s.Lk * 2 * s.d * (f32 ? 4 : 2) / 1e6;
-  const double step128 = f32 ? (s.d == 64 ? 3.5 : 7.0) : (s.d == 64 ? 0.75 : 1.2), step32 = f32 ? step128 : 0.75;
+  const double step128 = f32 ? (s.d == 64 ? 3.5 : 7.0) : (s.d == 64 ? 0.75 : 1.2), step32 = f32 ? step128 : s.d == 64 ? 1.1 : 1.7, ends = f32 ? 1 : 0;
   const int blocks = (s.Lk + 31) / 32;
   auto rounds = [](double n, double at_once) { return ceil(n / at_once); };
   auto longer = [](double a, double b) { return a > b ? a : b; };
@@ -941,7 +941,7 @@ CrossPlan cross_plan(int act_dtype, const CrossShape& s) {
   double least = 4 + longer(step128 * (f32 ? blocks : (blocks + 1) / 2) * rounds(pairs * ((s.columns() + 127) / 128), f32 ? kUnits : 2 * kUnits), mb / 5.0);
   for (int splits = 1; splits <= 64 && splits <= (blocks + 3) / 4; splits *= 2) {
     const double items = pairs * ((s.columns() + 31) / 32) * splits, at_once = !f32 && s.d == 64 ? 2 * kUnits : kUnits;
-    const double us = 6 + (splits > 1 ? 4 : 0) + longer(step32 * ((blocks + 4 * splits - 1) / (4 * splits)) * rounds(items, at_once),
+    const double us = 6 + (splits > 1 ? 4 : 0) + longer((step32 * ((blocks + 4 * splits - 1) / (4 * splits)) + ends) * rounds(items, at_once),
                                                        mb / 5.0 * (items < kUnits ? kUnits / items : 1.0));
     if (us < least) {
       least = us;
@@ -993,8 +993,8 @@ int launch_cross_attention_bwd(int act_dtype, const CrossShape& s, const void* q
 int launch_held_rows(int act_dtype, const void* mem, const int32_t* src_len, void* out, long long B, int Lk, int M, hipStream_t st) {
   const int vecs = M / (act_dtype == MOE_F32 ? 4 : 8);
   const long long total = B * Lk * vecs;
-  if ((total + 255) / 256 > 0xffffffLL) return MOE_EUNSUPPORTED;          // (a launch has less than 2^32 threads)
-  hipLaunchKernelGGL(held_rows_kernel, dim3((unsigned)((total + 255) / 256)), dim3(256), 0, st, static_cast<const uint4*>(mem), src_len,
+  const long long blocks = (total + 255) / 256, most = 1 << 16;
+  hipLaunchKernelGGL(held_rows_kernel, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, st, static_cast<const uint4*>(mem), src_len,
                      static_cast<uint4*>(out), Lk, vecs, total);
   return check_launch();
 }

@@ -350,7 +350,6 @@ inline bool share_columns(long long columns, int L, double ends) {
   {                                                                                                                \
     const int per = SPLIT ? 32 : 32 * kWaves;                                                                      \
     const long long blocks = s.B * s.kv_heads * ((COUNT + per - 1) / per) * (SPLITS);                              \
-    if (blocks > 0x7fffffffLL) return MOE_EUNSUPPORTED;                                                            \
     const dim3 grid((unsigned)blocks), threads(64 * kWaves);                                                       \
     if (s.d == 64) {                                                                                               \
       if (SPLIT) hipLaunchKernelGGL((KERNEL<64, true>), grid, threads, 0, st, g, __VA_ARGS__);                     \

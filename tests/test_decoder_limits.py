@@ -41,13 +41,29 @@ def backward(cfg=CFG, dims=None, at=None, fwd=0, ws=0):
 @pytest.mark.parametrize("dims,status", [
     (cross(B=3), EINVAL), (cross(Lq=0, B=0), EINVAL), (cross(Lk=0), EINVAL), (cross(heads=4, kv_heads=3), EINVAL), (cross(kv_heads=0), EINVAL),
     (cross(heads=-4), EINVAL), (cross(d=32), EUNSUPPORTED), (cross(d=96), EUNSUPPORTED), (cross(heads=6, kv_heads=2), EUNSUPPORTED),
-    (cross(heads=64, kv_heads=1), EUNSUPPORTED), (cross(heads=1 << 17, kv_heads=1 << 17), EUNSUPPORTED), (cross(Lk=1 << 30), EUNSUPPORTED)])
+    (cross(heads=64, kv_heads=1), EUNSUPPORTED), (cross(heads=1 << 17, kv_heads=1 << 17), EUNSUPPORTED), (cross(Lk=1 << 30), EUNSUPPORTED),
+    (cross(Lk=1 << 28), EUNSUPPORTED), (cross(Lk=(1 << 27) + 1, heads=64, kv_heads=64), EUNSUPPORTED)])
 def test_shapes_of_cross_attention(dims, status):
     n = SZ()
     for name in ("moe_cross_workspace_bytes", "moe_cross_train_workspace_bytes", "moe_cross_backward_workspace_bytes"):
         assert call(name, CFG, dims, [ctypes.cast(ctypes.pointer(n), VP)]) == status
     assert forward(dims=dims) == forward(dims=dims, name="moe_cross_attention_train") == backward(dims=dims) == status
     assert call("moe_cross_keys", CFG, dims, [VP(4096)] * 3 + [None]) == status
+
+
+def test_sizes_at_the_ends_of_what_a_launch_takes():
+    """Blocks of 256 threads: less than 2^24 of them, by columns and by states."""
+    n = SZ()
+    at = [ctypes.cast(ctypes.pointer(n), VP)]
+    for (G, S, dims, status) in (((1 << 20) - 1, 1, cross(B=(1 << 20) - 1, Lq=1, Lk=1, heads=16, kv_heads=16), 0),
+                                 (1 << 20, 1, cross(B=1 << 20, Lq=1, Lk=1, heads=16, kv_heads=16), EUNSUPPORTED),
+                                 (1, (1 << 25) - 32, cross(B=1, Lq=(1 << 25) - 32, Lk=1, heads=16, kv_heads=16), 0),
+                                 (1, (1 << 25) - 31, cross(B=1, Lq=(1 << 25) - 31, Lk=1, heads=16, kv_heads=16), EUNSUPPORTED),
+                                 (1, 1, cross(B=1, Lq=1, Lk=(1 << 25) - 32, heads=16, kv_heads=16), 0),
+                                 (1, 1, cross(B=1, Lq=1, Lk=(1 << 25) - 31, heads=16, kv_heads=16), EUNSUPPORTED),
+                                 (1, 1 << 24, cross(B=1, Lq=1 << 24, Lk=1, heads=32, kv_heads=1), EUNSUPPORTED)):
+        for name in ("moe_cross_workspace_bytes", "moe_cross_train_workspace_bytes", "moe_cross_backward_workspace_bytes"):
+            assert call(name, _C(G, S, 64, 64, 2, 1, 1), dims, at) == status, (name, G, S)
 
 
 def test_arguments_of_cross_attention():
@@ -77,6 +93,11 @@ def test_workspaces_grow_with_the_calls():
     assert 2 * n <= moe.moe_cross_workspace_bytes(sh, dims)
     assert 2 * n + rows * 16 * 4 <= moe.moe_cross_train_workspace_bytes(sh, dims)
     assert 2 * n + 2 * n + rows * 1024 * 2 <= moe.moe_cross_backward_workspace_bytes(sh, dims)
+
+
+def test_more_pairs_than_a_launch_takes():
+    for P, status in (((1 << 24) - 1, EINVAL), (1 << 24, EUNSUPPORTED)):       # (a missing address, found after)
+        assert call("moe_preference_loss", CFG, _PreferenceDims(P, 9, 0, 0.1, 0.0), [VP(0)] * 6 + [None]) == status
 
 
 NAN, INF = float("nan"), float("inf")

@@ -64,7 +64,8 @@ CASES = [(1, 1, 1, 1, 1, 64, None), (6, 1, 1, 2, 2, 128, "ends"), (6, 3, 64, 2, 
          (2, 1, 333, 32, 1, 64, "any"), (1, 515, 77, 2, 2, 64, None), (1, 1, 2000, 1, 1, 128, None), (40, 2, 190, 3, 3, 64, "any"),
          (130, 130, 70, 2, 2, 128, "any"),
          # two tiles of states a wavefront backward; as many ranges of states as there are; ranges, some of which a short source leaves empty
-         (40, 70, 200, 8, 8, 128, "any"), (1, 2, 8200, 1, 1, 64, None), (6, 4, 2500, 1, 1, 128, "ends"), (70, 31, 33, 4, 4, 128, "any")]
+         (40, 70, 200, 8, 8, 128, "any"), (1, 2, 8200, 1, 1, 64, None), (6, 4, 2500, 1, 1, 128, "ends"), (70, 31, 33, 4, 4, 128, "any"),
+         (2, 500, 890, 8, 8, 64, "any"), (1, 500, 500, 8, 8, 128, "any")]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
