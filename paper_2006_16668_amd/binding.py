@@ -67,6 +67,17 @@ class _VocabDims(ctypes.Structure):
     _fields_ = [("V", ctypes.c_int32), ("K", ctypes.c_int32), ("piece", ctypes.c_int32), ("temperature", ctypes.c_float)]
 
 
+_TORCH_DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def _kept(dims, make, key="_struct"):
+    """The C struct of dimensions that never change, made once (the calls only read it)."""
+    c = dims.__dict__.get(key)
+    if c is None:
+        c = dims.__dict__[key] = make()
+    return c
+
+
 @dataclass(frozen=True)
 class VocabDims:
     """V vocabulary entries, K teacher entries per token and the temperature of a distillation, entries worked on at a
@@ -114,7 +125,7 @@ class CrossDims:
         return self.kv_heads or self.heads
 
     def _c(self):
-        return _CrossDims(self.B, self.Lq, self.Lk, self.heads, self.key_heads, self.d)
+        return _kept(self, lambda: _CrossDims(self.B, self.Lq, self.Lk, self.heads, self.key_heads, self.d))
 
 
 @dataclass(frozen=True)
@@ -127,7 +138,7 @@ class PreferenceDims:
     kind: str = "logistic"
 
     def _c(self):
-        return _PreferenceDims(self.P, self.V, PREFERENCE_KINDS[self.kind], self.beta, self.smoothing)
+        return _kept(self, lambda: _PreferenceDims(self.P, self.V, PREFERENCE_KINDS[self.kind], self.beta, self.smoothing))
 
 
 @dataclass(frozen=True)
@@ -139,7 +150,8 @@ class PolicyDims:
     beta: float = 0.0
 
     def _c(self, adv_per_token):
-        return _PolicyDims(self.V, int(adv_per_token), self.clip_low, self.clip_high, self.beta)
+        return _kept(self, lambda: _PolicyDims(self.V, int(adv_per_token), self.clip_low, self.clip_high, self.beta),
+                     "_per_token" if adv_per_token else "_per_group")
 
 
 @dataclass(frozen=True)
@@ -167,11 +179,10 @@ class MoEShape:
 
     @property
     def torch_dtype(self):
-        return {"f32": torch.float32, "bf16": torch.bfloat16}[self.act_dtype]
+        return _TORCH_DTYPES[self.act_dtype]
 
     def _c(self) -> _Config:
-        return _Config(self.G, self.S, self.M, self.H, self.E, self.C,
-                       {"f32": MOE_F32, "bf16": MOE_BF16}[self.act_dtype])
+        return _kept(self, lambda: _Config(self.G, self.S, self.M, self.H, self.E, self.C, {"f32": MOE_F32, "bf16": MOE_BF16}[self.act_dtype]))
 
 
 def library_path() -> str:

@@ -9,6 +9,7 @@
 //             fill a tile of columns of few tokens, and the gradients of a shared head are one sum, in a fixed order.
 //   states    a source's own number of them, read on the device.  Rows past it are staged as zeros and their probabilities are
 //             0 (what memory holds there has no part); a source without any gives rows of zeros.
+//   lse       is kept in units of log2 (fp32: natural): the exponentials of the backward pass are powers of two.
 //   P, dS     are rounded to bf16 in front of the second products, as the self-attention of whole blocks does: three terms of them
 //             (attention_mfma.hip, RAGGED) cost a fifth more, and q, ctx and the results are rounded as much anyway.
 #include <float.h>
@@ -285,8 +286,8 @@ __global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossGeo g, const
   step(nkb - 1, std::true_type{});
   __syncthreads();                                             // the other wavefronts have read the last blocks
   const int c = w.col0 + r;
-  // row statistic for the backward pass: log sum_k exp(score) in natural-log units
-  if (lse != nullptr && hf == 0 && c < cols.count) lse[(size_t)w.bk * cols.count + c] = (m_run + log2f(l_run)) * 0.6931471805599453f;
+  // row statistic for the backward pass: log2 sum_k exp(score)
+  if (lse != nullptr && hf == 0 && c < cols.count) lse[(size_t)w.bk * cols.count + c] = m_run + log2f(l_run);
   const f32x16_t (&tiles)[1][DT] = reinterpret_cast<const f32x16_t (&)[1][DT]>(o);
   store_rows<D, CT>(tiles, 1.0f / l_run, lds0 + own, lane, [&](int row, int chunk, const u32x4_t& v) __attribute__((always_inline)) {
     if (w.col0 + row < cols.count) *reinterpret_cast<u32x4_t*>(ctx + head + cols.offset<D>(w.col0 + row) + 8 * chunk) = v;
@@ -426,7 +427,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void cross_few_kernel(CrossGeo g
   const size_t column = ((size_t)b * g.kv_heads + k) * cols.count + c;
   if (wave == 0 && hf == 0) {
     if (parts.splits > 1) parts.stats[column * parts.splits + split] = float2{m, l};
-    else if (lse != nullptr) lse[column] = n == 0 ? 0.f : (m + log2f(l)) * 0.6931471805599453f;
+    else if (lse != nullptr) lse[column] = n == 0 ? 0.f : m + log2f(l);
   }
   const float inv = n == 0 ? 0.f : 1.0f / l;
 #pragma unroll
@@ -480,7 +481,7 @@ __global__ __launch_bounds__(256) void cross_join_kernel(CrossGeo g, CrossParts 
       for (int i = 0; i < D / 64; ++i) v[i] = fmaf(x[j][i], __shfl(f, s + j, 64), v[i]);
   }
   const bool none = held_states(src_len, b, g.Lk) == 0;
-  if (lse != nullptr && lane == 0) lse[column] = none ? 0.f : F32 ? m + logf(l) : (m + log2f(l)) * 0.6931471805599453f;
+  if (lse != nullptr && lane == 0) lse[column] = none ? 0.f : F32 ? m + logf(l) : m + log2f(l);
   const float inv = none ? 0.f : 1.0f / l;
   T* const to = ctx + cols.base(b, k, D) + cols.offset<D>(c) + lane * (D / 64);
 #pragma unroll
@@ -583,7 +584,7 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(CrossGeo g, const bf16
     }
     dd += __shfl_xor(dd, 32, 64);
     if (hf == 0 && c < cols.count) dvec[(size_t)w.bk * cols.count + c] = dd;
-    lse2 = lse[(size_t)w.bk * cols.count + cols.within(c)] * 1.4426950408889634f;
+    lse2 = lse[(size_t)w.bk * cols.count + cols.within(c)];
 #pragma unroll
     for (int t = 0; t < DT; ++t) clear_acc(dq[0][t]);
   }
@@ -817,7 +818,7 @@ __global__ __launch_bounds__(256, 1) void cross_dkv_kernel(CrossGeo g, const bf1
             if constexpr (first % (4 * CT) == 0 && first + 4 * CT < 16 * CT) l4[(first / (4 * CT) + 1) % 2] = stat4(sst, t, first / (4 * CT) + 1);
 #pragma unroll
             for (int j = first; j < to; ++j)
-              p[j % CT][j / CT] = __builtin_amdgcn_exp2f(fmaf(p[j % CT][j / CT], sl2, -(l4[j / (4 * CT) % 2][j / CT % 4] * 1.4426950408889634f)));
+              p[j % CT][j / CT] = __builtin_amdgcn_exp2f(fmaf(p[j % CT][j / CT], sl2, -l4[j / (4 * CT) % 2][j / CT % 4]));
             if constexpr (LAST && to % (8 * CT) == 0) end_mask(p, t, to / CT - 8);
             if constexpr (u == KS + KS / 2 + 1) pt[0][pc] = pack8(p[pc], 0);
             if constexpr (u == 2 * KS - 1 && pc == 0) d4[0] = stat4(sst + 256, t, 0);
