@@ -78,6 +78,11 @@ __device__ __forceinline__ void store_rows(const f32x16_t (&acc)[CT][D / 32], fl
   }
 }
 
+// a b, rounded: the difference to a number that was computed so is exact
+__device__ __forceinline__ float rounded_product(float a, float b) {
+#pragma clang fp contract(off)
+  return a * b;
+}
 // the block's (source, key head), and the wavefront's first column of `blocks` blocks of 128 CT
 template <int CT> struct CrossWork {
   long long bk, b;
@@ -660,6 +665,101 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(CrossGeo g, const bf16
   });
 }
 
+// ---------------------------------------------------------------- dq (and D) of up to 64 states
+// D = sum p dP of the probabilities at hand.  Of few states dP - D is a difference of near numbers, of whose error the rounding of the stored ctx, in
+// rowsum(dO * ctx), is more than half (two states: dq off by 0.0053 in norm, 0.0038 without it); of one it is 0, as it is here to the last
+// bit: p is exactly 1.  K and V lie in LDS whole, the columns' rows come straight from memory.
+template <int D>
+__global__ __launch_bounds__(256, 2) void cross_dq_short_kernel(CrossGeo g, const bf16_t* __restrict__ q, const bf16_t* __restrict__ kv,
+                                                                const int32_t* __restrict__ src_len, const bf16_t* __restrict__ dctx,
+                                                                bf16_t* __restrict__ dqo, float* __restrict__ dvec) {
+  using GM = AttGeom<D>;
+  constexpr int CT = 1, KS = D / 16, DT = D / 32, kOwnBlock = 32 * CT * GM::kRow, kV = GM::kBlock;
+  extern __shared__ __attribute__((aligned(256))) unsigned char att_lds[];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)((lds_ptr)att_lds);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 31, hf = lane >> 5;
+  const CrossCols cols(g, D);
+  const CrossWork<CT> w(cols.count, g.kv_heads, wave);
+  const size_t head = cols.base(w.b, w.k, D), column = (size_t)w.bk * cols.count + w.col0 + r;
+  const int n = held_states(src_len, w.b, g.Lk), Akv = g.kv_heads * D;
+  if (n == 0) {                                                // (no state asks for D)
+    clear_columns<D>(dqo + head, cols, w.block0);
+    return;
+  }
+  const size_t ld = (size_t)2 * Akv;
+  const bf16_t* const keys = kv + (size_t)w.b * g.Lk * ld + (size_t)w.k * D;
+  const bool live = w.col0 < cols.count;
+  uint32_t off[GM::kCopies];
+  copy_offsets<D>(off, ld, wave, lane);
+#pragma unroll
+  for (int x = 0; x < GM::kCopies; ++x) {
+    stage_rows<D>(lds0, keys, n, off, x, wave, lane);
+    stage_rows<D>(lds0 + kV, keys + Akv, n, off, x, wave, lane);
+  }
+  const size_t row = head + cols.offset<D>(cols.within(w.col0 + r));
+  u32x4_t qf[KS], dof[KS];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    qf[s] = *reinterpret_cast<const u32x4_t*>(q + row + 16 * s + 8 * hf);
+    dof[s] = *reinterpret_cast<const u32x4_t*>(dctx + row + 16 * s + 8 * hf);
+  }
+  wait_all_copies();
+  __syncthreads();
+  f32x16_t dq[CT][DT];
+  const float scale = 1.0f / sqrtf((float)D), sl2 = 1.4426950408889634f * scale;
+  if (live) {
+    const AttReads<D> rd(lds0, lane);
+    f32x16_t sc[2], dp[2];
+    float m = -FLT_MAX, sum = 0.f, dsum = 0.f;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int x = 0; x < KS; ++x) {
+        sc[t] = MOE_MFMA(rd.row(0, t, x), qf[x], x == 0 ? f32x16_t{} : sc[t]);
+        dp[t] = MOE_MFMA(rd.row(kV, t, x), dof[x], x == 0 ? f32x16_t{} : dp[t]);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        sc[t][i] = 32 * t + 8 * (i >> 2) + 4 * hf + (i & 3) < n ? rounded_product(sc[t][i], sl2) : -INFINITY;
+        m = fmaxf(m, sc[t][i]);
+      }
+    }
+    m = fmaxf(m, __shfl_xor(m, 32, 64));
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        sc[t][i] = __builtin_amdgcn_exp2f(sc[t][i] - m);
+        sum += sc[t][i];
+        dsum += sc[t][i] * dp[t][i];
+      }
+    sum += __shfl_xor(sum, 32, 64);
+    dsum += __shfl_xor(dsum, 32, 64);
+    const float inv = 1.0f / sum;
+    dsum *= inv;
+    if (hf == 0 && w.col0 + r < cols.count) dvec[column] = dsum;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) dq[0][dt] = f32x16_t{};
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[t][i] *= inv * (dp[t][i] - dsum);
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const u32x4_t f = pack8(sc[t], 8 * x);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) dq[0][dt] = MOE_MFMA(rd.transposed(0, 32 * t + 16 * x, dt), f, dq[0][dt]);
+      }
+    }
+  }
+  __syncthreads();                                             // K and V are read: the results go through their places
+  if (!live) return;
+  store_rows<D, CT>(dq, scale, lds0 + wave * kOwnBlock, lane, [&](int i, int chunk, const u32x4_t& v) __attribute__((always_inline)) {
+    if (w.col0 + i < cols.count) *reinterpret_cast<u32x4_t*>(dqo + head + cols.offset<D>(w.col0 + i) + 8 * chunk) = v;
+  });
+}
+
 // ---------------------------------------------------------------- dK, dV
 template <int D, int CT>
 __global__ __launch_bounds__(256, 1) void cross_dkv_kernel(CrossGeo g, const bf16_t* __restrict__ q, const bf16_t* __restrict__ kv,
@@ -852,6 +952,8 @@ __global__ __launch_bounds__(256, 1) void cross_dkv_kernel(CrossGeo g, const bf1
 template <int D> constexpr int kLdsFew = kFewWaves * 2 * 64 * AttGeom<D>::kRow;
 template <int D> constexpr int kLdsForward = 4 * AttGeom<D>::kBlock;
 template <int D> constexpr int kLdsQ = 5 * AttGeom<D>::kBlock;
+template <int D> constexpr int kLdsQShort = 2 * AttGeom<D>::kBlock;
+static_assert(kLdsQShort<128> <= 65536, "without a raised limit");
 template <int D, int CT> constexpr int kLdsKV = 2 * (2 * AttGeom<D>::kBlock + 512) + 128 * CT * AttGeom<D>::kRow;
 
 template <int D>
@@ -895,7 +997,8 @@ int backward(const CrossShape& s, const bf16_t* q, const bf16_t* kv, const int32
   const long long blocks = s.B * s.kv_heads * ((s.columns() + 127) / 128), blocks1 = s.B * s.kv_heads * ((s.Lk + 127) / 128),
                   blocks2 = s.B * s.kv_heads * ((s.Lk + 255) / 256);
   const CrossGeo g(s);
-  hipLaunchKernelGGL((cross_dq_kernel<D>), dim3((unsigned)blocks), dim3(256), kLdsQ<D>, st, g, q, kv, src_len, ctx, dctx, lse, dq, dvec);
+  if (s.Lk <= 64) hipLaunchKernelGGL((cross_dq_short_kernel<D>), dim3((unsigned)blocks), dim3(256), kLdsQShort<D>, st, g, q, kv, src_len, dctx, dq, dvec);
+  else hipLaunchKernelGGL((cross_dq_kernel<D>), dim3((unsigned)blocks), dim3(256), kLdsQ<D>, st, g, q, kv, src_len, ctx, dctx, lse, dq, dvec);
   // two tiles of 32 states per wavefront where that takes fewer rounds of blocks (1.46 times as long each: attention_dkv_wide)
   if constexpr (D == 128)
     if (1.46 * (double)((blocks2 + cus - 1) / cus) < (double)((blocks1 + cus - 1) / cus)) {

@@ -173,7 +173,9 @@ __global__ __launch_bounds__(64 * kWaves, 1) void cross_f32_dq_kernel(CrossGeo g
     for (int j = 0; j < 4; ++j) part[j] = fmaf(gf.v[i][j], kf.v[i][j], part[j]);
   float dd = (part[0] + part[1]) + (part[2] + part[3]);
   dd += __shfl_xor(dd, 32, 64);
-  if (hf == 0 && c < cols.count && (!SPLIT || wave == 0)) dvec[column] = dd;
+  const int nkb = (n + 31) / 32;
+  // (one block of states: see score_gradients)
+  if (nkb > 1 && hf == 0 && c < cols.count && (!SPLIT || wave == 0)) dvec[column] = dd;
   const float ls = lse[column];
   const float scale = 1.0f / sqrtf((float)D);
   auto load_keys = [&](int kb) __attribute__((always_inline)) {
@@ -184,20 +186,28 @@ __global__ __launch_bounds__(64 * kWaves, 1) void cross_f32_dq_kernel(CrossGeo g
   };
   f32x16_t dq[D / 32];
   clear<D>(dq);
-  const int nkb = (n + 31) / 32;
-  auto score_gradients = [&](int kb, const f32x16_t& s, f32x16_t& ds) __attribute__((always_inline)) {
+  // Up to 32 states: D = sum p dP of the probabilities at hand, without the rounding of ctx: of one state p is exactly 1, and dP - D is 0.
+  auto score_gradients = [&](int kb, f32x16_t& s, f32x16_t& ds) __attribute__((always_inline)) {
+#pragma clang fp contract(off)
+    float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      ds[i] = expf(s[i] * scale - ls) * (ds[i] - dd) * scale;
-      if (32 * kb + 8 * (i >> 2) + 4 * hf + (i & 3) >= n) ds[i] = 0.f;
+      s[i] = 32 * kb + 8 * (i >> 2) + 4 * hf + (i & 3) < n ? expf(s[i] * scale - ls) : 0.f;
+      sum += s[i] * ds[i];
     }
+    if (nkb == 1) {                                            // uniform
+      dd = sum + __shfl_xor(sum, 32, 64);
+      if (hf == 0 && c < cols.count) dvec[column] = dd;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) ds[i] = s[i] == 0.f ? 0.f : s[i] * (ds[i] - dd) * scale;
   };
   if constexpr (SPLIT) {
     if (wave < nkb) load_keys(wave);
     for (int kb = wave; kb < nkb; kb += kWaves) {
       Rows<D> kr;
       kr.load(keys, ld, 32 * kb, n, r, hf);
-      const f32x16_t s = over_d<D>(kf, qf);
+      f32x16_t s = over_d<D>(kf, qf);
       f32x16_t ds = over_d<D>(vf, gf);
       load_keys(kb + kWaves);
       score_gradients(kb, s, ds);
@@ -212,7 +222,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void cross_f32_dq_kernel(CrossGeo g
       next.put(ks, vs, kb, n);
       __syncthreads();
       if (kb + 1 < nkb) next.fetch(keys, ld, keys + Akv, ld, kb + 1, n);
-      const f32x16_t s = over_d<D>(Staged<D>{ks, r, hf}, qf);
+      f32x16_t s = over_d<D>(Staged<D>{ks, r, hf}, qf);
       f32x16_t ds = over_d<D>(Staged<D>{vs, r, hf}, gf);
       score_gradients(kb, s, ds);
       over_rows<D>(dq, Staged<D>{ks, r, hf}, ds);
