@@ -578,7 +578,7 @@ typedef struct {
   int32_t V;                 /* entries of the vocabulary */
   int32_t adv_per_token;     /* adv is [G,S], or 0: [G] */
   double clip_low, clip_high;/* the ratio is bounded to 1 - clip_low .. 1 + clip_high; 0 <= clip_low <= 1, clip_high >= 0 */
-  double beta;               /* of the KL term, >= 0 and finite; 0: without one */
+  double beta;               /* of the KL term, >= 0 and finite in fp32; 0: without one */
 } moe_policy_dims;
 
 /* r = exp(old_nll - nll), x = nll - ref_nll, per token:

@@ -1,6 +1,7 @@
 // C ABI of the library: argument checks, workspace carving, kernel sequencing.
 // Every step of the layer runs in the kernels of gate.hip, dispatch_combine.hip
 // and expert_gemm.hip; nothing here computes.
+#include <float.h>
 #include <math.h>
 #include <mutex>
 #include "common.h"
@@ -468,7 +469,7 @@ int policy_call(const moe_config* cfg, const moe_policy_dims* d, const moe::Poli
   if (rc != MOE_OK) return rc;
   if (d == nullptr || d->V < 1 || (d->adv_per_token != 0 && d->adv_per_token != 1)) return MOE_EINVAL;
   if (!(d->clip_low >= 0.0 && d->clip_low <= 1.0) || !(d->clip_high >= 0.0 && d->clip_high < INFINITY) ||
-      !(d->beta >= 0.0 && d->beta < INFINITY))
+      !(d->beta >= 0.0 && d->beta <= FLT_MAX))               // (fp32 in the kernel)
     return MOE_EINVAL;
   if (a.ref == nullptr && d->beta != 0.0) return MOE_EINVAL;
   const void* req[] = {a.nll, a.old_nll, a.adv, a.target, backward ? a.dloss : a.nll, backward ? a.dnll : a.loss};

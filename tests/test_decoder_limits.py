@@ -117,6 +117,13 @@ def test_policies_refused(d):
         assert call(name, CFG, _PolicyDims(*d), [VP(4096)] * 7 + [None]) == EINVAL
 
 
+@pytest.mark.parametrize("beta", [3.5e38, 1e39, 1e300])
+def test_weights_of_the_kl_term_past_fp32(beta):
+    """The term is formed in fp32: such a weight would be infinite there, and the loss of a token whose term is 0 NaN."""
+    for name in ("moe_policy_loss", "moe_policy_loss_backward"):
+        assert call(name, CFG, _PolicyDims(9, 0, 0.2, 0.2, beta), [VP(4096)] * 7 + [None]) == EINVAL
+
+
 def test_addresses_of_the_losses():
     pd, qd = _PreferenceDims(2, 9, 0, 0.1, 0.0), _PolicyDims(9, 1, 0.2, 0.2, 0.1)
     for name, dims, n, optional in (("moe_preference_loss", pd, 6, ()), ("moe_preference_loss_backward", pd, 5, ()), ("moe_policy_loss", qd, 7, (6,)),
