@@ -95,15 +95,21 @@ __global__ __launch_bounds__(1024) void gradient_norm_kernel(const double* __res
   if (threadIdx.x == 0) *norm = (float)sqrt(s);
 }
 
+// A scale as m 2^e, m in [1/2, 1]: max_norm / norm may be below the normal numbers of fp32 where the clipped gradients are not.
+struct Scale {
+  float m;
+  int e;
+  __device__ __forceinline__ float operator()(float x) const { return __builtin_amdgcn_ldexpf(x * m, e); }
+};
 template <typename T, bool STREAM>
-__device__ __forceinline__ void scale_chunk(const Chunk& c, float scale) {
+__device__ __forceinline__ void scale_chunk(const Chunk& c, const Scale& scale) {
   constexpr int E = Vec16<T>::kElts, AHEAD = 4;
   const unsigned vecs = c.bytes / 16;
   auto scaled = [&](const uint4& v) __attribute__((always_inline)) {
     float f[E];
     Vec16<T>::unpack(v, f);
 #pragma unroll
-    for (int i = 0; i < E; ++i) f[i] *= scale;
+    for (int i = 0; i < E; ++i) f[i] = scale(f[i]);
     return Vec16<T>::pack(f);
   };
   typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
@@ -126,7 +132,7 @@ __device__ __forceinline__ void scale_chunk(const Chunk& c, float scale) {
   const unsigned tail = (c.bytes - vecs * 16) / sizeof(T);
   if (threadIdx.x < tail) {
     const T* from = reinterpret_cast<const T*>(c.src + vecs * 16) + threadIdx.x;
-    Elt<T>::store(reinterpret_cast<T*>(c.dst + vecs * 16) + threadIdx.x, Elt<T>::load(from) * scale);
+    Elt<T>::store(reinterpret_cast<T*>(c.dst + vecs * 16) + threadIdx.x, scale(Elt<T>::load(from)));
   }
 }
 __device__ __forceinline__ void copy_chunk(const Chunk& c) {
@@ -150,7 +156,9 @@ __global__ __launch_bounds__(256) void clip_gradients_kernel(Table tab, const fl
     if (c.dst != c.src) copy_chunk(c);
     return;
   }
-  const float scale = (float)(max_norm / (double)n);
+  int e = 0;
+  const float m = (float)frexp(max_norm / (double)n, &e);
+  const Scale scale{m, e};
   if (c.f32) scale_chunk<float, STREAM>(c, scale);
   else scale_chunk<bf16_t, STREAM>(c, scale);
 }

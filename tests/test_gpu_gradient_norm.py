@@ -74,6 +74,21 @@ def test_values_whose_squares_leave_fp32(value):
     assert got == float("inf") if want > 3.4028235e38 else abs(got - want) <= U * want + 2.0 ** -150
 
 
+@pytest.mark.parametrize("norm, limit", [(1e20, 1e-25), (1e30, 1e-12), (3e38, 1e-5), (3e38, 1e-40), (1e20, 1e-18)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_scales_below_the_normal_numbers(norm, limit, dtype):
+    """limit / norm may be below 2^-126 (or the least number of fp32) where the clipped gradients are not: they keep their digits.  The
+    mantissa's rounding, the product's and the result's, U each or half a step; below 2^-126 half of the least step, twice."""
+    t = torch.tensor([1.0, -0.75, 0.3, 1e-3, 0.0], device=DEV).repeat(500) * (norm / 4)
+    t = t.to(dtype)
+    out = torch.full_like(t, float("nan"))
+    n = torch.tensor([norm], device=DEV)
+    moe.moe_clip_gradients(moe.GradientList([t], [out]), n, limit)
+    want = t.double() * (limit / float(n))
+    least = 2.0 ** -149 if dtype == torch.float32 else 2.0 ** -133
+    assert ((out.double() - want).abs() <= (HALF[dtype] * 1.01 + 3 * U) * want.abs() + 1.01 * least).all()
+
+
 @pytest.mark.parametrize("bad", [float("inf"), float("nan"), -float("inf")])
 def test_a_norm_that_is_no_number_changes_nothing(bad):
     g = torch.Generator(device=DEV).manual_seed(1)
