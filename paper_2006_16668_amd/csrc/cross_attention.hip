@@ -304,6 +304,24 @@ __global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossGeo g, const
   });
 }
 
+// Start the copies of a wavefront's block of 32 states: rows of K, then of V, zeros from row `rows` on.
+template <int D>
+__device__ __forceinline__ void stage_few(uint32_t lds, const bf16_t* keys, int Akv, int rows, const uint32_t (&off)[32 * AttGeom<D>::kRow / 1024], int lane) {
+  using GM = AttGeom<D>;
+  constexpr int COPIES = 32 * GM::kRow / 1024;
+#pragma unroll
+  for (int x = 0; x < 2 * COPIES; ++x) {
+    const bf16_t* const from = x < COPIES ? keys : keys + Akv;
+    if (rows < 32) {
+      const int i = GM::kRowsPerCopy * (x % COPIES) + lane / GM::kChunks;
+      const uint64_t a = i < rows ? (uint64_t)(uintptr_t)from + off[x % COPIES] : (uint64_t)(uintptr_t)&att_zero_line;
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds + x * 1024), "v"(a) : "memory");
+    } else {
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds + x * 1024), "v"(off[x % COPIES]), "s"(from) : "memory");
+    }
+  }
+}
+
 // ---------------------------------------------------------------- forward of few columns
 // A block's wavefronts share 32 columns and take blocks of 32 states in turn, each through two places of its own in LDS, one on its
 // way while the other is used: no barrier, 64 KB (d 128) on their way to a compute unit.  Memory bounds it, so the products are
@@ -343,22 +361,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void cross_few_kernel(CrossGeo g
     const int at = GM::kRowsPerCopy * x + lane / GM::kChunks;
     off[x] = (uint32_t)(at * ld * 2) + 16 * ((lane % GM::kChunks) ^ att_swizzle<D>(at));
   }
-  // block kb to place p: K rows, V rows (zeros past the end)
   auto start = [&](int kb, int p) __attribute__((always_inline)) {
-    const uint32_t at = lds0 + (2 * wave + p) * kPlace;
-    const bf16_t* const src = keys + (size_t)32 * kb * ld;
-    const int rows = n - 32 * kb;
-#pragma unroll
-    for (int x = 0; x < 2 * COPIES; ++x) {
-      const bf16_t* const from_ = x < COPIES ? src : src + Akv;
-      if (rows < 32) {
-        const int i = GM::kRowsPerCopy * (x % COPIES) + lane / GM::kChunks;
-        const uint64_t a = i < rows ? (uint64_t)(uintptr_t)from_ + off[x % COPIES] : (uint64_t)(uintptr_t)&att_zero_line;
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at + x * 1024), "v"(a) : "memory");
-      } else {
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at + x * 1024), "v"(off[x % COPIES]), "s"(from_) : "memory");
-      }
-    }
+    stage_few<D>(lds0 + (2 * wave + p) * kPlace, keys + (size_t)32 * kb * ld, Akv, n - 32 * kb, off, lane);
   };
   const float sl2 = 1.4426950408889634f / sqrtf((float)D);
   const AttReads<D> rd(lds0, lane);
@@ -670,6 +674,117 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(CrossGeo g, const bf16
   });
 }
 
+// ---------------------------------------------------------------- dq (and D) of few columns
+// As the forward pass of few columns: 32 of them a block, whose wavefronts take blocks of 32 states in turn and add up their sums at the end.  A
+// wavefront's chain of blocks bounds it (40.5 -> 22.6 us for 1 x 128 tokens of 4 heads of 128, 1500 states: 16 blocks instead of 4, a quarter of the states each).
+template <int D>
+__global__ __launch_bounds__(64 * kFewWaves, 1) void cross_dq_few_kernel(CrossGeo g, const bf16_t* __restrict__ q, const bf16_t* __restrict__ kv,
+                                                              const int32_t* __restrict__ src_len, const bf16_t* __restrict__ ctx,
+                                                              const bf16_t* __restrict__ dctx, const float* __restrict__ lse,
+                                                              bf16_t* __restrict__ dqo, float* __restrict__ dvec) {
+  using GM = AttGeom<D>;
+  constexpr int W = kFewWaves, KS = D / 16, DT = D / 32, kHalf = 32 * GM::kRow, kPlace = 2 * kHalf, COPIES = kHalf / 1024;
+  extern __shared__ __attribute__((aligned(256))) unsigned char att_lds[];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)((lds_ptr)att_lds);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 31, hf = lane >> 5;
+  const CrossCols cols(g, D);
+  const int tiles = (cols.count + 31) / 32;
+  const unsigned item = xcd_contiguous(blockIdx.x, gridDim.x), pair = item / tiles;
+  const int k = __builtin_amdgcn_readfirstlane(pair % g.kv_heads), b = __builtin_amdgcn_readfirstlane(pair / g.kv_heads);
+  const int c = (int)(item % tiles) * 32 + r;
+  const size_t row = cols.base(b, k, D) + cols.offset<D>(cols.within(c));
+  const size_t column = ((size_t)b * g.kv_heads + k) * cols.count + cols.within(c);
+  const int n = held_states(src_len, b, g.Lk), Akv = g.kv_heads * D;
+  const size_t ld = (size_t)2 * Akv;
+  const bf16_t* const keys = kv + (size_t)b * g.Lk * ld + (size_t)k * D;
+  const int nkb = (n + 31) / 32;
+  uint32_t off[COPIES];
+#pragma unroll
+  for (int x = 0; x < COPIES; ++x) {
+    const int at = GM::kRowsPerCopy * x + lane / GM::kChunks;
+    off[x] = (uint32_t)(at * ld * 2) + 16 * ((lane % GM::kChunks) ^ att_swizzle<D>(at));
+  }
+  auto start = [&](int kb, int p) __attribute__((always_inline)) {
+    stage_few<D>(lds0 + (2 * wave + p) * kPlace, keys + (size_t)32 * kb * ld, Akv, n - 32 * kb, off, lane);
+  };
+  u32x4_t qf[KS], dof[KS];
+  float dd = 0.f;
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    qf[s] = *reinterpret_cast<const u32x4_t*>(q + row + 16 * s + 8 * hf);
+    dof[s] = *reinterpret_cast<const u32x4_t*>(dctx + row + 16 * s + 8 * hf);
+    const u32x4_t of = *reinterpret_cast<const u32x4_t*>(ctx + row + 16 * s + 8 * hf);
+    float gr[8], ov[8];
+    Vec16<bf16_t>::unpack(uint4{dof[s][0], dof[s][1], dof[s][2], dof[s][3]}, gr);
+    Vec16<bf16_t>::unpack(uint4{of[0], of[1], of[2], of[3]}, ov);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dd = fmaf(gr[i], ov[i], dd);
+  }
+  dd += __shfl_xor(dd, 32, 64);
+  const float lse2 = lse[column];
+  const float scale = 1.0f / sqrtf((float)D), sl2 = 1.4426950408889634f * scale;
+  const AttReads<D> rd(lds0, lane);
+  f32x16_t dq[DT];
+#pragma unroll
+  for (int t = 0; t < DT; ++t) dq[t] = f32x16_t{};
+  if (wave < nkb) start(wave, 0);
+  int p = 0;
+  for (int kb = wave; kb < nkb; kb += W, p ^= 1) {
+    if (kb + W < nkb) {
+      start(kb + W, p ^ 1);
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * COPIES) : "memory");
+    } else {
+      wait_all_copies();
+    }
+    const uint32_t place = (2 * wave + p) * kPlace;
+    f32x16_t s, dp;
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      s = MOE_MFMA(rd.row(place, 0, i), qf[i], i == 0 ? f32x16_t{} : s);
+      dp = MOE_MFMA(rd.row(place + kHalf, 0, i), dof[i], i == 0 ? f32x16_t{} : dp);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float e = __builtin_amdgcn_exp2f(fmaf(s[i], sl2, -lse2)) * (dp[i] - dd);
+      s[i] = 32 * kb + 8 * (i >> 2) + 4 * hf + (i & 3) >= n ? 0.f : e;
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const u32x4_t dsf = pack8(s, 8 * h);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) dq[dt] = MOE_MFMA(rd.transposed(place, 16 * h, dt), dsf, dq[dt]);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // the place is read before the next copies go there
+  }
+  // LDS: [wavefront][DT][16][64]; each wavefront adds up 32 values of d
+  typedef float __attribute__((address_space(3))) * lds_f_ptr;
+  auto at = [&](uint32_t byte) __attribute__((always_inline)) { return (lds_f_ptr)(uintptr_t)(lds0 + byte); };
+  __syncthreads();
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) *at(((wave * DT + t) * 16 + i) * 256 + lane * 4) = dq[t][i];
+  __syncthreads();
+  if (c >= cols.count) return;
+  if (wave == 0 && hf == 0) dvec[column] = dd;
+#pragma unroll
+  for (int dt = wave; dt < DT; dt += W) {
+    float v[16];                                               // d = 32 dt + 8 (i/4) + 4 hf + i%4 of column c
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      v[i] = 0.f;
+#pragma unroll
+      for (int x = 0; x < W; ++x) v[i] += *at(((x * DT + dt) * 16 + i) * 256 + lane * 4);
+      v[i] *= scale;
+    }
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      *reinterpret_cast<u32x2_t*>(dqo + row + 32 * dt + 8 * x + 4 * hf) =
+          u32x2_t{pack_bf16x2(v[4 * x], v[4 * x + 1]), pack_bf16x2(v[4 * x + 2], v[4 * x + 3])};
+  }
+}
+
 // ---------------------------------------------------------------- dq (and D) of up to 64 states
 // D = sum p dP of the probabilities at hand.  Of few states dP - D is a difference of near numbers, of whose error the rounding of the stored ctx, in
 // rowsum(dO * ctx), is more than half (two states: dq off by 0.0053 in norm, 0.0038 without it); of one it is 0, as it is here to the last
@@ -963,11 +1078,12 @@ template <int D, int CT> constexpr int kLdsKV = 2 * (2 * AttGeom<D>::kBlock + 51
 
 template <int D>
 int prepare_kernels() {
-  static LdsLimitOnce once, once_few, once_q, once_kv1, once_kv2;
+  static LdsLimitOnce once, once_few, once_q, once_qfew, once_kv1, once_kv2;
   static_assert(kLdsFew<D> >= kFewWaves * (128 * D + 512), "the wavefronts' sums and statistics");
   int rc = ensure_lds_limit(once, reinterpret_cast<const void*>(cross_forward_kernel<D>), kLdsForward<D>);
   if (rc == MOE_OK) rc = ensure_lds_limit(once_few, reinterpret_cast<const void*>(cross_few_kernel<D>), kLdsFew<D>);
   if (rc == MOE_OK) rc = ensure_lds_limit(once_q, reinterpret_cast<const void*>(cross_dq_kernel<D>), kLdsQ<D>);
+  if (rc == MOE_OK) rc = ensure_lds_limit(once_qfew, reinterpret_cast<const void*>(cross_dq_few_kernel<D>), kLdsFew<D>);
   if (rc == MOE_OK) rc = ensure_lds_limit(once_kv1, reinterpret_cast<const void*>(cross_dkv_kernel<D, 1>), (kLdsKV<D, 1>));
   if constexpr (D == 128)
     if (rc == MOE_OK) rc = ensure_lds_limit(once_kv2, reinterpret_cast<const void*>(cross_dkv_kernel<D, 2>), (kLdsKV<D, 2>));
@@ -1002,7 +1118,14 @@ int backward(const CrossShape& s, const bf16_t* q, const bf16_t* kv, const int32
   const long long blocks = s.B * s.kv_heads * ((s.columns() + 127) / 128), blocks1 = s.B * s.kv_heads * ((s.Lk + 127) / 128),
                   blocks2 = s.B * s.kv_heads * ((s.Lk + 255) / 256);
   const CrossGeo g(s);
+  // dq of few columns where its blocks run all at once: one a unit, two at d 64 if the other kernel's blocks leave half of the units idle.  us, blocks of
+  // 128 / 32 columns, on 256 units:  d 64  1 x 20 tokens, 1862 states, 2 key heads 19.4 / 11.4; 2 x 300, 2000 34.8 / 20.4; 2 x 1000, 1000 (512 blocks of 32)
+  // 21.9 / 17.6; 31 x 40, 200 (186 blocks of 128, 372 of 32) 7.3 / 8.0; 11 x 333, 777 25.6 / 44.2;  d 128  4 x 64, 1000 29.2 / 17.8; 16 x 64, 256 (256 of
+  // 32) 12.8 / 9.7; 3 x 700, 700 (264 of 32) 22.3 / 25.9; 4 x 400, 1000 32.5 / 36.6
+  const long long blocks32 = s.B * s.kv_heads * ((s.columns() + 31) / 32);
+  const bool few_dq = blocks32 <= cus || (D == 64 && blocks32 <= 2LL * cus && 2 * blocks <= cus);
   if (s.Lk <= 64) hipLaunchKernelGGL((cross_dq_short_kernel<D>), dim3((unsigned)blocks), dim3(256), kLdsQShort<D>, st, g, q, kv, src_len, dctx, dq, dvec);
+  else if (few_dq) hipLaunchKernelGGL((cross_dq_few_kernel<D>), dim3((unsigned)blocks32), dim3(64 * kFewWaves), kLdsFew<D>, st, g, q, kv, src_len, ctx, dctx, lse, dq, dvec);
   else hipLaunchKernelGGL((cross_dq_kernel<D>), dim3((unsigned)blocks), dim3(256), kLdsQ<D>, st, g, q, kv, src_len, ctx, dctx, lse, dq, dvec);
   // two tiles of 32 states per wavefront where that takes fewer rounds of blocks (1.46 times as long each: attention_dkv_wide)
   if constexpr (D == 128)

@@ -65,7 +65,11 @@ CASES = [(1, 1, 1, 1, 1, 64, None), (6, 1, 1, 2, 2, 128, "ends"), (4, 40, 1, 4, 
          (130, 130, 70, 2, 2, 128, "any"),
          # two tiles of states a wavefront backward; as many ranges of states as there are; ranges, some of which a short source leaves empty
          (40, 70, 200, 8, 8, 128, "any"), (1, 2, 8200, 1, 1, 64, None), (6, 4, 2500, 1, 1, 128, "ends"), (70, 31, 33, 4, 4, 128, "any"),
-         (2, 500, 890, 8, 8, 64, "any"), (1, 500, 500, 8, 8, 128, "any")]
+         (2, 500, 890, 8, 8, 64, "any"), (1, 500, 500, 8, 8, 128, "any"),
+         # dq in blocks of 128 columns: more blocks of 32 than the units take at once, with each end of the states
+         (33, 100, 130, 4, 4, 64, "ends"), (24, 100, 97, 4, 4, 128, "ends"), (33, 17, 130, 8, 4, 64, "ends"), (66, 40, 193, 4, 1, 128, "ends"),
+         # and as many as they take
+         (16, 63, 256, 8, 8, 128, "ends"), (2, 1000, 100, 8, 8, 64, "ends")]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
