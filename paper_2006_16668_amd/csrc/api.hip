@@ -402,7 +402,7 @@ CrossBwdWs carve_cross_bwd(const moe_config& c, const moe_cross_dims& d) {
   const size_t parts[] = {moe::dense_wgrad_partial_bytes(c.act_dtype, (long long)N, (int)A, c.M),
                           moe::dense_wgrad_partial_bytes(c.act_dtype, (long long)N, c.M, (int)A),
                           moe::dense_wgrad_partial_bytes(c.act_dtype, (long long)rows, c.M, Akv2)};
-  size_t most = 0;
+  size_t most = moe::cross_bwd_scratch_bytes(c.act_dtype, cross_shape(d));
   for (size_t p : parts) most = p > most ? p : most;
   w.wpart = take(most);
   w.total = off;
@@ -1180,7 +1180,7 @@ int moe_cross_attention_backward(const moe_config* cfg, const moe_cross_dims* di
   if (rc != MOE_OK) return rc;
   rc = moe::launch_cross_attention_bwd(cfg->act_dtype, cross_shape(*dims), fwd + f.q, kv, src_len, fwd + f.ctx, base + w.dctx,
                                        reinterpret_cast<const float*>(fwd + f.lse), base + w.dq, base + w.dkv,
-                                       reinterpret_cast<float*>(base + w.dvec), st);
+                                       reinterpret_cast<float*>(base + w.dvec), wpart, st);
   if (rc != MOE_OK) return rc;
   // q = u . wq
   rc = cross_gradients(*cfg, N, cfg->M, A, u, base + w.dq, wq, du, dwq, wpart, st);

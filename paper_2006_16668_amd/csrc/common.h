@@ -428,9 +428,12 @@ struct CrossShape {
 size_t cross_scratch_bytes(int act_dtype, const CrossShape& s);
 int launch_cross_attention(int act_dtype, const CrossShape& s, const void* q, const void* kv, const int32_t* src_len, void* ctx,
                            float* lse, void* scratch, hipStream_t st);
-// dvec: [B kv_heads columns] of scratch; dkv: zeros in the rows of states that do not hold
+// dvec: [B kv_heads columns] of scratch; dkv: zeros in the rows of states that do not hold; sums: cross_bwd_scratch_bytes()
+size_t cross_bwd_scratch_bytes(int act_dtype, const CrossShape& s);
 int launch_cross_attention_bwd(int act_dtype, const CrossShape& s, const void* q, const void* kv, const int32_t* src_len,
-                               const void* ctx, const void* dctx, const float* lse, void* dq, void* dkv, float* dvec, hipStream_t st);
+                               const void* ctx, const void* dctx, const float* lse, void* dq, void* dkv, float* dvec, float* sums, hipStream_t st);
+// out[i] = sum of partial[range][i] in order, rounded to bf16; elems a multiple of 8 (encoder_bwd.hip)
+int launch_add_ranges(const float* partial, int ranges, long long elems, void* out, hipStream_t st);
 // out = mem with zeros in those rows
 int launch_held_rows(int act_dtype, const void* mem, const int32_t* src_len, void* out, long long B, int Lk, int M, hipStream_t st);
 

@@ -37,6 +37,13 @@ struct CrossParts {
 // few: blocks of 32 columns whose wavefronts take the states' blocks in turn, in `splits` ranges; else blocks of 128 columns
 struct CrossPlan { bool few; int splits; };
 CrossPlan cross_plan(int act_dtype, const CrossShape& s);
+// Blocks of 64 columns in a range of dK's and dV's (bf16), by what the calls are expected to take (us): a block of 128 states walks its range's blocks in
+// steps, the ranges' sums cost a launch and their way to memory and back, and ranges are only made while all blocks run at once (a unit has two at d 64).
+// us of one range / the best number of them: 4 x 2000 tokens, 1000 states, 8 heads of 128 on one 455 / 87 (8), of 64 295 / 51 (16); 7 x 1561, up to 66, 2 on one
+// of 128 93 / 19 (16), of 64 61 / 16 (16); 1 x 2000, 60, 2 heads of 128 63 / 17 (12); 8 x 1000, 100, 8 heads of 64 24 / 18 (4), of 128 37 / 26 (4); 1 x 500, 500,
+// 8 heads of 64 14.5 / 15.9 (4).  Left to one range although more are a little faster: 3 x 700, up to 700, 4 heads of 128 28.2 / 24.8 (3); 2 x 1000, 1000, 8
+// heads of 128 39.3 / 37.2 (2).
+int cross_dkv_blocks(const CrossShape& s);
 
 // fp32 (cross_attention_f32.hip)
 int launch_cross_attention_f32(const CrossShape& s, const CrossPlan& plan, const float* q, const float* kv, const int32_t* src_len,

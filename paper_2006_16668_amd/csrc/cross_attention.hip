@@ -91,10 +91,13 @@ __device__ __forceinline__ float rounded_product(float a, float b) {
 // the block's (source, key head), and the wavefront's first column of `blocks` blocks of 128 CT
 template <int CT> struct CrossWork {
   long long bk, b;
-  int k, block0, col0;
-  __device__ __forceinline__ CrossWork(int count, int kv_heads, int wave) {
+  int k, block0, col0, range;
+  __device__ __forceinline__ CrossWork(int count, int kv_heads, int wave, unsigned ranges = 1) {
     const int blocks = (count + 128 * CT - 1) / (128 * CT);
-    const unsigned work = xcd_contiguous(blockIdx.x, gridDim.x), pair = work / blocks;
+    unsigned work = xcd_contiguous(blockIdx.x, gridDim.x);
+    range = __builtin_amdgcn_readfirstlane(work % ranges);
+    work /= ranges;
+    const unsigned pair = work / blocks;
     bk = pair;
     k = __builtin_amdgcn_readfirstlane(pair % kv_heads);
     b = __builtin_amdgcn_readfirstlane(pair / kv_heads);
@@ -881,11 +884,17 @@ __global__ __launch_bounds__(256, 2) void cross_dq_short_kernel(CrossGeo g, cons
 }
 
 // ---------------------------------------------------------------- dK, dV
-template <int D, int CT>
+// RANGES: of a range of the columns, as fp32 sums, which one more launch adds up in order.
+struct CrossRanges {
+  int count, blocks;         // ranges, and the blocks of 64 columns of each (the last may have fewer, none has none)
+  size_t elems;              // of dkv
+  float* sums;               // [ranges][dkv]
+};
+template <int D, int CT, bool RANGES = false>
 __global__ __launch_bounds__(256, 1) void cross_dkv_kernel(CrossGeo g, const bf16_t* __restrict__ q, const bf16_t* __restrict__ kv,
                                                            const int32_t* __restrict__ src_len, const bf16_t* __restrict__ dctx,
                                                            const float* __restrict__ lse, const float* __restrict__ dvec,
-                                                           bf16_t* __restrict__ dkv) {
+                                                           bf16_t* __restrict__ dkv, CrossRanges ranges) {
   using GM = AttGeom<D>;
   constexpr int KS = D / 16, DT = D / 32, kOwnBlock = 32 * CT * GM::kRow;
   constexpr int kGrad = GM::kBlock, kStats = 2 * GM::kBlock, kStage = kStats + 512;   // Q rows, dO rows, 64 lse, 64 D
@@ -896,16 +905,21 @@ __global__ __launch_bounds__(256, 1) void cross_dkv_kernel(CrossGeo g, const bf1
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 31, hf = lane >> 5;
   const CrossCols cols(g, D);
-  const CrossWork<CT> w(g.Lk, g.kv_heads, wave);
+  const CrossWork<CT> w(g.Lk, g.kv_heads, wave, RANGES ? ranges.count : 1);
   const int n = held_states(src_len, w.b, g.Lk), Akv = g.kv_heads * D;
   const size_t ld = (size_t)2 * Akv;
   const size_t states = (size_t)w.b * g.Lk * ld + (size_t)w.k * D;
   // zeros to the rows first .. first + count - 1 that there are, by `threads` threads of which this is number i0
+  using Out = std::conditional_t<RANGES, float, bf16_t>;
+  Out* out;
+  if constexpr (RANGES) out = ranges.sums + w.range * ranges.elems + states;
+  else out = dkv + states;
   auto clear = [&](int first, int count, int i0, int threads) __attribute__((always_inline)) {
-    for (int i = i0; i < count * (D / 8); i += threads) {
-      const int row = first + i / (D / 8);
+    constexpr int E = 16 / sizeof(Out);
+    for (int i = i0; i < count * (D / E); i += threads) {
+      const int row = first + i / (D / E);
       if (row >= g.Lk) return;
-      bf16_t* const at = dkv + states + (size_t)row * ld + 8 * (i % (D / 8));
+      Out* const at = out + (size_t)row * ld + E * (i % (D / E));
       *reinterpret_cast<u32x4_t*>(at) = u32x4_t{0u, 0u, 0u, 0u};
       *reinterpret_cast<u32x4_t*>(at + Akv) = u32x4_t{0u, 0u, 0u, 0u};
     }
@@ -921,7 +935,11 @@ __global__ __launch_bounds__(256, 1) void cross_dkv_kernel(CrossGeo g, const bf1
 
   uint32_t off[GM::kCopies];
   column_offsets<D>(off, cols, wave, lane);
-  const int nqb = (cols.count + 63) / 64;
+  int qb0 = 0, nqb = (cols.count + 63) / 64;
+  if constexpr (RANGES) {
+    qb0 = w.range * ranges.blocks;
+    nqb = qb0 + ranges.blocks < nqb ? qb0 + ranges.blocks : nqb;
+  }
   // copy x of block j: Q rows, dO rows, 64 values of lse and D
   auto start = [&](int j, int x) __attribute__((always_inline)) {
     const uint32_t st = lds0 + (j & 1) * kStage;
@@ -961,9 +979,9 @@ __global__ __launch_bounds__(256, 1) void cross_dkv_kernel(CrossGeo g, const bf1
   }
   __syncthreads();
 #pragma unroll
-  for (int x = 0; x < COPIES; ++x) start(0, x);
+  for (int x = 0; x < COPIES; ++x) start(qb0, x);
   if (!live) {                                                 // a wavefront without states that hold stages, and clears its rows
-    for (int qb = 0; qb + 1 < nqb; ++qb) {
+    for (int qb = qb0; qb + 1 < nqb; ++qb) {
       wait_all_copies();
       __syncthreads();
 #pragma unroll
@@ -1055,10 +1073,31 @@ __global__ __launch_bounds__(256, 1) void cross_dkv_kernel(CrossGeo g, const bf1
           if constexpr (x == 0) dst[1][pc] = pack8(ds[pc], 8);
         });
   };
-  for (int qb = 0; qb + 1 < nqb; ++qb) step(qb, std::false_type{});
+  for (int qb = qb0; qb + 1 < nqb; ++qb) step(qb, std::false_type{});
   step(nqb - 1, std::true_type{});
   settle_all(dk);
   settle_all(dv);
+  if constexpr (RANGES) {
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      const int at = w.col0 + 32 * c + r;
+      if (at >= g.Lk) continue;
+      float* const to = out + (size_t)at * ld + 4 * hf;
+#pragma unroll
+      for (int i = 0; i < 4 * DT; ++i) {                       // d = 8 i + 4 hf ..
+        f32x4_t k4 = {0.f, 0.f, 0.f, 0.f}, v4 = k4;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (at < n) {
+            k4[j] = dk[c][i / 4][4 * (i % 4) + j] * scale;
+            v4[j] = dv[c][i / 4][4 * (i % 4) + j];
+          }
+        *reinterpret_cast<f32x4_t*>(to + 8 * i) = k4;
+        *reinterpret_cast<f32x4_t*>(to + Akv + 8 * i) = v4;
+      }
+    }
+    return;
+  }
   auto put = [&](bf16_t* to) __attribute__((always_inline)) {
     return [=](int row, int chunk, const u32x4_t& v) __attribute__((always_inline)) {
       const int at = w.col0 + row;
@@ -1078,13 +1117,14 @@ template <int D, int CT> constexpr int kLdsKV = 2 * (2 * AttGeom<D>::kBlock + 51
 
 template <int D>
 int prepare_kernels() {
-  static LdsLimitOnce once, once_few, once_q, once_qfew, once_kv1, once_kv2;
+  static LdsLimitOnce once, once_few, once_q, once_qfew, once_kvr, once_kv1, once_kv2;
   static_assert(kLdsFew<D> >= kFewWaves * (128 * D + 512), "the wavefronts' sums and statistics");
   int rc = ensure_lds_limit(once, reinterpret_cast<const void*>(cross_forward_kernel<D>), kLdsForward<D>);
   if (rc == MOE_OK) rc = ensure_lds_limit(once_few, reinterpret_cast<const void*>(cross_few_kernel<D>), kLdsFew<D>);
   if (rc == MOE_OK) rc = ensure_lds_limit(once_q, reinterpret_cast<const void*>(cross_dq_kernel<D>), kLdsQ<D>);
   if (rc == MOE_OK) rc = ensure_lds_limit(once_qfew, reinterpret_cast<const void*>(cross_dq_few_kernel<D>), kLdsFew<D>);
   if (rc == MOE_OK) rc = ensure_lds_limit(once_kv1, reinterpret_cast<const void*>(cross_dkv_kernel<D, 1>), (kLdsKV<D, 1>));
+  if (rc == MOE_OK) rc = ensure_lds_limit(once_kvr, reinterpret_cast<const void*>(cross_dkv_kernel<D, 1, true>), (kLdsKV<D, 1>));
   if constexpr (D == 128)
     if (rc == MOE_OK) rc = ensure_lds_limit(once_kv2, reinterpret_cast<const void*>(cross_dkv_kernel<D, 2>), (kLdsKV<D, 2>));
   return rc;
@@ -1112,7 +1152,7 @@ int join(const CrossShape& s, const CrossParts& parts, const int32_t* src_len, T
 }
 template <int D>
 int backward(const CrossShape& s, const bf16_t* q, const bf16_t* kv, const int32_t* src_len, const bf16_t* ctx, const bf16_t* dctx,
-             const float* lse, bf16_t* dq, bf16_t* dkv, float* dvec, hipStream_t st) {
+             const float* lse, bf16_t* dq, bf16_t* dkv, float* dvec, float* sums, hipStream_t st) {
   int cus = 0;
   if (prepare_kernels<D>() != MOE_OK || compute_units(&cus) != MOE_OK) return MOE_EHIP;
   const long long blocks = s.B * s.kv_heads * ((s.columns() + 127) / 128), blocks1 = s.B * s.kv_heads * ((s.Lk + 127) / 128),
@@ -1127,13 +1167,20 @@ int backward(const CrossShape& s, const bf16_t* q, const bf16_t* kv, const int32
   if (s.Lk <= 64) hipLaunchKernelGGL((cross_dq_short_kernel<D>), dim3((unsigned)blocks), dim3(256), kLdsQShort<D>, st, g, q, kv, src_len, dctx, dq, dvec);
   else if (few_dq) hipLaunchKernelGGL((cross_dq_few_kernel<D>), dim3((unsigned)blocks32), dim3(64 * kFewWaves), kLdsFew<D>, st, g, q, kv, src_len, ctx, dctx, lse, dq, dvec);
   else hipLaunchKernelGGL((cross_dq_kernel<D>), dim3((unsigned)blocks), dim3(256), kLdsQ<D>, st, g, q, kv, src_len, ctx, dctx, lse, dq, dvec);
+  const int each = cross_dkv_blocks(s), blocks64 = (int)((s.columns() + 63) / 64);
+  const CrossRanges ranges{(blocks64 + each - 1) / each, each, (size_t)s.B * s.Lk * 2 * s.kv_heads * D, sums};
+  if (ranges.count > 1) {
+    hipLaunchKernelGGL((cross_dkv_kernel<D, 1, true>), dim3((unsigned)(blocks1 * ranges.count)), dim3(256), (kLdsKV<D, 1>), st, g, q, kv, src_len, dctx, lse, dvec, dkv, ranges);
+    const int rc = check_launch();
+    return rc != MOE_OK ? rc : launch_add_ranges(sums, ranges.count, (long long)ranges.elems, dkv, st);
+  }
   // two tiles of 32 states per wavefront where that takes fewer rounds of blocks (1.46 times as long each: attention_dkv_wide)
   if constexpr (D == 128)
     if (1.46 * (double)((blocks2 + cus - 1) / cus) < (double)((blocks1 + cus - 1) / cus)) {
-      hipLaunchKernelGGL((cross_dkv_kernel<D, 2>), dim3((unsigned)blocks2), dim3(256), (kLdsKV<D, 2>), st, g, q, kv, src_len, dctx, lse, dvec, dkv);
+      hipLaunchKernelGGL((cross_dkv_kernel<D, 2>), dim3((unsigned)blocks2), dim3(256), (kLdsKV<D, 2>), st, g, q, kv, src_len, dctx, lse, dvec, dkv, ranges);
       return check_launch();
     }
-  hipLaunchKernelGGL((cross_dkv_kernel<D, 1>), dim3((unsigned)blocks1), dim3(256), (kLdsKV<D, 1>), st, g, q, kv, src_len, dctx, lse, dvec, dkv);
+  hipLaunchKernelGGL((cross_dkv_kernel<D, 1>), dim3((unsigned)blocks1), dim3(256), (kLdsKV<D, 1>), st, g, q, kv, src_len, dctx, lse, dvec, dkv, ranges);
   return check_launch();
 }
 
@@ -1189,6 +1236,31 @@ size_t cross_scratch_bytes(int act_dtype, const CrossShape& s) {
   return p.splits > 1 ? align_up(columns * p.splits * sizeof(float2), 256) + columns * p.splits * s.d * sizeof(float) : 0;
 }
 
+int cross_dkv_blocks(const CrossShape& s) {
+  constexpr double kUnits = 256;                               // of a whole device: the choice sizes a workspace
+  const double blocks = (double)s.B * s.kv_heads * ((s.Lk + 127) / 128), at_once = s.d == 64 ? 2 * kUnits : kUnits;
+  const double step = s.d == 64 ? 1.18 : 1.8, mb = blocks * 128 * 2 * s.d * sizeof(float) / 1e6;
+  const int all = (int)((s.columns() + 63) / 64);
+  int best = all;
+  double least = 5 + step * all;
+  for (int ranges : {2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+    if (ranges > all || blocks * ranges > at_once) break;
+    const int each = (all + ranges - 1) / ranges;
+    const double us = 9 + step * each + 0.5 * mb * ranges;
+    if (us < least) {
+      least = us;
+      best = each;
+    }
+  }
+  return best;
+}
+
+size_t cross_bwd_scratch_bytes(int act_dtype, const CrossShape& s) {
+  if (act_dtype == MOE_F32) return 0;
+  const long long all = (s.columns() + 63) / 64, each = cross_dkv_blocks(s), ranges = (all + each - 1) / each;
+  return ranges > 1 ? (size_t)ranges * s.B * s.Lk * 2 * s.kv_heads * s.d * sizeof(float) : 0;
+}
+
 int launch_cross_attention(int act_dtype, const CrossShape& s, const void* q, const void* kv, const int32_t* src_len, void* ctx,
                            float* lse, void* scratch, hipStream_t st) {
   const CrossPlan plan = cross_plan(act_dtype, s);
@@ -1208,7 +1280,7 @@ int launch_cross_attention(int act_dtype, const CrossShape& s, const void* q, co
 }
 
 int launch_cross_attention_bwd(int act_dtype, const CrossShape& s, const void* q, const void* kv, const int32_t* src_len,
-                               const void* ctx, const void* dctx, const float* lse, void* dq, void* dkv, float* dvec, hipStream_t st) {
+                               const void* ctx, const void* dctx, const float* lse, void* dq, void* dkv, float* dvec, float* sums, hipStream_t st) {
   if (act_dtype == MOE_F32)
     return launch_cross_attention_f32_bwd(s, static_cast<const float*>(q), static_cast<const float*>(kv), src_len, static_cast<const float*>(ctx),
                                           static_cast<const float*>(dctx), lse, static_cast<float*>(dq), static_cast<float*>(dkv), dvec, st);
@@ -1218,8 +1290,8 @@ int launch_cross_attention_bwd(int act_dtype, const CrossShape& s, const void* q
   auto gb = static_cast<const bf16_t*>(dctx);
   auto dqb = static_cast<bf16_t*>(dq);
   auto dkb = static_cast<bf16_t*>(dkv);
-  return s.d == 64 ? backward<64>(s, qb, kb, src_len, c, gb, lse, dqb, dkb, dvec, st)
-                   : backward<128>(s, qb, kb, src_len, c, gb, lse, dqb, dkb, dvec, st);
+  return s.d == 64 ? backward<64>(s, qb, kb, src_len, c, gb, lse, dqb, dkb, dvec, sums, st)
+                   : backward<128>(s, qb, kb, src_len, c, gb, lse, dqb, dkb, dvec, sums, st);
 }
 
 int launch_held_rows(int act_dtype, const void* mem, const int32_t* src_len, void* out, long long B, int Lk, int M, hipStream_t st) {

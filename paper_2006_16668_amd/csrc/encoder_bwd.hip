@@ -490,6 +490,12 @@ __global__ __launch_bounds__(256) void splitk_reduce_kernel(const float* __restr
 
 }  // namespace
 
+int launch_add_ranges(const float* partial, int ranges, long long elems, void* out, hipStream_t st) {
+  hipLaunchKernelGGL(splitk_reduce_kernel, dim3((unsigned)((elems / 8 + 255) / 256)), dim3(256), 0, st, partial, ranges, elems,
+                     static_cast<uint4*>(out));
+  return check_launch();
+}
+
 // Weight gradient of a dense layer, dW [in,out] = X^T dY over `rows` tokens.  Its output has few tiles but a very
 // long K (the tokens), so one product alone would leave most compute units idle: the tokens are cut into ranges
 // (dense_wgrad_plan) that run as a batch with fp32 results, and one pass adds the ranges in order and rounds once.
@@ -517,10 +523,7 @@ int launch_dense_grads(const moe_config& c, long long rows, int in, int out, con
   }
   if (rc != MOE_OK) return rc;
   if (plan.splits > 1) {
-    const long long elems = (long long)in * out;
-    hipLaunchKernelGGL(splitk_reduce_kernel, dim3((unsigned)((elems / 8 + 255) / 256)), dim3(256), 0, st,
-                       partial, plan.splits, elems, static_cast<uint4*>(dW));
-    if ((rc = check_launch()) != MOE_OK) return rc;
+    if ((rc = launch_add_ranges(partial, plan.splits, (long long)in * out, dW, st)) != MOE_OK) return rc;
   }
   if (done) return MOE_OK;
   // (the second product of a feed-forward layer is its transpose in the expert's naming)

@@ -52,6 +52,39 @@ def test_the_cases_reach_every_form():
     assert seen == {(dtype, few, split, d) for dtype in (BF16, F32) for few, split in ((False, False), (True, False), (True, True)) for d in (64, 128)}
 
 
+def ranges(B, Lq, Lk, heads, kv_heads, d):
+    f = LIB._ZN3moe16cross_dkv_blocksERKNS_10CrossShapeE
+    f.argtypes, f.restype = [ctypes.c_void_p], ctypes.c_int
+    s = _Shape(B, Lq, Lk, heads, kv_heads, d)
+    all_, each = (Lq * (heads // kv_heads) + 63) // 64, f(ctypes.byref(s))
+    assert 1 <= each <= all_
+    return -(-all_ // each)
+
+
+# us of dK and dV by one range of the columns, and by the best number of them with the launch that adds them up
+@pytest.mark.parametrize("shape,one,more", [
+    ((4, 2000, 1000, 8, 1, 128), 455, 87.4), ((4, 2000, 1000, 8, 1, 64), 295, 50.9), ((7, 1561, 66, 2, 1, 128), 93.0, 19.3),
+    ((7, 1561, 66, 2, 1, 64), 61.1, 15.9), ((1, 2000, 60, 2, 2, 128), 62.6, 16.7), ((1, 1000, 500, 8, 8, 128), 36.1, 23.0),
+    ((1, 1000, 500, 8, 8, 64), 23.8, 18.7), ((8, 1000, 100, 8, 8, 64), 24.4, 17.9), ((8, 1000, 100, 8, 8, 128), 36.7, 25.8),
+    ((6, 900, 130, 4, 4, 64), 22.4, 15.6), ((1, 500, 500, 8, 8, 64), 14.5, 15.9), ((1, 500, 500, 8, 8, 128), 21.7, 22.4),
+    ((2, 300, 2000, 8, 8, 64), 16.2, 23.6), ((2, 300, 2000, 8, 8, 128), 20.3, 46.0), ((4, 100, 100, 4, 4, 128), 10.0, 14.4),
+    ((16, 200, 256, 8, 8, 128), 18.0, 42.7), ((27, 834, 100, 8, 8, 128), 35.2, 54.2), ((8, 1000, 1000, 8, 8, 64), 42.7, 64.5)])
+def test_ranges_of_columns(shape, one, more):
+    assert (ranges(*shape) > 1) == (more < one)
+
+
+def test_ranges_run_at_once_and_none_is_empty():
+    for d in (64, 128):
+        for B in (1, 2, 7, 64, 300, 4000):
+            for Lq in (1, 63, 64, 65, 1000, 4097, 1 << 20):
+                for Lk in (1, 128, 129, 5000):
+                    n = ranges(B, Lq, Lk, 4, 2, d)
+                    all_ = (2 * Lq + 63) // 64
+                    assert 1 <= n <= 32 and (n - 1) * -(-all_ // n) < all_
+                    assert n == 1 or n * B * 2 * ((Lk + 127) // 128) <= (512 if d == 64 else 256)
+    assert {(ranges(*c[:6]) > 1, c[5]) for c in CASES} == {(False, 64), (True, 64), (False, 128), (True, 128)}
+
+
 # K, N, rows; us of the kernels for many rows and of this one
 @pytest.mark.parametrize("dtype,K,N,rows,many,few", [
     (BF16, 1024, 2048, 1, 5.7, 3.4), (BF16, 1024, 2048, 128, 6.0, 4.4), (BF16, 1024, 2048, 192, 6.1, 7.2), (BF16, 2048, 1024, 256, 9.6, 6.1),

@@ -69,7 +69,9 @@ CASES = [(1, 1, 1, 1, 1, 64, None), (6, 1, 1, 2, 2, 128, "ends"), (4, 40, 1, 4, 
          # dq in blocks of 128 columns: more blocks of 32 than the units take at once, with each end of the states
          (33, 100, 130, 4, 4, 64, "ends"), (24, 100, 97, 4, 4, 128, "ends"), (33, 17, 130, 8, 4, 64, "ends"), (66, 40, 193, 4, 1, 128, "ends"),
          # and as many as they take
-         (16, 63, 256, 8, 8, 128, "ends"), (2, 1000, 100, 8, 8, 64, "ends")]
+         (16, 63, 256, 8, 8, 128, "ends"), (2, 1000, 100, 8, 8, 64, "ends"),
+         # dK and dV in ranges of columns: whole ones, a last one that is shorter, whose last block is not whole, sources of every length
+         (1, 1024, 60, 2, 2, 128, None), (6, 900, 130, 4, 4, 64, "ends"), (7, 401, 70, 2, 1, 128, "ends"), (2, 777, 300, 4, 1, 64, "any")]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

@@ -172,7 +172,8 @@ def cross_call(c, dtype, seed=0, ws_fill=255):
     return need, run
 
 
-FORMS = [(3, 200, 300, 4, 2, 64, "any"), (1, 300, 1000, 2, 2, 128, "any"), (2, 1, 4100, 2, 2, 128, "any"), (40, 70, 200, 8, 8, 128, "any"), (9, 5, 700, 16, 2, 64, None)]
+FORMS = [(3, 200, 300, 4, 2, 64, "any"), (1, 300, 1000, 2, 2, 128, "any"), (2, 1, 4100, 2, 2, 128, "any"), (40, 70, 200, 8, 8, 128, "any"), (9, 5, 700, 16, 2, 64, None),
+         (2, 1500, 70, 4, 1, 64, "any")]                  # dK and dV in ranges of columns
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -189,7 +190,7 @@ def test_same_bits_whatever_the_workspace_held(c, dtype):
 def test_captured_graphs_share_workspaces(dtype):
     """Each call leaves nothing in its workspace that another needs (but for the backward pass's own forward): graphs of different sizes in turn."""
     moe.moe_prepare()
-    jobs = [cross_call(c, dtype) for c in FORMS[:4]]
+    jobs = [cross_call(c, dtype) for c in FORMS[:4] + FORMS[5:]]
     ws = [torch.full((max(j[0][i] for j in jobs),), 255, dtype=torch.uint8, device=DEV) for i in range(3)]
     wants = [run() for _, run in jobs]
     graphs = []
@@ -198,7 +199,7 @@ def test_captured_graphs_share_workspaces(dtype):
         with torch.cuda.graph(graph):
             out = run(ws)
         graphs.append((graph, out))
-    for turn in (0, 1, 2, 3, 3, 1, 0, 2):
+    for turn in (0, 1, 2, 3, 4, 3, 1, 4, 0, 2):
         graph, out = graphs[turn]
         graph.replay()
         torch.cuda.synchronize()
@@ -206,7 +207,7 @@ def test_captured_graphs_share_workspaces(dtype):
             assert torch.equal(out[k], v), (turn, k)
 
 
-@pytest.mark.parametrize("one,other,dtype", [(FORMS[0], FORMS[2], "bf16"), (FORMS[3], FORMS[1], "bf16"), (FORMS[0], FORMS[3], "f32"), (FORMS[2], FORMS[4], "f32")])
+@pytest.mark.parametrize("one,other,dtype", [(FORMS[0], FORMS[2], "bf16"), (FORMS[3], FORMS[1], "bf16"), (FORMS[5], FORMS[0], "bf16"), (FORMS[0], FORMS[3], "f32"), (FORMS[2], FORMS[4], "f32")])
 def test_streams_that_run_at_once(one, other, dtype):
     """All enqueued on two streams before the first may start: kernels of one call run beside kernels of the other."""
     moe.moe_prepare()
