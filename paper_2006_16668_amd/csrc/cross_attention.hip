@@ -1203,7 +1203,11 @@ int prepare_cross_attention() {
 
 // Which form a forward call takes, by what both are expected to take (us).  A block of 128 columns walks its states in steps, two blocks on a unit
 // (fp32: one at a time multiplies); one of 32 columns shares them among its wavefronts and `splits` blocks, which cost a launch to join and
-// bring only as much memory as they have units.  us, 128 / 32 columns in the best number of ranges, bf16, heads of 128: 64 x 1 tokens, 410 to 2048
+// bring only as much memory as they have units.  What the ranges leave of each column is written and read once more, 0.5 to 0.8 us a MB, and so there are no more
+// blocks in ranges than four rounds of the device: without that, a rounded number of rounds asked for up to 64 ranges of many columns.  us of calls in 1 / 4 /
+// 64 ranges, bf16, heads of 64: 10 x 1162 tokens, 8161 states, 1 head 111 / 93 / 197; 19 x 83, 8174, 8 on 4 114 / 117 / 251; 19 x 15, 8100, 24 on 3
+// 94 / 70 / 130; fp32, 19 x 83, 8174, 8 on 4 381 / 382 / 571.
+// us, 128 / 32 columns in the best number of ranges, bf16, heads of 128: 64 x 1 tokens, 410 to 2048
 // states, 16 heads 120 / 128; 1 x 4, 53 5.0 / 6.1; 1 x 1, 1000 23.7 / 10.1 (8); 1 x 1, 8000 155 / 23 (16); 8 x 1, 1000 23.2 / 19.1 (2); 4 x 8, 4000, 2 key
 // heads of 16 82 / 13.7 (16); 4 x 64, 1000, 8 heads 26.9 / 14.2 (4); 3 x 700, up to 700, 4 heads 20.4 / 29; of 64: 16 x 1, 2000, 8 heads 28.2 / 16.9 (4);
 // 2 x 300, 2000 34.5 / 23.0 (2); 27 x 834, up to 100 18.9 / 47; fp32, of 64: 5 x 187, up to 411, 8 heads 40.8 / 16.3; 8 x 500, 500 59 / 64; 27 x 834, up to
@@ -1220,8 +1224,10 @@ CrossPlan cross_plan(int act_dtype, const CrossShape& s) {
   double least = 4 + longer(step128 * (f32 ? blocks : (blocks + 1) / 2) * rounds(pairs * ((s.columns() + 127) / 128), f32 ? kUnits : 2 * kUnits), mb / 5.0);
   for (int splits = 1; splits <= 64 && splits <= (blocks + 3) / 4; splits *= 2) {
     const double items = pairs * ((s.columns() + 31) / 32) * splits, at_once = !f32 && s.d == 64 ? 2 * kUnits : kUnits;
-    const double us = 6 + (splits > 1 ? 4 : 0) + longer((step32 * ((blocks + 4 * splits - 1) / (4 * splits)) + ends) * rounds(items, at_once),
-                                                       mb / 5.0 * (items < kUnits ? kUnits / items : 1.0));
+    if (splits > 1 && items > 4 * at_once) break;
+    const double joined = splits > 1 ? 4 + 0.55 * pairs * s.columns() * splits * (4 * s.d + 8) / 1e6 : 0;
+    const double us = 6 + joined + longer((step32 * ((blocks + 4 * splits - 1) / (4 * splits)) + ends) * rounds(items, at_once),
+                                           mb / 5.0 * (items < kUnits ? kUnits / items : 1.0));
     if (us < least) {
       least = us;
       best = {true, splits};
