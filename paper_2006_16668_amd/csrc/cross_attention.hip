@@ -505,6 +505,114 @@ __global__ __launch_bounds__(256) void cross_join_kernel(CrossGeo g, CrossParts 
   for (int i = 0; i < D / 64; ++i) Elt<T>::store(to + i, v[i] * inv);
 }
 
+// ---------------------------------------------------------------- dq (and D) of up to 64 states
+// D = sum p dP of the probabilities at hand.  Of few states dP - D is a difference of near numbers, of whose error the rounding of the stored ctx, in
+// rowsum(dO * ctx), is more than half (two states: dq off by 0.0053 in norm, 0.0038 without it); of one it is 0, as it is here to the last
+// bit: p is exactly 1.  What a source holds decides, not what its batch is padded to, so every kernel of dq has this form of its own and padding
+// changes no bits.  K and V are two blocks of 32 rows each, zeros from n on: K's first at k0, V's at v0, the second ones `step` behind.
+template <int D>
+__device__ __forceinline__ void few_states_dq(f32x16_t (&dq)[D / 32], float& dd, const AttReads<D>& rd, uint32_t k0, uint32_t v0, uint32_t step,
+                                              const u32x4_t (&qf)[D / 16], const u32x4_t (&dof)[D / 16], int n, int hf) {
+  constexpr int KS = D / 16, DT = D / 32;
+  const float sl2 = 1.4426950408889634f / sqrtf((float)D);
+  f32x16_t sc[2], dp[2];
+  float m = -FLT_MAX, sum = 0.f, dsum = 0.f;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+#pragma unroll
+    for (int x = 0; x < KS; ++x) {
+      sc[t] = MOE_MFMA(rd.row(k0 + t * step, 0, x), qf[x], x == 0 ? f32x16_t{} : sc[t]);
+      dp[t] = MOE_MFMA(rd.row(v0 + t * step, 0, x), dof[x], x == 0 ? f32x16_t{} : dp[t]);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      sc[t][i] = 32 * t + 8 * (i >> 2) + 4 * hf + (i & 3) < n ? rounded_product(sc[t][i], sl2) : -INFINITY;
+      m = fmaxf(m, sc[t][i]);
+    }
+  }
+  m = fmaxf(m, __shfl_xor(m, 32, 64));
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      sc[t][i] = __builtin_amdgcn_exp2f(sc[t][i] - m);
+      sum += sc[t][i];
+      dsum += sc[t][i] * dp[t][i];
+    }
+  sum += __shfl_xor(sum, 32, 64);
+  dsum += __shfl_xor(dsum, 32, 64);
+  const float inv = 1.0f / sum;
+  dd = dsum * inv;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) dq[dt] = f32x16_t{};
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sc[t][i] *= inv * (dp[t][i] - dd);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const u32x4_t f = pack8(sc[t], 8 * x);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) dq[dt] = MOE_MFMA(rd.transposed(k0 + t * step, 16 * x, dt), f, dq[dt]);
+    }
+  }
+}
+// A block of 128 columns of such a source.  K and V lie in LDS whole, the columns' rows come straight from memory.
+template <int D>
+__device__ __forceinline__ void few_states_block(const CrossCols& cols, const CrossWork<1>& w, size_t head, int n, int Akv,
+                                                 const uint32_t (&off)[AttGeom<D>::kCopies], const bf16_t* q, const bf16_t* keys,
+                                                 const bf16_t* dctx, bf16_t* dqo, float* dvec, uint32_t lds0, int wave, int lane) {
+  using GM = AttGeom<D>;
+  constexpr int CT = 1, KS = D / 16, DT = D / 32, kOwnBlock = 32 * CT * GM::kRow, kV = GM::kBlock;
+  const int r = lane & 31, hf = lane >> 5;
+  const bool live = w.col0 < cols.count;
+#pragma unroll
+  for (int x = 0; x < GM::kCopies; ++x) {
+    stage_rows<D>(lds0, keys, n, off, x, wave, lane);
+    stage_rows<D>(lds0 + kV, keys + Akv, n, off, x, wave, lane);
+  }
+  const size_t row = head + cols.offset<D>(cols.within(w.col0 + r));
+  u32x4_t qf[KS], dof[KS];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    qf[s] = *reinterpret_cast<const u32x4_t*>(q + row + 16 * s + 8 * hf);
+    dof[s] = *reinterpret_cast<const u32x4_t*>(dctx + row + 16 * s + 8 * hf);
+  }
+  wait_all_copies();
+  __syncthreads();
+  f32x16_t dq[CT][DT];
+  if (live) {
+    float dd;
+    few_states_dq<D>(dq[0], dd, AttReads<D>(lds0, lane), 0, kV, kOwnBlock, qf, dof, n, hf);
+    if (hf == 0 && w.col0 + r < cols.count) dvec[(size_t)w.bk * cols.count + w.col0 + r] = dd;
+  }
+  __syncthreads();                                             // K and V are read: the results go through their places
+  if (!live) return;
+  store_rows<D, CT>(dq, 1.0f / sqrtf((float)D), lds0 + wave * kOwnBlock, lane, [&](int i, int chunk, const u32x4_t& v) __attribute__((always_inline)) {
+    if (w.col0 + i < cols.count) *reinterpret_cast<u32x4_t*>(dqo + head + cols.offset<D>(w.col0 + i) + 8 * chunk) = v;
+  });
+}
+// All sources of a call have up to 64 states.
+template <int D>
+__global__ __launch_bounds__(256, 2) void cross_dq_short_kernel(CrossGeo g, const bf16_t* __restrict__ q, const bf16_t* __restrict__ kv,
+                                                                const int32_t* __restrict__ src_len, const bf16_t* __restrict__ dctx,
+                                                                bf16_t* __restrict__ dqo, float* __restrict__ dvec) {
+  extern __shared__ __attribute__((aligned(256))) unsigned char att_lds[];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)((lds_ptr)att_lds);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const CrossCols cols(g, D);
+  const CrossWork<1> w(cols.count, g.kv_heads, wave);
+  const size_t head = cols.base(w.b, w.k, D);
+  const int n = held_states(src_len, w.b, g.Lk), Akv = g.kv_heads * D;
+  if (n == 0) {                                                // (no state asks for D)
+    clear_columns<D>(dqo + head, cols, w.block0);
+    return;
+  }
+  uint32_t off[AttGeom<D>::kCopies];
+  copy_offsets<D>(off, (size_t)2 * Akv, wave, lane);
+  few_states_block<D>(cols, w, head, n, Akv, off, q, kv + (size_t)w.b * g.Lk * 2 * Akv + (size_t)w.k * D, dctx, dqo, dvec, lds0, wave, lane);
+}
+
 // ---------------------------------------------------------------- dq (and D)
 template <int D>
 __global__ __launch_bounds__(256, 2) void cross_dq_kernel(CrossGeo g, const bf16_t* __restrict__ q, const bf16_t* __restrict__ kv,
@@ -535,6 +643,10 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(CrossGeo g, const bf16
 
   uint32_t off[GM::kCopies];
   copy_offsets<D>(off, ld, wave, lane);
+  if (n <= 64) {
+    few_states_block<D>(cols, w, head, n, Akv, off, q, keys, dctx, dqo, dvec, lds0, wave, lane);
+    return;
+  }
   const int nkb = (n + 63) / 64;
   // copy x of step j's: K block j + 1 to place `slot`, V block j (after the last ones, those once more)
   auto start = [&](int j, int slot, int x) __attribute__((always_inline)) {
@@ -725,10 +837,26 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void cross_dq_few_kernel(CrossGe
     for (int i = 0; i < 8; ++i) dd = fmaf(gr[i], ov[i], dd);
   }
   dd += __shfl_xor(dd, 32, 64);
-  const float lse2 = lse[column];
   const float scale = 1.0f / sqrtf((float)D), sl2 = 1.4426950408889634f * scale;
   const AttReads<D> rd(lds0, lane);
   f32x16_t dq[DT];
+  if (n > 0 && n <= 64) {                                      // block-uniform: one wavefront has both blocks of states
+    if (wave > 0) return;
+    start(0, 0);
+    start(1, 1);
+    wait_all_copies();
+    few_states_dq<D>(dq, dd, rd, 0, kHalf, kPlace, qf, dof, n, hf);
+    if (c >= cols.count) return;
+    if (hf == 0) dvec[column] = dd;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        *reinterpret_cast<u32x2_t*>(dqo + row + 32 * dt + 8 * x + 4 * hf) =
+            u32x2_t{pack_bf16x2(dq[dt][4 * x] * scale, dq[dt][4 * x + 1] * scale), pack_bf16x2(dq[dt][4 * x + 2] * scale, dq[dt][4 * x + 3] * scale)};
+    return;
+  }
+  const float lse2 = lse[column];
 #pragma unroll
   for (int t = 0; t < DT; ++t) dq[t] = f32x16_t{};
   if (wave < nkb) start(wave, 0);
@@ -786,101 +914,6 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void cross_dq_few_kernel(CrossGe
       *reinterpret_cast<u32x2_t*>(dqo + row + 32 * dt + 8 * x + 4 * hf) =
           u32x2_t{pack_bf16x2(v[4 * x], v[4 * x + 1]), pack_bf16x2(v[4 * x + 2], v[4 * x + 3])};
   }
-}
-
-// ---------------------------------------------------------------- dq (and D) of up to 64 states
-// D = sum p dP of the probabilities at hand.  Of few states dP - D is a difference of near numbers, of whose error the rounding of the stored ctx, in
-// rowsum(dO * ctx), is more than half (two states: dq off by 0.0053 in norm, 0.0038 without it); of one it is 0, as it is here to the last
-// bit: p is exactly 1.  K and V lie in LDS whole, the columns' rows come straight from memory.
-template <int D>
-__global__ __launch_bounds__(256, 2) void cross_dq_short_kernel(CrossGeo g, const bf16_t* __restrict__ q, const bf16_t* __restrict__ kv,
-                                                                const int32_t* __restrict__ src_len, const bf16_t* __restrict__ dctx,
-                                                                bf16_t* __restrict__ dqo, float* __restrict__ dvec) {
-  using GM = AttGeom<D>;
-  constexpr int CT = 1, KS = D / 16, DT = D / 32, kOwnBlock = 32 * CT * GM::kRow, kV = GM::kBlock;
-  extern __shared__ __attribute__((aligned(256))) unsigned char att_lds[];
-  const uint32_t lds0 = (uint32_t)(uintptr_t)((lds_ptr)att_lds);
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r = lane & 31, hf = lane >> 5;
-  const CrossCols cols(g, D);
-  const CrossWork<CT> w(cols.count, g.kv_heads, wave);
-  const size_t head = cols.base(w.b, w.k, D), column = (size_t)w.bk * cols.count + w.col0 + r;
-  const int n = held_states(src_len, w.b, g.Lk), Akv = g.kv_heads * D;
-  if (n == 0) {                                                // (no state asks for D)
-    clear_columns<D>(dqo + head, cols, w.block0);
-    return;
-  }
-  const size_t ld = (size_t)2 * Akv;
-  const bf16_t* const keys = kv + (size_t)w.b * g.Lk * ld + (size_t)w.k * D;
-  const bool live = w.col0 < cols.count;
-  uint32_t off[GM::kCopies];
-  copy_offsets<D>(off, ld, wave, lane);
-#pragma unroll
-  for (int x = 0; x < GM::kCopies; ++x) {
-    stage_rows<D>(lds0, keys, n, off, x, wave, lane);
-    stage_rows<D>(lds0 + kV, keys + Akv, n, off, x, wave, lane);
-  }
-  const size_t row = head + cols.offset<D>(cols.within(w.col0 + r));
-  u32x4_t qf[KS], dof[KS];
-#pragma unroll
-  for (int s = 0; s < KS; ++s) {
-    qf[s] = *reinterpret_cast<const u32x4_t*>(q + row + 16 * s + 8 * hf);
-    dof[s] = *reinterpret_cast<const u32x4_t*>(dctx + row + 16 * s + 8 * hf);
-  }
-  wait_all_copies();
-  __syncthreads();
-  f32x16_t dq[CT][DT];
-  const float scale = 1.0f / sqrtf((float)D), sl2 = 1.4426950408889634f * scale;
-  if (live) {
-    const AttReads<D> rd(lds0, lane);
-    f32x16_t sc[2], dp[2];
-    float m = -FLT_MAX, sum = 0.f, dsum = 0.f;
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-#pragma unroll
-      for (int x = 0; x < KS; ++x) {
-        sc[t] = MOE_MFMA(rd.row(0, t, x), qf[x], x == 0 ? f32x16_t{} : sc[t]);
-        dp[t] = MOE_MFMA(rd.row(kV, t, x), dof[x], x == 0 ? f32x16_t{} : dp[t]);
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        sc[t][i] = 32 * t + 8 * (i >> 2) + 4 * hf + (i & 3) < n ? rounded_product(sc[t][i], sl2) : -INFINITY;
-        m = fmaxf(m, sc[t][i]);
-      }
-    }
-    m = fmaxf(m, __shfl_xor(m, 32, 64));
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        sc[t][i] = __builtin_amdgcn_exp2f(sc[t][i] - m);
-        sum += sc[t][i];
-        dsum += sc[t][i] * dp[t][i];
-      }
-    sum += __shfl_xor(sum, 32, 64);
-    dsum += __shfl_xor(dsum, 32, 64);
-    const float inv = 1.0f / sum;
-    dsum *= inv;
-    if (hf == 0 && w.col0 + r < cols.count) dvec[column] = dsum;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) dq[0][dt] = f32x16_t{};
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sc[t][i] *= inv * (dp[t][i] - dsum);
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const u32x4_t f = pack8(sc[t], 8 * x);
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) dq[0][dt] = MOE_MFMA(rd.transposed(0, 32 * t + 16 * x, dt), f, dq[0][dt]);
-      }
-    }
-  }
-  __syncthreads();                                             // K and V are read: the results go through their places
-  if (!live) return;
-  store_rows<D, CT>(dq, scale, lds0 + wave * kOwnBlock, lane, [&](int i, int chunk, const u32x4_t& v) __attribute__((always_inline)) {
-    if (w.col0 + i < cols.count) *reinterpret_cast<u32x4_t*>(dqo + head + cols.offset<D>(w.col0 + i) + 8 * chunk) = v;
-  });
 }
 
 // ---------------------------------------------------------------- dK, dV
