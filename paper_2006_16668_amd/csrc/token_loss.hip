@@ -150,7 +150,10 @@ __global__ __launch_bounds__(256) void preference_bwd_kernel(moe_preference_dims
 
 // e^x - 1 - x.  Below 1 the terms of its series from x^2/2 on: the difference would lose 2 / x of its digits.
 __device__ __forceinline__ float exp_rest(float x) {
-  if (fabsf(x) >= 1.f) return expf(x) - 1.f - x;
+  if (fabsf(x) >= 1.f) {
+    const float e = expf(x);
+    return e == INFINITY ? e : e - 1.f - x;                    // (of x = inf too)
+  }
   float s = 1.f / 39916800.f;                                  // the first left out, x^12 / 12!, is below 5e-9 of the sum
   s = fmaf(s, x, 1.f / 3628800.f);
   s = fmaf(s, x, 1.f / 362880.f);
