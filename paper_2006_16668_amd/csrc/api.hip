@@ -36,6 +36,12 @@ int gate_scratch_ptr(void** out) {
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// what counts where only tokens do: their number
+int check_tokens(const moe_config* c) {
+  if (c == nullptr || c->G < 1 || c->S < 1) return MOE_EINVAL;
+  return (long long)c->G * c->S > 0x3fffffffLL ? MOE_EUNSUPPORTED : MOE_OK;
+}
+
 int check_config(const moe_config* c) {
   if (c == nullptr) return MOE_EINVAL;
   if (c->G < 1 || c->S < 1 || c->M < 1 || c->H < 1 || c->E < 2 || c->C < 1) return MOE_EINVAL;
@@ -43,7 +49,7 @@ int check_config(const moe_config* c) {
   // rows are moved and multiplied in 16-byte pieces: 8 bf16 or 4 fp32 elements
   const int piece = c->act_dtype == MOE_F32 ? 4 : 8;
   if (c->M % piece != 0 || c->H % piece != 0) return MOE_EUNSUPPORTED;
-  if ((long long)c->G * c->S > 0x3fffffffLL) return MOE_EUNSUPPORTED;
+  if (check_tokens(c) != MOE_OK) return MOE_EUNSUPPORTED;
   if ((long long)c->E * c->G * c->C > 0x7fffffffLL) return MOE_EUNSUPPORTED;
   return MOE_OK;
 }
@@ -458,14 +464,14 @@ int cross_forward(const moe_config* cfg, const moe_cross_dims* dims, const void*
 }
 
 int check_preference(const moe_config* cfg, const moe_preference_dims* d) {
-  const int rc = check_config(cfg);
+  const int rc = check_tokens(cfg);
   if (rc != MOE_OK) return rc;
   if (d == nullptr || d->P < 1 || d->V < 1 || (d->kind != MOE_PREFERENCE_LOGISTIC && d->kind != MOE_PREFERENCE_SQUARED)) return MOE_EINVAL;
   if (!(d->beta > 0.0 && d->beta < INFINITY) || !(d->smoothing >= 0.0 && d->smoothing < 1.0)) return MOE_EINVAL;
   return d->P >= 1 << 24 ? MOE_EUNSUPPORTED : MOE_OK;           // (a block of 256 threads each)
 }
 int policy_call(const moe_config* cfg, const moe_policy_dims* d, const moe::PolicyCall& a, bool backward, void* stream) {
-  const int rc = check_config(cfg);
+  const int rc = check_tokens(cfg);
   if (rc != MOE_OK) return rc;
   if (d == nullptr || d->V < 1 || (d->adv_per_token != 0 && d->adv_per_token != 1)) return MOE_EINVAL;
   if (!(d->clip_low >= 0.0 && d->clip_low <= 1.0) || !(d->clip_high >= 0.0 && d->clip_high < INFINITY) ||
