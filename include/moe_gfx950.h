@@ -565,12 +565,13 @@ typedef struct {
  *   logistic  loss[p] = -(1 - smoothing) log sigmoid(beta h) - smoothing log sigmoid(-beta h)
  *   squared   loss[p] = (h - 1 / (2 beta))^2
  * in: nll, ref_nll [G,S] fp32, target [G,S] i32; start [2P+1] i32, ascending: sequence i is the tokens start[i] .. start[i+1] - 1
- * of the G S in order (values outside 0 .. G S count as the nearest of these).  out: loss [P], ratio [2P] fp32.  Sums in 64 bits. */
+ * of the G S in order (values outside 0 .. G S count as the nearest of these).  out: loss [P], ratio [2P] fp32.  Sums in 64 bits: the loss is that of
+ * the margin h before the ratios are rounded to fp32. */
 int moe_preference_loss(const moe_config* cfg, const moe_preference_dims* dims, const float* nll, const float* ref_nll,
                         const int32_t* target, const int32_t* start, float* loss, float* ratio, void* stream);
 
-/* dnll [G,S] of L = sum dloss[p] loss[p]; ratio as moe_preference_loss left it.  Every element is written, 0 outside the
- * sequences. */
+/* dnll [G,S] of L = sum dloss[p] loss[p] at the margin of the two ratios as given: as moe_preference_loss left them, h is off by up to
+ * 2^-24 (|ratio[2p]| + |ratio[2p + 1]|), and d loss / d h by beta^2 / 4 (squared: 2) of that.  Every element is written, 0 outside the sequences. */
 int moe_preference_loss_backward(const moe_config* cfg, const moe_preference_dims* dims, const int32_t* target, const int32_t* start,
                                  const float* ratio, const float* dloss, float* dnll, void* stream);
 

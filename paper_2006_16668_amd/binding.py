@@ -892,7 +892,7 @@ def moe_preference_loss(shape: MoEShape, dims: PreferenceDims, nll, ref_nll, tar
 
 
 def moe_preference_loss_backward(shape: MoEShape, dims: PreferenceDims, target, start, ratio, dloss, dnll):
-    """Gradient dnll [G,S] of sum(dloss * loss); ratio as moe_preference_loss left it."""
+    """Gradient dnll [G,S] of sum(dloss * loss) at the margin of the ratios as stored: ratio as moe_preference_loss left it, rounded to fp32."""
     t, f32, i32, P, here = (shape.G, shape.S), torch.float32, torch.int32, dims.P, _here()
     c, d = shape._c(), dims._c()
     _run(load_library().moe_preference_loss_backward(
