@@ -614,7 +614,8 @@ int moe_gradient_norm_workspace_bytes(const moe_gradient* list, int32_t n, size_
  * ws >= moe_gradient_norm_workspace_bytes, 256-byte aligned. */
 int moe_gradient_norm(const moe_gradient* list, int32_t n, float* norm, void* ws, size_t ws_bytes, void* stream);
 
-/* dst = src min(1, max_norm / norm[0]), rounded once, for all n tensors.  A norm that is infinite or NaN leaves the gradients as
+/* dst = src min(1, max_norm / norm[0]) for all n tensors: the scale is rounded to 24 bits, the product to fp32, and that once more to bf16 (or below
+ * the normal numbers).  A norm that is infinite or NaN leaves the gradients as
  * they are, for the caller to see.  max_norm >= 0.  norm is a device pointer: a caller with shards on several devices puts the
  * root of the sum of their squares there. */
 int moe_clip_gradients(const moe_gradient* list, int32_t n, const float* norm, double max_norm, void* stream);
