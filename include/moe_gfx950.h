@@ -527,7 +527,8 @@ int moe_cross_keys(const moe_config* cfg, const moe_cross_dims* dims, const void
 
 /* in: u [G,S,M], kv as moe_cross_keys leaves it, src_len [B] i32 or NULL (all states hold), wq [M,A], wo [A,M].  out [G,S,M].
  * ws >= moe_cross_workspace_bytes, 256-byte aligned.  bf16: q, ctx and, where a block has 128 columns (many tokens), the
- * probabilities are rounded once each; softmax statistics and sums are fp32, sums in a fixed order. */
+ * probabilities are rounded once each; softmax statistics and sums are fp32, sums in a fixed order.  The form of a call goes by its type, B, Lq, Lk
+ * and heads: in a batch of another size, or padded to another Lk, a source's tokens may differ by that rounding and by the order of their sums. */
 int moe_cross_attention(const moe_config* cfg, const moe_cross_dims* dims, const void* u, const void* kv, const int32_t* src_len,
                         const void* wq, const void* wo, void* out, void* ws, size_t ws_bytes, void* stream);
 
