@@ -379,8 +379,14 @@ int check_cross(const moe_config* cfg, const moe_cross_dims* d) {
 }
 moe::CrossShape cross_shape(const moe_cross_dims& d) { return {d.B, d.Lq, d.Lk, d.heads, d.kv_heads, d.d}; }
 
-// train: with the row statistics.  q, ctx and lse come first, so the backward pass finds them.
-struct CrossWs { size_t q, ctx, lse, scratch, total; };
+// Calls of few tokens carry q and ctx as pairs of bf16 through the forward pass (and P): their roundings are as large as that of the result, and where products
+// are of few rows and the states' bytes are what counts, pairs cost next to nothing.
+bool cross_pairs(const moe_config& c, const moe_cross_dims& d) {
+  const long long N = (long long)c.G * c.S;
+  return c.act_dtype == MOE_BF16 && moe::few_rows_ok(MOE_BF16, N, d.heads * d.d) && moe::few_rows_pair_ok(N, c.M);
+}
+// train: with the row statistics.  q, ctx and lse come first, so the backward pass, which has no second terms, finds them.
+struct CrossWs { size_t q, ctx, lse, q_rest, ctx_rest, scratch, total; };
 CrossWs carve_cross(const moe_config& c, const moe_cross_dims& d, bool train) {
   const size_t elt = c.act_dtype == MOE_F32 ? 4 : 2, N = (size_t)c.G * c.S, A = (size_t)d.heads * d.d;
   CrossWs w{};
@@ -389,7 +395,10 @@ CrossWs carve_cross(const moe_config& c, const moe_cross_dims& d, bool train) {
   w.q = take(N * A * elt);
   w.ctx = take(N * A * elt);
   w.lse = take(train ? N * d.heads * 4 : 0);
-  w.scratch = take(moe::cross_scratch_bytes(c.act_dtype, cross_shape(d)));
+  const bool pairs = cross_pairs(c, d);
+  w.q_rest = take(pairs ? N * A * elt : 0);
+  w.ctx_rest = take(pairs ? N * A * elt : 0);
+  w.scratch = take(pairs ? moe::cross_pair_scratch_bytes(cross_shape(d)) : moe::cross_scratch_bytes(c.act_dtype, cross_shape(d)));
   w.total = off;
   return w;
 }
@@ -456,9 +465,15 @@ int cross_forward(const moe_config* cfg, const moe_cross_dims* dims, const void*
   hipStream_t st = static_cast<hipStream_t>(stream);
   const long long N = (long long)cfg->G * cfg->S;
   const int A = dims->heads * dims->d;
+  float* const lse = train ? reinterpret_cast<float*>(base + w.lse) : nullptr;
+  if (cross_pairs(*cfg, *dims)) {
+    if ((rc = moe::launch_few_rows_pair(u, nullptr, wq, base + w.q, base + w.q_rest, (int)N, A, cfg->M, st)) != MOE_OK) return rc;
+    rc = moe::launch_cross_attention_pair(cross_shape(*dims), base + w.q, base + w.q_rest, kv, src_len, base + w.ctx, base + w.ctx_rest, lse, base + w.scratch, st);
+    if (rc != MOE_OK) return rc;
+    return moe::launch_few_rows_pair(base + w.ctx, base + w.ctx_rest, wo, out, nullptr, (int)N, cfg->M, A, st);
+  }
   if ((rc = cross_product(*cfg, N, cfg->M, A, u, wq, base + w.q, st)) != MOE_OK) return rc;
-  rc = moe::launch_cross_attention(cfg->act_dtype, cross_shape(*dims), base + w.q, kv, src_len, base + w.ctx,
-                                   train ? reinterpret_cast<float*>(base + w.lse) : nullptr, base + w.scratch, st);
+  rc = moe::launch_cross_attention(cfg->act_dtype, cross_shape(*dims), base + w.q, kv, src_len, base + w.ctx, lse, base + w.scratch, st);
   if (rc != MOE_OK) return rc;
   return cross_product(*cfg, N, A, cfg->M, base + w.ctx, wo, out, st);
 }

@@ -51,6 +51,17 @@ __device__ __forceinline__ void split_bf16x8(const V& v, int first, bf16x8_bits_
     }
   }
 }
+// What bf16 leaves of a number that it rounded to `rounded`: the second of a pair of bf16 that holds 16 bits.  0 where that is no number, so that an infinity stays one.
+__device__ __forceinline__ float bf16_rest(float v, float rounded) {
+  const float rest = v - rounded;
+  return fabsf(rest) < __builtin_inff() ? rest : 0.f;
+}
+__device__ __forceinline__ uint32_t bf16_rest_x2(float a, float b, uint32_t rounded) {
+  return pack_bf16x2(bf16_rest(a, __uint_as_float(rounded << 16)), bf16_rest(b, __uint_as_float(rounded & 0xffff0000u)));
+}
+// The sum of what the two terms of a pair made.  An infinite factor may make no number of the second term (0 times infinity); the first has made an infinity or no
+// number then, which any number leaves as it is.
+__device__ __forceinline__ float pair_sum(float first, float second) { return first + __builtin_amdgcn_fmed3f(second, -3.402823466e38f, 3.402823466e38f); }
 // max(v, 0) on two packed bf16 in one op: a negative bf16 is a negative 16-bit integer
 __device__ __forceinline__ uint32_t relu_bf16x2(uint32_t v) {
   typedef short s16x2_t __attribute__((ext_vector_type(2)));
@@ -428,6 +439,10 @@ struct CrossShape {
 size_t cross_scratch_bytes(int act_dtype, const CrossShape& s);
 int launch_cross_attention(int act_dtype, const CrossShape& s, const void* q, const void* kv, const int32_t* src_len, void* ctx,
                            float* lse, void* scratch, hipStream_t st);
+// bf16, few tokens: q and ctx in pairs (q + q_rest, ctx + ctx_rest), and so the probabilities; lse is of q alone; scratch: cross_pair_scratch_bytes()
+size_t cross_pair_scratch_bytes(const CrossShape& s);
+int launch_cross_attention_pair(const CrossShape& s, const void* q, const void* q_rest, const void* kv, const int32_t* src_len, void* ctx, void* ctx_rest,
+                                float* lse, void* scratch, hipStream_t st);
 // dvec: [B kv_heads columns] of scratch; dkv: zeros in the rows of states that do not hold; sums: cross_bwd_scratch_bytes()
 size_t cross_bwd_scratch_bytes(int act_dtype, const CrossShape& s);
 int launch_cross_attention_bwd(int act_dtype, const CrossShape& s, const void* q, const void* kv, const int32_t* src_len,
@@ -440,6 +455,9 @@ int launch_held_rows(int act_dtype, const void* mem, const int32_t* src_len, voi
 // C [R,N] = A [R,K] . B [K,N] (b_kc, fp32: B [N,K]^T) of few rows or columns (few_rows.hip)
 bool few_rows_ok(int act_dtype, long long rows, int N);
 int launch_few_rows(int act_dtype, bool b_kc, const void* A, const void* B, void* C, int R, int N, int K, hipStream_t st);
+// bf16: A + A_rest where A_rest is given (few_rows_pair_ok), and what C leaves to C_rest where that is
+bool few_rows_pair_ok(long long rows, int N);
+int launch_few_rows_pair(const void* A, const void* A_rest, const void* B, void* C, void* C_rest, int R, int N, int K, hipStream_t st);
 
 // Losses on token losses (token_loss.hip)
 int launch_preference(const moe_preference_dims& d, long long N, const float* nll, const float* ref, const int32_t* target,

@@ -33,10 +33,12 @@ struct CrossParts {
   int splits;
   float2* stats;             // [B kv_heads columns, splits]
   float* sums;               // [B kv_heads columns, splits, d]
+  float* firsts;             // [B kv_heads columns, splits]: in pairs with statistics, the sum of exponentials of the first terms' scores
 };
 // few: blocks of 32 columns whose wavefronts take the states' blocks in turn, in `splits` ranges; else blocks of 128 columns
 struct CrossPlan { bool few; int splits; };
 CrossPlan cross_plan(int act_dtype, const CrossShape& s);
+CrossPlan cross_pair_plan(const CrossShape& s);            // q and ctx in pairs: of 16 and 64 columns
 // Blocks of 64 columns in a range of dK's and dV's (bf16), by what the calls are expected to take (us): a block of 128 states walks its range's blocks in
 // steps, the ranges' sums cost a launch and their way to memory and back, and ranges are only made while all blocks run at once (a unit has two at d 64).
 // us of one range / the best number of them: 4 x 2000 tokens, 1000 states, 8 heads of 128 on one 455 / 87 (8), of 64 295 / 51 (16); 7 x 1561, up to 66, 2 on one

@@ -12,6 +12,10 @@
 //   lse       is kept in units of log2 (fp32: natural): the exponentials of the backward pass are powers of two.
 //   P, dS     are rounded to bf16 in front of the second products, as the self-attention of whole blocks does: three terms of them
 //             (attention_mfma.hip, RAGGED) triple those products, and q, ctx and the results are rounded as much anyway.
+//   pairs     where tokens are few (generation) the forward pass carries q, P and ctx as pairs of bf16, 16 bits.  A wavefront's tile then has 16
+//             columns, first terms in its columns 0 .. 15 and second ones in 16 .. 31: scores are the sums of both halves, P goes into the products as
+//             both, ctx is the sum of both again.  That takes no more products or reads than a tile that few tokens do not fill, and as the lanes of
+//             a pair share the exponentials, no more instructions.
 //
 // us (16 heads of 128, 32 x 1024 tokens and states): forward 338, dq 412, dK and dV 550, i.e. 0.81, 1.0 and 1.0 PFLOP/s, 4 to 5 % behind the
 // self-attention's; what bounds them is the same: the vector unit forward, the matrix pipes backward, at the 1.7 to 1.9 GHz that power leaves.  One token
@@ -60,9 +64,10 @@ __device__ __forceinline__ void stage_own_rows(uint32_t lds, int lane, F&& addre
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds + q * 1024), "v"(src) : "memory");
   }
 }
-// The wavefront's result tiles times factor as whole rows, turned through its own LDS block: put(row, chunk, 16 bytes).
-template <int D, int CT, typename F>
-__device__ __forceinline__ void store_rows(const f32x16_t (&acc)[CT][D / 32], float factor, uint32_t lds, int lane, F&& put) {
+// The wavefront's result tiles as whole rows, turned through its own LDS block: packed(c, dt, i) is bf16 of the values 2 i and 2 i + 1 of tile dt of
+// the columns 32 c .. + 31; put(row, chunk, 16 bytes).
+template <int D, int CT, typename P, typename F>
+__device__ __forceinline__ void store_packed(P&& packed, uint32_t lds, int lane, F&& put) {
   using GM = AttGeom<D>;
   typedef u32x2_t __attribute__((address_space(3))) * lds_u2_ptr;
   const int r = lane & 31, hf = lane >> 5;
@@ -73,8 +78,7 @@ __device__ __forceinline__ void store_rows(const f32x16_t (&acc)[CT][D / 32], fl
 #pragma unroll
       for (int g = 0; g < 4; ++g)
         *(lds_u2_ptr)(uintptr_t)(lds + (32 * c + r) * GM::kRow + (((4 * dt + g) ^ att_swizzle<D>(r)) << 4) + 8 * hf) =
-            u32x2_t{pack_bf16x2(acc[c][dt][4 * g] * factor, acc[c][dt][4 * g + 1] * factor),
-                    pack_bf16x2(acc[c][dt][4 * g + 2] * factor, acc[c][dt][4 * g + 3] * factor)};
+            u32x2_t{packed(c, dt, 2 * g), packed(c, dt, 2 * g + 1)};
 #pragma unroll
   for (int q = 0; q < 32 * CT * GM::kRow / 1024; ++q) {
     const int row = GM::kRowsPerCopy * q + lane / GM::kChunks, chunk = lane % GM::kChunks;
@@ -82,18 +86,24 @@ __device__ __forceinline__ void store_rows(const f32x16_t (&acc)[CT][D / 32], fl
     put(row, chunk, v);
   }
 }
+// The tiles times factor.
+template <int D, int CT, typename F>
+__device__ __forceinline__ void store_rows(const f32x16_t (&acc)[CT][D / 32], float factor, uint32_t lds, int lane, F&& put) {
+  store_packed<D, CT>([&](int c, int dt, int i) __attribute__((always_inline)) { return pack_bf16x2(acc[c][dt][2 * i] * factor, acc[c][dt][2 * i + 1] * factor); },
+                      lds, lane, put);
+}
 
 // a b, rounded: the difference to a number that was computed so is exact
 __device__ __forceinline__ float rounded_product(float a, float b) {
 #pragma clang fp contract(off)
   return a * b;
 }
-// the block's (source, key head), and the wavefront's first column of `blocks` blocks of 128 CT
-template <int CT> struct CrossWork {
+// the block's (source, key head), and the wavefront's first column, of blocks of PER columns, a quarter a wavefront
+template <int PER> struct CrossWork {
   long long bk, b;
   int k, block0, col0, range;
   __device__ __forceinline__ CrossWork(int count, int kv_heads, int wave, unsigned ranges = 1) {
-    const int blocks = (count + 128 * CT - 1) / (128 * CT);
+    const int blocks = (count + PER - 1) / PER;
     unsigned work = xcd_contiguous(blockIdx.x, gridDim.x);
     range = __builtin_amdgcn_readfirstlane(work % ranges);
     work /= ranges;
@@ -101,39 +111,74 @@ template <int CT> struct CrossWork {
     bk = pair;
     k = __builtin_amdgcn_readfirstlane(pair % kv_heads);
     b = __builtin_amdgcn_readfirstlane(pair / kv_heads);
-    block0 = __builtin_amdgcn_readfirstlane((int)(work % blocks) * (128 * CT));
-    col0 = block0 + wave * (32 * CT);
+    block0 = __builtin_amdgcn_readfirstlane((int)(work % blocks) * PER);
+    col0 = block0 + wave * (PER / 4);
   }
 };
 
-// zeros to the columns first .. first + 127 of a block, 256 threads
-template <int D>
+// zeros to the columns first .. first + PER - 1 of a block, 256 threads
+template <int D, int PER = 128>
 __device__ __forceinline__ void clear_columns(bf16_t* base, const CrossCols& c, int first) {
-  for (int i = threadIdx.x; i < 128 * (D / 8); i += 256) {
+  for (int i = threadIdx.x; i < PER * (D / 8); i += 256) {
     const int col = first + i / (D / 8);
     if (col < c.count) *reinterpret_cast<u32x4_t*>(base + c.offset<D>(col) + 8 * (i % (D / 8))) = u32x4_t{0u, 0u, 0u, 0u};
   }
 }
 
+// Of a pair of columns c and c + 16, which lanes c and c + 16 hold (one row of 16 lanes and the next; a swap exchanges the odd rows of its first operand with
+// the even ones of its second): the sums over the pair of two values, a's in the first lane and b's in the second, and the first terms of these sums.
+struct PairFold { float sum, first; };
+__device__ __forceinline__ PairFold pair_fold(float a, float b) {
+  const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+  return {pair_sum(__uint_as_float(x[0]), __uint_as_float(x[1])), __uint_as_float(x[0])};
+}
+// over the four lanes of a pair of columns
+__device__ __forceinline__ float pair_max(float v) {
+  const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  const uint32_t m = __float_as_uint(fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])));
+  const auto y = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+  return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+__device__ __forceinline__ float pair_total(float v) {
+  const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  const uint32_t t = __float_as_uint(__uint_as_float(x[0]) + __uint_as_float(x[1]));
+  const auto y = __builtin_amdgcn_permlane32_swap(t, t, false, false);
+  return __uint_as_float(y[0]) + __uint_as_float(y[1]);
+}
+// The way back for two numbers of each lane: those of the first lane (a) and of the second (b), as bf16 terms, first ones in the first lane.
+struct PairTerms { uint32_t a, b; };
+template <bool FINITE>
+__device__ __forceinline__ PairTerms pair_terms(float x, float y) {
+  const uint32_t rounded = pack_bf16x2(x, y);
+  const uint32_t rest = FINITE ? pack_bf16x2(x - __uint_as_float(rounded << 16), y - __uint_as_float(rounded & 0xffff0000u)) : bf16_rest_x2(x, y, rounded);
+  const auto f = __builtin_amdgcn_permlane16_swap(rounded, rest, false, false);
+  return {f[0], f[1]};
+}
+
 // ---------------------------------------------------------------- forward
-template <int D>
-__global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossGeo g, const bf16_t* __restrict__ q, const bf16_t* __restrict__ kv,
-                                                               const int32_t* __restrict__ src_len, bf16_t* __restrict__ ctx,
-                                                               float* __restrict__ lse) {
+// PAIR: q + q_rest, ctx + ctx_rest.  STATS: with row statistics.  The backward pass has a q of one term, of whose scores the statistics of a pair are: its
+// probabilities add up to 1.
+template <int D, bool PAIR, bool STATS>
+__global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossGeo g, const bf16_t* __restrict__ q, const bf16_t* __restrict__ q_rest,
+                                                               const bf16_t* __restrict__ kv, const int32_t* __restrict__ src_len,
+                                                               bf16_t* __restrict__ ctx, bf16_t* __restrict__ ctx_rest, float* __restrict__ lse) {
   using GM = AttGeom<D>;
-  constexpr int CT = 1, KS = D / 16, DT = D / 32, kOwnBlock = 32 * CT * GM::kRow;
+  static_assert(PAIR || STATS, "a single term's statistics take nothing: written where there is an lse");
+  constexpr int CT = 1, KS = D / 16, DT = D / 32, kOwnBlock = 32 * CT * GM::kRow, kTile = PAIR ? 16 : 32;
   constexpr int kV = 2 * GM::kBlock;                           // LDS: two K blocks, two V blocks
   extern __shared__ __attribute__((aligned(256))) unsigned char att_lds[];
   const uint32_t lds0 = (uint32_t)(uintptr_t)((lds_ptr)att_lds);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 31, hf = lane >> 5;
+  const bool second = PAIR && r >= 16;
   const CrossCols cols(g, D);
-  const CrossWork<CT> w(cols.count, g.kv_heads, wave);
+  const CrossWork<4 * kTile> w(cols.count, g.kv_heads, wave);
   const size_t head = cols.base(w.b, w.k, D);
   const int n = held_states(src_len, w.b, g.Lk);
   if (n == 0) {
-    clear_columns<D>(ctx + head, cols, w.block0);
-    if (lse != nullptr && threadIdx.x < 128 && w.block0 + (int)threadIdx.x < cols.count) lse[(size_t)w.bk * cols.count + w.block0 + threadIdx.x] = 0.f;
+    clear_columns<D, 4 * kTile>(ctx + head, cols, w.block0);
+    if constexpr (PAIR) clear_columns<D, 4 * kTile>(ctx_rest + head, cols, w.block0);
+    if (STATS && lse != nullptr && threadIdx.x < 4 * kTile && w.block0 + (int)threadIdx.x < cols.count) lse[(size_t)w.bk * cols.count + w.block0 + threadIdx.x] = 0.f;
     return;
   }
   const int Akv = g.kv_heads * D;
@@ -156,7 +201,9 @@ __global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossGeo g, const
 #pragma unroll
   for (int x = 0; x < GM::kCopies; ++x) { start(-1, x); start(0, GM::kCopies + x); }     // K and V block 0
   if (live)
-    stage_own_rows<D, CT>(lds0 + own, lane, [&](int row) __attribute__((always_inline)) { return q + head + cols.offset<D>(cols.within(w.col0 + row)); });
+    stage_own_rows<D, CT>(lds0 + own, lane, [&](int row) __attribute__((always_inline)) {
+      return (row < kTile ? q : q_rest) + head + cols.offset<D>(cols.within(w.col0 + row % kTile));
+    });
   wait_all_copies();
 
   const float sl2 = 1.4426950408889634f / sqrtf((float)D);
@@ -191,30 +238,48 @@ __global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossGeo g, const
     for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
   // running maximum (in log2 units) and sum; the maximum starts finite, so that a block of states whose scores
   // are all -inf adds nothing
-  float m_run = -FLT_MAX, l_run = 0.f, m_new;
-  f32x16_t sacc[2];                                            // scores of block kb [32-state tile], and the maximum with them
+  float m_run = -FLT_MAX, l_run = 0.f, l_first = 0.f, m_new;
+  // scores of block kb [32-state tile], and the maximum with them; PAIR: [0] only, of the tile 0 in the first lane of a pair and of 1 in the second.  Their first
+  // terms wait in LDS (16 registers more spill at d 128: 64 x 2 tokens, 1000 states, 16 heads 100 us, not 68).
+  f32x16_t sacc[2];
+  auto first_terms = [&](int i4) __attribute__((always_inline)) { return (lds_f4_ptr)(uintptr_t)(lds0 + 2 * kV + (4 * wave + i4) * 1024 + lane * 16); };
   auto mask_end = [&](f32x16_t (&acc)[2], int kb) __attribute__((always_inline)) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int t = 0; t < (PAIR ? 1 : 2); ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i)
-        if (kb * 64 + 32 * t + 8 * (i >> 2) + 4 * hf + (i & 3) >= n) acc[t][i] = -INFINITY;
+        if (kb * 64 + 32 * (PAIR ? second : t) + 8 * (i >> 2) + 4 * hf + (i & 3) >= n) acc[t][i] = -INFINITY;
   };
   auto block_max = [&](const f32x16_t (&acc)[2]) __attribute__((always_inline)) {
     float mx = -INFINITY;
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int t = 0; t < (PAIR ? 1 : 2); ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, acc[t][i]);
     return mx;
   };
+  auto fold4 = [&](f32x16_t (&acc)[2], int i4) __attribute__((always_inline)) {
+    f32x4_t first;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const PairFold f = pair_fold(acc[0][4 * i4 + i], acc[1][4 * i4 + i]);
+      acc[0][4 * i4 + i] = f.sum;
+      first[i] = f.first;
+    }
+    if constexpr (STATS) *first_terms(i4) = first;
+  };
   auto new_max = [&](float mx) __attribute__((always_inline)) {
-    m_new = fmaxf(m_run, fmaxf(mx, __shfl_xor(mx, 32, 64)) * sl2);        // sl2 > 0: scaling commutes with max
+    mx = PAIR ? pair_max(mx) : fmaxf(mx, __shfl_xor(mx, 32, 64));
+    m_new = fmaxf(m_run, mx * sl2);                            // sl2 > 0: scaling commutes with max
   };
 #pragma unroll
   for (int t = 0; t < 2; ++t)
 #pragma unroll
     for (int s = 0; s < KS; ++s) sacc[t] = MOE_MFMA(rd.row(0, t, s), qf[s], s == 0 ? f32x16_t{} : sacc[t]);
+  if constexpr (PAIR) {
+#pragma unroll
+    for (int i4 = 0; i4 < 4; ++i4) fold4(sacc, i4);
+  }
   if (64 > n) mask_end(sacc, 0);
   new_max(block_max(sacc));
 
@@ -222,6 +287,7 @@ __global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossGeo g, const
   auto step = [&](int kb, auto last) __attribute__((always_inline)) {
     constexpr bool LAST = decltype(last)::value;
     constexpr int FIRST = LAST ? 2 * KS : 0;                   // (units 0 .. 2 KS - 1 are those scores)
+    constexpr int kAhead = PAIR && STATS && D == 128 ? 3 : 4;  // (registers)
     wait_all_copies();                                         // K block kb + 1 and V block kb are there;
     __syncthreads();                                           // K block kb and V block kb - 1 are read, their places free
     const uint32_t kst = ((kb + 1) & 1) * GM::kBlock, vst = kV + (kb & 1) * GM::kBlock;
@@ -229,6 +295,7 @@ __global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossGeo g, const
     if (__builtin_amdgcn_ballot_w64(m_new != m_run) != 0) {
       const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);   // 0 on the first block
       l_run *= alpha;
+      if constexpr (PAIR && STATS) l_first *= alpha;
 #pragma unroll
       for (int t = 0; t < DT; ++t)
 #pragma unroll
@@ -237,23 +304,40 @@ __global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossGeo g, const
     m_run = m_new;
     float psum = 0.f, mx = -INFINITY;
     f32x16_t snext[2];
-    u32x4_t pf[2];                                             // P^T, k step % 2
-    auto exponentials = [&](int t, int first, int last) __attribute__((always_inline)) {
+    constexpr int PF = PAIR ? 4 : 2;
+    u32x4_t pf[PF];                                            // P^T, k step % PF
+    // probabilities 2 i and 2 i + 1 of both lanes of a pair to the fragments of tile 0 and of tile 1
+    auto terms = [&](int i) __attribute__((always_inline)) {
+      const PairTerms p = pair_terms<true>(sacc[0][2 * i], sacc[0][2 * i + 1]);
+      pf[i / 4][i % 4] = p.a;
+      pf[(2 + i / 4) % PF][i % 4] = p.b;
+    };
+    f32x4_t first;
+    auto exponentials = [&](int t, int from, int to) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = first; i < last; ++i) {
+      for (int i = from; i < to; ++i) {
         const float v = __builtin_amdgcn_exp2f(fmaf(sacc[t][i], sl2, -m_run));
         sacc[t][i] = v;
         psum += v;
+        if constexpr (PAIR && STATS) {
+          if (i % 4 == 0) first = *first_terms(i / 4);
+          l_first += v == 0.f ? 0.f : __builtin_amdgcn_exp2f(fmaf(first[i % 4], sl2, -m_run));      // (of a state past the end: v is 0)
+        }
       }
     };
     if constexpr (LAST) {
       exponentials(0, 0, 16);
-      pf[0] = pack8(sacc[0], 0);
-      pf[1] = pack8(sacc[0], 8);
+      if constexpr (PAIR) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) terms(i);
+      } else {
+        pf[0] = pack8(sacc[0], 0);
+        pf[1] = pack8(sacc[0], 8);
+      }
     }
     // units 0 .. 2 KS - 1: scores of block kb + 1, under them the first tile's exponentials; then 4 DT units of O^T, under
     // them the second tile's and the next block's maximum
-    run_units<FIRST, 2 * KS + 4 * DT, 4>(
+    run_units<FIRST, 2 * KS + 4 * DT, kAhead>(
         [&](auto) __attribute__((always_inline)) { return std::integral_constant<int, 1>{}; },
         [&](auto U) __attribute__((always_inline)) {
           constexpr int u = decltype(U)::value, v = u - 2 * KS;
@@ -263,15 +347,29 @@ __global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossGeo g, const
         [&](auto U, auto, const u32x4_t& f) __attribute__((always_inline)) {
           constexpr int u = decltype(U)::value, v = u - 2 * KS;
           if constexpr (u < 2 * KS) snext[u / KS] = MOE_MFMA(f, qf[u % KS], u % KS == 0 ? f32x16_t{} : snext[u / KS]);
-          else o[v % DT] = MOE_MFMA(f, pf[(v / DT) % 2], o[v % DT]);
+          else o[v % DT] = MOE_MFMA(f, pf[(v / DT) % PF], o[v % DT]);
         },
         [&](auto U, auto, auto) __attribute__((always_inline)) {
           constexpr int u = decltype(U)::value, v = u - 2 * KS;
           if constexpr (!LAST && u < COPIES) start(kb + 1, u);
           if constexpr (u < 2 * KS) {
             exponentials(0, u * 8 / KS, (u + 1) * 8 / KS);
-            if constexpr (u == KS + 1) pf[0] = pack8(sacc[0], 0);
-            if constexpr (u == 2 * KS - 1) pf[1] = pack8(sacc[0], 8);
+            if constexpr (PAIR) {                              // (two at a time: a swap's operands and results take wait states)
+              if constexpr (u > 0 && u % (KS / 2) == 0) { terms(u / (KS / 2) * 2 - 2); terms(u / (KS / 2) * 2 - 1); }
+            } else {
+              if constexpr (u == KS + 1) pf[0] = pack8(sacc[0], 0);
+              if constexpr (u == 2 * KS - 1) pf[1] = pack8(sacc[0], 8);
+            }
+          } else if constexpr (PAIR) {
+            if constexpr (!LAST && v == 0) { terms(6); terms(7); }
+            constexpr int gap = 4 * DT / 5, x = v - 1;         // four scores at a time (not right behind their last product), a unit later their maximum
+            if constexpr (!LAST && x >= 0 && x % gap == 0 && x / gap < 4) {
+              fold4(snext, x / gap);
+            }
+            if constexpr (!LAST && x >= 1 && (x - 1) % gap == 0 && (x - 1) / gap < 4) {
+#pragma unroll
+              for (int j = (x - 1) / gap * 4; j < (x - 1) / gap * 4 + 4; ++j) mx = fmaxf(mx, snext[0][j]);
+            }
           } else if constexpr (v < 2 * DT) {
             exponentials(1, v * 16 / (2 * DT), (v + 1) * 16 / (2 * DT));
             // the fragment of k step 0 is free after DT units, the second tile's first 8 values done by then
@@ -285,7 +383,7 @@ __global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossGeo g, const
             }
           }
         });
-    l_run += psum + __shfl_xor(psum, 32, 64);
+    l_run += PAIR ? psum : psum + __shfl_xor(psum, 32, 64);    // PAIR: each lane's own, added up at the end
     if constexpr (LAST) return;
     if (kb + 2 == nkb && (n & 63) != 0) {                      // the last block comes next: without its rows past the end
       mask_end(snext, kb + 1);
@@ -293,18 +391,36 @@ __global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossGeo g, const
     }
     new_max(mx);
     sacc[0] = snext[0];
-    sacc[1] = snext[1];
+    if constexpr (!PAIR) sacc[1] = snext[1];
   };
   for (int kb = 0; kb + 1 < nkb; ++kb) step(kb, std::false_type{});
   step(nkb - 1, std::true_type{});
   __syncthreads();                                             // the other wavefronts have read the last blocks
-  const int c = w.col0 + r;
+  const int c = w.col0 + r % kTile;
   // row statistic for the backward pass: log2 sum_k exp(score)
-  if (lse != nullptr && hf == 0 && c < cols.count) lse[(size_t)w.bk * cols.count + c] = m_run + log2f(l_run);
-  const f32x16_t (&tiles)[1][DT] = reinterpret_cast<const f32x16_t (&)[1][DT]>(o);
-  store_rows<D, CT>(tiles, 1.0f / l_run, lds0 + own, lane, [&](int row, int chunk, const u32x4_t& v) __attribute__((always_inline)) {
-    if (w.col0 + row < cols.count) *reinterpret_cast<u32x4_t*>(ctx + head + cols.offset<D>(w.col0 + row) + 8 * chunk) = v;
-  });
+  if constexpr (STATS) {
+    const float l = PAIR ? pair_total(l_first) : l_run;
+    if (lse != nullptr && hf == 0 && !second && c < cols.count) lse[(size_t)w.bk * cols.count + c] = m_run + log2f(l);
+  }
+  const float inv = 1.0f / (PAIR ? pair_total(l_run) : l_run);
+  auto put = [&](int row, int chunk, const u32x4_t& v) __attribute__((always_inline)) {
+    const int col = w.col0 + row % kTile;
+    if (col < cols.count) *reinterpret_cast<u32x4_t*>((row < kTile ? ctx : ctx_rest) + head + cols.offset<D>(col) + 8 * chunk) = v;
+  };
+  if constexpr (PAIR) {                                        // tiles t and t + 1: the sums of the one in the first lane of a pair, of the other in the second
+    uint32_t terms[DT][8];
+#pragma unroll
+    for (int t = 0; t < DT; t += 2)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const PairTerms p = pair_terms<false>(pair_fold(o[t][2 * i], o[t + 1][2 * i]).sum * inv, pair_fold(o[t][2 * i + 1], o[t + 1][2 * i + 1]).sum * inv);
+        terms[t][i] = p.a;
+        terms[t + 1][i] = p.b;
+      }
+    store_packed<D, CT>([&](int, int dt, int i) __attribute__((always_inline)) { return terms[dt][i]; }, lds0 + own, lane, put);
+  } else {
+    store_rows<D, CT>(reinterpret_cast<const f32x16_t (&)[1][DT]>(o), inv, lds0 + own, lane, put);
+  }
 }
 
 // Start the copies of a wavefront's block of 32 states: rows of K, then of V, zeros from row `rows` on.
@@ -330,28 +446,31 @@ __device__ __forceinline__ void stage_few(uint32_t lds, const bf16_t* keys, int 
 // way while the other is used: no barrier, 64 KB (d 128) on their way to a compute unit.  Memory bounds it, so the products are
 // not what counts: P keeps its 24 bits as three terms.
 constexpr int kFewWaves = 4;
-template <int D>
-__global__ __launch_bounds__(64 * kFewWaves, 1) void cross_few_kernel(CrossGeo g, const bf16_t* __restrict__ q, const bf16_t* __restrict__ kv,
-                                                           const int32_t* __restrict__ src_len, bf16_t* __restrict__ ctx,
-                                                           float* __restrict__ lse, CrossParts parts) {
+template <int D, bool PAIR, bool STATS>
+__global__ __launch_bounds__(64 * kFewWaves, 1) void cross_few_kernel(CrossGeo g, const bf16_t* __restrict__ q, const bf16_t* __restrict__ q_rest,
+                                                           const bf16_t* __restrict__ kv, const int32_t* __restrict__ src_len,
+                                                           bf16_t* __restrict__ ctx, bf16_t* __restrict__ ctx_rest, float* __restrict__ lse,
+                                                           CrossParts parts) {
   using GM = AttGeom<D>;
   constexpr int W = kFewWaves, KS = D / 16, DT = D / 32, kHalf = 32 * GM::kRow, kPlace = 2 * kHalf, COPIES = kHalf / 1024;      // K rows, V rows
+  constexpr int kTile = PAIR ? 16 : 32;
   extern __shared__ __attribute__((aligned(256))) unsigned char att_lds[];
   const uint32_t lds0 = (uint32_t)(uintptr_t)((lds_ptr)att_lds);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 31, hf = lane >> 5;
+  const bool second = PAIR && r >= 16;
   const CrossCols cols(g, D);
-  const int tiles = (cols.count + 31) / 32;
+  const int tiles = (cols.count + kTile - 1) / kTile;
   unsigned item = xcd_contiguous(blockIdx.x, gridDim.x);
   const int split = __builtin_amdgcn_readfirstlane(item % parts.splits);
   item /= parts.splits;
   const unsigned pair = item / tiles;
   const int k = __builtin_amdgcn_readfirstlane(pair % g.kv_heads), b = __builtin_amdgcn_readfirstlane(pair / g.kv_heads);
-  const int c = (int)(item % tiles) * 32 + r;
+  const int c = (int)(item % tiles) * kTile + r % kTile;
   const size_t row = cols.base(b, k, D) + cols.offset<D>(cols.within(c));
   u32x4_t qf[KS];
 #pragma unroll
-  for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const u32x4_t*>(q + row + 16 * s + 8 * hf);
+  for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const u32x4_t*>((second ? q_rest : q) + row + 16 * s + 8 * hf);
   const int n = held_states(src_len, b, g.Lk), Akv = g.kv_heads * D;
   const size_t ld = (size_t)2 * Akv;
   const bf16_t* const keys = kv + (size_t)b * g.Lk * ld + (size_t)k * D;
@@ -372,7 +491,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void cross_few_kernel(CrossGeo g
   f32x16_t o[DT];
 #pragma unroll
   for (int t = 0; t < DT; ++t) o[t] = f32x16_t{};
-  float m_run = -FLT_MAX, l_run = 0.f;                         // (finite: a block whose scores are all -inf adds nothing)
+  float m_run = -FLT_MAX, l_run = 0.f, l_first = 0.f;          // (finite: a block whose scores are all -inf adds nothing)
   if (from < to) start(from, 0);
   int p = 0;
   for (int kb = from; kb < to; kb += W, p ^= 1) {
@@ -386,16 +505,31 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void cross_few_kernel(CrossGeo g
     f32x16_t s;
 #pragma unroll
     for (int i = 0; i < KS; ++i) s = MOE_MFMA(rd.row(place, 0, i), qf[i], i == 0 ? f32x16_t{} : s);
+    // PAIR: the first lane of a pair has the scores of the block's first 16 states, the second one those of the others
+    constexpr int VALUES = PAIR ? 8 : 16;
+    if constexpr (PAIR) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const PairFold f = pair_fold(s[i], s[i + 8]);
+        s[i] = f.sum;
+        if constexpr (STATS) s[i + 8] = f.first;
+      }
+    }
     float mx = -INFINITY, psum = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      if (32 * kb + 8 * (i >> 2) + 4 * hf + (i & 3) >= n) s[i] = -INFINITY;
+    for (int i = 0; i < VALUES; ++i) {
+      if (32 * kb + 16 * second + 8 * (i >> 2) + 4 * hf + (i & 3) >= n) {
+        s[i] = -INFINITY;
+        if constexpr (PAIR && STATS) s[i + 8] = -INFINITY;
+      }
       mx = fmaxf(mx, s[i]);
     }
-    const float m_new = fmaxf(m_run, fmaxf(mx, __shfl_xor(mx, 32, 64)) * sl2);
+    mx = PAIR ? pair_max(mx) : fmaxf(mx, __shfl_xor(mx, 32, 64));
+    const float m_new = fmaxf(m_run, mx * sl2);
     if (__builtin_amdgcn_ballot_w64(m_new != m_run) != 0) {
       const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
       l_run *= alpha;
+      if constexpr (PAIR && STATS) l_first *= alpha;
 #pragma unroll
       for (int t = 0; t < DT; ++t)
 #pragma unroll
@@ -403,20 +537,32 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void cross_few_kernel(CrossGeo g
       m_run = m_new;
     }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < VALUES; ++i) {
       s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], sl2, -m_run));
       psum += s[i];
+      if constexpr (PAIR && STATS) l_first += __builtin_amdgcn_exp2f(fmaf(s[i + 8], sl2, -m_run));
     }
-    l_run += psum + __shfl_xor(psum, 32, 64);
+    l_run += PAIR ? pair_total(psum) : psum + __shfl_xor(psum, 32, 64);
+    u32x4_t both[2];
+    if constexpr (PAIR) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const PairTerms p = pair_terms<true>(s[2 * i], s[2 * i + 1]);
+        both[0][i] = p.a;
+        both[1][i] = p.b;
+      }
+    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      bf16x8_bits_t pf[3];
-      split_bf16x8(s, 8 * h, pf);
+      constexpr int TERMS = PAIR ? 1 : 3;
+      bf16x8_bits_t pf[TERMS];
+      if constexpr (PAIR) pf[0] = both[h];
+      else split_bf16x8(s, 8 * h, pf);
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
         const u32x4_t vt = rd.transposed(place + kHalf, 16 * h, dt);
 #pragma unroll
-        for (int x = 2; x >= 0; --x) o[dt] = MOE_MFMA(vt, pf[x], o[dt]);
+        for (int x = TERMS - 1; x >= 0; --x) o[dt] = MOE_MFMA(vt, pf[x], o[dt]);
       }
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // the place is read before the next copies go there
@@ -428,12 +574,18 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void cross_few_kernel(CrossGeo g
   auto at = [&](uint32_t byte) __attribute__((always_inline)) { return (lds_f_ptr)(uintptr_t)(lds0 + byte); };
   *at(kStats + (wave * 64 + lane) * 4) = m_run;
   *at(kStats + 256 * W + (wave * 64 + lane) * 4) = l_run;
+  if constexpr (PAIR && STATS) *at(kStats + 512 * W + (wave * 64 + lane) * 4) = pair_total(l_first);
   __syncthreads();
   float m = m_run, l = 0.f;
+  l_first = 0.f;
 #pragma unroll
   for (int x = 0; x < W; ++x) m = fmaxf(m, *at(kStats + (x * 64 + lane) * 4));
 #pragma unroll
   for (int x = 0; x < W; ++x) l += *at(kStats + 256 * W + (x * 64 + lane) * 4) * __builtin_amdgcn_exp2f(*at(kStats + (x * 64 + lane) * 4) - m);
+  if constexpr (PAIR && STATS) {
+#pragma unroll
+    for (int x = 0; x < W; ++x) l_first += *at(kStats + 512 * W + (x * 64 + lane) * 4) * __builtin_amdgcn_exp2f(*at(kStats + (x * 64 + lane) * 4) - m);
+  }
   const float alpha = __builtin_amdgcn_exp2f(m_run - m);       // (a wavefront without a block: sums of 0)
 #pragma unroll
   for (int t = 0; t < DT; ++t)
@@ -442,9 +594,13 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void cross_few_kernel(CrossGeo g
   __syncthreads();
   if (c >= cols.count) return;
   const size_t column = ((size_t)b * g.kv_heads + k) * cols.count + c;
-  if (wave == 0 && hf == 0) {
-    if (parts.splits > 1) parts.stats[column * parts.splits + split] = float2{m, l};
-    else if (lse != nullptr) lse[column] = n == 0 ? 0.f : m + log2f(l);
+  if (wave == 0 && hf == 0 && !second) {
+    if (parts.splits > 1) {
+      parts.stats[column * parts.splits + split] = float2{m, l};
+      if constexpr (PAIR && STATS) parts.firsts[column * parts.splits + split] = l_first;
+    } else if (STATS && lse != nullptr) {
+      lse[column] = n == 0 ? 0.f : m + log2f(PAIR ? l_first : l);
+    }
   }
   const float inv = n == 0 ? 0.f : 1.0f / l;
 #pragma unroll
@@ -455,16 +611,28 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void cross_few_kernel(CrossGeo g
       v[i] = 0.f;
 #pragma unroll
       for (int x = 0; x < W; ++x) v[i] += *at(((x * DT + dt) * 16 + i) * 256 + lane * 4);
+      if constexpr (PAIR) v[i] = pair_fold(v[i], v[i]).sum;
     }
     if (parts.splits > 1) {
+      if (second) continue;
       float* const to_ = parts.sums + (column * parts.splits + split) * D + 32 * dt + 4 * hf;
 #pragma unroll
       for (int x = 0; x < 4; ++x) *reinterpret_cast<f32x4_t*>(to_ + 8 * x) = f32x4_t{v[4 * x], v[4 * x + 1], v[4 * x + 2], v[4 * x + 3]};
     } else {
+      if constexpr (PAIR) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          v[i] *= inv;
+          v[i] = second ? bf16_rest(v[i], (float)(__bf16)v[i]) : v[i];
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] *= inv;
+      }
 #pragma unroll
       for (int x = 0; x < 4; ++x)
-        *reinterpret_cast<u32x2_t*>(ctx + row + 32 * dt + 8 * x + 4 * hf) =
-            u32x2_t{pack_bf16x2(v[4 * x] * inv, v[4 * x + 1] * inv), pack_bf16x2(v[4 * x + 2] * inv, v[4 * x + 3] * inv)};
+        *reinterpret_cast<u32x2_t*>((second ? ctx_rest : ctx) + row + 32 * dt + 8 * x + 4 * hf) =
+            u32x2_t{pack_bf16x2(v[4 * x], v[4 * x + 1]), pack_bf16x2(v[4 * x + 2], v[4 * x + 3])};
     }
   }
 }
@@ -472,7 +640,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void cross_few_kernel(CrossGeo g
 // The ranges of a column put together: a wavefront a column, lanes over the ranges (64 at most), then over d.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void cross_join_kernel(CrossGeo g, CrossParts parts, const int32_t* __restrict__ src_len, T* __restrict__ ctx,
-                                                         float* __restrict__ lse, long long columns) {
+                                                         T* __restrict__ ctx_rest, float* __restrict__ lse, long long columns) {
   constexpr bool F32 = sizeof(T) == 4;                         // (units of the maxima)
   const int lane = threadIdx.x & 63;
   const long long column = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -484,6 +652,8 @@ __global__ __launch_bounds__(256) void cross_join_kernel(CrossGeo g, CrossParts 
   const float m = wave_max(st.x);
   const float f = F32 ? expf(st.x - m) : __builtin_amdgcn_exp2f(st.x - m);
   const float l = wave_sum(st.y * f);
+  float l_stat = l;                                            // (of a pair's first terms: what the forward pass's kernel left)
+  if (!F32 && ctx_rest != nullptr && lse != nullptr) l_stat = wave_sum((lane < parts.splits ? parts.firsts[column * parts.splits + lane] : 0.f) * f);
   float v[D / 64] = {};
   const float* const sums = parts.sums + column * parts.splits * D + lane * (D / 64);
   for (int s = 0; s < parts.splits; s += 8) {                  // eight on their way at a time
@@ -498,11 +668,15 @@ __global__ __launch_bounds__(256) void cross_join_kernel(CrossGeo g, CrossParts 
       for (int i = 0; i < D / 64; ++i) v[i] = fmaf(x[j][i], __shfl(f, s + j, 64), v[i]);
   }
   const bool none = held_states(src_len, b, g.Lk) == 0;
-  if (lse != nullptr && lane == 0) lse[column] = none ? 0.f : F32 ? m + logf(l) : m + log2f(l);
+  if (lse != nullptr && lane == 0) lse[column] = none ? 0.f : F32 ? m + logf(l_stat) : m + log2f(l_stat);
   const float inv = none ? 0.f : 1.0f / l;
-  T* const to = ctx + cols.base(b, k, D) + cols.offset<D>(c) + lane * (D / 64);
+  const size_t to = cols.base(b, k, D) + cols.offset<D>(c) + lane * (D / 64);
 #pragma unroll
-  for (int i = 0; i < D / 64; ++i) Elt<T>::store(to + i, v[i] * inv);
+  for (int i = 0; i < D / 64; ++i) {
+    Elt<T>::store(ctx + to + i, v[i] * inv);
+    if constexpr (!F32)
+      if (ctx_rest != nullptr) Elt<T>::store(ctx_rest + to + i, bf16_rest(v[i] * inv, (float)(__bf16)(v[i] * inv)));
+  }
 }
 
 // ---------------------------------------------------------------- dq (and D) of up to 64 states
@@ -559,7 +733,7 @@ __device__ __forceinline__ void few_states_dq(f32x16_t (&dq)[D / 32], float& dd,
 }
 // A block of 128 columns of such a source.  K and V lie in LDS whole, the columns' rows come straight from memory.
 template <int D>
-__device__ __forceinline__ void few_states_block(const CrossCols& cols, const CrossWork<1>& w, size_t head, int n, int Akv,
+__device__ __forceinline__ void few_states_block(const CrossCols& cols, const CrossWork<128>& w, size_t head, int n, int Akv,
                                                  const uint32_t (&off)[AttGeom<D>::kCopies], const bf16_t* q, const bf16_t* keys,
                                                  const bf16_t* dctx, bf16_t* dqo, float* dvec, uint32_t lds0, int wave, int lane) {
   using GM = AttGeom<D>;
@@ -601,7 +775,7 @@ __global__ __launch_bounds__(256, 2) void cross_dq_short_kernel(CrossGeo g, cons
   const uint32_t lds0 = (uint32_t)(uintptr_t)((lds_ptr)att_lds);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const CrossCols cols(g, D);
-  const CrossWork<1> w(cols.count, g.kv_heads, wave);
+  const CrossWork<128> w(cols.count, g.kv_heads, wave);
   const size_t head = cols.base(w.b, w.k, D);
   const int n = held_states(src_len, w.b, g.Lk), Akv = g.kv_heads * D;
   if (n == 0) {                                                // (no state asks for D)
@@ -629,7 +803,7 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(CrossGeo g, const bf16
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 31, hf = lane >> 5;
   const CrossCols cols(g, D);
-  const CrossWork<CT> w(cols.count, g.kv_heads, wave);
+  const CrossWork<128 * CT> w(cols.count, g.kv_heads, wave);
   const size_t head = cols.base(w.b, w.k, D);
   const int n = held_states(src_len, w.b, g.Lk);
   if (n == 0) {                                                // (no state asks for D)
@@ -938,7 +1112,7 @@ __global__ __launch_bounds__(256, 1) void cross_dkv_kernel(CrossGeo g, const bf1
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 31, hf = lane >> 5;
   const CrossCols cols(g, D);
-  const CrossWork<CT> w(g.Lk, g.kv_heads, wave, RANGES ? ranges.count : 1);
+  const CrossWork<128 * CT> w(g.Lk, g.kv_heads, wave, RANGES ? ranges.count : 1);
   const int n = held_states(src_len, w.b, g.Lk), Akv = g.kv_heads * D;
   const size_t ld = (size_t)2 * Akv;
   const size_t states = (size_t)w.b * g.Lk * ld + (size_t)w.k * D;
@@ -1143,6 +1317,7 @@ __global__ __launch_bounds__(256, 1) void cross_dkv_kernel(CrossGeo g, const bf1
 
 template <int D> constexpr int kLdsFew = kFewWaves * 2 * 64 * AttGeom<D>::kRow;
 template <int D> constexpr int kLdsForward = 4 * AttGeom<D>::kBlock;
+template <int D> constexpr int kLdsForwardPairs = kLdsForward<D> + 16384;        // (two blocks a unit)
 template <int D> constexpr int kLdsQ = 5 * AttGeom<D>::kBlock;
 template <int D> constexpr int kLdsQShort = 2 * AttGeom<D>::kBlock;
 static_assert(kLdsQShort<128> <= 65536, "without a raised limit");
@@ -1150,10 +1325,14 @@ template <int D, int CT> constexpr int kLdsKV = 2 * (2 * AttGeom<D>::kBlock + 51
 
 template <int D>
 int prepare_kernels() {
-  static LdsLimitOnce once, once_few, once_q, once_qfew, once_kvr, once_kv1, once_kv2;
-  static_assert(kLdsFew<D> >= kFewWaves * (128 * D + 512), "the wavefronts' sums and statistics");
-  int rc = ensure_lds_limit(once, reinterpret_cast<const void*>(cross_forward_kernel<D>), kLdsForward<D>);
-  if (rc == MOE_OK) rc = ensure_lds_limit(once_few, reinterpret_cast<const void*>(cross_few_kernel<D>), kLdsFew<D>);
+  static LdsLimitOnce once, once_pair, once_pairs, once_few, once_few_pair, once_few_pairs, once_q, once_qfew, once_kvr, once_kv1, once_kv2;
+  static_assert(kLdsFew<D> >= kFewWaves * (128 * D + 768), "the wavefronts' sums and statistics");
+  int rc = ensure_lds_limit(once, reinterpret_cast<const void*>(cross_forward_kernel<D, false, true>), kLdsForward<D>);
+  if (rc == MOE_OK) rc = ensure_lds_limit(once_pair, reinterpret_cast<const void*>(cross_forward_kernel<D, true, false>), kLdsForward<D>);
+  if (rc == MOE_OK) rc = ensure_lds_limit(once_pairs, reinterpret_cast<const void*>(cross_forward_kernel<D, true, true>), kLdsForwardPairs<D>);
+  if (rc == MOE_OK) rc = ensure_lds_limit(once_few, reinterpret_cast<const void*>(cross_few_kernel<D, false, true>), kLdsFew<D>);
+  if (rc == MOE_OK) rc = ensure_lds_limit(once_few_pair, reinterpret_cast<const void*>(cross_few_kernel<D, true, false>), kLdsFew<D>);
+  if (rc == MOE_OK) rc = ensure_lds_limit(once_few_pairs, reinterpret_cast<const void*>(cross_few_kernel<D, true, true>), kLdsFew<D>);
   if (rc == MOE_OK) rc = ensure_lds_limit(once_q, reinterpret_cast<const void*>(cross_dq_kernel<D>), kLdsQ<D>);
   if (rc == MOE_OK) rc = ensure_lds_limit(once_qfew, reinterpret_cast<const void*>(cross_dq_few_kernel<D>), kLdsFew<D>);
   if (rc == MOE_OK) rc = ensure_lds_limit(once_kv1, reinterpret_cast<const void*>(cross_dkv_kernel<D, 1>), (kLdsKV<D, 1>));
@@ -1163,24 +1342,39 @@ int prepare_kernels() {
   return rc;
 }
 
+// what a forward call has besides the shape; q_rest: in pairs
+struct CrossForward {
+  const bf16_t *q, *q_rest, *kv;
+  const int32_t* src_len;
+  bf16_t *ctx, *ctx_rest;
+  float* lse;
+};
 template <int D>
-int forward(const CrossShape& s, const CrossPlan& plan, const bf16_t* q, const bf16_t* kv, const int32_t* src_len, bf16_t* ctx, float* lse,
-            const CrossParts& parts, hipStream_t st) {
+int forward(const CrossShape& s, const CrossPlan& plan, const CrossForward& f, const CrossParts& parts, hipStream_t st) {
   if (prepare_kernels<D>() != MOE_OK) return MOE_EHIP;
-  const int per = plan.few ? 32 : 128;
+  const bool pair = f.q_rest != nullptr;
+  const int per = (plan.few ? 32 : 128) / (pair ? 2 : 1);
   const long long blocks = s.B * s.kv_heads * ((s.columns() + per - 1) / per) * plan.splits;
   const CrossGeo g(s);
-  const dim3 grid((unsigned)blocks);
-  if (plan.few) hipLaunchKernelGGL((cross_few_kernel<D>), grid, dim3(64 * kFewWaves), kLdsFew<D>, st, g, q, kv, src_len, ctx, lse, parts);
-  else hipLaunchKernelGGL((cross_forward_kernel<D>), grid, dim3(256), kLdsForward<D>, st, g, q, kv, src_len, ctx, lse);
+  const dim3 grid((unsigned)blocks), threads(256);
+  static_assert(64 * kFewWaves == 256, "threads of both kernels");
+  auto run = [&](auto kernel, int lds, auto... last) {
+    hipLaunchKernelGGL(kernel, grid, threads, lds, st, g, f.q, f.q_rest, f.kv, f.src_len, f.ctx, f.ctx_rest, f.lse, last...);
+  };
+  if (plan.few && !pair) run(cross_few_kernel<D, false, true>, kLdsFew<D>, parts);
+  else if (plan.few && f.lse != nullptr) run(cross_few_kernel<D, true, true>, kLdsFew<D>, parts);
+  else if (plan.few) run(cross_few_kernel<D, true, false>, kLdsFew<D>, parts);
+  else if (!pair) run(cross_forward_kernel<D, false, true>, kLdsForward<D>);
+  else if (f.lse != nullptr) run(cross_forward_kernel<D, true, true>, kLdsForwardPairs<D>);
+  else run(cross_forward_kernel<D, true, false>, kLdsForward<D>);
   return check_launch();
 }
 template <typename T>
-int join(const CrossShape& s, const CrossParts& parts, const int32_t* src_len, T* ctx, float* lse, hipStream_t st) {
+int join(const CrossShape& s, const CrossParts& parts, const int32_t* src_len, T* ctx, T* ctx_rest, float* lse, hipStream_t st) {
   const long long columns = s.B * s.kv_heads * s.columns();
   const dim3 grid((unsigned)((columns + 3) / 4)), threads(256);
-  if (s.d == 64) hipLaunchKernelGGL((cross_join_kernel<T, 64>), grid, threads, 0, st, CrossGeo(s), parts, src_len, ctx, lse, columns);
-  else hipLaunchKernelGGL((cross_join_kernel<T, 128>), grid, threads, 0, st, CrossGeo(s), parts, src_len, ctx, lse, columns);
+  if (s.d == 64) hipLaunchKernelGGL((cross_join_kernel<T, 64>), grid, threads, 0, st, CrossGeo(s), parts, src_len, ctx, ctx_rest, lse, columns);
+  else hipLaunchKernelGGL((cross_join_kernel<T, 128>), grid, threads, 0, st, CrossGeo(s), parts, src_len, ctx, ctx_rest, lse, columns);
   return check_launch();
 }
 template <int D>
@@ -1245,22 +1439,27 @@ int prepare_cross_attention() {
 // heads of 16 82 / 13.7 (16); 4 x 64, 1000, 8 heads 26.9 / 14.2 (4); 3 x 700, up to 700, 4 heads 20.4 / 29; of 64: 16 x 1, 2000, 8 heads 28.2 / 16.9 (4);
 // 2 x 300, 2000 34.5 / 23.0 (2); 27 x 834, up to 100 18.9 / 47; fp32, of 64: 5 x 187, up to 411, 8 heads 40.8 / 16.3; 8 x 500, 500 59 / 64; 27 x 834, up to
 // 100 56 / 95.
-CrossPlan cross_plan(int act_dtype, const CrossShape& s) {
+// In pairs, blocks have half the columns.  us of the kernels, 64 / 16 columns in the best number of ranges: heads of 128: 55 x 4 tokens, 131 states, 8 heads 9.3 / 14.3;
+// 47 x 1, 267, 16 26.0 / 34.4; 1 x 2, 23, 3 5.1 / 7.0; 1 x 16, 115, 4 7.3 / 6.2; 5 x 1, 935, 8 23.7 / 13.3 (4); 8 x 12, 2761, 4 63.1 / 17.7 (8); 3 x 4, 5147, 3
+// 108.5 / 14.6 (16); of 64: 4 x 1, 55, 3 4.1 / 4.9; 106 x 1, 633, 2 12.8 / 9.6; 83 x 4, 2954, 2 46.9 / 27.9 (2); 7 x 1, 5269, 8 on 4 77.2 / 15.0 (16).
+static CrossPlan plan_of(int act_dtype, const CrossShape& s, bool pair) {
   constexpr double kUnits = 256;                               // of a whole device: the choice sizes a workspace
   const bool f32 = act_dtype == MOE_F32;
   const double pairs = (double)s.B * s.kv_heads, mb = pairs * s.Lk * 2 * s.d * (f32 ? 4 : 2) / 1e6;
-  const double step128 = f32 ? (s.d == 64 ? 3.5 : 7.0) : (s.d == 64 ? 0.75 : 1.2), step32 = f32 ? step128 : s.d == 64 ? 1.1 : 1.7, ends = f32 ? 1 : 0;
-  const int blocks = (s.Lk + 31) / 32;
+  const double step128 = f32 ? (s.d == 64 ? 3.5 : 7.0) : pair ? (s.d == 64 ? 0.8 : 1.3) : s.d == 64 ? 0.75 : 1.2;
+  const double step32 = f32 ? step128 : pair ? (s.d == 64 ? 1.1 : 1.9) : s.d == 64 ? 1.1 : 1.7, ends = f32 ? 1 : 0;
+  const double base128 = pair ? 5 : 4, base32 = pair ? 5 : 6, join = pair ? 7 : 4, rate = pair ? 8 : 5;         // us, us, us, MB/us
+  const int blocks = (s.Lk + 31) / 32, wide = pair ? 64 : 128, narrow = pair ? 16 : 32;
   auto rounds = [](double n, double at_once) { return ceil(n / at_once); };
   auto longer = [](double a, double b) { return a > b ? a : b; };
   CrossPlan best{false, 1};
-  double least = 4 + longer(step128 * (f32 ? blocks : (blocks + 1) / 2) * rounds(pairs * ((s.columns() + 127) / 128), f32 ? kUnits : 2 * kUnits), mb / 5.0);
+  double least = base128 + longer(step128 * (f32 ? blocks : (blocks + 1) / 2) * rounds(pairs * ((s.columns() + wide - 1) / wide), f32 ? kUnits : 2 * kUnits), mb / rate);
   for (int splits = 1; splits <= 64 && splits <= (blocks + 3) / 4; splits *= 2) {
-    const double items = pairs * ((s.columns() + 31) / 32) * splits, at_once = !f32 && s.d == 64 ? 2 * kUnits : kUnits;
+    const double items = pairs * ((s.columns() + narrow - 1) / narrow) * splits, at_once = !f32 && s.d == 64 ? 2 * kUnits : kUnits;
     if (splits > 1 && items > 4 * at_once) break;
-    const double joined = splits > 1 ? 4 + 0.55 * pairs * s.columns() * splits * (4 * s.d + 8) / 1e6 : 0;
-    const double us = 6 + joined + longer((step32 * ((blocks + 4 * splits - 1) / (4 * splits)) + ends) * rounds(items, at_once),
-                                           mb / 5.0 * (items < kUnits ? kUnits / items : 1.0));
+    const double joined = splits > 1 ? join + 0.55 * pairs * s.columns() * splits * (4 * s.d + 8) / 1e6 : 0;
+    const double us = base32 + joined + longer((step32 * ((blocks + 4 * splits - 1) / (4 * splits)) + ends) * rounds(items, at_once),
+                                           mb / rate * (items < kUnits ? kUnits / items : 1.0));
     if (us < least) {
       least = us;
       best = {true, splits};
@@ -1269,11 +1468,16 @@ CrossPlan cross_plan(int act_dtype, const CrossShape& s) {
   return best;
 }
 
-size_t cross_scratch_bytes(int act_dtype, const CrossShape& s) {
-  const CrossPlan p = cross_plan(act_dtype, s);
+CrossPlan cross_plan(int act_dtype, const CrossShape& s) { return plan_of(act_dtype, s, false); }
+CrossPlan cross_pair_plan(const CrossShape& s) { return plan_of(MOE_BF16, s, true); }
+
+static size_t scratch_of(const CrossShape& s, const CrossPlan& p, bool pair) {
   const size_t columns = (size_t)s.B * s.kv_heads * s.columns();
-  return p.splits > 1 ? align_up(columns * p.splits * sizeof(float2), 256) + columns * p.splits * s.d * sizeof(float) : 0;
+  return p.splits > 1 ? align_up(columns * p.splits * sizeof(float2), 256) + columns * p.splits * (s.d + pair) * sizeof(float) : 0;
 }
+
+size_t cross_scratch_bytes(int act_dtype, const CrossShape& s) { return scratch_of(s, cross_plan(act_dtype, s), false); }
+size_t cross_pair_scratch_bytes(const CrossShape& s) { return scratch_of(s, cross_pair_plan(s), true); }
 
 int cross_dkv_blocks(const CrossShape& s) {
   constexpr double kUnits = 256;                               // of a whole device: the choice sizes a workspace
@@ -1300,22 +1504,33 @@ size_t cross_bwd_scratch_bytes(int act_dtype, const CrossShape& s) {
   return ranges > 1 ? (size_t)ranges * s.B * s.Lk * 2 * s.kv_heads * s.d * sizeof(float) : 0;
 }
 
+static CrossParts parts_of(const CrossShape& s, const CrossPlan& plan, void* scratch) {
+  const size_t columns = (size_t)s.B * s.kv_heads * s.columns();
+  float* const sums = reinterpret_cast<float*>(static_cast<char*>(scratch) + align_up(columns * plan.splits * sizeof(float2), 256));
+  return {plan.splits, static_cast<float2*>(scratch), sums, sums + columns * plan.splits * s.d};
+}
+static int launch_bf16(const CrossShape& s, const CrossPlan& plan, const CrossForward& f, void* scratch, hipStream_t st) {
+  const CrossParts parts = parts_of(s, plan, scratch);
+  const int rc = s.d == 64 ? forward<64>(s, plan, f, parts, st) : forward<128>(s, plan, f, parts, st);
+  return rc != MOE_OK || plan.splits == 1 ? rc : join(s, parts, f.src_len, f.ctx, f.ctx_rest, f.lse, st);
+}
+
 int launch_cross_attention(int act_dtype, const CrossShape& s, const void* q, const void* kv, const int32_t* src_len, void* ctx,
                            float* lse, void* scratch, hipStream_t st) {
   const CrossPlan plan = cross_plan(act_dtype, s);
-  const size_t columns = (size_t)s.B * s.kv_heads * s.columns();
-  const CrossParts parts{plan.splits, static_cast<float2*>(scratch),
-                         reinterpret_cast<float*>(static_cast<char*>(scratch) + align_up(columns * plan.splits * sizeof(float2), 256))};
   if (act_dtype == MOE_F32) {
+    const CrossParts parts = parts_of(s, plan, scratch);
     float* const c = static_cast<float*>(ctx);
     const int rc = launch_cross_attention_f32(s, plan, static_cast<const float*>(q), static_cast<const float*>(kv), src_len, c, lse, parts, st);
-    return rc != MOE_OK || plan.splits == 1 ? rc : join(s, parts, src_len, c, lse, st);
+    return rc != MOE_OK || plan.splits == 1 ? rc : join<float>(s, parts, src_len, c, nullptr, lse, st);
   }
-  auto qb = static_cast<const bf16_t*>(q);
-  auto kb = static_cast<const bf16_t*>(kv);
-  auto c = static_cast<bf16_t*>(ctx);
-  const int rc = s.d == 64 ? forward<64>(s, plan, qb, kb, src_len, c, lse, parts, st) : forward<128>(s, plan, qb, kb, src_len, c, lse, parts, st);
-  return rc != MOE_OK || plan.splits == 1 ? rc : join(s, parts, src_len, c, lse, st);
+  return launch_bf16(s, plan, {static_cast<const bf16_t*>(q), nullptr, static_cast<const bf16_t*>(kv), src_len, static_cast<bf16_t*>(ctx), nullptr, lse}, scratch, st);
+}
+
+int launch_cross_attention_pair(const CrossShape& s, const void* q, const void* q_rest, const void* kv, const int32_t* src_len, void* ctx, void* ctx_rest,
+                                float* lse, void* scratch, hipStream_t st) {
+  return launch_bf16(s, cross_pair_plan(s), {static_cast<const bf16_t*>(q), static_cast<const bf16_t*>(q_rest), static_cast<const bf16_t*>(kv), src_len,
+                     static_cast<bf16_t*>(ctx), static_cast<bf16_t*>(ctx_rest), lse}, scratch, st);
 }
 
 int launch_cross_attention_bwd(int act_dtype, const CrossShape& s, const void* q, const void* kv, const int32_t* src_len,

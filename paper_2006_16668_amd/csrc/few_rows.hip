@@ -7,6 +7,9 @@
 // A's rows of 128 bytes sits at c ^ (row / 2) % 8, which spreads 16 rows over all banks.  (Read as fragments from memory, 16 bytes of 32 rows at a
 // time, A costs as much as B.)  Transposed as in attention_mfma.hip, C^T = B^T A^T: a lane holds columns of one row.  The
 // wavefronts' sums meet in LDS, in order.
+//
+// PAIR: the rows are pairs of bf16, A + A_rest.  A tile has 16 of them, first terms in its rows 0 .. 15 and second ones in 16 .. 31, whose products add up: neither more
+// operands nor more products than a tile of 32 rows.
 #include "attention_tiles.h"
 
 namespace moe {
@@ -15,14 +18,17 @@ namespace {
 constexpr int kWaves = 8, kBytesB = 64 * 64, kBytesA = 32 * 128, kPlace = kBytesB + kBytesA, kAhead = 2;
 constexpr int kLds = kWaves * kAhead * kPlace;
 
-__global__ __launch_bounds__(64 * kWaves, 1) void few_rows_kernel(const bf16_t* __restrict__ A, const bf16_t* __restrict__ B,
-                                                                  bf16_t* __restrict__ C, int R, int N, int K) {
+template <bool PAIR>
+__global__ __launch_bounds__(64 * kWaves, 1) void few_rows_kernel(const bf16_t* __restrict__ A, const bf16_t* __restrict__ A_rest,
+                                                                  const bf16_t* __restrict__ B, bf16_t* __restrict__ C, bf16_t* __restrict__ C_rest,
+                                                                  int R, int N, int K) {
+  constexpr int kRows = PAIR ? 16 : 32;
   extern __shared__ __attribute__((aligned(256))) unsigned char few_lds[];
   const uint32_t lds0 = (uint32_t)(uintptr_t)((lds_ptr)few_lds);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 31, hf = lane >> 5, p16 = lane & 15, b1 = (lane >> 4) & 1;
-  const unsigned item = xcd_contiguous(blockIdx.x, gridDim.x), row_tiles = (R + 31) / 32;
-  const int col0 = (int)(item / row_tiles) * 32, row0 = (int)(item % row_tiles) * 32;
+  const unsigned item = xcd_contiguous(blockIdx.x, gridDim.x), row_tiles = (R + kRows - 1) / kRows;
+  const int col0 = (int)(item / row_tiles) * 32, row0 = (int)(item % row_tiles) * kRows;
   const uint32_t own = lds0 + wave * (kAhead * kPlace);
   const uint32_t tr0 = own + (8 * hf + (p16 >> 2)) * 64 + 32 * b1 + 8 * (p16 & 3);
   const uint32_t a0 = own + kBytesB + r * 128 + ((hf ^ ((r >> 1) & 7)) << 4);
@@ -45,7 +51,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void few_rows_kernel(const bf16_t* 
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
         const int i = 8 * x + lane / 8, k = k0 + 8 * ((lane % 8) ^ ((i >> 1) & 7));
-        copy(own + j * kPlace + kBytesB + x * 1024, A + (size_t)(row0 + i) * K + k, row0 + i < R && k < K);
+        const int row = row0 + i % kRows;
+        copy(own + j * kPlace + kBytesB + x * 1024, (i < kRows ? A : A_rest) + (size_t)row * K + k, row < R && k < K);
       }
     }
     wait_all_copies();
@@ -77,7 +84,16 @@ __global__ __launch_bounds__(64 * kWaves, 1) void few_rows_kernel(const bf16_t* 
     v[0] += *at(w, 2 * wave);
     v[1] += *at(w, 2 * wave + 1);
   }
-  if (row0 + r < R && c < N) *reinterpret_cast<uint32_t*>(C + (size_t)(row0 + r) * N + c) = pack_bf16x2(v[0], v[1]);
+  if constexpr (PAIR) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) v[i] = pair_sum(v[i], __shfl_xor(v[i], 16, 64));
+  }
+  if (r < kRows && row0 + r < R && c < N) {
+    const uint32_t rounded = pack_bf16x2(v[0], v[1]);
+    const size_t to = (size_t)(row0 + r) * N + c;
+    *reinterpret_cast<uint32_t*>(C + to) = rounded;
+    if (C_rest != nullptr) *reinterpret_cast<uint32_t*>(C_rest + to) = bf16_rest_x2(v[0], v[1], rounded);
+  }
 }
 
 // fp32 on v_mfma_f32_16x16x4, tiles of 16 x 16: a tile of 32 x 32 would keep its unit's matrix cores busy for 7 us at K 2048 and leave most units
@@ -131,8 +147,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void few_rows_f32_kernel(const floa
 }  // namespace
 
 int prepare_few_rows() {
-  static LdsLimitOnce once;
-  return ensure_lds_limit(once, reinterpret_cast<const void*>(few_rows_kernel), kLds);
+  static LdsLimitOnce once, once_pair;
+  const int rc = ensure_lds_limit(once, reinterpret_cast<const void*>(few_rows_kernel<false>), kLds);
+  return rc != MOE_OK ? rc : ensure_lds_limit(once_pair, reinterpret_cast<const void*>(few_rows_kernel<true>), kLds);
 }
 
 // bf16 blocks fill the device once at most, fp32 blocks, of which several share a unit, three times.  us, gemm_f32.hip / this, fp32: 1024, 2048, 1 16.6 / 4.3;
@@ -145,9 +162,8 @@ bool few_rows_ok(int act_dtype, long long rows, int N) {
 }
 
 int launch_few_rows(int act_dtype, bool b_kc, const void* A, const void* B, void* C, int R, int N, int K, hipStream_t st) {
-  const int side = act_dtype == MOE_F32 ? 16 : 32;
-  const dim3 grid((unsigned)((N + side - 1) / side * ((R + side - 1) / side))), threads(64 * kWaves);
   if (act_dtype == MOE_F32) {
+    const dim3 grid((unsigned)((N + 15) / 16 * ((R + 15) / 16))), threads(64 * kWaves);
     auto a = static_cast<const float*>(A);
     auto b = static_cast<const float*>(B);
     auto c = static_cast<float*>(C);
@@ -155,10 +171,22 @@ int launch_few_rows(int act_dtype, bool b_kc, const void* A, const void* B, void
     else hipLaunchKernelGGL((few_rows_f32_kernel<false>), grid, threads, 0, st, a, b, c, R, N, K);
     return check_launch();
   }
-  if (b_kc) return MOE_EUNSUPPORTED;
+  return b_kc ? MOE_EUNSUPPORTED : launch_few_rows_pair(A, nullptr, B, C, nullptr, R, N, K, st);
+}
+
+bool few_rows_pair_ok(long long rows, int N) { return rows <= 16 * 256 && (rows + 15) / 16 * ((N + 31) / 32) <= 256; }
+
+int launch_few_rows_pair(const void* A, const void* A_rest, const void* B, void* C, void* C_rest, int R, int N, int K, hipStream_t st) {
   if (prepare_few_rows() != MOE_OK) return MOE_EHIP;
-  hipLaunchKernelGGL(few_rows_kernel, grid, threads, kLds, st, static_cast<const bf16_t*>(A), static_cast<const bf16_t*>(B),
-                     static_cast<bf16_t*>(C), R, N, K);
+  const int rows = A_rest != nullptr ? 16 : 32;
+  const dim3 grid((unsigned)((N + 31) / 32 * ((R + rows - 1) / rows))), threads(64 * kWaves);
+  auto a = static_cast<const bf16_t*>(A);
+  auto r = static_cast<const bf16_t*>(A_rest);
+  auto b = static_cast<const bf16_t*>(B);
+  auto c = static_cast<bf16_t*>(C);
+  auto e = static_cast<bf16_t*>(C_rest);
+  if (r != nullptr) hipLaunchKernelGGL((few_rows_kernel<true>), grid, threads, kLds, st, a, r, b, c, e, R, N, K);
+  else hipLaunchKernelGGL((few_rows_kernel<false>), grid, threads, kLds, st, a, r, b, c, e, R, N, K);
   return check_launch();
 }
 
