@@ -533,7 +533,7 @@ int moe_cross_keys(const moe_config* cfg, const moe_cross_dims* dims, const void
 int moe_cross_attention(const moe_config* cfg, const moe_cross_dims* dims, const void* u, const void* kv, const int32_t* src_len,
                         const void* wq, const void* wo, void* out, void* ws, size_t ws_bytes, void* stream);
 
-/* The same result; ws (>= moe_cross_train_workspace_bytes) keeps q, ctx (bf16: rounded) and the row statistics for the backward pass. */
+/* The same result; ws (>= moe_cross_train_workspace_bytes) keeps q, ctx and the row statistics for the backward pass. */
 int moe_cross_attention_train(const moe_config* cfg, const moe_cross_dims* dims, const void* u, const void* kv,
                               const int32_t* src_len, const void* wq, const void* wo, void* out, void* ws, size_t ws_bytes,
                               void* stream);
@@ -541,8 +541,8 @@ int moe_cross_attention_train(const moe_config* cfg, const moe_cross_dims* dims,
 /* Gradients of L = sum dout out, through kv to mem and wkv.  in: as given to moe_cross_keys and moe_cross_attention_train, kv as the
  * first and fwd_ws as the second left it (read only); dout [G,S,M].  out, every element written: du [G,S,M], dmem [B,Lk,M] (zeros
  * for states that do not hold), dwq, dwkv, dwo.  They must not overlap the inputs.  ws >= moe_cross_backward_workspace_bytes,
- * 256-byte aligned.  bf16: dctx, the probabilities, their gradients, dq, dK and dV are rounded once each.  No atomics: results are
- * reproducible bit for bit. */
+ * 256-byte aligned.  bf16: dctx, the probabilities, their gradients, dq, dK and dV are rounded once each; calls of few tokens (as above) carry the first
+ * three as pairs of bf16.  No atomics: results are reproducible bit for bit. */
 int moe_cross_attention_backward(const moe_config* cfg, const moe_cross_dims* dims, const void* u, const void* mem, const void* kv,
                                  const int32_t* src_len, const void* wq, const void* wkv, const void* wo, const void* dout,
                                  const void* fwd_ws, size_t fwd_ws_bytes, void* du, void* dmem, void* dwq, void* dwkv, void* dwo,

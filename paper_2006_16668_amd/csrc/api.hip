@@ -379,13 +379,14 @@ int check_cross(const moe_config* cfg, const moe_cross_dims* d) {
 }
 moe::CrossShape cross_shape(const moe_cross_dims& d) { return {d.B, d.Lq, d.Lk, d.heads, d.kv_heads, d.d}; }
 
-// Calls of few tokens carry q and ctx as pairs of bf16 through the forward pass (and P): their roundings are as large as that of the result, and where products
-// are of few rows and the states' bytes are what counts, pairs cost next to nothing.
+// Calls of few tokens carry q and ctx, and in the backward pass dctx, as pairs of bf16 (and P and dS): what q or dctx loses moves all of a head's scores or all of
+// their gradients at once, so that a few tokens' results are off by several roundings; where products are of few rows and the states' bytes are what counts,
+// pairs cost next to nothing.
 bool cross_pairs(const moe_config& c, const moe_cross_dims& d) {
   const long long N = (long long)c.G * c.S;
   return c.act_dtype == MOE_BF16 && moe::few_rows_ok(MOE_BF16, N, d.heads * d.d) && moe::few_rows_pair_ok(N, c.M);
 }
-// train: with the row statistics.  q, ctx and lse come first, so the backward pass, which has no second terms, finds them.
+// train: with the row statistics.  The scratch comes last, so the backward pass finds what it reads.
 struct CrossWs { size_t q, ctx, lse, q_rest, ctx_rest, scratch, total; };
 CrossWs carve_cross(const moe_config& c, const moe_cross_dims& d, bool train) {
   const size_t elt = c.act_dtype == MOE_F32 ? 4 : 2, N = (size_t)c.G * c.S, A = (size_t)d.heads * d.d;
@@ -402,13 +403,14 @@ CrossWs carve_cross(const moe_config& c, const moe_cross_dims& d, bool train) {
   w.total = off;
   return w;
 }
-struct CrossBwdWs { size_t dctx, dq, dkv, mem, dvec, wpart, total; };
+struct CrossBwdWs { size_t dctx, dctx_rest, dq, dkv, mem, dvec, wpart, total; };
 CrossBwdWs carve_cross_bwd(const moe_config& c, const moe_cross_dims& d) {
   const size_t elt = c.act_dtype == MOE_F32 ? 4 : 2, N = (size_t)c.G * c.S, A = (size_t)d.heads * d.d, rows = (size_t)d.B * d.Lk;
   CrossBwdWs w{};
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off += align_up(bytes, 256); return o; };
   w.dctx = take(N * A * elt);
+  w.dctx_rest = take(cross_pairs(c, d) ? N * A * elt : 0);
   w.dq = take(N * A * elt);
   w.dkv = take(rows * 2 * d.kv_heads * d.d * elt);
   w.mem = take(rows * c.M * elt);
@@ -417,7 +419,7 @@ CrossBwdWs carve_cross_bwd(const moe_config& c, const moe_cross_dims& d) {
   const size_t parts[] = {moe::dense_wgrad_partial_bytes(c.act_dtype, (long long)N, (int)A, c.M),
                           moe::dense_wgrad_partial_bytes(c.act_dtype, (long long)N, c.M, (int)A),
                           moe::dense_wgrad_partial_bytes(c.act_dtype, (long long)rows, c.M, Akv2)};
-  size_t most = moe::cross_bwd_scratch_bytes(c.act_dtype, cross_shape(d));
+  size_t most = moe::cross_bwd_scratch_bytes(c.act_dtype, cross_shape(d), cross_pairs(c, d));
   for (size_t p : parts) most = p > most ? p : most;
   w.wpart = take(most);
   w.total = off;
@@ -428,19 +430,22 @@ int cross_product(const moe_config& c, long long rows, int K, int N, const void*
   if (moe::few_rows_ok(c.act_dtype, rows, N)) return moe::launch_few_rows(c.act_dtype, false, A, B, C, (int)rows, N, K, st);
   return dense_gemm(c, rows, K, N, false, A, B, C, st);
 }
+// dB [K,N] = A^T . dC of few rows, as the weight gradient of one expert
+int weight_gradient(const moe_config& c, int rows, int K, int N, const void* A, const void* dC, void* dB, hipStream_t st) {
+  moe_config g = c;
+  g.E = g.G = 1;
+  g.S = g.C = rows;
+  g.M = K;
+  g.H = N;
+  return moe::launch_expert_wgrad1(g, A, dC, dB, nullptr, st);
+}
 // its gradients: dA = dC . B^T, dB = A^T . dC
 int cross_gradients(const moe_config& c, long long rows, int K, int N, const void* A, const void* dC, const void* B, void* dA, void* dB,
                     float* wpart, hipStream_t st) {
   if (c.act_dtype != MOE_F32 || !moe::few_rows_ok(c.act_dtype, rows, K))
     return moe::launch_dense_grads(c, rows, K, N, A, dC, B, nullptr, dA, dB, wpart, st);
   const int rc = moe::launch_few_rows(c.act_dtype, true, dC, B, dA, (int)rows, K, N, st);
-  if (rc != MOE_OK) return rc;
-  moe_config g = c;                                            // dB as the weight gradient of one expert
-  g.E = g.G = 1;
-  g.S = g.C = (int)rows;
-  g.M = K;
-  g.H = N;
-  return moe::launch_expert_wgrad1(g, A, dC, dB, nullptr, st);
+  return rc != MOE_OK ? rc : weight_gradient(c, (int)rows, K, N, A, dC, dB, st);
 }
 // what: 0 inference, 1 training, 2 backward
 int cross_bytes(const moe_config* cfg, const moe_cross_dims* dims, int what, size_t* bytes) {
@@ -1196,12 +1201,20 @@ int moe_cross_attention_backward(const moe_config* cfg, const moe_cross_dims* di
   const long long N = (long long)cfg->G * cfg->S, rows = (long long)dims->B * dims->Lk;
   const int A = dims->heads * dims->d, Akv2 = 2 * dims->kv_heads * dims->d;
   float* wpart = reinterpret_cast<float*>(base + w.wpart);
+  const float* const lse = reinterpret_cast<const float*>(fwd + f.lse);
+  float* const dvec = reinterpret_cast<float*>(base + w.dvec);
   // out = ctx . wo
-  rc = cross_gradients(*cfg, N, A, cfg->M, fwd + f.ctx, dout, wo, base + w.dctx, dwo, wpart, st);
-  if (rc != MOE_OK) return rc;
-  rc = moe::launch_cross_attention_bwd(cfg->act_dtype, cross_shape(*dims), fwd + f.q, kv, src_len, fwd + f.ctx, base + w.dctx,
-                                       reinterpret_cast<const float*>(fwd + f.lse), base + w.dq, base + w.dkv,
-                                       reinterpret_cast<float*>(base + w.dvec), wpart, st);
+  if (cross_pairs(*cfg, *dims)) {
+    if ((rc = moe::launch_few_rows_transposed(dout, wo, base + w.dctx, base + w.dctx_rest, (int)N, A, cfg->M, st)) != MOE_OK) return rc;
+    if ((rc = weight_gradient(*cfg, (int)N, A, cfg->M, fwd + f.ctx, dout, dwo, st)) != MOE_OK) return rc;
+    rc = moe::launch_cross_attention_pair_bwd(cross_shape(*dims), {fwd + f.q, fwd + f.q_rest}, kv, src_len, {fwd + f.ctx, fwd + f.ctx_rest},
+                                              {base + w.dctx, base + w.dctx_rest}, lse, base + w.dq, base + w.dkv, dvec, wpart, st);
+  } else {
+    rc = cross_gradients(*cfg, N, A, cfg->M, fwd + f.ctx, dout, wo, base + w.dctx, dwo, wpart, st);
+    if (rc != MOE_OK) return rc;
+    rc = moe::launch_cross_attention_bwd(cfg->act_dtype, cross_shape(*dims), fwd + f.q, kv, src_len, fwd + f.ctx, base + w.dctx, lse, base + w.dq, base + w.dkv,
+                                         dvec, wpart, st);
+  }
   if (rc != MOE_OK) return rc;
   // q = u . wq
   rc = cross_gradients(*cfg, N, cfg->M, A, u, base + w.dq, wq, du, dwq, wpart, st);

@@ -439,14 +439,18 @@ struct CrossShape {
 size_t cross_scratch_bytes(int act_dtype, const CrossShape& s);
 int launch_cross_attention(int act_dtype, const CrossShape& s, const void* q, const void* kv, const int32_t* src_len, void* ctx,
                            float* lse, void* scratch, hipStream_t st);
-// bf16, few tokens: q and ctx in pairs (q + q_rest, ctx + ctx_rest), and so the probabilities; lse is of q alone; scratch: cross_pair_scratch_bytes()
+// bf16, few tokens: q and ctx in pairs (q + q_rest, ctx + ctx_rest), and so the probabilities; scratch: cross_pair_scratch_bytes()
 size_t cross_pair_scratch_bytes(const CrossShape& s);
 int launch_cross_attention_pair(const CrossShape& s, const void* q, const void* q_rest, const void* kv, const int32_t* src_len, void* ctx, void* ctx_rest,
                                 float* lse, void* scratch, hipStream_t st);
 // dvec: [B kv_heads columns] of scratch; dkv: zeros in the rows of states that do not hold; sums: cross_bwd_scratch_bytes()
-size_t cross_bwd_scratch_bytes(int act_dtype, const CrossShape& s);
+size_t cross_bwd_scratch_bytes(int act_dtype, const CrossShape& s, bool pair);
 int launch_cross_attention_bwd(int act_dtype, const CrossShape& s, const void* q, const void* kv, const int32_t* src_len,
                                const void* ctx, const void* dctx, const float* lse, void* dq, void* dkv, float* dvec, float* sums, hipStream_t st);
+// bf16, few tokens: q, ctx and dctx in pairs, and so P and dS
+struct CrossPair { const void *first, *rest; };
+int launch_cross_attention_pair_bwd(const CrossShape& s, const CrossPair& q, const void* kv, const int32_t* src_len, const CrossPair& ctx, const CrossPair& dctx,
+                                    const float* lse, void* dq, void* dkv, float* dvec, float* sums, hipStream_t st);
 // out[i] = sum of partial[range][i] in order, rounded to bf16; elems a multiple of 8 (encoder_bwd.hip)
 int launch_add_ranges(const float* partial, int ranges, long long elems, void* out, hipStream_t st);
 // out = mem with zeros in those rows
@@ -458,6 +462,8 @@ int launch_few_rows(int act_dtype, bool b_kc, const void* A, const void* B, void
 // bf16: A + A_rest where A_rest is given (few_rows_pair_ok), and what C leaves to C_rest where that is
 bool few_rows_pair_ok(long long rows, int N);
 int launch_few_rows_pair(const void* A, const void* A_rest, const void* B, void* C, void* C_rest, int R, int N, int K, hipStream_t st);
+// C + C_rest = A . B^T, B [N,K]
+int launch_few_rows_transposed(const void* A, const void* B, void* C, void* C_rest, int R, int N, int K, hipStream_t st);
 
 // Losses on token losses (token_loss.hip)
 int launch_preference(const moe_preference_dims& d, long long N, const float* nll, const float* ref, const int32_t* target,

@@ -33,7 +33,6 @@ struct CrossParts {
   int splits;
   float2* stats;             // [B kv_heads columns, splits]
   float* sums;               // [B kv_heads columns, splits, d]
-  float* firsts;             // [B kv_heads columns, splits]: in pairs with statistics, the sum of exponentials of the first terms' scores
 };
 // few: blocks of 32 columns whose wavefronts take the states' blocks in turn, in `splits` ranges; else blocks of 128 columns
 struct CrossPlan { bool few; int splits; };
@@ -46,6 +45,7 @@ CrossPlan cross_pair_plan(const CrossShape& s);            // q and ctx in pairs
 // 8 heads of 64 14.5 / 15.9 (4).  Left to one range although more are a little faster: 3 x 700, up to 700, 4 heads of 128 28.2 / 24.8 (3); 2 x 1000, 1000, 8
 // heads of 128 39.3 / 37.2 (2).
 int cross_dkv_blocks(const CrossShape& s);
+int cross_pair_dkv_blocks(const CrossShape& s);
 
 // fp32 (cross_attention_f32.hip)
 int launch_cross_attention_f32(const CrossShape& s, const CrossPlan& plan, const float* q, const float* kv, const int32_t* src_len,

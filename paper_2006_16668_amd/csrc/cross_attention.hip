@@ -12,7 +12,7 @@
 //   lse       is kept in units of log2 (fp32: natural): the exponentials of the backward pass are powers of two.
 //   P, dS     are rounded to bf16 in front of the second products, as the self-attention of whole blocks does: three terms of them
 //             (attention_mfma.hip, RAGGED) triple those products, and q, ctx and the results are rounded as much anyway.
-//   pairs     where tokens are few (generation) the forward pass carries q, P and ctx as pairs of bf16, 16 bits.  A wavefront's tile then has 16
+//   pairs     where tokens are few (generation) q, P and ctx, backward dctx and dS, are pairs of bf16, 16 bits.  A wavefront's tile then has 16
 //             columns, first terms in its columns 0 .. 15 and second ones in 16 .. 31: scores are the sums of both halves, P goes into the products as
 //             both, ctx is the sum of both again.  That takes no more products or reads than a tile that few tokens do not fill, and as the lanes of
 //             a pair share the exponentials, no more instructions.
@@ -126,11 +126,10 @@ __device__ __forceinline__ void clear_columns(bf16_t* base, const CrossCols& c, 
 }
 
 // Of a pair of columns c and c + 16, which lanes c and c + 16 hold (one row of 16 lanes and the next; a swap exchanges the odd rows of its first operand with
-// the even ones of its second): the sums over the pair of two values, a's in the first lane and b's in the second, and the first terms of these sums.
-struct PairFold { float sum, first; };
-__device__ __forceinline__ PairFold pair_fold(float a, float b) {
+// the even ones of its second): the sums over the pair of two values, a's in the first lane and b's in the second.
+__device__ __forceinline__ float pair_fold(float a, float b) {
   const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
-  return {pair_sum(__uint_as_float(x[0]), __uint_as_float(x[1])), __uint_as_float(x[0])};
+  return pair_sum(__uint_as_float(x[0]), __uint_as_float(x[1]));
 }
 // over the four lanes of a pair of columns
 __device__ __forceinline__ float pair_max(float v) {
@@ -156,14 +155,12 @@ __device__ __forceinline__ PairTerms pair_terms(float x, float y) {
 }
 
 // ---------------------------------------------------------------- forward
-// PAIR: q + q_rest, ctx + ctx_rest.  STATS: with row statistics.  The backward pass has a q of one term, of whose scores the statistics of a pair are: its
-// probabilities add up to 1.
-template <int D, bool PAIR, bool STATS>
+// PAIR: q + q_rest, ctx + ctx_rest.
+template <int D, bool PAIR>
 __global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossGeo g, const bf16_t* __restrict__ q, const bf16_t* __restrict__ q_rest,
                                                                const bf16_t* __restrict__ kv, const int32_t* __restrict__ src_len,
                                                                bf16_t* __restrict__ ctx, bf16_t* __restrict__ ctx_rest, float* __restrict__ lse) {
   using GM = AttGeom<D>;
-  static_assert(PAIR || STATS, "a single term's statistics take nothing: written where there is an lse");
   constexpr int CT = 1, KS = D / 16, DT = D / 32, kOwnBlock = 32 * CT * GM::kRow, kTile = PAIR ? 16 : 32;
   constexpr int kV = 2 * GM::kBlock;                           // LDS: two K blocks, two V blocks
   extern __shared__ __attribute__((aligned(256))) unsigned char att_lds[];
@@ -178,7 +175,7 @@ __global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossGeo g, const
   if (n == 0) {
     clear_columns<D, 4 * kTile>(ctx + head, cols, w.block0);
     if constexpr (PAIR) clear_columns<D, 4 * kTile>(ctx_rest + head, cols, w.block0);
-    if (STATS && lse != nullptr && threadIdx.x < 4 * kTile && w.block0 + (int)threadIdx.x < cols.count) lse[(size_t)w.bk * cols.count + w.block0 + threadIdx.x] = 0.f;
+    if (lse != nullptr && threadIdx.x < 4 * kTile && w.block0 + (int)threadIdx.x < cols.count) lse[(size_t)w.bk * cols.count + w.block0 + threadIdx.x] = 0.f;
     return;
   }
   const int Akv = g.kv_heads * D;
@@ -238,11 +235,9 @@ __global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossGeo g, const
     for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
   // running maximum (in log2 units) and sum; the maximum starts finite, so that a block of states whose scores
   // are all -inf adds nothing
-  float m_run = -FLT_MAX, l_run = 0.f, l_first = 0.f, m_new;
-  // scores of block kb [32-state tile], and the maximum with them; PAIR: [0] only, of the tile 0 in the first lane of a pair and of 1 in the second.  Their first
-  // terms wait in LDS (16 registers more spill at d 128: 64 x 2 tokens, 1000 states, 16 heads 100 us, not 68).
+  float m_run = -FLT_MAX, l_run = 0.f, m_new;
+  // scores of block kb [32-state tile], and the maximum with them; PAIR: [0] only, of the tile 0 in the first lane of a pair and of 1 in the second
   f32x16_t sacc[2];
-  auto first_terms = [&](int i4) __attribute__((always_inline)) { return (lds_f4_ptr)(uintptr_t)(lds0 + 2 * kV + (4 * wave + i4) * 1024 + lane * 16); };
   auto mask_end = [&](f32x16_t (&acc)[2], int kb) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < (PAIR ? 1 : 2); ++t)
@@ -259,14 +254,8 @@ __global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossGeo g, const
     return mx;
   };
   auto fold4 = [&](f32x16_t (&acc)[2], int i4) __attribute__((always_inline)) {
-    f32x4_t first;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const PairFold f = pair_fold(acc[0][4 * i4 + i], acc[1][4 * i4 + i]);
-      acc[0][4 * i4 + i] = f.sum;
-      first[i] = f.first;
-    }
-    if constexpr (STATS) *first_terms(i4) = first;
+    for (int i = 4 * i4; i < 4 * i4 + 4; ++i) acc[0][i] = pair_fold(acc[0][i], acc[1][i]);
   };
   auto new_max = [&](float mx) __attribute__((always_inline)) {
     mx = PAIR ? pair_max(mx) : fmaxf(mx, __shfl_xor(mx, 32, 64));
@@ -287,7 +276,6 @@ __global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossGeo g, const
   auto step = [&](int kb, auto last) __attribute__((always_inline)) {
     constexpr bool LAST = decltype(last)::value;
     constexpr int FIRST = LAST ? 2 * KS : 0;                   // (units 0 .. 2 KS - 1 are those scores)
-    constexpr int kAhead = PAIR && STATS && D == 128 ? 3 : 4;  // (registers)
     wait_all_copies();                                         // K block kb + 1 and V block kb are there;
     __syncthreads();                                           // K block kb and V block kb - 1 are read, their places free
     const uint32_t kst = ((kb + 1) & 1) * GM::kBlock, vst = kV + (kb & 1) * GM::kBlock;
@@ -295,7 +283,6 @@ __global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossGeo g, const
     if (__builtin_amdgcn_ballot_w64(m_new != m_run) != 0) {
       const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);   // 0 on the first block
       l_run *= alpha;
-      if constexpr (PAIR && STATS) l_first *= alpha;
 #pragma unroll
       for (int t = 0; t < DT; ++t)
 #pragma unroll
@@ -312,17 +299,12 @@ __global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossGeo g, const
       pf[i / 4][i % 4] = p.a;
       pf[(2 + i / 4) % PF][i % 4] = p.b;
     };
-    f32x4_t first;
     auto exponentials = [&](int t, int from, int to) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = from; i < to; ++i) {
         const float v = __builtin_amdgcn_exp2f(fmaf(sacc[t][i], sl2, -m_run));
         sacc[t][i] = v;
         psum += v;
-        if constexpr (PAIR && STATS) {
-          if (i % 4 == 0) first = *first_terms(i / 4);
-          l_first += v == 0.f ? 0.f : __builtin_amdgcn_exp2f(fmaf(first[i % 4], sl2, -m_run));      // (of a state past the end: v is 0)
-        }
       }
     };
     if constexpr (LAST) {
@@ -337,7 +319,7 @@ __global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossGeo g, const
     }
     // units 0 .. 2 KS - 1: scores of block kb + 1, under them the first tile's exponentials; then 4 DT units of O^T, under
     // them the second tile's and the next block's maximum
-    run_units<FIRST, 2 * KS + 4 * DT, kAhead>(
+    run_units<FIRST, 2 * KS + 4 * DT, 4>(
         [&](auto) __attribute__((always_inline)) { return std::integral_constant<int, 1>{}; },
         [&](auto U) __attribute__((always_inline)) {
           constexpr int u = decltype(U)::value, v = u - 2 * KS;
@@ -398,11 +380,9 @@ __global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossGeo g, const
   __syncthreads();                                             // the other wavefronts have read the last blocks
   const int c = w.col0 + r % kTile;
   // row statistic for the backward pass: log2 sum_k exp(score)
-  if constexpr (STATS) {
-    const float l = PAIR ? pair_total(l_first) : l_run;
-    if (lse != nullptr && hf == 0 && !second && c < cols.count) lse[(size_t)w.bk * cols.count + c] = m_run + log2f(l);
-  }
-  const float inv = 1.0f / (PAIR ? pair_total(l_run) : l_run);
+  const float l = PAIR ? pair_total(l_run) : l_run;
+  if (lse != nullptr && hf == 0 && !second && c < cols.count) lse[(size_t)w.bk * cols.count + c] = m_run + log2f(l);
+  const float inv = 1.0f / l;
   auto put = [&](int row, int chunk, const u32x4_t& v) __attribute__((always_inline)) {
     const int col = w.col0 + row % kTile;
     if (col < cols.count) *reinterpret_cast<u32x4_t*>((row < kTile ? ctx : ctx_rest) + head + cols.offset<D>(col) + 8 * chunk) = v;
@@ -413,7 +393,7 @@ __global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossGeo g, const
     for (int t = 0; t < DT; t += 2)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const PairTerms p = pair_terms<false>(pair_fold(o[t][2 * i], o[t + 1][2 * i]).sum * inv, pair_fold(o[t][2 * i + 1], o[t + 1][2 * i + 1]).sum * inv);
+        const PairTerms p = pair_terms<false>(pair_fold(o[t][2 * i], o[t + 1][2 * i]) * inv, pair_fold(o[t][2 * i + 1], o[t + 1][2 * i + 1]) * inv);
         terms[t][i] = p.a;
         terms[t + 1][i] = p.b;
       }
@@ -446,7 +426,7 @@ __device__ __forceinline__ void stage_few(uint32_t lds, const bf16_t* keys, int 
 // way while the other is used: no barrier, 64 KB (d 128) on their way to a compute unit.  Memory bounds it, so the products are
 // not what counts: P keeps its 24 bits as three terms.
 constexpr int kFewWaves = 4;
-template <int D, bool PAIR, bool STATS>
+template <int D, bool PAIR>
 __global__ __launch_bounds__(64 * kFewWaves, 1) void cross_few_kernel(CrossGeo g, const bf16_t* __restrict__ q, const bf16_t* __restrict__ q_rest,
                                                            const bf16_t* __restrict__ kv, const int32_t* __restrict__ src_len,
                                                            bf16_t* __restrict__ ctx, bf16_t* __restrict__ ctx_rest, float* __restrict__ lse,
@@ -491,7 +471,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void cross_few_kernel(CrossGeo g
   f32x16_t o[DT];
 #pragma unroll
   for (int t = 0; t < DT; ++t) o[t] = f32x16_t{};
-  float m_run = -FLT_MAX, l_run = 0.f, l_first = 0.f;          // (finite: a block whose scores are all -inf adds nothing)
+  float m_run = -FLT_MAX, l_run = 0.f;                         // (finite: a block whose scores are all -inf adds nothing)
   if (from < to) start(from, 0);
   int p = 0;
   for (int kb = from; kb < to; kb += W, p ^= 1) {
@@ -509,19 +489,12 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void cross_few_kernel(CrossGeo g
     constexpr int VALUES = PAIR ? 8 : 16;
     if constexpr (PAIR) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const PairFold f = pair_fold(s[i], s[i + 8]);
-        s[i] = f.sum;
-        if constexpr (STATS) s[i + 8] = f.first;
-      }
+      for (int i = 0; i < 8; ++i) s[i] = pair_fold(s[i], s[i + 8]);
     }
     float mx = -INFINITY, psum = 0.f;
 #pragma unroll
     for (int i = 0; i < VALUES; ++i) {
-      if (32 * kb + 16 * second + 8 * (i >> 2) + 4 * hf + (i & 3) >= n) {
-        s[i] = -INFINITY;
-        if constexpr (PAIR && STATS) s[i + 8] = -INFINITY;
-      }
+      if (32 * kb + 16 * second + 8 * (i >> 2) + 4 * hf + (i & 3) >= n) s[i] = -INFINITY;
       mx = fmaxf(mx, s[i]);
     }
     mx = PAIR ? pair_max(mx) : fmaxf(mx, __shfl_xor(mx, 32, 64));
@@ -529,7 +502,6 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void cross_few_kernel(CrossGeo g
     if (__builtin_amdgcn_ballot_w64(m_new != m_run) != 0) {
       const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
       l_run *= alpha;
-      if constexpr (PAIR && STATS) l_first *= alpha;
 #pragma unroll
       for (int t = 0; t < DT; ++t)
 #pragma unroll
@@ -540,7 +512,6 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void cross_few_kernel(CrossGeo g
     for (int i = 0; i < VALUES; ++i) {
       s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], sl2, -m_run));
       psum += s[i];
-      if constexpr (PAIR && STATS) l_first += __builtin_amdgcn_exp2f(fmaf(s[i + 8], sl2, -m_run));
     }
     l_run += PAIR ? pair_total(psum) : psum + __shfl_xor(psum, 32, 64);
     u32x4_t both[2];
@@ -574,18 +545,12 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void cross_few_kernel(CrossGeo g
   auto at = [&](uint32_t byte) __attribute__((always_inline)) { return (lds_f_ptr)(uintptr_t)(lds0 + byte); };
   *at(kStats + (wave * 64 + lane) * 4) = m_run;
   *at(kStats + 256 * W + (wave * 64 + lane) * 4) = l_run;
-  if constexpr (PAIR && STATS) *at(kStats + 512 * W + (wave * 64 + lane) * 4) = pair_total(l_first);
   __syncthreads();
   float m = m_run, l = 0.f;
-  l_first = 0.f;
 #pragma unroll
   for (int x = 0; x < W; ++x) m = fmaxf(m, *at(kStats + (x * 64 + lane) * 4));
 #pragma unroll
   for (int x = 0; x < W; ++x) l += *at(kStats + 256 * W + (x * 64 + lane) * 4) * __builtin_amdgcn_exp2f(*at(kStats + (x * 64 + lane) * 4) - m);
-  if constexpr (PAIR && STATS) {
-#pragma unroll
-    for (int x = 0; x < W; ++x) l_first += *at(kStats + 512 * W + (x * 64 + lane) * 4) * __builtin_amdgcn_exp2f(*at(kStats + (x * 64 + lane) * 4) - m);
-  }
   const float alpha = __builtin_amdgcn_exp2f(m_run - m);       // (a wavefront without a block: sums of 0)
 #pragma unroll
   for (int t = 0; t < DT; ++t)
@@ -595,12 +560,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void cross_few_kernel(CrossGeo g
   if (c >= cols.count) return;
   const size_t column = ((size_t)b * g.kv_heads + k) * cols.count + c;
   if (wave == 0 && hf == 0 && !second) {
-    if (parts.splits > 1) {
-      parts.stats[column * parts.splits + split] = float2{m, l};
-      if constexpr (PAIR && STATS) parts.firsts[column * parts.splits + split] = l_first;
-    } else if (STATS && lse != nullptr) {
-      lse[column] = n == 0 ? 0.f : m + log2f(PAIR ? l_first : l);
-    }
+    if (parts.splits > 1) parts.stats[column * parts.splits + split] = float2{m, l};
+    else if (lse != nullptr) lse[column] = n == 0 ? 0.f : m + log2f(l);
   }
   const float inv = n == 0 ? 0.f : 1.0f / l;
 #pragma unroll
@@ -611,7 +572,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void cross_few_kernel(CrossGeo g
       v[i] = 0.f;
 #pragma unroll
       for (int x = 0; x < W; ++x) v[i] += *at(((x * DT + dt) * 16 + i) * 256 + lane * 4);
-      if constexpr (PAIR) v[i] = pair_fold(v[i], v[i]).sum;
+      if constexpr (PAIR) v[i] = pair_fold(v[i], v[i]);
     }
     if (parts.splits > 1) {
       if (second) continue;
@@ -652,8 +613,6 @@ __global__ __launch_bounds__(256) void cross_join_kernel(CrossGeo g, CrossParts 
   const float m = wave_max(st.x);
   const float f = F32 ? expf(st.x - m) : __builtin_amdgcn_exp2f(st.x - m);
   const float l = wave_sum(st.y * f);
-  float l_stat = l;                                            // (of a pair's first terms: what the forward pass's kernel left)
-  if (!F32 && ctx_rest != nullptr && lse != nullptr) l_stat = wave_sum((lane < parts.splits ? parts.firsts[column * parts.splits + lane] : 0.f) * f);
   float v[D / 64] = {};
   const float* const sums = parts.sums + column * parts.splits * D + lane * (D / 64);
   for (int s = 0; s < parts.splits; s += 8) {                  // eight on their way at a time
@@ -668,7 +627,7 @@ __global__ __launch_bounds__(256) void cross_join_kernel(CrossGeo g, CrossParts 
       for (int i = 0; i < D / 64; ++i) v[i] = fmaf(x[j][i], __shfl(f, s + j, 64), v[i]);
   }
   const bool none = held_states(src_len, b, g.Lk) == 0;
-  if (lse != nullptr && lane == 0) lse[column] = none ? 0.f : F32 ? m + logf(l_stat) : m + log2f(l_stat);
+  if (lse != nullptr && lane == 0) lse[column] = none ? 0.f : F32 ? m + logf(l) : m + log2f(l);
   const float inv = none ? 0.f : 1.0f / l;
   const size_t to = cols.base(b, k, D) + cols.offset<D>(c) + lane * (D / 64);
 #pragma unroll
@@ -684,51 +643,80 @@ __global__ __launch_bounds__(256) void cross_join_kernel(CrossGeo g, CrossParts 
 // rowsum(dO * ctx), is more than half (two states: dq off by 0.0053 in norm, 0.0038 without it); of one it is 0, as it is here to the last
 // bit: p is exactly 1.  What a source holds decides, not what its batch is padded to, so every kernel of dq has this form of its own and padding
 // changes no bits.  K and V are two blocks of 32 rows each, zeros from n on: K's first at k0, V's at v0, the second ones `step` behind.
-template <int D>
+// PAIR: of columns in pairs; dq is rounded by the caller, the sums of both terms in both lanes.
+template <int D, bool PAIR = false>
 __device__ __forceinline__ void few_states_dq(f32x16_t (&dq)[D / 32], float& dd, const AttReads<D>& rd, uint32_t k0, uint32_t v0, uint32_t step,
-                                              const u32x4_t (&qf)[D / 16], const u32x4_t (&dof)[D / 16], int n, int hf) {
-  constexpr int KS = D / 16, DT = D / 32;
+                                              const u32x4_t (&qf)[D / 16], const u32x4_t (&dof)[D / 16], int n, int hf, bool second = false) {
+  constexpr int KS = D / 16, DT = D / 32, T = PAIR ? 1 : 2;    // PAIR: the first lane has the first 32 states, the second one the others
   const float sl2 = 1.4426950408889634f / sqrtf((float)D);
   f32x16_t sc[2], dp[2];
   float m = -FLT_MAX, sum = 0.f, dsum = 0.f;
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
+  for (int t = 0; t < 2; ++t)
 #pragma unroll
     for (int x = 0; x < KS; ++x) {
       sc[t] = MOE_MFMA(rd.row(k0 + t * step, 0, x), qf[x], x == 0 ? f32x16_t{} : sc[t]);
       dp[t] = MOE_MFMA(rd.row(v0 + t * step, 0, x), dof[x], x == 0 ? f32x16_t{} : dp[t]);
     }
+  if constexpr (PAIR) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      sc[t][i] = 32 * t + 8 * (i >> 2) + 4 * hf + (i & 3) < n ? rounded_product(sc[t][i], sl2) : -INFINITY;
-      m = fmaxf(m, sc[t][i]);
+      sc[0][i] = pair_fold(sc[0][i], sc[1][i]);
+      dp[0][i] = pair_fold(dp[0][i], dp[1][i]);
     }
   }
-  m = fmaxf(m, __shfl_xor(m, 32, 64));
 #pragma unroll
-  for (int t = 0; t < 2; ++t)
+  for (int t = 0; t < T; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      sc[t][i] = 32 * (PAIR ? second : t) + 8 * (i >> 2) + 4 * hf + (i & 3) < n ? rounded_product(sc[t][i], sl2) : -INFINITY;
+      m = fmaxf(m, sc[t][i]);
+    }
+  m = PAIR ? pair_max(m) : fmaxf(m, __shfl_xor(m, 32, 64));
+#pragma unroll
+  for (int t = 0; t < T; ++t)
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       sc[t][i] = __builtin_amdgcn_exp2f(sc[t][i] - m);
       sum += sc[t][i];
       dsum += sc[t][i] * dp[t][i];
     }
-  sum += __shfl_xor(sum, 32, 64);
-  dsum += __shfl_xor(dsum, 32, 64);
+  sum = PAIR ? pair_total(sum) : sum + __shfl_xor(sum, 32, 64);
+  dsum = PAIR ? pair_total(dsum) : dsum + __shfl_xor(dsum, 32, 64);
   const float inv = 1.0f / sum;
   dd = dsum * inv;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) dq[dt] = f32x16_t{};
+  u32x4_t f[2][2];
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
+  for (int t = 0; t < T; ++t)
 #pragma unroll
     for (int i = 0; i < 16; ++i) sc[t][i] *= inv * (dp[t][i] - dd);
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const u32x4_t f = pack8(sc[t], 8 * x);
+  for (int x = 0; x < 2; ++x) {
+    if constexpr (PAIR) {
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) dq[dt] = MOE_MFMA(rd.transposed(k0 + t * step, 16 * x, dt), f, dq[dt]);
+      for (int i = 0; i < 4; ++i) {
+        const PairTerms p = pair_terms<false>(sc[0][8 * x + 2 * i], sc[0][8 * x + 2 * i + 1]);
+        f[0][x][i] = p.a;
+        f[1][x][i] = p.b;
+      }
+    } else {
+      f[0][x] = pack8(sc[0], 8 * x);
+      f[1][x] = pack8(sc[1], 8 * x);
     }
+  }
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) dq[dt] = MOE_MFMA(rd.transposed(k0 + t * step, 16 * x, dt), f[t][x], dq[dt]);
+  if constexpr (PAIR) {
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) dq[dt][i] = pair_fold(dq[dt][i], dq[dt][i]);
   }
 }
 // A block of 128 columns of such a source.  K and V lie in LDS whole, the columns' rows come straight from memory.
@@ -966,22 +954,26 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(CrossGeo g, const bf16
 // ---------------------------------------------------------------- dq (and D) of few columns
 // As the forward pass of few columns: 32 of them a block, whose wavefronts take blocks of 32 states in turn and add up their sums at the end.  A
 // wavefront's chain of blocks bounds it (40.5 -> 22.6 us for 1 x 128 tokens of 4 heads of 128, 1500 states: 16 blocks instead of 4, a quarter of the states each).
-template <int D>
+// PAIR: q, ctx and dctx in pairs, and so dS; rest: their second terms.
+struct CrossRest { const bf16_t *q, *ctx, *dctx; };
+template <int D, bool PAIR>
 __global__ __launch_bounds__(64 * kFewWaves, 1) void cross_dq_few_kernel(CrossGeo g, const bf16_t* __restrict__ q, const bf16_t* __restrict__ kv,
                                                               const int32_t* __restrict__ src_len, const bf16_t* __restrict__ ctx,
                                                               const bf16_t* __restrict__ dctx, const float* __restrict__ lse,
-                                                              bf16_t* __restrict__ dqo, float* __restrict__ dvec) {
+                                                              bf16_t* __restrict__ dqo, float* __restrict__ dvec, CrossRest rest) {
   using GM = AttGeom<D>;
   constexpr int W = kFewWaves, KS = D / 16, DT = D / 32, kHalf = 32 * GM::kRow, kPlace = 2 * kHalf, COPIES = kHalf / 1024;
+  constexpr int kTile = PAIR ? 16 : 32;
   extern __shared__ __attribute__((aligned(256))) unsigned char att_lds[];
   const uint32_t lds0 = (uint32_t)(uintptr_t)((lds_ptr)att_lds);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 31, hf = lane >> 5;
+  const bool second = PAIR && r >= 16;
   const CrossCols cols(g, D);
-  const int tiles = (cols.count + 31) / 32;
+  const int tiles = (cols.count + kTile - 1) / kTile;
   const unsigned item = xcd_contiguous(blockIdx.x, gridDim.x), pair = item / tiles;
   const int k = __builtin_amdgcn_readfirstlane(pair % g.kv_heads), b = __builtin_amdgcn_readfirstlane(pair / g.kv_heads);
-  const int c = (int)(item % tiles) * 32 + r;
+  const int c = (int)(item % tiles) * kTile + r % kTile;
   const size_t row = cols.base(b, k, D) + cols.offset<D>(cols.within(c));
   const size_t column = ((size_t)b * g.kv_heads + k) * cols.count + cols.within(c);
   const int n = held_states(src_len, b, g.Lk), Akv = g.kv_heads * D;
@@ -1001,12 +993,24 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void cross_dq_few_kernel(CrossGe
   float dd = 0.f;
 #pragma unroll
   for (int s = 0; s < KS; ++s) {
-    qf[s] = *reinterpret_cast<const u32x4_t*>(q + row + 16 * s + 8 * hf);
-    dof[s] = *reinterpret_cast<const u32x4_t*>(dctx + row + 16 * s + 8 * hf);
-    const u32x4_t of = *reinterpret_cast<const u32x4_t*>(ctx + row + 16 * s + 8 * hf);
+    const size_t at = row + 16 * s + 8 * hf;
+    qf[s] = *reinterpret_cast<const u32x4_t*>((second ? rest.q : q) + at);
+    dof[s] = *reinterpret_cast<const u32x4_t*>((second ? rest.dctx : dctx) + at);
     float gr[8], ov[8];
-    Vec16<bf16_t>::unpack(uint4{dof[s][0], dof[s][1], dof[s][2], dof[s][3]}, gr);
-    Vec16<bf16_t>::unpack(uint4{of[0], of[1], of[2], of[3]}, ov);
+    Vec16<bf16_t>::unpack(*reinterpret_cast<const uint4*>(ctx + at), ov);
+    if constexpr (PAIR) {
+      float gr2[8], ov2[8];
+      Vec16<bf16_t>::unpack(*reinterpret_cast<const uint4*>(dctx + at), gr);
+      Vec16<bf16_t>::unpack(*reinterpret_cast<const uint4*>(rest.dctx + at), gr2);
+      Vec16<bf16_t>::unpack(*reinterpret_cast<const uint4*>(rest.ctx + at), ov2);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        gr[i] += gr2[i];
+        ov[i] += ov2[i];
+      }
+    } else {
+      Vec16<bf16_t>::unpack(uint4{dof[s][0], dof[s][1], dof[s][2], dof[s][3]}, gr);
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i) dd = fmaf(gr[i], ov[i], dd);
   }
@@ -1019,8 +1023,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void cross_dq_few_kernel(CrossGe
     start(0, 0);
     start(1, 1);
     wait_all_copies();
-    few_states_dq<D>(dq, dd, rd, 0, kHalf, kPlace, qf, dof, n, hf);
-    if (c >= cols.count) return;
+    few_states_dq<D, PAIR>(dq, dd, rd, 0, kHalf, kPlace, qf, dof, n, hf, second);
+    if (c >= cols.count || second) return;
     if (hf == 0) dvec[column] = dd;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
@@ -1049,14 +1053,30 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void cross_dq_few_kernel(CrossGe
       s = MOE_MFMA(rd.row(place, 0, i), qf[i], i == 0 ? f32x16_t{} : s);
       dp = MOE_MFMA(rd.row(place + kHalf, 0, i), dof[i], i == 0 ? f32x16_t{} : dp);
     }
+    if constexpr (PAIR) {                                      // the first lane has the block's first 16 states, the second one the others
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
+      for (int i = 0; i < 8; ++i) {
+        s[i] = pair_fold(s[i], s[i + 8]);
+        dp[i] = pair_fold(dp[i], dp[i + 8]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < (PAIR ? 8 : 16); ++i) {
       const float e = __builtin_amdgcn_exp2f(fmaf(s[i], sl2, -lse2)) * (dp[i] - dd);
-      s[i] = 32 * kb + 8 * (i >> 2) + 4 * hf + (i & 3) >= n ? 0.f : e;
+      s[i] = 32 * kb + 16 * second + 8 * (i >> 2) + 4 * hf + (i & 3) >= n ? 0.f : e;
+    }
+    u32x4_t both[2];
+    if constexpr (PAIR) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const PairTerms p = pair_terms<false>(s[2 * i], s[2 * i + 1]);
+        both[0][i] = p.a;
+        both[1][i] = p.b;
+      }
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const u32x4_t dsf = pack8(s, 8 * h);
+      const u32x4_t dsf = PAIR ? both[h] : pack8(s, 8 * h);
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) dq[dt] = MOE_MFMA(rd.transposed(place, 16 * h, dt), dsf, dq[dt]);
     }
@@ -1072,7 +1092,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void cross_dq_few_kernel(CrossGe
     for (int i = 0; i < 16; ++i) *at(((wave * DT + t) * 16 + i) * 256 + lane * 4) = dq[t][i];
   __syncthreads();
   if (c >= cols.count) return;
-  if (wave == 0 && hf == 0) dvec[column] = dd;
+  if (wave == 0 && hf == 0 && !second) dvec[column] = dd;
 #pragma unroll
   for (int dt = wave; dt < DT; dt += W) {
     float v[16];                                               // d = 32 dt + 8 (i/4) + 4 hf + i%4 of column c
@@ -1081,8 +1101,10 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void cross_dq_few_kernel(CrossGe
       v[i] = 0.f;
 #pragma unroll
       for (int x = 0; x < W; ++x) v[i] += *at(((x * DT + dt) * 16 + i) * 256 + lane * 4);
+      if constexpr (PAIR) v[i] = pair_fold(v[i], v[i]);
       v[i] *= scale;
     }
+    if (second) continue;
 #pragma unroll
     for (int x = 0; x < 4; ++x)
       *reinterpret_cast<u32x2_t*>(dqo + row + 32 * dt + 8 * x + 4 * hf) =
@@ -1097,15 +1119,18 @@ struct CrossRanges {
   size_t elems;              // of dkv
   float* sums;               // [ranges][dkv]
 };
-template <int D, int CT, bool RANGES = false>
+// PAIR: blocks of 32 columns, rows 0 .. 31 of a staged block first terms and 32 .. 63 second ones; P and dS in pairs too.
+template <int D, int CT, bool RANGES = false, bool PAIR = false>
 __global__ __launch_bounds__(256, 1) void cross_dkv_kernel(CrossGeo g, const bf16_t* __restrict__ q, const bf16_t* __restrict__ kv,
                                                            const int32_t* __restrict__ src_len, const bf16_t* __restrict__ dctx,
                                                            const float* __restrict__ lse, const float* __restrict__ dvec,
-                                                           bf16_t* __restrict__ dkv, CrossRanges ranges) {
+                                                           bf16_t* __restrict__ dkv, CrossRanges ranges, CrossRest rest) {
+  static_assert(!PAIR || CT == 1, "");
   using GM = AttGeom<D>;
   constexpr int KS = D / 16, DT = D / 32, kOwnBlock = 32 * CT * GM::kRow;
   constexpr int kGrad = GM::kBlock, kStats = 2 * GM::kBlock, kStage = kStats + 512;   // Q rows, dO rows, 64 lse, 64 D
-  constexpr bool kValuesInLds = D == 128 && CT == 2;           // there both operands' fragments and both results are
+  constexpr int kColumns = PAIR ? 32 : 64;
+  constexpr bool kValuesInLds = D == 128 && (CT == 2 || PAIR); // there both operands' fragments and both results are
   constexpr int kOwn = 2 * kStage;                             // 384 registers, too many beside S and dP
   extern __shared__ __attribute__((aligned(256))) unsigned char att_lds[];
   const uint32_t lds0 = (uint32_t)(uintptr_t)((lds_ptr)att_lds);
@@ -1136,24 +1161,26 @@ __global__ __launch_bounds__(256, 1) void cross_dkv_kernel(CrossGeo g, const bf1
     return;
   }
   const size_t head = cols.base(w.b, w.k, D);
-  const bf16_t *const qbase = q + head, *const gbase = dctx + head;
+  const bool second = PAIR && wave >= 2;
+  const bf16_t *const qbase = (second ? rest.q : q) + head, *const gbase = (second ? rest.dctx : dctx) + head;
   const float* const stat = (wave & 1 ? dvec : lse) + (size_t)w.bk * cols.count;      // (two wavefronts copy the same 64 values)
   const bool live = w.col0 < n;
 
   uint32_t off[GM::kCopies];
-  column_offsets<D>(off, cols, wave, lane);
-  int qb0 = 0, nqb = (cols.count + 63) / 64;
+  const int row_wave = PAIR ? wave & 1 : wave;                 // whose rows of a block of columns the wavefront copies
+  column_offsets<D>(off, cols, row_wave, lane);
+  int qb0 = 0, nqb = (cols.count + kColumns - 1) / kColumns;
   if constexpr (RANGES) {
     qb0 = w.range * ranges.blocks;
     nqb = qb0 + ranges.blocks < nqb ? qb0 + ranges.blocks : nqb;
   }
   // copy x of block j: Q rows, dO rows, 64 values of lse and D
   auto start = [&](int j, int x) __attribute__((always_inline)) {
-    const uint32_t st = lds0 + (j & 1) * kStage;
-    const int first = 64 * j;
+    const uint32_t st = lds0 + (j & 1) * kStage, to = st + (wave - row_wave) * GM::kCopies * 1024;
+    const int first = kColumns * j;
     const size_t at = cols.offset<D>(first);
-    if (x < GM::kCopies) stage_rows<D>(st, qbase + at, cols.count - first, off, x, wave, lane);
-    else if (x < 2 * GM::kCopies) stage_rows<D>(st + kGrad, gbase + at, cols.count - first, off, x - GM::kCopies, wave, lane);
+    if (x < GM::kCopies) stage_rows<D>(to, qbase + at, cols.count - first, off, x, row_wave, lane);
+    else if (x < 2 * GM::kCopies) stage_rows<D>(to + kGrad, gbase + at, cols.count - first, off, x - GM::kCopies, row_wave, lane);
     else {
       const uint32_t soff = 4 * cols.within(first + lane);
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(st + kStats + (wave & 1) * 256),
@@ -1203,7 +1230,10 @@ __global__ __launch_bounds__(256, 1) void cross_dkv_kernel(CrossGeo g, const bf1
 #pragma unroll
   for (int c = 0; c < CT; ++c)
 #pragma unroll
-    for (int t = 0; t < DT; ++t) { clear_acc(dk[c][t]); clear_acc(dv[c][t]); }
+    for (int t = 0; t < DT; ++t) {
+      if constexpr (PAIR) dk[c][t] = dv[c][t] = f32x16_t{};
+      else { clear_acc(dk[c][t]); clear_acc(dv[c][t]); }
+    }
   const float scale = 1.0f / sqrtf((float)D), sl2 = 1.4426950408889634f * scale;
   // value i of a tile belongs to column 32 t + 8 (i/4) + 4 hf + i%4: four consecutive columns per i/4
   auto stat4 = [&](uint32_t block, int t, int i4) __attribute__((always_inline)) {
@@ -1280,10 +1310,60 @@ __global__ __launch_bounds__(256, 1) void cross_dkv_kernel(CrossGeo g, const bf1
           if constexpr (x == 0) dst[1][pc] = pack8(ds[pc], 8);
         });
   };
-  for (int qb = qb0; qb + 1 < nqb; ++qb) step(qb, std::false_type{});
-  step(nqb - 1, std::true_type{});
-  settle_all(dk);
-  settle_all(dv);
+  auto pair_step = [&](int qb) __attribute__((always_inline)) {
+    wait_all_copies();                                         // block qb is there;
+    __syncthreads();                                           // block qb - 1 is read, its place free
+    if (qb + 1 < nqb) {
+#pragma unroll
+      for (int x = 0; x < COPIES; ++x) start(qb + 1, x);
+    }
+    const uint32_t qst = (qb & 1) * kStage, gst = qst + kGrad, sst = qst + kStats;
+    f32x16_t s[2], dp[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int x = 0; x < KS; ++x) {
+        u32x4_t col;
+        if constexpr (kValuesInLds) col = rd.row(own, 0, x);
+        else col = vf[0][x];
+        s[t] = MOE_MFMA(rd.row(qst, t, x), kf[0][x], x == 0 ? f32x16_t{} : s[t]);
+        dp[t] = MOE_MFMA(rd.row(gst, t, x), col, x == 0 ? f32x16_t{} : dp[t]);
+      }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const bool there = kColumns * qb + 8 * (i >> 2) + 4 * hf + (i & 3) < cols.count;
+      const float p = __builtin_amdgcn_exp2f(fmaf(pair_sum(s[0][i], s[1][i]), sl2, -stat4(sst, 0, i / 4)[i % 4]));
+      const float ds = p * (pair_sum(dp[0][i], dp[1][i]) - stat4(sst + 256, 0, i / 4)[i % 4]);
+      s[0][i] = there ? p : 0.f;
+      dp[0][i] = there ? ds : 0.f;
+    }
+    auto product = [&](f32x16_t (&acc)[DT], const f32x16_t& v, uint32_t block) __attribute__((always_inline)) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const u32x4_t first = pack8(v, 8 * h);
+        u32x4_t left;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) left[i] = bf16_rest_x2(v[8 * h + 2 * i], v[8 * h + 2 * i + 1], first[i]);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          const u32x4_t a = rd.transposed(block, 16 * h, dt);
+          acc[dt] = MOE_MFMA(rd.transposed(block, 32 + 16 * h, dt), first, acc[dt]);
+          acc[dt] = MOE_MFMA(a, left, acc[dt]);
+          acc[dt] = MOE_MFMA(a, first, acc[dt]);
+        }
+      }
+    };
+    product(dv[0], s[0], gst);
+    product(dk[0], dp[0], qst);
+  };
+  if constexpr (PAIR) {
+    for (int qb = qb0; qb < nqb; ++qb) pair_step(qb);
+  } else {
+    for (int qb = qb0; qb + 1 < nqb; ++qb) step(qb, std::false_type{});
+    step(nqb - 1, std::true_type{});
+    settle_all(dk);
+    settle_all(dv);
+  }
   if constexpr (RANGES) {
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
@@ -1317,7 +1397,6 @@ __global__ __launch_bounds__(256, 1) void cross_dkv_kernel(CrossGeo g, const bf1
 
 template <int D> constexpr int kLdsFew = kFewWaves * 2 * 64 * AttGeom<D>::kRow;
 template <int D> constexpr int kLdsForward = 4 * AttGeom<D>::kBlock;
-template <int D> constexpr int kLdsForwardPairs = kLdsForward<D> + 16384;        // (two blocks a unit)
 template <int D> constexpr int kLdsQ = 5 * AttGeom<D>::kBlock;
 template <int D> constexpr int kLdsQShort = 2 * AttGeom<D>::kBlock;
 static_assert(kLdsQShort<128> <= 65536, "without a raised limit");
@@ -1325,16 +1404,17 @@ template <int D, int CT> constexpr int kLdsKV = 2 * (2 * AttGeom<D>::kBlock + 51
 
 template <int D>
 int prepare_kernels() {
-  static LdsLimitOnce once, once_pair, once_pairs, once_few, once_few_pair, once_few_pairs, once_q, once_qfew, once_kvr, once_kv1, once_kv2;
-  static_assert(kLdsFew<D> >= kFewWaves * (128 * D + 768), "the wavefronts' sums and statistics");
-  int rc = ensure_lds_limit(once, reinterpret_cast<const void*>(cross_forward_kernel<D, false, true>), kLdsForward<D>);
-  if (rc == MOE_OK) rc = ensure_lds_limit(once_pair, reinterpret_cast<const void*>(cross_forward_kernel<D, true, false>), kLdsForward<D>);
-  if (rc == MOE_OK) rc = ensure_lds_limit(once_pairs, reinterpret_cast<const void*>(cross_forward_kernel<D, true, true>), kLdsForwardPairs<D>);
-  if (rc == MOE_OK) rc = ensure_lds_limit(once_few, reinterpret_cast<const void*>(cross_few_kernel<D, false, true>), kLdsFew<D>);
-  if (rc == MOE_OK) rc = ensure_lds_limit(once_few_pair, reinterpret_cast<const void*>(cross_few_kernel<D, true, false>), kLdsFew<D>);
-  if (rc == MOE_OK) rc = ensure_lds_limit(once_few_pairs, reinterpret_cast<const void*>(cross_few_kernel<D, true, true>), kLdsFew<D>);
+  static LdsLimitOnce once, once_pair, once_few, once_few_pair, once_q, once_qfew, once_qpair, once_kvr, once_kv1, once_kvp, once_kvrp, once_kv2;
+  static_assert(kLdsFew<D> >= kFewWaves * (128 * D + 512), "the wavefronts' sums and statistics");
+  int rc = ensure_lds_limit(once, reinterpret_cast<const void*>(cross_forward_kernel<D, false>), kLdsForward<D>);
+  if (rc == MOE_OK) rc = ensure_lds_limit(once_pair, reinterpret_cast<const void*>(cross_forward_kernel<D, true>), kLdsForward<D>);
+  if (rc == MOE_OK) rc = ensure_lds_limit(once_few, reinterpret_cast<const void*>(cross_few_kernel<D, false>), kLdsFew<D>);
+  if (rc == MOE_OK) rc = ensure_lds_limit(once_few_pair, reinterpret_cast<const void*>(cross_few_kernel<D, true>), kLdsFew<D>);
   if (rc == MOE_OK) rc = ensure_lds_limit(once_q, reinterpret_cast<const void*>(cross_dq_kernel<D>), kLdsQ<D>);
-  if (rc == MOE_OK) rc = ensure_lds_limit(once_qfew, reinterpret_cast<const void*>(cross_dq_few_kernel<D>), kLdsFew<D>);
+  if (rc == MOE_OK) rc = ensure_lds_limit(once_qfew, reinterpret_cast<const void*>(cross_dq_few_kernel<D, false>), kLdsFew<D>);
+  if (rc == MOE_OK) rc = ensure_lds_limit(once_qpair, reinterpret_cast<const void*>(cross_dq_few_kernel<D, true>), kLdsFew<D>);
+  if (rc == MOE_OK) rc = ensure_lds_limit(once_kvp, reinterpret_cast<const void*>(cross_dkv_kernel<D, 1, false, true>), (kLdsKV<D, 1>));
+  if (rc == MOE_OK) rc = ensure_lds_limit(once_kvrp, reinterpret_cast<const void*>(cross_dkv_kernel<D, 1, true, true>), (kLdsKV<D, 1>));
   if (rc == MOE_OK) rc = ensure_lds_limit(once_kv1, reinterpret_cast<const void*>(cross_dkv_kernel<D, 1>), (kLdsKV<D, 1>));
   if (rc == MOE_OK) rc = ensure_lds_limit(once_kvr, reinterpret_cast<const void*>(cross_dkv_kernel<D, 1, true>), (kLdsKV<D, 1>));
   if constexpr (D == 128)
@@ -1361,12 +1441,10 @@ int forward(const CrossShape& s, const CrossPlan& plan, const CrossForward& f, c
   auto run = [&](auto kernel, int lds, auto... last) {
     hipLaunchKernelGGL(kernel, grid, threads, lds, st, g, f.q, f.q_rest, f.kv, f.src_len, f.ctx, f.ctx_rest, f.lse, last...);
   };
-  if (plan.few && !pair) run(cross_few_kernel<D, false, true>, kLdsFew<D>, parts);
-  else if (plan.few && f.lse != nullptr) run(cross_few_kernel<D, true, true>, kLdsFew<D>, parts);
-  else if (plan.few) run(cross_few_kernel<D, true, false>, kLdsFew<D>, parts);
-  else if (!pair) run(cross_forward_kernel<D, false, true>, kLdsForward<D>);
-  else if (f.lse != nullptr) run(cross_forward_kernel<D, true, true>, kLdsForwardPairs<D>);
-  else run(cross_forward_kernel<D, true, false>, kLdsForward<D>);
+  if (plan.few && pair) run(cross_few_kernel<D, true>, kLdsFew<D>, parts);
+  else if (plan.few) run(cross_few_kernel<D, false>, kLdsFew<D>, parts);
+  else if (pair) run(cross_forward_kernel<D, true>, kLdsForward<D>);
+  else run(cross_forward_kernel<D, false>, kLdsForward<D>);
   return check_launch();
 }
 template <typename T>
@@ -1379,7 +1457,8 @@ int join(const CrossShape& s, const CrossParts& parts, const int32_t* src_len, T
 }
 template <int D>
 int backward(const CrossShape& s, const bf16_t* q, const bf16_t* kv, const int32_t* src_len, const bf16_t* ctx, const bf16_t* dctx,
-             const float* lse, bf16_t* dq, bf16_t* dkv, float* dvec, float* sums, hipStream_t st) {
+             const float* lse, bf16_t* dq, bf16_t* dkv, float* dvec, float* sums, const CrossRest& rest, hipStream_t st) {
+  const bool pair = rest.q != nullptr;
   int cus = 0;
   if (prepare_kernels<D>() != MOE_OK || compute_units(&cus) != MOE_OK) return MOE_EHIP;
   const long long blocks = s.B * s.kv_heads * ((s.columns() + 127) / 128), blocks1 = s.B * s.kv_heads * ((s.Lk + 127) / 128),
@@ -1391,23 +1470,31 @@ int backward(const CrossShape& s, const bf16_t* q, const bf16_t* kv, const int32
   // 32) 12.8 / 9.7; 3 x 700, 700 (264 of 32) 22.3 / 25.9; 4 x 400, 1000 32.5 / 36.6
   const long long blocks32 = s.B * s.kv_heads * ((s.columns() + 31) / 32);
   const bool few_dq = blocks32 <= cus || (D == 64 && blocks32 <= 2LL * cus && 2 * blocks <= cus);
-  if (s.Lk <= 64) hipLaunchKernelGGL((cross_dq_short_kernel<D>), dim3((unsigned)blocks), dim3(256), kLdsQShort<D>, st, g, q, kv, src_len, dctx, dq, dvec);
-  else if (few_dq) hipLaunchKernelGGL((cross_dq_few_kernel<D>), dim3((unsigned)blocks32), dim3(64 * kFewWaves), kLdsFew<D>, st, g, q, kv, src_len, ctx, dctx, lse, dq, dvec);
+  const long long blocks16 = s.B * s.kv_heads * ((s.columns() + 15) / 16);
+  if (pair) hipLaunchKernelGGL((cross_dq_few_kernel<D, true>), dim3((unsigned)blocks16), dim3(64 * kFewWaves), kLdsFew<D>, st, g, q, kv, src_len, ctx, dctx, lse, dq, dvec, rest);
+  else if (s.Lk <= 64) hipLaunchKernelGGL((cross_dq_short_kernel<D>), dim3((unsigned)blocks), dim3(256), kLdsQShort<D>, st, g, q, kv, src_len, dctx, dq, dvec);
+  else if (few_dq) hipLaunchKernelGGL((cross_dq_few_kernel<D, false>), dim3((unsigned)blocks32), dim3(64 * kFewWaves), kLdsFew<D>, st, g, q, kv, src_len, ctx, dctx, lse, dq, dvec, rest);
   else hipLaunchKernelGGL((cross_dq_kernel<D>), dim3((unsigned)blocks), dim3(256), kLdsQ<D>, st, g, q, kv, src_len, ctx, dctx, lse, dq, dvec);
-  const int each = cross_dkv_blocks(s), blocks64 = (int)((s.columns() + 63) / 64);
-  const CrossRanges ranges{(blocks64 + each - 1) / each, each, (size_t)s.B * s.Lk * 2 * s.kv_heads * D, sums};
+  const int each = pair ? cross_pair_dkv_blocks(s) : cross_dkv_blocks(s), blocks64 = (int)((s.columns() + 63) / 64);
+  const CrossRanges ranges{(blocks64 + each - 1) / each, pair ? 2 * each : each, (size_t)s.B * s.Lk * 2 * s.kv_heads * D, sums};
   if (ranges.count > 1) {
-    hipLaunchKernelGGL((cross_dkv_kernel<D, 1, true>), dim3((unsigned)(blocks1 * ranges.count)), dim3(256), (kLdsKV<D, 1>), st, g, q, kv, src_len, dctx, lse, dvec, dkv, ranges);
+    const dim3 grid((unsigned)(blocks1 * ranges.count));
+    if (pair) hipLaunchKernelGGL((cross_dkv_kernel<D, 1, true, true>), grid, dim3(256), (kLdsKV<D, 1>), st, g, q, kv, src_len, dctx, lse, dvec, dkv, ranges, rest);
+    else hipLaunchKernelGGL((cross_dkv_kernel<D, 1, true>), grid, dim3(256), (kLdsKV<D, 1>), st, g, q, kv, src_len, dctx, lse, dvec, dkv, ranges, rest);
     const int rc = check_launch();
     return rc != MOE_OK ? rc : launch_add_ranges(sums, ranges.count, (long long)ranges.elems, dkv, st);
+  }
+  if (pair) {
+    hipLaunchKernelGGL((cross_dkv_kernel<D, 1, false, true>), dim3((unsigned)blocks1), dim3(256), (kLdsKV<D, 1>), st, g, q, kv, src_len, dctx, lse, dvec, dkv, ranges, rest);
+    return check_launch();
   }
   // two tiles of 32 states per wavefront where that takes fewer rounds of blocks (1.46 times as long each: attention_dkv_wide)
   if constexpr (D == 128)
     if (1.46 * (double)((blocks2 + cus - 1) / cus) < (double)((blocks1 + cus - 1) / cus)) {
-      hipLaunchKernelGGL((cross_dkv_kernel<D, 2>), dim3((unsigned)blocks2), dim3(256), (kLdsKV<D, 2>), st, g, q, kv, src_len, dctx, lse, dvec, dkv, ranges);
+      hipLaunchKernelGGL((cross_dkv_kernel<D, 2>), dim3((unsigned)blocks2), dim3(256), (kLdsKV<D, 2>), st, g, q, kv, src_len, dctx, lse, dvec, dkv, ranges, rest);
       return check_launch();
     }
-  hipLaunchKernelGGL((cross_dkv_kernel<D, 1>), dim3((unsigned)blocks1), dim3(256), (kLdsKV<D, 1>), st, g, q, kv, src_len, dctx, lse, dvec, dkv, ranges);
+  hipLaunchKernelGGL((cross_dkv_kernel<D, 1>), dim3((unsigned)blocks1), dim3(256), (kLdsKV<D, 1>), st, g, q, kv, src_len, dctx, lse, dvec, dkv, ranges, rest);
   return check_launch();
 }
 
@@ -1471,18 +1558,19 @@ static CrossPlan plan_of(int act_dtype, const CrossShape& s, bool pair) {
 CrossPlan cross_plan(int act_dtype, const CrossShape& s) { return plan_of(act_dtype, s, false); }
 CrossPlan cross_pair_plan(const CrossShape& s) { return plan_of(MOE_BF16, s, true); }
 
-static size_t scratch_of(const CrossShape& s, const CrossPlan& p, bool pair) {
+static size_t scratch_of(const CrossShape& s, const CrossPlan& p) {
   const size_t columns = (size_t)s.B * s.kv_heads * s.columns();
-  return p.splits > 1 ? align_up(columns * p.splits * sizeof(float2), 256) + columns * p.splits * (s.d + pair) * sizeof(float) : 0;
+  return p.splits > 1 ? align_up(columns * p.splits * sizeof(float2), 256) + columns * p.splits * s.d * sizeof(float) : 0;
 }
 
-size_t cross_scratch_bytes(int act_dtype, const CrossShape& s) { return scratch_of(s, cross_plan(act_dtype, s), false); }
-size_t cross_pair_scratch_bytes(const CrossShape& s) { return scratch_of(s, cross_pair_plan(s), true); }
+size_t cross_scratch_bytes(int act_dtype, const CrossShape& s) { return scratch_of(s, cross_plan(act_dtype, s)); }
+size_t cross_pair_scratch_bytes(const CrossShape& s) { return scratch_of(s, cross_pair_plan(s)); }
 
-int cross_dkv_blocks(const CrossShape& s) {
+// in pairs a step has 32 columns, of as many products and more vector work
+static int dkv_blocks_of(const CrossShape& s, bool pair) {
   constexpr double kUnits = 256;                               // of a whole device: the choice sizes a workspace
   const double blocks = (double)s.B * s.kv_heads * ((s.Lk + 127) / 128), at_once = s.d == 64 ? 2 * kUnits : kUnits;
-  const double step = s.d == 64 ? 1.18 : 1.8, mb = blocks * 128 * 2 * s.d * sizeof(float) / 1e6;
+  const double step = pair ? (s.d == 64 ? 3.8 : 4.6) : s.d == 64 ? 1.18 : 1.8, mb = blocks * 128 * 2 * s.d * sizeof(float) / 1e6;
   const int all = (int)((s.columns() + 63) / 64);
   int best = all;
   double least = 5 + step * all;
@@ -1498,16 +1586,18 @@ int cross_dkv_blocks(const CrossShape& s) {
   return best;
 }
 
-size_t cross_bwd_scratch_bytes(int act_dtype, const CrossShape& s) {
+int cross_dkv_blocks(const CrossShape& s) { return dkv_blocks_of(s, false); }
+int cross_pair_dkv_blocks(const CrossShape& s) { return dkv_blocks_of(s, true); }
+
+size_t cross_bwd_scratch_bytes(int act_dtype, const CrossShape& s, bool pair) {
   if (act_dtype == MOE_F32) return 0;
-  const long long all = (s.columns() + 63) / 64, each = cross_dkv_blocks(s), ranges = (all + each - 1) / each;
+  const long long all = (s.columns() + 63) / 64, each = dkv_blocks_of(s, pair), ranges = (all + each - 1) / each;
   return ranges > 1 ? (size_t)ranges * s.B * s.Lk * 2 * s.kv_heads * s.d * sizeof(float) : 0;
 }
 
 static CrossParts parts_of(const CrossShape& s, const CrossPlan& plan, void* scratch) {
   const size_t columns = (size_t)s.B * s.kv_heads * s.columns();
-  float* const sums = reinterpret_cast<float*>(static_cast<char*>(scratch) + align_up(columns * plan.splits * sizeof(float2), 256));
-  return {plan.splits, static_cast<float2*>(scratch), sums, sums + columns * plan.splits * s.d};
+  return {plan.splits, static_cast<float2*>(scratch), reinterpret_cast<float*>(static_cast<char*>(scratch) + align_up(columns * plan.splits * sizeof(float2), 256))};
 }
 static int launch_bf16(const CrossShape& s, const CrossPlan& plan, const CrossForward& f, void* scratch, hipStream_t st) {
   const CrossParts parts = parts_of(s, plan, scratch);
@@ -1533,19 +1623,30 @@ int launch_cross_attention_pair(const CrossShape& s, const void* q, const void* 
                      static_cast<bf16_t*>(ctx), static_cast<bf16_t*>(ctx_rest), lse}, scratch, st);
 }
 
-int launch_cross_attention_bwd(int act_dtype, const CrossShape& s, const void* q, const void* kv, const int32_t* src_len,
-                               const void* ctx, const void* dctx, const float* lse, void* dq, void* dkv, float* dvec, float* sums, hipStream_t st) {
-  if (act_dtype == MOE_F32)
-    return launch_cross_attention_f32_bwd(s, static_cast<const float*>(q), static_cast<const float*>(kv), src_len, static_cast<const float*>(ctx),
-                                          static_cast<const float*>(dctx), lse, static_cast<float*>(dq), static_cast<float*>(dkv), dvec, st);
+static int launch_bf16_bwd(const CrossShape& s, const void* q, const void* kv, const int32_t* src_len, const void* ctx, const void* dctx, const float* lse,
+                           void* dq, void* dkv, float* dvec, float* sums, const CrossRest& rest, hipStream_t st) {
   auto qb = static_cast<const bf16_t*>(q);
   auto kb = static_cast<const bf16_t*>(kv);
   auto c = static_cast<const bf16_t*>(ctx);
   auto gb = static_cast<const bf16_t*>(dctx);
   auto dqb = static_cast<bf16_t*>(dq);
   auto dkb = static_cast<bf16_t*>(dkv);
-  return s.d == 64 ? backward<64>(s, qb, kb, src_len, c, gb, lse, dqb, dkb, dvec, sums, st)
-                   : backward<128>(s, qb, kb, src_len, c, gb, lse, dqb, dkb, dvec, sums, st);
+  return s.d == 64 ? backward<64>(s, qb, kb, src_len, c, gb, lse, dqb, dkb, dvec, sums, rest, st)
+                   : backward<128>(s, qb, kb, src_len, c, gb, lse, dqb, dkb, dvec, sums, rest, st);
+}
+
+int launch_cross_attention_bwd(int act_dtype, const CrossShape& s, const void* q, const void* kv, const int32_t* src_len,
+                               const void* ctx, const void* dctx, const float* lse, void* dq, void* dkv, float* dvec, float* sums, hipStream_t st) {
+  if (act_dtype == MOE_F32)
+    return launch_cross_attention_f32_bwd(s, static_cast<const float*>(q), static_cast<const float*>(kv), src_len, static_cast<const float*>(ctx),
+                                          static_cast<const float*>(dctx), lse, static_cast<float*>(dq), static_cast<float*>(dkv), dvec, st);
+  return launch_bf16_bwd(s, q, kv, src_len, ctx, dctx, lse, dq, dkv, dvec, sums, CrossRest{}, st);
+}
+
+int launch_cross_attention_pair_bwd(const CrossShape& s, const CrossPair& q, const void* kv, const int32_t* src_len, const CrossPair& ctx, const CrossPair& dctx,
+                                    const float* lse, void* dq, void* dkv, float* dvec, float* sums, hipStream_t st) {
+  const CrossRest rest{static_cast<const bf16_t*>(q.rest), static_cast<const bf16_t*>(ctx.rest), static_cast<const bf16_t*>(dctx.rest)};
+  return launch_bf16_bwd(s, q.first, kv, src_len, ctx.first, dctx.first, lse, dq, dkv, dvec, sums, rest, st);
 }
 
 int launch_held_rows(int act_dtype, const void* mem, const int32_t* src_len, void* out, long long B, int Lk, int M, hipStream_t st) {

@@ -18,7 +18,8 @@ namespace {
 constexpr int kWaves = 8, kBytesB = 64 * 64, kBytesA = 32 * 128, kPlace = kBytesB + kBytesA, kAhead = 2;
 constexpr int kLds = kWaves * kAhead * kPlace;
 
-template <bool PAIR>
+// B_KC: B is [N,K], its rows staged and read as A's.
+template <bool PAIR, bool B_KC>
 __global__ __launch_bounds__(64 * kWaves, 1) void few_rows_kernel(const bf16_t* __restrict__ A, const bf16_t* __restrict__ A_rest,
                                                                   const bf16_t* __restrict__ B, bf16_t* __restrict__ C, bf16_t* __restrict__ C_rest,
                                                                   int R, int N, int K) {
@@ -31,7 +32,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void few_rows_kernel(const bf16_t* 
   const int col0 = (int)(item / row_tiles) * 32, row0 = (int)(item % row_tiles) * kRows;
   const uint32_t own = lds0 + wave * (kAhead * kPlace);
   const uint32_t tr0 = own + (8 * hf + (p16 >> 2)) * 64 + 32 * b1 + 8 * (p16 & 3);
-  const uint32_t a0 = own + kBytesB + r * 128 + ((hf ^ ((r >> 1) & 7)) << 4);
+  const uint32_t row_at = r * 128 + ((hf ^ ((r >> 1) & 7)) << 4), a0 = own + kBytesB + row_at, b0 = own + row_at;
   auto copy = [&](uint32_t to, const bf16_t* from, bool there) __attribute__((always_inline)) {
     const uint64_t at = there ? (uint64_t)(uintptr_t)from : (uint64_t)(uintptr_t)&att_zero_line;
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(at) : "memory");
@@ -45,8 +46,13 @@ __global__ __launch_bounds__(64 * kWaves, 1) void few_rows_kernel(const bf16_t* 
       if (k0 >= K) break;                                      // wavefront-uniform
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
-        const int k = k0 + 16 * x + lane / 4, c = col0 + 8 * (lane % 4);
-        copy(own + j * kPlace + x * 1024, B + (size_t)k * N + c, k < K && c < N);
+        if constexpr (B_KC) {
+          const int i = 8 * x + lane / 8, k = k0 + 8 * ((lane % 8) ^ ((i >> 1) & 7));
+          copy(own + j * kPlace + x * 1024, B + (size_t)(col0 + i) * K + k, col0 + i < N && k < K);
+        } else {
+          const int k = k0 + 16 * x + lane / 4, c = col0 + 8 * (lane % 4);
+          copy(own + j * kPlace + x * 1024, B + (size_t)k * N + c, k < K && c < N);
+        }
       }
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
@@ -61,11 +67,15 @@ __global__ __launch_bounds__(64 * kWaves, 1) void few_rows_kernel(const bf16_t* 
       if (64 * (first + kWaves * j) >= K) break;
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
-        const uint32_t at = tr0 + j * kPlace + s * 1024;
-        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(uintptr_t)at);
-        const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(uintptr_t)(at + 256));
         const u32x4_t a = *(lds_u4_ptr)(uintptr_t)((a0 ^ (s << 5)) + j * kPlace);
-        acc = MOE_MFMA(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), a, acc);
+        if constexpr (B_KC) {
+          acc = MOE_MFMA(*(lds_u4_ptr)(uintptr_t)((b0 ^ (s << 5)) + j * kPlace), a, acc);
+        } else {
+          const uint32_t at = tr0 + j * kPlace + s * 1024;
+          const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(uintptr_t)at);
+          const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(uintptr_t)(at + 256));
+          acc = MOE_MFMA(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), a, acc);
+        }
       }
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // read before the next copies go there
@@ -147,9 +157,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void few_rows_f32_kernel(const floa
 }  // namespace
 
 int prepare_few_rows() {
-  static LdsLimitOnce once, once_pair;
-  const int rc = ensure_lds_limit(once, reinterpret_cast<const void*>(few_rows_kernel<false>), kLds);
-  return rc != MOE_OK ? rc : ensure_lds_limit(once_pair, reinterpret_cast<const void*>(few_rows_kernel<true>), kLds);
+  static LdsLimitOnce once, once_pair, once_kc;
+  int rc = ensure_lds_limit(once, reinterpret_cast<const void*>(few_rows_kernel<false, false>), kLds);
+  if (rc == MOE_OK) rc = ensure_lds_limit(once_pair, reinterpret_cast<const void*>(few_rows_kernel<true, false>), kLds);
+  return rc != MOE_OK ? rc : ensure_lds_limit(once_kc, reinterpret_cast<const void*>(few_rows_kernel<false, true>), kLds);
 }
 
 // bf16 blocks fill the device once at most, fp32 blocks, of which several share a unit, three times.  us, gemm_f32.hip / this, fp32: 1024, 2048, 1 16.6 / 4.3;
@@ -176,18 +187,24 @@ int launch_few_rows(int act_dtype, bool b_kc, const void* A, const void* B, void
 
 bool few_rows_pair_ok(long long rows, int N) { return rows <= 16 * 256 && (rows + 15) / 16 * ((N + 31) / 32) <= 256; }
 
-int launch_few_rows_pair(const void* A, const void* A_rest, const void* B, void* C, void* C_rest, int R, int N, int K, hipStream_t st) {
+static int launch_bf16(const void* A, const void* A_rest, bool b_kc, const void* B, void* C, void* C_rest, int R, int N, int K, hipStream_t st) {
   if (prepare_few_rows() != MOE_OK) return MOE_EHIP;
   const int rows = A_rest != nullptr ? 16 : 32;
   const dim3 grid((unsigned)((N + 31) / 32 * ((R + rows - 1) / rows))), threads(64 * kWaves);
-  auto a = static_cast<const bf16_t*>(A);
-  auto r = static_cast<const bf16_t*>(A_rest);
-  auto b = static_cast<const bf16_t*>(B);
-  auto c = static_cast<bf16_t*>(C);
-  auto e = static_cast<bf16_t*>(C_rest);
-  if (r != nullptr) hipLaunchKernelGGL((few_rows_kernel<true>), grid, threads, kLds, st, a, r, b, c, e, R, N, K);
-  else hipLaunchKernelGGL((few_rows_kernel<false>), grid, threads, kLds, st, a, r, b, c, e, R, N, K);
+  auto run = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, threads, kLds, st, static_cast<const bf16_t*>(A), static_cast<const bf16_t*>(A_rest), static_cast<const bf16_t*>(B),
+                       static_cast<bf16_t*>(C), static_cast<bf16_t*>(C_rest), R, N, K);
+  };
+  if (b_kc) run(few_rows_kernel<false, true>);
+  else if (A_rest != nullptr) run(few_rows_kernel<true, false>);
+  else run(few_rows_kernel<false, false>);
   return check_launch();
+}
+int launch_few_rows_pair(const void* A, const void* A_rest, const void* B, void* C, void* C_rest, int R, int N, int K, hipStream_t st) {
+  return launch_bf16(A, A_rest, false, B, C, C_rest, R, N, K, st);
+}
+int launch_few_rows_transposed(const void* A, const void* B, void* C, void* C_rest, int R, int N, int K, hipStream_t st) {
+  return launch_bf16(A, nullptr, true, B, C, C_rest, R, N, K, st);
 }
 
 }  // namespace moe

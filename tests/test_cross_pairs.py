@@ -6,7 +6,7 @@ import pytest
 import paper_2006_16668_amd as moe
 from test_cross_ranges import scratch
 from test_cross_rules import BF16, LIB, _Plan, _Shape
-from test_gpu_cross_few_tokens import CASES
+from test_gpu_cross_few_tokens import CASES, GRADIENT_CASES
 
 
 def pair_plan(*shape):
@@ -39,6 +39,22 @@ def test_the_cases_reach_every_form():
         assert pair_ok(rows, M) and -(-rows // 32) * -(-heads * d // 32) <= 256 and in_pairs(B, Lq, Lk, M, heads, kv_heads, d)
     seen = {(*(lambda p: (p[0], p[1] > 1))(pair_plan(*c[:3], *c[4:7])), c[6]) for c in CASES}
     assert seen == {(few, split, d) for few, split in ((False, False), (True, False), (True, True)) for d in (64, 128)}
+
+
+def pair_ranges(B, Lq, Lk, heads, kv_heads, d):
+    f = LIB._ZN3moe21cross_pair_dkv_blocksERKNS_10CrossShapeE
+    f.argtypes, f.restype = [ctypes.c_void_p], ctypes.c_int
+    all_, each = (Lq * (heads // kv_heads) + 63) // 64, f(ctypes.byref(_Shape(B, Lq, Lk, heads, kv_heads, d)))
+    assert 1 <= each <= all_
+    return -(-all_ // each)
+
+
+def test_the_gradients_cases_reach_every_form():
+    """Ranges of columns or none, sources of up to 64 states and more."""
+    for B, Lq, Lk, M, heads, kv_heads, d, _ in GRADIENT_CASES:
+        assert in_pairs(B, Lq, Lk, M, heads, kv_heads, d)
+    seen = {(pair_ranges(*c[:3], *c[4:7]) > 1, c[2] > 64, c[6]) for c in GRADIENT_CASES}
+    assert {(r, d) for r, _, d in seen} == {(r, d) for r in (False, True) for d in (64, 128)} and {(f, d) for _, f, d in seen} == {(f, d) for f in (False, True) for d in (64, 128)}
 
 
 # us of the kernels in that many ranges of blocks of 16 columns; 0: blocks of 64
