@@ -526,8 +526,8 @@ int moe_cross_backward_workspace_bytes(const moe_config* cfg, const moe_cross_di
 int moe_cross_keys(const moe_config* cfg, const moe_cross_dims* dims, const void* mem, const void* wkv, void* kv, void* stream);
 
 /* in: u [G,S,M], kv as moe_cross_keys leaves it, src_len [B] i32 or NULL (all states hold), wq [M,A], wo [A,M].  out [G,S,M].
- * ws >= moe_cross_workspace_bytes, 256-byte aligned.  bf16: calls of few tokens (generation: ceil(G S / 32) ceil(A / 32) and ceil(G S / 16) ceil(M / 32) up to 256)
- * carry q, the probabilities and ctx as pairs of bf16, 16 bits, and round the result alone; others round q, ctx and, where a block has 128 columns, the
+ * ws >= moe_cross_workspace_bytes, 256-byte aligned.  bf16: calls of few tokens (generation: G S up to 128, ceil(G S / 32) ceil(A / 32) and ceil(G S / 16) ceil(M / 32)
+ * up to 256) carry q, the probabilities and ctx as pairs of bf16, 16 bits, and round the result alone; others round q, ctx and, where a block has 128 columns, the
  * probabilities once each.  Softmax statistics and sums are fp32, sums in a fixed order.  The form of a call goes by its type, B, Lq, Lk and heads: in
  * a batch of another size, or padded to another Lk, a source's tokens may differ by those roundings and by the order of their sums. */
 int moe_cross_attention(const moe_config* cfg, const moe_cross_dims* dims, const void* u, const void* kv, const int32_t* src_len,

@@ -80,6 +80,7 @@ def test_products_of_pairs_fill_the_device_once(rows, N, ok):
 def test_steps_of_generation_are_in_pairs_and_batches_of_training_are_not():
     for B in (1, 4, 64, 128):
         assert in_pairs(B, 1, 2048, 1024, 16, 16, 128)
+    assert in_pairs(1, 128, 300, 64, 1, 1, 64) and not in_pairs(1, 129, 300, 64, 1, 1, 64)
     assert not in_pairs(129, 1, 300, 1024, 16, 16, 128) and not in_pairs(32, 1024, 1024, 1024, 16, 16, 128)
     # (fp32 has no pairs)
     sh, dims = moe.MoEShape(4, 1, 1024, 64, 2, 1, "f32"), moe.CrossDims(4, 1, 53, 16, 128)

@@ -17,7 +17,7 @@ CASES = [(1, 1, 55, 200, 1, 1, 64, None), (1, 4, 385, 848, 2, 2, 128, None), (2,
          (1, 4, 53, 1024, 16, 16, 128, None), (64, 1, 300, 1024, 16, 16, 128, "any"), (6, 2, 1, 64, 1, 1, 64, "ends"), (6, 3, 64, 256, 2, 1, 128, "ends"),
          (6, 5, 65, 264, 8, 2, 64, "ends"), (1, 16, 700, 512, 4, 4, 64, None), (1, 17, 129, 512, 4, 4, 128, None), (3, 31, 190, 72, 2, 2, 64, "any"),
          (1, 65, 333, 512, 4, 4, 64, "any"), (2, 33, 1000, 256, 16, 1, 64, "any"), (1, 128, 260, 1024, 4, 4, 128, None), (3, 1, 8200, 136, 2, 2, 64, "any"),
-         (5, 2, 4100, 520, 16, 2, 128, "any"), (2, 48, 757, 512, 8, 2, 64, "any"), (1, 30, 344, 256, 1, 1, 128, None), (7, 29, 765, 512, 4, 1, 64, "ends")]
+         (5, 2, 4100, 520, 16, 2, 128, "any"), (2, 48, 757, 512, 8, 2, 64, "any"), (1, 30, 344, 256, 1, 1, 128, None), (7, 18, 765, 512, 4, 1, 64, "ends")]
 
 
 def inputs(c, seed=0, scale=1.5):
@@ -140,7 +140,7 @@ def backward(c, seed=0, scale=1.5, select=False, fill=255):
 
 # besides: dK and dV in ranges of columns, two columns and many of them to a key head, one state
 GRADIENT_CASES = CASES + [(1, 128, 100, 512, 8, 2, 64, None), (2, 48, 2000, 512, 8, 1, 64, "any"), (1, 128, 300, 1024, 8, 2, 128, "any"), (3, 9, 2, 264, 1, 1, 128, None),
-                          (11, 1, 2, 136, 1, 1, 64, None), (64, 2, 40, 512, 4, 4, 128, "any"), (4, 100, 64, 72, 2, 2, 64, "ends")]
+                          (11, 1, 2, 136, 1, 1, 64, None), (64, 2, 40, 512, 4, 4, 128, "any"), (4, 32, 64, 72, 2, 2, 64, "ends")]
 
 
 @pytest.mark.parametrize("c", GRADIENT_CASES)
@@ -206,7 +206,7 @@ def test_gradients_repeat_whatever_the_workspaces_held(c):
 
 
 @pytest.mark.parametrize("c", [(6, 3, 64, 256, 2, 1, 128, "ends"), (6, 3, 65, 256, 2, 2, 64, "ends"), (6, 2, 4100, 512, 2, 2, 64, "ends"), (6, 2, 4100, 512, 2, 1, 128, "ends"),
-                               (7, 29, 765, 512, 4, 1, 64, "ends"), (6, 16, 500, 512, 2, 2, 128, "ends")])
+                               (7, 18, 765, 512, 4, 1, 64, "ends"), (6, 16, 500, 512, 2, 2, 128, "ends")])
 def test_probabilities_add_up(c):
     """With scores of some hundred, what q loses in bf16 moves a probability by far more than a rounding: statistics and scores are of the same q, so that of one
     state p is 1 (dV is the sum of dctx over the tokens), and of all the probabilities add up to 1."""
