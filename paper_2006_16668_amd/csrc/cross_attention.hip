@@ -17,9 +17,10 @@
 //             both, ctx is the sum of both again.  That takes no more products or reads than a tile that few tokens do not fill, and as the lanes of
 //             a pair share the exponentials, no more instructions.
 //
-// us (16 heads of 128, 32 x 1024 tokens and states): forward 338, dq 412, dK and dV 550, i.e. 0.81, 1.0 and 1.0 PFLOP/s, 4 to 5 % behind the
-// self-attention's; what bounds them is the same: the vector unit forward, the matrix pipes backward, at the 1.7 to 1.9 GHz that power leaves.  One token
-// each of 64 sources of 410 to 2048 states: 138 (4.75 TB/s).  For dK and dV, staging two blocks
+// us (16 heads of 128, 32 x 1024 tokens and states): forward 338, dq 412, dK and dV 550, i.e. 0.81, 1.0 and 1.0 PFLOP/s; in turn with the self-attention's
+// on two cards 335 and 349 (320, 328 there), 416 and 431 (392, 406), 572 and 596 (529, 549), 5 to 8 % behind; what bounds them is the same: the
+// vector unit forward, the matrix pipes backward, at the 1.7 to 1.9 GHz that power leaves.  One token each of 64 sources of 410 to 2048 states: 141
+// (4.7 TB/s).  For dK and dV, staging two blocks
 // ahead was within 5 %; two groups of wavefronts with half the blocks each (d 64) made 46 us 54 at 308 blocks, 24 us 21 at 32.
 #include <float.h>
 #include <math.h>
